@@ -33,7 +33,8 @@
  *   - No exceptions, aborts or device traps cross this boundary; errors are status codes.
  *     There is no CPU fallback: without a usable CUDA device calls fail with APAR_ERR_CUDA.
  *
- * Layout of the KV pool (fixed): K pool and V pool are each
+ * Layout of the KV pool (of a context made by apar_create; apar_create_kv also offers 4-bit
+ * rows): K pool and V pool are each
  *       bf16 [num_layers][num_blocks][num_kv_heads][block_size = 16][head_dim = 128],
  *   so the rows of one (layer, block, kv head) form a contiguous 4 KiB tile.  All layers share
  *   one set of block tables: block b of layer l is the same logical block in every layer.  Q, out:
@@ -135,6 +136,47 @@ apar_status apar_create(const apar_config* cfg /*[host]*/, apar_ctx** out /*[hos
  * and for checking the bookkeeping on a machine without a GPU. */
 apar_status apar_create_host_only(const apar_config* cfg /*[host]*/, apar_ctx** out /*[host]*/);
 apar_status apar_destroy(apar_ctx* ctx);
+
+/* A KV cache held in 4 bits (the paper has no counterpart: its caches are 16-bit).  A context
+ * created with APAR_KV_Q4 quantises every row on its way into the pool and attends over the
+ * 4-bit rows; block tables, forks, releases and thread ids are those of a bf16 context.
+ *   Values.  A row (128 dims of one kv head, of K or of V) is four groups of 32 consecutive dims.
+ *   Of a group are kept lo = min(x), s = bf16((max(x) - lo) / 15) and, for each x, the integer
+ *   c = round((x - lo) / s) in 0..15, ties to even, differences and quotients taken in 32 bits; x
+ *   then stands for lo + s * c.  A scale that would be below 2^-100 is stored as 0 with all c = 0.
+ *   A group that holds a NaN or an infinity, or whose range overflows, reads as NaN throughout.
+ *   Bytes.  80 per row (64 of codes, then {s, lo} of each group as two bf16) instead of 256;
+ *   each pool is [num_layers][num_blocks][num_kv_heads][16 rows][80 bytes].  The order of the
+ *   codes inside a row is the library's own; apar_read_kv gives the rows as numbers.
+ *   Attention reads q and writes out as bf16, sums in 32 bits and rounds the weights to 11
+ *   bits after they are scaled: results are as exact as 32-bit arithmetic on the values above
+ *   rounded to bf16.  A NaN row makes NaN of the outputs that see it, and only of those.
+ * All calls of this header work on such a context, except apar_tree_prefill_attention, which
+ * returns APAR_ERR_UNSUPPORTED (apar_tree_prefix_attention serves runs of up to max_threads
+ * queries).  Device row pointers (q, out, k_new, v_new) must be 16-byte aligned: otherwise
+ * APAR_ERR_INVALID_ARG. */
+enum {
+  APAR_KV_BF16 = 0,
+  APAR_KV_Q4 = 1
+};
+/* Bytes of each of k_pool and v_pool for this configuration and format (all layers); 0 for an
+ * unsupported configuration or format. */
+size_t apar_kv_pool_bytes(const apar_config* cfg /*[host]*/, int32_t kv_format);
+/* apar_create with a choice of format; cfg->k_pool and v_pool hold apar_kv_pool_bytes() each, and
+ * the workspace is the same for both formats.  Errors: as apar_create; INVALID_ARG also for an
+ * unknown format. */
+apar_status apar_create_kv(const apar_config* cfg /*[host]*/, int32_t kv_format,
+                           apar_ctx** out /*[host]*/);
+/* Reads rows of the cache back as bf16 (4-bit rows: lo + s * c, rounded once): for entry i the
+ * rows of thread tid[i] at chain positions begin[i] .. begin[i] + count[i] - 1 of pool layer
+ * `layer`, entries one after the other.  A thread may be listed several times, count 0 is allowed.
+ *   k_out, v_out [device] bf16 [sum count][num_kv_heads][128], 16-byte aligned.
+ * Works on both formats.  Uses the staging buffers, so it cannot be captured.
+ * Errors: INVALID_ARG (also rows outside a thread, a misaligned output, a capturing stream),
+ * BAD_THREAD, UNSUPPORTED (host-only context), CUDA. */
+apar_status apar_read_kv(apar_ctx* ctx, int32_t layer, int32_t n, const int32_t* tid /*[host]*/,
+                         const int32_t* begin /*[host]*/, const int32_t* count /*[host]*/,
+                         void* k_out /*[device]*/, void* v_out /*[device]*/, void* cuda_stream);
 
 /* n new prompt sequences (roots of paragraph trees; the initial sequence group of Algorithm 1): empty block
  * tables, length 0.  tid_out [host] receives n ids.  Errors: NO_THREADS. */
@@ -362,6 +404,57 @@ apar_status apar_tree_decode_attention_static(const void* k_pool /*[device]*/,
                                               int32_t max_ctx_len, const void* q /*[device]*/,
                                               void* out /*[device]*/, float sm_scale,
                                               void* cuda_stream);
+
+/* Rotary positions (the paper's models apply them before attention; keys enter the cache rotated).
+ * Every row of 128 dims is turned pair by pair: with angle = position * theta_i, i < rotary_dim / 2,
+ *     (a, b) -> attn_scale * (a cos - b sin, b cos + a sin)
+ * (a, b) = dims (i, rotary_dim / 2 + i) in APAR_ROPE_HALF, (2 i, 2 i + 1) in APAR_ROPE_INTERLEAVED;
+ * dims from rotary_dim on are copied.  theta_i = base^(-2 i / rotary_dim), and with a scaling:
+ *   LINEAR  theta_i / factor
+ *   BANDS   with turns = original_len * theta_i / (2 pi) and t = (turns - low) / (high - low)
+ *           clamped to [0, 1]: (1 - t) theta_i / factor + t theta_i
+ *   YARN    r_i theta_i / factor + (1 - r_i) theta_i with the ramp r_i = (i - a) / max(b - a, 0.001)
+ *           clamped to [0, 1] between the pairs that make `high` and `low` turns over
+ *           original_len: a = max(0, floor(p(high))), b = min(rotary_dim - 1, ceil(p(low))),
+ *           p(x) = rotary_dim ln(original_len / (2 pi x)) / (2 ln base)
+ * Angles are computed in 64 bits, the products in 32, and the result is rounded to bf16. */
+enum {
+  APAR_ROPE_HALF = 0,
+  APAR_ROPE_INTERLEAVED = 1
+};
+enum {
+  APAR_ROPE_PLAIN = 0,
+  APAR_ROPE_LINEAR = 1,
+  APAR_ROPE_BANDS = 2,
+  APAR_ROPE_YARN = 3
+};
+typedef struct {
+  int32_t head_dim;               /* must be 128                                                 */
+  int32_t rotary_dim;             /* even, 2..128                                                */
+  int32_t layout;                 /* APAR_ROPE_HALF | APAR_ROPE_INTERLEAVED                      */
+  int32_t scaling;                /* APAR_ROPE_PLAIN | LINEAR | BANDS | YARN                     */
+  int32_t original_len;           /* BANDS, YARN: the trained length, > 0                        */
+  int32_t reserved;               /* 0                                                           */
+  double  base;                   /* > 0 (YARN: > 1)                                             */
+  double  factor;                 /* any scaling: > 0                                            */
+  double  low, high;              /* BANDS, YARN: turns, 0 < low < high                          */
+  double  attn_scale;             /* factor on the turned dims, normally 1                       */
+} apar_rope_config;
+/* Rotates the query and key rows of n tokens in one launch.
+ *   positions [device] int32 [n]
+ *   q, q_out  [device] bf16, head h of token i at q + i * q_stride + h * 128 elements; a stride of
+ *             0 means contiguous rows (num_q_heads * 128); k, k_out likewise
+ *   q_out == q with equal strides rotates in place; any other overlap of an input with its own
+ *   output is refused.  num_q_heads or num_kv_heads may be 0 (that side's pointers are ignored).
+ * Rows on 16-byte boundaries (and rotary_dim a multiple of 16 in the half layout) take a vectorised
+ * kernel, others an element-wise one.  No context, no workspace; can be captured in a graph.
+ * Errors: INVALID_ARG, UNSUPPORTED (head_dim), CUDA (read it with cudaGetLastError). */
+apar_status apar_rope(const apar_rope_config* cfg /*[host]*/, int32_t n,
+                      const int32_t* positions /*[device]*/, int32_t num_q_heads,
+                      const void* q /*[device]*/, int64_t q_stride, void* q_out /*[device]*/,
+                      int64_t q_out_stride, int32_t num_kv_heads, const void* k /*[device]*/,
+                      int64_t k_stride, void* k_out /*[device]*/, int64_t k_out_stride,
+                      void* cuda_stream);
 
 /* Paragraph tree of Algorithm 1 (host only): which slice of which sequence belongs where in the
  * final text.  apar_paragraph_root makes thread tid (a prompt sequence, already holding its

@@ -38,6 +38,18 @@ class apar_config(C.Structure):
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
+class apar_rope_config(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rotary_dim", C.c_int32), ("layout", C.c_int32),
+                ("scaling", C.c_int32), ("original_len", C.c_int32), ("reserved", C.c_int32),
+                ("base", C.c_double), ("factor", C.c_double), ("low", C.c_double),
+                ("high", C.c_double), ("attn_scale", C.c_double)]
+
+
+KV_FORMATS = {"bf16": 0, "q4": 1}
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "bands": 2, "yarn": 3}
+
+
 class apar_stats(C.Structure):
     _fields_ = [(n, C.c_int64) for n in (
         "live_threads", "free_blocks", "used_blocks", "forks", "cow_blocks", "cow_rows",
@@ -58,6 +70,13 @@ _SIGS = {
     "apar_workspace_bytes": (C.c_size_t, [_cfgp]),
     "apar_create": (C.c_int32, [_cfgp, C.POINTER(_ctx)]),
     "apar_create_host_only": (C.c_int32, [_cfgp, C.POINTER(_ctx)]),
+    "apar_create_kv": (C.c_int32, [_cfgp, C.c_int32, C.POINTER(_ctx)]),
+    "apar_kv_pool_bytes": (C.c_size_t, [_cfgp, C.c_int32]),
+    "apar_read_kv": (C.c_int32, [_ctx, C.c_int32, C.c_int32, _i32p, _i32p, _i32p, C.c_void_p,
+                                 C.c_void_p, C.c_void_p]),
+    "apar_rope": (C.c_int32, [C.POINTER(apar_rope_config), C.c_int32, C.c_void_p, C.c_int32,
+                              C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p,
+                              C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]),
     "apar_destroy": (C.c_int32, [_ctx]),
     "apar_new_threads": (C.c_int32, [_ctx, C.c_int32, _i32p]),
     "apar_fork": (C.c_int32, [_ctx, C.c_int32, _i32p, _i32p, C.c_void_p]),
@@ -152,6 +171,17 @@ def apar_create_host_only(cfg: apar_config):
     return ctx
 
 
+def apar_create_kv(cfg: apar_config, kv_format: int):
+    """kv_format: a value of KV_FORMATS."""
+    ctx = _ctx()
+    _check(lib.apar_create_kv(C.byref(cfg), kv_format, C.byref(ctx)))
+    return ctx
+
+
+def apar_kv_pool_bytes(cfg: apar_config, kv_format: int) -> int:
+    return lib.apar_kv_pool_bytes(C.byref(cfg), kv_format)
+
+
 def apar_destroy(ctx):
     _check(lib.apar_destroy(ctx))
 
@@ -235,6 +265,26 @@ def apar_steps_before_new_block(ctx) -> int:
 
 def apar_note_step_replay(ctx):
     _check(lib.apar_note_step_replay(ctx))
+
+
+def apar_read_kv(ctx, layer: int, tid, begin, count, k_out: int, v_out: int, stream=0):
+    tids, n = _arr(tid)
+    begins, _ = _arr(begin)
+    counts, _ = _arr(count)
+    _check(lib.apar_read_kv(ctx, layer, n, tids, begins, counts, k_out, v_out, stream))
+
+
+def make_rope_config(rotary_dim=128, layout="half", base=10000.0, scaling="none", factor=1.0,
+                     original_len=0, low=1.0, high=4.0, attn_scale=1.0, head_dim=128):
+    return apar_rope_config(head_dim, rotary_dim, ROPE_LAYOUTS[layout], ROPE_SCALINGS[scaling],
+                            original_len, 0, base, factor, low, high, attn_scale)
+
+
+def apar_rope(cfg: apar_rope_config, n: int, positions: int, num_q_heads: int, q: int,
+              q_stride: int, q_out: int, q_out_stride: int, num_kv_heads: int, k: int,
+              k_stride: int, k_out: int, k_out_stride: int, stream=0):
+    _check(lib.apar_rope(C.byref(cfg), n, positions, num_q_heads, q, q_stride, q_out, q_out_stride,
+                         num_kv_heads, k, k_stride, k_out, k_out_stride, stream))
 
 
 def apar_release(ctx, tid):

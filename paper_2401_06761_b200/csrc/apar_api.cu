@@ -11,6 +11,7 @@
 
 #include "../../include/apar.h"
 #include "apar_internal.h"
+#include "kv4.cuh"
 
 using namespace apar;
 
@@ -136,6 +137,8 @@ struct apar_ctx {
   int plan_verify_n = 0;                      // candidate descriptors that belong to the plan
   int32_t last_cuda = 0;
   bool host_only = false;                     // bookkeeping only: no device, nothing is launched
+  bool q4 = false;                            // the pools hold 4-bit rows (kv4.cuh)
+  int32_t plan_max_rows[4] = {0, 0, 0, 0};    // widest item of each class of the plan (4-bit pools)
   // Every thread's table as runs of groups (blocks held by the same set of threads).  A
   // thread's blocks since it was last forked form its own, open group; a fork closes the full
   // blocks of that group (the child lists them from then on) and opens a new one.
@@ -201,6 +204,12 @@ apar_status send(apar_ctx* c, Staging* s, void* dst, size_t bytes, cudaStream_t 
 int slot_of(apar_ctx* c, int32_t tid) {
   if (tid < 0 || tid >= (int32_t)c->tid_slot.size()) return -1;
   return c->tid_slot[tid];
+}
+
+// Rows are read and written sixteen bytes at a time; calls on a 4-bit context check for it.
+bool misaligned(const apar_ctx* c, const void* a, const void* b, const void* d = nullptr,
+                const void* e = nullptr) {
+  return c->q4 && (((uintptr_t)a | (uintptr_t)b | (uintptr_t)d | (uintptr_t)e) & 15);
 }
 
 uint32_t next_mark(apar_ctx* c) {
@@ -376,8 +385,10 @@ apar_status launch_plan(apar_ctx* c, int layer, const void* q, void* out, float 
   a.part_ml = (float2*)c->ws(c->lay.part_ml);
   a.shape = c->shape;
   a.scale_log2e = sm_scale * 1.4426950408889634f;
-  a.tm_k = &c->tm_k[layer];
-  a.tm_v = &c->tm_v[layer];
+  if (!c->q4) {
+    a.tm_k = &c->tm_k[layer];
+    a.tm_v = &c->tm_v[layer];
+  }
   a.d_error = (int*)c->ws(c->lay.err);
   a.num_sms = c->num_sms;
   a.umma_heads = c->umma_heads;
@@ -391,6 +402,23 @@ apar_status launch_plan(apar_ctx* c, int layer, const void* q, void* out, float 
   // kernels follow each other (config 5), nothing on config 4; the single-row kernel lost
   // 10-25 % when its finishing items started early (configs 2 and 3), so it and the merge are
   // launched the ordinary way, which also orders them after everything before them.
+  if (c->q4) {
+    if (p.n_mma) {
+      APAR_CUDA(c, launch_attention_q4(a, p.n_mma_tiles, c->plan_max_rows, st));
+      ++*launches_out;
+    }
+    if (c->plan_verify_n > 0) {
+      APAR_CUDA(c, launch_q4_verify_tail(a, (const VerifyDesc*)c->ws(c->lay.verify),
+                                         c->plan_verify_n, st));
+      ++*launches_out;
+    }
+    if (!p.merges.empty()) {
+      APAR_CUDA(c, launch_merge(a, (const MergeRef*)c->ws(c->lay.plan_merges),
+                                (int)p.merges.size(), st));
+      ++*launches_out;
+    }
+    return APAR_OK;
+  }
   const int chain = c->use_pdl ? 1 : 0;
   bool first = true;
   // Single-tile items go to the warp-stream kernel (unless the tcgen05 kernel is forced for
@@ -499,13 +527,21 @@ apar_status run_attention(apar_ctx* c, int n, const int32_t* qslots, const int32
     c->plan_min_rows = c->mma_min_rows;
     if (c->auto_path && c->shape.group == 1 && n <= kFewQueries) c->plan_min_rows = 1;
     // finishing items land in the single-row vector kernel or the warp-stream kernel
-    const bool fuse_final = c->use_ws && c->plan_min_rows <= 2 && !verify;
+    const bool fuse_final = c->use_ws && c->plan_min_rows <= 2 && !verify && !c->q4;
     if (!c->planner.build(c->pq.data(), n, c->lay.slot_capacity, cacheable, c->plan_min_rows,
                           fuse_final, &c->plan, by_runs))
       return APAR_ERR_WORKSPACE_TOO_SMALL;
     if ((int64_t)c->plan.users.size() > c->lay.entry_capacity ||
         (int64_t)c->plan.items.size() > c->lay.entry_capacity)
       return APAR_ERR_WORKSPACE_TOO_SMALL;
+    if (c->q4) {
+      for (int32_t& m : c->plan_max_rows) m = 0;
+      for (const WorkItem& w : c->plan.items) {
+        const int32_t rows = w.n_users * c->shape.group;
+        int32_t& m = c->plan_max_rows[(rows + 15) / 16 - 1];
+        m = std::max(m, rows);
+      }
+    }
     c->last.attn_plan_host_us = std::chrono::duration_cast<std::chrono::microseconds>(
                                     std::chrono::steady_clock::now() - t_plan).count();
   }
@@ -579,8 +615,10 @@ apar_status run_attention(apar_ctx* c, int n, const int32_t* qslots, const int32
   return APAR_OK;
 }
 
-apar_status create_impl(const apar_config* cfg, bool external, bool host_only, apar_ctx** out) {
-  if (!cfg || !out) return APAR_ERR_INVALID_ARG;
+apar_status create_impl(const apar_config* cfg, bool external, bool host_only, int32_t kv_format,
+                        apar_ctx** out) {
+  if (!cfg || !out || kv_format < APAR_KV_BF16 || kv_format > APAR_KV_Q4)
+    return APAR_ERR_INVALID_ARG;
   if (!supported(cfg)) return APAR_ERR_UNSUPPORTED;
   const Layout lay = make_layout(cfg);
   if (!host_only) {
@@ -593,6 +631,7 @@ apar_status create_impl(const apar_config* cfg, bool external, bool host_only, a
   if (!c) return APAR_ERR_INVALID_ARG;
   c->cfg = *cfg;
   c->host_only = host_only;
+  c->q4 = kv_format == APAR_KV_Q4;
   c->track_runs = !external;
   c->runs.resize(cfg->max_threads);
   c->own_open.assign(cfg->max_threads, 0);
@@ -631,7 +670,11 @@ apar_status create_impl(const apar_config* cfg, bool external, bool host_only, a
   c->plan_by_runs = !(planner && !strcmp(planner, "tables"));
   c->ring_bytes = lay.stage_cap;
   c->num_layers = std::max(1, cfg->num_layers);
-  c->layer_bytes = (size_t)cfg->num_blocks * cfg->num_kv_heads * kTileBytes;
+  c->layer_bytes = (size_t)cfg->num_blocks * cfg->num_kv_heads * (c->q4 ? kQ4TileBytes : kTileBytes);
+  if (c->q4) {                       // one kernel takes every item, whatever the switches say
+    c->mma_min_rows = 1;
+    c->auto_path = false;
+  }
   if (host_only) {
     *out = c;
     return APAR_OK;
@@ -646,7 +689,7 @@ apar_status create_impl(const apar_config* cfg, bool external, bool host_only, a
   c->tm_k.resize(c->num_layers);
   c->tm_v.resize(c->num_layers);
   bool maps_ok = true;
-  for (int l = 0; l < c->num_layers && maps_ok; ++l)
+  for (int l = 0; l < c->num_layers && maps_ok && !c->q4; ++l)
     maps_ok = make_pool_tensor_maps((char*)cfg->k_pool + l * c->layer_bytes,
                                     (char*)cfg->v_pool + l * c->layer_bytes, cfg->num_blocks,
                                     cfg->num_kv_heads, &c->tm_k[l], &c->tm_v[l]) == 0;
@@ -683,11 +726,21 @@ size_t apar_workspace_bytes(const apar_config* cfg) {
 }
 
 apar_status apar_create(const apar_config* cfg, apar_ctx** out) {
-  return create_impl(cfg, false, false, out);
+  return create_impl(cfg, false, false, APAR_KV_BF16, out);
+}
+
+size_t apar_kv_pool_bytes(const apar_config* cfg, int32_t kv_format) {
+  if (!supported(cfg) || kv_format < APAR_KV_BF16 || kv_format > APAR_KV_Q4) return 0;
+  return (size_t)std::max(1, cfg->num_layers) * cfg->num_blocks * cfg->num_kv_heads *
+         (kv_format == APAR_KV_Q4 ? kQ4TileBytes : kTileBytes);
+}
+
+apar_status apar_create_kv(const apar_config* cfg, int32_t kv_format, apar_ctx** out) {
+  return create_impl(cfg, false, false, kv_format, out);
 }
 
 apar_status apar_create_host_only(const apar_config* cfg, apar_ctx** out) {
-  return create_impl(cfg, false, true, out);
+  return create_impl(cfg, false, true, APAR_KV_BF16, out);
 }
 
 apar_status apar_destroy(apar_ctx* c) {
@@ -775,9 +828,10 @@ apar_status apar_fork(apar_ctx* c, int32_t n, const int32_t* parent_tid, int32_t
     apar_status rc = send(c, stg, d_stage, (size_t)nc * sizeof(CowCopy), st);
     if (rc) return rc;
     for (int l = 0; l < c->num_layers; ++l) {
-      APAR_CUDA(c, launch_cow_copy((char*)c->cfg.k_pool + l * c->layer_bytes,
-                                   (char*)c->cfg.v_pool + l * c->layer_bytes,
-                                   (const CowCopy*)d_stage, nc, c->cfg.num_kv_heads, st));
+      auto copy = c->q4 ? launch_q4_cow_copy : launch_cow_copy;
+      APAR_CUDA(c, copy((char*)c->cfg.k_pool + l * c->layer_bytes,
+                        (char*)c->cfg.v_pool + l * c->layer_bytes, (const CowCopy*)d_stage, nc,
+                        c->cfg.num_kv_heads, st));
       ++c->kernels_total;
     }
   }
@@ -788,6 +842,7 @@ apar_status apar_append_kv(apar_ctx* c, int32_t n, const int32_t* tid, const int
                            const void* k_new, const void* v_new, void* cuda_stream) {
   if (!c || n < 0 || (n > 0 && (!tid || ((!k_new || !v_new) && !c->host_only))))
     return APAR_ERR_INVALID_ARG;
+  if (misaligned(c, k_new, v_new)) return APAR_ERR_INVALID_ARG;
   cudaStream_t st = (cudaStream_t)cuda_stream;
   for (int i = 0; i < n; ++i)
     if (slot_of(c, tid[i]) < 0) return APAR_ERR_BAD_THREAD;
@@ -824,9 +879,9 @@ apar_status apar_append_kv(apar_ctx* c, int32_t n, const int32_t* tid, const int
     char* d_stage = keep ? c->ws(c->lay.slot_map) + (size_t)first_row * 4 : c->ws(c->lay.stage);
     apar_status rc = send(c, stg, d_stage, filled * 4, st);
     if (rc) return rc;
-    APAR_CUDA(c, launch_append(c->cfg.k_pool, c->cfg.v_pool, k_new, v_new,
-                               (const int32_t*)d_stage, first_row, (int)filled,
-                               c->cfg.num_kv_heads, st));
+    auto scatter = c->q4 ? launch_q4_append : launch_append;
+    APAR_CUDA(c, scatter(c->cfg.k_pool, c->cfg.v_pool, k_new, v_new, (const int32_t*)d_stage,
+                         first_row, (int)filled, c->cfg.num_kv_heads, st));
     ++c->kernels_total;
     first_row += (int64_t)filled;
     filled = 0;
@@ -877,6 +932,7 @@ apar_status apar_decode_step(apar_ctx* c, int32_t n, const int32_t* tid, const v
   if (!c || n < 0 || n > c->cfg.max_threads ||
       (n > 0 && (!tid || !k_new || !v_new || !q || !out)))
     return APAR_ERR_INVALID_ARG;
+  if (misaligned(c, k_new, v_new, q, out)) return APAR_ERR_INVALID_ARG;
   if (c->host_only) return APAR_ERR_UNSUPPORTED;
   if (n == 0) return APAR_OK;
   cudaStream_t st = (cudaStream_t)cuda_stream;
@@ -989,9 +1045,9 @@ apar_status apar_decode_step(apar_ctx* c, int32_t n, const int32_t* tid, const v
     rc = send(c, stg, nullptr, 0, st);    // nothing to copy: only marks the buffer in flight
     if (rc) return rc;
   }
-  APAR_CUDA(c, launch_append(c->cfg.k_pool, c->cfg.v_pool, k_new, v_new,
-                             (const int32_t*)c->ws(c->lay.slot_map), 0, n, c->cfg.num_kv_heads,
-                             st));
+  auto scatter = c->q4 ? launch_q4_append : launch_append;
+  APAR_CUDA(c, scatter(c->cfg.k_pool, c->cfg.v_pool, k_new, v_new,
+                       (const int32_t*)c->ws(c->lay.slot_map), 0, n, c->cfg.num_kv_heads, st));
   c->kernels_total += 2;
   return run_attention(c, n, sl, tid, false, q, out, sm_scale, st, nullptr, true);
 }
@@ -1032,6 +1088,7 @@ apar_status apar_tree_decode_attention(apar_ctx* c, int32_t n, const int32_t* ti
                                        void* out, float sm_scale, void* cuda_stream) {
   if (!c || n < 0 || n > c->cfg.max_threads || (n > 0 && (!tid || !q || !out)))
     return APAR_ERR_INVALID_ARG;
+  if (misaligned(c, q, out)) return APAR_ERR_INVALID_ARG;
   if (c->host_only) return APAR_ERR_UNSUPPORTED;
   if (n == 0) return APAR_OK;
   std::vector<int32_t> qslots(n);
@@ -1056,6 +1113,7 @@ apar_status apar_tree_prefix_attention(apar_ctx* c, int32_t n, const int32_t* ti
                                        float sm_scale, void* cuda_stream) {
   if (!c || n < 0 || n > c->cfg.max_threads || (n > 0 && (!tid || !attend_len || !q || !out)))
     return APAR_ERR_INVALID_ARG;
+  if (misaligned(c, q, out)) return APAR_ERR_INVALID_ARG;
   if (c->host_only) return APAR_ERR_UNSUPPORTED;
   if (n == 0) return APAR_OK;
   std::vector<int32_t> qslots(n);
@@ -1078,6 +1136,7 @@ apar_status apar_tree_verify_attention(apar_ctx* c, int32_t n, const int32_t* ti
                                        void* cuda_stream) {
   if (!c || n < 0 || (n > 0 && (!tid || !n_cand || !anc_mask || !q || !out)))
     return APAR_ERR_INVALID_ARG;
+  if (misaligned(c, q, out)) return APAR_ERR_INVALID_ARG;
   if (c->host_only) return APAR_ERR_UNSUPPORTED;
   if (n == 0) return APAR_OK;
   int64_t total = 0;
@@ -1208,11 +1267,11 @@ apar_status apar_accept_candidates(apar_ctx* c, int32_t n, const int32_t* tid,
     apar_status rc = send(c, stg, d_stage, bytes, st);
     if (rc) return rc;
     for (int l = 0; l < c->num_layers; ++l) {
-      APAR_CUDA(c, launch_row_moves((char*)c->cfg.k_pool + l * c->layer_bytes,
-                                    (char*)c->cfg.v_pool + l * c->layer_bytes,
-                                    (const RowMove*)d_stage,
-                                    (const int32_t*)(d_stage + (size_t)n_moves * sizeof(RowMove)),
-                                    (int)ng, c->cfg.num_kv_heads, st));
+      auto move = c->q4 ? launch_q4_row_moves : launch_row_moves;
+      APAR_CUDA(c, move((char*)c->cfg.k_pool + l * c->layer_bytes,
+                        (char*)c->cfg.v_pool + l * c->layer_bytes, (const RowMove*)d_stage,
+                        (const int32_t*)(d_stage + (size_t)n_moves * sizeof(RowMove)), (int)ng,
+                        c->cfg.num_kv_heads, st));
       ++c->kernels_total;
     }
   }
@@ -1226,7 +1285,7 @@ apar_status apar_tree_prefill_attention(apar_ctx* c, int32_t layer, int32_t n,
   if (!c || n < 0 || layer < 0 || layer >= c->num_layers ||
       (n > 0 && (!tid || !q_begin || !q_count || !q || !out)))
     return APAR_ERR_INVALID_ARG;
-  if (c->host_only) return APAR_ERR_UNSUPPORTED;
+  if (c->host_only || c->q4) return APAR_ERR_UNSUPPORTED;
   if (n == 0) return APAR_OK;
   cudaStream_t st = (cudaStream_t)cuda_stream;
   std::vector<int32_t> seg_slot(n);
@@ -1366,13 +1425,15 @@ apar_status apar_tree_prefill_attention(apar_ctx* c, int32_t layer, int32_t n,
 apar_status apar_append_kv_layer(apar_ctx* c, int32_t layer, const void* k_new, const void* v_new,
                                  void* cuda_stream) {
   if (!c || layer < 0 || layer >= c->num_layers || !k_new || !v_new) return APAR_ERR_INVALID_ARG;
+  if (misaligned(c, k_new, v_new)) return APAR_ERR_INVALID_ARG;
   if (c->host_only) return APAR_ERR_UNSUPPORTED;
   if (c->last_append_rows < 0) return APAR_ERR_WORKSPACE_TOO_SMALL;
   if (c->last_append_rows == 0) return APAR_OK;
-  APAR_CUDA(c, launch_append((char*)c->cfg.k_pool + layer * c->layer_bytes,
-                             (char*)c->cfg.v_pool + layer * c->layer_bytes, k_new, v_new,
-                             (const int32_t*)c->ws(c->lay.slot_map), 0, (int)c->last_append_rows,
-                             c->cfg.num_kv_heads, (cudaStream_t)cuda_stream));
+  auto scatter = c->q4 ? launch_q4_append : launch_append;
+  APAR_CUDA(c, scatter((char*)c->cfg.k_pool + layer * c->layer_bytes,
+                       (char*)c->cfg.v_pool + layer * c->layer_bytes, k_new, v_new,
+                       (const int32_t*)c->ws(c->lay.slot_map), 0, (int)c->last_append_rows,
+                       c->cfg.num_kv_heads, (cudaStream_t)cuda_stream));
   ++c->kernels_total;
   return APAR_OK;
 }
@@ -1380,6 +1441,7 @@ apar_status apar_append_kv_layer(apar_ctx* c, int32_t layer, const void* k_new, 
 apar_status apar_tree_decode_attention_layer(apar_ctx* c, int32_t layer, const void* q, void* out,
                                              float sm_scale, void* cuda_stream) {
   if (!c || layer < 0 || layer >= c->num_layers || !q || !out) return APAR_ERR_INVALID_ARG;
+  if (misaligned(c, q, out)) return APAR_ERR_INVALID_ARG;
   if (c->host_only) return APAR_ERR_UNSUPPORTED;
   // the device-resident plan, tables and lengths must still describe the pool
   if (c->attn_book_seq != c->book_seq || c->plan.items.empty()) return APAR_ERR_INVALID_ARG;
@@ -1390,6 +1452,63 @@ apar_status apar_tree_decode_attention_layer(apar_ctx* c, int32_t layer, const v
   if (rc == APAR_OK && c->time_stop)
     APAR_CUDA(c, cudaEventRecord(c->time_stop, (cudaStream_t)cuda_stream));
   return rc;
+}
+
+apar_status apar_read_kv(apar_ctx* c, int32_t layer, int32_t n, const int32_t* tid,
+                         const int32_t* begin, const int32_t* count, void* k_out, void* v_out,
+                         void* cuda_stream) {
+  if (!c || n < 0 || layer < 0 || layer >= c->num_layers ||
+      (n > 0 && (!tid || !begin || !count || !k_out || !v_out)) ||
+      (((uintptr_t)k_out | (uintptr_t)v_out) & 15))
+    return APAR_ERR_INVALID_ARG;
+  if (c->host_only) return APAR_ERR_UNSUPPORTED;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  int64_t rows = 0;
+  for (int i = 0; i < n; ++i) {
+    const int s = slot_of(c, tid[i]);
+    if (s < 0) return APAR_ERR_BAD_THREAD;
+    if (begin[i] < 0 || count[i] < 0 || (int64_t)begin[i] + count[i] > c->slots[s].len)
+      return APAR_ERR_INVALID_ARG;
+    rows += count[i];
+  }
+  if (rows == 0) return APAR_OK;
+  {
+    // the list of rows goes through the staging buffers, which a captured call may not use
+    cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+    APAR_CUDA(c, cudaStreamIsCapturing(st, &cap));
+    if (cap != cudaStreamCaptureStatusNone) return APAR_ERR_INVALID_ARG;
+  }
+  const char* kp = (const char*)c->cfg.k_pool + (size_t)layer * c->layer_bytes;
+  const char* vp = (const char*)c->cfg.v_pool + (size_t)layer * c->layer_bytes;
+  char* d_stage = c->ws(c->lay.stage);
+  const int64_t cap_rows = (int64_t)(c->lay.stage_cap / 4);
+  int64_t first_row = 0;
+  int i = 0;
+  int32_t done = 0;                     // rows of entry i already listed
+  while (first_row < rows) {
+    Staging* stg;
+    apar_status rc = acquire(c, &stg);
+    if (rc) return rc;
+    int32_t* list = (int32_t*)stg->host;
+    int64_t filled = 0;
+    while (i < n && filled < cap_rows) {
+      const int32_t* tab = c->row(slot_of(c, tid[i]));
+      for (; done < count[i] && filled < cap_rows; ++done) {
+        const int32_t pos = begin[i] + done;
+        list[filled++] = tab[pos / kBlock] * kBlock + pos % kBlock;
+      }
+      if (done < count[i]) break;
+      ++i;
+      done = 0;
+    }
+    rc = send(c, stg, d_stage, (size_t)filled * 4, st);
+    if (rc) return rc;
+    APAR_CUDA(c, launch_read_rows(c->q4, kp, vp, k_out, v_out, (const int32_t*)d_stage, first_row,
+                                  (int)filled, c->cfg.num_kv_heads, st));
+    ++c->kernels_total;
+    first_row += filled;
+  }
+  return APAR_OK;
 }
 
 apar_status apar_release(apar_ctx* c, int32_t n, const int32_t* tid) {
@@ -1439,7 +1558,7 @@ apar_status apar_tree_decode_attention_tables(const apar_config* cfg, int32_t n,
   }
   if (n == 0) return APAR_OK;
   apar_ctx* c = nullptr;
-  apar_status rc = create_impl(cfg, true, false, &c);
+  apar_status rc = create_impl(cfg, true, false, APAR_KV_BF16, &c);
   if (rc) return rc;
   std::vector<int32_t> qslots(n);
   for (int i = 0; i < n; ++i) {

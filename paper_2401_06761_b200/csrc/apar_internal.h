@@ -206,6 +206,31 @@ cudaError_t launch_row_moves(void* k_pool, void* v_pool, const RowMove* d_moves,
                              cudaStream_t st);
 cudaError_t launch_merge(const AttnArgs& a, const MergeRef* d_merge, int n_merge, cudaStream_t st);
 
+// ---- pools held in 4 bits (kv4.cu, attn_q4.cu; layout in kv4.cuh) ----
+// The same jobs as launch_append, launch_cow_copy and launch_row_moves above.
+cudaError_t launch_q4_append(void* k_pool, void* v_pool, const void* k_new, const void* v_new,
+                             const int32_t* d_slots, int64_t first_row, int n_rows,
+                             int num_kv_heads, cudaStream_t st);
+cudaError_t launch_q4_cow_copy(void* k_pool, void* v_pool, const CowCopy* d_copies, int n,
+                               int num_kv_heads, cudaStream_t st);
+cudaError_t launch_q4_row_moves(void* k_pool, void* v_pool, const RowMove* d_moves,
+                                const int32_t* d_group_begin, int n_groups, int num_kv_heads,
+                                cudaStream_t st);
+// Rows d_slots[0..n_rows) of a pool as bf16, to rows first_row.. of k_out and v_out.
+cudaError_t launch_read_rows(bool q4, const void* k_pool, const void* v_pool, void* k_out,
+                             void* v_out, const int32_t* d_slots, int64_t first_row, int n_rows,
+                             int num_kv_heads, cudaStream_t st);
+// The CTAs of an attention launch, in the planner's item order (four classes, widest first).
+struct Q4Grid {
+  int32_t cta_end[4], item_begin[4], tiles[4];
+};
+// Every item of a plan made with mma_min_rows = 1: n_items[k] items of class k (k + 1 tiles of
+// 16 rows), none of them with more than max_rows[k] rows.  Uses no a.tm_k / a.tm_v / a.d_ticket.
+cudaError_t launch_attention_q4(const AttnArgs& a, const int32_t n_items[4],
+                                const int32_t max_rows[4], cudaStream_t st);
+cudaError_t launch_q4_verify_tail(const AttnArgs& a, const VerifyDesc* d_desc, int n_desc,
+                                  cudaStream_t st);
+
 // ---- planner (planner.cpp) ----
 // A run of consecutive table positions whose blocks are held by the same set of threads
 // ("group"): blocks become shared only through fork, so the host keeps, per thread, its table

@@ -1,0 +1,210 @@
+// Kernels that move rows of a 4-bit KV pool (layout and arithmetic: kv4.cuh): the quantising
+// scatter of new rows, the copy of a partial block at fork, the moves of accepted candidate rows,
+// and the reading of rows back as bf16 values (which also serves bf16 pools).
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include "apar_internal.h"
+#include "kv4.cuh"
+
+namespace apar {
+namespace {
+
+// ------------------------------------------------------------------ append: quantise and scatter
+// Sixteen lanes hold one row, eight dims (16 bytes) each; the four lanes of a group find its
+// range with two shuffles.  The kernel reads 256 bytes and writes 80 for each row and is bound by
+// HBM for prompts, by its launch for decode steps.
+__global__ void __launch_bounds__(256) q4_append_kernel(uint8_t* __restrict__ k_pool,
+                                                        uint8_t* __restrict__ v_pool,
+                                                        const uint4* __restrict__ k_new,
+                                                        const uint4* __restrict__ v_new,
+                                                        const int32_t* __restrict__ slots,
+                                                        long long first_row, int n_rows,
+                                                        int num_kv_heads) {
+  const long long idx = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+  const long long rh = idx >> 4;                       // (row, head)
+  const int c = (int)idx & 15;
+  const bool on = rh < (long long)n_rows * num_kv_heads;
+  const bool is_v = blockIdx.y != 0;
+  const int r = on ? (int)(rh / num_kv_heads) : 0, h = on ? (int)(rh % num_kv_heads) : 0;
+  uint4 x = make_uint4(0u, 0u, 0u, 0u);
+  if (on) x = __ldg((is_v ? v_new : k_new) + ((first_row + r) * num_kv_heads + h) * 16 + c);
+  const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
+  float f[8];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    f[2 * e] = bf16_lo(xs[e]);
+    f[2 * e + 1] = bf16_hi(xs[e]);
+  }
+  // range of the group; the NaN-propagating minimum lets a NaN reach s
+  __nv_bfloat162 mn = *(__nv_bfloat162*)&xs[0], mx = mn;
+#pragma unroll
+  for (int e = 1; e < 4; ++e) {
+    mn = __hmin2_nan(mn, *(__nv_bfloat162*)&xs[e]);
+    mx = __hmax2_nan(mx, *(__nv_bfloat162*)&xs[e]);
+  }
+#pragma unroll
+  for (int o = 1; o <= 2; o <<= 1) {
+    uint32_t a = __shfl_xor_sync(0xffffffffu, *(uint32_t*)&mn, o);
+    uint32_t b = __shfl_xor_sync(0xffffffffu, *(uint32_t*)&mx, o);
+    mn = __hmin2_nan(mn, *(__nv_bfloat162*)&a);
+    mx = __hmax2_nan(mx, *(__nv_bfloat162*)&b);
+  }
+  const float lo = __bfloat162float(__hmin_nan(mn.x, mn.y));
+  const float hi = __bfloat162float(__hmax_nan(mx.x, mx.y));
+  const float range = hi - lo;
+  float s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(range, 15.f)));
+  const bool bad = !(range <= 3.402823466e38f);        // NaN, or an infinity
+  if (!(s >= kQ4MinScale)) s = 0.f;
+  // c = round((x - lo) / s).  The quotient is correctly rounded, as a division would give it: one
+  // residual step on a correctly rounded reciprocal (Markstein 1990; the divisor has eight
+  // significant bits, so the theorem's one exception, a significand of all ones, cannot occur).
+  // Adding 1.5 * 2^23 leaves the integer, ties to even, in the low bits.
+  const float inv = s > 0.f ? __frcp_rn(s) : 0.f;
+  uint32_t w = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float d = f[e] - lo;
+    const float q = d * inv;
+    const float t = fmaf(fmaf(-q, s, d), inv, q);
+    const uint32_t code = (uint32_t)__float_as_int(t + 12582912.f) & 15u;
+    // K: nibble e / 2 + 4 (e & 1); V: nibble e
+    w |= code << (is_v ? 4 * e : 4 * ((e >> 1) + 4 * (e & 1)));
+  }
+  if (bad) w = 0;
+  const int G = c >> 2, xq = c & 3;
+  if (is_v) {
+    // 16-bit pieces: this lane holds, for its group G, pieces 2 xq (low half) and 2 xq + 1; it
+    // ends up with two groups of one piece, i.e. the word at 16 xq + 4 G
+    const int base = (threadIdx.x & 16) + xq + 8 * (G & 1);
+    const uint32_t a = __shfl_sync(0xffffffffu, w, base);
+    const uint32_t b = __shfl_sync(0xffffffffu, w, base + 4);
+    w = __byte_perm(a, b, (G & 2) ? 0x7632 : 0x5410);
+  }
+  if (!on) return;
+  const int slot = slots[r];
+  uint8_t* row = (is_v ? v_pool : k_pool) +
+                 (((size_t)(slot >> 4) * num_kv_heads + h) * kBlock + (slot & 15)) * kQ4RowBytes;
+  *(uint32_t*)(row + xq * 16 + G * 4) = w;
+  if (xq == 0) {
+    // (a NaN scale carries the sign bit: integer comparisons of scales rank it below all others)
+    const uint32_t lo_bits = __float_as_uint(lo) >> 16;
+    *(uint32_t*)(row + kQ4CodeBytes + 4 * G) =
+        bad ? 0xffc0ffc0u : (__float_as_uint(s) >> 16) | (lo_bits << 16);
+  }
+}
+
+// ------------------------------------------------------------------ fork: copy r rows
+__global__ void __launch_bounds__(96) q4_cow_copy_kernel(uint4* __restrict__ k_pool,
+                                                         uint4* __restrict__ v_pool,
+                                                         const CowCopy* __restrict__ copies,
+                                                         int num_kv_heads) {
+  const CowCopy c = copies[blockIdx.x];
+  uint4* pool = blockIdx.z ? v_pool : k_pool;
+  const size_t tile = kQ4TileBytes / 16;
+  const uint4* src = pool + ((size_t)c.src_block * num_kv_heads + blockIdx.y) * tile;
+  uint4* dst = pool + ((size_t)c.dst_block * num_kv_heads + blockIdx.y) * tile;
+  for (int i = threadIdx.x; i < c.rows * kQ4RowVec; i += blockDim.x) dst[i] = src[i];
+}
+
+// ------------------------------------------------------------------ accepted candidates: row moves
+// As row_move_kernel: every source row of a group is read before the first one is written.
+__global__ void __launch_bounds__(160) q4_row_move_kernel(uint4* __restrict__ k_pool,
+                                                          uint4* __restrict__ v_pool,
+                                                          const RowMove* __restrict__ moves,
+                                                          const int32_t* __restrict__ group_begin,
+                                                          int num_kv_heads) {
+  __shared__ uint4 rows[64 * kQ4RowVec];
+  const int m0 = group_begin[blockIdx.x], n = group_begin[blockIdx.x + 1] - m0;
+  uint4* pool = blockIdx.z ? v_pool : k_pool;
+  const int h = blockIdx.y;
+  auto at = [&](int slot, int x) {
+    return (((size_t)(slot >> 4) * num_kv_heads + h) * kBlock + (slot & 15)) * kQ4RowVec + x;
+  };
+  for (int x = threadIdx.x; x < n * kQ4RowVec; x += blockDim.x)
+    rows[x] = pool[at(moves[m0 + x / kQ4RowVec].src_slot, x % kQ4RowVec)];
+  __syncthreads();
+  for (int x = threadIdx.x; x < n * kQ4RowVec; x += blockDim.x)
+    pool[at(moves[m0 + x / kQ4RowVec].dst_slot, x % kQ4RowVec)] = rows[x];
+}
+
+// ------------------------------------------------------------------ rows read back as bf16
+// One thread per eight dims of a row; blockIdx.y selects K or V.  A 4-bit row reads as
+// bf16(lo + s * c), the sum taken in 32 bits and rounded once more to the output's type.
+template <bool kQ4>
+__global__ void __launch_bounds__(256) read_rows_kernel(const uint8_t* __restrict__ k_pool,
+                                                        const uint8_t* __restrict__ v_pool,
+                                                        uint4* __restrict__ k_out,
+                                                        uint4* __restrict__ v_out,
+                                                        const int32_t* __restrict__ slots,
+                                                        long long first_row, int n_rows,
+                                                        int num_kv_heads) {
+  const long long idx = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+  if (idx >= (long long)n_rows * num_kv_heads * 16) return;
+  const long long rh = idx >> 4;
+  const int c = (int)idx & 15;
+  const int r = (int)(rh / num_kv_heads), h = (int)(rh % num_kv_heads);
+  const int slot = slots[r];
+  const size_t row = ((size_t)(slot >> 4) * num_kv_heads + h) * kBlock + (slot & 15);
+  const uint8_t* pool = blockIdx.y ? v_pool : k_pool;
+  uint4 out;
+  if (kQ4) {
+    float f[8];
+    if (blockIdx.y) q4_load8_v(pool + row * kQ4RowBytes, c, f);
+    else q4_load8_k(pool + row * kQ4RowBytes, c, f);
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * e], f[2 * e + 1]);
+      w[e] = *(uint32_t*)&p;
+    }
+    out = make_uint4(w[0], w[1], w[2], w[3]);
+  } else {
+    out = ((const uint4*)pool)[row * 16 + c];
+  }
+  (blockIdx.y ? v_out : k_out)[(first_row * num_kv_heads + rh) * 16 + c] = out;
+}
+
+}  // namespace
+
+cudaError_t launch_q4_append(void* k_pool, void* v_pool, const void* k_new, const void* v_new,
+                             const int32_t* d_slots, int64_t first_row, int n_rows,
+                             int num_kv_heads, cudaStream_t st) {
+  if (n_rows <= 0) return cudaSuccess;
+  const long long total = (long long)n_rows * num_kv_heads * 16;
+  q4_append_kernel<<<dim3((unsigned)((total + 255) / 256), 2), 256, 0, st>>>(
+      (uint8_t*)k_pool, (uint8_t*)v_pool, (const uint4*)k_new, (const uint4*)v_new, d_slots,
+      (long long)first_row, n_rows, num_kv_heads);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_q4_cow_copy(void* k_pool, void* v_pool, const CowCopy* d_copies, int n,
+                               int num_kv_heads, cudaStream_t st) {
+  if (n <= 0) return cudaSuccess;
+  q4_cow_copy_kernel<<<dim3(n, num_kv_heads, 2), 96, 0, st>>>((uint4*)k_pool, (uint4*)v_pool,
+                                                              d_copies, num_kv_heads);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_q4_row_moves(void* k_pool, void* v_pool, const RowMove* d_moves,
+                                const int32_t* d_group_begin, int n_groups, int num_kv_heads,
+                                cudaStream_t st) {
+  if (n_groups <= 0) return cudaSuccess;
+  q4_row_move_kernel<<<dim3(n_groups, num_kv_heads, 2), 160, 0, st>>>(
+      (uint4*)k_pool, (uint4*)v_pool, d_moves, d_group_begin, num_kv_heads);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_read_rows(bool q4, const void* k_pool, const void* v_pool, void* k_out,
+                             void* v_out, const int32_t* d_slots, int64_t first_row, int n_rows,
+                             int num_kv_heads, cudaStream_t st) {
+  if (n_rows <= 0) return cudaSuccess;
+  const long long total = (long long)n_rows * num_kv_heads * 16;
+  const dim3 grid((unsigned)((total + 255) / 256), 2);
+  auto kernel = q4 ? read_rows_kernel<true> : read_rows_kernel<false>;
+  kernel<<<grid, 256, 0, st>>>((const uint8_t*)k_pool, (const uint8_t*)v_pool, (uint4*)k_out,
+                               (uint4*)v_out, d_slots, (long long)first_row, n_rows, num_kv_heads);
+  return cudaGetLastError();
+}
+
+}  // namespace apar

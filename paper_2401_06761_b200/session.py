@@ -19,37 +19,78 @@ def pool_requirements(spec: ForestSpec, slack: float = 0.05):
     return (int(blocks * (1 + slack)) + 16, len(spec.nodes) + 8, -(-longest // bs) + depth + 1)
 
 
+class Rope:
+    """Rotary positions of a model: the parameters of apar_rope_config, applied by calling.
+
+    q [n][heads][128] and k (or None) are bf16 and may be views with any stride between tokens;
+    positions is int32 [n].  Returns rotated (q, k): new contiguous tensors, or the inputs
+    themselves with inplace=True."""
+
+    def __init__(self, **params):
+        self.cfg = B.make_rope_config(**params)
+
+    def __call__(self, q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, inplace=False):
+        n = q.shape[0]
+        assert positions.dtype == torch.int32 and positions.is_contiguous() and positions.is_cuda
+        assert positions.shape == (n,)
+        outs, sides = [], []
+        for x in (q, k):
+            if x is None:
+                outs.append(None)
+                sides += [0, 0, 0, 0, 0]
+                continue
+            assert x.is_cuda and x.dtype == torch.bfloat16 and x.dim() == 3 and x.shape[0] == n
+            assert x.shape[2] == self.cfg.head_dim
+            assert x.stride(2) == 1 and (x.shape[1] == 1 or x.stride(1) == x.shape[2])
+            out = x if inplace else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            stride = x.stride(0) if n > 1 else 0       # (0: contiguous)
+            outs.append(out)
+            sides += [x.shape[1], x.data_ptr(), stride, out.data_ptr(), stride if inplace else 0]
+        B.apar_rope(self.cfg, n, positions.data_ptr(), *sides, PagedSession._stream())
+        return tuple(outs)
+
+
 class PagedSession:
     def __init__(self, shape: LayerShape, num_blocks: int, max_threads: int,
                  max_blocks_per_thread: int, device="cuda", poison: bool = False,
-                 num_layers: int = 1):
+                 num_layers: int = 1, kv_format: str = "bf16"):
         if not torch.cuda.is_available():
             raise RuntimeError("the APAR library needs a CUDA device; there is no CPU path")
         self.shape, self.device = shape, torch.device(device)
         self.num_blocks = num_blocks
         self.num_layers = num_layers
+        self.kv_format = kv_format
+        cfg = B.make_config(num_blocks, shape.num_q_heads, shape.num_kv_heads, max_threads,
+                            max_blocks_per_thread, num_layers=num_layers)
         pool_shape = (num_layers * num_blocks, shape.num_kv_heads, shape.block_size,
                       shape.head_dim)
-        if poison:   # NaN bit patterns everywhere: any read of an unwritten row shows up
+        if kv_format != "bf16":   # rows of a library-defined layout, as bytes
+            nbytes = B.apar_kv_pool_bytes(cfg, B.KV_FORMATS[kv_format])
+            # (0xFF: the scales of unwritten rows are NaN)
+            fill = 0xFF if poison else 0
+            self.k_pool = torch.full((nbytes,), fill, dtype=torch.uint8, device=device)
+            self.v_pool = torch.full((nbytes,), fill, dtype=torch.uint8, device=device)
+        elif poison:   # NaN bit patterns everywhere: any read of an unwritten row shows up
             self.k_pool = torch.full(pool_shape, float("nan"), dtype=torch.bfloat16, device=device)
             self.v_pool = torch.full(pool_shape, float("nan"), dtype=torch.bfloat16, device=device)
         else:
             self.k_pool = torch.zeros(pool_shape, dtype=torch.bfloat16, device=device)
             self.v_pool = torch.zeros(pool_shape, dtype=torch.bfloat16, device=device)
-        cfg = B.make_config(num_blocks, shape.num_q_heads, shape.num_kv_heads, max_threads,
-                            max_blocks_per_thread, num_layers=num_layers)
         ws_bytes = B.apar_workspace_bytes(cfg)
         self.workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=device)
         cfg.k_pool, cfg.v_pool = self.k_pool.data_ptr(), self.v_pool.data_ptr()
         cfg.workspace, cfg.workspace_bytes = self.workspace.data_ptr(), ws_bytes
         self.cfg = cfg
-        self.ctx = B.apar_create(cfg)
+        self.ctx = None
+        self.ctx = (B.apar_create(cfg) if kv_format == "bf16" else
+                    B.apar_create_kv(cfg, B.KV_FORMATS[kv_format]))
         self.sm_scale = 1.0 / math.sqrt(shape.head_dim)
 
     @classmethod
-    def for_spec(cls, spec: ForestSpec, device="cuda", poison=False, extra_blocks=0):
+    def for_spec(cls, spec: ForestSpec, device="cuda", poison=False, extra_blocks=0,
+                 kv_format="bf16"):
         nb, nt, mb = pool_requirements(spec)
-        return cls(spec.shape, nb + extra_blocks, nt, mb, device, poison)
+        return cls(spec.shape, nb + extra_blocks, nt, mb, device, poison, kv_format=kv_format)
 
     def close(self):
         if self.ctx is not None:
@@ -146,6 +187,15 @@ class PagedSession:
                                            self.sm_scale if sm_scale is None else sm_scale,
                                            self._stream())
         return out
+
+    def read_kv(self, tids, begin, count, layer: int = 0):
+        """Rows begin[i] .. begin[i] + count[i] - 1 of each thread's chain, as bf16 (k, v)."""
+        shape = (sum(count), self.shape.num_kv_heads, self.shape.head_dim)
+        k = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+        v = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+        B.apar_read_kv(self.ctx, layer, tids, begin, count, k.data_ptr(), v.data_ptr(),
+                       self._stream())
+        return k, v
 
     def release(self, tids):
         B.apar_release(self.ctx, tids)

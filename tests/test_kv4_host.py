@@ -1,0 +1,104 @@
+"""What of the 4-bit cache and the rotary operator can be checked without a GPU."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+from oracle import kv4
+from paper_2401_06761_b200 import binding as B
+
+
+def test_pool_bytes():
+    cfg = B.make_config(1000, 32, 8, 64, 40, num_layers=3)
+    assert B.apar_kv_pool_bytes(cfg, B.KV_FORMATS["bf16"]) == 3 * 1000 * 8 * 16 * 256
+    assert B.apar_kv_pool_bytes(cfg, B.KV_FORMATS["q4"]) == 3 * 1000 * 8 * 16 * 80
+    assert B.apar_kv_pool_bytes(cfg, 2) == 0 and B.apar_kv_pool_bytes(cfg, -1) == 0
+    assert B.apar_kv_pool_bytes(B.make_config(1000, 32, 8, 64, 40, head_dim=64), 1) == 0
+
+
+def test_create_refusals():
+    cfg = B.make_config(1000, 32, 8, 64, 40)
+    for fmt in (0, 1, 2, -1):
+        with pytest.raises(B.AparError) as e:
+            B.apar_create_kv(cfg, fmt)                 # no pools
+        assert e.value.code == "INVALID_ARG"
+    bad = B.make_config(1000, 32, 8, 64, 40, block_size=32)
+    with pytest.raises(B.AparError) as e:
+        B.apar_create_kv(bad, 1)
+    assert e.value.code == "UNSUPPORTED"
+
+
+def test_read_kv_needs_a_device():
+    ctx = B.apar_create_host_only(B.make_config(100, 8, 2, 4, 10))
+    (t,) = B.apar_new_threads(ctx, 1)
+    B.apar_append_kv(ctx, [t], [5], 0, 0)
+    with pytest.raises(B.AparError) as e:
+        B.apar_read_kv(ctx, 0, [t], [0], [5], 256, 256)
+    assert e.value.code == "UNSUPPORTED"
+    B.apar_destroy(ctx)
+
+
+def test_checker_of_the_format():
+    """Hand-worked groups, the half-step bound, and its own rounding."""
+    x = np.zeros((1, 128), dtype=np.float32)
+    x[0, :16] = np.arange(16)
+    x[0, 16:32] = [0.5, 1.5, 2.5, 14.5] * 4                    # s = 1: ties go to the even code
+    x[0, 32:64] = 7.0
+    x[0, 64:96] = np.linspace(-3, 4.5, 32).astype(np.float16)  # s = 0.5
+    c, s, lo = kv4.quantise(kv4.round_bf16(x))
+    assert s[0, 0] == 1 and lo[0, 0] == 0 and list(c[0, 0, :16]) == list(range(16))
+    assert list(c[0, 0, 16:20]) == [0, 2, 2, 14]
+    assert s[0, 1] == 0 and lo[0, 1] == 7 and not c[0, 1].any()
+    assert s[0, 2] == 0.5 and lo[0, 2] == -3
+    rng = np.random.default_rng(0)
+    y = kv4.round_bf16(rng.normal(size=(500, 128)))
+    c, s, lo = kv4.quantise(y)
+    err = np.abs(kv4.values(c, s, lo) - y).reshape(500, 4, 32)
+    # half a step, and at the top of the range what rounding s to eight bits costs
+    assert (err <= s[..., None] * (0.5 + 15 * 2.0 ** -8)).all()
+    assert kv4.round_bf16(np.float32(1 + 2.0 ** -8)) == 1.0
+    assert kv4.round_bf16(np.float32(1 + 3 * 2.0 ** -8)) == np.float32(1 + 2.0 ** -6)
+
+
+ROPE_REFUSED = [dict(rotary_dim=3), dict(rotary_dim=0), dict(rotary_dim=130), dict(base=0.0),
+                dict(base=float("nan")), dict(base=float("inf")), dict(scaling="linear", factor=0.0),
+                dict(scaling="linear", factor=-2.0), dict(scaling="bands", factor=2.0),
+                dict(scaling="bands", factor=2.0, original_len=100, low=4.0, high=4.0),
+                dict(scaling="yarn", factor=2.0, original_len=100, base=1.0, high=32.0),
+                dict(scaling="yarn", factor=2.0, original_len=100, low=0.0, high=32.0),
+                dict(attn_scale=float("nan"))]
+
+
+@pytest.mark.parametrize("params", ROPE_REFUSED)
+def test_rope_parameters_refused(params):
+    cfg = B.make_rope_config(**params)
+    with pytest.raises(B.AparError) as e:
+        B.apar_rope(cfg, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
+    assert e.value.code == "INVALID_ARG"
+
+
+def test_rope_arguments_refused():
+    """Every refusal comes before a launch: the addresses are never used."""
+    cfg, p = B.make_rope_config(), 1 << 20
+
+    def refused(code, *args):
+        with pytest.raises(B.AparError) as e:
+            B.apar_rope(*args)
+        assert e.value.code == code
+
+    refused("UNSUPPORTED", B.make_rope_config(head_dim=64, rotary_dim=64), 1, p, 1, p, 0, p, 0, 0, 0, 0, 0, 0)
+    refused("INVALID_ARG", cfg, -1, p, 1, p, 0, p, 0, 0, 0, 0, 0, 0)
+    refused("INVALID_ARG", cfg, 1, 0, 1, p, 0, p, 0, 0, 0, 0, 0, 0)                # no positions
+    refused("INVALID_ARG", cfg, 1, p, 1, 0, 0, p, 0, 0, 0, 0, 0, 0)                # no q
+    refused("INVALID_ARG", cfg, 1, p, 0, 0, 0, 0, 0, 2, p, 0, 0, 0)                # no k_out
+    refused("INVALID_ARG", cfg, 4, p, 2, p, 255, 2 * p, 0, 0, 0, 0, 0, 0)          # stride below a row
+    refused("INVALID_ARG", cfg, 4, p, 2, p + 1, 0, 2 * p, 0, 0, 0, 0, 0, 0)        # odd address
+    refused("INVALID_ARG", cfg, 4, p, 2, p, 0, p + 256, 0, 0, 0, 0, 0, 0)          # overlap
+    refused("INVALID_ARG", cfg, 4, p, 2, p, 0, p, 512, 0, 0, 0, 0, 0)              # in place, other stride
+    refused("INVALID_ARG", cfg, 4, p, 40000, p, 0, 4 * p, 0, 40000, p, 0, 8 * p, 0)
+    B.apar_rope(cfg, 0, 0, 4, 0, 0, 0, 0, 4, 0, 0, 0, 0)                           # nothing to do
+    B.apar_rope(cfg, 5, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
+
+
+def test_rope_config_layout():
+    assert C.sizeof(B.apar_rope_config) == 64
