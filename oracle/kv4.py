@@ -40,6 +40,6 @@ def values(codes, s, lo):
 
 
 def spread(codes, s):
-    """|s (c - 8)|: the part of a value that the attention weights multiply after rounding."""
-    v = np.abs(s[..., None] * (codes - 8))
+    """s c: the part of a value that the attention weights multiply after rounding."""
+    v = s[..., None] * codes
     return v.reshape(*v.shape[:-2], 4 * GROUP)

@@ -4,19 +4,23 @@
 // fourth block of the item, each with its own ring of tiles (K and V of one block: 2560 bytes)
 // filled with cp.async, and fold their (reference, l, O) at the end.
 //
-// Products run on mma.sync m16n8k16 with the *cache* as the 16-row operand and the queries as
-// the 8-column one, so that a call with few rows per block wastes little of a product, and the
-// codes of a block are turned into operand registers once:
-//   S^T = K Q^T     A = K codes, 16 tokens x 16 dims.  Codes become bf16 numbers 128 + c with one
-//                   logical instruction per pair (0x4300 is 128 with the last seven bits free).
-//                   A group of 32 dims is two products; its scale and offset are applied to the
-//                   32-bit sums: score = sum_j s_j (acc_j - 128 qsum_j) + lo_j qsum_j, with qsum_j
-//                   the sum of the query over the group.  Scores are thus exact to 32 bits.
-//   O^T += V^T P^T  A = V codes, 16 dims x 16 tokens, as f16 numbers c - 8 (1024 + c by the same
-//                   trick, less 1032).  B = P s_j, one operand per group, rounded once to f16: it
-//                   is below 2^10 by the choice of reference, and 11 bits against bf16's eight keep
-//                   the result as good as 32-bit arithmetic rounded to bf16.  The offsets
-//                   lo_j + 8 s_j are summed in 32 bits on the side, once per group and row.
+// Products run on mma.sync m16n8k16 (f16) with the *cache* as the 16-row operand and the queries
+// as the 8-column one, so that a call with few rows per block wastes little of a product, and the
+// codes of a block are turned into operand registers once.  A code is used as it lies in the
+// word: four bits in the low end of a 16-bit lane are the subnormal f16 number c * 2^-24, and
+// four bits higher up c * 2^-20, both exact in the tensor core, so a pair of codes costs one AND
+// (and every other pair no shift).  The powers of two come out again for nothing:
+//   S^T = K Q^T     A = K codes, 16 tokens x 16 dims.  B = the query row in f16, scaled by the power
+//                   of two that brings its largest value to 2^14 (exact, but for values 2^-38 of
+//                   the largest), and by another 2^-4 where codes stand four bits higher.  A
+//                   group of 32 dims is two products; its scale and offset are applied to the
+//                   32-bit sums: score = sum_j s_j acc_j + lo_j qsum_j, with qsum_j the sum of the
+//                   query over the group, and the powers of two are part of the softmax scale.
+//                   Scores are exact to 32 bits.
+//   O^T += V^T P^T  A = V codes, 16 dims x 16 tokens.  B = P s_j, one operand per group, rounded
+//                   once to f16: it is below 2^10 by the choice of reference, and 11 bits against
+//                   bf16's eight keep the result as good as 32-bit arithmetic rounded to bf16.
+//                   The offsets lo_j are summed in 32 bits on the side, once per group and row.
 // The reference subtracted in the exponent is the running maximum of score + log2(largest
 // scale of the token's V row), not of the score: P s_j is then bounded whatever the scales are,
 // and f16's narrow exponent is spent on the largest terms of the sum.  It moves lazily (kSlack).
@@ -45,16 +49,9 @@ constexpr int kFoldFloats = kRows * kDim;            // one warp's O when it is 
 constexpr int kSmemQ4 = kWarps * kRing;
 static_assert(kWarps * kFoldFloats * 4 <= kSmemQ4, "the fold takes the place of the rings");
 constexpr float kSlack = 8.f;                        // the reference moves only past 2^8
+constexpr float kCodeUnit = 1.f / 16777216.f;        // what a code of 1 counts as in a product: 2^-24
 constexpr float kMinScaleLog2 = -60.f;               // V scales below 2^-60 count as 2^-60
 
-__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
-                                         uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
-      "{%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
                                         uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile(
@@ -72,15 +69,9 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   __half2 h = __floats2half2_rn(lo, hi);
   return *(uint32_t*)&h;
 }
-// nibbles n and n + 4 of w as the bf16 pair 128 + c
-__device__ __forceinline__ uint32_t codes_bf16(uint32_t w, int n) {
-  return ((w >> (4 * n)) & 0x000f000fu) | 0x43004300u;
-}
-// nibbles n of both halves of w as the f16 pair c - 8
+// nibbles n and n + 4 of w as an f16 pair: c * 2^-24 for even n, c * 2^-20 for odd n
 __device__ __forceinline__ uint32_t codes_f16(uint32_t w, int n) {
-  uint32_t x = ((w >> (4 * n)) & 0x000f000fu) | 0x64006400u;
-  __half2 h = __hsub2(*(__half2*)&x, __half2half2(__ushort_as_half(0x6408)));   // 1032
-  return *(uint32_t*)&h;
+  return (n < 2 ? w : w >> 8) & ((n & 1) ? 0x00f000f0u : 0x000f000fu);
 }
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -144,6 +135,7 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
 
   // ---- queries: row r0 + g, dims 32 j + 8 q .. + 7, as B fragments
   uint32_t qb[4][4];
+  float qs[4][2], unit[2];       // of rows 2 q, 2 q + 1: sums over each group; 2^24 / their factor
   {
     const int r = r0 + g;
 #pragma unroll
@@ -159,18 +151,35 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
         qb[j][0] = v.x; qb[j][1] = v.y; qb[j][2] = v.z; qb[j][3] = v.w;
       }
     }
-  }
-  // sums of the rows 2 q and 2 q + 1 of the unit over each group of dims
-  float qs[4][2];
+    uint32_t top = 0;            // bits of the row's largest magnitude (bf16, in the high half)
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    float x = 0.f;
+    for (int j = 0; j < 4; ++j)
 #pragma unroll
-    for (int p = 0; p < 4; ++p) x += bf16_lo(qb[j][p]) + bf16_hi(qb[j][p]);
-    x += __shfl_xor_sync(0xffffffffu, x, 1);
-    x += __shfl_xor_sync(0xffffffffu, x, 2);
-    qs[j][0] = __shfl_sync(0xffffffffu, x, 8 * q);
-    qs[j][1] = __shfl_sync(0xffffffffu, x, 8 * q + 4);
+      for (int p = 0; p < 4; ++p)
+        top = max(top, max(qb[j][p] << 17, (qb[j][p] & 0x7fff0000u) << 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    // the factor 2^k; a row of zeros or subnormal numbers has k at its limit
+    const int k = min(126, 14 + 127 - (int)(top >> 24));
+    const float f = __uint_as_float((uint32_t)(k + 127) << 23);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float x = 0.f;
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const float e0 = bf16_lo(qb[j][p]) * f, e1 = bf16_hi(qb[j][p]) * f;
+        x += e0 + e1;
+        qb[j][p] = (p & 1) ? pack_f16(e0 * 0.0625f, e1 * 0.0625f) : pack_f16(e0, e1);
+      }
+      x += __shfl_xor_sync(0xffffffffu, x, 1);
+      x += __shfl_xor_sync(0xffffffffu, x, 2);
+      qs[j][0] = __shfl_sync(0xffffffffu, x, 8 * q) * kCodeUnit;
+      qs[j][1] = __shfl_sync(0xffffffffu, x, 8 * q + 4) * kCodeUnit;
+    }
+    // score * log2(e) * scale = (what the products give) * unit
+    const float u = a.scale_log2e * (1.f / kCodeUnit) * __uint_as_float((uint32_t)(127 - k) << 23);
+    unit[0] = __shfl_sync(0xffffffffu, u, 8 * q);
+    unit[1] = __shfl_sync(0xffffffffu, u, 8 * q + 4);
   }
 
   float o[8][4], lsum[4][2], ref[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
@@ -202,20 +211,22 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         float acc[4] = {0.f, 0.f, 0.f, 0.f};
-        mma_bf16(acc, codes_bf16(w0[j], 0), codes_bf16(w1[j], 0), codes_bf16(w0[j], 1),
-                 codes_bf16(w1[j], 1), qb[j][0], qb[j][1]);
-        mma_bf16(acc, codes_bf16(w0[j], 2), codes_bf16(w1[j], 2), codes_bf16(w0[j], 3),
-                 codes_bf16(w1[j], 3), qb[j][2], qb[j][3]);
+        mma_f16(acc, codes_f16(w0[j], 0), codes_f16(w1[j], 0), codes_f16(w0[j], 1),
+                codes_f16(w1[j], 1), qb[j][0], qb[j][1]);
+        mma_f16(acc, codes_f16(w0[j], 2), codes_f16(w1[j], 2), codes_f16(w0[j], 3),
+                codes_f16(w1[j], 3), qb[j][2], qb[j][3]);
         const float sa = bf16_lo(t0[j]), sb = bf16_lo(t1[j]);
-        const float la = fmaf(-128.f, sa, bf16_hi(t0[j])), lb = fmaf(-128.f, sb, bf16_hi(t1[j]));
+        const float la = bf16_hi(t0[j]), lb = bf16_hi(t1[j]);
         x[0] = fmaf(sa, acc[0], fmaf(la, qs[j][0], x[0]));
         x[1] = fmaf(sa, acc[1], fmaf(la, qs[j][1], x[1]));
         x[2] = fmaf(sb, acc[2], fmaf(lb, qs[j][0], x[2]));
         x[3] = fmaf(sb, acc[3], fmaf(lb, qs[j][1], x[3]));
       }
     }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] *= a.scale_log2e;
+    x[0] *= unit[0];
+    x[1] *= unit[1];
+    x[2] *= unit[0];
+    x[3] *= unit[1];
 
     // ---- V scales of tokens g and g + 8; rows past the length hold unspecified bits
     uint4 v0 = lds128(vt + g * kQ4RowBytes + kQ4CodeBytes);
@@ -280,7 +291,7 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
       const float sa = bf16_lo(z0[j]), sb = bf16_lo(z1[j]);
       const uint32_t b0 = transpose8x8(pack_f16(p0 * sa, p1 * sa));
       const uint32_t b1 = transpose8x8(pack_f16(p2 * sb, p3 * sb));
-      const float la = fmaf(8.f, sa, bf16_hi(z0[j])), lb = fmaf(8.f, sb, bf16_hi(z1[j]));
+      const float la = bf16_hi(z0[j]), lb = bf16_hi(z1[j]);
       lsum[j][0] = fmaf(p0, la, fmaf(p2, lb, lsum[j][0]));
       lsum[j][1] = fmaf(p1, la, fmaf(p3, lb, lsum[j][1]));
       const uint32_t sel = (j & 1) ? 0x7632 : 0x5410;
@@ -308,6 +319,7 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
   // ---- fold of the four warps (the rings are no longer needed)
   __syncthreads();
   float* fo = (float*)smem;
+  constexpr float kLow = 1.f / kCodeUnit, kHigh = kLow / 16.f;   // (odd nibbles counted 16 times)
   if (g == 0) {
     fold_m[warp][2 * q] = ref[0];
     fold_m[warp][2 * q + 1] = ref[1];
@@ -319,8 +331,9 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       *(float4*)(fo + warp * kFoldFloats + (2 * q + e) * kDim + 32 * j + 4 * g) =
-          make_float4(o[2 * j][e] + lsum[j][e], o[2 * j][2 + e] + lsum[j][e],
-                      o[2 * j + 1][e] + lsum[j][e], o[2 * j + 1][2 + e] + lsum[j][e]);
+          make_float4(fmaf(o[2 * j][e], kLow, lsum[j][e]), fmaf(o[2 * j][2 + e], kHigh, lsum[j][e]),
+                      fmaf(o[2 * j + 1][e], kLow, lsum[j][e]),
+                      fmaf(o[2 * j + 1][2 + e], kHigh, lsum[j][e]));
   __syncthreads();
 #pragma unroll
   for (int rr = 0; rr < kRows / kWarps; ++rr) {

@@ -14,7 +14,7 @@ def host(t):
 
 class Kv4Pair:
     """A 4-bit PagedSession with two checkers: one holds the rows' values, the other has the
-    values' distance to the middle of their group in place of V (what the rounding of the
+    values' height over the lowest of their group, s c, in place of V (what the rounding of the
     weights is relative to)."""
 
     def __init__(self, hq, hk, num_blocks=256, max_threads=64, max_blocks=64, num_layers=1):
@@ -70,7 +70,7 @@ def check(got, ref, mid, what=""):
     """got bf16 against the 64-bit result ref.  The output is rounded to bf16 (half a step is 2^-8
     of it).  The weights are rounded to f16 after their scale (half a step 2^-11 of each term,
     terms below 2^-14 of the largest 2^-25 of it: with fewer than 2^14 tokens no more than
-    another 2^-11), and multiply s (c - 8), whose mean size is mid.  What is left, sums and scores
+    another 2^-11), and multiply s c, whose weighted mean is mid.  What is left, sums and scores
     in 32 bits, is far below either."""
     got = host(got).astype(np.float64)
     assert np.isfinite(got).all(), f"{what}: non-finite output"
