@@ -674,6 +674,7 @@ apar_status create_impl(const apar_config* cfg, bool external, bool host_only, i
   if (c->q4) {                       // one kernel takes every item, whatever the switches say
     c->mma_min_rows = 1;
     c->auto_path = false;
+    if (getenv("APAR_Q4_UNITS")) c->planner.set_units_per_sm(atoi(getenv("APAR_Q4_UNITS")));
   }
   if (host_only) {
     *out = c;

@@ -220,9 +220,10 @@ cudaError_t launch_q4_row_moves(void* k_pool, void* v_pool, const RowMove* d_mov
 cudaError_t launch_read_rows(bool q4, const void* k_pool, const void* v_pool, void* k_out,
                              void* v_out, const int32_t* d_slots, int64_t first_row, int n_rows,
                              int num_kv_heads, cudaStream_t st);
-// The CTAs of an attention launch, in the planner's item order (four classes, widest first).
+// The units of an attention launch, in the planner's item order (four classes, widest first; the
+// items of a class have the same number of row tiles).
 struct Q4Grid {
-  int32_t cta_end[4], item_begin[4], tiles[4];
+  int32_t unit_end[4], item_begin[4], tiles[4];
 };
 // Every item of a plan made with mma_min_rows = 1: n_items[k] items of class k (k + 1 tiles of
 // 16 rows), none of them with more than max_rows[k] rows.  Uses no a.tm_k / a.tm_v / a.d_ticket.
@@ -284,13 +285,16 @@ class Planner {
   bool build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_tails,
              int mma_min_rows, bool fuse_final, Plan* out, bool by_runs = false);
   void set_num_sms(int n) { num_sms_ = n > 0 ? n : 148; }
+  // Units (item x kv head) per SM that long runs are cut for.
+  void set_units_per_sm(int n) { units_per_sm_ = n; }
 
  private:
   template <bool kRuns>
   void find_segments(const PlanQuery* q, int n, bool open_tails, int64_t* unique,
                      int64_t* attended);
   void ensure_keys(size_t n);
-  int num_blocks_ = 0, group_ = 1, hint_kv_heads_ = 1, num_sms_ = 148;
+  int num_blocks_ = 0, group_ = 1, hint_kv_heads_ = 1, num_sms_ = 148,
+      units_per_sm_ = 8;
   uint32_t epoch_ = 0;
   std::vector<uint32_t> stamp_;
   std::vector<int32_t> cnt_, seg_of_;

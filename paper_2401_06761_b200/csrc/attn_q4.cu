@@ -1,8 +1,14 @@
 // Tree attention over a KV pool held in 4 bits (layout: kv4.cuh).
 //
-// A unit is eight query rows of one work item and one kv head; its CTA's four warps take every
-// fourth block of the item, each with its own ring of tiles (K and V of one block: 2560 bytes)
-// filled with cp.async, and fold their (reference, l, O) at the end.
+// A unit is eight query rows of one work item and one kv head.  Twelve warps per SM each work
+// through units of their own, from first to last block, with no barrier between them: a warp
+// streams the tiles of its blocks (K and V of one block: 2560 bytes) through a private ring with
+// cp.async, and the copies run ahead *across* units - the next unit's description, query rows and
+// first blocks are on their way while the current one is computed.  (The form before this one, a
+// CTA per unit whose four warps shared its blocks, spent some 5 us per unit on the chain item ->
+// table -> tile and on the fold: 158 us instead of the figure below on the same case.)  Units are
+// dealt out in the planner's order, longest first, forwards and backwards in turn, so no counter
+// in memory is needed and the kernel can be captured and replayed as it is.
 //
 // Products run on mma.sync m16n8k16 (f16) with the *cache* as the 16-row operand and the queries
 // as the 8-column one, so that a call with few rows per block wastes little of a product, and the
@@ -13,10 +19,11 @@
 //   S^T = K Q^T     A = K codes, 16 tokens x 16 dims.  B = the query row in f16, scaled by the power
 //                   of two that brings its largest value to 2^14 (exact, but for values 2^-38 of
 //                   the largest), and by another 2^-4 where codes stand four bits higher.  A
-//                   group of 32 dims is two products; its scale and offset are applied to the
-//                   32-bit sums: score = sum_j s_j acc_j + lo_j qsum_j, with qsum_j the sum of the
-//                   query over the group, and the powers of two are part of the softmax scale.
-//                   Scores are exact to 32 bits.
+//                   group of 32 dims is two products, and its scale is applied to the 32-bit sums:
+//                   score = sum_j s_j acc_j + sum_j lo_j qsum_j, with qsum_j the sum of the query over
+//                   the group; the powers of two are part of the softmax scale.  The second sum is
+//                   one more product: lo_j is a bf16 number, and qsum_j the sum of three, so
+//                   that four groups fill a k of 16.  Scores are exact to 32 bits.
 //   O^T += V^T P^T  A = V codes, 16 dims x 16 tokens.  B = P s_j, one operand per group, rounded
 //                   once to f16: it is below 2^10 by the choice of reference, and 11 bits against
 //                   bf16's eight keep the result as good as 32-bit arithmetic rounded to bf16.
@@ -28,6 +35,7 @@
 // The C fragment of S^T holds tokens in rows, the B operand wants them in the k index: a
 // movmatrix of the 8 x 8 halves brings one into the other.
 #include <algorithm>
+#include <climits>
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -41,13 +49,17 @@ namespace apar {
 namespace {
 
 constexpr int kRows = 8;                             // query rows of a unit
-constexpr int kDepth = 5;                            // tiles in flight per warp
-constexpr int kWarps = 4;
-constexpr int kSlot = 2 * kQ4TileBytes;              // K and V of one block
-constexpr int kRing = kDepth * kSlot;
-constexpr int kFoldFloats = kRows * kDim;            // one warp's O when it is folded
-constexpr int kSmemQ4 = kWarps * kRing;
-static_assert(kWarps * kFoldFloats * 4 <= kSmemQ4, "the fold takes the place of the rings");
+constexpr int kWarps = 12;
+constexpr int kStep = 2;                             // blocks computed together
+constexpr int kTile = 2 * kQ4TileBytes;              // K and V of one block
+constexpr int kSlot = kStep * kTile;
+constexpr int kDepth = 3;                            // slots of a warp's ring
+constexpr int kHdrs = 4;                             // unit descriptions a warp holds
+constexpr int kHdrInts = 32;
+constexpr int kOffQ = kWarps * kDepth * kSlot;       // the next unit's query rows, per warp
+constexpr int kOffHdr = kOffQ + kWarps * kRows * kDim * 2;
+constexpr int kSmemQ4 = kOffHdr + kWarps * kHdrs * kHdrInts * 4;
+static_assert(kSmemQ4 <= 227 * 1024, "shared memory");
 constexpr float kSlack = 8.f;                        // the reference moves only past 2^8
 constexpr float kCodeUnit = 1.f / 16777216.f;        // what a code of 1 counts as in a product: 2^-24
 constexpr float kMinScaleLog2 = -60.f;               // V scales below 2^-60 count as 2^-60
@@ -56,6 +68,14 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
                                         uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+      "{%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+                                         uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
       "{%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -82,74 +102,171 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
                : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
   return v;
 }
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
+  return v;
+}
 __device__ __forceinline__ uint2 lds64(uint32_t a) {
   uint2 v;
   asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
   return v;
 }
 
-__global__ void __launch_bounds__(32 * kWarps, 4)
+// words of a unit description; query and slot of row r at H_QUERY + r, H_SLOT + r
+enum { H_ROW = 0, H_BEGIN = 1, H_TOK = 2, H_NUSERS = 4, H_ADD = 5, H_R0 = 8, H_KVH = 9, H_BID = 10,   // the first two block ids
+       H_QUERY = 16, H_SLOT = 24 };
+
+__global__ void __launch_bounds__(32 * kWarps, 1)
 attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ float fold_m[kWarps][kRows], fold_l[kWarps][kRows];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, q = lane & 3;
-  const int kvh = blockIdx.y;
   const int G = a.shape.group, HQ = a.shape.num_q_heads, HKV = a.shape.num_kv_heads;
+  const uint32_t ring = s32(smem) + warp * kDepth * kSlot;
+  const uint32_t qrows = s32(smem) + kOffQ + warp * kRows * kDim * 2;
+  int* const hdrs = (int*)(smem + kOffHdr) + warp * kHdrs * kHdrInts;
+  auto hdr = [&](int seq) { return hdrs + (seq & (kHdrs - 1)) * kHdrInts; };
 
-  // the CTA's item and row tile: items of a class have the same number of row tiles
-  int cls = 0;
-  while (cls < 3 && (int)blockIdx.x >= grid.cta_end[cls]) ++cls;
-  const int cta = (int)blockIdx.x - (cls ? grid.cta_end[cls - 1] : 0);
-  const WorkItem it = a.d_items[grid.item_begin[cls] + cta / grid.tiles[cls]];
-  const int r0 = cta % grid.tiles[cls] * kRows;
-  const int R = it.n_users * G;
-  if (r0 >= R) return;                               // (an item narrower than its class)
-
-  const int tok_end = it.tok_end < 0 ? a.d_lens[it.table_row] : it.tok_end;
-  const int n_tok = tok_end - it.tok_begin;
-  const int n_blk = (n_tok + kBlock - 1) / kBlock;
-  const int32_t* table = a.d_tables + (size_t)it.table_row * a.shape.table_stride +
-                         it.tok_begin / kBlock;
-  const uint32_t ring = s32(smem) + warp * kRing;
-
-  // ---- loads: this warp's k-th block is block warp + 4 k of the item
-  const int my_blk = n_blk > warp ? (n_blk - warp + kWarps - 1) / kWarps : 0;
-  auto issue = [&](int k, int bid) {
-    const size_t tile = ((size_t)bid * HKV + kvh) * kQ4TileBytes;
-    const uint8_t* kt = (const uint8_t*)a.k_pool + tile;
-    const uint8_t* vt = (const uint8_t*)a.v_pool + tile - kQ4TileBytes;
-    const uint32_t dst = ring + (k % kDepth) * kSlot;
+  // ---- descriptions, one phase per call: item; its users, first block id and length; stored
+  int f_seq = 0, f_phase = 0, f_pass = 0;            // units described so far; pass over the list
+  bool f_end = false;
+  int t0 = 0, t1 = 0, t2 = 0, t4 = 0, f_r0 = 0, f_kvh = 0;
+  uint2 t3 = make_uint2(0u, 0u);
+  auto fetch_step = [&]() {
+    if (f_phase == 0) {
+      const int W = gridDim.x * kWarps, w = warp * gridDim.x + blockIdx.x;
+      const int u = f_pass * W + ((f_pass & 1) ? W - 1 - w : w);
+      ++f_pass;
+      if (u >= grid.unit_end[3]) {
+        f_end = (long long)f_pass * W >= grid.unit_end[3];   // (a backward pass may start past the end)
+        return;
+      }
+      int x = u, item = grid.item_begin[0], tiles = grid.tiles[0];
 #pragma unroll
-    for (int j = 0; j < 2 * kQ4TileBytes / 512; ++j) {
-      const int x = (j * 32 + lane) * 16;
-      cp_async16(dst + x, (x < kQ4TileBytes ? kt : vt) + x);
+      for (int k = 1; k < 4; ++k)
+        if (u >= grid.unit_end[k - 1]) {
+          x = u - grid.unit_end[k - 1];
+          item = grid.item_begin[k];
+          tiles = grid.tiles[k];
+        }
+      f_r0 = x % tiles * kRows;
+      x /= tiles;
+      f_kvh = x % HKV;
+      t0 = lane < 8 ? __ldg((const int*)(a.d_items + item + x / HKV) + lane) : 0;
+      f_phase = 1;
+    } else if (f_phase == 1) {
+      const int row = __shfl_sync(0xffffffffu, t0, 0), begin = __shfl_sync(0xffffffffu, t0, 1);
+      const int end = __shfl_sync(0xffffffffu, t0, 2), ub = __shfl_sync(0xffffffffu, t0, 3);
+      const int R = __shfl_sync(0xffffffffu, t0, 4) * G;
+      f_phase = 0;
+      if (f_r0 >= R) return;                         // an item narrower than its class
+      t1 = (end < 0 ? a.d_lens[row] : end) - begin;
+      const int32_t* tab = a.d_tables + (size_t)row * a.shape.table_stride;
+      t2 = tab[begin / kBlock];
+      t4 = tab[min(begin / kBlock + 1, a.shape.table_stride - 1)];   // (unused if there is none)
+      const int r = f_r0 + (lane & 7);
+      t3 = make_uint2(0u, 0u);
+      if (r < R) t3 = *(const uint2*)(a.d_users + ub + r / G);
+      f_phase = 2;
+    } else {
+      int* h = hdr(f_seq);
+      if (lane < 8 && lane != H_TOK) h[lane] = t0;
+      if (lane == 8) {
+        h[H_TOK] = t1;
+        h[H_R0] = f_r0;
+        h[H_KVH] = f_kvh;
+        h[H_BID] = t2;
+        h[H_BID + 1] = t4;
+      }
+      if (lane >= 16) h[lane] = lane < 24 ? (int)t3.x : (int)t3.y;
+      __syncwarp();
+      ++f_seq;
+      f_phase = 0;
     }
   };
-#pragma unroll
-  for (int k = 0; k < kDepth - 1; ++k) {
-    if (k < my_blk) issue(k, table[warp + kWarps * k]);
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  }
-  int next_bid = kDepth - 1 < my_blk ? table[warp + kWarps * (kDepth - 1)] : 0;
 
-  // ---- queries: row r0 + g, dims 32 j + 8 q .. + 7, as B fragments
-  uint32_t qb[4][4];
-  float qs[4][2], unit[2];       // of rows 2 q, 2 q + 1: sums over each group; 2^24 / their factor
-  {
-    const int r = r0 + g;
+  // ---- loads: at most one unit ahead of the one that is computed, and not before that one's
+  // query rows have been read (the next unit's take their place)
+  int c_seq = 0, k = 0;                              // the unit being computed; its next block
+  int l_seq = -1, l_k = 0, l_n = 0, l_bid = 0, l_bid1 = 0, l_kvh = 0;
+  const int32_t* l_tab = nullptr;
+  int issue_slot = 0, use_slot = 0, ahead = 0;       // ring; steps requested and not computed
+  auto issue_block = [&](int bid, uint32_t dst) {
+    const size_t tile = ((size_t)bid * HKV + l_kvh) * kQ4TileBytes + lane * 16;
+    const uint8_t* kt = (const uint8_t*)a.k_pool + tile;
+    const uint8_t* vt = (const uint8_t*)a.v_pool + tile - kQ4TileBytes;
+    cp_async16(dst, kt);
+    cp_async16(dst + 512, kt + 512);
+    cp_async16(dst + 1024, (lane < 16 ? kt : vt) + 1024);
+    cp_async16(dst + 1536, vt + 1536);
+    cp_async16(dst + 2048, vt + 2048);
+  };
+  auto issue = [&]() {                               // blocks l_k and l_k + 1 of the loads' unit
+    const uint32_t dst = ring + issue_slot * kSlot + lane * 16;
+    issue_block(l_bid, dst);
+    if (l_k + 1 < l_n) issue_block(l_bid1, dst + kTile);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    issue_slot = issue_slot == kDepth - 1 ? 0 : issue_slot + 1;
+    ++ahead;
+    l_k += kStep;
+    if (l_k < l_n) {                                 // (arrive while a step is computed)
+      l_bid = l_tab[l_k];
+      l_bid1 = l_tab[min(l_k + 1, l_n - 1)];
+    }
+  };
+  auto next_unit = [&]() -> bool {                   // moves the loads on to it
+    if (l_seq > c_seq || (l_seq == c_seq && k == 0)) return false;
+    while (f_seq <= l_seq + 1 && !f_end) fetch_step();
+    if (f_seq <= l_seq + 1) return false;            // no more units
+    const int* h = hdr(++l_seq);
+    l_n = (h[H_TOK] + kBlock - 1) / kBlock;
+    l_k = 0;
+    l_kvh = h[H_KVH];
+    l_bid = h[H_BID];
+    l_bid1 = h[H_BID + 1];
+    l_tab = a.d_tables + (size_t)h[H_ROW] * a.shape.table_stride + h[H_BEGIN] / kBlock;
+    // the query rows, committed with the first tile: half a warp copies one
+    const int rows = h[H_NUSERS] * G - h[H_R0];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < kRows / 2; ++j) {
+      const int r = 2 * j + (lane >> 4);
+      if (r < rows)
+        cp_async16(qrows + r * kDim * 2 + (lane & 15) * 16,
+                   (const uint4*)a.q + ((size_t)h[H_QUERY + r] * HQ + l_kvh * G +
+                                        (h[H_R0] + r) % G) * 16 + (lane & 15));
+    }
+    return true;
+  };
+
+  // ---- state of the unit being computed
+  int n_tok = 0, rows = 0;
+  uint32_t qb[4][4];             // row r0 + g, dims 32 j + 8 q .. + 7, as B fragments
+  uint32_t qsum[2];              // row r0 + g: the sum over group q as three bf16 numbers
+  float unit[2];                 // rows 2 q, 2 q + 1: scale * 2^24 / their factor
+  float o[8][4], lsum[4][2], ref[2], l[2];
+
+#pragma unroll 1
+  for (;;) {
+  __syncwarp();                  // (the tile and the description read last may be overwritten)
+  if (k < 4 * kStep && !f_end && f_seq < c_seq + kHdrs) fetch_step();
+#pragma unroll 1
+  do {                           // (once, but for the start and units too short to run ahead of)
+    if (l_k >= l_n && !next_unit()) break;
+    issue();
+  } while (ahead < kDepth);
+  if (ahead == 0) break;
+  if (ahead == kDepth) asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+  else asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncwarp();
+  if (k == 0) {
+    n_tok = hdr(c_seq)[H_TOK];
+    rows = hdr(c_seq)[H_NUSERS] * G - hdr(c_seq)[H_R0];
 #pragma unroll
-      for (int p = 0; p < 4; ++p) qb[j][p] = 0u;
-    if (r < R) {
-      const int query = a.d_users[it.user_begin + r / G].query;
-      const uint4* src = (const uint4*)a.q + ((size_t)query * HQ + kvh * G + r % G) * 16 + q;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint4 v = __ldg(src + 4 * j);
-        qb[j][0] = v.x; qb[j][1] = v.y; qb[j][2] = v.z; qb[j][3] = v.w;
-      }
+    for (int j = 0; j < 4; ++j) {
+      uint4 v = make_uint4(0u, 0u, 0u, 0u);
+      if (g < rows) v = lds128(qrows + g * kDim * 2 + (32 * j + 8 * q) * 2);
+      qb[j][0] = v.x; qb[j][1] = v.y; qb[j][2] = v.z; qb[j][3] = v.w;
     }
     uint32_t top = 0;            // bits of the row's largest magnitude (bf16, in the high half)
 #pragma unroll
@@ -159,9 +276,10 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
         top = max(top, max(qb[j][p] << 17, (qb[j][p] & 0x7fff0000u) << 1));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    // the factor 2^k; a row of zeros or subnormal numbers has k at its limit
-    const int k = min(126, 14 + 127 - (int)(top >> 24));
-    const float f = __uint_as_float((uint32_t)(k + 127) << 23);
+    // the factor 2^lift; a row of zeros or subnormal numbers has it at its limit
+    const int lift = min(126, 14 + 127 - (int)(top >> 24));
+    const float f = __uint_as_float((uint32_t)(lift + 127) << 23);
+    float mine = 0.f;            // of group q
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       float x = 0.f;
@@ -173,41 +291,47 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
       }
       x += __shfl_xor_sync(0xffffffffu, x, 1);
       x += __shfl_xor_sync(0xffffffffu, x, 2);
-      qs[j][0] = __shfl_sync(0xffffffffu, x, 8 * q) * kCodeUnit;
-      qs[j][1] = __shfl_sync(0xffffffffu, x, 8 * q + 4) * kCodeUnit;
+      if (j == q) mine = x * kCodeUnit;
     }
-    // score * log2(e) * scale = (what the products give) * unit
-    const float u = a.scale_log2e * (1.f / kCodeUnit) * __uint_as_float((uint32_t)(127 - k) << 23);
+    const float m0 = __bfloat162float(__float2bfloat16_rn(mine)), m1 = mine - m0;
+    qsum[0] = pack2(m0, m1);
+    qsum[1] = pack2(m1 - __bfloat162float(__float2bfloat16_rn(m1)), 0.f);
+    // score * log2(e) * scale = (what the products give) * unit; never 0, so that the -inf of
+    // a masked score stays one
+    float u = a.scale_log2e * (1.f / kCodeUnit) * __uint_as_float((uint32_t)(127 - lift) << 23);
+    if (fabsf(u) < 1.17549435e-38f) u = 1.17549435e-38f;
     unit[0] = __shfl_sync(0xffffffffu, u, 8 * q);
     unit[1] = __shfl_sync(0xffffffffu, u, 8 * q + 4);
+#pragma unroll
+    for (int m = 0; m < 8; ++m)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[m][e] = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) lsum[j][0] = lsum[j][1] = 0.f;
+    ref[0] = ref[1] = -INFINITY;
+    l[0] = l[1] = 0.f;
   }
+  const uint32_t tile0 = ring + use_slot * kSlot;
 
-  float o[8][4], lsum[4][2], ref[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    // ---- scores of tokens g and g + 8 of each block for rows 2 q, 2 q + 1, up to the factor `unit`
+    float x[kStep][4];
 #pragma unroll
-  for (int m = 0; m < 8; ++m)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[m][e] = 0.f;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) lsum[j][0] = lsum[j][1] = 0.f;
-
-  for (int k = 0; k < my_blk; ++k) {
-    asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 2) : "memory");
-    __syncwarp();
-    const uint32_t kt = ring + (k % kDepth) * kSlot, vt = kt + kQ4TileBytes;
-    // the slot after the last one in flight was read in the previous pass: refill it
-    if (k + kDepth - 1 < my_blk) issue(k + kDepth - 1, next_bid);
-    asm volatile("cp.async.commit_group;" ::: "memory");
-    next_bid = k + kDepth < my_blk ? table[warp + kWarps * (k + kDepth)] : 0;
-
-    // ---- scores of tokens g and g + 8 for rows 2 q and 2 q + 1
-    float x[4] = {0.f, 0.f, 0.f, 0.f};
-    {
+    for (int b = 0; b < kStep; ++b) {
+      const uint32_t kt = tile0 + b * kTile;
       const uint4 k0 = lds128(kt + g * kQ4RowBytes + q * 16);
       const uint4 k1 = lds128(kt + (g + 8) * kQ4RowBytes + q * 16);
       const uint4 s0 = lds128(kt + g * kQ4RowBytes + kQ4CodeBytes);
       const uint4 s1 = lds128(kt + (g + 8) * kQ4RowBytes + kQ4CodeBytes);
+      const uint32_t lo0 = lds32(kt + g * kQ4RowBytes + kQ4CodeBytes + 4 * q);
+      const uint32_t lo1 = lds32(kt + (g + 8) * kQ4RowBytes + kQ4CodeBytes + 4 * q);
       const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
       const uint32_t t0[4] = {s0.x, s0.y, s0.z, s0.w}, t1[4] = {s1.x, s1.y, s1.z, s1.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[b][e] = 0.f;
+      {
+        const uint32_t a0 = __byte_perm(lo0, 0u, 0x3232), a1 = __byte_perm(lo1, 0u, 0x3232);
+        mma_bf16(x[b], a0, a1, a0, a1, qsum[0], qsum[1]);
+      }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         float acc[4] = {0.f, 0.f, 0.f, 0.f};
@@ -216,54 +340,59 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
         mma_f16(acc, codes_f16(w0[j], 2), codes_f16(w1[j], 2), codes_f16(w0[j], 3),
                 codes_f16(w1[j], 3), qb[j][2], qb[j][3]);
         const float sa = bf16_lo(t0[j]), sb = bf16_lo(t1[j]);
-        const float la = bf16_hi(t0[j]), lb = bf16_hi(t1[j]);
-        x[0] = fmaf(sa, acc[0], fmaf(la, qs[j][0], x[0]));
-        x[1] = fmaf(sa, acc[1], fmaf(la, qs[j][1], x[1]));
-        x[2] = fmaf(sb, acc[2], fmaf(lb, qs[j][0], x[2]));
-        x[3] = fmaf(sb, acc[3], fmaf(lb, qs[j][1], x[3]));
+        x[b][0] = fmaf(sa, acc[0], x[b][0]);
+        x[b][1] = fmaf(sa, acc[1], x[b][1]);
+        x[b][2] = fmaf(sb, acc[2], x[b][2]);
+        x[b][3] = fmaf(sb, acc[3], x[b][3]);
       }
     }
-    x[0] *= unit[0];
-    x[1] *= unit[1];
-    x[2] *= unit[0];
-    x[3] *= unit[1];
 
-    // ---- V scales of tokens g and g + 8; rows past the length hold unspecified bits
-    uint4 v0 = lds128(vt + g * kQ4RowBytes + kQ4CodeBytes);
-    uint4 v1 = lds128(vt + (g + 8) * kQ4RowBytes + kQ4CodeBytes);
-    const int nv = n_tok - (warp + kWarps * k) * kBlock;
-    if (nv < kBlock) {
-      if (g >= nv) {
-        x[0] = x[1] = -INFINITY;
-        v0 = make_uint4(0u, 0u, 0u, 0u);
-      }
-      if (g + 8 >= nv) {
-        x[2] = x[3] = -INFINITY;
-        v1 = make_uint4(0u, 0u, 0u, 0u);
-      }
+    // ---- V scales of the same tokens; rows past the length hold unspecified bits
+    uint32_t z[kStep][2][4];
+#pragma unroll
+    for (int b = 0; b < kStep; ++b) {
+      const uint32_t vs = tile0 + b * kTile + kQ4TileBytes + kQ4CodeBytes;
+      const uint4 v0 = lds128(vs + g * kQ4RowBytes), v1 = lds128(vs + (g + 8) * kQ4RowBytes);
+      z[b][0][0] = v0.x; z[b][0][1] = v0.y; z[b][0][2] = v0.z; z[b][0][3] = v0.w;
+      z[b][1][0] = v1.x; z[b][1][1] = v1.y; z[b][1][2] = v1.z; z[b][1][3] = v1.w;
     }
-    const uint32_t z0[4] = {v0.x, v0.y, v0.z, v0.w}, z1[4] = {v1.x, v1.y, v1.z, v1.w};
+    const int nv = n_tok - k * kBlock;
+    if (nv < kStep * kBlock) {
+#pragma unroll
+      for (int b = 0; b < kStep; ++b)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          if (g + 8 * e + kBlock * b >= nv) {
+            x[b][2 * e] = copysignf(INFINITY, -unit[0]);
+            x[b][2 * e + 1] = copysignf(INFINITY, -unit[1]);
+            z[b][e][0] = z[b][e][1] = z[b][e][2] = z[b][e][3] = 0u;
+          }
+    }
     // log2 of a token's largest scale, from the bits of the number (below by at most 0.09)
-    auto scale_log2 = [](const uint32_t (&z)[4]) {
-      const int top = max(max((int)(z[0] << 16), (int)(z[1] << 16)),
-                          max((int)(z[2] << 16), (int)(z[3] << 16)));
-      return fmaxf(fmaf((float)top, 1.f / 8388608.f, -127.f), kMinScaleLog2);
-    };
-    const float e0 = scale_log2(z0), e1 = scale_log2(z1);
-    const float y0 = fmaxf(x[0] + e0, x[2] + e1), y1 = fmaxf(x[1] + e0, x[3] + e1);
+    float y0 = -INFINITY, y1 = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < kStep; ++b)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t(&w)[4] = z[b][e];
+        const int top = max(max(max((int)(w[0] << 16), (int)(w[1] << 16)), (int)(w[2] << 16)),
+                            (int)(w[3] << 16));
+        const float sl = fmaxf(fmaf((float)top, 1.f / 8388608.f, -127.f), kMinScaleLog2);
+        y0 = fmaxf(y0, fmaf(x[b][2 * e], unit[0], sl));
+        y1 = fmaxf(y1, fmaf(x[b][2 * e + 1], unit[1], sl));
+      }
     if (__any_sync(0xffffffffu, y0 > ref[0] + kSlack || y1 > ref[1] + kSlack)) {
-      float m0 = y0, m1 = y1;
 #pragma unroll
       for (int d = 4; d < 32; d <<= 1) {
-        m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, d));
-        m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, d));
+        y0 = fmaxf(y0, __shfl_xor_sync(0xffffffffu, y0, d));
+        y1 = fmaxf(y1, __shfl_xor_sync(0xffffffffu, y1, d));
       }
-      m0 = fmaxf(m0, ref[0]);
-      m1 = fmaxf(m1, ref[1]);
-      const float f0 = ref[0] == -INFINITY ? 0.f : ex2(ref[0] - m0);
-      const float f1 = ref[1] == -INFINITY ? 0.f : ex2(ref[1] - m1);
-      ref[0] = m0;
-      ref[1] = m1;
+      y0 = fmaxf(y0, ref[0]);
+      y1 = fmaxf(y1, ref[1]);
+      const float f0 = ref[0] == -INFINITY ? 0.f : ex2(ref[0] - y0);
+      const float f1 = ref[1] == -INFINITY ? 0.f : ex2(ref[1] - y1);
+      ref[0] = y0;
+      ref[1] = y1;
       l[0] *= f0;
       l[1] *= f1;
 #pragma unroll
@@ -276,36 +405,45 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
         lsum[j][1] *= f1;
       }
     }
-    const float p0 = ex2(x[0] - ref[0]), p1 = ex2(x[1] - ref[1]);
-    const float p2 = ex2(x[2] - ref[0]), p3 = ex2(x[3] - ref[1]);
-    l[0] += p0 + p2;
-    l[1] += p1 + p3;
+#pragma unroll
+    for (int b = 0; b < kStep; ++b) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[b][e] = ex2(fmaf(x[b][e], unit[e & 1], -ref[e & 1]));
+      l[0] += x[b][0] + x[b][2];
+      l[1] += x[b][1] + x[b][3];
+    }
 
     // ---- O^T += V^T P^T
-    const uint2 t0 = lds64(vt + (2 * q) * kQ4RowBytes + 8 * g);
-    const uint2 t1 = lds64(vt + (2 * q + 1) * kQ4RowBytes + 8 * g);
-    const uint2 t2 = lds64(vt + (2 * q + 8) * kQ4RowBytes + 8 * g);
-    const uint2 t3 = lds64(vt + (2 * q + 9) * kQ4RowBytes + 8 * g);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float sa = bf16_lo(z0[j]), sb = bf16_lo(z1[j]);
-      const uint32_t b0 = transpose8x8(pack_f16(p0 * sa, p1 * sa));
-      const uint32_t b1 = transpose8x8(pack_f16(p2 * sb, p3 * sb));
-      const float la = bf16_hi(z0[j]), lb = bf16_hi(z1[j]);
-      lsum[j][0] = fmaf(p0, la, fmaf(p2, lb, lsum[j][0]));
-      lsum[j][1] = fmaf(p1, la, fmaf(p3, lb, lsum[j][1]));
-      const uint32_t sel = (j & 1) ? 0x7632 : 0x5410;
-      const uint32_t xl = __byte_perm(j < 2 ? t0.x : t0.y, j < 2 ? t1.x : t1.y, sel);
-      const uint32_t xh = __byte_perm(j < 2 ? t2.x : t2.y, j < 2 ? t3.x : t3.y, sel);
-      mma_f16(o[2 * j], codes_f16(xl, 0), codes_f16(xl, 1), codes_f16(xh, 0), codes_f16(xh, 1),
-              b0, b1);
-      mma_f16(o[2 * j + 1], codes_f16(xl, 2), codes_f16(xl, 3), codes_f16(xh, 2), codes_f16(xh, 3),
-              b0, b1);
+    for (int b = 0; b < kStep; ++b) {
+      const uint32_t vt = tile0 + b * kTile + kQ4TileBytes + 8 * g;
+      const uint2 t0 = lds64(vt + (2 * q) * kQ4RowBytes), t1 = lds64(vt + (2 * q + 1) * kQ4RowBytes);
+      const uint2 t2 = lds64(vt + (2 * q + 8) * kQ4RowBytes);
+      const uint2 t3 = lds64(vt + (2 * q + 9) * kQ4RowBytes);
+      const float(&p)[4] = x[b];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float sa = bf16_lo(z[b][0][j]), sb = bf16_lo(z[b][1][j]);
+        const uint32_t b0 = transpose8x8(pack_f16(p[0] * sa, p[1] * sa));
+        const uint32_t b1 = transpose8x8(pack_f16(p[2] * sb, p[3] * sb));
+        const float la = bf16_hi(z[b][0][j]), lb = bf16_hi(z[b][1][j]);
+        lsum[j][0] = fmaf(p[0], la, fmaf(p[2], lb, lsum[j][0]));
+        lsum[j][1] = fmaf(p[1], la, fmaf(p[3], lb, lsum[j][1]));
+        const uint32_t sel = (j & 1) ? 0x7632 : 0x5410;
+        const uint32_t xl = __byte_perm(j < 2 ? t0.x : t0.y, j < 2 ? t1.x : t1.y, sel);
+        const uint32_t xh = __byte_perm(j < 2 ? t2.x : t2.y, j < 2 ? t3.x : t3.y, sel);
+        mma_f16(o[2 * j], codes_f16(xl, 0), codes_f16(xl, 1), codes_f16(xh, 0), codes_f16(xh, 1),
+                b0, b1);
+        mma_f16(o[2 * j + 1], codes_f16(xl, 2), codes_f16(xl, 3), codes_f16(xh, 2),
+                codes_f16(xh, 3), b0, b1);
+      }
     }
-  }
-  asm volatile("cp.async.wait_all;" ::: "memory");
+  --ahead;
+  use_slot = use_slot == kDepth - 1 ? 0 : use_slot + 1;
+  k += kStep;
+  if (k * kBlock < n_tok) continue;
 
-  // ---- sums over the lanes that hold other tokens of the same rows
+  // ---- end of the unit: sums over the lanes that hold other tokens of the same rows
 #pragma unroll
   for (int d = 4; d < 32; d <<= 1) {
     l[0] += __shfl_xor_sync(0xffffffffu, l[0], d);
@@ -316,54 +454,33 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
       lsum[j][1] += __shfl_xor_sync(0xffffffffu, lsum[j][1], d);
     }
   }
-  // ---- fold of the four warps (the rings are no longer needed)
-  __syncthreads();
-  float* fo = (float*)smem;
-  constexpr float kLow = 1.f / kCodeUnit, kHigh = kLow / 16.f;   // (odd nibbles counted 16 times)
-  if (g == 0) {
-    fold_m[warp][2 * q] = ref[0];
-    fold_m[warp][2 * q + 1] = ref[1];
-    fold_l[warp][2 * q] = l[0];
-    fold_l[warp][2 * q + 1] = l[1];
+  // ---- row 2 q + e: dims 32 j + 4 g .. + 3, to the output or to a partial result
+  const int* h = hdr(c_seq);
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int r = 2 * q + e;
+    if (r >= rows) continue;
+    constexpr float kLow = 1.f / kCodeUnit, kHigh = kLow / 16.f;   // (odd nibbles counted 16 times)
+    const int head = h[H_KVH] * G + (h[H_R0] + r) % G;
+    const int query = h[H_QUERY + r], slot = h[H_SLOT + r];
+    const float inv = slot < 0 ? 1.f / l[e] : 1.f;
+    const size_t prow = (size_t)(slot + h[H_ADD]) * HQ + head;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float4 v = make_float4(fmaf(o[2 * j][e], kLow, lsum[j][e]) * inv,
+                                   fmaf(o[2 * j][2 + e], kHigh, lsum[j][e]) * inv,
+                                   fmaf(o[2 * j + 1][e], kLow, lsum[j][e]) * inv,
+                                   fmaf(o[2 * j + 1][2 + e], kHigh, lsum[j][e]) * inv);
+      if (slot < 0)
+        *(uint2*)((__nv_bfloat16*)a.out + ((size_t)query * HQ + head) * kDim + 32 * j + 4 * g) =
+            make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
+      else
+        *(float4*)(a.part_o + prow * kDim + 32 * j + 4 * g) = v;
+    }
+    if (slot >= 0 && g == 0) a.part_ml[prow] = make_float2(ref[e], l[e]);
   }
-#pragma unroll
-  for (int e = 0; e < 2; ++e)                      // row 2 q + e: dims 32 j + 4 g .. + 3
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      *(float4*)(fo + warp * kFoldFloats + (2 * q + e) * kDim + 32 * j + 4 * g) =
-          make_float4(fmaf(o[2 * j][e], kLow, lsum[j][e]), fmaf(o[2 * j][2 + e], kHigh, lsum[j][e]),
-                      fmaf(o[2 * j + 1][e], kLow, lsum[j][e]),
-                      fmaf(o[2 * j + 1][2 + e], kHigh, lsum[j][e]));
-  __syncthreads();
-#pragma unroll
-  for (int rr = 0; rr < kRows / kWarps; ++rr) {
-    const int row = warp + kWarps * rr, r = r0 + row;
-    if (r >= R) continue;
-    float M = fold_m[0][row];
-#pragma unroll
-    for (int w = 1; w < kWarps; ++w) M = fmaxf(M, fold_m[w][row]);
-    float L = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      const float4 v = *(const float4*)(fo + w * kFoldFloats + row * kDim + 4 * lane);
-      // (a warp without blocks has -inf and zeros; a row of NaN scores has l = NaN)
-      const float f = fold_m[w][row] == M ? 1.f : ex2(fold_m[w][row] - M);
-      L = fmaf(fold_l[w][row], f, L);
-      acc.x = fmaf(v.x, f, acc.x); acc.y = fmaf(v.y, f, acc.y);
-      acc.z = fmaf(v.z, f, acc.z); acc.w = fmaf(v.w, f, acc.w);
-    }
-    const UserRef ur = a.d_users[it.user_begin + r / G];
-    const int head = kvh * G + r % G;
-    if (ur.slot < 0) {
-      const float inv = 1.f / L;
-      *((uint2*)((__nv_bfloat16*)a.out + ((size_t)ur.query * HQ + head) * kDim) + lane) =
-          make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
-    } else {
-      const size_t prow = (size_t)(ur.slot + it.slot_add) * HQ + head;
-      *((float4*)(a.part_o + prow * kDim) + lane) = acc;
-      if (lane == 0) a.part_ml[prow] = make_float2(M, L);
-    }
+  ++c_seq;
+  k = 0;
   }
 }
 
@@ -442,16 +559,18 @@ cudaError_t launch_attention_q4(const AttnArgs& a, const int32_t n_items[4],
                                 const int32_t max_rows[4], cudaStream_t st) {
   // classes as the planner orders them: items of 4, 3, 2 and 1 tiles of 16 rows
   Q4Grid g;
-  int ctas = 0, items = 0;
+  int64_t units = 0;
+  int items = 0;
   for (int k = 0; k < 4; ++k) {
     const int n = n_items[3 - k];
     g.tiles[k] = std::max(1, (max_rows[3 - k] + kRows - 1) / kRows);
     g.item_begin[k] = items;
     items += n;
-    ctas += n * g.tiles[k];
-    g.cta_end[k] = ctas;
+    units += (int64_t)n * g.tiles[k] * a.shape.num_kv_heads;
+    if (units > INT32_MAX - (1 << 20)) return cudaErrorInvalidValue;
+    g.unit_end[k] = (int32_t)units;
   }
-  if (ctas == 0) return cudaSuccess;
+  if (units == 0) return cudaSuccess;
   static bool configured[64] = {};
   int dev = 0;
   cudaGetDevice(&dev);
@@ -462,7 +581,8 @@ cudaError_t launch_attention_q4(const AttnArgs& a, const int32_t n_items[4],
     if (e != cudaSuccess) return e;
     configured[dev] = true;
   }
-  attn_q4_kernel<<<dim3(ctas, a.shape.num_kv_heads), 32 * kWarps, kSmemQ4, st>>>(a, g);
+  const int ctas = (int)std::min<int64_t>(units, a.num_sms);
+  attn_q4_kernel<<<ctas, 32 * kWarps, kSmemQ4, st>>>(a, g);
   return cudaGetLastError();
 }
 

@@ -137,7 +137,7 @@ bool Planner::build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_
 
   // ---- chunk length: enough items to fill the machine, never below 128 tokens
   const int64_t kInf = (int64_t)1 << 40;
-  int64_t chunk = std::max<int64_t>(128, round_up16(unique * hint_kv_heads_ / (num_sms_ * 8)));
+  int64_t chunk = std::max<int64_t>(128, round_up16(unique * hint_kv_heads_ / (num_sms_ * units_per_sm_)));
   // `chunk` is sized for the kernels that keep a CTA's loads in flight through TMA rings.  The
   // single-row kernel has no such staging and needs several CTAs per SM to cover the latency:
   // when its runs, dealt out four kv heads to a CTA, would give fewer than four CTAs per SM,
