@@ -61,6 +61,8 @@ constexpr int kOffHdr = kOffQ + kWarps * kRows * kDim * 2;
 constexpr int kSmemQ4 = kOffHdr + kWarps * kHdrs * kHdrInts * 4;
 static_assert(kSmemQ4 <= 227 * 1024, "shared memory");
 constexpr float kSlack = 8.f;                        // the reference moves only past 2^8
+constexpr float kNoRef = -3e38f;                      // of a row that has seen nothing (finite: a
+                                                     // masked score less this is still -inf)
 constexpr float kCodeUnit = 1.f / 16777216.f;        // what a code of 1 counts as in a product: 2^-24
 constexpr float kMinScaleLog2 = -60.f;               // V scales below 2^-60 count as 2^-60
 
@@ -243,6 +245,7 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
   int n_tok = 0, rows = 0;
   uint32_t qb[4][4];             // row r0 + g, dims 32 j + 8 q .. + 7, as B fragments
   uint32_t qsum[2];              // row r0 + g: the sum over group q as three bf16 numbers
+  bool narrow = false;           // at most four rows: columns 4-7 are theirs again (see below)
   float unit[2];                 // rows 2 q, 2 q + 1: scale * 2^24 / their factor
   float o[8][4], lsum[4][2], ref[2], l[2];
 
@@ -262,10 +265,12 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
   if (k == 0) {
     n_tok = hdr(c_seq)[H_TOK];
     rows = hdr(c_seq)[H_NUSERS] * G - hdr(c_seq)[H_R0];
+    narrow = rows <= kRows / 2;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       uint4 v = make_uint4(0u, 0u, 0u, 0u);
-      if (g < rows) v = lds128(qrows + g * kDim * 2 + (32 * j + 8 * q) * 2);
+      const int r = narrow ? g & 3 : g;
+      if (r < rows) v = lds128(qrows + r * kDim * 2 + (32 * j + 8 * q) * 2);
       qb[j][0] = v.x; qb[j][1] = v.y; qb[j][2] = v.z; qb[j][3] = v.w;
     }
     uint32_t top = 0;            // bits of the row's largest magnitude (bf16, in the high half)
@@ -308,80 +313,67 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
       for (int e = 0; e < 4; ++e) o[m][e] = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) lsum[j][0] = lsum[j][1] = 0.f;
-    ref[0] = ref[1] = -INFINITY;
+    ref[0] = ref[1] = kNoRef;
     l[0] = l[1] = 0.f;
   }
   const uint32_t tile0 = ring + use_slot * kSlot;
 
-    // ---- scores of tokens g and g + 8 of each block for rows 2 q, 2 q + 1, up to the factor `unit`
-    float x[kStep][4];
-#pragma unroll
-    for (int b = 0; b < kStep; ++b) {
-      const uint32_t kt = tile0 + b * kTile;
-      const uint4 k0 = lds128(kt + g * kQ4RowBytes + q * 16);
-      const uint4 k1 = lds128(kt + (g + 8) * kQ4RowBytes + q * 16);
-      const uint4 s0 = lds128(kt + g * kQ4RowBytes + kQ4CodeBytes);
-      const uint4 s1 = lds128(kt + (g + 8) * kQ4RowBytes + kQ4CodeBytes);
+    // ---- scores of tokens g and g + 8 of a block for rows 2 q, 2 q + 1, up to the factor `unit`
+    auto load_k = [&](uint32_t kt, uint4& k0, uint4& k1, float (&x)[4]) {
+      k0 = lds128(kt + g * kQ4RowBytes + q * 16);
+      k1 = lds128(kt + (g + 8) * kQ4RowBytes + q * 16);
       const uint32_t lo0 = lds32(kt + g * kQ4RowBytes + kQ4CodeBytes + 4 * q);
       const uint32_t lo1 = lds32(kt + (g + 8) * kQ4RowBytes + kQ4CodeBytes + 4 * q);
-      const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
-      const uint32_t t0[4] = {s0.x, s0.y, s0.z, s0.w}, t1[4] = {s1.x, s1.y, s1.z, s1.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[b][e] = 0.f;
-      {
-        const uint32_t a0 = __byte_perm(lo0, 0u, 0x3232), a1 = __byte_perm(lo1, 0u, 0x3232);
-        mma_bf16(x[b], a0, a1, a0, a1, qsum[0], qsum[1]);
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float acc[4] = {0.f, 0.f, 0.f, 0.f};
-        mma_f16(acc, codes_f16(w0[j], 0), codes_f16(w1[j], 0), codes_f16(w0[j], 1),
-                codes_f16(w1[j], 1), qb[j][0], qb[j][1]);
-        mma_f16(acc, codes_f16(w0[j], 2), codes_f16(w1[j], 2), codes_f16(w0[j], 3),
-                codes_f16(w1[j], 3), qb[j][2], qb[j][3]);
-        const float sa = bf16_lo(t0[j]), sb = bf16_lo(t1[j]);
-        x[b][0] = fmaf(sa, acc[0], x[b][0]);
-        x[b][1] = fmaf(sa, acc[1], x[b][1]);
-        x[b][2] = fmaf(sb, acc[2], x[b][2]);
-        x[b][3] = fmaf(sb, acc[3], x[b][3]);
-      }
-    }
-
-    // ---- V scales of the same tokens; rows past the length hold unspecified bits
-    uint32_t z[kStep][2][4];
-#pragma unroll
-    for (int b = 0; b < kStep; ++b) {
-      const uint32_t vs = tile0 + b * kTile + kQ4TileBytes + kQ4CodeBytes;
+      const uint32_t a0 = __byte_perm(lo0, 0u, 0x3232), a1 = __byte_perm(lo1, 0u, 0x3232);
+      x[0] = x[1] = x[2] = x[3] = 0.f;
+      mma_bf16(x, a0, a1, a0, a1, qsum[0], qsum[1]);
+    };
+    auto group_dot = [&](const uint4& k0, const uint4& k1, int j, float (&acc)[4]) {
+      const uint32_t w0 = j == 0 ? k0.x : j == 1 ? k0.y : j == 2 ? k0.z : k0.w;
+      const uint32_t w1 = j == 0 ? k1.x : j == 1 ? k1.y : j == 2 ? k1.z : k1.w;
+      acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
+      mma_f16(acc, codes_f16(w0, 0), codes_f16(w1, 0), codes_f16(w0, 1), codes_f16(w1, 1), qb[j][0],
+              qb[j][1]);
+      mma_f16(acc, codes_f16(w0, 2), codes_f16(w1, 2), codes_f16(w0, 3), codes_f16(w1, 3), qb[j][2],
+              qb[j][3]);
+    };
+    auto scale_add = [&](const uint4& s0, const uint4& s1, int j, const float (&acc)[4],
+                         float (&x)[4]) {
+      const float sa = bf16_lo(j == 0 ? s0.x : j == 1 ? s0.y : j == 2 ? s0.z : s0.w);
+      const float sb = bf16_lo(j == 0 ? s1.x : j == 1 ? s1.y : j == 2 ? s1.z : s1.w);
+      x[0] = fmaf(sa, acc[0], x[0]);
+      x[1] = fmaf(sa, acc[1], x[1]);
+      x[2] = fmaf(sb, acc[2], x[2]);
+      x[3] = fmaf(sb, acc[3], x[3]);
+    };
+    // V scales of the same tokens; rows past the length hold unspecified bits.  nv: tokens that count
+    auto load_z = [&](uint32_t vs, int nv, uint32_t (&z)[2][4], float (&x)[4]) {
       const uint4 v0 = lds128(vs + g * kQ4RowBytes), v1 = lds128(vs + (g + 8) * kQ4RowBytes);
-      z[b][0][0] = v0.x; z[b][0][1] = v0.y; z[b][0][2] = v0.z; z[b][0][3] = v0.w;
-      z[b][1][0] = v1.x; z[b][1][1] = v1.y; z[b][1][2] = v1.z; z[b][1][3] = v1.w;
-    }
-    const int nv = n_tok - k * kBlock;
-    if (nv < kStep * kBlock) {
-#pragma unroll
-      for (int b = 0; b < kStep; ++b)
+      z[0][0] = v0.x; z[0][1] = v0.y; z[0][2] = v0.z; z[0][3] = v0.w;
+      z[1][0] = v1.x; z[1][1] = v1.y; z[1][2] = v1.z; z[1][3] = v1.w;
+      if (nv < kBlock) {
 #pragma unroll
         for (int e = 0; e < 2; ++e)
-          if (g + 8 * e + kBlock * b >= nv) {
-            x[b][2 * e] = copysignf(INFINITY, -unit[0]);
-            x[b][2 * e + 1] = copysignf(INFINITY, -unit[1]);
-            z[b][e][0] = z[b][e][1] = z[b][e][2] = z[b][e][3] = 0u;
+          if (g + 8 * e >= nv) {
+            x[2 * e] = copysignf(INFINITY, -unit[0]);
+            x[2 * e + 1] = copysignf(INFINITY, -unit[1]);
+            z[e][0] = z[e][1] = z[e][2] = z[e][3] = 0u;
           }
-    }
-    // log2 of a token's largest scale, from the bits of the number (below by at most 0.09)
-    float y0 = -INFINITY, y1 = -INFINITY;
-#pragma unroll
-    for (int b = 0; b < kStep; ++b)
+      }
+    };
+    // score + log2 of the token's largest scale (from the bits of the number, below by at most 0.09)
+    auto tops = [&](const uint32_t (&z)[2][4], const float (&x)[4], float& y0, float& y1) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const uint32_t(&w)[4] = z[b][e];
-        const int top = max(max(max((int)(w[0] << 16), (int)(w[1] << 16)), (int)(w[2] << 16)),
-                            (int)(w[3] << 16));
+        const int top = max(max(max((int)(z[e][0] << 16), (int)(z[e][1] << 16)),
+                                (int)(z[e][2] << 16)), (int)(z[e][3] << 16));
         const float sl = fmaxf(fmaf((float)top, 1.f / 8388608.f, -127.f), kMinScaleLog2);
-        y0 = fmaxf(y0, fmaf(x[b][2 * e], unit[0], sl));
-        y1 = fmaxf(y1, fmaf(x[b][2 * e + 1], unit[1], sl));
+        y0 = fmaxf(y0, fmaf(x[2 * e], unit[0], sl));
+        y1 = fmaxf(y1, fmaf(x[2 * e + 1], unit[1], sl));
       }
-    if (__any_sync(0xffffffffu, y0 > ref[0] + kSlack || y1 > ref[1] + kSlack)) {
+    };
+    auto move_reference = [&](float y0, float y1) {
+      if (!__any_sync(0xffffffffu, y0 > ref[0] + kSlack || y1 > ref[1] + kSlack)) return;
 #pragma unroll
       for (int d = 4; d < 32; d <<= 1) {
         y0 = fmaxf(y0, __shfl_xor_sync(0xffffffffu, y0, d));
@@ -389,8 +381,7 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
       }
       y0 = fmaxf(y0, ref[0]);
       y1 = fmaxf(y1, ref[1]);
-      const float f0 = ref[0] == -INFINITY ? 0.f : ex2(ref[0] - y0);
-      const float f1 = ref[1] == -INFINITY ? 0.f : ex2(ref[1] - y1);
+      const float f0 = ex2(ref[0] - y0), f1 = ex2(ref[1] - y1);
       ref[0] = y0;
       ref[1] = y1;
       l[0] *= f0;
@@ -404,38 +395,116 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
         lsum[j][0] *= f0;
         lsum[j][1] *= f1;
       }
-    }
+    };
+    auto weights = [&](float (&x)[4]) {
 #pragma unroll
-    for (int b = 0; b < kStep; ++b) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[b][e] = ex2(fmaf(x[b][e], unit[e & 1], -ref[e & 1]));
-      l[0] += x[b][0] + x[b][2];
-      l[1] += x[b][1] + x[b][3];
-    }
+      for (int e = 0; e < 4; ++e) x[e] = ex2(fmaf(x[e], unit[e & 1], -ref[e & 1]));
+      l[0] += x[0] + x[2];
+      l[1] += x[1] + x[3];
+    };
+    // the B operand of group j, and the offsets' share
+    auto weights_b = [&](const uint32_t (&z)[2][4], const float (&p)[4], int j, uint32_t& b0,
+                         uint32_t& b1) {
+      const float sa = bf16_lo(z[0][j]), sb = bf16_lo(z[1][j]);
+      b0 = transpose8x8(pack_f16(p[0] * sa, p[1] * sa));
+      b1 = transpose8x8(pack_f16(p[2] * sb, p[3] * sb));
+      const float la = bf16_hi(z[0][j]), lb = bf16_hi(z[1][j]);
+      lsum[j][0] = fmaf(p[0], la, fmaf(p[2], lb, lsum[j][0]));
+      lsum[j][1] = fmaf(p[1], la, fmaf(p[3], lb, lsum[j][1]));
+    };
+    struct VWords { uint2 t0, t1, t2, t3; };
+    auto load_v = [&](uint32_t vt) {
+      VWords v;
+      v.t0 = lds64(vt + (2 * q) * kQ4RowBytes + 8 * g);
+      v.t1 = lds64(vt + (2 * q + 1) * kQ4RowBytes + 8 * g);
+      v.t2 = lds64(vt + (2 * q + 8) * kQ4RowBytes + 8 * g);
+      v.t3 = lds64(vt + (2 * q + 9) * kQ4RowBytes + 8 * g);
+      return v;
+    };
+    auto accumulate = [&](const VWords& v, int j, uint32_t b0, uint32_t b1) {
+      const uint32_t sel = (j & 1) ? 0x7632 : 0x5410;
+      const uint32_t xl = __byte_perm(j < 2 ? v.t0.x : v.t0.y, j < 2 ? v.t1.x : v.t1.y, sel);
+      const uint32_t xh = __byte_perm(j < 2 ? v.t2.x : v.t2.y, j < 2 ? v.t3.x : v.t3.y, sel);
+      mma_f16(o[2 * j], codes_f16(xl, 0), codes_f16(xl, 1), codes_f16(xh, 0), codes_f16(xh, 1), b0,
+              b1);
+      mma_f16(o[2 * j + 1], codes_f16(xl, 2), codes_f16(xl, 3), codes_f16(xh, 2), codes_f16(xh, 3),
+              b0, b1);
+    };
 
-    // ---- O^T += V^T P^T
+    const int nv = n_tok - k * kBlock;
+    if (narrow) {
+      // Columns 0-3 carry the rows over the step's first block, columns 4-7 the same rows over
+      // its second one, as if they were other rows (they meet at the end of the unit): everything
+      // that is done per score is done once for both blocks.  A lane's block is q / 2.
+      const uint32_t mine = tile0 + (q >> 1) * kTile;
+      float x[4], x1[4];
+      uint4 k0, k1, k2, k3;
+      load_k(tile0, k0, k1, x);
+      load_k(tile0 + kTile, k2, k3, x1);
+      const bool second = q & 2;
 #pragma unroll
-    for (int b = 0; b < kStep; ++b) {
-      const uint32_t vt = tile0 + b * kTile + kQ4TileBytes + 8 * g;
-      const uint2 t0 = lds64(vt + (2 * q) * kQ4RowBytes), t1 = lds64(vt + (2 * q + 1) * kQ4RowBytes);
-      const uint2 t2 = lds64(vt + (2 * q + 8) * kQ4RowBytes);
-      const uint2 t3 = lds64(vt + (2 * q + 9) * kQ4RowBytes);
-      const float(&p)[4] = x[b];
+      for (int e = 0; e < 4; ++e) x[e] = second ? x1[e] : x[e];
+      const uint4 s0 = lds128(mine + g * kQ4RowBytes + kQ4CodeBytes);
+      const uint4 s1 = lds128(mine + (g + 8) * kQ4RowBytes + kQ4CodeBytes);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float sa = bf16_lo(z[b][0][j]), sb = bf16_lo(z[b][1][j]);
-        const uint32_t b0 = transpose8x8(pack_f16(p[0] * sa, p[1] * sa));
-        const uint32_t b1 = transpose8x8(pack_f16(p[2] * sb, p[3] * sb));
-        const float la = bf16_hi(z[b][0][j]), lb = bf16_hi(z[b][1][j]);
-        lsum[j][0] = fmaf(p[0], la, fmaf(p[2], lb, lsum[j][0]));
-        lsum[j][1] = fmaf(p[1], la, fmaf(p[3], lb, lsum[j][1]));
-        const uint32_t sel = (j & 1) ? 0x7632 : 0x5410;
-        const uint32_t xl = __byte_perm(j < 2 ? t0.x : t0.y, j < 2 ? t1.x : t1.y, sel);
-        const uint32_t xh = __byte_perm(j < 2 ? t2.x : t2.y, j < 2 ? t3.x : t3.y, sel);
-        mma_f16(o[2 * j], codes_f16(xl, 0), codes_f16(xl, 1), codes_f16(xh, 0), codes_f16(xh, 1),
-                b0, b1);
-        mma_f16(o[2 * j + 1], codes_f16(xl, 2), codes_f16(xl, 3), codes_f16(xh, 2),
-                codes_f16(xh, 3), b0, b1);
+        float acc[4], acc1[4];
+        group_dot(k0, k1, j, acc);
+        group_dot(k2, k3, j, acc1);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = second ? acc1[e] : acc[e];
+        scale_add(s0, s1, j, acc, x);
+      }
+      uint32_t z[2][4];
+      load_z(mine + kQ4TileBytes + kQ4CodeBytes, nv - (q >> 1) * kBlock, z, x);
+      float y0 = -INFINITY, y1 = -INFINITY;
+      tops(z, x, y0, y1);
+      move_reference(y0, y1);
+      weights(x);
+      const uint32_t first_only = g < 4 ? ~0u : 0u;
+      const VWords va = load_v(tile0 + kQ4TileBytes), vb = load_v(tile0 + kTile + kQ4TileBytes);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t b0, b1;
+        weights_b(z, x, j, b0, b1);
+        accumulate(va, j, b0 & first_only, b1 & first_only);
+        accumulate(vb, j, b0 & ~first_only, b1 & ~first_only);
+      }
+    } else {
+      float x[kStep][4];
+      uint32_t z[kStep][2][4];
+      float y0 = -INFINITY, y1 = -INFINITY;
+#pragma unroll
+      for (int b = 0; b < kStep; ++b) {
+        const uint32_t kt = tile0 + b * kTile;
+        uint4 k0, k1;
+        load_k(kt, k0, k1, x[b]);
+        const uint4 s0 = lds128(kt + g * kQ4RowBytes + kQ4CodeBytes);
+        const uint4 s1 = lds128(kt + (g + 8) * kQ4RowBytes + kQ4CodeBytes);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float acc[4];
+          group_dot(k0, k1, j, acc);
+          scale_add(s0, s1, j, acc, x[b]);
+        }
+      }
+#pragma unroll
+      for (int b = 0; b < kStep; ++b) {
+        load_z(tile0 + b * kTile + kQ4TileBytes + kQ4CodeBytes, nv - b * kBlock, z[b], x[b]);
+        tops(z[b], x[b], y0, y1);
+      }
+      move_reference(y0, y1);
+#pragma unroll
+      for (int b = 0; b < kStep; ++b) weights(x[b]);
+#pragma unroll
+      for (int b = 0; b < kStep; ++b) {
+        const VWords v = load_v(tile0 + b * kTile + kQ4TileBytes);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t b0, b1;
+          weights_b(z[b], x[b], j, b0, b1);
+          accumulate(v, j, b0, b1);
+        }
       }
     }
   --ahead;
@@ -452,6 +521,29 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
     for (int j = 0; j < 4; ++j) {
       lsum[j][0] += __shfl_xor_sync(0xffffffffu, lsum[j][0], d);
       lsum[j][1] += __shfl_xor_sync(0xffffffffu, lsum[j][1], d);
+    }
+  }
+  if (narrow) {                  // row r over the first blocks and over the second ones: lanes q and q ^ 2
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const float other = __shfl_xor_sync(0xffffffffu, ref[e], 2);
+      const float m = fmaxf(ref[e], other);
+      const float f = ref[e] == m ? 1.f : ex2(ref[e] - m);   // (no second block: kNoRef and zeros)
+      ref[e] = m;
+      l[e] *= f;
+      l[e] += __shfl_xor_sync(0xffffffffu, l[e], 2);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        lsum[j][e] *= f;
+        lsum[j][e] += __shfl_xor_sync(0xffffffffu, lsum[j][e], 2);
+      }
+#pragma unroll
+      for (int m8 = 0; m8 < 8; ++m8) {
+        o[m8][e] *= f;
+        o[m8][e] += __shfl_xor_sync(0xffffffffu, o[m8][e], 2);
+        o[m8][2 + e] *= f;
+        o[m8][2 + e] += __shfl_xor_sync(0xffffffffu, o[m8][2 + e], 2);
+      }
     }
   }
   // ---- row 2 q + e: dims 32 j + 4 g .. + 3, to the output or to a partial result
