@@ -138,7 +138,7 @@ struct apar_ctx {
   int32_t last_cuda = 0;
   bool host_only = false;                     // bookkeeping only: no device, nothing is launched
   bool q4 = false;                            // the pools hold 4-bit rows (kv4.cuh)
-  int32_t plan_max_rows[4] = {0, 0, 0, 0};    // widest item of each class of the plan (4-bit pools)
+  Q4Items q4_items;                           // the plan's items by width (4-bit pools)
   // Every thread's table as runs of groups (blocks held by the same set of threads).  A
   // thread's blocks since it was last forked form its own, open group; a fork closes the full
   // blocks of that group (the child lists them from then on) and opens a new one.
@@ -404,7 +404,7 @@ apar_status launch_plan(apar_ctx* c, int layer, const void* q, void* out, float 
   // launched the ordinary way, which also orders them after everything before them.
   if (c->q4) {
     if (p.n_mma) {
-      APAR_CUDA(c, launch_attention_q4(a, p.n_mma_tiles, c->plan_max_rows, st));
+      APAR_CUDA(c, launch_attention_q4(a, c->q4_items, st));
       ++*launches_out;
     }
     if (c->plan_verify_n > 0) {
@@ -535,11 +535,16 @@ apar_status run_attention(apar_ctx* c, int n, const int32_t* qslots, const int32
         (int64_t)c->plan.items.size() > c->lay.entry_capacity)
       return APAR_ERR_WORKSPACE_TOO_SMALL;
     if (c->q4) {
-      for (int32_t& m : c->plan_max_rows) m = 0;
-      for (const WorkItem& w : c->plan.items) {
-        const int32_t rows = w.n_users * c->shape.group;
-        int32_t& m = c->plan_max_rows[(rows + 15) / 16 - 1];
-        m = std::max(m, rows);
+      std::vector<WorkItem>& items = c->plan.items;
+      auto rows = [&](const WorkItem& w) { return w.n_users * c->shape.group; };
+      const auto cut = std::stable_partition(
+          items.begin(), items.end(), [&](const WorkItem& w) { return rows(w) > kQ4NarrowRows; });
+      c->q4_items = Q4Items();
+      c->q4_items.n_narrow = (int32_t)(items.end() - cut);
+      for (auto w = items.begin(); w != cut; ++w) {
+        const int k = (rows(*w) + 15) / 16 - 1;
+        ++c->q4_items.n_items[k];
+        c->q4_items.max_rows[k] = std::max(c->q4_items.max_rows[k], rows(*w));
       }
     }
     c->last.attn_plan_host_us = std::chrono::duration_cast<std::chrono::microseconds>(

@@ -220,15 +220,20 @@ cudaError_t launch_q4_row_moves(void* k_pool, void* v_pool, const RowMove* d_mov
 cudaError_t launch_read_rows(bool q4, const void* k_pool, const void* v_pool, void* k_out,
                              void* v_out, const int32_t* d_slots, int64_t first_row, int n_rows,
                              int num_kv_heads, cudaStream_t st);
-// The units of an attention launch, in the planner's item order (four classes, widest first; the
-// items of a class have the same number of row tiles).
-struct Q4Grid {
-  int32_t unit_end[4], item_begin[4], tiles[4];
+// The items of a plan made with mma_min_rows = 1, reordered so that those with at most
+// kQ4NarrowRows rows come last: n_items[k] wider items of class k (k + 1 tiles of 16 rows), none
+// of them with more than max_rows[k] rows, and n_narrow narrow ones.
+constexpr int kQ4NarrowRows = 4;
+struct Q4Items {
+  int32_t n_items[4] = {0, 0, 0, 0}, max_rows[4] = {0, 0, 0, 0}, n_narrow = 0;
 };
-// Every item of a plan made with mma_min_rows = 1: n_items[k] items of class k (k + 1 tiles of
-// 16 rows), none of them with more than max_rows[k] rows.  Uses no a.tm_k / a.tm_v / a.d_ticket.
-cudaError_t launch_attention_q4(const AttnArgs& a, const int32_t n_items[4],
-                                const int32_t max_rows[4], cudaStream_t st);
+// The units of a launch: wide classes in the planner's order (widest first; the items of a class
+// have the same number of row tiles), then the narrow items.
+struct Q4Grid {
+  int32_t unit_end[4], item_begin[4], tiles[4], narrow_begin, narrow_units;
+};
+// Uses no a.tm_k / a.tm_v / a.d_ticket.
+cudaError_t launch_attention_q4(const AttnArgs& a, const Q4Items& items, cudaStream_t st);
 cudaError_t launch_q4_verify_tail(const AttnArgs& a, const VerifyDesc* d_desc, int n_desc,
                                   cudaStream_t st);
 

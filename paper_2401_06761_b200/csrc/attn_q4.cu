@@ -64,6 +64,8 @@ constexpr float kSlack = 8.f;                        // the reference moves only
 constexpr float kNoRef = -3e38f;                      // of a row that has seen nothing (finite: a
                                                      // masked score less this is still -inf)
 constexpr float kCodeUnit = 1.f / 16777216.f;        // what a code of 1 counts as in a product: 2^-24
+constexpr uint32_t kEven = 0x000f000fu;             // nibbles 0 and 4 of a word: f16 pair c * 2^-24
+constexpr uint32_t kOdd = 0x00f000f0u;              // nibbles 1 and 5: c * 2^-20
 constexpr float kMinScaleLog2 = -60.f;               // V scales below 2^-60 count as 2^-60
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
@@ -91,10 +93,6 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   __half2 h = __floats2half2_rn(lo, hi);
   return *(uint32_t*)&h;
 }
-// nibbles n and n + 4 of w as an f16 pair: c * 2^-24 for even n, c * 2^-20 for odd n
-__device__ __forceinline__ uint32_t codes_f16(uint32_t w, int n) {
-  return (n < 2 ? w : w >> 8) & ((n & 1) ? 0x00f000f0u : 0x000f000fu);
-}
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -116,12 +114,20 @@ __device__ __forceinline__ uint2 lds64(uint32_t a) {
 }
 
 // words of a unit description; query and slot of row r at H_QUERY + r, H_SLOT + r
-enum { H_ROW = 0, H_BEGIN = 1, H_TOK = 2, H_NUSERS = 4, H_ADD = 5, H_R0 = 8, H_KVH = 9, H_BID = 10,   // the first two block ids
-       H_QUERY = 16, H_SLOT = 24 };
+enum { H_ROW = 0, H_BEGIN = 1, H_TOK = 2, H_NUSERS = 4, H_ADD = 5, H_R0 = 8, H_KVH = 9, H_BID = 10,
+       H_QUERY = 16, H_SLOT = 24 };                  // (H_BID: the first two block ids)
 
-__global__ void __launch_bounds__(32 * kWarps, 1)
-attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
-  extern __shared__ __align__(128) uint8_t smem[];
+// One warp's share of the units of a launch.
+//
+// kNarrow: units of at most four rows.  Columns 0-3 carry the rows over a step's first block,
+// columns 4-7 the same rows over its second one, as if they were other rows (they meet at the end
+// of the unit): S^T of both blocks comes out of one accumulator, because each block is
+// multiplied with the queries in its own columns and zeros in the others, and everything that is
+// done per score is done once for both.  A lane's block is q / 2.  For O^T the weights of the other
+// block's columns are masked out of the B operand.
+template <bool kNarrow>
+__device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Grid& grid, uint8_t* smem) {
+  constexpr int kSets = kNarrow ? 2 : 1;             // query operands
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, q = lane & 3;
   const int G = a.shape.group, HQ = a.shape.num_q_heads, HKV = a.shape.num_kv_heads;
@@ -129,10 +135,11 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
   const uint32_t qrows = s32(smem) + kOffQ + warp * kRows * kDim * 2;
   int* const hdrs = (int*)(smem + kOffHdr) + warp * kHdrs * kHdrInts;
   auto hdr = [&](int seq) { return hdrs + (seq & (kHdrs - 1)) * kHdrInts; };
+  const int n_units = kNarrow ? grid.narrow_units : grid.unit_end[3];
 
-  // ---- descriptions, one phase per call: item; its users, first block id and length; stored
+  // ---- descriptions, one phase per call: item; its users, first block ids and length; stored
   int f_seq = 0, f_phase = 0, f_pass = 0;            // units described so far; pass over the list
-  bool f_end = false;
+  bool f_end = n_units == 0;
   int t0 = 0, t1 = 0, t2 = 0, t4 = 0, f_r0 = 0, f_kvh = 0;
   uint2 t3 = make_uint2(0u, 0u);
   auto fetch_step = [&]() {
@@ -140,20 +147,24 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
       const int W = gridDim.x * kWarps, w = warp * gridDim.x + blockIdx.x;
       const int u = f_pass * W + ((f_pass & 1) ? W - 1 - w : w);
       ++f_pass;
-      if (u >= grid.unit_end[3]) {
-        f_end = (long long)f_pass * W >= grid.unit_end[3];   // (a backward pass may start past the end)
+      if (u >= n_units) {
+        f_end = (long long)f_pass * W >= n_units;    // (a backward pass may start past the end)
         return;
       }
-      int x = u, item = grid.item_begin[0], tiles = grid.tiles[0];
+      int x = u, item = kNarrow ? grid.narrow_begin : grid.item_begin[0];
+      f_r0 = 0;
+      if (!kNarrow) {
+        int tiles = grid.tiles[0];
 #pragma unroll
-      for (int k = 1; k < 4; ++k)
-        if (u >= grid.unit_end[k - 1]) {
-          x = u - grid.unit_end[k - 1];
-          item = grid.item_begin[k];
-          tiles = grid.tiles[k];
-        }
-      f_r0 = x % tiles * kRows;
-      x /= tiles;
+        for (int k = 1; k < 4; ++k)
+          if (u >= grid.unit_end[k - 1]) {
+            x = u - grid.unit_end[k - 1];
+            item = grid.item_begin[k];
+            tiles = grid.tiles[k];
+          }
+        f_r0 = x % tiles * kRows;
+        x /= tiles;
+      }
       f_kvh = x % HKV;
       t0 = lane < 8 ? __ldg((const int*)(a.d_items + item + x / HKV) + lane) : 0;
       f_phase = 1;
@@ -193,7 +204,7 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
   int c_seq = 0, k = 0;                              // the unit being computed; its next block
   int l_seq = -1, l_k = 0, l_n = 0, l_bid = 0, l_bid1 = 0, l_kvh = 0;
   const int32_t* l_tab = nullptr;
-  int issue_slot = 0, use_slot = 0, ahead = 0;       // ring; steps requested and not computed
+  int issue_slot = 0, use_slot = 0, ahead = 0;       // steps requested and not computed
   auto issue_block = [&](int bid, uint32_t dst) {
     const size_t tile = ((size_t)bid * HKV + l_kvh) * kQ4TileBytes + lane * 16;
     const uint8_t* kt = (const uint8_t*)a.k_pool + tile;
@@ -231,7 +242,7 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
     // the query rows, committed with the first tile: half a warp copies one
     const int rows = h[H_NUSERS] * G - h[H_R0];
 #pragma unroll
-    for (int j = 0; j < kRows / 2; ++j) {
+    for (int j = 0; j < (kNarrow ? kRows / 4 : kRows / 2); ++j) {
       const int r = 2 * j + (lane >> 4);
       if (r < rows)
         cp_async16(qrows + r * kDim * 2 + (lane & 15) * 16,
@@ -243,118 +254,122 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
 
   // ---- state of the unit being computed
   int n_tok = 0, rows = 0;
-  uint32_t qb[4][4];             // row r0 + g, dims 32 j + 8 q .. + 7, as B fragments
-  uint32_t qsum[2];              // row r0 + g: the sum over group q as three bf16 numbers
-  bool narrow = false;           // at most four rows: columns 4-7 are theirs again (see below)
+  uint32_t qb[kSets][4][4];      // the column's row, dims 32 j + 8 q .. + 7, as B fragments
+  uint32_t qsum[kSets][2];       // its sum over group q as three bf16 numbers
   float unit[2];                 // rows 2 q, 2 q + 1: scale * 2^24 / their factor
   float o[8][4], lsum[4][2], ref[2], l[2];
 
 #pragma unroll 1
   for (;;) {
-  __syncwarp();                  // (the tile and the description read last may be overwritten)
-  if (k < 4 * kStep && !f_end && f_seq < c_seq + kHdrs) fetch_step();
+    __syncwarp();                // (the tiles and the description read last may be overwritten)
+    if (k < 4 * kStep && !f_end && f_seq < c_seq + kHdrs) fetch_step();
 #pragma unroll 1
-  do {                           // (once, but for the start and units too short to run ahead of)
-    if (l_k >= l_n && !next_unit()) break;
-    issue();
-  } while (ahead < kDepth);
-  if (ahead == 0) break;
-  if (ahead == kDepth) asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
-  else asm volatile("cp.async.wait_all;" ::: "memory");
-  __syncwarp();
-  if (k == 0) {
-    n_tok = hdr(c_seq)[H_TOK];
-    rows = hdr(c_seq)[H_NUSERS] * G - hdr(c_seq)[H_R0];
-    narrow = rows <= kRows / 2;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      uint4 v = make_uint4(0u, 0u, 0u, 0u);
-      const int r = narrow ? g & 3 : g;
-      if (r < rows) v = lds128(qrows + r * kDim * 2 + (32 * j + 8 * q) * 2);
-      qb[j][0] = v.x; qb[j][1] = v.y; qb[j][2] = v.z; qb[j][3] = v.w;
-    }
-    uint32_t top = 0;            // bits of the row's largest magnitude (bf16, in the high half)
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int p = 0; p < 4; ++p)
-        top = max(top, max(qb[j][p] << 17, (qb[j][p] & 0x7fff0000u) << 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    // the factor 2^lift; a row of zeros or subnormal numbers has it at its limit
-    const int lift = min(126, 14 + 127 - (int)(top >> 24));
-    const float f = __uint_as_float((uint32_t)(lift + 127) << 23);
-    float mine = 0.f;            // of group q
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float x = 0.f;
-#pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        const float e0 = bf16_lo(qb[j][p]) * f, e1 = bf16_hi(qb[j][p]) * f;
-        x += e0 + e1;
-        qb[j][p] = (p & 1) ? pack_f16(e0 * 0.0625f, e1 * 0.0625f) : pack_f16(e0, e1);
-      }
-      x += __shfl_xor_sync(0xffffffffu, x, 1);
-      x += __shfl_xor_sync(0xffffffffu, x, 2);
-      if (j == q) mine = x * kCodeUnit;
-    }
-    const float m0 = __bfloat162float(__float2bfloat16_rn(mine)), m1 = mine - m0;
-    qsum[0] = pack2(m0, m1);
-    qsum[1] = pack2(m1 - __bfloat162float(__float2bfloat16_rn(m1)), 0.f);
-    // score * log2(e) * scale = (what the products give) * unit; never 0, so that the -inf of
-    // a masked score stays one
-    float u = a.scale_log2e * (1.f / kCodeUnit) * __uint_as_float((uint32_t)(127 - lift) << 23);
-    if (fabsf(u) < 1.17549435e-38f) u = 1.17549435e-38f;
-    unit[0] = __shfl_sync(0xffffffffu, u, 8 * q);
-    unit[1] = __shfl_sync(0xffffffffu, u, 8 * q + 4);
-#pragma unroll
-    for (int m = 0; m < 8; ++m)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[m][e] = 0.f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) lsum[j][0] = lsum[j][1] = 0.f;
-    ref[0] = ref[1] = kNoRef;
-    l[0] = l[1] = 0.f;
-  }
-  const uint32_t tile0 = ring + use_slot * kSlot;
+    do {                         // (once, but for the start and units too short to run ahead of)
+      if (l_k >= l_n && !next_unit()) break;
+      issue();
+    } while (ahead < kDepth);
+    if (ahead == 0) break;
+    if (ahead == kDepth) asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+    else asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncwarp();
 
-    // ---- scores of tokens g and g + 8 of a block for rows 2 q, 2 q + 1, up to the factor `unit`
-    auto load_k = [&](uint32_t kt, uint4& k0, uint4& k1, float (&x)[4]) {
-      k0 = lds128(kt + g * kQ4RowBytes + q * 16);
-      k1 = lds128(kt + (g + 8) * kQ4RowBytes + q * 16);
-      const uint32_t lo0 = lds32(kt + g * kQ4RowBytes + kQ4CodeBytes + 4 * q);
-      const uint32_t lo1 = lds32(kt + (g + 8) * kQ4RowBytes + kQ4CodeBytes + 4 * q);
+    if (k == 0) {                // ---- a unit begins
+      n_tok = hdr(c_seq)[H_TOK];
+      rows = hdr(c_seq)[H_NUSERS] * G - hdr(c_seq)[H_R0];
+      const int r = kNarrow ? g & 3 : g;
+      uint32_t top = 0;          // bits of the row's largest magnitude, without the sign
+      uint4 v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[j] = make_uint4(0u, 0u, 0u, 0u);
+        if (r < rows) v[j] = lds128(qrows + r * kDim * 2 + (32 * j + 8 * q) * 2);
+        const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+#pragma unroll
+        for (int p = 0; p < 4; ++p) top = max(top, max(w[p] << 17, (w[p] & 0x7fff0000u) << 1));
+      }
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      // the factor 2^lift; a row of zeros or subnormal numbers has it at its limit
+      const int lift = min(126, 14 + 127 - (int)(top >> 24));
+      const float f = __uint_as_float((uint32_t)(lift + 127) << 23);
+      float mine = 0.f;          // the sum over group q
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+        float x = 0.f;
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const float e0 = bf16_lo(w[p]) * f, e1 = bf16_hi(w[p]) * f;
+          x += e0 + e1;
+          const uint32_t b = (p & 1) ? pack_f16(e0 * 0.0625f, e1 * 0.0625f) : pack_f16(e0, e1);
+          qb[0][j][p] = kNarrow && g >= 4 ? 0u : b;
+          if (kNarrow) qb[kSets - 1][j][p] = g >= 4 ? b : 0u;
+        }
+        x += __shfl_xor_sync(0xffffffffu, x, 1);
+        x += __shfl_xor_sync(0xffffffffu, x, 2);
+        if (j == q) mine = x * kCodeUnit;
+      }
+      const float m0 = __bfloat162float(__float2bfloat16_rn(mine)), m1 = mine - m0;
+      const uint32_t s0 = pack2(m0, m1);
+      const uint32_t s1 = pack2(m1 - __bfloat162float(__float2bfloat16_rn(m1)), 0.f);
+      qsum[0][0] = kNarrow && g >= 4 ? 0u : s0;
+      qsum[0][1] = kNarrow && g >= 4 ? 0u : s1;
+      if (kNarrow) {
+        qsum[kSets - 1][0] = g >= 4 ? s0 : 0u;
+        qsum[kSets - 1][1] = g >= 4 ? s1 : 0u;
+      }
+      // score * log2(e) * scale = (what the products give) * unit; never 0, so that the -inf of
+      // a masked score stays one
+      float u = a.scale_log2e * (1.f / kCodeUnit) * __uint_as_float((uint32_t)(127 - lift) << 23);
+      if (fabsf(u) < 1.17549435e-38f) u = 1.17549435e-38f;
+      unit[0] = __shfl_sync(0xffffffffu, u, 8 * q);
+      unit[1] = __shfl_sync(0xffffffffu, u, 8 * q + 4);
+#pragma unroll
+      for (int m = 0; m < 8; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[m][e] = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) lsum[j][0] = lsum[j][1] = 0.f;
+      ref[0] = ref[1] = kNoRef;
+      l[0] = l[1] = 0.f;
+    }
+    const uint32_t tile0 = ring + use_slot * kSlot;
+    const int nv = n_tok - k * kBlock;
+
+    // ---- pieces of a step.  Scores are those of tokens g and g + 8 of a block for rows 2 q and
+    // 2 q + 1, up to the factor `unit`.
+    auto offsets = [&](uint32_t kt, int n, const uint32_t (&sum)[2], float (&x)[4]) {
+      uint32_t lo0 = lds32(kt + g * kQ4RowBytes + kQ4CodeBytes + 4 * q);
+      uint32_t lo1 = lds32(kt + (g + 8) * kQ4RowBytes + kQ4CodeBytes + 4 * q);
+      if (kNarrow && n < kBlock) {   // (unspecified bits may be NaN, and meet the other columns' zeros)
+        if (g >= n) lo0 = 0u;
+        if (g + 8 >= n) lo1 = 0u;
+      }
       const uint32_t a0 = __byte_perm(lo0, 0u, 0x3232), a1 = __byte_perm(lo1, 0u, 0x3232);
-      x[0] = x[1] = x[2] = x[3] = 0.f;
-      mma_bf16(x, a0, a1, a0, a1, qsum[0], qsum[1]);
+      mma_bf16(x, a0, a1, a0, a1, sum[0], sum[1]);
     };
-    auto group_dot = [&](const uint4& k0, const uint4& k1, int j, float (&acc)[4]) {
-      const uint32_t w0 = j == 0 ? k0.x : j == 1 ? k0.y : j == 2 ? k0.z : k0.w;
-      const uint32_t w1 = j == 0 ? k1.x : j == 1 ? k1.y : j == 2 ? k1.z : k1.w;
-      acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
-      mma_f16(acc, codes_f16(w0, 0), codes_f16(w1, 0), codes_f16(w0, 1), codes_f16(w1, 1), qb[j][0],
-              qb[j][1]);
-      mma_f16(acc, codes_f16(w0, 2), codes_f16(w1, 2), codes_f16(w0, 3), codes_f16(w1, 3), qb[j][2],
-              qb[j][3]);
+    auto dot = [&](uint32_t w0, uint32_t w1, const uint32_t (&b)[4], float (&acc)[4]) {
+      const uint32_t h0 = w0 >> 8, h1 = w1 >> 8;
+      mma_f16(acc, w0 & kEven, w1 & kEven, w0 & kOdd, w1 & kOdd, b[0], b[1]);
+      mma_f16(acc, h0 & kEven, h1 & kEven, h0 & kOdd, h1 & kOdd, b[2], b[3]);
     };
-    auto scale_add = [&](const uint4& s0, const uint4& s1, int j, const float (&acc)[4],
-                         float (&x)[4]) {
-      const float sa = bf16_lo(j == 0 ? s0.x : j == 1 ? s0.y : j == 2 ? s0.z : s0.w);
-      const float sb = bf16_lo(j == 0 ? s1.x : j == 1 ? s1.y : j == 2 ? s1.z : s1.w);
+    auto scale_add = [&](uint32_t s0, uint32_t s1, const float (&acc)[4], float (&x)[4]) {
+      const float sa = bf16_lo(s0), sb = bf16_lo(s1);
       x[0] = fmaf(sa, acc[0], x[0]);
       x[1] = fmaf(sa, acc[1], x[1]);
       x[2] = fmaf(sb, acc[2], x[2]);
       x[3] = fmaf(sb, acc[3], x[3]);
     };
-    // V scales of the same tokens; rows past the length hold unspecified bits.  nv: tokens that count
-    auto load_z = [&](uint32_t vs, int nv, uint32_t (&z)[2][4], float (&x)[4]) {
-      const uint4 v0 = lds128(vs + g * kQ4RowBytes), v1 = lds128(vs + (g + 8) * kQ4RowBytes);
+    // V scales of the same tokens; rows past the length hold unspecified bits.  n: tokens that count
+    auto v_scales = [&](uint32_t vt, int n, uint32_t (&z)[2][4], float (&x)[4]) {
+      const uint32_t at = vt + (g >> 1) * kQ4PairBytes + 2 * kQ4CodeBytes + 16 * (g & 1);
+      const uint4 v0 = lds128(at), v1 = lds128(at + 4 * kQ4PairBytes);
       z[0][0] = v0.x; z[0][1] = v0.y; z[0][2] = v0.z; z[0][3] = v0.w;
       z[1][0] = v1.x; z[1][1] = v1.y; z[1][2] = v1.z; z[1][3] = v1.w;
-      if (nv < kBlock) {
+      if (n < kBlock) {
 #pragma unroll
         for (int e = 0; e < 2; ++e)
-          if (g + 8 * e >= nv) {
+          if (g + 8 * e >= n) {
             x[2 * e] = copysignf(INFINITY, -unit[0]);
             x[2 * e + 1] = copysignf(INFINITY, -unit[1]);
             z[e][0] = z[e][1] = z[e][2] = z[e][3] = 0u;
@@ -403,72 +418,70 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
       l[1] += x[1] + x[3];
     };
     // the B operand of group j, and the offsets' share
-    auto weights_b = [&](const uint32_t (&z)[2][4], const float (&p)[4], int j, uint32_t& b0,
+    auto weights_b = [&](uint32_t z0, uint32_t z1, const float (&p)[4], int j, uint32_t& b0,
                          uint32_t& b1) {
-      const float sa = bf16_lo(z[0][j]), sb = bf16_lo(z[1][j]);
+      const float sa = bf16_lo(z0), sb = bf16_lo(z1);
       b0 = transpose8x8(pack_f16(p[0] * sa, p[1] * sa));
       b1 = transpose8x8(pack_f16(p[2] * sb, p[3] * sb));
-      const float la = bf16_hi(z[0][j]), lb = bf16_hi(z[1][j]);
+      const float la = bf16_hi(z0), lb = bf16_hi(z1);
       lsum[j][0] = fmaf(p[0], la, fmaf(p[2], lb, lsum[j][0]));
       lsum[j][1] = fmaf(p[1], la, fmaf(p[3], lb, lsum[j][1]));
     };
-    struct VWords { uint2 t0, t1, t2, t3; };
-    auto load_v = [&](uint32_t vt) {
-      VWords v;
-      v.t0 = lds64(vt + (2 * q) * kQ4RowBytes + 8 * g);
-      v.t1 = lds64(vt + (2 * q + 1) * kQ4RowBytes + 8 * g);
-      v.t2 = lds64(vt + (2 * q + 8) * kQ4RowBytes + 8 * g);
-      v.t3 = lds64(vt + (2 * q + 9) * kQ4RowBytes + 8 * g);
-      return v;
+    auto accumulate = [&](uint32_t xl, uint32_t xh, uint32_t b0, uint32_t b1, float (&d0)[4],
+                          float (&d1)[4]) {
+      const uint32_t hl = xl >> 8, hh = xh >> 8;
+      mma_f16(d0, xl & kEven, xl & kOdd, xh & kEven, xh & kOdd, b0, b1);
+      mma_f16(d1, hl & kEven, hl & kOdd, hh & kEven, hh & kOdd, b0, b1);
     };
-    auto accumulate = [&](const VWords& v, int j, uint32_t b0, uint32_t b1) {
-      const uint32_t sel = (j & 1) ? 0x7632 : 0x5410;
-      const uint32_t xl = __byte_perm(j < 2 ? v.t0.x : v.t0.y, j < 2 ? v.t1.x : v.t1.y, sel);
-      const uint32_t xh = __byte_perm(j < 2 ? v.t2.x : v.t2.y, j < 2 ? v.t3.x : v.t3.y, sel);
-      mma_f16(o[2 * j], codes_f16(xl, 0), codes_f16(xl, 1), codes_f16(xh, 0), codes_f16(xh, 1), b0,
-              b1);
-      mma_f16(o[2 * j + 1], codes_f16(xl, 2), codes_f16(xl, 3), codes_f16(xh, 2), codes_f16(xh, 3),
-              b0, b1);
+    auto k_words = [&](uint32_t kt, uint4& w0, uint4& w1) {
+      w0 = lds128(kt + g * kQ4RowBytes + q * 16);
+      w1 = lds128(kt + (g + 8) * kQ4RowBytes + q * 16);
+    };
+    auto v_words = [&](uint32_t vt, uint4& w0, uint4& w1) {      // pairs q and q + 4
+      w0 = lds128(vt + q * kQ4PairBytes + g * 16);
+      w1 = lds128(vt + (q + 4) * kQ4PairBytes + g * 16);
     };
 
-    const int nv = n_tok - k * kBlock;
-    if (narrow) {
-      // Columns 0-3 carry the rows over the step's first block, columns 4-7 the same rows over
-      // its second one, as if they were other rows (they meet at the end of the unit): everything
-      // that is done per score is done once for both blocks.  A lane's block is q / 2.
+    if (kNarrow) {
       const uint32_t mine = tile0 + (q >> 1) * kTile;
-      float x[4], x1[4];
-      uint4 k0, k1, k2, k3;
-      load_k(tile0, k0, k1, x);
-      load_k(tile0 + kTile, k2, k3, x1);
-      const bool second = q & 2;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = second ? x1[e] : x[e];
-      const uint4 s0 = lds128(mine + g * kQ4RowBytes + kQ4CodeBytes);
-      const uint4 s1 = lds128(mine + (g + 8) * kQ4RowBytes + kQ4CodeBytes);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float acc[4], acc1[4];
-        group_dot(k0, k1, j, acc);
-        group_dot(k2, k3, j, acc1);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] = second ? acc1[e] : acc[e];
-        scale_add(s0, s1, j, acc, x);
+      float x[4] = {0.f, 0.f, 0.f, 0.f};
+      offsets(tile0, nv, qsum[0], x);
+      offsets(tile0 + kTile, nv - kBlock, qsum[kSets - 1], x);
+      {
+        uint4 a0, a1, c0, c1;
+        k_words(tile0, a0, a1);
+        k_words(tile0 + kTile, c0, c1);
+        const uint4 s0 = lds128(mine + g * kQ4RowBytes + kQ4CodeBytes);
+        const uint4 s1 = lds128(mine + (g + 8) * kQ4RowBytes + kQ4CodeBytes);
+        float acc[4][4] = {};
+        dot(a0.x, a1.x, qb[0][0], acc[0]); dot(c0.x, c1.x, qb[kSets - 1][0], acc[0]);
+        dot(a0.y, a1.y, qb[0][1], acc[1]); dot(c0.y, c1.y, qb[kSets - 1][1], acc[1]);
+        dot(a0.z, a1.z, qb[0][2], acc[2]); dot(c0.z, c1.z, qb[kSets - 1][2], acc[2]);
+        dot(a0.w, a1.w, qb[0][3], acc[3]); dot(c0.w, c1.w, qb[kSets - 1][3], acc[3]);
+        scale_add(s0.x, s1.x, acc[0], x);
+        scale_add(s0.y, s1.y, acc[1], x);
+        scale_add(s0.z, s1.z, acc[2], x);
+        scale_add(s0.w, s1.w, acc[3], x);
       }
       uint32_t z[2][4];
-      load_z(mine + kQ4TileBytes + kQ4CodeBytes, nv - (q >> 1) * kBlock, z, x);
+      v_scales(mine + kQ4TileBytes, nv - (q >> 1) * kBlock, z, x);
       float y0 = -INFINITY, y1 = -INFINITY;
       tops(z, x, y0, y1);
       move_reference(y0, y1);
       weights(x);
-      const uint32_t first_only = g < 4 ? ~0u : 0u;
-      const VWords va = load_v(tile0 + kQ4TileBytes), vb = load_v(tile0 + kTile + kQ4TileBytes);
+      uint4 v0, v1, v2, v3;
+      v_words(tile0 + kQ4TileBytes, v0, v1);
+      v_words(tile0 + kTile + kQ4TileBytes, v2, v3);
+      const uint32_t al[4] = {v0.x, v0.y, v0.z, v0.w}, ah[4] = {v1.x, v1.y, v1.z, v1.w};
+      const uint32_t cl[4] = {v2.x, v2.y, v2.z, v2.w}, ch[4] = {v3.x, v3.y, v3.z, v3.w};
+      const uint32_t first_columns = g < 4 ? ~0u : 0u;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         uint32_t b0, b1;
-        weights_b(z, x, j, b0, b1);
-        accumulate(va, j, b0 & first_only, b1 & first_only);
-        accumulate(vb, j, b0 & ~first_only, b1 & ~first_only);
+        weights_b(z[0][j], z[1][j], x, j, b0, b1);
+        const uint32_t c0 = b0 & first_columns, c1 = b1 & first_columns;
+        accumulate(al[j], ah[j], c0, c1, o[2 * j], o[2 * j + 1]);
+        accumulate(cl[j], ch[j], b0 ^ c0, b1 ^ c1, o[2 * j], o[2 * j + 1]);
       }
     } else {
       float x[kStep][4];
@@ -477,20 +490,24 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
 #pragma unroll
       for (int b = 0; b < kStep; ++b) {
         const uint32_t kt = tile0 + b * kTile;
-        uint4 k0, k1;
-        load_k(kt, k0, k1, x[b]);
+        uint4 w0, w1;
+        k_words(kt, w0, w1);
         const uint4 s0 = lds128(kt + g * kQ4RowBytes + kQ4CodeBytes);
         const uint4 s1 = lds128(kt + (g + 8) * kQ4RowBytes + kQ4CodeBytes);
+        const uint32_t wa[4] = {w0.x, w0.y, w0.z, w0.w}, wb[4] = {w1.x, w1.y, w1.z, w1.w};
+        const uint32_t sa[4] = {s0.x, s0.y, s0.z, s0.w}, sb[4] = {s1.x, s1.y, s1.z, s1.w};
+        x[b][0] = x[b][1] = x[b][2] = x[b][3] = 0.f;
+        offsets(kt, nv - b * kBlock, qsum[0], x[b]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          float acc[4];
-          group_dot(k0, k1, j, acc);
-          scale_add(s0, s1, j, acc, x[b]);
+          float acc[4] = {};
+          dot(wa[j], wb[j], qb[0][j], acc);
+          scale_add(sa[j], sb[j], acc, x[b]);
         }
       }
 #pragma unroll
       for (int b = 0; b < kStep; ++b) {
-        load_z(tile0 + b * kTile + kQ4TileBytes + kQ4CodeBytes, nv - b * kBlock, z[b], x[b]);
+        v_scales(tile0 + b * kTile + kQ4TileBytes, nv - b * kBlock, z[b], x[b]);
         tops(z[b], x[b], y0, y1);
       }
       move_reference(y0, y1);
@@ -498,82 +515,92 @@ attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
       for (int b = 0; b < kStep; ++b) weights(x[b]);
 #pragma unroll
       for (int b = 0; b < kStep; ++b) {
-        const VWords v = load_v(tile0 + b * kTile + kQ4TileBytes);
+        uint4 w0, w1;
+        v_words(tile0 + b * kTile + kQ4TileBytes, w0, w1);
+        const uint32_t xl[4] = {w0.x, w0.y, w0.z, w0.w}, xh[4] = {w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           uint32_t b0, b1;
-          weights_b(z[b], x[b], j, b0, b1);
-          accumulate(v, j, b0, b1);
+          weights_b(z[b][0][j], z[b][1][j], x[b], j, b0, b1);
+          accumulate(xl[j], xh[j], b0, b1, o[2 * j], o[2 * j + 1]);
         }
       }
     }
-  --ahead;
-  use_slot = use_slot == kDepth - 1 ? 0 : use_slot + 1;
-  k += kStep;
-  if (k * kBlock < n_tok) continue;
+    --ahead;
+    use_slot = use_slot == kDepth - 1 ? 0 : use_slot + 1;
+    k += kStep;
+    if (k * kBlock < n_tok) continue;
 
-  // ---- end of the unit: sums over the lanes that hold other tokens of the same rows
+    // ---- end of the unit: sums over the lanes that hold other tokens of the same rows
 #pragma unroll
-  for (int d = 4; d < 32; d <<= 1) {
-    l[0] += __shfl_xor_sync(0xffffffffu, l[0], d);
-    l[1] += __shfl_xor_sync(0xffffffffu, l[1], d);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      lsum[j][0] += __shfl_xor_sync(0xffffffffu, lsum[j][0], d);
-      lsum[j][1] += __shfl_xor_sync(0xffffffffu, lsum[j][1], d);
-    }
-  }
-  if (narrow) {                  // row r over the first blocks and over the second ones: lanes q and q ^ 2
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const float other = __shfl_xor_sync(0xffffffffu, ref[e], 2);
-      const float m = fmaxf(ref[e], other);
-      const float f = ref[e] == m ? 1.f : ex2(ref[e] - m);   // (no second block: kNoRef and zeros)
-      ref[e] = m;
-      l[e] *= f;
-      l[e] += __shfl_xor_sync(0xffffffffu, l[e], 2);
+    for (int d = 4; d < 32; d <<= 1) {
+      l[0] += __shfl_xor_sync(0xffffffffu, l[0], d);
+      l[1] += __shfl_xor_sync(0xffffffffu, l[1], d);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        lsum[j][e] *= f;
-        lsum[j][e] += __shfl_xor_sync(0xffffffffu, lsum[j][e], 2);
-      }
-#pragma unroll
-      for (int m8 = 0; m8 < 8; ++m8) {
-        o[m8][e] *= f;
-        o[m8][e] += __shfl_xor_sync(0xffffffffu, o[m8][e], 2);
-        o[m8][2 + e] *= f;
-        o[m8][2 + e] += __shfl_xor_sync(0xffffffffu, o[m8][2 + e], 2);
+        lsum[j][0] += __shfl_xor_sync(0xffffffffu, lsum[j][0], d);
+        lsum[j][1] += __shfl_xor_sync(0xffffffffu, lsum[j][1], d);
       }
     }
-  }
-  // ---- row 2 q + e: dims 32 j + 4 g .. + 3, to the output or to a partial result
-  const int* h = hdr(c_seq);
+    if (kNarrow) {               // row r over the first blocks and over the second: lanes q and q ^ 2
 #pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    const int r = 2 * q + e;
-    if (r >= rows) continue;
-    constexpr float kLow = 1.f / kCodeUnit, kHigh = kLow / 16.f;   // (odd nibbles counted 16 times)
-    const int head = h[H_KVH] * G + (h[H_R0] + r) % G;
-    const int query = h[H_QUERY + r], slot = h[H_SLOT + r];
-    const float inv = slot < 0 ? 1.f / l[e] : 1.f;
-    const size_t prow = (size_t)(slot + h[H_ADD]) * HQ + head;
+      for (int e = 0; e < 2; ++e) {
+        const float other = __shfl_xor_sync(0xffffffffu, ref[e], 2);
+        const float m = fmaxf(ref[e], other);
+        const float f = ref[e] == m ? 1.f : ex2(ref[e] - m);   // (no second block: kNoRef and zeros)
+        ref[e] = m;
+        l[e] *= f;
+        l[e] += __shfl_xor_sync(0xffffffffu, l[e], 2);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float4 v = make_float4(fmaf(o[2 * j][e], kLow, lsum[j][e]) * inv,
-                                   fmaf(o[2 * j][2 + e], kHigh, lsum[j][e]) * inv,
-                                   fmaf(o[2 * j + 1][e], kLow, lsum[j][e]) * inv,
-                                   fmaf(o[2 * j + 1][2 + e], kHigh, lsum[j][e]) * inv);
-      if (slot < 0)
-        *(uint2*)((__nv_bfloat16*)a.out + ((size_t)query * HQ + head) * kDim + 32 * j + 4 * g) =
-            make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
-      else
-        *(float4*)(a.part_o + prow * kDim + 32 * j + 4 * g) = v;
+        for (int j = 0; j < 4; ++j) {
+          lsum[j][e] *= f;
+          lsum[j][e] += __shfl_xor_sync(0xffffffffu, lsum[j][e], 2);
+        }
+#pragma unroll
+        for (int m8 = 0; m8 < 8; ++m8)
+#pragma unroll
+          for (int x = e; x < 4; x += 2) {
+            o[m8][x] *= f;
+            o[m8][x] += __shfl_xor_sync(0xffffffffu, o[m8][x], 2);
+          }
+      }
     }
-    if (slot >= 0 && g == 0) a.part_ml[prow] = make_float2(ref[e], l[e]);
+    // ---- row 2 q + e: dims 32 j + 4 g .. + 3, to the output or to a partial result
+    const int* h = hdr(c_seq);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int r = 2 * q + e;
+      if (r >= rows) continue;
+      constexpr float kLow = 1.f / kCodeUnit, kHigh = kLow / 16.f;   // (odd nibbles counted 16 times)
+      const int head = h[H_KVH] * G + (h[H_R0] + r) % G;
+      const int query = h[H_QUERY + r], slot = h[H_SLOT + r];
+      const float inv = slot < 0 ? 1.f / l[e] : 1.f;
+      const size_t prow = (size_t)(slot + h[H_ADD]) * HQ + head;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float4 v = make_float4(fmaf(o[2 * j][e], kLow, lsum[j][e]) * inv,
+                                     fmaf(o[2 * j][2 + e], kHigh, lsum[j][e]) * inv,
+                                     fmaf(o[2 * j + 1][e], kLow, lsum[j][e]) * inv,
+                                     fmaf(o[2 * j + 1][2 + e], kHigh, lsum[j][e]) * inv);
+        if (slot < 0)
+          *(uint2*)((__nv_bfloat16*)a.out + ((size_t)query * HQ + head) * kDim + 32 * j + 4 * g) =
+              make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
+        else
+          *(float4*)(a.part_o + prow * kDim + 32 * j + 4 * g) = v;
+      }
+      if (slot >= 0 && g == 0) a.part_ml[prow] = make_float2(ref[e], l[e]);
+    }
+    ++c_seq;
+    k = 0;
   }
-  ++c_seq;
-  k = 0;
-  }
+}
+
+__global__ void __launch_bounds__(32 * kWarps, 1)
+attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  stream_units<false>(a, grid, smem);
+  __syncwarp();
+  stream_units<true>(a, grid, smem);
 }
 
 // Candidate tokens of a verification: as verify_tail_kernel, rows read from the 4-bit pool.
@@ -605,10 +632,10 @@ __global__ void __launch_bounds__(128) q4_verify_tail_kernel(const AttnArgs a,
       float t = 0.f, vf[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
       if (on) {
         const int pos = d.base + i;
-        const size_t row = (((size_t)table[pos >> 4] * HKV + kvh) * kBlock + (pos & (kBlock - 1)));
+        const size_t tile = ((size_t)table[pos >> 4] * HKV + kvh) * kQ4TileBytes;
         float kf[8];
-        q4_load8_k((const uint8_t*)a.k_pool + row * kQ4RowBytes, c, kf);
-        q4_load8_v((const uint8_t*)a.v_pool + row * kQ4RowBytes, c, vf);
+        q4_load8_k((const uint8_t*)a.k_pool + tile, pos & (kBlock - 1), c, kf);
+        q4_load8_v((const uint8_t*)a.v_pool + tile, pos & (kBlock - 1), c, vf);
 #pragma unroll
         for (int x = 0; x < 8; ++x) t = fmaf(qf[x], kf[x], t);
       }
@@ -647,22 +674,25 @@ __global__ void __launch_bounds__(128) q4_verify_tail_kernel(const AttnArgs a,
 
 }  // namespace
 
-cudaError_t launch_attention_q4(const AttnArgs& a, const int32_t n_items[4],
-                                const int32_t max_rows[4], cudaStream_t st) {
-  // classes as the planner orders them: items of 4, 3, 2 and 1 tiles of 16 rows
+cudaError_t launch_attention_q4(const AttnArgs& a, const Q4Items& it, cudaStream_t st) {
+  // classes as the planner orders them: items of 4, 3, 2 and 1 tiles of 16 rows, narrow ones last
   Q4Grid g;
   int64_t units = 0;
   int items = 0;
   for (int k = 0; k < 4; ++k) {
-    const int n = n_items[3 - k];
-    g.tiles[k] = std::max(1, (max_rows[3 - k] + kRows - 1) / kRows);
+    const int n = it.n_items[3 - k];
+    g.tiles[k] = std::max(1, (it.max_rows[3 - k] + kRows - 1) / kRows);
     g.item_begin[k] = items;
     items += n;
     units += (int64_t)n * g.tiles[k] * a.shape.num_kv_heads;
     if (units > INT32_MAX - (1 << 20)) return cudaErrorInvalidValue;
     g.unit_end[k] = (int32_t)units;
   }
-  if (units == 0) return cudaSuccess;
+  const int64_t narrow = (int64_t)it.n_narrow * a.shape.num_kv_heads;
+  if (narrow > INT32_MAX - (1 << 20)) return cudaErrorInvalidValue;
+  g.narrow_begin = items;
+  g.narrow_units = (int32_t)narrow;
+  if (units + narrow == 0) return cudaSuccess;
   static bool configured[64] = {};
   int dev = 0;
   cudaGetDevice(&dev);
@@ -673,7 +703,7 @@ cudaError_t launch_attention_q4(const AttnArgs& a, const int32_t n_items[4],
     if (e != cudaSuccess) return e;
     configured[dev] = true;
   }
-  const int ctas = (int)std::min<int64_t>(units, a.num_sms);
+  const int ctas = (int)std::min<int64_t>(units + narrow, a.num_sms);
   attn_q4_kernel<<<ctas, 32 * kWarps, kSmemQ4, st>>>(a, g);
   return cudaGetLastError();
 }

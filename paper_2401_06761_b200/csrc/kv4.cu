@@ -11,24 +11,13 @@ namespace apar {
 namespace {
 
 // ------------------------------------------------------------------ append: quantise and scatter
+struct Q4Group {          // one lane's share of a row: eight codes and its group's scale word
+  uint32_t codes, scale;
+};
+
 // Sixteen lanes hold one row, eight dims (16 bytes) each; the four lanes of a group find its
-// range with two shuffles.  The kernel reads 256 bytes and writes 80 for each row and is bound by
-// HBM for prompts, by its launch for decode steps.
-__global__ void __launch_bounds__(256) q4_append_kernel(uint8_t* __restrict__ k_pool,
-                                                        uint8_t* __restrict__ v_pool,
-                                                        const uint4* __restrict__ k_new,
-                                                        const uint4* __restrict__ v_new,
-                                                        const int32_t* __restrict__ slots,
-                                                        long long first_row, int n_rows,
-                                                        int num_kv_heads) {
-  const long long idx = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-  const long long rh = idx >> 4;                       // (row, head)
-  const int c = (int)idx & 15;
-  const bool on = rh < (long long)n_rows * num_kv_heads;
-  const bool is_v = blockIdx.y != 0;
-  const int r = on ? (int)(rh / num_kv_heads) : 0, h = on ? (int)(rh % num_kv_heads) : 0;
-  uint4 x = make_uint4(0u, 0u, 0u, 0u);
-  if (on) x = __ldg((is_v ? v_new : k_new) + ((first_row + r) * num_kv_heads + h) * 16 + c);
+// range with two shuffles.  Nibble order of the codes: K e / 2 + 4 (e & 1), V e.
+__device__ __forceinline__ Q4Group q4_quantise(const uint4& x, bool is_v) {
   const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
   float f[8];
 #pragma unroll
@@ -36,7 +25,7 @@ __global__ void __launch_bounds__(256) q4_append_kernel(uint8_t* __restrict__ k_
     f[2 * e] = bf16_lo(xs[e]);
     f[2 * e + 1] = bf16_hi(xs[e]);
   }
-  // range of the group; the NaN-propagating minimum lets a NaN reach s
+  // the NaN-propagating minimum lets a NaN reach the scale
   __nv_bfloat162 mn = *(__nv_bfloat162*)&xs[0], mx = mn;
 #pragma unroll
   for (int e = 1; e < 4; ++e) {
@@ -68,29 +57,64 @@ __global__ void __launch_bounds__(256) q4_append_kernel(uint8_t* __restrict__ k_
     const float q = d * inv;
     const float t = fmaf(fmaf(-q, s, d), inv, q);
     const uint32_t code = (uint32_t)__float_as_int(t + 12582912.f) & 15u;
-    // K: nibble e / 2 + 4 (e & 1); V: nibble e
     w |= code << (is_v ? 4 * e : 4 * ((e >> 1) + 4 * (e & 1)));
   }
-  if (bad) w = 0;
-  const int G = c >> 2, xq = c & 3;
-  if (is_v) {
-    // 16-bit pieces: this lane holds, for its group G, pieces 2 xq (low half) and 2 xq + 1; it
-    // ends up with two groups of one piece, i.e. the word at 16 xq + 4 G
-    const int base = (threadIdx.x & 16) + xq + 8 * (G & 1);
-    const uint32_t a = __shfl_sync(0xffffffffu, w, base);
-    const uint32_t b = __shfl_sync(0xffffffffu, w, base + 4);
-    w = __byte_perm(a, b, (G & 2) ? 0x7632 : 0x5410);
-  }
-  if (!on) return;
+  // (a NaN scale carries the sign bit: integer comparisons of scales rank it below all others)
+  if (bad) return Q4Group{0u, 0xffc0ffc0u};
+  return Q4Group{w, (__float_as_uint(s) >> 16) | (__float_as_uint(lo) & 0xffff0000u)};
+}
+
+// Two rows that are neighbours in the pool, an even one and the odd one after it, are written by
+// the sixteen lanes of the first, so that the pair's interleaved V codes leave as whole words;
+// the lanes of the second have nothing to do.  The kernel reads 256 bytes and writes 80 for each
+// row and is bound by HBM for prompts, by its launch for decode steps.
+__global__ void __launch_bounds__(256) q4_append_kernel(uint8_t* __restrict__ k_pool,
+                                                        uint8_t* __restrict__ v_pool,
+                                                        const uint4* __restrict__ k_new,
+                                                        const uint4* __restrict__ v_new,
+                                                        const int32_t* __restrict__ slots,
+                                                        long long first_row, int n_rows,
+                                                        int num_kv_heads) {
+  const long long idx = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+  const long long rh = idx >> 4;                       // (row, head)
+  const int c = (int)idx & 15;
+  const bool is_v = blockIdx.y != 0;
+  bool on = rh < (long long)n_rows * num_kv_heads;
+  const int r = on ? (int)(rh / num_kv_heads) : 0, h = on ? (int)(rh % num_kv_heads) : 0;
   const int slot = slots[r];
-  uint8_t* row = (is_v ? v_pool : k_pool) +
-                 (((size_t)(slot >> 4) * num_kv_heads + h) * kBlock + (slot & 15)) * kQ4RowBytes;
-  *(uint32_t*)(row + xq * 16 + G * 4) = w;
-  if (xq == 0) {
-    // (a NaN scale carries the sign bit: integer comparisons of scales rank it below all others)
-    const uint32_t lo_bits = __float_as_uint(lo) >> 16;
-    *(uint32_t*)(row + kQ4CodeBytes + 4 * G) =
-        bad ? 0xffc0ffc0u : (__float_as_uint(s) >> 16) | (lo_bits << 16);
+  const bool pair = on && !(slot & 1) && r + 1 < n_rows && slots[r + 1] == slot + 1;
+  if ((slot & 1) && r > 0 && slots[r - 1] == slot - 1) on = false;
+  if (!__any_sync(0xffffffffu, on)) return;
+  const uint4* src = (is_v ? v_new : k_new) + ((first_row + r) * num_kv_heads + h) * 16 + c;
+  uint4 x0 = make_uint4(0u, 0u, 0u, 0u), x1 = x0;
+  if (on) x0 = __ldg(src);
+  if (pair) x1 = __ldg(src + (size_t)num_kv_heads * 16);
+  const Q4Group a = q4_quantise(x0, is_v), b = q4_quantise(x1, is_v);
+  if (!on) return;
+  uint8_t* tile = (is_v ? v_pool : k_pool) +
+                  ((size_t)(slot >> 4) * num_kv_heads + h) * kQ4TileBytes;
+  const int off = slot & 15, G = c >> 2, x = c & 3;
+  if (is_v) {
+    uint8_t* p = tile + q4_v_piece(off, 2 * x, G);     // pieces 2 x (low half) and 2 x + 1
+    if (pair) {
+      *(uint32_t*)p = __byte_perm(a.codes, b.codes, 0x5410);
+      *(uint32_t*)(p + 16) = __byte_perm(a.codes, b.codes, 0x7632);
+    } else {
+      *(uint16_t*)p = (uint16_t)a.codes;
+      *(uint16_t*)(p + 16) = (uint16_t)(a.codes >> 16);
+    }
+    if (x == 0) {
+      *(uint32_t*)(tile + q4_v_scales(off) + 4 * G) = a.scale;
+      if (pair) *(uint32_t*)(tile + q4_v_scales(off + 1) + 4 * G) = b.scale;
+    }
+  } else {
+    uint8_t* row = tile + off * kQ4RowBytes;
+    *(uint32_t*)(row + x * 16 + G * 4) = a.codes;
+    if (pair) *(uint32_t*)(row + kQ4RowBytes + x * 16 + G * 4) = b.codes;
+    if (x == 0) {
+      *(uint32_t*)(row + kQ4CodeBytes + 4 * G) = a.scale;
+      if (pair) *(uint32_t*)(row + kQ4RowBytes + kQ4CodeBytes + 4 * G) = b.scale;
+    }
   }
 }
 
@@ -104,28 +128,37 @@ __global__ void __launch_bounds__(96) q4_cow_copy_kernel(uint4* __restrict__ k_p
   const size_t tile = kQ4TileBytes / 16;
   const uint4* src = pool + ((size_t)c.src_block * num_kv_heads + blockIdx.y) * tile;
   uint4* dst = pool + ((size_t)c.dst_block * num_kv_heads + blockIdx.y) * tile;
-  for (int i = threadIdx.x; i < c.rows * kQ4RowVec; i += blockDim.x) dst[i] = src[i];
+  // (V rows lie in pairs: the partner of an odd last row is copied along, unspecified as it is)
+  const int rows = blockIdx.z ? (c.rows + 1) & ~1 : c.rows;
+  for (int i = threadIdx.x; i < rows * kQ4RowVec; i += blockDim.x) dst[i] = src[i];
 }
 
 // ------------------------------------------------------------------ accepted candidates: row moves
-// As row_move_kernel: every source row of a group is read before the first one is written.
-__global__ void __launch_bounds__(160) q4_row_move_kernel(uint4* __restrict__ k_pool,
-                                                          uint4* __restrict__ v_pool,
+// As row_move_kernel: every source row of a group is read before the first one is written.  A
+// row is 32 pieces of 16 bits and 16 bytes of scales, which holds for K and V rows alike.
+__global__ void __launch_bounds__(256) q4_row_move_kernel(uint8_t* __restrict__ k_pool,
+                                                          uint8_t* __restrict__ v_pool,
                                                           const RowMove* __restrict__ moves,
                                                           const int32_t* __restrict__ group_begin,
                                                           int num_kv_heads) {
-  __shared__ uint4 rows[64 * kQ4RowVec];
+  __shared__ uint16_t rows[64 * kQ4RowBytes / 2];
+  constexpr int kPieces = kQ4RowBytes / 2, kCodes = kQ4CodeBytes / 2;
   const int m0 = group_begin[blockIdx.x], n = group_begin[blockIdx.x + 1] - m0;
-  uint4* pool = blockIdx.z ? v_pool : k_pool;
+  const bool is_v = blockIdx.z != 0;
+  uint8_t* pool = is_v ? v_pool : k_pool;
   const int h = blockIdx.y;
-  auto at = [&](int slot, int x) {
-    return (((size_t)(slot >> 4) * num_kv_heads + h) * kBlock + (slot & 15)) * kQ4RowVec + x;
+  auto at = [&](int slot, int i) {
+    uint8_t* tile = pool + ((size_t)(slot >> 4) * num_kv_heads + h) * kQ4TileBytes;
+    const int off = slot & 15;
+    if (!is_v) return (uint16_t*)(tile + off * kQ4RowBytes) + i;
+    if (i >= kCodes) return (uint16_t*)(tile + q4_v_scales(off)) + (i - kCodes);
+    return (uint16_t*)(tile + q4_v_piece(off, i >> 2, i & 3));
   };
-  for (int x = threadIdx.x; x < n * kQ4RowVec; x += blockDim.x)
-    rows[x] = pool[at(moves[m0 + x / kQ4RowVec].src_slot, x % kQ4RowVec)];
+  for (int x = threadIdx.x; x < n * kPieces; x += blockDim.x)
+    rows[x] = *at(moves[m0 + x / kPieces].src_slot, x % kPieces);
   __syncthreads();
-  for (int x = threadIdx.x; x < n * kQ4RowVec; x += blockDim.x)
-    pool[at(moves[m0 + x / kQ4RowVec].dst_slot, x % kQ4RowVec)] = rows[x];
+  for (int x = threadIdx.x; x < n * kPieces; x += blockDim.x)
+    *at(moves[m0 + x / kPieces].dst_slot, x % kPieces) = rows[x];
 }
 
 // ------------------------------------------------------------------ rows read back as bf16
@@ -145,13 +178,13 @@ __global__ void __launch_bounds__(256) read_rows_kernel(const uint8_t* __restric
   const int c = (int)idx & 15;
   const int r = (int)(rh / num_kv_heads), h = (int)(rh % num_kv_heads);
   const int slot = slots[r];
-  const size_t row = ((size_t)(slot >> 4) * num_kv_heads + h) * kBlock + (slot & 15);
+  const size_t tile = (size_t)(slot >> 4) * num_kv_heads + h;
   const uint8_t* pool = blockIdx.y ? v_pool : k_pool;
   uint4 out;
   if (kQ4) {
     float f[8];
-    if (blockIdx.y) q4_load8_v(pool + row * kQ4RowBytes, c, f);
-    else q4_load8_k(pool + row * kQ4RowBytes, c, f);
+    if (blockIdx.y) q4_load8_v(pool + tile * kQ4TileBytes, slot & 15, c, f);
+    else q4_load8_k(pool + tile * kQ4TileBytes, slot & 15, c, f);
     uint32_t w[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -160,7 +193,7 @@ __global__ void __launch_bounds__(256) read_rows_kernel(const uint8_t* __restric
     }
     out = make_uint4(w[0], w[1], w[2], w[3]);
   } else {
-    out = ((const uint4*)pool)[row * 16 + c];
+    out = ((const uint4*)pool)[(tile * kBlock + (slot & 15)) * 16 + c];
   }
   (blockIdx.y ? v_out : k_out)[(first_row * num_kv_heads + rh) * 16 + c] = out;
 }
@@ -190,8 +223,8 @@ cudaError_t launch_q4_row_moves(void* k_pool, void* v_pool, const RowMove* d_mov
                                 const int32_t* d_group_begin, int n_groups, int num_kv_heads,
                                 cudaStream_t st) {
   if (n_groups <= 0) return cudaSuccess;
-  q4_row_move_kernel<<<dim3(n_groups, num_kv_heads, 2), 160, 0, st>>>(
-      (uint4*)k_pool, (uint4*)v_pool, d_moves, d_group_begin, num_kv_heads);
+  q4_row_move_kernel<<<dim3(n_groups, num_kv_heads, 2), 256, 0, st>>>(
+      (uint8_t*)k_pool, (uint8_t*)v_pool, d_moves, d_group_begin, num_kv_heads);
   return cudaGetLastError();
 }
 
