@@ -413,8 +413,9 @@ apar_status launch_plan(apar_ctx* c, int layer, const void* q, void* out, float 
       ++*launches_out;
     }
     if (!p.merges.empty()) {
-      APAR_CUDA(c, launch_merge(a, (const MergeRef*)c->ws(c->lay.plan_merges),
-                                (int)p.merges.size(), st));
+      a.pdl = c->use_pdl && p.n_mma && c->plan_verify_n == 0;   // (directly after the attention)
+      APAR_CUDA(c, launch_q4_merge(a, (const MergeRef*)c->ws(c->lay.plan_merges),
+                                   (int)p.merges.size(), c->q4_items.max_parts, st));
       ++*launches_out;
     }
     return APAR_OK;
@@ -507,18 +508,25 @@ apar_status run_attention(apar_ctx* c, int n, const int32_t* qslots, const int32
   if (!tables_in_sync) c->last.attn_upload_bytes = 0;   // (else the caller's uploads count too)
   if (!reuse) {
     const auto t_plan = std::chrono::steady_clock::now();
-    c->pq.resize(n);
+    c->pq.clear();
     // every query attends its thread's whole chain and no thread is listed twice: the planner
     // may count per group of blocks instead of per block
     const bool by_runs = cacheable && c->track_runs && c->plan_by_runs;
     for (int i = 0; i < n; ++i) {
-      c->pq[i] = PlanQuery{c->row(qslots[i]), qslots[i],
-                           qlens ? qlens[i] : c->slots[qslots[i]].len};
-      if (by_runs) {
-        c->pq[i].runs = c->runs[qslots[i]].data();
-        c->pq[i].n_runs = (int32_t)c->runs[qslots[i]].size();
+      // on a 4-bit pool the candidates of a thread are planned as one (its kernel takes any number
+      // of rows; the others' plans stay as they are)
+      if (c->q4 && verify && i > 0 && qslots[i] == qslots[i - 1]) {
+        ++c->pq.back().mult;
+        continue;
       }
-      if (verify) c->pq[i].extra_parts = 1;
+      PlanQuery pq{c->row(qslots[i]), qslots[i], qlens ? qlens[i] : c->slots[qslots[i]].len};
+      if (by_runs) {
+        pq.runs = c->runs[qslots[i]].data();
+        pq.n_runs = (int32_t)c->runs[qslots[i]].size();
+      }
+      if (verify) pq.extra_parts = 1;
+      if (c->q4 && verify) pq.first_query = i;
+      c->pq.push_back(pq);
     }
     c->plan_verify_n = 0;
     // Single-row items (no GQA group, private tail): the vector kernel keeps up to 16 CTAs per
@@ -528,7 +536,7 @@ apar_status run_attention(apar_ctx* c, int n, const int32_t* qslots, const int32
     if (c->auto_path && c->shape.group == 1 && n <= kFewQueries) c->plan_min_rows = 1;
     // finishing items land in the single-row vector kernel or the warp-stream kernel
     const bool fuse_final = c->use_ws && c->plan_min_rows <= 2 && !verify && !c->q4;
-    if (!c->planner.build(c->pq.data(), n, c->lay.slot_capacity, cacheable, c->plan_min_rows,
+    if (!c->planner.build(c->pq.data(), (int)c->pq.size(), c->lay.slot_capacity, cacheable, c->plan_min_rows,
                           fuse_final, &c->plan, by_runs))
       return APAR_ERR_WORKSPACE_TOO_SMALL;
     if ((int64_t)c->plan.users.size() > c->lay.entry_capacity ||
@@ -541,6 +549,8 @@ apar_status run_attention(apar_ctx* c, int n, const int32_t* qslots, const int32
           items.begin(), items.end(), [&](const WorkItem& w) { return rows(w) > kQ4NarrowRows; });
       c->q4_items = Q4Items();
       c->q4_items.n_narrow = (int32_t)(items.end() - cut);
+      for (const MergeRef& m : c->plan.merges)
+        c->q4_items.max_parts = std::max(c->q4_items.max_parts, m.n);
       for (auto w = items.begin(); w != cut; ++w) {
         const int k = (rows(*w) + 15) / 16 - 1;
         ++c->q4_items.n_items[k];
@@ -679,7 +689,7 @@ apar_status create_impl(const apar_config* cfg, bool external, bool host_only, i
   if (c->q4) {                       // one kernel takes every item, whatever the switches say
     c->mma_min_rows = 1;
     c->auto_path = false;
-    if (getenv("APAR_Q4_UNITS")) c->planner.set_units_per_sm(atoi(getenv("APAR_Q4_UNITS")));
+    c->planner.set_streams(kQ4Streams, kQ4Rows);
   }
   if (host_only) {
     *out = c;

@@ -224,8 +224,10 @@ cudaError_t launch_read_rows(bool q4, const void* k_pool, const void* v_pool, vo
 // kQ4NarrowRows rows come last: n_items[k] wider items of class k (k + 1 tiles of 16 rows), none
 // of them with more than max_rows[k] rows, and n_narrow narrow ones.
 constexpr int kQ4NarrowRows = 4;
+constexpr int kQ4Rows = 8, kQ4Streams = 12;     // rows of a wide unit; warps per SM
 struct Q4Items {
   int32_t n_items[4] = {0, 0, 0, 0}, max_rows[4] = {0, 0, 0, 0}, n_narrow = 0;
+  int32_t max_parts = 0;            // partial results of the query that has most
 };
 // The units of a launch: wide classes in the planner's order (widest first; the items of a class
 // have the same number of row tiles), then the narrow items.
@@ -234,6 +236,10 @@ struct Q4Grid {
 };
 // Uses no a.tm_k / a.tm_v / a.d_ticket.
 cudaError_t launch_attention_q4(const AttnArgs& a, const Q4Items& items, cudaStream_t st);
+// Merge of partial results; a.pdl: it may be launched before the attention kernel has finished.
+// max_parts: parts of the row that has most.
+cudaError_t launch_q4_merge(const AttnArgs& a, const MergeRef* d_merge, int n_merge, int max_parts,
+                            cudaStream_t st);
 cudaError_t launch_q4_verify_tail(const AttnArgs& a, const VerifyDesc* d_desc, int n_desc,
                                   cudaStream_t st);
 
@@ -260,6 +266,10 @@ struct PlanQuery {
   // candidate tokens of a verification step); a slot is reserved for it (Plan::extra_slot)
   // and the query is merged.  len may then be 0 (nothing but that result).
   int32_t extra_parts = 0;
+  // > 1: this many queries, numbered from first_query on, that attend the same tokens of the same
+  // thread (the candidates of a verification); they share every item.  The merges, slots and
+  // extra_slot entries of a plan are per numbered query.  Only without fuse_final.
+  int32_t mult = 1, first_query = -1;
 };
 
 struct Plan {
@@ -290,22 +300,27 @@ class Planner {
   bool build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_tails,
              int mma_min_rows, bool fuse_final, Plan* out, bool by_runs = false);
   void set_num_sms(int n) { num_sms_ = n > 0 ? n : 148; }
-  // Units (item x kv head) per SM that long runs are cut for.
-  void set_units_per_sm(int n) { units_per_sm_ = n; }
+  // For a kernel whose warps each work through units of their own (an item, a kv head and `rows`
+  // of its query rows): `streams` warps per SM.  Runs are then cut so that the units come out
+  // even over the warps, and a run's chunks are of equal length.
+  void set_streams(int streams, int rows) {
+    streams_ = streams;
+    stream_rows_ = rows;
+  }
 
  private:
   template <bool kRuns>
   void find_segments(const PlanQuery* q, int n, bool open_tails, int64_t* unique,
                      int64_t* attended);
   void ensure_keys(size_t n);
-  int num_blocks_ = 0, group_ = 1, hint_kv_heads_ = 1, num_sms_ = 148,
-      units_per_sm_ = 8;
+  int num_blocks_ = 0, group_ = 1, hint_kv_heads_ = 1, num_sms_ = 148;
+  int streams_ = 0, stream_rows_ = 8;
   uint32_t epoch_ = 0;
   std::vector<uint32_t> stamp_;
   std::vector<int32_t> cnt_, seg_of_;
   std::vector<uint8_t> partial_;
   struct Seg { int32_t table_row, tok_begin, tok_end, n_blocks, n_users, user_off, priv, open; };
-  struct SegUser { int32_t seg, query, ord; };
+  struct SegUser { int32_t seg, query, ord; };   // (query: index of the PlanQuery)
   std::vector<Seg> segs_;
   std::vector<SegUser> seg_users_;
   std::vector<int32_t> n_parts_, qbeg_, part_off_;

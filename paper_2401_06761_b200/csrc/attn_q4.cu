@@ -48,8 +48,8 @@
 namespace apar {
 namespace {
 
-constexpr int kRows = 8;                             // query rows of a unit
-constexpr int kWarps = 12;
+constexpr int kRows = kQ4Rows;                       // query rows of a unit
+constexpr int kWarps = kQ4Streams;
 constexpr int kStep = 2;                             // blocks computed together
 constexpr int kTile = 2 * kQ4TileBytes;              // K and V of one block
 constexpr int kSlot = kStep * kTile;
@@ -598,12 +598,14 @@ __device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Grid& gr
 __global__ void __launch_bounds__(32 * kWarps, 1)
 attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
   extern __shared__ __align__(128) uint8_t smem[];
+  pdl_launch_dependents();
   stream_units<false>(a, grid, smem);
   __syncwarp();
   stream_units<true>(a, grid, smem);
 }
 
-// Candidate tokens of a verification: as verify_tail_kernel, rows read from the 4-bit pool.
+// Candidate tokens of a verification, as verify_tail_kernel, rows read from the 4-bit pool.  The
+// halves of a warp take the set bits of the mask in turn: a candidate of a tree sees few others.
 __global__ void __launch_bounds__(128) q4_verify_tail_kernel(const AttnArgs a,
                                                              const VerifyDesc* __restrict__ descs) {
   const VerifyDesc d = descs[blockIdx.x];
@@ -626,11 +628,17 @@ __global__ void __launch_bounds__(128) q4_verify_tail_kernel(const AttnArgs a,
       }
     }
     float m = -INFINITY, l = 0.f;
-    for (int i0 = 0; i0 < d.n_cand; i0 += 2) {
-      const int i = i0 + half;
-      const bool on = i < d.n_cand && ((d.mask >> i) & 1ull);
+    uint64_t left = d.mask;
+    while (left) {
+      const int i_first = __ffsll((long long)left) - 1;
+      left &= left - 1;
+      const bool two = left != 0;
+      const int i_second = two ? __ffsll((long long)left) - 1 : 0;
+      left &= left - 1;                            // (0 stays 0)
+      const bool on = half == 0 || two, other_on = half == 1 || two;
       float t = 0.f, vf[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
       if (on) {
+        const int i = half ? i_second : i_first;
         const int pos = d.base + i;
         const size_t tile = ((size_t)table[pos >> 4] * HKV + kvh) * kQ4TileBytes;
         float kf[8];
@@ -643,8 +651,6 @@ __global__ void __launch_bounds__(128) q4_verify_tail_kernel(const AttnArgs a,
       for (int x = 8; x; x >>= 1) t += __shfl_xor_sync(0xffffffffu, t, x);
       const float s = on ? t : -INFINITY;
       const float other = __shfl_xor_sync(0xffffffffu, s, 16);
-      const bool other_on = __shfl_xor_sync(0xffffffffu, (int)on, 16) != 0;
-      if (!on && !other_on) continue;              // both tokens masked
       const float mn = fmaxf(m, fmaxf(s, other));
       const float corr = m == -INFINITY ? 0.f : ex2(m - mn);
       const float p = on ? ex2(s - mn) : 0.f;
@@ -672,7 +678,88 @@ __global__ void __launch_bounds__(128) q4_verify_tail_kernel(const AttnArgs a,
   }
 }
 
+// out = sum_j o_j 2^(m_j - M) / sum_j l_j 2^(m_j - M) over the partial results of one (query, head).
+// kWarpsPerRow warps share a row's parts (1: four rows to a CTA); (m, l) and o of up to eight parts
+// are requested together, so that a row of few parts costs one trip to memory.
+template <int kWarpsPerRow>
+__global__ void __launch_bounds__(128) q4_merge_kernel(const AttnArgs a,
+                                                       const MergeRef* __restrict__ merges) {
+  __shared__ float sm_m[4], sm_l[4];
+  __shared__ __align__(16) float sm_o[kWarpsPerRow > 1 ? 4 : 1][kDim];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int HQ = a.shape.num_q_heads;
+  const int head = kWarpsPerRow == 1 ? blockIdx.y * 4 + warp : blockIdx.y;
+  const MergeRef mr = merges[blockIdx.x];
+  pdl_wait();                                        // (the attention launch before this one)
+  if (head >= HQ) return;                            // (whole warps, and only where rows are warps)
+  float M = -INFINITY, L = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int j0 = kWarpsPerRow == 1 ? 0 : warp; j0 < mr.n; j0 += 8 * kWarpsPerRow) {
+    float2 ml[8];
+    float4 o[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int j = j0 + k * kWarpsPerRow;
+      ml[k] = make_float2(-INFINITY, 0.f);
+      o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (j < mr.n) {
+        const size_t prow = (size_t)(mr.slot_begin + j) * HQ + head;
+        ml[k] = a.part_ml[prow];
+        o[k] = ((const float4*)(a.part_o + prow * kDim))[lane];
+      }
+    }
+    float m = M;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) m = fmaxf(m, ml[k].x);
+    const float f = M == -INFINITY ? 0.f : ex2(M - m);
+    M = m;
+    L *= f;
+    acc.x *= f; acc.y *= f; acc.z *= f; acc.w *= f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float w = ml[k].x == -INFINITY ? 0.f : ex2(ml[k].x - m);
+      L = fmaf(ml[k].y, w, L);
+      acc.x = fmaf(o[k].x, w, acc.x); acc.y = fmaf(o[k].y, w, acc.y);
+      acc.z = fmaf(o[k].z, w, acc.z); acc.w = fmaf(o[k].w, w, acc.w);
+    }
+  }
+  if (kWarpsPerRow > 1) {
+    if (lane == 0) {
+      sm_m[warp] = M;
+      sm_l[warp] = L;
+    }
+    *(float4*)&sm_o[warp][4 * lane] = acc;
+    __syncthreads();
+    if (warp > 0) return;
+    const float m = fmaxf(fmaxf(sm_m[0], sm_m[1]), fmaxf(sm_m[2], sm_m[3]));
+    L = 0.f;
+    acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = sm_m[w] == -INFINITY ? 0.f : ex2(sm_m[w] - m);
+      const float4 v = *(const float4*)&sm_o[w][4 * lane];
+      L = fmaf(sm_l[w], f, L);
+      acc.x = fmaf(v.x, f, acc.x); acc.y = fmaf(v.y, f, acc.y);
+      acc.z = fmaf(v.z, f, acc.z); acc.w = fmaf(v.w, f, acc.w);
+    }
+  }
+  const float inv = 1.f / L;
+  *((uint2*)((__nv_bfloat16*)a.out + ((size_t)mr.query * HQ + head) * kDim) + lane) =
+      make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
+}
+
 }  // namespace
+
+cudaError_t launch_q4_merge(const AttnArgs& a, const MergeRef* d_merge, int n_merge, int max_parts,
+                            cudaStream_t st) {
+  if (n_merge <= 0) return cudaSuccess;
+  const int HQ = a.shape.num_q_heads;
+  // One warp takes a row unless the parts of some row need more than one round of its loads.
+  if (max_parts <= 8)
+    return launch_kernel(q4_merge_kernel<1>, dim3(n_merge, (HQ + 3) / 4), dim3(128), 0, st, a.pdl != 0,
+                         a, d_merge);
+  return launch_kernel(q4_merge_kernel<4>, dim3(n_merge, HQ), dim3(128), 0, st, a.pdl != 0, a, d_merge);
+}
 
 cudaError_t launch_attention_q4(const AttnArgs& a, const Q4Items& it, cudaStream_t st) {
   // classes as the planner orders them: items of 4, 3, 2 and 1 tiles of 16 rows, narrow ones last

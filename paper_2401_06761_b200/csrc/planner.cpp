@@ -57,7 +57,7 @@ void Planner::find_segments(const PlanQuery* q, int n, bool open_tails, int64_t*
   int64_t attended = 0;
   for (int i = 0; i < n; ++i) {
     const int ne = n_entries(i);
-    attended += q[i].len;
+    attended += (int64_t)q[i].len * q[i].mult;
     for (int e = 0; e < ne; ++e) {
       const int32_t b = key_of(i, e);
       if (kRuns) ensure_keys((size_t)b + 1);
@@ -115,7 +115,7 @@ void Planner::find_segments(const PlanQuery* q, int n, bool open_tails, int64_t*
         if (!priv0 && seg_of_[b0] < 0) seg_of_[b0] = s;
         unique += t1 - t0;
       }
-      ++segs_[s].n_users;
+      segs_[s].n_users += q[i].mult;
       seg_users_.push_back(SegUser{s, i, 0});
       e0 = e1;
     }
@@ -137,7 +137,39 @@ bool Planner::build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_
 
   // ---- chunk length: enough items to fill the machine, never below 128 tokens
   const int64_t kInf = (int64_t)1 << 40;
-  int64_t chunk = std::max<int64_t>(128, round_up16(unique * hint_kv_heads_ / (num_sms_ * units_per_sm_)));
+  int64_t chunk = std::max<int64_t>(128, round_up16(unique * hint_kv_heads_ / (num_sms_ * 8)));
+  if (streams_) {
+    // The fewest chunks that give every warp a unit and none a second one; with more units than
+    // warps from the start, no unit longer than a warp's even share.
+    const int64_t warps = (int64_t)num_sms_ * streams_;
+    auto units_of = [&](const Seg& g) {
+      const int64_t full = g.n_users / std::max(1, kMaxRowsPerItem / group_);
+      const int64_t rest = g.n_users % std::max(1, kMaxRowsPerItem / group_);
+      auto tiles = [&](int64_t users) { return (users * group_ + stream_rows_ - 1) / stream_rows_; };
+      return (full * tiles(std::max(1, kMaxRowsPerItem / group_)) + tiles(rest)) * hint_kv_heads_;
+    };
+    int64_t uncut = 0, work = 0, longest = 0;
+    for (const Seg& g : segs_) {
+      uncut += units_of(g);
+      work += units_of(g) * (g.tok_end - g.tok_begin);
+      longest = std::max<int64_t>(longest, g.tok_end - g.tok_begin);
+    }
+    chunk = std::max<int64_t>(128, round_up16(work / warps));
+    if (uncut <= warps) {
+      auto count = [&](int64_t ck) {
+        int64_t u = 0;
+        for (const Seg& g : segs_) u += units_of(g) * ((g.tok_end - g.tok_begin + ck - 1) / ck);
+        return u;
+      };
+      int64_t lo = chunk / 16, hi = std::max(chunk, round_up16(longest)) / 16;   // blocks; hi fits
+      while (lo < hi) {
+        const int64_t mid = (lo + hi) / 2;
+        if (count(mid * 16) <= warps) hi = mid;
+        else lo = mid + 1;
+      }
+      chunk = lo * 16;
+    }
+  }
   // `chunk` is sized for the kernels that keep a CTA's loads in flight through TMA rings.  The
   // single-row kernel has no such staging and needs several CTAs per SM to cover the latency:
   // when its runs, dealt out four kv heads to a CTA, would give fewer than four CTAs per SM,
@@ -157,6 +189,10 @@ bool Planner::build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_
   }
   auto seg_chunk = [&](const Seg& g) -> int64_t {
     if (chunk >= kInf) return kInf;
+    if (streams_) {
+      const int64_t len = std::max(1, g.tok_end - g.tok_begin), pieces = (len + chunk - 1) / chunk;
+      return round_up16((len + pieces - 1) / pieces);
+    }
     if (vec_div == 1 || !single_row(g)) return chunk;
     return std::max<int64_t>(128, round_up16(chunk / vec_div));
   };
@@ -174,7 +210,7 @@ bool Planner::build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_
       }
       ord += q[i].extra_parts;        // results the caller computes itself (see PlanQuery)
       n_parts_[i] = ord;
-      if (ord >= 2) total_slots += ord;
+      if (ord >= 2) total_slots += (int64_t)ord * q[i].mult;
     }
     if (total_slots <= slot_capacity) break;
     if (chunk >= kInf) return false;
@@ -183,7 +219,10 @@ bool Planner::build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_
 
   // ---- partial slots and merges
   out->merges.clear();
-  out->extra_slot.assign(n, -1);
+  int n_numbered = 0;                    // queries, each entry of q counted mult times
+  for (int i = 0; i < n; ++i) n_numbered += q[i].mult;
+  auto number = [&](int i) { return q[i].first_query >= 0 ? q[i].first_query : i; };
+  out->extra_slot.assign(n_numbered, -1);
   part_off_.assign(n, -1);
   int32_t off = 0;
   fused_.assign(n, 0);
@@ -197,9 +236,11 @@ bool Planner::build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_
           q[i].extra_parts == 0)
         fused_[i] = 1;
       // the caller's own partial result takes the last slot of the query
-      if (q[i].extra_parts) out->extra_slot[i] = off + n_parts_[i] - 1;
-      if (!fused_[i]) out->merges.push_back(MergeRef{i, off, n_parts_[i], 0});
-      off += n_parts_[i];
+      for (int m = 0; m < q[i].mult; ++m) {
+        if (q[i].extra_parts) out->extra_slot[number(i) + m] = off + n_parts_[i] - 1;
+        if (!fused_[i]) out->merges.push_back(MergeRef{number(i) + m, off, n_parts_[i], 0});
+        off += n_parts_[i];
+      }
     }
   }
   // ---- users grouped by segment
@@ -209,11 +250,13 @@ bool Planner::build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_
     uo += g.n_users;
     g.n_users = 0;
   }
-  out->users.resize(seg_users_.size());
+  out->users.resize(uo);
   for (const SegUser& su : seg_users_) {
     Seg& g = segs_[su.seg];
-    out->users[g.user_off + g.n_users++] =
-        UserRef{su.query, part_off_[su.query] >= 0 ? part_off_[su.query] + su.ord : -1};
+    const int i = su.query;
+    for (int m = 0; m < q[i].mult; ++m)
+      out->users[g.user_off + g.n_users++] =
+          UserRef{number(i) + m, part_off_[i] >= 0 ? part_off_[i] + m * n_parts_[i] + su.ord : -1};
   }
   // ---- items
   vec_items_.clear();
@@ -239,7 +282,7 @@ bool Planner::build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_
         it.fin_n = it.fin_begin = 0;
         const int rows = nu * group_;
         const bool to_mma = rows >= mma_min_rows;
-        if (g.priv && g.n_users == 1 && c == n_chunks - 1) {
+        if (fuse_final && g.priv && g.n_users == 1 && c == n_chunks - 1) {
           // private runs hold exactly one query; is this the end of a fused query's chain?
           const int qi = out->users[g.user_off].query;
           if (fused_[qi] && g.tok_end == q[qi].len) {
