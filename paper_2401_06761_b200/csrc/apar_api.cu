@@ -403,8 +403,14 @@ apar_status launch_plan(apar_ctx* c, int layer, const void* q, void* out, float 
   // 10-25 % when its finishing items started early (configs 2 and 3), so it and the merge are
   // launched the ordinary way, which also orders them after everything before them.
   if (c->q4) {
-    if (p.n_mma) {
-      APAR_CUDA(c, launch_attention_q4(a, c->q4_items, st));
+    const Q4Items& it = c->q4_items;
+    if (it.n_wide) {
+      APAR_CUDA(c, launch_attention_q4_wide(a, 0, it.n_wide, st));
+      ++*launches_out;
+    }
+    if (it.n_mid + it.n_narrow) {
+      a.pdl = c->use_pdl && it.n_wide;
+      APAR_CUDA(c, launch_attention_q4(a, it, st));
       ++*launches_out;
     }
     if (c->plan_verify_n > 0) {
@@ -545,17 +551,16 @@ apar_status run_attention(apar_ctx* c, int n, const int32_t* qslots, const int32
     if (c->q4) {
       std::vector<WorkItem>& items = c->plan.items;
       auto rows = [&](const WorkItem& w) { return w.n_users * c->shape.group; };
-      const auto cut = std::stable_partition(
-          items.begin(), items.end(), [&](const WorkItem& w) { return rows(w) > kQ4NarrowRows; });
+      const auto mid = std::stable_partition(
+          items.begin(), items.end(), [&](const WorkItem& w) { return rows(w) > kQ4Rows; });
+      const auto narrow = std::stable_partition(
+          mid, items.end(), [&](const WorkItem& w) { return rows(w) > kQ4NarrowRows; });
       c->q4_items = Q4Items();
-      c->q4_items.n_narrow = (int32_t)(items.end() - cut);
+      c->q4_items.n_wide = (int32_t)(mid - items.begin());
+      c->q4_items.n_mid = (int32_t)(narrow - mid);
+      c->q4_items.n_narrow = (int32_t)(items.end() - narrow);
       for (const MergeRef& m : c->plan.merges)
         c->q4_items.max_parts = std::max(c->q4_items.max_parts, m.n);
-      for (auto w = items.begin(); w != cut; ++w) {
-        const int k = (rows(*w) + 15) / 16 - 1;
-        ++c->q4_items.n_items[k];
-        c->q4_items.max_rows[k] = std::max(c->q4_items.max_rows[k], rows(*w));
-      }
     }
     c->last.attn_plan_host_us = std::chrono::duration_cast<std::chrono::microseconds>(
                                     std::chrono::steady_clock::now() - t_plan).count();

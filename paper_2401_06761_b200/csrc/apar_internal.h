@@ -220,21 +220,20 @@ cudaError_t launch_q4_row_moves(void* k_pool, void* v_pool, const RowMove* d_mov
 cudaError_t launch_read_rows(bool q4, const void* k_pool, const void* v_pool, void* k_out,
                              void* v_out, const int32_t* d_slots, int64_t first_row, int n_rows,
                              int num_kv_heads, cudaStream_t st);
-// The items of a plan made with mma_min_rows = 1, reordered so that those with at most
-// kQ4NarrowRows rows come last: n_items[k] wider items of class k (k + 1 tiles of 16 rows), none
-// of them with more than max_rows[k] rows, and n_narrow narrow ones.
-constexpr int kQ4NarrowRows = 4;
-constexpr int kQ4Rows = 8, kQ4Streams = 12;     // rows of a wide unit; warps per SM
+// The items of a plan made with mma_min_rows = 1, reordered by width: n_wide with more than kQ4Rows
+// rows (tcgen05 kernel), n_mid, n_narrow with at most kQ4NarrowRows (both warp-stream kernel).
+constexpr int kQ4Rows = 8, kQ4NarrowRows = 4;
+constexpr int kQ4Streams = 12;      // warps per SM of the warp-stream kernel
 struct Q4Items {
-  int32_t n_items[4] = {0, 0, 0, 0}, max_rows[4] = {0, 0, 0, 0}, n_narrow = 0;
+  int32_t n_wide = 0, n_mid = 0, n_narrow = 0;
   int32_t max_parts = 0;            // partial results of the query that has most
 };
-// The units of a launch: wide classes in the planner's order (widest first; the items of a class
-// have the same number of row tiles), then the narrow items.
-struct Q4Grid {
-  int32_t unit_end[4], item_begin[4], tiles[4], narrow_begin, narrow_units;
+struct Q4Units {                    // (an item and a kv head each)
+  int32_t mid_begin, mid_units, narrow_begin, narrow_units;
 };
-// Uses no a.tm_k / a.tm_v / a.d_ticket.
+// Both use no a.tm_k / a.tm_v / a.d_ticket.  a.pdl: the launch may start before the wide one
+// directly before it has finished.
+cudaError_t launch_attention_q4_wide(const AttnArgs& a, int item_begin, int n_items, cudaStream_t st);
 cudaError_t launch_attention_q4(const AttnArgs& a, const Q4Items& items, cudaStream_t st);
 // Merge of partial results; a.pdl: it may be launched before the attention kernel has finished.
 // max_parts: parts of the row that has most.
@@ -300,9 +299,9 @@ class Planner {
   bool build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_tails,
              int mma_min_rows, bool fuse_final, Plan* out, bool by_runs = false);
   void set_num_sms(int n) { num_sms_ = n > 0 ? n : 148; }
-  // For a kernel whose warps each work through units of their own (an item, a kv head and `rows`
-  // of its query rows): `streams` warps per SM.  Runs are then cut so that the units come out
-  // even over the warps, and a run's chunks are of equal length.
+  // For the kernels of 4-bit pools: items of up to `rows` query rows are units of single warps,
+  // `streams` of them per SM; wider ones count double (measured time per token and kv head).
+  // Runs are cut so that the work comes out even, a run's chunks of equal length.
   void set_streams(int streams, int rows) {
     streams_ = streams;
     stream_rows_ = rows;

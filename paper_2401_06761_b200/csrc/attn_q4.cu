@@ -1,6 +1,7 @@
-// Tree attention over a KV pool held in 4 bits (layout: kv4.cuh).
+// Tree attention over a KV pool held in 4 bits (layout: kv4.cuh) for work items with at most eight
+// query rows; wider ones go to attn_q4_wide.cu.
 //
-// A unit is eight query rows of one work item and one kv head.  Twelve warps per SM each work
+// A unit is one work item and one kv head.  Twelve warps per SM each work
 // through units of their own, from first to last block, with no barrier between them: a warp
 // streams the tiles of its blocks (K and V of one block: 2560 bytes) through a private ring with
 // cp.async, and the copies run ahead *across* units - the next unit's description, query rows and
@@ -114,7 +115,7 @@ __device__ __forceinline__ uint2 lds64(uint32_t a) {
 }
 
 // words of a unit description; query and slot of row r at H_QUERY + r, H_SLOT + r
-enum { H_ROW = 0, H_BEGIN = 1, H_TOK = 2, H_NUSERS = 4, H_ADD = 5, H_R0 = 8, H_KVH = 9, H_BID = 10,
+enum { H_ROW = 0, H_BEGIN = 1, H_TOK = 2, H_NUSERS = 4, H_ADD = 5, H_KVH = 9, H_BID = 10,
        H_QUERY = 16, H_SLOT = 24 };                  // (H_BID: the first two block ids)
 
 // One warp's share of the units of a launch.
@@ -126,7 +127,7 @@ enum { H_ROW = 0, H_BEGIN = 1, H_TOK = 2, H_NUSERS = 4, H_ADD = 5, H_R0 = 8, H_K
 // done per score is done once for both.  A lane's block is q / 2.  For O^T the weights of the other
 // block's columns are masked out of the B operand.
 template <bool kNarrow>
-__device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Grid& grid, uint8_t* smem) {
+__device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Units& units, uint8_t* smem) {
   constexpr int kSets = kNarrow ? 2 : 1;             // query operands
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, q = lane & 3;
@@ -135,12 +136,12 @@ __device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Grid& gr
   const uint32_t qrows = s32(smem) + kOffQ + warp * kRows * kDim * 2;
   int* const hdrs = (int*)(smem + kOffHdr) + warp * kHdrs * kHdrInts;
   auto hdr = [&](int seq) { return hdrs + (seq & (kHdrs - 1)) * kHdrInts; };
-  const int n_units = kNarrow ? grid.narrow_units : grid.unit_end[3];
+  const int n_units = kNarrow ? units.narrow_units : units.mid_units;
 
   // ---- descriptions, one phase per call: item; its users, first block ids and length; stored
   int f_seq = 0, f_phase = 0, f_pass = 0;            // units described so far; pass over the list
   bool f_end = n_units == 0;
-  int t0 = 0, t1 = 0, t2 = 0, t4 = 0, f_r0 = 0, f_kvh = 0;
+  int t0 = 0, t1 = 0, t2 = 0, t4 = 0, f_kvh = 0;
   uint2 t3 = make_uint2(0u, 0u);
   auto fetch_step = [&]() {
     if (f_phase == 0) {
@@ -151,34 +152,19 @@ __device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Grid& gr
         f_end = (long long)f_pass * W >= n_units;    // (a backward pass may start past the end)
         return;
       }
-      int x = u, item = kNarrow ? grid.narrow_begin : grid.item_begin[0];
-      f_r0 = 0;
-      if (!kNarrow) {
-        int tiles = grid.tiles[0];
-#pragma unroll
-        for (int k = 1; k < 4; ++k)
-          if (u >= grid.unit_end[k - 1]) {
-            x = u - grid.unit_end[k - 1];
-            item = grid.item_begin[k];
-            tiles = grid.tiles[k];
-          }
-        f_r0 = x % tiles * kRows;
-        x /= tiles;
-      }
-      f_kvh = x % HKV;
-      t0 = lane < 8 ? __ldg((const int*)(a.d_items + item + x / HKV) + lane) : 0;
+      f_kvh = u % HKV;
+      t0 = lane < 8 ? __ldg((const int*)(a.d_items + (kNarrow ? units.narrow_begin : units.mid_begin) +
+                                         u / HKV) + lane) : 0;
       f_phase = 1;
     } else if (f_phase == 1) {
       const int row = __shfl_sync(0xffffffffu, t0, 0), begin = __shfl_sync(0xffffffffu, t0, 1);
       const int end = __shfl_sync(0xffffffffu, t0, 2), ub = __shfl_sync(0xffffffffu, t0, 3);
       const int R = __shfl_sync(0xffffffffu, t0, 4) * G;
-      f_phase = 0;
-      if (f_r0 >= R) return;                         // an item narrower than its class
       t1 = (end < 0 ? a.d_lens[row] : end) - begin;
       const int32_t* tab = a.d_tables + (size_t)row * a.shape.table_stride;
       t2 = tab[begin / kBlock];
       t4 = tab[min(begin / kBlock + 1, a.shape.table_stride - 1)];   // (unused if there is none)
-      const int r = f_r0 + (lane & 7);
+      const int r = lane & 7;
       t3 = make_uint2(0u, 0u);
       if (r < R) t3 = *(const uint2*)(a.d_users + ub + r / G);
       f_phase = 2;
@@ -187,7 +173,6 @@ __device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Grid& gr
       if (lane < 8 && lane != H_TOK) h[lane] = t0;
       if (lane == 8) {
         h[H_TOK] = t1;
-        h[H_R0] = f_r0;
         h[H_KVH] = f_kvh;
         h[H_BID] = t2;
         h[H_BID + 1] = t4;
@@ -240,14 +225,13 @@ __device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Grid& gr
     l_bid1 = h[H_BID + 1];
     l_tab = a.d_tables + (size_t)h[H_ROW] * a.shape.table_stride + h[H_BEGIN] / kBlock;
     // the query rows, committed with the first tile: half a warp copies one
-    const int rows = h[H_NUSERS] * G - h[H_R0];
+    const int rows = h[H_NUSERS] * G;
 #pragma unroll
     for (int j = 0; j < (kNarrow ? kRows / 4 : kRows / 2); ++j) {
       const int r = 2 * j + (lane >> 4);
       if (r < rows)
         cp_async16(qrows + r * kDim * 2 + (lane & 15) * 16,
-                   (const uint4*)a.q + ((size_t)h[H_QUERY + r] * HQ + l_kvh * G +
-                                        (h[H_R0] + r) % G) * 16 + (lane & 15));
+                   (const uint4*)a.q + ((size_t)h[H_QUERY + r] * HQ + l_kvh * G + r % G) * 16 + (lane & 15));
     }
     return true;
   };
@@ -275,7 +259,7 @@ __device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Grid& gr
 
     if (k == 0) {                // ---- a unit begins
       n_tok = hdr(c_seq)[H_TOK];
-      rows = hdr(c_seq)[H_NUSERS] * G - hdr(c_seq)[H_R0];
+      rows = hdr(c_seq)[H_NUSERS] * G;
       const int r = kNarrow ? g & 3 : g;
       uint32_t top = 0;          // bits of the row's largest magnitude, without the sign
       uint4 v[4];
@@ -572,7 +556,7 @@ __device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Grid& gr
       const int r = 2 * q + e;
       if (r >= rows) continue;
       constexpr float kLow = 1.f / kCodeUnit, kHigh = kLow / 16.f;   // (odd nibbles counted 16 times)
-      const int head = h[H_KVH] * G + (h[H_R0] + r) % G;
+      const int head = h[H_KVH] * G + r % G;
       const int query = h[H_QUERY + r], slot = h[H_SLOT + r];
       const float inv = slot < 0 ? 1.f / l[e] : 1.f;
       const size_t prow = (size_t)(slot + h[H_ADD]) * HQ + head;
@@ -596,12 +580,13 @@ __device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Grid& gr
 }
 
 __global__ void __launch_bounds__(32 * kWarps, 1)
-attn_q4_kernel(const AttnArgs a, const Q4Grid grid) {
+attn_q4_kernel(const AttnArgs a, const Q4Units units) {
   extern __shared__ __align__(128) uint8_t smem[];
   pdl_launch_dependents();
-  stream_units<false>(a, grid, smem);
+  stream_units<false>(a, units, smem);
   __syncwarp();
-  stream_units<true>(a, grid, smem);
+  stream_units<true>(a, units, smem);
+  pdl_wait();                        // "this grid has completed" implies the one before it has
 }
 
 // Candidate tokens of a verification, as verify_tail_kernel, rows read from the 4-bit pool.  The
@@ -762,24 +747,11 @@ cudaError_t launch_q4_merge(const AttnArgs& a, const MergeRef* d_merge, int n_me
 }
 
 cudaError_t launch_attention_q4(const AttnArgs& a, const Q4Items& it, cudaStream_t st) {
-  // classes as the planner orders them: items of 4, 3, 2 and 1 tiles of 16 rows, narrow ones last
-  Q4Grid g;
-  int64_t units = 0;
-  int items = 0;
-  for (int k = 0; k < 4; ++k) {
-    const int n = it.n_items[3 - k];
-    g.tiles[k] = std::max(1, (it.max_rows[3 - k] + kRows - 1) / kRows);
-    g.item_begin[k] = items;
-    items += n;
-    units += (int64_t)n * g.tiles[k] * a.shape.num_kv_heads;
-    if (units > INT32_MAX - (1 << 20)) return cudaErrorInvalidValue;
-    g.unit_end[k] = (int32_t)units;
-  }
+  const int64_t mid = (int64_t)it.n_mid * a.shape.num_kv_heads;
   const int64_t narrow = (int64_t)it.n_narrow * a.shape.num_kv_heads;
-  if (narrow > INT32_MAX - (1 << 20)) return cudaErrorInvalidValue;
-  g.narrow_begin = items;
-  g.narrow_units = (int32_t)narrow;
-  if (units + narrow == 0) return cudaSuccess;
+  if (mid + narrow == 0) return cudaSuccess;
+  if (std::max(mid, narrow) > INT32_MAX - (1 << 20)) return cudaErrorInvalidValue;
+  const Q4Units u = {it.n_wide, (int32_t)mid, it.n_wide + it.n_mid, (int32_t)narrow};
   static bool configured[64] = {};
   int dev = 0;
   cudaGetDevice(&dev);
@@ -790,9 +762,8 @@ cudaError_t launch_attention_q4(const AttnArgs& a, const Q4Items& it, cudaStream
     if (e != cudaSuccess) return e;
     configured[dev] = true;
   }
-  const int ctas = (int)std::min<int64_t>(units + narrow, a.num_sms);
-  attn_q4_kernel<<<ctas, 32 * kWarps, kSmemQ4, st>>>(a, g);
-  return cudaGetLastError();
+  const int ctas = (int)std::min<int64_t>(mid + narrow, a.num_sms);
+  return launch_kernel(attn_q4_kernel, dim3(ctas), dim3(32 * kWarps), kSmemQ4, st, a.pdl != 0, a, u);
 }
 
 cudaError_t launch_q4_verify_tail(const AttnArgs& a, const VerifyDesc* d_desc, int n_desc,

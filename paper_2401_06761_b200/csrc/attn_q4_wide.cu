@@ -1,0 +1,494 @@
+// Tree attention over a KV pool held in 4 bits for work items with more than eight query rows
+// (prompts shared by siblings, candidates of a verification, GQA groups above eight), on the
+// Blackwell tensor cores (tcgen05).
+//
+// mma.sync has to turn the codes of a block into operand registers once per eight rows, which for
+// 64 rows costs eight times the arithmetic of one; here a block is turned into f16 operand tiles in
+// shared memory once for all of an item's rows.  A CTA owns one item and kv head (at most 64
+// rows) and walks its run in tiles of 64 tokens, two CTAs to an SM:
+//   warps 2-5  one block of the tile each: its 4-bit K and V tiles arrive through a private cp.async
+//              ring, two tiles ahead, and leave as f16 operands.  K' = K 2^-(E + 8) with E the
+//              exponent of the block's largest value, V' = V 2^-(F + 8) with F that of the token's,
+//              so that f16's range is never an issue; a code enters the conversion as the
+//              subnormal number it is in place (c * 2^-24, or * 2^-20 a nibble up), one
+//              fused multiply-add per pair of values.
+//   warp 6     issues S = Q K'^T (M 128, N 64, K 128) and, one tile behind, O += P V' (M 128, N 128,
+//              K 64, P from tensor memory).  Rows past 63 of the A operands are whatever lies
+//              there; their results are not read.  (M 64 takes the pipe just as long.)
+//   warps 0-1  one thread per row: x = S u 2^(E + 8) + F + 8, P = 2^(x - ref) in f16, its sum less
+//              the token's factor in 32 bits, and P back over the scores it came from.  The
+//              reference follows score and size of V together and moves lazily, as in attn_q4.cu.
+// K, V and S are double-buffered.  Both operands and the weights are rounded to 11 bits (K' and V'
+// of values far below their maximum to 2^-18 of it), against eight of the output.
+// All waits are bounded; a wait that gives up raises the error word and every role unwinds to the
+// common exit where TMEM is released.
+#include <algorithm>
+#include <climits>
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include "apar_internal.h"
+#include "kv4.cuh"
+#include "ptx.cuh"
+#include "tcgen05.cuh"
+
+namespace apar {
+namespace {
+
+constexpr int kTok = 64;                             // tokens of a tile: one block per converter warp
+constexpr int kConv = 4;                             // converter warps
+constexpr int kThreads = 32 * (2 + kConv + 1);
+constexpr int kBlk = 2 * kQ4TileBytes;               // K and V of one block, as stored
+constexpr int kDepthW = 3;                           // blocks of a converter's ring
+constexpr int kHalfOp = 64 * 128;                    // 64 rows x 64 dims f16, 128-byte swizzle
+constexpr int kOpBytes = 2 * kHalfOp;                // K' or V' of a tile, or Q
+constexpr int kOffK = kOpBytes;                      // (Q first: its rows 64..127 run into K')
+constexpr int kOffVw = kOffK + 2 * kOpBytes;
+constexpr int kOffRaw = kOffVw + 2 * kOpBytes;
+constexpr int kOffTok = kOffRaw + kConv * kDepthW * kBlk;     // [2] F + 8 and 2^-(F + 8) of 64 tokens
+constexpr int kOffKb = kOffTok + 2 * 2 * kTok * 4;            // [2][4] 2^(E + 8)
+constexpr int kOffBarW = kOffKb + 2 * 4 * 4;
+enum { BW_KFULL = 0, BW_KEMPTY = 2, BW_VFULL = 4, BW_VEMPTY = 6, BW_SFULL = 8, BW_PFULL = 10,
+       BW_PVDONE = 12, BW_TOTAL = 14 };
+constexpr int kSmemWide = kOffBarW + 8 * BW_TOTAL + 16 + 1024;
+static_assert(2 * (kSmemWide + 1024) <= 228 * 1024, "two CTAs per SM");
+constexpr int kTmemColsW = 256;                      // S at 0 and 64, O at 128
+constexpr float kSlackW = 8.f;
+constexpr float kNoRefW = -3e38f;
+constexpr int kLift = 8;                             // operands stay below 2^(1 - kLift)
+constexpr uint32_t kEvenW = 0x000f000fu, kOddW = 0x00f000f0u;
+
+// D fp32, A and B f16, both K-major.
+__host__ __device__ constexpr uint32_t instr_desc_f16(int n, int m) {
+  return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+__device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
+  __half2 h = __floats2half2_rn(lo, hi);
+  return *(uint32_t*)&h;
+}
+__device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
+  __half2 r = __hfma2(*(__half2*)&a, *(__half2*)&b, *(__half2*)&c);
+  return *(uint32_t*)&r;
+}
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+// exponent of a non-negative number, kept away from the ends of the range
+__device__ __forceinline__ int exponent_of(float x) {
+  return min(110, max(-100, (int)(__float_as_uint(x) >> 23) - 127));
+}
+// largest magnitude a group can stand for
+__device__ __forceinline__ float group_top(uint32_t sl) {
+  const float s = bf16_lo(sl), lo = bf16_hi(sl);
+  return fmaxf(fabsf(lo), fabsf(fmaf(15.f, s, lo)));   // (a NaN group counts as 0)
+}
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
+__global__ void __launch_bounds__(kThreads, 2)
+attn_q4_wide_kernel(const AttnArgs a, int item_begin) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (s32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* bp = smem_raw + (base - s32(smem_raw));
+  auto bar = [&](int i) { return base + kOffBarW + 8u * i; };
+  volatile int* cta_abort = (volatile int*)(bp + kOffBarW + 8 * BW_TOTAL);
+  volatile uint32_t* tmem_slot = (volatile uint32_t*)(bp + kOffBarW + 8 * BW_TOTAL + 8);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int G = a.shape.group, HQ = a.shape.num_q_heads, HKV = a.shape.num_kv_heads;
+  pdl_launch_dependents();
+
+  if (threadIdx.x == 0) {
+    *cta_abort = *(volatile int*)a.d_error;          // an earlier kernel gave up: do not pile up
+    for (int b = 0; b < 2; ++b) {
+      bar_init(bar(BW_KFULL + b), kConv);
+      bar_init(bar(BW_KEMPTY + b), 1);
+      bar_init(bar(BW_VFULL + b), kConv);
+      bar_init(bar(BW_VEMPTY + b), 1);
+      bar_init(bar(BW_SFULL + b), 1);
+      bar_init(bar(BW_PFULL + b), 2);
+      bar_init(bar(BW_PVDONE + b), 1);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 6) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                 ::"r"(s32((const void*)tmem_slot)), "r"(kTmemColsW) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  const WorkItem it = a.d_items[item_begin + blockIdx.x];
+  const int kvh = blockIdx.y;
+  const int tok_end = it.tok_end < 0 ? a.d_lens[it.table_row] : it.tok_end;
+  const int n_tok = tok_end - it.tok_begin;
+  const int n_blk = (n_tok + kBlock - 1) / kBlock;
+  const int n_tiles = (n_blk + kConv - 1) / kConv;
+  const int R = it.n_users * G;
+
+  // ---- query rows, in f16 under a power of two of their own
+  const int row = threadIdx.x;                       // (softmax warps)
+  float u = 0.f;                                     // scale * log2(e) / the row's factor
+  UserRef user = UserRef{0, -1};
+  int head = 0;
+  if (warp < 2) {
+    uint4 v[16];
+    uint32_t top = 0;
+#pragma unroll
+    for (int c = 0; c < 16; ++c) v[c] = make_uint4(0u, 0u, 0u, 0u);
+    if (row < R) {
+      user = a.d_users[it.user_begin + row / G];
+      head = kvh * G + row % G;
+      const uint4* src = (const uint4*)a.q + ((size_t)user.query * HQ + head) * 16;
+#pragma unroll
+      for (int c = 0; c < 16; ++c) {
+        v[c] = __ldg(src + c);
+        const uint32_t w[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
+#pragma unroll
+        for (int p = 0; p < 4; ++p) top = max(top, max(w[p] << 17, (w[p] & 0x7fff0000u) << 1));
+      }
+    }
+    const int lift = min(126, 14 + 127 - (int)(top >> 24));
+    const float f = pow2(lift);
+    u = a.scale_log2e * pow2(-lift);
+#pragma unroll
+    for (int c = 0; c < 16; ++c) {
+      const uint32_t w[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
+      uint32_t h[4];
+#pragma unroll
+      for (int p = 0; p < 4; ++p) h[p] = f16x2(bf16_lo(w[p]) * f, bf16_hi(w[p]) * f);
+      *(uint4*)(bp + (c >> 3) * kHalfOp + row * 128 + (((c & 7) ^ (row & 7)) << 4)) =
+          make_uint4(h[0], h[1], h[2], h[3]);
+    }
+    fence_async_smem();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  if (*cta_abort) {
+    // nothing is started
+  } else if (warp >= 2 && warp < 2 + kConv) {
+    // ---------------------------------------------------------------- converters
+    const int cw = warp - 2;
+    const uint32_t raw = base + kOffRaw + cw * kDepthW * kBlk;
+    const int32_t* table = a.d_tables + (size_t)it.table_row * a.shape.table_stride +
+                           it.tok_begin / kBlock;
+    auto issue = [&](int t, int bid) {               // this warp's block of tile t
+      const size_t tile = ((size_t)bid * HKV + kvh) * kQ4TileBytes + lane * 16;
+      const uint8_t* kt = (const uint8_t*)a.k_pool + tile;
+      const uint8_t* vt = (const uint8_t*)a.v_pool + tile - kQ4TileBytes;
+      const uint32_t dst = raw + (t % kDepthW) * kBlk + lane * 16;
+      cp16(dst, kt);
+      cp16(dst + 512, kt + 512);
+      cp16(dst + 1024, (lane < 16 ? kt : vt) + 1024);
+      cp16(dst + 1536, vt + 1536);
+      cp16(dst + 2048, vt + 2048);
+    };
+#pragma unroll
+    for (int t = 0; t < kDepthW - 1; ++t) {
+      if (t * kConv + cw < n_blk) issue(t, table[t * kConv + cw]);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    auto id_of = [&](int t) { return t * kConv + cw < n_blk ? table[t * kConv + cw] : 0; };
+    int next_bid = id_of(kDepthW - 1);
+    for (int t = 0; t < n_tiles; ++t) {
+      const int b = t & 1;
+      asm volatile("cp.async.wait_group %0;" ::"n"(kDepthW - 2) : "memory");
+      __syncwarp();
+      if ((t + kDepthW - 1) * kConv + cw < n_blk) issue(t + kDepthW - 1, next_bid);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      next_bid = id_of(t + kDepthW);
+      const uint8_t* kt = bp + (raw - base) + (t % kDepthW) * kBlk;
+      const uint8_t* vt = kt + kQ4TileBytes;
+      const int nv = n_tok - (t * kConv + cw) * kBlock;      // tokens of the block that count
+
+      // ---- K: lane = (token, half of its 16-byte pieces)
+      int ek;
+      {
+        const int tok = lane >> 1, h = lane & 1;
+        uint4 sc = *(const uint4*)(kt + tok * kQ4RowBytes + kQ4CodeBytes);
+        const uint4 c0 = *(const uint4*)(kt + tok * kQ4RowBytes + 32 * h);
+        const uint4 c1 = *(const uint4*)(kt + tok * kQ4RowBytes + 32 * h + 16);
+        if (tok >= nv) sc = make_uint4(0u, 0u, 0u, 0u);      // (unspecified bits: the row is zeros)
+        const uint32_t sl[4] = {sc.x, sc.y, sc.z, sc.w};
+        float top = fmaxf(fmaxf(group_top(sl[0]), group_top(sl[1])),
+                          fmaxf(group_top(sl[2]), group_top(sl[3])));
+#pragma unroll
+        for (int d = 2; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        ek = exponent_of(top) + kLift;
+        const float down = pow2(-ek), up = down * 16777216.f;
+        if (t >= 2 && !__all_sync(0xffffffffu, bar_wait(bar(BW_KEMPTY + b), ((t >> 1) - 1) & 1, cta_abort,
+                                                        a.d_error, 23000)))
+          break;
+        const uint32_t w0[4] = {c0.x, c0.y, c0.z, c0.w}, w1[4] = {c1.x, c1.y, c1.z, c1.w};
+        const int r = cw * kBlock + tok;
+        uint8_t* dst = bp + kOffK + b * kOpBytes + r * 128;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float s = bf16_lo(sl[j]) * up, lo = bf16_hi(sl[j]) * down;
+          const uint32_t s1 = f16x2(s, s), s16 = f16x2(s * 0.0625f, s * 0.0625f), lo2 = f16x2(lo, lo);
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const uint32_t w = x ? w1[j] : w0[j], wh = w >> 8;
+            const int c = 4 * j + 2 * h + x;                 // dims 8 c .. 8 c + 7
+            *(uint4*)(dst + (c >> 3) * kHalfOp + (((c & 7) ^ (r & 7)) << 4)) =
+                make_uint4(hfma2(w & kEvenW, s1, lo2), hfma2(w & kOddW, s16, lo2),
+                           hfma2(wh & kEvenW, s1, lo2), hfma2(wh & kOddW, s16, lo2));
+          }
+        }
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) bar_arrive(bar(BW_KFULL + b));
+      }
+      // ---- V: constants of (pair, group), then words of four pairs at a time
+      if (t >= 2 && !__all_sync(0xffffffffu, bar_wait(bar(BW_VEMPTY + b), ((t >> 1) - 1) & 1, cta_abort,
+                                                      a.d_error, 23100)))
+        break;
+      {
+        uint8_t* const vc = const_cast<uint8_t*>(kt);        // [pair][group]: K has been read
+        const int pair = lane >> 2, g4 = lane & 3;
+        const uint8_t* sc = vt + pair * kQ4PairBytes + 2 * kQ4CodeBytes + 4 * g4;
+        uint32_t se = *(const uint32_t*)sc, so = *(const uint32_t*)(sc + 16);
+        if (2 * pair >= nv) se = 0u;
+        if (2 * pair + 1 >= nv) so = 0u;
+        float te = group_top(se), to = group_top(so);
+#pragma unroll
+        for (int d = 1; d <= 2; d <<= 1) {
+          te = fmaxf(te, __shfl_xor_sync(0xffffffffu, te, d));
+          to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, d));
+        }
+        const int fe = exponent_of(te) + kLift, fo = exponent_of(to) + kLift;
+        const float de = pow2(-fe), dn = pow2(-fo);
+        const float s0 = bf16_lo(se) * (de * 16777216.f), s1 = bf16_lo(so) * (dn * 16777216.f);
+        *(uint4*)(vc + lane * 16) = make_uint4(f16x2(s0, s1), f16x2(s0 * 0.0625f, s1 * 0.0625f),
+                                               f16x2(bf16_hi(se) * de, bf16_hi(so) * dn), 0u);
+        float* tokc = (float*)(bp + kOffTok) + b * 2 * kTok;
+        const int tk = cw * kBlock + 2 * pair;
+        if (g4 == 0) {
+          *(float2*)(tokc + tk) = make_float2(2 * pair < nv ? (float)fe : -INFINITY,
+                                              2 * pair + 1 < nv ? (float)fo : -INFINITY);
+          *(float2*)(tokc + kTok + tk) =
+              make_float2(2 * pair < nv ? de : 0.f, 2 * pair + 1 < nv ? dn : 0.f);
+        }
+        if (lane == 0) ((float*)(bp + kOffKb))[b * 4 + cw] = pow2(ek);
+        __syncwarp();
+        const int pg = lane & 1;                             // pairs 4 pg .. 4 pg + 3
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int word = (lane >> 1) + 16 * i;             // 4 g + G
+          const int g = word >> 2, GG = word & 3;
+          uint32_t out[4][4];                                // [dim][pair]
+#pragma unroll
+          for (int p = 0; p < 4; ++p) {
+            const uint32_t w = *(const uint32_t*)(vt + (4 * pg + p) * kQ4PairBytes + 4 * word);
+            const uint4 c = *(const uint4*)(vc + ((4 * pg + p) * 4 + GG) * 16);
+            const uint32_t wh = w >> 8;
+            out[0][p] = hfma2(w & kEvenW, c.x, c.z);
+            out[1][p] = hfma2(w & kOddW, c.y, c.z);
+            out[2][p] = hfma2(wh & kEvenW, c.x, c.z);
+            out[3][p] = hfma2(wh & kOddW, c.y, c.z);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int d = 32 * GG + 4 * g + e;               // operand row; tokens 16 cw + 8 pg ..
+            *(uint4*)(bp + kOffVw + b * kOpBytes + d * 128 + (((2 * cw + pg) ^ (d & 7)) << 4)) =
+                make_uint4(out[e][0], out[e][1], out[e][2], out[e][3]);
+          }
+        }
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) bar_arrive(bar(BW_VFULL + b));
+      }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+  } else if (warp == 2 + kConv) {
+    // ---------------------------------------------------------------- MMA issuer
+    constexpr uint32_t kIdescQK = instr_desc_f16(kTok, 128), kIdescPV = instr_desc_f16(kDim, 128);
+    constexpr unsigned kAll = 0xffffffffu;
+    for (int t = 0; t <= n_tiles; ++t) {
+      if (t < n_tiles) {
+        const int b = t & 1;
+        if (!__all_sync(kAll, bar_wait(bar(BW_KFULL + b), (t >> 1) & 1, cta_abort, a.d_error, 24000)))
+          break;
+        tc_fence_after();
+        if (lane == 0) {
+#pragma unroll
+          for (int ks = 0; ks < 8; ++ks) {
+            const uint32_t off = (ks >> 2) * kHalfOp + (ks & 3) * 32;
+            umma_bf16(tmem + 64u * b, smem_desc(base + off, 16, 1024),
+                      smem_desc(base + kOffK + b * kOpBytes + off, 16, 1024), kIdescQK, ks > 0);
+          }
+          umma_commit(bar(BW_SFULL + b));
+          umma_commit(bar(BW_KEMPTY + b));
+        }
+        __syncwarp();
+      }
+      if (t > 0) {
+        const int p = t - 1, b = p & 1;
+        bool ok = bar_wait(bar(BW_PFULL + b), (p >> 1) & 1, cta_abort, a.d_error, 24100);
+        ok = ok && bar_wait(bar(BW_VFULL + b), (p >> 1) & 1, cta_abort, a.d_error, 24200);
+        if (!__all_sync(kAll, ok)) break;
+        tc_fence_after();
+        if (lane == 0) {
+#pragma unroll
+          for (int kk = 0; kk < kTok / 16; ++kk)
+            umma_bf16_ts(tmem + 128u, tmem + 64u * b + 8u * kk,
+                         smem_desc(base + kOffVw + b * kOpBytes + kk * 32, 16, 1024), kIdescPV,
+                         p > 0 || kk > 0);
+          umma_commit(bar(BW_VEMPTY + b));
+          umma_commit(bar(BW_PVDONE + b));
+        }
+        __syncwarp();
+      }
+    }
+  } else if (warp < 2) {
+    // ---------------------------------------------------------------- softmax: a thread, a row
+    const uint32_t lane_sel = (uint32_t)(warp * 32) << 16;
+    const bool idle = warp * 32 >= R;                // (no rows here: only keeps the phases)
+    float ref = kNoRefW, l = 0.f;
+    bool alive = true;
+    for (int t = 0; t < n_tiles; ++t) {
+      const int b = t & 1;
+      bool ok = bar_wait(bar(BW_SFULL + b), (t >> 1) & 1, cta_abort, a.d_error, 22000);
+      ok = ok && bar_wait(bar(BW_VFULL + b), (t >> 1) & 1, cta_abort, a.d_error, 22100);
+      if (!__all_sync(0xffffffffu, ok)) {
+        alive = false;
+        break;
+      }
+      tc_fence_after();
+      if (!idle) {
+        uint32_t sr[64];
+        TMEM_LD_32((tmem + 64u * b) | lane_sel, sr, 0);
+        TMEM_LD_32((tmem + 64u * b + 32u) | lane_sel, sr, 32);
+        tmem_wait_ld();
+        const float* tokc = (const float*)(bp + kOffTok) + b * 2 * kTok;
+        const float* kb = (const float*)(bp + kOffKb) + b * 4;
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int j = 0; j < 64; j += 4) {
+          const float s = u * kb[j >> 4];
+          const float4 f = *(const float4*)(tokc + j);       // (the same address in every lane)
+          const float x0 = fmaf(__uint_as_float(sr[j]), s, f.x);
+          const float x1 = fmaf(__uint_as_float(sr[j + 1]), s, f.y);
+          const float x2 = fmaf(__uint_as_float(sr[j + 2]), s, f.z);
+          const float x3 = fmaf(__uint_as_float(sr[j + 3]), s, f.w);
+          mx[0] = fmaxf(mx[0], x0);
+          mx[1] = fmaxf(mx[1], x1);
+          mx[2] = fmaxf(mx[2], x2);
+          mx[3] = fmaxf(mx[3], x3);
+          sr[j] = __float_as_uint(x0);
+          sr[j + 1] = __float_as_uint(x1);
+          sr[j + 2] = __float_as_uint(x2);
+          sr[j + 3] = __float_as_uint(x3);
+        }
+        const float m = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        if (__any_sync(0xffffffffu, m > ref + kSlackW)) {
+          const float now = fmaxf(m, ref), f = ex2(ref - now);
+          ref = now;
+          l *= f;
+          if (t > 0) {
+            // (P V of the tile before has to be complete; the phase before on its barrier is,
+            // because this tile's scores came after that product)
+            if (!__all_sync(0xffffffffu, bar_wait(bar(BW_PVDONE + (b ^ 1)), ((t - 1) >> 1) & 1,
+                                                  cta_abort, a.d_error, 22200))) {
+              alive = false;
+              break;
+            }
+            tc_fence_after();
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              uint32_t orow[32];
+              TMEM_LD_32((tmem + 128u + 32u * c) | lane_sel, orow, 0);
+              tmem_wait_ld();
+#pragma unroll
+              for (int j = 0; j < 32; ++j) orow[j] = __float_as_uint(__uint_as_float(orow[j]) * f);
+              TMEM_ST_32((tmem + 128u + 32u * c) | lane_sel, orow);
+            }
+            tmem_wait_st();
+          }
+        }
+        uint32_t pk[32];
+        float ls[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 64; j += 4) {
+          const float4 n = *(const float4*)(tokc + kTok + j);
+          const float p0 = ex2(__uint_as_float(sr[j]) - ref);
+          const float p1 = ex2(__uint_as_float(sr[j + 1]) - ref);
+          const float p2 = ex2(__uint_as_float(sr[j + 2]) - ref);
+          const float p3 = ex2(__uint_as_float(sr[j + 3]) - ref);
+          ls[0] = fmaf(p0, n.x, ls[0]);
+          ls[1] = fmaf(p1, n.y, ls[1]);
+          ls[2] = fmaf(p2, n.z, ls[2]);
+          ls[3] = fmaf(p3, n.w, ls[3]);
+          pk[j >> 1] = f16x2(p0, p1);
+          pk[(j >> 1) + 1] = f16x2(p2, p3);
+        }
+        l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+        TMEM_ST_32((tmem + 64u * b) | lane_sel, pk);
+        tmem_wait_st();
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) bar_arrive(bar(BW_PFULL + b));
+    }
+    alive = alive && __all_sync(0xffffffffu, bar_wait(bar(BW_PVDONE + ((n_tiles - 1) & 1)),
+                                                      ((n_tiles - 1) >> 1) & 1, cta_abort, a.d_error,
+                                                      22300));
+    if (alive && !idle) {
+      tc_fence_after();
+      const float inv = user.slot < 0 ? 1.f / l : 1.f;
+      const size_t prow = (size_t)(user.slot + it.slot_add) * HQ + head;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t o[32];
+        TMEM_LD_32((tmem + 128u + 32u * c) | lane_sel, o, 0);
+        tmem_wait_ld();
+        if (row < R) {
+          if (user.slot < 0) {
+            uint4* dst = (uint4*)((__nv_bfloat16*)a.out + ((size_t)user.query * HQ + head) * kDim) + 4 * c;
+#pragma unroll
+            for (int j = 0; j < 32; j += 8)
+              dst[j >> 3] = make_uint4(
+                  pack2(__uint_as_float(o[j]) * inv, __uint_as_float(o[j + 1]) * inv),
+                  pack2(__uint_as_float(o[j + 2]) * inv, __uint_as_float(o[j + 3]) * inv),
+                  pack2(__uint_as_float(o[j + 4]) * inv, __uint_as_float(o[j + 5]) * inv),
+                  pack2(__uint_as_float(o[j + 6]) * inv, __uint_as_float(o[j + 7]) * inv));
+          } else {
+            uint4* dst = (uint4*)(a.part_o + prow * kDim) + 8 * c;
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) dst[j >> 2] = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+          }
+        }
+      }
+      if (row < R && user.slot >= 0) a.part_ml[prow] = make_float2(ref, l);
+    }
+  }
+  // ---- common exit: every role arrives here, then the allocating warp frees TMEM
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 6) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem),
+                 "r"(kTmemColsW) : "memory");
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_attention_q4_wide(const AttnArgs& a, int item_begin, int n_items, cudaStream_t st) {
+  if (n_items <= 0) return cudaSuccess;
+  static bool configured[64] = {};
+  int dev = 0;
+  cudaGetDevice(&dev);
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  if (!configured[dev]) {
+    cudaError_t e = cudaFuncSetAttribute(attn_q4_wide_kernel,
+                                         cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemWide);
+    if (e != cudaSuccess) return e;
+    configured[dev] = true;
+  }
+  attn_q4_wide_kernel<<<dim3(n_items, a.shape.num_kv_heads), kThreads, kSmemWide, st>>>(a, item_begin);
+  return cudaGetLastError();
+}
+
+}  // namespace apar

@@ -28,6 +28,7 @@ void Planner::init(int num_blocks, int group, int num_kv_heads) {
 }
 
 static inline int64_t round_up16(int64_t x) { return (x + 15) / 16 * 16; }
+constexpr int kWideCost = 2;         // time of a wide unit of a 4-bit pool, in those of a warp
 constexpr int kMaxFoldedParts = 8;   // partial results a finishing item may fold by itself
 
 void Planner::ensure_keys(size_t n) {
@@ -142,11 +143,13 @@ bool Planner::build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_
     // The fewest chunks that give every warp a unit and none a second one; with more units than
     // warps from the start, no unit longer than a warp's even share.
     const int64_t warps = (int64_t)num_sms_ * streams_;
+    // warps' worth of time per token of a run
     auto units_of = [&](const Seg& g) {
-      const int64_t full = g.n_users / std::max(1, kMaxRowsPerItem / group_);
-      const int64_t rest = g.n_users % std::max(1, kMaxRowsPerItem / group_);
-      auto tiles = [&](int64_t users) { return (users * group_ + stream_rows_ - 1) / stream_rows_; };
-      return (full * tiles(std::max(1, kMaxRowsPerItem / group_)) + tiles(rest)) * hint_kv_heads_;
+      const int64_t per = std::max(1, kMaxRowsPerItem / group_);
+      auto cost = [&](int64_t users) -> int64_t {
+        return users == 0 ? 0 : users * group_ > stream_rows_ ? kWideCost : 1;
+      };
+      return (g.n_users / per * cost(per) + cost(g.n_users % per)) * hint_kv_heads_;
     };
     int64_t uncut = 0, work = 0, longest = 0;
     for (const Seg& g : segs_) {
