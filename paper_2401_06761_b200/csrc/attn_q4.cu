@@ -115,7 +115,7 @@ __device__ __forceinline__ uint2 lds64(uint32_t a) {
 }
 
 // words of a unit description; query and slot of row r at H_QUERY + r, H_SLOT + r
-enum { H_ROW = 0, H_BEGIN = 1, H_TOK = 2, H_NUSERS = 4, H_ADD = 5, H_KVH = 9, H_BID = 10,
+enum { H_ROW = 0, H_BEGIN = 1, H_TOK = 2, H_NUSERS = 4, H_ADD = 5, H_KVH = 9, H_BID = 10, H_TAB = 12,
        H_QUERY = 16, H_SLOT = 24 };                  // (H_BID: the first two block ids)
 
 // One warp's share of the units of a launch.
@@ -170,12 +170,14 @@ __device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Units& u
       f_phase = 2;
     } else {
       int* h = hdr(f_seq);
+      const int row = __shfl_sync(0xffffffffu, t0, 0), begin = __shfl_sync(0xffffffffu, t0, 1);
       if (lane < 8 && lane != H_TOK) h[lane] = t0;
       if (lane == 8) {
         h[H_TOK] = t1;
         h[H_KVH] = f_kvh;
         h[H_BID] = t2;
         h[H_BID + 1] = t4;
+        *(const int32_t**)(h + H_TAB) = a.d_tables + (size_t)row * a.shape.table_stride + begin / kBlock;
       }
       if (lane >= 16) h[lane] = lane < 24 ? (int)t3.x : (int)t3.y;
       __syncwarp();
@@ -187,11 +189,10 @@ __device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Units& u
   // ---- loads: at most one unit ahead of the one that is computed, and not before that one's
   // query rows have been read (the next unit's take their place)
   int c_seq = 0, k = 0;                              // the unit being computed; its next block
-  int l_seq = -1, l_k = 0, l_n = 0, l_bid = 0, l_bid1 = 0, l_kvh = 0;
-  const int32_t* l_tab = nullptr;
+  int l_seq = -1, l_k = 0, l_n = 0, l_bid = 0, l_bid1 = 0;
   int issue_slot = 0, use_slot = 0, ahead = 0;       // steps requested and not computed
   auto issue_block = [&](int bid, uint32_t dst) {
-    const size_t tile = ((size_t)bid * HKV + l_kvh) * kQ4TileBytes + lane * 16;
+    const size_t tile = ((size_t)bid * HKV + hdr(l_seq)[H_KVH]) * kQ4TileBytes + lane * 16;
     const uint8_t* kt = (const uint8_t*)a.k_pool + tile;
     const uint8_t* vt = (const uint8_t*)a.v_pool + tile - kQ4TileBytes;
     cp_async16(dst, kt);
@@ -209,8 +210,9 @@ __device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Units& u
     ++ahead;
     l_k += kStep;
     if (l_k < l_n) {                                 // (arrive while a step is computed)
-      l_bid = l_tab[l_k];
-      l_bid1 = l_tab[min(l_k + 1, l_n - 1)];
+      const int32_t* tab = *(const int32_t**)(hdr(l_seq) + H_TAB);
+      l_bid = tab[l_k];
+      l_bid1 = tab[min(l_k + 1, l_n - 1)];
     }
   };
   auto next_unit = [&]() -> bool {                   // moves the loads on to it
@@ -220,10 +222,8 @@ __device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Units& u
     const int* h = hdr(++l_seq);
     l_n = (h[H_TOK] + kBlock - 1) / kBlock;
     l_k = 0;
-    l_kvh = h[H_KVH];
     l_bid = h[H_BID];
     l_bid1 = h[H_BID + 1];
-    l_tab = a.d_tables + (size_t)h[H_ROW] * a.shape.table_stride + h[H_BEGIN] / kBlock;
     // the query rows, committed with the first tile: half a warp copies one
     const int rows = h[H_NUSERS] * G;
 #pragma unroll
@@ -231,13 +231,12 @@ __device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Units& u
       const int r = 2 * j + (lane >> 4);
       if (r < rows)
         cp_async16(qrows + r * kDim * 2 + (lane & 15) * 16,
-                   (const uint4*)a.q + ((size_t)h[H_QUERY + r] * HQ + l_kvh * G + r % G) * 16 + (lane & 15));
+                   (const uint4*)a.q + ((size_t)h[H_QUERY + r] * HQ + h[H_KVH] * G + r % G) * 16 + (lane & 15));
     }
     return true;
   };
 
   // ---- state of the unit being computed
-  int n_tok = 0, rows = 0;
   uint32_t qb[kSets][4][4];      // the column's row, dims 32 j + 8 q .. + 7, as B fragments
   uint32_t qsum[kSets][2];       // its sum over group q as three bf16 numbers
   float unit[2];                 // rows 2 q, 2 q + 1: scale * 2^24 / their factor
@@ -258,8 +257,7 @@ __device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Units& u
     __syncwarp();
 
     if (k == 0) {                // ---- a unit begins
-      n_tok = hdr(c_seq)[H_TOK];
-      rows = hdr(c_seq)[H_NUSERS] * G;
+      const int rows = hdr(c_seq)[H_NUSERS] * G;
       const int r = kNarrow ? g & 3 : g;
       uint32_t top = 0;          // bits of the row's largest magnitude, without the sign
       uint4 v[4];
@@ -318,7 +316,7 @@ __device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Units& u
       l[0] = l[1] = 0.f;
     }
     const uint32_t tile0 = ring + use_slot * kSlot;
-    const int nv = n_tok - k * kBlock;
+    const int nv = hdr(c_seq)[H_TOK] - k * kBlock;   // tokens from this step on
 
     // ---- pieces of a step.  Scores are those of tokens g and g + 8 of a block for rows 2 q and
     // 2 q + 1, up to the factor `unit`.
@@ -437,15 +435,16 @@ __device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Units& u
         k_words(tile0 + kTile, c0, c1);
         const uint4 s0 = lds128(mine + g * kQ4RowBytes + kQ4CodeBytes);
         const uint4 s1 = lds128(mine + (g + 8) * kQ4RowBytes + kQ4CodeBytes);
-        float acc[4][4] = {};
-        dot(a0.x, a1.x, qb[0][0], acc[0]); dot(c0.x, c1.x, qb[kSets - 1][0], acc[0]);
-        dot(a0.y, a1.y, qb[0][1], acc[1]); dot(c0.y, c1.y, qb[kSets - 1][1], acc[1]);
-        dot(a0.z, a1.z, qb[0][2], acc[2]); dot(c0.z, c1.z, qb[kSets - 1][2], acc[2]);
-        dot(a0.w, a1.w, qb[0][3], acc[3]); dot(c0.w, c1.w, qb[kSets - 1][3], acc[3]);
-        scale_add(s0.x, s1.x, acc[0], x);
-        scale_add(s0.y, s1.y, acc[1], x);
-        scale_add(s0.z, s1.z, acc[2], x);
-        scale_add(s0.w, s1.w, acc[3], x);
+        const uint32_t wa[4] = {a0.x, a0.y, a0.z, a0.w}, wb[4] = {a1.x, a1.y, a1.z, a1.w};
+        const uint32_t wc[4] = {c0.x, c0.y, c0.z, c0.w}, wd[4] = {c1.x, c1.y, c1.z, c1.w};
+        const uint32_t sa[4] = {s0.x, s0.y, s0.z, s0.w}, sb[4] = {s1.x, s1.y, s1.z, s1.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float acc[4] = {};
+          dot(wa[j], wb[j], qb[0][j], acc);
+          dot(wc[j], wd[j], qb[kSets - 1][j], acc);
+          scale_add(sa[j], sb[j], acc, x);
+        }
       }
       uint32_t z[2][4];
       v_scales(mine + kQ4TileBytes, nv - (q >> 1) * kBlock, z, x);
@@ -513,7 +512,7 @@ __device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Units& u
     --ahead;
     use_slot = use_slot == kDepth - 1 ? 0 : use_slot + 1;
     k += kStep;
-    if (k * kBlock < n_tok) continue;
+    if (nv > kStep * kBlock) continue;
 
     // ---- end of the unit: sums over the lanes that hold other tokens of the same rows
 #pragma unroll
@@ -551,6 +550,7 @@ __device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Units& u
     }
     // ---- row 2 q + e: dims 32 j + 4 g .. + 3, to the output or to a partial result
     const int* h = hdr(c_seq);
+    const int rows = h[H_NUSERS] * G;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const int r = 2 * q + e;

@@ -82,6 +82,12 @@ __device__ __forceinline__ float group_top(uint32_t sl) {
   const float s = bf16_lo(sl), lo = bf16_hi(sl);
   return fmaxf(fabsf(lo), fabsf(fmaf(15.f, s, lo)));   // (a NaN group counts as 0)
 }
+// Orders chosen so that the converters' shared-memory accesses fall into different banks.  Token of
+// a block that takes row (K', and column of V') pos of it: bits 2 and 3 change places.  Row of V'
+// that holds dim 32 G + 4 g + e: 32 G + 4 g + (e + G) % 4.
+__device__ __forceinline__ int token_at(int pos) {
+  return (pos & 3) | ((pos & 4) << 1) | ((pos & 8) >> 1);
+}
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -202,10 +208,10 @@ attn_q4_wide_kernel(const AttnArgs a, int item_begin) {
       const uint8_t* vt = kt + kQ4TileBytes;
       const int nv = n_tok - (t * kConv + cw) * kBlock;      // tokens of the block that count
 
-      // ---- K: lane = (token, half of its 16-byte pieces)
+      // ---- K: lane = (operand row, half of its 16-byte pieces)
       int ek;
       {
-        const int tok = lane >> 1, h = lane & 1;
+        const int pos = lane & 15, h = lane >> 4, tok = token_at(pos);
         uint4 sc = *(const uint4*)(kt + tok * kQ4RowBytes + kQ4CodeBytes);
         const uint4 c0 = *(const uint4*)(kt + tok * kQ4RowBytes + 32 * h);
         const uint4 c1 = *(const uint4*)(kt + tok * kQ4RowBytes + 32 * h + 16);
@@ -214,14 +220,14 @@ attn_q4_wide_kernel(const AttnArgs a, int item_begin) {
         float top = fmaxf(fmaxf(group_top(sl[0]), group_top(sl[1])),
                           fmaxf(group_top(sl[2]), group_top(sl[3])));
 #pragma unroll
-        for (int d = 2; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
         ek = exponent_of(top) + kLift;
         const float down = pow2(-ek), up = down * 16777216.f;
         if (t >= 2 && !__all_sync(0xffffffffu, bar_wait(bar(BW_KEMPTY + b), ((t >> 1) - 1) & 1, cta_abort,
                                                         a.d_error, 23000)))
           break;
         const uint32_t w0[4] = {c0.x, c0.y, c0.z, c0.w}, w1[4] = {c1.x, c1.y, c1.z, c1.w};
-        const int r = cw * kBlock + tok;
+        const int r = cw * kBlock + pos;
         uint8_t* dst = bp + kOffK + b * kOpBytes + r * 128;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -263,7 +269,7 @@ attn_q4_wide_kernel(const AttnArgs a, int item_begin) {
         *(uint4*)(vc + lane * 16) = make_uint4(f16x2(s0, s1), f16x2(s0 * 0.0625f, s1 * 0.0625f),
                                                f16x2(bf16_hi(se) * de, bf16_hi(so) * dn), 0u);
         float* tokc = (float*)(bp + kOffTok) + b * 2 * kTok;
-        const int tk = cw * kBlock + 2 * pair;
+        const int tk = cw * kBlock + token_at(2 * pair);     // (a pair stays together)
         if (g4 == 0) {
           *(float2*)(tokc + tk) = make_float2(2 * pair < nv ? (float)fe : -INFINITY,
                                               2 * pair + 1 < nv ? (float)fo : -INFINITY);
@@ -272,25 +278,32 @@ attn_q4_wide_kernel(const AttnArgs a, int item_begin) {
         }
         if (lane == 0) ((float*)(bp + kOffKb))[b * 4 + cw] = pow2(ek);
         __syncwarp();
-        const int pg = lane & 1;                             // pairs 4 pg .. 4 pg + 3
+        // a lane's group is that of its words, lane % 4, in both rounds; its pairs are those of
+        // operand columns 8 pg .. 8 pg + 7
+        const int pg = lane >> 4, GG = lane & 3;
+        uint4 c[4];
+        int at[4];
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const int pr = token_at(8 * pg + 2 * p) >> 1;
+          c[p] = *(const uint4*)(vc + (pr * 4 + GG) * 16);
+          at[p] = pr * kQ4PairBytes;
+        }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int word = (lane >> 1) + 16 * i;             // 4 g + G
-          const int g = word >> 2, GG = word & 3;
+          const int word = (lane & 15) + 16 * i;             // 4 g + G
           uint32_t out[4][4];                                // [dim][pair]
 #pragma unroll
           for (int p = 0; p < 4; ++p) {
-            const uint32_t w = *(const uint32_t*)(vt + (4 * pg + p) * kQ4PairBytes + 4 * word);
-            const uint4 c = *(const uint4*)(vc + ((4 * pg + p) * 4 + GG) * 16);
-            const uint32_t wh = w >> 8;
-            out[0][p] = hfma2(w & kEvenW, c.x, c.z);
-            out[1][p] = hfma2(w & kOddW, c.y, c.z);
-            out[2][p] = hfma2(wh & kEvenW, c.x, c.z);
-            out[3][p] = hfma2(wh & kOddW, c.y, c.z);
+            const uint32_t w = *(const uint32_t*)(vt + at[p] + 4 * word), wh = w >> 8;
+            out[0][p] = hfma2(w & kEvenW, c[p].x, c[p].z);
+            out[1][p] = hfma2(w & kOddW, c[p].y, c[p].z);
+            out[2][p] = hfma2(wh & kEvenW, c[p].x, c[p].z);
+            out[3][p] = hfma2(wh & kOddW, c[p].y, c[p].z);
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int d = 32 * GG + 4 * g + e;               // operand row; tokens 16 cw + 8 pg ..
+            const int d = 32 * GG + 4 * (word >> 2) + ((e + GG) & 3);        // operand row
             *(uint4*)(bp + kOffVw + b * kOpBytes + d * 128 + (((2 * cw + pg) ^ (d & 7)) << 4)) =
                 make_uint4(out[e][0], out[e][1], out[e][2], out[e][3]);
           }
@@ -443,20 +456,22 @@ attn_q4_wide_kernel(const AttnArgs a, int item_begin) {
         uint32_t o[32];
         TMEM_LD_32((tmem + 128u + 32u * c) | lane_sel, o, 0);
         tmem_wait_ld();
+        auto at = [&](int j) { return o[(j & ~3) | ((j + c) & 3)]; };        // dim 32 c + j
         if (row < R) {
           if (user.slot < 0) {
             uint4* dst = (uint4*)((__nv_bfloat16*)a.out + ((size_t)user.query * HQ + head) * kDim) + 4 * c;
 #pragma unroll
-            for (int j = 0; j < 32; j += 8)
-              dst[j >> 3] = make_uint4(
-                  pack2(__uint_as_float(o[j]) * inv, __uint_as_float(o[j + 1]) * inv),
-                  pack2(__uint_as_float(o[j + 2]) * inv, __uint_as_float(o[j + 3]) * inv),
-                  pack2(__uint_as_float(o[j + 4]) * inv, __uint_as_float(o[j + 5]) * inv),
-                  pack2(__uint_as_float(o[j + 6]) * inv, __uint_as_float(o[j + 7]) * inv));
+            for (int j = 0; j < 32; j += 8) {
+              uint32_t w[4];
+#pragma unroll
+              for (int p = 0; p < 4; ++p)
+                w[p] = pack2(__uint_as_float(at(j + 2 * p)) * inv, __uint_as_float(at(j + 2 * p + 1)) * inv);
+              dst[j >> 3] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
           } else {
             uint4* dst = (uint4*)(a.part_o + prow * kDim) + 8 * c;
 #pragma unroll
-            for (int j = 0; j < 32; j += 4) dst[j >> 2] = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
+            for (int j = 0; j < 32; j += 4) dst[j >> 2] = make_uint4(at(j), at(j + 1), at(j + 2), at(j + 3));
           }
         }
       }
