@@ -405,7 +405,7 @@ apar_status launch_plan(apar_ctx* c, int layer, const void* q, void* out, float 
   if (c->q4) {
     const Q4Items& it = c->q4_items;
     if (it.n_wide) {
-      APAR_CUDA(c, launch_attention_q4_wide(a, 0, it.n_wide, st));
+      APAR_CUDA(c, launch_attention_q4_wide(a, it.n_wide, st));
       ++*launches_out;
     }
     if (it.n_mid + it.n_narrow) {

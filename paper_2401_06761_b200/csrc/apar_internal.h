@@ -233,7 +233,7 @@ struct Q4Units {                    // (an item and a kv head each)
 };
 // Both use no a.tm_k / a.tm_v / a.d_ticket.  a.pdl: the launch may start before the wide one
 // directly before it has finished.
-cudaError_t launch_attention_q4_wide(const AttnArgs& a, int item_begin, int n_items, cudaStream_t st);
+cudaError_t launch_attention_q4_wide(const AttnArgs& a, int n_items, cudaStream_t st);
 cudaError_t launch_attention_q4(const AttnArgs& a, const Q4Items& items, cudaStream_t st);
 // Merge of partial results; a.pdl: it may be launched before the attention kernel has finished.
 // max_parts: parts of the row that has most.

@@ -4,8 +4,10 @@
 //
 // mma.sync has to turn the codes of a block into operand registers once per eight rows, which for
 // 64 rows costs eight times the arithmetic of one; here a block is turned into f16 operand tiles in
-// shared memory once for all of an item's rows.  A CTA owns one item and kv head (at most 64
-// rows) and walks its run in tiles of 64 tokens, two CTAs to an SM:
+// shared memory once for all of an item's rows.  A unit is one item and kv head (at most 64 rows),
+// walked in tiles of 64 tokens; two persistent CTAs per SM take units in the planner's order, forwards
+// and backwards in turn, and every role runs on from one unit into the next (a CTA per unit spent
+// some 6 us on each: 92 of 178 us of a case whose roles did nothing else):
 //   warps 2-5  one block of the tile each: its 4-bit K and V tiles arrive through a private cp.async
 //              ring, two tiles ahead, and leave as f16 operands.  K' = K 2^-(E + 8) with E the
 //              exponent of the block's largest value, V' = V 2^-(F + 8) with F that of the token's,
@@ -51,7 +53,7 @@ constexpr int kOffTok = kOffRaw + kConv * kDepthW * kBlk;     // [2] F + 8 and 2
 constexpr int kOffKb = kOffTok + 2 * 2 * kTok * 4;            // [2][4] 2^(E + 8)
 constexpr int kOffBarW = kOffKb + 2 * 4 * 4;
 enum { BW_KFULL = 0, BW_KEMPTY = 2, BW_VFULL = 4, BW_VEMPTY = 6, BW_SFULL = 8, BW_PFULL = 10,
-       BW_PVDONE = 12, BW_TOTAL = 14 };
+       BW_PVDONE = 12, BW_QFULL = 14, BW_ODONE = 15, BW_TOTAL = 16 };
 constexpr int kSmemWide = kOffBarW + 8 * BW_TOTAL + 16 + 1024;
 static_assert(2 * (kSmemWide + 1024) <= 228 * 1024, "two CTAs per SM");
 constexpr int kTmemColsW = 256;                      // S at 0 and 64, O at 128
@@ -93,7 +95,7 @@ __device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
 }
 
 __global__ void __launch_bounds__(kThreads, 2)
-attn_q4_wide_kernel(const AttnArgs a, int item_begin) {
+attn_q4_wide_kernel(const AttnArgs a, int n_units) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (s32(smem_raw) + 1023u) & ~1023u;
   uint8_t* bp = smem_raw + (base - s32(smem_raw));
@@ -115,6 +117,8 @@ attn_q4_wide_kernel(const AttnArgs a, int item_begin) {
       bar_init(bar(BW_PFULL + b), 2);
       bar_init(bar(BW_PVDONE + b), 1);
     }
+    bar_init(bar(BW_QFULL), 2);
+    bar_init(bar(BW_ODONE), 2);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 6) {
@@ -122,50 +126,28 @@ attn_q4_wide_kernel(const AttnArgs a, int item_begin) {
                  ::"r"(s32((const void*)tmem_slot)), "r"(kTmemColsW) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  const WorkItem it = a.d_items[item_begin + blockIdx.x];
-  const int kvh = blockIdx.y;
-  const int tok_end = it.tok_end < 0 ? a.d_lens[it.table_row] : it.tok_end;
-  const int n_tok = tok_end - it.tok_begin;
-  const int n_blk = (n_tok + kBlock - 1) / kBlock;
-  const int n_tiles = (n_blk + kConv - 1) / kConv;
-  const int R = it.n_users * G;
-
-  // ---- query rows, in f16 under a power of two of their own
-  const int row = threadIdx.x;                       // (softmax warps)
-  float u = 0.f;                                     // scale * log2(e) / the row's factor
-  UserRef user = UserRef{0, -1};
-  int head = 0;
-  if (warp < 2) {
-    uint4 v[16];
-    uint32_t top = 0;
-#pragma unroll
-    for (int c = 0; c < 16; ++c) v[c] = make_uint4(0u, 0u, 0u, 0u);
-    if (row < R) {
-      user = a.d_users[it.user_begin + row / G];
-      head = kvh * G + row % G;
-      const uint4* src = (const uint4*)a.q + ((size_t)user.query * HQ + head) * 16;
-#pragma unroll
-      for (int c = 0; c < 16; ++c) {
-        v[c] = __ldg(src + c);
-        const uint32_t w[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
-#pragma unroll
-        for (int p = 0; p < 4; ++p) top = max(top, max(w[p] << 17, (w[p] & 0x7fff0000u) << 1));
-      }
-    }
-    const int lift = min(126, 14 + 127 - (int)(top >> 24));
-    const float f = pow2(lift);
-    u = a.scale_log2e * pow2(-lift);
-#pragma unroll
-    for (int c = 0; c < 16; ++c) {
-      const uint32_t w[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
-      uint32_t h[4];
-#pragma unroll
-      for (int p = 0; p < 4; ++p) h[p] = f16x2(bf16_lo(w[p]) * f, bf16_hi(w[p]) * f);
-      *(uint4*)(bp + (c >> 3) * kHalfOp + row * 128 + (((c & 7) ^ (row & 7)) << 4)) =
-          make_uint4(h[0], h[1], h[2], h[3]);
-    }
-    fence_async_smem();
-  }
+  // this CTA's units: number `pass` of the list, or -1
+  const int W = gridDim.x;
+  auto unit_of = [&](int pass) {
+    const int u = pass * W + ((pass & 1) ? W - 1 - (int)blockIdx.x : (int)blockIdx.x);
+    return u < n_units ? u : -1;
+  };
+  const int n_passes = (n_units + W - 1) / W;        // (the last one may have no unit for this CTA)
+  const int my_units = n_passes - (unit_of(n_passes - 1) < 0 ? 1 : 0);
+  struct Unit {
+    int row, begin, n_tok, n_tiles, kvh;
+  };
+  auto describe = [&](int pass) {
+    const int u = unit_of(pass);
+    const WorkItem& it = a.d_items[u / HKV];
+    Unit d;
+    d.row = it.table_row;
+    d.begin = it.tok_begin;
+    d.n_tok = (it.tok_end < 0 ? a.d_lens[d.row] : it.tok_end) - d.begin;
+    d.n_tiles = (d.n_tok + kTok - 1) / kTok;
+    d.kvh = u % HKV;
+    return d;
+  };
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -177,36 +159,54 @@ attn_q4_wide_kernel(const AttnArgs a, int item_begin) {
     // ---------------------------------------------------------------- converters
     const int cw = warp - 2;
     const uint32_t raw = base + kOffRaw + cw * kDepthW * kBlk;
-    const int32_t* table = a.d_tables + (size_t)it.table_row * a.shape.table_stride +
-                           it.tok_begin / kBlock;
-    auto issue = [&](int t, int bid) {               // this warp's block of tile t
-      const size_t tile = ((size_t)bid * HKV + kvh) * kQ4TileBytes + lane * 16;
-      const uint8_t* kt = (const uint8_t*)a.k_pool + tile;
-      const uint8_t* vt = (const uint8_t*)a.v_pool + tile - kQ4TileBytes;
-      const uint32_t dst = raw + (t % kDepthW) * kBlk + lane * 16;
-      cp16(dst, kt);
-      cp16(dst + 512, kt + 512);
-      cp16(dst + 1024, (lane < 16 ? kt : vt) + 1024);
-      cp16(dst + 1536, vt + 1536);
-      cp16(dst + 2048, vt + 2048);
-    };
-#pragma unroll
-    for (int t = 0; t < kDepthW - 1; ++t) {
-      if (t * kConv + cw < n_blk) issue(t, table[t * kConv + cw]);
+    // the loads run kDepthW - 1 tiles ahead, into the next units too
+    Unit lu = {0, 0, 0, 0, 0}, nu = my_units ? describe(0) : lu;   // the loads' unit; the one after it
+    int l_pass = -1, l_t = 0, l_slot = 0, l_bid = 0;
+    const int32_t* l_tab = nullptr;
+    auto load_tile = [&]() {                         // this warp's block of the next tile, if any
+      if (l_t == lu.n_tiles && l_pass + 1 < my_units) {
+        lu = nu;
+        ++l_pass;
+        l_t = 0;
+        l_tab = a.d_tables + (size_t)lu.row * a.shape.table_stride + lu.begin / kBlock;
+        l_bid = cw * kBlock < lu.n_tok ? l_tab[cw] : 0;
+        if (l_pass + 1 < my_units) nu = describe(l_pass + 1);
+      }
+      if (l_t < lu.n_tiles) {
+        if ((l_t * kConv + cw) * kBlock < lu.n_tok) {
+          const size_t tile = ((size_t)l_bid * HKV + lu.kvh) * kQ4TileBytes + lane * 16;
+          const uint8_t* kt = (const uint8_t*)a.k_pool + tile;
+          const uint8_t* vt = (const uint8_t*)a.v_pool + tile - kQ4TileBytes;
+          const uint32_t dst = raw + l_slot * kBlk + lane * 16;
+          cp16(dst, kt);
+          cp16(dst + 512, kt + 512);
+          cp16(dst + 1024, (lane < 16 ? kt : vt) + 1024);
+          cp16(dst + 1536, vt + 1536);
+          cp16(dst + 2048, vt + 2048);
+        }
+        ++l_t;
+        const int nb = l_t * kConv + cw;
+        if (nb * kBlock < lu.n_tok) l_bid = l_tab[nb];         // (arrives while a tile is converted)
+      }
+      l_slot = l_slot == kDepthW - 1 ? 0 : l_slot + 1;
       asm volatile("cp.async.commit_group;" ::: "memory");
-    }
-    auto id_of = [&](int t) { return t * kConv + cw < n_blk ? table[t * kConv + cw] : 0; };
-    int next_bid = id_of(kDepthW - 1);
-    for (int t = 0; t < n_tiles; ++t) {
-      const int b = t & 1;
+    };
+#pragma unroll 1
+    for (int i = 0; i < kDepthW - 1; ++i) load_tile();
+    int T = 0, slot = 0;                             // tiles of all units
+    bool ok = true;
+#pragma unroll 1
+    for (int pass = 0; pass < my_units && ok; ++pass) {
+      const Unit cu = describe(pass);                // (in the L1 cache by now)
+#pragma unroll 1
+    for (int t = 0; t < cu.n_tiles; ++t, ++T, slot = slot == kDepthW - 1 ? 0 : slot + 1) {
+      const int b = T & 1;
       asm volatile("cp.async.wait_group %0;" ::"n"(kDepthW - 2) : "memory");
       __syncwarp();
-      if ((t + kDepthW - 1) * kConv + cw < n_blk) issue(t + kDepthW - 1, next_bid);
-      asm volatile("cp.async.commit_group;" ::: "memory");
-      next_bid = id_of(t + kDepthW);
-      const uint8_t* kt = bp + (raw - base) + (t % kDepthW) * kBlk;
+      load_tile();
+      const uint8_t* kt = bp + (raw - base) + slot * kBlk;
       const uint8_t* vt = kt + kQ4TileBytes;
-      const int nv = n_tok - (t * kConv + cw) * kBlock;      // tokens of the block that count
+      const int nv = cu.n_tok - (t * kConv + cw) * kBlock;   // tokens of the block that count
 
       // ---- K: lane = (operand row, half of its 16-byte pieces)
       int ek;
@@ -223,9 +223,11 @@ attn_q4_wide_kernel(const AttnArgs a, int item_begin) {
         for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
         ek = exponent_of(top) + kLift;
         const float down = pow2(-ek), up = down * 16777216.f;
-        if (t >= 2 && !__all_sync(0xffffffffu, bar_wait(bar(BW_KEMPTY + b), ((t >> 1) - 1) & 1, cta_abort,
-                                                        a.d_error, 23000)))
+        if (T >= 2 && !__all_sync(0xffffffffu, bar_wait(bar(BW_KEMPTY + b), ((T >> 1) - 1) & 1, cta_abort,
+                                                        a.d_error, 23000))) {
+          ok = false;
           break;
+        }
         const uint32_t w0[4] = {c0.x, c0.y, c0.z, c0.w}, w1[4] = {c1.x, c1.y, c1.z, c1.w};
         const int r = cw * kBlock + pos;
         uint8_t* dst = bp + kOffK + b * kOpBytes + r * 128;
@@ -247,9 +249,11 @@ attn_q4_wide_kernel(const AttnArgs a, int item_begin) {
         if (lane == 0) bar_arrive(bar(BW_KFULL + b));
       }
       // ---- V: constants of (pair, group), then words of four pairs at a time
-      if (t >= 2 && !__all_sync(0xffffffffu, bar_wait(bar(BW_VEMPTY + b), ((t >> 1) - 1) & 1, cta_abort,
-                                                      a.d_error, 23100)))
+      if (T >= 2 && !__all_sync(0xffffffffu, bar_wait(bar(BW_VEMPTY + b), ((T >> 1) - 1) & 1, cta_abort,
+                                                      a.d_error, 23100))) {
+        ok = false;
         break;
+      }
       {
         uint8_t* const vc = const_cast<uint8_t*>(kt);        // [pair][group]: K has been read
         const int pair = lane >> 2, g4 = lane & 3;
@@ -313,16 +317,51 @@ attn_q4_wide_kernel(const AttnArgs a, int item_begin) {
         if (lane == 0) bar_arrive(bar(BW_VFULL + b));
       }
     }
+    }
     asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp == 2 + kConv) {
     // ---------------------------------------------------------------- MMA issuer
     constexpr uint32_t kIdescQK = instr_desc_f16(kTok, 128), kIdescPV = instr_desc_f16(kDim, 128);
     constexpr unsigned kAll = 0xffffffffu;
-    for (int t = 0; t <= n_tiles; ++t) {
-      if (t < n_tiles) {
-        const int b = t & 1;
-        if (!__all_sync(kAll, bar_wait(bar(BW_KFULL + b), (t >> 1) & 1, cta_abort, a.d_error, 24000)))
+    int T = 0, due = -1;                             // tiles so far; the tile whose P V is due
+    bool due_first = false, ok = true;
+    int due_pass = 0;
+    auto product_pv = [&]() -> bool {
+      const int b = due & 1;
+      bool w8 = bar_wait(bar(BW_PFULL + b), (due >> 1) & 1, cta_abort, a.d_error, 24100);
+      w8 = w8 && bar_wait(bar(BW_VFULL + b), (due >> 1) & 1, cta_abort, a.d_error, 24200);
+      if (due_first && due_pass > 0)                 // the unit before has read its O out
+        w8 = w8 && bar_wait(bar(BW_ODONE), (due_pass - 1) & 1, cta_abort, a.d_error, 24300);
+      if (!__all_sync(kAll, w8)) return false;
+      tc_fence_after();
+      if (lane == 0) {
+#pragma unroll
+        for (int kk = 0; kk < kTok / 16; ++kk)
+          umma_bf16_ts(tmem + 128u, tmem + 64u * b + 8u * kk,
+                       smem_desc(base + kOffVw + b * kOpBytes + kk * 32, 16, 1024), kIdescPV,
+                       !due_first || kk > 0);
+        umma_commit(bar(BW_VEMPTY + b));
+        umma_commit(bar(BW_PVDONE + b));
+      }
+      __syncwarp();
+      due = -1;
+      return true;
+    };
+    for (int pass = 0; pass < my_units && ok; ++pass) {
+      const int n_tiles = describe(pass).n_tiles;
+      for (int t = 0; t < n_tiles; ++t, ++T) {
+        const int b = T & 1;
+        // between units the last P V goes first: the rows of the next unit come after it
+        if (t == 0 && due >= 0 && !product_pv()) {
+          ok = false;
           break;
+        }
+        bool w8 = bar_wait(bar(BW_KFULL + b), (T >> 1) & 1, cta_abort, a.d_error, 24000);
+        if (t == 0) w8 = w8 && bar_wait(bar(BW_QFULL), pass & 1, cta_abort, a.d_error, 24400);
+        if (!__all_sync(kAll, w8)) {
+          ok = false;
+          break;
+        }
         tc_fence_after();
         if (lane == 0) {
 #pragma unroll
@@ -335,35 +374,82 @@ attn_q4_wide_kernel(const AttnArgs a, int item_begin) {
           umma_commit(bar(BW_KEMPTY + b));
         }
         __syncwarp();
-      }
-      if (t > 0) {
-        const int p = t - 1, b = p & 1;
-        bool ok = bar_wait(bar(BW_PFULL + b), (p >> 1) & 1, cta_abort, a.d_error, 24100);
-        ok = ok && bar_wait(bar(BW_VFULL + b), (p >> 1) & 1, cta_abort, a.d_error, 24200);
-        if (!__all_sync(kAll, ok)) break;
-        tc_fence_after();
-        if (lane == 0) {
-#pragma unroll
-          for (int kk = 0; kk < kTok / 16; ++kk)
-            umma_bf16_ts(tmem + 128u, tmem + 64u * b + 8u * kk,
-                         smem_desc(base + kOffVw + b * kOpBytes + kk * 32, 16, 1024), kIdescPV,
-                         p > 0 || kk > 0);
-          umma_commit(bar(BW_VEMPTY + b));
-          umma_commit(bar(BW_PVDONE + b));
+        if (due >= 0 && !product_pv()) {
+          ok = false;
+          break;
         }
-        __syncwarp();
+        due = T;
+        due_first = t == 0;
+        due_pass = pass;
       }
     }
+    if (ok && due >= 0) product_pv();
   } else if (warp < 2) {
     // ---------------------------------------------------------------- softmax: a thread, a row
     const uint32_t lane_sel = (uint32_t)(warp * 32) << 16;
-    const bool idle = warp * 32 >= R;                // (no rows here: only keeps the phases)
-    float ref = kNoRefW, l = 0.f;
+    const int row = threadIdx.x;
+    float u = 0.f;                                   // scale * log2(e) / the row's factor
+    // what a unit's rows are and where they go
+    struct Rows {
+      int query, slot, head, count;                  // slot < 0: the output; count: rows of the unit
+    } cur, nxt;
+    // Query rows of a unit into the operand, in f16 under a power of two of their own.  The
+    // products of the unit before with its rows are complete: their scores have been read.
+    auto stage_rows = [&](int pass) {
+      const int un = unit_of(pass);
+      const WorkItem& it = a.d_items[un / HKV];
+      const int kvh = un % HKV;
+      nxt.count = it.n_users * G;
+      nxt.head = kvh * G + row % G;
+      nxt.query = 0;
+      nxt.slot = -1;
+      uint4 v[16];
+      uint32_t top = 0;
+#pragma unroll
+      for (int c = 0; c < 16; ++c) v[c] = make_uint4(0u, 0u, 0u, 0u);
+      if (row < nxt.count) {
+        const UserRef user = a.d_users[it.user_begin + row / G];
+        nxt.query = user.query;
+        nxt.slot = user.slot < 0 ? -1 : user.slot + it.slot_add;
+        const uint4* src = (const uint4*)a.q + ((size_t)user.query * HQ + nxt.head) * 16;
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {
+          v[c] = __ldg(src + c);
+          const uint32_t w[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
+#pragma unroll
+          for (int p = 0; p < 4; ++p) top = max(top, max(w[p] << 17, (w[p] & 0x7fff0000u) << 1));
+        }
+      }
+      const int lift = min(126, 14 + 127 - (int)(top >> 24));
+      const float f = pow2(lift);
+      u = a.scale_log2e * pow2(-lift);
+#pragma unroll
+      for (int c = 0; c < 16; ++c) {
+        const uint32_t w[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
+        uint32_t h[4];
+#pragma unroll
+        for (int p = 0; p < 4; ++p) h[p] = f16x2(bf16_lo(w[p]) * f, bf16_hi(w[p]) * f);
+        *(uint4*)(bp + (c >> 3) * kHalfOp + row * 128 + (((c & 7) ^ (row & 7)) << 4)) =
+            make_uint4(h[0], h[1], h[2], h[3]);
+      }
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) bar_arrive(bar(BW_QFULL));
+    };
     bool alive = true;
-    for (int t = 0; t < n_tiles; ++t) {
-      const int b = t & 1;
-      bool ok = bar_wait(bar(BW_SFULL + b), (t >> 1) & 1, cta_abort, a.d_error, 22000);
-      ok = ok && bar_wait(bar(BW_VFULL + b), (t >> 1) & 1, cta_abort, a.d_error, 22100);
+    int T = 0;
+    if (my_units) stage_rows(0);
+#pragma unroll 1
+    for (int pass = 0; pass < my_units; ++pass) {
+    cur = nxt;
+    const int n_tiles = describe(pass).n_tiles;
+    const bool idle = warp * 32 >= cur.count;        // (no rows here: only keeps the phases)
+    float ref = kNoRefW, l = 0.f;
+#pragma unroll 1
+    for (int t = 0; t < n_tiles; ++t, ++T) {
+      const int b = T & 1;
+      bool ok = bar_wait(bar(BW_SFULL + b), (T >> 1) & 1, cta_abort, a.d_error, 22000);
+      ok = ok && bar_wait(bar(BW_VFULL + b), (T >> 1) & 1, cta_abort, a.d_error, 22100);
       if (!__all_sync(0xffffffffu, ok)) {
         alive = false;
         break;
@@ -402,7 +488,7 @@ attn_q4_wide_kernel(const AttnArgs a, int item_begin) {
           if (t > 0) {
             // (P V of the tile before has to be complete; the phase before on its barrier is,
             // because this tile's scores came after that product)
-            if (!__all_sync(0xffffffffu, bar_wait(bar(BW_PVDONE + (b ^ 1)), ((t - 1) >> 1) & 1,
+            if (!__all_sync(0xffffffffu, bar_wait(bar(BW_PVDONE + (b ^ 1)), ((T - 1) >> 1) & 1,
                                                   cta_abort, a.d_error, 22200))) {
               alive = false;
               break;
@@ -444,22 +530,24 @@ attn_q4_wide_kernel(const AttnArgs a, int item_begin) {
       __syncwarp();
       if (lane == 0) bar_arrive(bar(BW_PFULL + b));
     }
-    alive = alive && __all_sync(0xffffffffu, bar_wait(bar(BW_PVDONE + ((n_tiles - 1) & 1)),
-                                                      ((n_tiles - 1) >> 1) & 1, cta_abort, a.d_error,
-                                                      22300));
-    if (alive && !idle) {
-      tc_fence_after();
-      const float inv = user.slot < 0 ? 1.f / l : 1.f;
-      const size_t prow = (size_t)(user.slot + it.slot_add) * HQ + head;
+    if (!alive) break;
+    if (pass + 1 < my_units) stage_rows(pass + 1);
+    if (!__all_sync(0xffffffffu, bar_wait(bar(BW_PVDONE + ((T - 1) & 1)), ((T - 1) >> 1) & 1, cta_abort,
+                                          a.d_error, 22300)))
+      break;
+    tc_fence_after();
+    if (!idle) {
+      const float inv = cur.slot < 0 ? 1.f / l : 1.f;
+      const size_t prow = (size_t)cur.slot * HQ + cur.head;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         uint32_t o[32];
         TMEM_LD_32((tmem + 128u + 32u * c) | lane_sel, o, 0);
         tmem_wait_ld();
         auto at = [&](int j) { return o[(j & ~3) | ((j + c) & 3)]; };        // dim 32 c + j
-        if (row < R) {
-          if (user.slot < 0) {
-            uint4* dst = (uint4*)((__nv_bfloat16*)a.out + ((size_t)user.query * HQ + head) * kDim) + 4 * c;
+        if (row < cur.count) {
+          if (cur.slot < 0) {
+            uint4* dst = (uint4*)((__nv_bfloat16*)a.out + ((size_t)cur.query * HQ + cur.head) * kDim) + 4 * c;
 #pragma unroll
             for (int j = 0; j < 32; j += 8) {
               uint32_t w[4];
@@ -475,7 +563,11 @@ attn_q4_wide_kernel(const AttnArgs a, int item_begin) {
           }
         }
       }
-      if (row < R && user.slot >= 0) a.part_ml[prow] = make_float2(ref, l);
+      if (row < cur.count && cur.slot >= 0) a.part_ml[prow] = make_float2(ref, l);
+    }
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) bar_arrive(bar(BW_ODONE));
     }
   }
   // ---- common exit: every role arrives here, then the allocating warp frees TMEM
@@ -490,8 +582,10 @@ attn_q4_wide_kernel(const AttnArgs a, int item_begin) {
 
 }  // namespace
 
-cudaError_t launch_attention_q4_wide(const AttnArgs& a, int item_begin, int n_items, cudaStream_t st) {
+cudaError_t launch_attention_q4_wide(const AttnArgs& a, int n_items, cudaStream_t st) {
   if (n_items <= 0) return cudaSuccess;
+  const int64_t units = (int64_t)n_items * a.shape.num_kv_heads;
+  if (units > INT32_MAX - (1 << 20)) return cudaErrorInvalidValue;
   static bool configured[64] = {};
   int dev = 0;
   cudaGetDevice(&dev);
@@ -502,7 +596,8 @@ cudaError_t launch_attention_q4_wide(const AttnArgs& a, int item_begin, int n_it
     if (e != cudaSuccess) return e;
     configured[dev] = true;
   }
-  attn_q4_wide_kernel<<<dim3(n_items, a.shape.num_kv_heads), kThreads, kSmemWide, st>>>(a, item_begin);
+  const int ctas = (int)std::min<int64_t>(units, 2 * a.num_sms);
+  attn_q4_wide_kernel<<<ctas, kThreads, kSmemWide, st>>>(a, (int)units);
   return cudaGetLastError();
 }
 
