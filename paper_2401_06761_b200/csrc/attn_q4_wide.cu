@@ -8,19 +8,21 @@
 // walked in tiles of 64 tokens; two persistent CTAs per SM take units in the planner's order, forwards
 // and backwards in turn, and every role runs on from one unit into the next (a CTA per unit spent
 // some 6 us on each: 92 of 178 us of a case whose roles did nothing else):
-//   warps 2-5  one block of the tile each: its 4-bit K and V tiles arrive through a private cp.async
-//              ring, two tiles ahead, and leave as f16 operands.  K' = K 2^-(E + 8) with E the
+//   warps 4-7  one block of the tile each: its 4-bit K and V tiles arrive through a private cp.async
+//              ring, a tile ahead, and leave as f16 operands.  K' = K 2^-(E + 8) with E the
 //              exponent of the block's largest value, V' = V 2^-(F + 8) with F that of the token's,
 //              so that f16's range is never an issue; a code enters the conversion as the
-//              subnormal number it is in place (c * 2^-24, or * 2^-20 a nibble up), one
-//              fused multiply-add per pair of values.
-//   warp 6     issues S = Q K'^T (M 128, N 64, K 128) and, one tile behind, O += P V' (M 128, N 128,
-//              K 64, P from tensor memory).  Rows past 63 of the A operands are whatever lies
-//              there; their results are not read.  (M 64 takes the pipe just as long.)
-//   warps 0-1  one thread per row: x = S u 2^(E + 8) + F + 8, P = 2^(x - ref) in f16, its sum less
-//              the token's factor in 32 bits, and P back over the scores it came from.  The
-//              reference follows score and size of V together and moves lazily, as in attn_q4.cu.
-// K, V and S are double-buffered.  Both operands and the weights are rounded to 11 bits (K' and V'
+//              subnormal number it is in place (c * 2^-24, or * 2^-20 a nibble up), one fused
+//              multiply-add per pair of values.
+//   warp 8     issues S = Q K'^T (M 64, N 64, K 128) and, one tile behind, O += P V' (M 64, N 128, K 64).
+//   warps 0-3  16 rows each, a row's scores spread over a quad: x = S u 2^(E + 8) + F + 8,
+//              P = 2^(x - ref) in f16, its sum less the token's factor in 32 bits, P to shared memory
+//              as an operand.  The reference follows score and size of V together and moves
+//              lazily, as in attn_q4.cu.
+// What bounds it is shared memory: operands are written and read there, next to the constants of
+// the tokens.  With a thread per row (M 128, P in tensor memory) every thread read every token's
+// constants, which took a quarter of the shared-memory cycles.
+// K', V' and S are double-buffered.  Both operands and the weights are rounded to 11 bits (K' and V'
 // of values far below their maximum to 2^-18 of it), against eight of the output.
 // All waits are bounded; a wait that gives up raises the error word and every role unwinds to the
 // common exit where TMEM is released.
@@ -39,22 +41,24 @@
 namespace apar {
 namespace {
 
-constexpr int kTok = 64;                             // tokens of a tile: one block per converter warp
-constexpr int kConv = 4;                             // converter warps
-constexpr int kThreads = 32 * (2 + kConv + 1);
+constexpr int kTok = 64;                             // tokens of a tile
+constexpr int kConv = 4, kSoftmax = 4;               // warps
+constexpr int kThreads = 32 * (kSoftmax + kConv + 1);
 constexpr int kBlk = 2 * kQ4TileBytes;               // K and V of one block, as stored
-constexpr int kDepthW = 3;                           // blocks of a converter's ring
+constexpr int kDepthW = 2;                           // blocks of a converter's ring
 constexpr int kHalfOp = 64 * 128;                    // 64 rows x 64 dims f16, 128-byte swizzle
 constexpr int kOpBytes = 2 * kHalfOp;                // K' or V' of a tile, or Q
-constexpr int kOffK = kOpBytes;                      // (Q first: its rows 64..127 run into K')
+constexpr int kOffK = kOpBytes;
 constexpr int kOffVw = kOffK + 2 * kOpBytes;
-constexpr int kOffRaw = kOffVw + 2 * kOpBytes;
+constexpr int kOffP = kOffVw + 2 * kOpBytes;         // P: 64 rows x 64 tokens f16
+constexpr int kOffRaw = kOffP + kHalfOp;
 constexpr int kOffTok = kOffRaw + kConv * kDepthW * kBlk;     // [2] F + 8 and 2^-(F + 8) of 64 tokens
 constexpr int kOffKb = kOffTok + 2 * 2 * kTok * 4;            // [2][4] 2^(E + 8)
-constexpr int kOffBarW = kOffKb + 2 * 4 * 4;
+constexpr int kOffRow = kOffKb + 2 * 4 * 4;                   // [64] the rows' factors
+constexpr int kOffBarW = kOffRow + 64 * 4;
 enum { BW_KFULL = 0, BW_KEMPTY = 2, BW_VFULL = 4, BW_VEMPTY = 6, BW_SFULL = 8, BW_PFULL = 10,
-       BW_PVDONE = 12, BW_QFULL = 14, BW_ODONE = 15, BW_TOTAL = 16 };
-constexpr int kSmemWide = kOffBarW + 8 * BW_TOTAL + 16 + 1024;
+       BW_PVDONE = 11, BW_QFULL = 12, BW_ODONE = 13, BW_TOTAL = 14 };
+constexpr int kSmemWide = kOffBarW + 8 * BW_TOTAL + 16;
 static_assert(2 * (kSmemWide + 1024) <= 228 * 1024, "two CTAs per SM");
 constexpr int kTmemColsW = 256;                      // S at 0 and 64, O at 128
 constexpr float kSlackW = 8.f;
@@ -90,15 +94,32 @@ __device__ __forceinline__ float group_top(uint32_t sl) {
 __device__ __forceinline__ int token_at(int pos) {
   return (pos & 3) | ((pos & 4) << 1) | ((pos & 8) >> 1);
 }
+#define TMEM_LD_16(taddr, r)                                                                     \
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 "                                         \
+               "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"                  \
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]),         \
+                 "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),       \
+                 "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])                              \
+               : "r"(taddr))
+#define TMEM_ST_16(taddr, r)                                                                     \
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "                                   \
+               "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"                        \
+               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]),   \
+                 "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), \
+                 "r"(r[13]), "r"(r[14]), "r"(r[15])                                              \
+               : "memory")
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 
 __global__ void __launch_bounds__(kThreads, 2)
 attn_q4_wide_kernel(const AttnArgs a, int n_units) {
-  extern __shared__ uint8_t smem_raw[];
-  const uint32_t base = (s32(smem_raw) + 1023u) & ~1023u;
-  uint8_t* bp = smem_raw + (base - s32(smem_raw));
+  extern __shared__ __align__(1024) uint8_t bp[];    // (swizzled operands want 1024)
+  const uint32_t base = s32(bp);
+  if (base & 1023u) {                                // no room to round it up: refuse
+    if (threadIdx.x == 0) atomicCAS(a.d_error, 0, 25000);
+    return;
+  }
   auto bar = [&](int i) { return base + kOffBarW + 8u * i; };
   volatile int* cta_abort = (volatile int*)(bp + kOffBarW + 8 * BW_TOTAL);
   volatile uint32_t* tmem_slot = (volatile uint32_t*)(bp + kOffBarW + 8 * BW_TOTAL + 8);
@@ -114,14 +135,14 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
       bar_init(bar(BW_VFULL + b), kConv);
       bar_init(bar(BW_VEMPTY + b), 1);
       bar_init(bar(BW_SFULL + b), 1);
-      bar_init(bar(BW_PFULL + b), 2);
-      bar_init(bar(BW_PVDONE + b), 1);
     }
-    bar_init(bar(BW_QFULL), 2);
-    bar_init(bar(BW_ODONE), 2);
+    bar_init(bar(BW_PFULL), kSoftmax);
+    bar_init(bar(BW_PVDONE), 1);
+    bar_init(bar(BW_QFULL), kSoftmax);
+    bar_init(bar(BW_ODONE), kSoftmax);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 6) {
+  if (warp == 8) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                  ::"r"(s32((const void*)tmem_slot)), "r"(kTmemColsW) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -155,9 +176,9 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
 
   if (*cta_abort) {
     // nothing is started
-  } else if (warp >= 2 && warp < 2 + kConv) {
+  } else if (warp >= kSoftmax && warp < kSoftmax + kConv) {
     // ---------------------------------------------------------------- converters
-    const int cw = warp - 2;
+    const int cw = warp - kSoftmax;
     const uint32_t raw = base + kOffRaw + cw * kDepthW * kBlk;
     // the loads run kDepthW - 1 tiles ahead, into the next units too
     Unit lu = {0, 0, 0, 0, 0}, nu = my_units ? describe(0) : lu;   // the loads' unit; the one after it
@@ -208,20 +229,57 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
       const uint8_t* vt = kt + kQ4TileBytes;
       const int nv = cu.n_tok - (t * kConv + cw) * kBlock;   // tokens of the block that count
 
-      // ---- K: lane = (operand row, half of its 16-byte pieces)
-      int ek;
-      {
-        const int pos = lane & 15, h = lane >> 4, tok = token_at(pos);
-        uint4 sc = *(const uint4*)(kt + tok * kQ4RowBytes + kQ4CodeBytes);
-        const uint4 c0 = *(const uint4*)(kt + tok * kQ4RowBytes + 32 * h);
-        const uint4 c1 = *(const uint4*)(kt + tok * kQ4RowBytes + 32 * h + 16);
-        if (tok >= nv) sc = make_uint4(0u, 0u, 0u, 0u);      // (unspecified bits: the row is zeros)
-        const uint32_t sl[4] = {sc.x, sc.y, sc.z, sc.w};
-        float top = fmaxf(fmaxf(group_top(sl[0]), group_top(sl[1])),
-                          fmaxf(group_top(sl[2]), group_top(sl[3])));
+      // ---- what the tile holds, and the factors (both chains of shuffles at once)
+      // K: lane = (operand row, half of its 16-byte pieces).  V: lane = (pair, group) for the
+      // factors; then its group is that of its words, lane % 4, in both rounds, and its pairs are
+      // those of operand columns 8 pg .. 8 pg + 7.
+      const int pos = lane & 15, h = lane >> 4, tok = token_at(pos);
+      const int pair = lane >> 2, g4 = lane & 3, pg = lane >> 4, GG = lane & 3;
+      uint4 sc = *(const uint4*)(kt + tok * kQ4RowBytes + kQ4CodeBytes);
+      const uint8_t* vsc = vt + pair * kQ4PairBytes + 2 * kQ4CodeBytes + 4 * g4;
+      uint32_t se = *(const uint32_t*)vsc, so = *(const uint32_t*)(vsc + 16);
+      const uint4 c0 = *(const uint4*)(kt + tok * kQ4RowBytes + 32 * h);
+      const uint4 c1 = *(const uint4*)(kt + tok * kQ4RowBytes + 32 * h + 16);
+      uint32_t w[2][4];
 #pragma unroll
-        for (int d = 1; d < 16; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-        ek = exponent_of(top) + kLift;
+      for (int p = 0; p < 4; ++p)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)                          // word 4 g + G
+          w[i][p] = *(const uint32_t*)(vt + (token_at(8 * pg + 2 * p) >> 1) * kQ4PairBytes +
+                                       4 * ((lane & 15) + 16 * i));
+      if (tok >= nv) sc = make_uint4(0u, 0u, 0u, 0u);        // (unspecified bits: the row is zeros)
+      if (2 * pair >= nv) se = 0u;
+      if (2 * pair + 1 >= nv) so = 0u;
+      const uint32_t sl[4] = {sc.x, sc.y, sc.z, sc.w};
+      float top = fmaxf(fmaxf(group_top(sl[0]), group_top(sl[1])),
+                        fmaxf(group_top(sl[2]), group_top(sl[3])));
+      float te = group_top(se), to = group_top(so);
+#pragma unroll
+      for (int d = 1; d < 16; d <<= 1) {
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        if (d <= 2) {
+          te = fmaxf(te, __shfl_xor_sync(0xffffffffu, te, d));
+          to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, d));
+        }
+      }
+      const int ek = exponent_of(top) + kLift;
+      const int ee = exponent_of(te) + kLift, eo = exponent_of(to) + kLift;
+      uint32_t v1[4], v16[4], vl[4];                         // of the four pairs
+      {
+        const float de = pow2(-ee), dn = pow2(-eo);
+        const float s0 = bf16_lo(se) * (de * 16777216.f), s1 = bf16_lo(so) * (dn * 16777216.f);
+        const uint32_t x1 = f16x2(s0, s1), x16 = f16x2(s0 * 0.0625f, s1 * 0.0625f);
+        const uint32_t xl = f16x2(bf16_hi(se) * de, bf16_hi(so) * dn);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {                        // from the lanes that made them
+          const int from = (token_at(8 * pg + 2 * p) >> 1) * 4 + GG;
+          v1[p] = __shfl_sync(0xffffffffu, x1, from);
+          v16[p] = __shfl_sync(0xffffffffu, x16, from);
+          vl[p] = __shfl_sync(0xffffffffu, xl, from);
+        }
+      }
+      // ---- K
+      {
         const float down = pow2(-ek), up = down * 16777216.f;
         if (T >= 2 && !__all_sync(0xffffffffu, bar_wait(bar(BW_KEMPTY + b), ((T >> 1) - 1) & 1, cta_abort,
                                                         a.d_error, 23000))) {
@@ -237,73 +295,42 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
           const uint32_t s1 = f16x2(s, s), s16 = f16x2(s * 0.0625f, s * 0.0625f), lo2 = f16x2(lo, lo);
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            const uint32_t w = x ? w1[j] : w0[j], wh = w >> 8;
+            const uint32_t kw = x ? w1[j] : w0[j], kh = kw >> 8;
             const int c = 4 * j + 2 * h + x;                 // dims 8 c .. 8 c + 7
             *(uint4*)(dst + (c >> 3) * kHalfOp + (((c & 7) ^ (r & 7)) << 4)) =
-                make_uint4(hfma2(w & kEvenW, s1, lo2), hfma2(w & kOddW, s16, lo2),
-                           hfma2(wh & kEvenW, s1, lo2), hfma2(wh & kOddW, s16, lo2));
+                make_uint4(hfma2(kw & kEvenW, s1, lo2), hfma2(kw & kOddW, s16, lo2),
+                           hfma2(kh & kEvenW, s1, lo2), hfma2(kh & kOddW, s16, lo2));
           }
         }
         fence_async_smem();
         __syncwarp();
         if (lane == 0) bar_arrive(bar(BW_KFULL + b));
       }
-      // ---- V: constants of (pair, group), then words of four pairs at a time
-      if (T >= 2 && !__all_sync(0xffffffffu, bar_wait(bar(BW_VEMPTY + b), ((T >> 1) - 1) & 1, cta_abort,
-                                                      a.d_error, 23100))) {
-        ok = false;
-        break;
-      }
+      // ---- V
       {
-        uint8_t* const vc = const_cast<uint8_t*>(kt);        // [pair][group]: K has been read
-        const int pair = lane >> 2, g4 = lane & 3;
-        const uint8_t* sc = vt + pair * kQ4PairBytes + 2 * kQ4CodeBytes + 4 * g4;
-        uint32_t se = *(const uint32_t*)sc, so = *(const uint32_t*)(sc + 16);
-        if (2 * pair >= nv) se = 0u;
-        if (2 * pair + 1 >= nv) so = 0u;
-        float te = group_top(se), to = group_top(so);
-#pragma unroll
-        for (int d = 1; d <= 2; d <<= 1) {
-          te = fmaxf(te, __shfl_xor_sync(0xffffffffu, te, d));
-          to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, d));
+        if (T >= 2 && !__all_sync(0xffffffffu, bar_wait(bar(BW_VEMPTY + b), ((T >> 1) - 1) & 1,
+                                                        cta_abort, a.d_error, 23200))) {
+          ok = false;
+          break;
         }
-        const int fe = exponent_of(te) + kLift, fo = exponent_of(to) + kLift;
-        const float de = pow2(-fe), dn = pow2(-fo);
-        const float s0 = bf16_lo(se) * (de * 16777216.f), s1 = bf16_lo(so) * (dn * 16777216.f);
-        *(uint4*)(vc + lane * 16) = make_uint4(f16x2(s0, s1), f16x2(s0 * 0.0625f, s1 * 0.0625f),
-                                               f16x2(bf16_hi(se) * de, bf16_hi(so) * dn), 0u);
-        float* tokc = (float*)(bp + kOffTok) + b * 2 * kTok;
-        const int tk = cw * kBlock + token_at(2 * pair);     // (a pair stays together)
-        if (g4 == 0) {
-          *(float2*)(tokc + tk) = make_float2(2 * pair < nv ? (float)fe : -INFINITY,
-                                              2 * pair + 1 < nv ? (float)fo : -INFINITY);
-          *(float2*)(tokc + kTok + tk) =
-              make_float2(2 * pair < nv ? de : 0.f, 2 * pair + 1 < nv ? dn : 0.f);
+        if (g4 == 0) {                                       // (a pair stays together)
+          float* tokc = (float*)(bp + kOffTok) + b * 2 * kTok + cw * kBlock + token_at(2 * pair);
+          const bool e_on = 2 * pair < nv, o_on = 2 * pair + 1 < nv;
+          *(float2*)tokc = make_float2(e_on ? (float)ee : -INFINITY, o_on ? (float)eo : -INFINITY);
+          *(float2*)(tokc + kTok) = make_float2(e_on ? pow2(-ee) : 0.f, o_on ? pow2(-eo) : 0.f);
         }
         if (lane == 0) ((float*)(bp + kOffKb))[b * 4 + cw] = pow2(ek);
-        __syncwarp();
-        // a lane's group is that of its words, lane % 4, in both rounds; its pairs are those of
-        // operand columns 8 pg .. 8 pg + 7
-        const int pg = lane >> 4, GG = lane & 3;
-        uint4 c[4];
-        int at[4];
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {
-          const int pr = token_at(8 * pg + 2 * p) >> 1;
-          c[p] = *(const uint4*)(vc + (pr * 4 + GG) * 16);
-          at[p] = pr * kQ4PairBytes;
-        }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int word = (lane & 15) + 16 * i;             // 4 g + G
+          const int word = (lane & 15) + 16 * i;
           uint32_t out[4][4];                                // [dim][pair]
 #pragma unroll
           for (int p = 0; p < 4; ++p) {
-            const uint32_t w = *(const uint32_t*)(vt + at[p] + 4 * word), wh = w >> 8;
-            out[0][p] = hfma2(w & kEvenW, c[p].x, c[p].z);
-            out[1][p] = hfma2(w & kOddW, c[p].y, c[p].z);
-            out[2][p] = hfma2(wh & kEvenW, c[p].x, c[p].z);
-            out[3][p] = hfma2(wh & kOddW, c[p].y, c[p].z);
+            const uint32_t x = w[i][p], xh = x >> 8;
+            out[0][p] = hfma2(x & kEvenW, v1[p], vl[p]);
+            out[1][p] = hfma2(x & kOddW, v16[p], vl[p]);
+            out[2][p] = hfma2(xh & kEvenW, v1[p], vl[p]);
+            out[3][p] = hfma2(xh & kOddW, v16[p], vl[p]);
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -319,16 +346,16 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
     }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
-  } else if (warp == 2 + kConv) {
+  } else if (warp == 8) {
     // ---------------------------------------------------------------- MMA issuer
-    constexpr uint32_t kIdescQK = instr_desc_f16(kTok, 128), kIdescPV = instr_desc_f16(kDim, 128);
+    constexpr uint32_t kIdescQK = instr_desc_f16(kTok, 64), kIdescPV = instr_desc_f16(kDim, 64);
     constexpr unsigned kAll = 0xffffffffu;
     int T = 0, due = -1;                             // tiles so far; the tile whose P V is due
     bool due_first = false, ok = true;
     int due_pass = 0;
     auto product_pv = [&]() -> bool {
       const int b = due & 1;
-      bool w8 = bar_wait(bar(BW_PFULL + b), (due >> 1) & 1, cta_abort, a.d_error, 24100);
+      bool w8 = bar_wait(bar(BW_PFULL), due & 1, cta_abort, a.d_error, 24100);
       w8 = w8 && bar_wait(bar(BW_VFULL + b), (due >> 1) & 1, cta_abort, a.d_error, 24200);
       if (due_first && due_pass > 0)                 // the unit before has read its O out
         w8 = w8 && bar_wait(bar(BW_ODONE), (due_pass - 1) & 1, cta_abort, a.d_error, 24300);
@@ -337,11 +364,11 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
       if (lane == 0) {
 #pragma unroll
         for (int kk = 0; kk < kTok / 16; ++kk)
-          umma_bf16_ts(tmem + 128u, tmem + 64u * b + 8u * kk,
-                       smem_desc(base + kOffVw + b * kOpBytes + kk * 32, 16, 1024), kIdescPV,
-                       !due_first || kk > 0);
+          umma_bf16(tmem + 128u, smem_desc(base + kOffP + kk * 32, 16, 1024),
+                    smem_desc(base + kOffVw + b * kOpBytes + kk * 32, 16, 1024), kIdescPV,
+                    !due_first || kk > 0);
         umma_commit(bar(BW_VEMPTY + b));
-        umma_commit(bar(BW_PVDONE + b));
+        umma_commit(bar(BW_PVDONE));
       }
       __syncwarp();
       due = -1;
@@ -384,196 +411,251 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
       }
     }
     if (ok && due >= 0) product_pv();
-  } else if (warp < 2) {
-    // ---------------------------------------------------------------- softmax: a thread, a row
-    const uint32_t lane_sel = (uint32_t)(warp * 32) << 16;
-    const int row = threadIdx.x;
-    float u = 0.f;                                   // scale * log2(e) / the row's factor
-    // what a unit's rows are and where they go
-    struct Rows {
-      int query, slot, head, count;                  // slot < 0: the output; count: rows of the unit
-    } cur, nxt;
+  } else {
+    // ---------------------------------------------------------------- softmax
+    // Warp w owns rows 16 w .. 16 w + 15 (an M 64 accumulator keeps them in the first 16 lanes of
+    // its quarter of tensor memory); a lane works on rows g8 and g8 + 8 of them and the tokens
+    // 8 k + 2 qd, 8 k + 2 qd + 1.
+    const int g8 = lane >> 2, qd = lane & 3;
+    const uint32_t lane_sel = (uint32_t)(warp * 32) << 16, tm_o = tmem + 128u;
+    float u_lo = 0.f, u_hi = 0.f;                    // scale * log2(e) / the rows' factors
     // Query rows of a unit into the operand, in f16 under a power of two of their own.  The
     // products of the unit before with its rows are complete: their scores have been read.
-    auto stage_rows = [&](int pass) {
+    // The unit's item and the users of its rows (lane i, i < 16: row 16 w + i) are read ahead.
+    struct Rows {
+      int count, begin, add, head0;
+      UserRef user;
+    } cur, nxt;
+    auto read_item = [&](int pass, Rows& r) {
       const int un = unit_of(pass);
       const WorkItem& it = a.d_items[un / HKV];
-      const int kvh = un % HKV;
-      nxt.count = it.n_users * G;
-      nxt.head = kvh * G + row % G;
-      nxt.query = 0;
-      nxt.slot = -1;
-      uint4 v[16];
-      uint32_t top = 0;
+      r.count = it.n_users * G;
+      r.begin = it.user_begin;
+      r.add = it.slot_add;
+      r.head0 = un % HKV * G;
+    };
+    auto read_users = [&](Rows& r) {
+      const int row = warp * 16 + (lane & 15);
+      r.user = UserRef{0, -1};
+      if (row < r.count) r.user = a.d_users[r.begin + row / G];
+    };
+    auto stage_rows = [&](const Rows& rw) {
+      uint4 v[8];
 #pragma unroll
-      for (int c = 0; c < 16; ++c) v[c] = make_uint4(0u, 0u, 0u, 0u);
-      if (row < nxt.count) {
-        const UserRef user = a.d_users[it.user_begin + row / G];
-        nxt.query = user.query;
-        nxt.slot = user.slot < 0 ? -1 : user.slot + it.slot_add;
-        const uint4* src = (const uint4*)a.q + ((size_t)user.query * HQ + nxt.head) * 16;
-#pragma unroll
-        for (int c = 0; c < 16; ++c) {
-          v[c] = __ldg(src + c);
-          const uint32_t w[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
-#pragma unroll
-          for (int p = 0; p < 4; ++p) top = max(top, max(w[p] << 17, (w[p] & 0x7fff0000u) << 1));
-        }
+      for (int k = 0; k < 8; ++k) {                  // half a warp per row
+        const int i = 2 * k + (lane >> 4), r = warp * 16 + i;
+        const int query = __shfl_sync(0xffffffffu, rw.user.query, i);
+        v[k] = make_uint4(0u, 0u, 0u, 0u);
+        if (r < rw.count)
+          v[k] = __ldg((const uint4*)a.q + ((size_t)query * HQ + rw.head0 + r % G) * 16 + (lane & 15));
       }
-      const int lift = min(126, 14 + 127 - (int)(top >> 24));
-      const float f = pow2(lift);
-      u = a.scale_log2e * pow2(-lift);
+      float* const factor = (float*)(bp + kOffRow);
 #pragma unroll
-      for (int c = 0; c < 16; ++c) {
-        const uint32_t w[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
+      for (int k = 0; k < 8; ++k) {
+        const int r = warp * 16 + 2 * k + (lane >> 4), c = lane & 15;
+        const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+        uint32_t top = 0;
+#pragma unroll
+        for (int p = 0; p < 4; ++p) top = max(top, max(w[p] << 17, (w[p] & 0x7fff0000u) << 1));
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
+        const int lift = min(126, 14 + 127 - (int)(top >> 24));
+        const float f = pow2(lift);
         uint32_t h[4];
 #pragma unroll
         for (int p = 0; p < 4; ++p) h[p] = f16x2(bf16_lo(w[p]) * f, bf16_hi(w[p]) * f);
-        *(uint4*)(bp + (c >> 3) * kHalfOp + row * 128 + (((c & 7) ^ (row & 7)) << 4)) =
+        *(uint4*)(bp + (c >> 3) * kHalfOp + r * 128 + (((c & 7) ^ (r & 7)) << 4)) =
             make_uint4(h[0], h[1], h[2], h[3]);
+        if (c == 0) factor[r] = a.scale_log2e * pow2(-lift);
       }
       fence_async_smem();
       __syncwarp();
       if (lane == 0) bar_arrive(bar(BW_QFULL));
+      u_lo = factor[warp * 16 + g8];
+      u_hi = factor[warp * 16 + g8 + 8];
+      __syncwarp();
     };
-    bool alive = true;
     int T = 0;
-    if (my_units) stage_rows(0);
+    bool alive = true;
+    if (my_units) {
+      read_item(0, nxt);
+      read_users(nxt);
+      stage_rows(nxt);
+    }
 #pragma unroll 1
     for (int pass = 0; pass < my_units; ++pass) {
-    cur = nxt;
-    const int n_tiles = describe(pass).n_tiles;
-    const bool idle = warp * 32 >= cur.count;        // (no rows here: only keeps the phases)
-    float ref = kNoRefW, l = 0.f;
+      cur = nxt;
+      const int R = cur.count;
+      const bool more = pass + 1 < my_units;
+      if (more) read_item(pass + 1, nxt);
+      const int n_tiles = describe(pass).n_tiles;
+      const bool idle = warp * 16 >= R;              // (no rows here: only keeps the phases)
+      float ref_lo = kNoRefW, ref_hi = kNoRefW, l_lo = 0.f, l_hi = 0.f;
 #pragma unroll 1
-    for (int t = 0; t < n_tiles; ++t, ++T) {
-      const int b = T & 1;
-      bool ok = bar_wait(bar(BW_SFULL + b), (T >> 1) & 1, cta_abort, a.d_error, 22000);
-      ok = ok && bar_wait(bar(BW_VFULL + b), (T >> 1) & 1, cta_abort, a.d_error, 22100);
-      if (!__all_sync(0xffffffffu, ok)) {
-        alive = false;
-        break;
+      for (int t = 0; t < n_tiles; ++t, ++T) {
+        const int b = T & 1;
+        bool ok = bar_wait(bar(BW_SFULL + b), (T >> 1) & 1, cta_abort, a.d_error, 22000);
+        ok = ok && bar_wait(bar(BW_VFULL + b), (T >> 1) & 1, cta_abort, a.d_error, 22100);
+        if (!__all_sync(0xffffffffu, ok)) {
+          alive = false;
+          break;
+        }
+        tc_fence_after();
+        uint32_t pk_lo[8], pk_hi[8];
+        if (!idle) {
+          uint32_t sr[32];
+          TMEM_LD_16x256((tmem + 64u * b) | lane_sel, sr);
+          const float* tokc = (const float*)(bp + kOffTok) + b * 2 * kTok + 2 * qd;
+          const float4 kb = *(const float4*)((const float*)(bp + kOffKb) + b * 4);
+          const float kbs[4] = {kb.x, kb.y, kb.z, kb.w};
+          float2 f[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) f[k] = *(const float2*)(tokc + 8 * k);
+          tmem_wait_ld();
+          float m_lo = -INFINITY, m_hi = -INFINITY;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float s_lo = u_lo * kbs[k >> 1], s_hi = u_hi * kbs[k >> 1];
+            const float x0 = fmaf(__uint_as_float(sr[4 * k]), s_lo, f[k].x);
+            const float x1 = fmaf(__uint_as_float(sr[4 * k + 1]), s_lo, f[k].y);
+            const float x2 = fmaf(__uint_as_float(sr[4 * k + 2]), s_hi, f[k].x);
+            const float x3 = fmaf(__uint_as_float(sr[4 * k + 3]), s_hi, f[k].y);
+            m_lo = fmaxf(m_lo, fmaxf(x0, x1));
+            m_hi = fmaxf(m_hi, fmaxf(x2, x3));
+            sr[4 * k] = __float_as_uint(x0);
+            sr[4 * k + 1] = __float_as_uint(x1);
+            sr[4 * k + 2] = __float_as_uint(x2);
+            sr[4 * k + 3] = __float_as_uint(x3);
+          }
+          if (__any_sync(0xffffffffu, m_lo > ref_lo + kSlackW || m_hi > ref_hi + kSlackW)) {
+#pragma unroll
+            for (int d = 1; d <= 2; d <<= 1) {
+              m_lo = fmaxf(m_lo, __shfl_xor_sync(0xffffffffu, m_lo, d));
+              m_hi = fmaxf(m_hi, __shfl_xor_sync(0xffffffffu, m_hi, d));
+            }
+            m_lo = fmaxf(m_lo, ref_lo);
+            m_hi = fmaxf(m_hi, ref_hi);
+            const float f_lo = ex2(ref_lo - m_lo), f_hi = ex2(ref_hi - m_hi);
+            ref_lo = m_lo;
+            ref_hi = m_hi;
+            l_lo *= f_lo;
+            l_hi *= f_hi;
+            if (t > 0) {                             // (P V of the tile before has to be complete)
+              if (!__all_sync(0xffffffffu, bar_wait(bar(BW_PVDONE), (T - 1) & 1, cta_abort, a.d_error,
+                                                    22200))) {
+                alive = false;
+                break;
+              }
+              tc_fence_after();
+              const float fa = __shfl_sync(0xffffffffu, f_lo, 4 * (lane & 7));
+              const float fb = __shfl_sync(0xffffffffu, f_hi, 4 * (lane & 7));
+              const float fr = (lane & 8) ? fb : fa; // of row lane % 16
+#pragma unroll
+              for (int c = 0; c < 8; ++c) {
+                uint32_t orow[16];
+                TMEM_LD_16((tm_o + 16u * c) | lane_sel, orow);
+                tmem_wait_ld();
+#pragma unroll
+                for (int j = 0; j < 16; ++j) orow[j] = __float_as_uint(__uint_as_float(orow[j]) * fr);
+                TMEM_ST_16((tm_o + 16u * c) | lane_sel, orow);
+              }
+              tmem_wait_st();
+              tc_fence_before();
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float2 n = *(const float2*)(tokc + kTok + 8 * k);
+            const float p0 = ex2(__uint_as_float(sr[4 * k]) - ref_lo);
+            const float p1 = ex2(__uint_as_float(sr[4 * k + 1]) - ref_lo);
+            const float p2 = ex2(__uint_as_float(sr[4 * k + 2]) - ref_hi);
+            const float p3 = ex2(__uint_as_float(sr[4 * k + 3]) - ref_hi);
+            l_lo = fmaf(p0, n.x, fmaf(p1, n.y, l_lo));
+            l_hi = fmaf(p2, n.x, fmaf(p3, n.y, l_hi));
+            pk_lo[k] = f16x2(p0, p1);
+            pk_hi[k] = f16x2(p2, p3);
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) pk_lo[k] = pk_hi[k] = 0u;
+        }
+        // P takes the place of the tile before's, once that has been used
+        if (T > 0 && !__all_sync(0xffffffffu, bar_wait(bar(BW_PVDONE), (T - 1) & 1, cta_abort, a.d_error,
+                                                       22250))) {
+          alive = false;
+          break;
+        }
+        if (!idle) {
+          const int r = warp * 16 + g8;              // (rows r and r + 8: the same swizzle)
+          uint8_t* p = bp + kOffP + r * 128 + 4 * qd;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const int off = (k ^ (r & 7)) << 4;
+            *(uint32_t*)(p + off) = pk_lo[k];
+            *(uint32_t*)(p + 8 * 128 + off) = pk_hi[k];
+          }
+          fence_async_smem();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(bar(BW_PFULL));
+        if (t == 0 && more) read_users(nxt);
       }
+      if (!alive) break;
+      if (more) stage_rows(nxt);
+      if (!__all_sync(0xffffffffu, bar_wait(bar(BW_PVDONE), (T - 1) & 1, cta_abort, a.d_error, 22300)))
+        break;
       tc_fence_after();
       if (!idle) {
-        uint32_t sr[64];
-        TMEM_LD_32((tmem + 64u * b) | lane_sel, sr, 0);
-        TMEM_LD_32((tmem + 64u * b + 32u) | lane_sel, sr, 32);
-        tmem_wait_ld();
-        const float* tokc = (const float*)(bp + kOffTok) + b * 2 * kTok;
-        const float* kb = (const float*)(bp + kOffKb) + b * 4;
-        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        l_lo += __shfl_xor_sync(0xffffffffu, l_lo, 1);
+        l_hi += __shfl_xor_sync(0xffffffffu, l_hi, 1);
+        l_lo += __shfl_xor_sync(0xffffffffu, l_lo, 2);
+        l_hi += __shfl_xor_sync(0xffffffffu, l_hi, 2);
+        const float la = __shfl_sync(0xffffffffu, l_lo, 4 * (lane & 7));
+        const float lb = __shfl_sync(0xffffffffu, l_hi, 4 * (lane & 7));
+        const float ra = __shfl_sync(0xffffffffu, ref_lo, 4 * (lane & 7));
+        const float rb = __shfl_sync(0xffffffffu, ref_hi, 4 * (lane & 7));
+        const float l = (lane & 8) ? lb : la, ref = (lane & 8) ? rb : ra;
+        const int row = warp * 16 + (lane & 15);
+        const bool mine = lane < 16 && row < R;
+        const UserRef user = cur.user;
+        const int head = cur.head0 + row % G;
+        const float inv = 1.f / l;
+        const size_t prow = (size_t)(user.slot + cur.add) * HQ + head;
 #pragma unroll
-        for (int j = 0; j < 64; j += 4) {
-          const float s = u * kb[j >> 4];
-          const float4 f = *(const float4*)(tokc + j);       // (the same address in every lane)
-          const float x0 = fmaf(__uint_as_float(sr[j]), s, f.x);
-          const float x1 = fmaf(__uint_as_float(sr[j + 1]), s, f.y);
-          const float x2 = fmaf(__uint_as_float(sr[j + 2]), s, f.z);
-          const float x3 = fmaf(__uint_as_float(sr[j + 3]), s, f.w);
-          mx[0] = fmaxf(mx[0], x0);
-          mx[1] = fmaxf(mx[1], x1);
-          mx[2] = fmaxf(mx[2], x2);
-          mx[3] = fmaxf(mx[3], x3);
-          sr[j] = __float_as_uint(x0);
-          sr[j + 1] = __float_as_uint(x1);
-          sr[j + 2] = __float_as_uint(x2);
-          sr[j + 3] = __float_as_uint(x3);
-        }
-        const float m = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-        if (__any_sync(0xffffffffu, m > ref + kSlackW)) {
-          const float now = fmaxf(m, ref), f = ex2(ref - now);
-          ref = now;
-          l *= f;
-          if (t > 0) {
-            // (P V of the tile before has to be complete; the phase before on its barrier is,
-            // because this tile's scores came after that product)
-            if (!__all_sync(0xffffffffu, bar_wait(bar(BW_PVDONE + (b ^ 1)), ((T - 1) >> 1) & 1,
-                                                  cta_abort, a.d_error, 22200))) {
-              alive = false;
-              break;
+        for (int c = 0; c < 8; ++c) {                // dims 16 c .. 16 c + 15
+          uint32_t o[16];
+          TMEM_LD_16((tm_o + 16u * c) | lane_sel, o);
+          tmem_wait_ld();
+          auto at = [&](int j) { return __uint_as_float(o[(j & ~3) | ((j + (c >> 1)) & 3)]); };
+          if (mine) {
+            if (user.slot < 0) {
+              uint4* dst = (uint4*)((__nv_bfloat16*)a.out + ((size_t)user.query * HQ + head) * kDim) + 2 * c;
+#pragma unroll
+              for (int j = 0; j < 16; j += 8)
+                dst[j >> 3] = make_uint4(pack2(at(j) * inv, at(j + 1) * inv),
+                                         pack2(at(j + 2) * inv, at(j + 3) * inv),
+                                         pack2(at(j + 4) * inv, at(j + 5) * inv),
+                                         pack2(at(j + 6) * inv, at(j + 7) * inv));
+            } else {
+              float4* dst = (float4*)(a.part_o + prow * kDim) + 4 * c;
+#pragma unroll
+              for (int j = 0; j < 16; j += 4)
+                dst[j >> 2] = make_float4(at(j), at(j + 1), at(j + 2), at(j + 3));
             }
-            tc_fence_after();
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              uint32_t orow[32];
-              TMEM_LD_32((tmem + 128u + 32u * c) | lane_sel, orow, 0);
-              tmem_wait_ld();
-#pragma unroll
-              for (int j = 0; j < 32; ++j) orow[j] = __float_as_uint(__uint_as_float(orow[j]) * f);
-              TMEM_ST_32((tmem + 128u + 32u * c) | lane_sel, orow);
-            }
-            tmem_wait_st();
           }
         }
-        uint32_t pk[32];
-        float ls[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < 64; j += 4) {
-          const float4 n = *(const float4*)(tokc + kTok + j);
-          const float p0 = ex2(__uint_as_float(sr[j]) - ref);
-          const float p1 = ex2(__uint_as_float(sr[j + 1]) - ref);
-          const float p2 = ex2(__uint_as_float(sr[j + 2]) - ref);
-          const float p3 = ex2(__uint_as_float(sr[j + 3]) - ref);
-          ls[0] = fmaf(p0, n.x, ls[0]);
-          ls[1] = fmaf(p1, n.y, ls[1]);
-          ls[2] = fmaf(p2, n.z, ls[2]);
-          ls[3] = fmaf(p3, n.w, ls[3]);
-          pk[j >> 1] = f16x2(p0, p1);
-          pk[(j >> 1) + 1] = f16x2(p2, p3);
-        }
-        l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
-        TMEM_ST_32((tmem + 64u * b) | lane_sel, pk);
-        tmem_wait_st();
+        if (mine && user.slot >= 0) a.part_ml[prow] = make_float2(ref, l);
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) bar_arrive(bar(BW_PFULL + b));
-    }
-    if (!alive) break;
-    if (pass + 1 < my_units) stage_rows(pass + 1);
-    if (!__all_sync(0xffffffffu, bar_wait(bar(BW_PVDONE + ((T - 1) & 1)), ((T - 1) >> 1) & 1, cta_abort,
-                                          a.d_error, 22300)))
-      break;
-    tc_fence_after();
-    if (!idle) {
-      const float inv = cur.slot < 0 ? 1.f / l : 1.f;
-      const size_t prow = (size_t)cur.slot * HQ + cur.head;
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint32_t o[32];
-        TMEM_LD_32((tmem + 128u + 32u * c) | lane_sel, o, 0);
-        tmem_wait_ld();
-        auto at = [&](int j) { return o[(j & ~3) | ((j + c) & 3)]; };        // dim 32 c + j
-        if (row < cur.count) {
-          if (cur.slot < 0) {
-            uint4* dst = (uint4*)((__nv_bfloat16*)a.out + ((size_t)cur.query * HQ + cur.head) * kDim) + 4 * c;
-#pragma unroll
-            for (int j = 0; j < 32; j += 8) {
-              uint32_t w[4];
-#pragma unroll
-              for (int p = 0; p < 4; ++p)
-                w[p] = pack2(__uint_as_float(at(j + 2 * p)) * inv, __uint_as_float(at(j + 2 * p + 1)) * inv);
-              dst[j >> 3] = make_uint4(w[0], w[1], w[2], w[3]);
-            }
-          } else {
-            uint4* dst = (uint4*)(a.part_o + prow * kDim) + 8 * c;
-#pragma unroll
-            for (int j = 0; j < 32; j += 4) dst[j >> 2] = make_uint4(at(j), at(j + 1), at(j + 2), at(j + 3));
-          }
-        }
-      }
-      if (row < cur.count && cur.slot >= 0) a.part_ml[prow] = make_float2(ref, l);
-    }
-    tc_fence_before();
-    __syncwarp();
-    if (lane == 0) bar_arrive(bar(BW_ODONE));
+      if (lane == 0) bar_arrive(bar(BW_ODONE));
     }
   }
   // ---- common exit: every role arrives here, then the allocating warp frees TMEM
   tc_fence_before();
   __syncthreads();
-  if (warp == 6) {
+  if (warp == 8) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem),
                  "r"(kTmemColsW) : "memory");
