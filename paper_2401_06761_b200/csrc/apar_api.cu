@@ -413,13 +413,12 @@ apar_status launch_plan(apar_ctx* c, int layer, const void* q, void* out, float 
       APAR_CUDA(c, launch_attention_q4(a, it, st));
       ++*launches_out;
     }
+    a.pdl = c->use_pdl && p.n_mma;           // (directly after the attention)
     if (c->plan_verify_n > 0) {
-      APAR_CUDA(c, launch_q4_verify_tail(a, (const VerifyDesc*)c->ws(c->lay.verify),
-                                         c->plan_verify_n, st));
+      APAR_CUDA(c, launch_q4_verify_finish(a, (const VerifyDesc*)c->ws(c->lay.verify),
+                                           c->plan_verify_n, st));
       ++*launches_out;
-    }
-    if (!p.merges.empty()) {
-      a.pdl = c->use_pdl && p.n_mma && c->plan_verify_n == 0;   // (directly after the attention)
+    } else if (!p.merges.empty()) {
       APAR_CUDA(c, launch_q4_merge(a, (const MergeRef*)c->ws(c->lay.plan_merges),
                                    (int)p.merges.size(), c->q4_items.max_parts, st));
       ++*launches_out;
@@ -595,6 +594,7 @@ apar_status run_attention(apar_ctx* c, int n, const int32_t* qslots, const int32
       // every candidate's descriptor learns where its partial result goes
       if ((size_t)n * sizeof(VerifyDesc) > c->ring_bytes) return APAR_ERR_WORKSPACE_TOO_SMALL;
       for (int i = 0; i < n; ++i) (*verify)[i].slot = p.extra_slot[i];
+      for (const MergeRef& m : p.merges) (*verify)[m.query].parts = m.n - 1;
       Staging* s;
       rc = acquire(c, &s);
       if (rc) return rc;

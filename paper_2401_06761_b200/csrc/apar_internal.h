@@ -71,7 +71,7 @@ struct CowCopy {
 struct VerifyDesc {
   int32_t row, base, n_cand, slot;
   uint64_t mask;
-  int32_t query, pad;
+  int32_t query, parts;            // (4-bit pools) parts: partial results in the slots before `slot`
 };
 
 // Rows to move when candidates are accepted: row src of the thread's chain becomes row dst.
@@ -239,8 +239,9 @@ cudaError_t launch_attention_q4(const AttnArgs& a, const Q4Items& items, cudaStr
 // max_parts: parts of the row that has most.
 cudaError_t launch_q4_merge(const AttnArgs& a, const MergeRef* d_merge, int n_merge, int max_parts,
                             cudaStream_t st);
-cudaError_t launch_q4_verify_tail(const AttnArgs& a, const VerifyDesc* d_desc, int n_desc,
-                                  cudaStream_t st);
+// Candidates of a verification and the merge with the parts before them, in one; a.pdl likewise.
+cudaError_t launch_q4_verify_finish(const AttnArgs& a, const VerifyDesc* d_desc, int n_desc,
+                                    cudaStream_t st);
 
 // ---- planner (planner.cpp) ----
 // A run of consecutive table positions whose blocks are held by the same set of threads

@@ -108,11 +108,6 @@ __device__ __forceinline__ uint32_t lds32(uint32_t a) {
   asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
   return v;
 }
-__device__ __forceinline__ uint2 lds64(uint32_t a) {
-  uint2 v;
-  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
-  return v;
-}
 
 // words of a unit description; query and slot of row r at H_QUERY + r, H_SLOT + r
 enum { H_ROW = 0, H_BEGIN = 1, H_TOK = 2, H_NUSERS = 4, H_ADD = 5, H_KVH = 9, H_BID = 10, H_TAB = 12,
@@ -589,78 +584,124 @@ attn_q4_kernel(const AttnArgs a, const Q4Units units) {
   pdl_wait();                        // "this grid has completed" implies the one before it has
 }
 
-// Candidate tokens of a verification, as verify_tail_kernel, rows read from the 4-bit pool.  The
-// halves of a warp take the set bits of the mask in turn: a candidate of a tree sees few others.
-__global__ void __launch_bounds__(128) q4_verify_tail_kernel(const AttnArgs a,
-                                                             const VerifyDesc* __restrict__ descs) {
+// End of a verification, one warp per (candidate, head): the candidates it sees, read straight from
+// the 4-bit pool, and the partial results of the committed tokens before them, folded into the
+// output.  The halves of the warp take the set bits of the mask in turn (a candidate of a tree
+// sees few others), and the partial results too; lane c of a half holds dims 8 c .. 8 c + 7.  What
+// it reads first depends on nothing the attention kernels write, so it may start before them.
+__global__ void __launch_bounds__(128) q4_verify_finish_kernel(const AttnArgs a,
+                                                               const VerifyDesc* __restrict__ descs) {
   const VerifyDesc d = descs[blockIdx.x];
-  const int kvh = blockIdx.y;
   const int G = a.shape.group, HQ = a.shape.num_q_heads, HKV = a.shape.num_kv_heads;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int half = lane >> 4, c = lane & 15;
+  const int head = blockIdx.y * 4 + warp;
+  if (head >= HQ) return;
+  const int kvh = head / G;
   const int32_t* table = a.d_tables + (size_t)d.row * a.shape.table_stride;
-  for (int hg = warp; hg < G; hg += 4) {
-    const int head = kvh * G + hg;
-    float qf[8], o[8];
-    {
-      const uint4 qv = __ldg((const uint4*)a.q + ((size_t)d.query * HQ + head) * 16 + c);
-      const uint32_t w[4] = {qv.x, qv.y, qv.z, qv.w};
+  float qf[8], o[8];
+  {
+    const uint4 qv = __ldg((const uint4*)a.q + ((size_t)d.query * HQ + head) * 16 + c);
+    const uint32_t w[4] = {qv.x, qv.y, qv.z, qv.w};
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        qf[2 * x] = bf16_lo(w[x]) * a.scale_log2e;
-        qf[2 * x + 1] = bf16_hi(w[x]) * a.scale_log2e;
-        o[2 * x] = o[2 * x + 1] = 0.f;
-      }
+    for (int x = 0; x < 4; ++x) {
+      qf[2 * x] = bf16_lo(w[x]) * a.scale_log2e;
+      qf[2 * x + 1] = bf16_hi(w[x]) * a.scale_log2e;
+      o[2 * x] = o[2 * x + 1] = 0.f;
     }
-    float m = -INFINITY, l = 0.f;
-    uint64_t left = d.mask;
-    while (left) {
+  }
+  float m = -INFINITY, l = 0.f;                      // of this half
+  uint64_t left = d.mask;
+  while (left) {
+    // two candidates per half at a time
+    float t[2], vf[2][8];
+    bool on[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
       const int i_first = __ffsll((long long)left) - 1;
-      left &= left - 1;
+      const bool any = left != 0;
+      left &= left - 1;                              // (0 stays 0)
+      const int i_second = __ffsll((long long)left) - 1;
       const bool two = left != 0;
-      const int i_second = two ? __ffsll((long long)left) - 1 : 0;
-      left &= left - 1;                            // (0 stays 0)
-      const bool on = half == 0 || two, other_on = half == 1 || two;
-      float t = 0.f, vf[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (on) {
-        const int i = half ? i_second : i_first;
-        const int pos = d.base + i;
+      left &= left - 1;
+      on[n] = half ? two : any;
+      t[n] = 0.f;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) vf[n][x] = 0.f;
+      if (on[n]) {
+        const int pos = d.base + (half ? i_second : i_first);
         const size_t tile = ((size_t)table[pos >> 4] * HKV + kvh) * kQ4TileBytes;
         float kf[8];
         q4_load8_k((const uint8_t*)a.k_pool + tile, pos & (kBlock - 1), c, kf);
-        q4_load8_v((const uint8_t*)a.v_pool + tile, pos & (kBlock - 1), c, vf);
+        q4_load8_v((const uint8_t*)a.v_pool + tile, pos & (kBlock - 1), c, vf[n]);
 #pragma unroll
-        for (int x = 0; x < 8; ++x) t = fmaf(qf[x], kf[x], t);
+        for (int x = 0; x < 8; ++x) t[n] = fmaf(qf[x], kf[x], t[n]);
       }
-#pragma unroll
-      for (int x = 8; x; x >>= 1) t += __shfl_xor_sync(0xffffffffu, t, x);
-      const float s = on ? t : -INFINITY;
-      const float other = __shfl_xor_sync(0xffffffffu, s, 16);
-      const float mn = fmaxf(m, fmaxf(s, other));
-      const float corr = m == -INFINITY ? 0.f : ex2(m - mn);
-      const float p = on ? ex2(s - mn) : 0.f;
-      l = l * corr + p + (other_on ? ex2(other - mn) : 0.f);   // identical in both halves
-      m = mn;
-#pragma unroll
-      for (int x = 0; x < 8; ++x) o[x] = fmaf(p, vf[x], o[x] * corr);
     }
 #pragma unroll
-    for (int x = 0; x < 8; ++x) o[x] += __shfl_xor_sync(0xffffffffu, o[x], 16);
-    if (half == 0) {
-      if (d.slot < 0) {
-        const float inv = 1.f / l;                 // (a candidate sees itself)
-        *((uint4*)((__nv_bfloat16*)a.out + ((size_t)d.query * HQ + head) * kDim) + c) =
-            make_uint4(pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv),
-                       pack2(o[4] * inv, o[5] * inv), pack2(o[6] * inv, o[7] * inv));
-      } else {
-        const size_t prow = (size_t)d.slot * HQ + head;
-        float4* dst = (float4*)(a.part_o + prow * kDim) + 2 * c;
-        dst[0] = make_float4(o[0], o[1], o[2], o[3]);
-        dst[1] = make_float4(o[4], o[5], o[6], o[7]);
-        if (c == 0) a.part_ml[prow] = make_float2(m, l);
+    for (int n = 0; n < 2; ++n) {
+#pragma unroll
+      for (int x = 8; x; x >>= 1) t[n] += __shfl_xor_sync(0xffffffffu, t[n], x);
+      if (!on[n]) t[n] = -INFINITY;
+    }
+    const float mn = fmaxf(m, fmaxf(t[0], t[1]));
+    const float corr = m == -INFINITY ? 0.f : ex2(m - mn);
+    const float p0 = on[0] ? ex2(t[0] - mn) : 0.f, p1 = on[1] ? ex2(t[1] - mn) : 0.f;
+    m = mn;
+    l = fmaf(l, corr, p0 + p1);
+#pragma unroll
+    for (int x = 0; x < 8; ++x) o[x] = fmaf(p0, vf[0][x], fmaf(p1, vf[1][x], o[x] * corr));
+  }
+  pdl_wait();                                        // partial results of the attention kernels
+  for (int j0 = half; j0 < d.parts; j0 += 8) {       // four per half at a time
+    float2 ml[4];
+    float4 x0[4], x1[4];
+    float mn = m;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const int j = j0 + 2 * n;
+      ml[n] = make_float2(-INFINITY, 0.f);
+      x0[n] = x1[n] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (j < d.parts) {
+        const size_t prow = (size_t)(d.slot - d.parts + j) * HQ + head;
+        ml[n] = a.part_ml[prow];
+        const float4* src = (const float4*)(a.part_o + prow * kDim) + 2 * c;
+        x0[n] = src[0];
+        x1[n] = src[1];
       }
+    }
+#pragma unroll
+    for (int n = 0; n < 4; ++n) mn = fmaxf(mn, ml[n].x);
+    const float corr = m == -INFINITY ? 0.f : ex2(m - mn);
+    m = mn;
+    l *= corr;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) o[x] *= corr;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const float w = ml[n].x == -INFINITY ? 0.f : ex2(ml[n].x - mn);
+      l = fmaf(ml[n].y, w, l);
+      o[0] = fmaf(x0[n].x, w, o[0]); o[1] = fmaf(x0[n].y, w, o[1]);
+      o[2] = fmaf(x0[n].z, w, o[2]); o[3] = fmaf(x0[n].w, w, o[3]);
+      o[4] = fmaf(x1[n].x, w, o[4]); o[5] = fmaf(x1[n].y, w, o[5]);
+      o[6] = fmaf(x1[n].z, w, o[6]); o[7] = fmaf(x1[n].w, w, o[7]);
     }
   }
+  __syncwarp();
+  const float M = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+  const float f = m == -INFINITY ? 0.f : ex2(m - M);   // (a half may have seen nothing)
+  l *= f;
+  l += __shfl_xor_sync(0xffffffffu, l, 16);
+#pragma unroll
+  for (int x = 0; x < 8; ++x) {
+    o[x] *= f;
+    o[x] += __shfl_xor_sync(0xffffffffu, o[x], 16);
+  }
+  const float inv = 1.f / l;                         // (a candidate sees itself)
+  if (half == 0)
+    *((uint4*)((__nv_bfloat16*)a.out + ((size_t)d.query * HQ + head) * kDim) + c) =
+        make_uint4(pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv),
+                   pack2(o[4] * inv, o[5] * inv), pack2(o[6] * inv, o[7] * inv));
 }
 
 // out = sum_j o_j 2^(m_j - M) / sum_j l_j 2^(m_j - M) over the partial results of one (query, head).
@@ -766,11 +807,11 @@ cudaError_t launch_attention_q4(const AttnArgs& a, const Q4Items& it, cudaStream
   return launch_kernel(attn_q4_kernel, dim3(ctas), dim3(32 * kWarps), kSmemQ4, st, a.pdl != 0, a, u);
 }
 
-cudaError_t launch_q4_verify_tail(const AttnArgs& a, const VerifyDesc* d_desc, int n_desc,
-                                  cudaStream_t st) {
+cudaError_t launch_q4_verify_finish(const AttnArgs& a, const VerifyDesc* d_desc, int n_desc,
+                                    cudaStream_t st) {
   if (n_desc <= 0) return cudaSuccess;
-  q4_verify_tail_kernel<<<dim3(n_desc, a.shape.num_kv_heads), 128, 0, st>>>(a, d_desc);
-  return cudaGetLastError();
+  return launch_kernel(q4_verify_finish_kernel, dim3(n_desc, (a.shape.num_q_heads + 3) / 4), dim3(128), 0,
+                       st, a.pdl != 0, a, d_desc);
 }
 
 }  // namespace apar
