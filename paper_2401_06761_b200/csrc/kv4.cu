@@ -11,31 +11,26 @@ namespace apar {
 namespace {
 
 // ------------------------------------------------------------------ append: quantise and scatter
-struct Q4Group {          // one lane's share of a row: eight codes and its group's scale word
-  uint32_t codes, scale;
+// Eight lanes hold one row, sixteen dims (32 bytes) each, half a group of 32: enough values to
+// spread the division and the reciprocal of a group's scale over.
+struct Q4Half {           // one lane's share of a row: sixteen codes and its group's scale word
+  uint32_t w0, w1, scale;
 };
 
-// Sixteen lanes hold one row, eight dims (16 bytes) each; the four lanes of a group find its
-// range with two shuffles.  Nibble order of the codes: K e / 2 + 4 (e & 1), V e.
-__device__ __forceinline__ Q4Group q4_quantise(const uint4& x, bool is_v) {
-  const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
-  float f[8];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    f[2 * e] = bf16_lo(xs[e]);
-    f[2 * e + 1] = bf16_hi(xs[e]);
-  }
+// Nibble order of each word's eight codes: K e / 2 + 4 (e & 1), V e.
+template <bool kV>
+__device__ __forceinline__ Q4Half q4_quantise(const uint4& xa, const uint4& xb) {
+  const uint32_t xs[8] = {xa.x, xa.y, xa.z, xa.w, xb.x, xb.y, xb.z, xb.w};
   // the NaN-propagating minimum lets a NaN reach the scale
   __nv_bfloat162 mn = *(__nv_bfloat162*)&xs[0], mx = mn;
 #pragma unroll
-  for (int e = 1; e < 4; ++e) {
+  for (int e = 1; e < 8; ++e) {
     mn = __hmin2_nan(mn, *(__nv_bfloat162*)&xs[e]);
     mx = __hmax2_nan(mx, *(__nv_bfloat162*)&xs[e]);
   }
-#pragma unroll
-  for (int o = 1; o <= 2; o <<= 1) {
-    uint32_t a = __shfl_xor_sync(0xffffffffu, *(uint32_t*)&mn, o);
-    uint32_t b = __shfl_xor_sync(0xffffffffu, *(uint32_t*)&mx, o);
+  {
+    uint32_t a = __shfl_xor_sync(0xffffffffu, *(uint32_t*)&mn, 1);
+    uint32_t b = __shfl_xor_sync(0xffffffffu, *(uint32_t*)&mx, 1);
     mn = __hmin2_nan(mn, *(__nv_bfloat162*)&a);
     mx = __hmax2_nan(mx, *(__nv_bfloat162*)&b);
   }
@@ -48,26 +43,97 @@ __device__ __forceinline__ Q4Group q4_quantise(const uint4& x, bool is_v) {
   // c = round((x - lo) / s).  The quotient is correctly rounded, as a division would give it: one
   // residual step on a correctly rounded reciprocal (Markstein 1990; the divisor has eight
   // significant bits, so the theorem's one exception, a significand of all ones, cannot occur).
-  // Adding 1.5 * 2^23 leaves the integer, ties to even, in the low bits.
+  // Adding 1.5 * 2^23 leaves the integer, ties to even, in the low bits of a number whose other
+  // bits are known: they are summed along and taken off once per word.
   const float inv = s > 0.f ? __frcp_rn(s) : 0.f;
-  uint32_t w = 0;
+  constexpr uint32_t kMagicBits = 0x4b400000u;
+  uint32_t w[2];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float d = f[e] - lo;
-    const float q = d * inv;
-    const float t = fmaf(fmaf(-q, s, d), inv, q);
-    const uint32_t code = (uint32_t)__float_as_int(t + 12582912.f) & 15u;
-    w |= code << (is_v ? 4 * e : 4 * ((e >> 1) + 4 * (e & 1)));
+  for (int n = 0; n < 2; ++n) {
+    uint32_t sum = 0, known = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t x = xs[4 * n + (e >> 1)];
+      const float d = ((e & 1) ? bf16_hi(x) : bf16_lo(x)) - lo;
+      const float q = d * inv;
+      const float t = fmaf(fmaf(-q, s, d), inv, q);
+      const uint32_t at = 1u << (kV ? 4 * e : 4 * ((e >> 1) + 4 * (e & 1)));
+      sum += __float_as_uint(t + 12582912.f) * at;
+      known += kMagicBits * at;
+    }
+    w[n] = sum - known;
   }
   // (a NaN scale carries the sign bit: integer comparisons of scales rank it below all others)
-  if (bad) return Q4Group{0u, 0xffc0ffc0u};
-  return Q4Group{w, (__float_as_uint(s) >> 16) | (__float_as_uint(lo) & 0xffff0000u)};
+  if (bad) return Q4Half{0u, 0u, 0xffc0ffc0u};
+  return Q4Half{w[0], w[1], (__float_as_uint(s) >> 16) | (__float_as_uint(lo) & 0xffff0000u)};
+}
+
+template <bool kV>
+__device__ __forceinline__ void q4_append_rows(uint8_t* __restrict__ pool, const uint4* __restrict__ rows,
+                                               const int32_t* __restrict__ slots, long long first_row,
+                                               int n_rows, int num_kv_heads) {
+  const uint32_t rh = blockIdx.x * (blockDim.x / 8) + (threadIdx.x >> 3);   // (row, head) < 2^31
+  const int c = threadIdx.x & 7;
+  bool on = rh < (uint32_t)n_rows * (uint32_t)num_kv_heads;
+  const int r = on ? (int)(rh / (uint32_t)num_kv_heads) : 0;
+  const int h = on ? (int)(rh - (uint32_t)r * (uint32_t)num_kv_heads) : 0;
+  const int slot = slots[r];
+  const bool pair = on && !(slot & 1) && r + 1 < n_rows && slots[r + 1] == slot + 1;
+  if ((slot & 1) && r > 0 && slots[r - 1] == slot - 1) on = false;
+  if (!__any_sync(0xffffffffu, on)) return;
+  const uint4* src = rows + ((first_row + r) * num_kv_heads + h) * 16 + 2 * c;
+  uint4 x[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = make_uint4(0u, 0u, 0u, 0u);
+  if (on) {
+    x[0] = __ldg(src);
+    x[1] = __ldg(src + 1);
+  }
+  if (pair) {
+    x[2] = __ldg(src + (size_t)num_kv_heads * 16);
+    x[3] = __ldg(src + (size_t)num_kv_heads * 16 + 1);
+  }
+  const Q4Half a = q4_quantise<kV>(x[0], x[1]), b = q4_quantise<kV>(x[2], x[3]);
+  if (!on) return;
+  uint8_t* tile = pool + ((size_t)(slot >> 4) * num_kv_heads + h) * kQ4TileBytes;
+  const int off = slot & 15, G = c >> 1;
+  if (kV) {
+    uint8_t* p = tile + q4_v_piece(off, 4 * (c & 1), G);     // pieces 4 (c & 1) .. + 3
+    if (pair) {
+      *(uint32_t*)p = __byte_perm(a.w0, b.w0, 0x5410);
+      *(uint32_t*)(p + 16) = __byte_perm(a.w0, b.w0, 0x7632);
+      *(uint32_t*)(p + 32) = __byte_perm(a.w1, b.w1, 0x5410);
+      *(uint32_t*)(p + 48) = __byte_perm(a.w1, b.w1, 0x7632);
+    } else {
+      *(uint16_t*)p = (uint16_t)a.w0;
+      *(uint16_t*)(p + 16) = (uint16_t)(a.w0 >> 16);
+      *(uint16_t*)(p + 32) = (uint16_t)a.w1;
+      *(uint16_t*)(p + 48) = (uint16_t)(a.w1 >> 16);
+    }
+    if (!(c & 1)) {
+      *(uint32_t*)(tile + q4_v_scales(off) + 4 * G) = a.scale;
+      if (pair) *(uint32_t*)(tile + q4_v_scales(off + 1) + 4 * G) = b.scale;
+    }
+  } else {
+    uint8_t* row = tile + off * kQ4RowBytes + (c & 1) * 32 + G * 4;    // word G of pieces 2 (c & 1), + 1
+    *(uint32_t*)row = a.w0;
+    *(uint32_t*)(row + 16) = a.w1;
+    if (pair) {
+      *(uint32_t*)(row + kQ4RowBytes) = b.w0;
+      *(uint32_t*)(row + kQ4RowBytes + 16) = b.w1;
+    }
+    if (!(c & 1)) {
+      uint8_t* sc = tile + off * kQ4RowBytes + kQ4CodeBytes + 4 * G;
+      *(uint32_t*)sc = a.scale;
+      if (pair) *(uint32_t*)(sc + kQ4RowBytes) = b.scale;
+    }
+  }
 }
 
 // Two rows that are neighbours in the pool, an even one and the odd one after it, are written by
-// the sixteen lanes of the first, so that the pair's interleaved V codes leave as whole words;
-// the lanes of the second have nothing to do.  The kernel reads 256 bytes and writes 80 for each
-// row and is bound by HBM for prompts, by its launch for decode steps.
+// the lanes of the first, so that the pair's interleaved V codes leave as whole words; the lanes
+// of the second have nothing to do.  blockIdx.y selects K or V.  The kernel reads 256 bytes and
+// writes 80 for each row.
 __global__ void __launch_bounds__(256) q4_append_kernel(uint8_t* __restrict__ k_pool,
                                                         uint8_t* __restrict__ v_pool,
                                                         const uint4* __restrict__ k_new,
@@ -75,47 +141,10 @@ __global__ void __launch_bounds__(256) q4_append_kernel(uint8_t* __restrict__ k_
                                                         const int32_t* __restrict__ slots,
                                                         long long first_row, int n_rows,
                                                         int num_kv_heads) {
-  const long long idx = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-  const long long rh = idx >> 4;                       // (row, head)
-  const int c = (int)idx & 15;
-  const bool is_v = blockIdx.y != 0;
-  bool on = rh < (long long)n_rows * num_kv_heads;
-  const int r = on ? (int)(rh / num_kv_heads) : 0, h = on ? (int)(rh % num_kv_heads) : 0;
-  const int slot = slots[r];
-  const bool pair = on && !(slot & 1) && r + 1 < n_rows && slots[r + 1] == slot + 1;
-  if ((slot & 1) && r > 0 && slots[r - 1] == slot - 1) on = false;
-  if (!__any_sync(0xffffffffu, on)) return;
-  const uint4* src = (is_v ? v_new : k_new) + ((first_row + r) * num_kv_heads + h) * 16 + c;
-  uint4 x0 = make_uint4(0u, 0u, 0u, 0u), x1 = x0;
-  if (on) x0 = __ldg(src);
-  if (pair) x1 = __ldg(src + (size_t)num_kv_heads * 16);
-  const Q4Group a = q4_quantise(x0, is_v), b = q4_quantise(x1, is_v);
-  if (!on) return;
-  uint8_t* tile = (is_v ? v_pool : k_pool) +
-                  ((size_t)(slot >> 4) * num_kv_heads + h) * kQ4TileBytes;
-  const int off = slot & 15, G = c >> 2, x = c & 3;
-  if (is_v) {
-    uint8_t* p = tile + q4_v_piece(off, 2 * x, G);     // pieces 2 x (low half) and 2 x + 1
-    if (pair) {
-      *(uint32_t*)p = __byte_perm(a.codes, b.codes, 0x5410);
-      *(uint32_t*)(p + 16) = __byte_perm(a.codes, b.codes, 0x7632);
-    } else {
-      *(uint16_t*)p = (uint16_t)a.codes;
-      *(uint16_t*)(p + 16) = (uint16_t)(a.codes >> 16);
-    }
-    if (x == 0) {
-      *(uint32_t*)(tile + q4_v_scales(off) + 4 * G) = a.scale;
-      if (pair) *(uint32_t*)(tile + q4_v_scales(off + 1) + 4 * G) = b.scale;
-    }
-  } else {
-    uint8_t* row = tile + off * kQ4RowBytes;
-    *(uint32_t*)(row + x * 16 + G * 4) = a.codes;
-    if (pair) *(uint32_t*)(row + kQ4RowBytes + x * 16 + G * 4) = b.codes;
-    if (x == 0) {
-      *(uint32_t*)(row + kQ4CodeBytes + 4 * G) = a.scale;
-      if (pair) *(uint32_t*)(row + kQ4RowBytes + kQ4CodeBytes + 4 * G) = b.scale;
-    }
-  }
+  if (blockIdx.y)
+    q4_append_rows<true>(v_pool, v_new, slots, first_row, n_rows, num_kv_heads);
+  else
+    q4_append_rows<false>(k_pool, k_new, slots, first_row, n_rows, num_kv_heads);
 }
 
 // ------------------------------------------------------------------ fork: copy r rows
@@ -172,11 +201,11 @@ __global__ void __launch_bounds__(256) read_rows_kernel(const uint8_t* __restric
                                                         const int32_t* __restrict__ slots,
                                                         long long first_row, int n_rows,
                                                         int num_kv_heads) {
-  const long long idx = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-  if (idx >= (long long)n_rows * num_kv_heads * 16) return;
-  const long long rh = idx >> 4;
-  const int c = (int)idx & 15;
-  const int r = (int)(rh / num_kv_heads), h = (int)(rh % num_kv_heads);
+  const uint32_t rh = blockIdx.x * (blockDim.x / 16) + (threadIdx.x >> 4);   // (row, head) < 2^31
+  if (rh >= (uint32_t)n_rows * (uint32_t)num_kv_heads) return;
+  const int c = threadIdx.x & 15;
+  const int r = (int)(rh / (uint32_t)num_kv_heads);
+  const int h = (int)(rh - (uint32_t)r * (uint32_t)num_kv_heads);
   const int slot = slots[r];
   const size_t tile = (size_t)(slot >> 4) * num_kv_heads + h;
   const uint8_t* pool = blockIdx.y ? v_pool : k_pool;
@@ -204,7 +233,7 @@ cudaError_t launch_q4_append(void* k_pool, void* v_pool, const void* k_new, cons
                              const int32_t* d_slots, int64_t first_row, int n_rows,
                              int num_kv_heads, cudaStream_t st) {
   if (n_rows <= 0) return cudaSuccess;
-  const long long total = (long long)n_rows * num_kv_heads * 16;
+  const long long total = (long long)n_rows * num_kv_heads * 8;
   q4_append_kernel<<<dim3((unsigned)((total + 255) / 256), 2), 256, 0, st>>>(
       (uint8_t*)k_pool, (uint8_t*)v_pool, (const uint4*)k_new, (const uint4*)v_new, d_slots,
       (long long)first_row, n_rows, num_kv_heads);

@@ -139,13 +139,21 @@ bool Planner::build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_
   // ---- chunk length: enough items to fill the machine, never below 128 tokens
   const int64_t kInf = (int64_t)1 << 40;
   int64_t chunk = std::max<int64_t>(128, round_up16(unique * hint_kv_heads_ / (num_sms_ * 8)));
+  int max_users = std::max(1, kMaxRowsPerItem / group_);
   if (streams_) {
+    // With little to do, everything goes to single warps: a wide unit takes some 10 us to come and
+    // go, in which a warp does about four blocks.
+    int64_t blocks = 0;
+    for (const Seg& g : segs_)
+      blocks += ((int64_t)g.n_users * group_ + stream_rows_ - 1) / stream_rows_ * hint_kv_heads_ *
+                ((g.tok_end - g.tok_begin + kBlock - 1) / kBlock);
+    if (blocks <= 4ll * num_sms_ * streams_) max_users = std::max(1, stream_rows_ / group_);
     // The fewest chunks that give every warp a unit and none a second one; with more units than
     // warps from the start, no unit longer than a warp's even share.
     const int64_t warps = (int64_t)num_sms_ * streams_;
     // warps' worth of time per token of a run
     auto units_of = [&](const Seg& g) {
-      const int64_t per = std::max(1, kMaxRowsPerItem / group_);
+      const int64_t per = max_users;
       auto cost = [&](int64_t users) -> int64_t {
         return users == 0 ? 0 : users * group_ > stream_rows_ ? kWideCost : 1;
       };
@@ -177,7 +185,6 @@ bool Planner::build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_
   // single-row kernel has no such staging and needs several CTAs per SM to cover the latency:
   // when its runs, dealt out four kv heads to a CTA, would give fewer than four CTAs per SM,
   // they are cut finer (up to eight times).  This only happens with a few very long threads.
-  const int max_users = std::max(1, kMaxRowsPerItem / group_);
   auto single_row = [&](const Seg& g) {
     return std::min(g.n_users, max_users) * group_ < mma_min_rows;
   };
