@@ -6,9 +6,9 @@ library has not been built, importing this module raises.
 """
 from __future__ import annotations
 
-import array
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -138,8 +138,9 @@ def _arr(xs):
     if isinstance(xs, tuple) and len(xs) == 2 and isinstance(xs[1], int):
         return xs          # already marshalled by int32_array()
     if not isinstance(xs, np.ndarray):
-        a = array.array("i", xs)
-        return (C.c_int32 * max(len(a), 1)).from_buffer(a if a else array.array("i", [0])), len(a)
+        xs = xs if isinstance(xs, (list, tuple)) else list(xs)
+        n = len(xs)
+        return (C.c_int32 * max(n, 1)).from_buffer_copy(struct.pack(f"{max(n, 1)}i", *(xs or (0,)))), n
     a = np.ascontiguousarray(xs.astype(np.int32, copy=False))
     buf = (C.c_int32 * max(a.size, 1)).from_buffer_copy(a.tobytes() if a.size else b"\0" * 4)
     return buf, int(a.size)
@@ -224,7 +225,8 @@ def apar_tree_verify_attention(ctx, tid, n_cand, anc_mask, q: int, out: int, sm_
     """anc_mask: one Python int (uint64 bit mask) per candidate, all threads' candidates in order."""
     tids, n = _arr(tid)
     cands, _ = _arr(n_cand)
-    masks = (C.c_uint64 * max(len(anc_mask), 1)).from_buffer(array.array("Q", anc_mask or [0]))
+    masks = (C.c_uint64 * max(len(anc_mask), 1)).from_buffer_copy(
+        struct.pack(f"{max(len(anc_mask), 1)}Q", *(anc_mask or (0,))))
     _check(lib.apar_tree_verify_attention(ctx, n, tids, cands, masks, q, out, sm_scale, stream))
 
 

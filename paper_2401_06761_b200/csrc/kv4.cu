@@ -191,7 +191,7 @@ __global__ void __launch_bounds__(256) q4_row_move_kernel(uint8_t* __restrict__ 
 }
 
 // ------------------------------------------------------------------ rows read back as bf16
-// One thread per eight dims of a row; blockIdx.y selects K or V.  A 4-bit row reads as
+// One thread per sixteen dims of a row; blockIdx.y selects K or V.  A 4-bit row reads as
 // bf16(lo + s * c), the sum taken in 32 bits and rounded once more to the output's type.
 template <bool kQ4>
 __global__ void __launch_bounds__(256) read_rows_kernel(const uint8_t* __restrict__ k_pool,
@@ -201,30 +201,35 @@ __global__ void __launch_bounds__(256) read_rows_kernel(const uint8_t* __restric
                                                         const int32_t* __restrict__ slots,
                                                         long long first_row, int n_rows,
                                                         int num_kv_heads) {
-  const uint32_t rh = blockIdx.x * (blockDim.x / 16) + (threadIdx.x >> 4);   // (row, head) < 2^31
+  const uint32_t rh = blockIdx.x * (blockDim.x / 8) + (threadIdx.x >> 3);   // (row, head) < 2^31
   if (rh >= (uint32_t)n_rows * (uint32_t)num_kv_heads) return;
-  const int c = threadIdx.x & 15;
+  const int c = threadIdx.x & 7;
   const int r = (int)(rh / (uint32_t)num_kv_heads);
   const int h = (int)(rh - (uint32_t)r * (uint32_t)num_kv_heads);
   const int slot = slots[r];
   const size_t tile = (size_t)(slot >> 4) * num_kv_heads + h;
   const uint8_t* pool = blockIdx.y ? v_pool : k_pool;
-  uint4 out;
-  if (kQ4) {
-    float f[8];
-    if (blockIdx.y) q4_load8_v(pool + tile * kQ4TileBytes, slot & 15, c, f);
-    else q4_load8_k(pool + tile * kQ4TileBytes, slot & 15, c, f);
-    uint32_t w[4];
+  uint4 out[2];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * e], f[2 * e + 1]);
-      w[e] = *(uint32_t*)&p;
+  for (int i = 0; i < 2; ++i) {
+    if (kQ4) {
+      float f[8];
+      if (blockIdx.y) q4_load8_v(pool + tile * kQ4TileBytes, slot & 15, 2 * c + i, f);
+      else q4_load8_k(pool + tile * kQ4TileBytes, slot & 15, 2 * c + i, f);
+      uint32_t w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * e], f[2 * e + 1]);
+        w[e] = *(uint32_t*)&p;
+      }
+      out[i] = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+      out[i] = ((const uint4*)pool)[(tile * kBlock + (slot & 15)) * 16 + 2 * c + i];
     }
-    out = make_uint4(w[0], w[1], w[2], w[3]);
-  } else {
-    out = ((const uint4*)pool)[(tile * kBlock + (slot & 15)) * 16 + c];
   }
-  (blockIdx.y ? v_out : k_out)[(first_row * num_kv_heads + rh) * 16 + c] = out;
+  uint4* dst = (blockIdx.y ? v_out : k_out) + (first_row * num_kv_heads + rh) * 16 + 2 * c;
+  dst[0] = out[0];
+  dst[1] = out[1];
 }
 
 }  // namespace
@@ -261,7 +266,7 @@ cudaError_t launch_read_rows(bool q4, const void* k_pool, const void* v_pool, vo
                              void* v_out, const int32_t* d_slots, int64_t first_row, int n_rows,
                              int num_kv_heads, cudaStream_t st) {
   if (n_rows <= 0) return cudaSuccess;
-  const long long total = (long long)n_rows * num_kv_heads * 16;
+  const long long total = (long long)n_rows * num_kv_heads * 8;
   const dim3 grid((unsigned)((total + 255) / 256), 2);
   auto kernel = q4 ? read_rows_kernel<true> : read_rows_kernel<false>;
   kernel<<<grid, 256, 0, st>>>((const uint8_t*)k_pool, (const uint8_t*)v_pool, (uint4*)k_out,
