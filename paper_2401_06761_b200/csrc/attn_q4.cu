@@ -26,12 +26,14 @@
 //                   one more product: lo_j is a bf16 number, and qsum_j the sum of three, so
 //                   that four groups fill a k of 16.  Scores are exact to 32 bits.
 //   O^T += V^T P^T  A = V codes, 16 dims x 16 tokens.  B = P s_j, one operand per group, rounded
-//                   once to f16: it is below 2^10 by the choice of reference, and 11 bits against
+//                   once to f16: it is below 2^16 by the choice of reference, and 11 bits against
 //                   bf16's eight keep the result as good as 32-bit arithmetic rounded to bf16.
 //                   The offsets lo_j are summed in 32 bits on the side, once per group and row.
 // The reference subtracted in the exponent is the running maximum of score + log2(largest
 // scale of the token's V row), not of the score: P s_j is then bounded whatever the scales are,
-// and f16's narrow exponent is spent on the largest terms of the sum.  It moves lazily (kSlack).
+// and f16's narrow exponent is spent on the largest terms of the sum.  It moves lazily (kSlack), and
+// to a little below the maximum (kHeadroom): f16 numbers are normal from 2^-14 to 2^16, and in a
+// long context most of the sum is in weights far below the largest.
 //
 // The C fragment of S^T holds tokens in rows, the B operand wants them in the k index: a
 // movmatrix of the 8 x 8 halves brings one into the other.
@@ -61,7 +63,8 @@ constexpr int kOffQ = kWarps * kDepth * kSlot;       // the next unit's query ro
 constexpr int kOffHdr = kOffQ + kWarps * kRows * kDim * 2;
 constexpr int kSmemQ4 = kOffHdr + kWarps * kHdrs * kHdrInts * 4;
 static_assert(kSmemQ4 <= 227 * 1024, "shared memory");
-constexpr float kSlack = 8.f;                        // the reference moves only past 2^8
+constexpr float kHeadroom = 6.f;                     // largest weight when the reference is set: 2^6
+constexpr float kSlack = 14.f;                       // and when it has to move: 2^14 (times 2^1.1)
 constexpr float kNoRef = -3e38f;                      // of a row that has seen nothing (finite: a
                                                      // masked score less this is still -inf)
 constexpr float kCodeUnit = 1.f / 16777216.f;        // what a code of 1 counts as in a product: 2^-24
@@ -371,8 +374,8 @@ __device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Units& u
         y0 = fmaxf(y0, __shfl_xor_sync(0xffffffffu, y0, d));
         y1 = fmaxf(y1, __shfl_xor_sync(0xffffffffu, y1, d));
       }
-      y0 = fmaxf(y0, ref[0]);
-      y1 = fmaxf(y1, ref[1]);
+      y0 = fmaxf(y0 - kHeadroom, ref[0]);
+      y1 = fmaxf(y1 - kHeadroom, ref[1]);
       const float f0 = ex2(ref[0] - y0), f1 = ex2(ref[1] - y1);
       ref[0] = y0;
       ref[1] = y1;

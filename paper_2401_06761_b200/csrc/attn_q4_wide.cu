@@ -61,7 +61,7 @@ enum { BW_KFULL = 0, BW_KEMPTY = 2, BW_VFULL = 4, BW_VEMPTY = 6, BW_SFULL = 8, B
 constexpr int kSmemWide = kOffBarW + 8 * BW_TOTAL + 16;
 static_assert(2 * (kSmemWide + 1024) <= 228 * 1024, "two CTAs per SM");
 constexpr int kTmemColsW = 256;                      // S at 0 and 64, O at 128
-constexpr float kSlackW = 8.f;
+constexpr float kHeadroomW = 6.f, kSlackW = 14.f;    // as in attn_q4.cu: weights 2^6 .. 2^14
 constexpr float kNoRefW = -3e38f;
 constexpr int kLift = 8;                             // operands stay below 2^(1 - kLift)
 constexpr uint32_t kEvenW = 0x000f000fu, kOddW = 0x00f000f0u;
@@ -533,8 +533,8 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
               m_lo = fmaxf(m_lo, __shfl_xor_sync(0xffffffffu, m_lo, d));
               m_hi = fmaxf(m_hi, __shfl_xor_sync(0xffffffffu, m_hi, d));
             }
-            m_lo = fmaxf(m_lo, ref_lo);
-            m_hi = fmaxf(m_hi, ref_hi);
+            m_lo = fmaxf(m_lo - kHeadroomW, ref_lo);
+            m_hi = fmaxf(m_hi - kHeadroomW, ref_hi);
             const float f_lo = ex2(ref_lo - m_lo), f_hi = ex2(ref_hi - m_hi);
             ref_lo = m_lo;
             ref_hi = m_hi;
