@@ -224,7 +224,8 @@ bool Planner::build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_
     }
     if (total_slots <= slot_capacity) break;
     if (chunk >= kInf) return false;
-    chunk = attempt >= 3 ? kInf : chunk * 4;
+    if (streams_) chunk = attempt >= 8 ? kInf : round_up16(chunk * 3 / 2);
+    else chunk = attempt >= 3 ? kInf : chunk * 4;
   }
 
   // ---- partial slots and merges

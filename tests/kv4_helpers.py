@@ -3,7 +3,7 @@ import numpy as np
 import torch
 
 from oracle import kv4
-from tests.helpers import OracleBackend, assert_same_bookkeeping
+from helpers import OracleBackend, assert_same_bookkeeping
 from paper_2401_06761_b200.session import PagedSession
 from paper_2401_06761_b200.synth import LayerShape
 
@@ -68,10 +68,12 @@ class Kv4Pair:
 
 def check(got, ref, mid, what=""):
     """got bf16 against the 64-bit result ref.  The output is rounded to bf16 (half a step is 2^-8
-    of it).  The weights are rounded to f16 after their scale (half a step 2^-11 of each term,
-    terms below 2^-14 of the largest 2^-25 of it: with fewer than 2^14 tokens no more than
-    another 2^-11), and multiply s c, whose weighted mean is mid.  What is left, sums and scores
-    in 32 bits, is far below either."""
+    of it).  The weights are rounded to f16 after their scale: half a step is 2^-11 of each term,
+    and for terms below 2^-20 of the largest 2^-31 of that (2^18 of them add up to no more than
+    2^-13); they multiply s c, whose weighted mean is mid.  Sums and scores are in 32 bits.  The
+    kernel for many rows rounds the values to f16 instead, which is no more, and K too: 128
+    independent errors of 2^-12 of a product each shift a score by some 2^-12 of its spread, a
+    tenth of what is left of 2^-10."""
     got = host(got).astype(np.float64)
     assert np.isfinite(got).all(), f"{what}: non-finite output"
     err = np.abs(got - ref)

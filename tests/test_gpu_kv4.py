@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from oracle import kv4
-from tests.kv4_helpers import Kv4Pair, check, host, rows
+from kv4_helpers import Kv4Pair, check, host, rows
 from paper_2401_06761_b200 import binding as B
 from paper_2401_06761_b200.session import PagedSession, Rope
 from paper_2401_06761_b200.synth import LayerShape
@@ -116,6 +116,11 @@ def test_layers_and_forks_keep_every_row():
 
 
 # ------------------------------------------------------------------------------------- attention
+# query heads per kv head of a single thread decide which kernel takes it: up to four rows, up to
+# eight, more
+WIDTHS = [(4, 2), (16, 2), (32, 2)]
+
+
 @pytest.mark.parametrize("hq,hk", [(2, 2), (8, 2), (6, 1), (32, 8), (40, 40), (64, 1), (24, 2)])
 @pytest.mark.parametrize("length", [1, 15, 16, 17, 63, 130, 600])
 def test_single_threads(hq, hk, length):
@@ -150,31 +155,34 @@ def test_forest(hq, hk, children, prompt):
     p.close()
 
 
+@pytest.mark.parametrize("hq,hk", WIDTHS)
 @pytest.mark.parametrize("scale", [0.0, -0.11, 0.7])
-def test_scale_argument(scale):
-    p = Kv4Pair(8, 2)
+def test_scale_argument(scale, hq, hk):
+    p = Kv4Pair(hq, hk)
     tids = p.new_threads(2)
-    p.append(tids, [77, 200], rows(277, 2, 41), rows(277, 2, 42))
-    p.check_attention(tids, rows(2, 8, 43), scale=scale)
+    p.append(tids, [77, 200], rows(277, hk, 41), rows(277, hk, 42))
+    p.check_attention(tids, rows(2, hq, 43), scale=scale)
     p.close()
 
 
-def test_scores_that_grow_along_the_chain():
+@pytest.mark.parametrize("hq,hk", WIDTHS)
+def test_scores_that_grow_along_the_chain(hq, hk):
     """The reference of the softmax has to move again and again."""
-    p = Kv4Pair(8, 2, num_blocks=128)
+    p = Kv4Pair(hq, hk, num_blocks=128)
     (t,) = p.new_threads(1)
     k = rows(700, 2, 44) * 0.1 + torch.linspace(0, 4, 700, device="cuda")[:, None, None]
-    q = torch.ones(1, 8, 128, device="cuda")
-    q[:, 4:] = -1.0
+    q = torch.ones(1, hq, 128, device="cuda")
+    q[:, hq // 2:] = -1.0
     p.append([t], [700], k.to(torch.bfloat16), rows(700, 2, 45))
     p.check_attention([t], q.to(torch.bfloat16))
     p.close()
 
 
+@pytest.mark.parametrize("hq,hk", WIDTHS)
 @pytest.mark.parametrize("order", ["rising", "falling", "mixed"])
-def test_v_rows_of_very_different_size(order):
+def test_v_rows_of_very_different_size(order, hq, hk):
     """Scales of V from 2^-75 to 2^30: the reference follows score and scale together."""
-    p = Kv4Pair(4, 2, num_blocks=128)
+    p = Kv4Pair(hq, hk, num_blocks=128)
     (t,) = p.new_threads(1)
     n = 180
     e = torch.linspace(-75, 30, n)
@@ -185,28 +193,30 @@ def test_v_rows_of_very_different_size(order):
     v = rows(n, 2, 46).float() * torch.exp2(e).cuda()[:, None, None]
     v[::9] = v[::9, :, :1]                                     # rows of equal values: scale 0
     p.append([t], [n], rows(n, 2, 47), v.to(torch.bfloat16))
-    p.check_attention([t], rows(1, 4, 48))
+    p.check_attention([t], rows(1, hq, 48))
     p.close()
 
 
-def test_small_v_rows_with_all_the_weight():
+@pytest.mark.parametrize("hq,hk", WIDTHS)
+def test_small_v_rows_with_all_the_weight(hq, hk):
     """The large rows have next to no weight: what remains is small and has to be exact."""
-    p = Kv4Pair(2, 2, num_blocks=64)
+    p = Kv4Pair(hq, hk, num_blocks=64)
     (t,) = p.new_threads(1)
     k = torch.zeros(200, 2, 128)
     k[100:, :, 0::2] = 1.0
     v = rows(200, 2, 49).float()
     v[:100] *= 1024.0
     v[100:] *= 2.0 ** -12
-    q = torch.full((1, 2, 128), 16.0)
+    q = torch.full((1, hq, 128), 16.0)
     p.append([t], [200], k.to(torch.bfloat16).cuda(), v.to(torch.bfloat16))
     p.check_attention([t], q.to(torch.bfloat16).cuda())
     p.close()
 
 
-def test_a_nan_row_reaches_only_the_threads_that_see_it():
+@pytest.mark.parametrize("hq,hk", WIDTHS)
+def test_a_nan_row_reaches_only_the_threads_that_see_it(hq, hk):
     for side in ("k", "v"):
-        p = Kv4Pair(8, 2)
+        p = Kv4Pair(hq, hk)
         (root,) = p.new_threads(1)
         p.append([root], [40], rows(40, 2, 51), rows(40, 2, 52))
         a, b = p.fork([root, root])
@@ -216,15 +226,15 @@ def test_a_nan_row_reaches_only_the_threads_that_see_it():
         bad[8, 1, 35] = float("nan")
         p.sess.append([b], [6], (bad if side == "k" else k)[6:].contiguous(),
                       (bad if side == "v" else v)[6:].contiguous())
-        q = rows(2, 8, 55)
+        q = rows(2, hq, 55)
         out = p.sess.attention([a, b], q)
         check(out[:1], *p.expected([a], q[:1], p.sess.sm_scale))
-        got = torch.isnan(out[1].float())
-        assert not got[:4].any()                               # the other kv head
+        got, h = torch.isnan(out[1].float()), hq // 2
+        assert not got[:h].any()                               # the other kv head
         if side == "k":
-            assert got[4:].all()
+            assert got[h:].all()
         else:                                                  # the other groups are untouched
-            assert got[4:, 32:64].all() and not got[4:, :32].any() and not got[4:, 64:].any()
+            assert got[h:, 32:64].all() and not got[h:, :32].any() and not got[h:, 64:].any()
         p.close()
 
 
@@ -402,6 +412,39 @@ def test_large_groups_of_items_and_long_chains():
     kids = p.fork([tids[0]] * 20)
     p.append(kids, [3] * 20, rows(60, 2, 154), rows(60, 2, 155))
     p.check_attention(kids, rows(20, 16, 156))
+    p.close()
+
+
+@pytest.mark.parametrize("hq,hk,requests,children", [(64, 16, 40, 4), (128, 16, 30, 4), (40, 40, 16, 3)])
+def test_more_units_than_one_round(hq, hk, requests, children):
+    """Every warp and every CTA works through several units, forwards and backwards: shared
+    prompts on the wide kernel, tails of four, eight and one row."""
+    p = Kv4Pair(hq, hk, num_blocks=2048, max_threads=256, max_blocks=32)
+    roots = p.new_threads(requests)
+    lens = [97 + 16 * (i % 5) + i for i in range(requests)]
+    p.append(roots, lens, rows(sum(lens), hk, 171), rows(sum(lens), hk, 172))
+    kids = p.fork([r for r in roots for _ in range(children)])
+    counts = [1 + (11 * i) % 70 for i in range(len(kids))]
+    p.append(kids, counts, rows(sum(counts), hk, 173), rows(sum(counts), hk, 174))
+    q = rows(len(kids), hq, 175)
+    got = p.sess.attention(kids, q)
+    again = p.sess.attention(kids, q)
+    assert torch.equal(got, again)                             # the same sums in the same order
+    some = list(range(0, len(kids), 7)) + [len(kids) - 1]
+    check(got[some], *p.expected([kids[i] for i in some], q[some], p.sess.sm_scale))
+    p.check_books()
+    p.close()
+
+
+def test_one_long_chain_on_one_kv_head():
+    """More chunks than partial-result rows: the chunks grow until they fit."""
+    p = Kv4Pair(4, 1, num_blocks=20000, max_threads=4, max_blocks=20000)
+    (t,) = p.new_threads(1)
+    n = 250007
+    k, v, q = rows(n, 1, 181), rows(n, 1, 182), rows(1, 4, 183)
+    p.append([t], [n], k, v)
+    got = p.sess.attention([t], q)
+    check(got, *p.expected([t], q, p.sess.sm_scale))
     p.close()
 
 

@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from tests.kv4_helpers import host
+from kv4_helpers import host
 from paper_2401_06761_b200 import binding as B
 from paper_2401_06761_b200.session import Rope
 
