@@ -90,7 +90,7 @@ __device__ __forceinline__ float group_top(uint32_t sl) {
 }
 // Orders chosen so that the converters' shared-memory accesses fall into different banks.  Token of
 // a block that takes row (K', and column of V') pos of it: bits 2 and 3 change places.  Row of V'
-// that holds dim 32 G + 4 g + e: 32 G + 4 g + (e + G) % 4.
+// that holds dim 32 G + 4 g + e: 32 G + 4 g + (e ^ G).
 __device__ __forceinline__ int token_at(int pos) {
   return (pos & 3) | ((pos & 4) << 1) | ((pos & 8) >> 1);
 }
@@ -334,7 +334,7 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int d = 32 * GG + 4 * (word >> 2) + ((e + GG) & 3);        // operand row
+            const int d = 32 * GG + 4 * (word >> 2) + (e ^ GG);      // operand row
             *(uint4*)(bp + kOffVw + b * kOpBytes + d * 128 + (((2 * cw + pg) ^ (d & 7)) << 4)) =
                 make_uint4(out[e][0], out[e][1], out[e][2], out[e][3]);
           }
@@ -607,45 +607,43 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
         break;
       tc_fence_after();
       if (!idle) {
-        l_lo += __shfl_xor_sync(0xffffffffu, l_lo, 1);
-        l_hi += __shfl_xor_sync(0xffffffffu, l_hi, 1);
-        l_lo += __shfl_xor_sync(0xffffffffu, l_lo, 2);
-        l_hi += __shfl_xor_sync(0xffffffffu, l_hi, 2);
-        const float la = __shfl_sync(0xffffffffu, l_lo, 4 * (lane & 7));
-        const float lb = __shfl_sync(0xffffffffu, l_hi, 4 * (lane & 7));
-        const float ra = __shfl_sync(0xffffffffu, ref_lo, 4 * (lane & 7));
-        const float rb = __shfl_sync(0xffffffffu, ref_hi, 4 * (lane & 7));
-        const float l = (lane & 8) ? lb : la, ref = (lane & 8) ? rb : ra;
-        const int row = warp * 16 + (lane & 15);
-        const bool mine = lane < 16 && row < R;
-        const UserRef user = cur.user;
-        const int head = cur.head0 + row % G;
-        const float inv = 1.f / l;
-        const size_t prow = (size_t)(user.slot + cur.add) * HQ + head;
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {                // dims 16 c .. 16 c + 15
-          uint32_t o[16];
-          TMEM_LD_16((tm_o + 16u * c) | lane_sel, o);
-          tmem_wait_ld();
-          auto at = [&](int j) { return __uint_as_float(o[(j & ~3) | ((j + (c >> 1)) & 3)]); };
-          if (mine) {
-            if (user.slot < 0) {
-              uint4* dst = (uint4*)((__nv_bfloat16*)a.out + ((size_t)user.query * HQ + head) * kDim) + 2 * c;
+        for (int d = 1; d <= 2; d <<= 1) {
+          l_lo += __shfl_xor_sync(0xffffffffu, l_lo, d);
+          l_hi += __shfl_xor_sync(0xffffffffu, l_hi, d);
+        }
+        // O in the layout of the scores: rows g8 and g8 + 8, columns 8 k + 2 qd and the next, i.e.
+        // the dims of the same numbers with their last two bits xor'ed with the group's number
 #pragma unroll
-              for (int j = 0; j < 16; j += 8)
-                dst[j >> 3] = make_uint4(pack2(at(j) * inv, at(j + 1) * inv),
-                                         pack2(at(j + 2) * inv, at(j + 3) * inv),
-                                         pack2(at(j + 4) * inv, at(j + 5) * inv),
-                                         pack2(at(j + 6) * inv, at(j + 7) * inv));
-            } else {
-              float4* dst = (float4*)(a.part_o + prow * kDim) + 4 * c;
+        for (int e = 0; e < 2; ++e) {                // (registers: O is read once per row of the lane)
+          const int i = g8 + 8 * e, row = warp * 16 + i;
+          const int query = __shfl_sync(0xffffffffu, cur.user.query, i);
+          const int slot = __shfl_sync(0xffffffffu, cur.user.slot, i);
+          const float l = e ? l_hi : l_lo, ref = e ? ref_hi : ref_lo;
+          const int head = cur.head0 + row % G;
+          const float inv = slot < 0 ? 1.f / l : 1.f;
+          const size_t prow = (size_t)(slot + cur.add) * HQ + head;
+          __nv_bfloat16* const out = (__nv_bfloat16*)a.out + ((size_t)query * HQ + head) * kDim;
+          float* const part = a.part_o + prow * kDim;
 #pragma unroll
-              for (int j = 0; j < 16; j += 4)
-                dst[j >> 2] = make_float4(at(j), at(j + 1), at(j + 2), at(j + 3));
+          for (int c = 0; c < 2; ++c) {              // dims 64 c ..
+            uint32_t o[32];
+            TMEM_LD_16x256((tm_o + 64u * c) | lane_sel, o);
+            tmem_wait_ld();
+            if (row < R) {
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const int GG = 2 * c + (k >> 2);     // columns n, n + 1 hold dims n ^ GG, (n + 1) ^ GG
+                const int n = 64 * c + 8 * k + ((2 * qd) ^ (GG & 2));
+                const float x = __uint_as_float(o[4 * k + 2 * e + (GG & 1)]) * inv;
+                const float y = __uint_as_float(o[4 * k + 2 * e + 1 - (GG & 1)]) * inv;
+                if (slot < 0) *(uint32_t*)(out + n) = pack2(x, y);
+                else *(float2*)(part + n) = make_float2(x, y);
+              }
             }
           }
+          if (row < R && slot >= 0 && qd == 0) a.part_ml[prow] = make_float2(ref, l);
         }
-        if (mine && user.slot >= 0) a.part_ml[prow] = make_float2(ref, l);
       }
       tc_fence_before();
       __syncwarp();

@@ -140,6 +140,7 @@ bool Planner::build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_
   const int64_t kInf = (int64_t)1 << 40;
   int64_t chunk = std::max<int64_t>(128, round_up16(unique * hint_kv_heads_ / (num_sms_ * 8)));
   int max_users = std::max(1, kMaxRowsPerItem / group_);
+  bool many_units = false;
   if (streams_) {
     // With little to do, everything goes to single warps: a wide unit takes some 10 us to come and
     // go, in which a warp does about four blocks.
@@ -166,6 +167,7 @@ bool Planner::build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_
       longest = std::max<int64_t>(longest, g.tok_end - g.tok_begin);
     }
     chunk = std::max<int64_t>(128, round_up16(work / warps));
+    many_units = uncut > warps;
     if (uncut <= warps) {
       auto count = [&](int64_t ck) {
         int64_t u = 0;
@@ -200,7 +202,9 @@ bool Planner::build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_
   auto seg_chunk = [&](const Seg& g) -> int64_t {
     if (chunk >= kInf) return kInf;
     if (streams_) {
-      const int64_t len = std::max(1, g.tok_end - g.tok_begin), pieces = (len + chunk - 1) / chunk;
+      // (with several rounds of units a run a little above the even share is not worth a cut)
+      const int64_t len = std::max(1, g.tok_end - g.tok_begin), over = many_units ? chunk * 2 / 5 : chunk - 1;
+      const int64_t pieces = std::max<int64_t>(1, (len + over) / chunk);
       return round_up16((len + pieces - 1) / pieces);
     }
     if (vec_div == 1 || !single_row(g)) return chunk;
