@@ -140,7 +140,11 @@ def _arr(xs):
     if not isinstance(xs, np.ndarray):
         xs = xs if isinstance(xs, (list, tuple)) else list(xs)
         n = len(xs)
-        return (C.c_int32 * max(n, 1)).from_buffer_copy(struct.pack(f"{max(n, 1)}i", *(xs or (0,)))), n
+        try:                           # (several times as fast as numpy for short lists)
+            raw = struct.pack(f"{max(n, 1)}i", *(xs or (0,)))
+        except struct.error:           # not plain ints of 32 bits: numpy's conversions and errors
+            raw = np.fromiter(xs, dtype=np.int32).tobytes()
+        return (C.c_int32 * max(n, 1)).from_buffer_copy(raw), n
     a = np.ascontiguousarray(xs.astype(np.int32, copy=False))
     buf = (C.c_int32 * max(a.size, 1)).from_buffer_copy(a.tobytes() if a.size else b"\0" * 4)
     return buf, int(a.size)
@@ -225,8 +229,11 @@ def apar_tree_verify_attention(ctx, tid, n_cand, anc_mask, q: int, out: int, sm_
     """anc_mask: one Python int (uint64 bit mask) per candidate, all threads' candidates in order."""
     tids, n = _arr(tid)
     cands, _ = _arr(n_cand)
-    masks = (C.c_uint64 * max(len(anc_mask), 1)).from_buffer_copy(
-        struct.pack(f"{max(len(anc_mask), 1)}Q", *(anc_mask or (0,))))
+    m = max(len(anc_mask), 1)
+    try:
+        masks = (C.c_uint64 * m).from_buffer_copy(struct.pack(f"{m}Q", *(anc_mask or (0,))))
+    except struct.error:               # (a negative int stands for its 64 low bits)
+        masks = (C.c_uint64 * m)(*anc_mask)
     _check(lib.apar_tree_verify_attention(ctx, n, tids, cands, masks, q, out, sm_scale, stream))
 
 

@@ -102,3 +102,28 @@ def test_rope_arguments_refused():
 
 def test_rope_config_layout():
     assert C.sizeof(B.apar_rope_config) == 64
+
+
+def test_argument_lists():
+    """Lists of anything numpy turns into 32-bit ints, as before lists of plain ints got a faster way."""
+    for xs in ([3, -1, 2**31 - 1], (x for x in (3, -1, 2**31 - 1)), [3.0, np.float32(-1), 2**31 - 1],
+               np.array([3, -1, 2**31 - 1]), [np.int64(3), -1, 2**31 - 1]):
+        buf, n = B._arr(xs)
+        assert n == 3 and list(buf) == [3, -1, 2**31 - 1]
+    assert B._arr([])[1] == 0 and B._arr(range(2))[1] == 2
+    with pytest.raises(OverflowError):
+        B._arr([2**31])
+
+
+def test_ancestor_masks_may_be_negative(monkeypatch):
+    seen = []
+
+    class Lib:
+        @staticmethod
+        def apar_tree_verify_attention(ctx, n, tids, cands, masks, q, out, scale, stream):
+            seen.append(list(masks))
+            return 0
+    monkeypatch.setattr(B, "lib", Lib)
+    B.apar_tree_verify_attention(None, [0], [2], [1, 2**64 - 1], 0, 0, 1.0)
+    B.apar_tree_verify_attention(None, [0], [2], [1, -1], 0, 0, 1.0)
+    assert seen == [[1, 2**64 - 1]] * 2
