@@ -54,10 +54,10 @@ constexpr int kOffP = kOffVw + 2 * kOpBytes;         // P: 64 rows x 64 tokens f
 constexpr int kOffRaw = kOffP + kHalfOp;
 constexpr int kOffTok = kOffRaw + kConv * kDepthW * kBlk;     // [2] F + 8 and 2^-(F + 8) of 64 tokens
 constexpr int kOffKb = kOffTok + 2 * 2 * kTok * 4;            // [2][4] 2^(E + 8)
-constexpr int kOffRow = kOffKb + 2 * 4 * 4;                   // [64] the rows' factors
-constexpr int kOffBarW = kOffRow + 64 * 4;
-enum { BW_KFULL = 0, BW_KEMPTY = 2, BW_VFULL = 4, BW_VEMPTY = 6, BW_SFULL = 8, BW_PFULL = 10,
-       BW_PVDONE = 11, BW_QFULL = 12, BW_ODONE = 13, BW_TOTAL = 14 };
+constexpr int kOffRow = kOffKb + 2 * 4 * 4;                   // [4 units][64] the rows' factors
+constexpr int kOffBarW = kOffRow + 4 * 64 * 4;
+enum { BW_FULL = 0, BW_KEMPTY = 2, BW_VEMPTY = 4, BW_SFULL = 6, BW_PFULL = 8, BW_PVDONE = 9,
+       BW_ODONE = 10, BW_TOTAL = 11 };
 constexpr int kSmemWide = kOffBarW + 8 * BW_TOTAL + 16;
 static_assert(2 * (kSmemWide + 1024) <= 228 * 1024, "two CTAs per SM");
 constexpr int kTmemColsW = 256;                      // S at 0 and 64, O at 128
@@ -78,6 +78,11 @@ __device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
   __half2 r = __hfma2(*(__half2*)&a, *(__half2*)&b, *(__half2*)&c);
   return *(uint32_t*)&r;
 }
+__device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
+  __half2 r = __hmul2(*(__half2*)&a, *(__half2*)&b);
+  return *(uint32_t*)&r;
+}
+constexpr uint32_t kSixteenth = 0x2c002c00u;         // f16 1/16 twice
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 // exponent of a non-negative number, kept away from the ends of the range
 __device__ __forceinline__ int exponent_of(float x) {
@@ -108,6 +113,13 @@ __device__ __forceinline__ int token_at(int pos) {
                  "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), \
                  "r"(r[13]), "r"(r[14]), "r"(r[15])                                              \
                : "memory")
+#define TMEM_LD_16x256_32(taddr, r)                                                              \
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 "                                         \
+               "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"                  \
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]),         \
+                 "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),       \
+                 "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])                              \
+               : "r"(taddr))
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -130,15 +142,13 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
   if (threadIdx.x == 0) {
     *cta_abort = *(volatile int*)a.d_error;          // an earlier kernel gave up: do not pile up
     for (int b = 0; b < 2; ++b) {
-      bar_init(bar(BW_KFULL + b), kConv);
+      bar_init(bar(BW_FULL + b), kConv);
       bar_init(bar(BW_KEMPTY + b), 1);
-      bar_init(bar(BW_VFULL + b), kConv);
       bar_init(bar(BW_VEMPTY + b), 1);
       bar_init(bar(BW_SFULL + b), 1);
     }
     bar_init(bar(BW_PFULL), kSoftmax);
     bar_init(bar(BW_PVDONE), 1);
-    bar_init(bar(BW_QFULL), kSoftmax);
     bar_init(bar(BW_ODONE), kSoftmax);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -215,6 +225,55 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
 #pragma unroll 1
     for (int i = 0; i < kDepthW - 1; ++i) load_tile();
     int T = 0, slot = 0;                             // tiles of all units
+    // The query rows of the unit whose first tile is T into the operand, in f16 under a power of two
+    // of their own: this warp's 16, a lane four pieces of rows lane / 4 and lane / 4 + 8.  (By these
+    // warps, which have the time: the softmax warps spent 6000 cycles on it between two units.)
+    auto stage_rows = [&](int pass) -> bool {
+      const int un = unit_of(pass), g8 = lane >> 2, qd = lane & 3;
+      const WorkItem& it = a.d_items[un / HKV];
+      const int count = it.n_users * G, head0 = un % HKV * G, first = it.user_begin;
+      uint4 v[2][4];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = cw * 16 + g8 + 8 * e, u = r / G;
+        const bool on = r < count;
+        const int query = on ? a.d_users[first + u].query : 0;
+        const uint4* src = (const uint4*)a.q + ((size_t)query * HQ + head0 + (r - u * G)) * 16 + qd;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[e][j] = on ? __ldg(src + 4 * j) : make_uint4(0u, 0u, 0u, 0u);
+      }
+      // the products of the unit before with its rows are complete
+      if (T > 0 && !__all_sync(0xffffffffu, bar_wait(bar(BW_KEMPTY + ((T - 1) & 1)), ((T - 1) >> 1) & 1,
+                                                     cta_abort, a.d_error, 23400)))
+        return false;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = cw * 16 + g8 + 8 * e;
+        uint32_t top = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          top = __vmaxu2(top, __vmaxu2(__vmaxu2(v[e][j].x & 0x7fff7fffu, v[e][j].y & 0x7fff7fffu),
+                                       __vmaxu2(v[e][j].z & 0x7fff7fffu, v[e][j].w & 0x7fff7fffu)));
+        top = max(top & 0xffffu, top >> 16);
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const int lift = min(126, 14 + 127 - (int)(top >> 7));
+        const float f = pow2(lift);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int c = qd + 4 * j;
+          const uint32_t w[4] = {v[e][j].x, v[e][j].y, v[e][j].z, v[e][j].w};
+          uint32_t h[4];
+#pragma unroll
+          for (int p = 0; p < 4; ++p) h[p] = f16x2(bf16_lo(w[p]) * f, bf16_hi(w[p]) * f);
+          *(uint4*)(bp + (c >> 3) * kHalfOp + r * 128 + (((c & 7) ^ (r & 7)) << 4)) =
+              make_uint4(h[0], h[1], h[2], h[3]);
+        }
+        // (the softmax warps read them at the unit's first tile: four units on they have)
+        if (qd == 0) ((float*)(bp + kOffRow))[(pass & 3) * 64 + r] = a.scale_log2e * pow2(-lift);
+      }
+      return true;
+    };
     bool ok = true;
 #pragma unroll 1
     for (int pass = 0; pass < my_units && ok; ++pass) {
@@ -245,8 +304,8 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
       for (int p = 0; p < 4; ++p)
 #pragma unroll
         for (int i = 0; i < 2; ++i)                          // word 4 g + G
-          w[i][p] = *(const uint32_t*)(vt + (token_at(8 * pg + 2 * p) >> 1) * kQ4PairBytes +
-                                       4 * ((lane & 15) + 16 * i));
+          w[i][p] = *(const uint32_t*)(vt + (2 * pg) * kQ4PairBytes + 4 * (lane & 15) +
+                                       ((p & 1) + 2 * (p & 2)) * kQ4PairBytes + 64 * i);
       if (tok >= nv) sc = make_uint4(0u, 0u, 0u, 0u);        // (unspecified bits: the row is zeros)
       if (2 * pair >= nv) se = 0u;
       if (2 * pair + 1 >= nv) so = 0u;
@@ -268,14 +327,14 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
       {
         const float de = pow2(-ee), dn = pow2(-eo);
         const float s0 = bf16_lo(se) * (de * 16777216.f), s1 = bf16_lo(so) * (dn * 16777216.f);
-        const uint32_t x1 = f16x2(s0, s1), x16 = f16x2(s0 * 0.0625f, s1 * 0.0625f);
+        const uint32_t x1 = f16x2(s0, s1);
         const uint32_t xl = f16x2(bf16_hi(se) * de, bf16_hi(so) * dn);
 #pragma unroll
         for (int p = 0; p < 4; ++p) {                        // from the lanes that made them
-          const int from = (token_at(8 * pg + 2 * p) >> 1) * 4 + GG;
+          const int from = 8 * pg + GG + 4 * ((p & 1) + 2 * (p & 2));    // pair token_at(8 pg + 2 p) / 2
           v1[p] = __shfl_sync(0xffffffffu, x1, from);
-          v16[p] = __shfl_sync(0xffffffffu, x16, from);
           vl[p] = __shfl_sync(0xffffffffu, xl, from);
+          v16[p] = hmul2(v1[p], kSixteenth);
         }
       }
       // ---- K
@@ -288,23 +347,25 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
         }
         const uint32_t w0[4] = {c0.x, c0.y, c0.z, c0.w}, w1[4] = {c1.x, c1.y, c1.z, c1.w};
         const int r = cw * kBlock + pos;
-        uint8_t* dst = bp + kOffK + b * kOpBytes + r * 128;
+        // 16-byte piece c of the row lies at c ^ (r % 8) of its half; c = 4 j + 2 h + x
+        uint8_t* const dst = bp + kOffK + b * kOpBytes + r * 128;
+        const uint32_t piece = (uint32_t)((2 * h) ^ (r & 7)) << 4;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const float s = bf16_lo(sl[j]) * up, lo = bf16_hi(sl[j]) * down;
-          const uint32_t s1 = f16x2(s, s), s16 = f16x2(s * 0.0625f, s * 0.0625f), lo2 = f16x2(lo, lo);
+          const uint32_t s1 = f16x2(s, s), s16 = hmul2(s1, kSixteenth), lo2 = f16x2(lo, lo);
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
             const uint32_t kw = x ? w1[j] : w0[j], kh = kw >> 8;
-            const int c = 4 * j + 2 * h + x;                 // dims 8 c .. 8 c + 7
-            *(uint4*)(dst + (c >> 3) * kHalfOp + (((c & 7) ^ (r & 7)) << 4)) =
+            *(uint4*)(dst + (j >> 1) * kHalfOp + (piece ^ ((4 * (j & 1) + x) << 4))) =
                 make_uint4(hfma2(kw & kEvenW, s1, lo2), hfma2(kw & kOddW, s16, lo2),
                            hfma2(kh & kEvenW, s1, lo2), hfma2(kh & kOddW, s16, lo2));
           }
         }
-        fence_async_smem();
-        __syncwarp();
-        if (lane == 0) bar_arrive(bar(BW_KFULL + b));
+      }
+      if (t == 0 && !stage_rows(pass)) {
+        ok = false;
+        break;
       }
       // ---- V
       {
@@ -320,9 +381,12 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
           *(float2*)(tokc + kTok) = make_float2(e_on ? pow2(-ee) : 0.f, o_on ? pow2(-eo) : 0.f);
         }
         if (lane == 0) ((float*)(bp + kOffKb))[b * 4 + cw] = pow2(ek);
+        // operand row of word 4 g + G, dim e: d = 32 G + 4 g + (e ^ G), piece 2 cw + pg at its
+        // place xor d % 8
+        const int d0 = 32 * GG + 4 * ((lane & 15) >> 2), at = (2 * cw + pg) ^ (d0 & 4);
+        uint8_t* const dst = bp + kOffVw + b * kOpBytes + d0 * 128;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int word = (lane & 15) + 16 * i;
           uint32_t out[4][4];                                // [dim][pair]
 #pragma unroll
           for (int p = 0; p < 4; ++p) {
@@ -334,14 +398,14 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int d = 32 * GG + 4 * (word >> 2) + (e ^ GG);      // operand row
-            *(uint4*)(bp + kOffVw + b * kOpBytes + d * 128 + (((2 * cw + pg) ^ (d & 7)) << 4)) =
+            const int u = e ^ GG;
+            *(uint4*)(dst + u * 128 + ((at ^ u) << 4) + i * 16 * 128) =
                 make_uint4(out[e][0], out[e][1], out[e][2], out[e][3]);
           }
         }
         fence_async_smem();
         __syncwarp();
-        if (lane == 0) bar_arrive(bar(BW_VFULL + b));
+        if (lane == 0) bar_arrive(bar(BW_FULL + b));
       }
     }
     }
@@ -350,23 +414,23 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
     // ---------------------------------------------------------------- MMA issuer
     constexpr uint32_t kIdescQK = instr_desc_f16(kTok, 64), kIdescPV = instr_desc_f16(kDim, 64);
     constexpr unsigned kAll = 0xffffffffu;
+    // (addresses stay below 2^18: adding to the address field, in 16 bytes, carries nowhere)
+    const uint64_t desc_q = smem_desc(base, 16, 1024), desc_p = smem_desc(base + kOffP, 16, 1024);
     int T = 0, due = -1;                             // tiles so far; the tile whose P V is due
     bool due_first = false, ok = true;
     int due_pass = 0;
     auto product_pv = [&]() -> bool {
       const int b = due & 1;
       bool w8 = bar_wait(bar(BW_PFULL), due & 1, cta_abort, a.d_error, 24100);
-      w8 = w8 && bar_wait(bar(BW_VFULL + b), (due >> 1) & 1, cta_abort, a.d_error, 24200);
       if (due_first && due_pass > 0)                 // the unit before has read its O out
         w8 = w8 && bar_wait(bar(BW_ODONE), (due_pass - 1) & 1, cta_abort, a.d_error, 24300);
       if (!__all_sync(kAll, w8)) return false;
       tc_fence_after();
       if (lane == 0) {
+        const uint64_t desc_v = smem_desc(base + kOffVw + b * kOpBytes, 16, 1024);
 #pragma unroll
         for (int kk = 0; kk < kTok / 16; ++kk)
-          umma_bf16(tmem + 128u, smem_desc(base + kOffP + kk * 32, 16, 1024),
-                    smem_desc(base + kOffVw + b * kOpBytes + kk * 32, 16, 1024), kIdescPV,
-                    !due_first || kk > 0);
+          umma_bf16(tmem + 128u, desc_p + 2 * kk, desc_v + 2 * kk, kIdescPV, !due_first || kk > 0);
         umma_commit(bar(BW_VEMPTY + b));
         umma_commit(bar(BW_PVDONE));
       }
@@ -383,19 +447,18 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
           ok = false;
           break;
         }
-        bool w8 = bar_wait(bar(BW_KFULL + b), (T >> 1) & 1, cta_abort, a.d_error, 24000);
-        if (t == 0) w8 = w8 && bar_wait(bar(BW_QFULL), pass & 1, cta_abort, a.d_error, 24400);
+        bool w8 = bar_wait(bar(BW_FULL + b), (T >> 1) & 1, cta_abort, a.d_error, 24000);
         if (!__all_sync(kAll, w8)) {
           ok = false;
           break;
         }
         tc_fence_after();
         if (lane == 0) {
+          const uint64_t desc_k = smem_desc(base + kOffK + b * kOpBytes, 16, 1024);
 #pragma unroll
           for (int ks = 0; ks < 8; ++ks) {
             const uint32_t off = (ks >> 2) * kHalfOp + (ks & 3) * 32;
-            umma_bf16(tmem + 64u * b, smem_desc(base + off, 16, 1024),
-                      smem_desc(base + kOffK + b * kOpBytes + off, 16, 1024), kIdescQK, ks > 0);
+            umma_bf16(tmem + 64u * b, desc_q + (off >> 4), desc_k + (off >> 4), kIdescQK, ks > 0);
           }
           umma_commit(bar(BW_SFULL + b));
           umma_commit(bar(BW_KEMPTY + b));
@@ -419,12 +482,10 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
     const int g8 = lane >> 2, qd = lane & 3;
     const uint32_t lane_sel = (uint32_t)(warp * 32) << 16, tm_o = tmem + 128u;
     float u_lo = 0.f, u_hi = 0.f;                    // scale * log2(e) / the rows' factors
-    // Query rows of a unit into the operand, in f16 under a power of two of their own.  The
-    // products of the unit before with its rows are complete: their scores have been read.
-    // The unit's item and the users of its rows (lane i, i < 16: row 16 w + i) are read ahead.
+    // The unit's item and the users of the lane's two rows are read ahead.
     struct Rows {
       int count, begin, add, head0;
-      UserRef user;
+      UserRef user[2];
     } cur, nxt;
     auto read_item = [&](int pass, Rows& r) {
       const int un = unit_of(pass);
@@ -435,52 +496,18 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
       r.head0 = un % HKV * G;
     };
     auto read_users = [&](Rows& r) {
-      const int row = warp * 16 + (lane & 15);
-      r.user = UserRef{0, -1};
-      if (row < r.count) r.user = a.d_users[r.begin + row / G];
-    };
-    auto stage_rows = [&](const Rows& rw) {
-      uint4 v[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {                  // half a warp per row
-        const int i = 2 * k + (lane >> 4), r = warp * 16 + i;
-        const int query = __shfl_sync(0xffffffffu, rw.user.query, i);
-        v[k] = make_uint4(0u, 0u, 0u, 0u);
-        if (r < rw.count)
-          v[k] = __ldg((const uint4*)a.q + ((size_t)query * HQ + rw.head0 + r % G) * 16 + (lane & 15));
+      for (int e = 0; e < 2; ++e) {
+        const int row = warp * 16 + g8 + 8 * e;
+        r.user[e] = UserRef{0, -1};
+        if (row < r.count) r.user[e] = a.d_users[r.begin + row / G];
       }
-      float* const factor = (float*)(bp + kOffRow);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int r = warp * 16 + 2 * k + (lane >> 4), c = lane & 15;
-        const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
-        uint32_t top = 0;
-#pragma unroll
-        for (int p = 0; p < 4; ++p) top = max(top, max(w[p] << 17, (w[p] & 0x7fff0000u) << 1));
-#pragma unroll
-        for (int d = 1; d < 16; d <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, d));
-        const int lift = min(126, 14 + 127 - (int)(top >> 24));
-        const float f = pow2(lift);
-        uint32_t h[4];
-#pragma unroll
-        for (int p = 0; p < 4; ++p) h[p] = f16x2(bf16_lo(w[p]) * f, bf16_hi(w[p]) * f);
-        *(uint4*)(bp + (c >> 3) * kHalfOp + r * 128 + (((c & 7) ^ (r & 7)) << 4)) =
-            make_uint4(h[0], h[1], h[2], h[3]);
-        if (c == 0) factor[r] = a.scale_log2e * pow2(-lift);
-      }
-      fence_async_smem();
-      __syncwarp();
-      if (lane == 0) bar_arrive(bar(BW_QFULL));
-      u_lo = factor[warp * 16 + g8];
-      u_hi = factor[warp * 16 + g8 + 8];
-      __syncwarp();
     };
     int T = 0;
     bool alive = true;
     if (my_units) {
       read_item(0, nxt);
       read_users(nxt);
-      stage_rows(nxt);
     }
 #pragma unroll 1
     for (int pass = 0; pass < my_units; ++pass) {
@@ -495,12 +522,17 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
       for (int t = 0; t < n_tiles; ++t, ++T) {
         const int b = T & 1;
         bool ok = bar_wait(bar(BW_SFULL + b), (T >> 1) & 1, cta_abort, a.d_error, 22000);
-        ok = ok && bar_wait(bar(BW_VFULL + b), (T >> 1) & 1, cta_abort, a.d_error, 22100);
+        ok = ok && bar_wait(bar(BW_FULL + b), (T >> 1) & 1, cta_abort, a.d_error, 22100);
         if (!__all_sync(0xffffffffu, ok)) {
           alive = false;
           break;
         }
         tc_fence_after();
+        if (t == 0) {
+          const float* factor = (const float*)(bp + kOffRow) + (pass & 3) * 64 + warp * 16 + g8;
+          u_lo = factor[0];
+          u_hi = factor[8];
+        }
         uint32_t pk_lo[8], pk_hi[8];
         if (!idle) {
           uint32_t sr[32];
@@ -587,12 +619,12 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
         }
         if (!idle) {
           const int r = warp * 16 + g8;              // (rows r and r + 8: the same swizzle)
-          uint8_t* p = bp + kOffP + r * 128 + 4 * qd;
+          uint8_t* const p = bp + kOffP + r * 128;
+          const uint32_t piece = (uint32_t)((r & 7) << 4 | 4 * qd);
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
-            const int off = (k ^ (r & 7)) << 4;
-            *(uint32_t*)(p + off) = pk_lo[k];
-            *(uint32_t*)(p + 8 * 128 + off) = pk_hi[k];
+            *(uint32_t*)(p + (piece ^ (k << 4))) = pk_lo[k];
+            *(uint32_t*)(p + (piece ^ (k << 4)) + 8 * 128) = pk_hi[k];
           }
           fence_async_smem();
         }
@@ -602,7 +634,6 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
         if (t == 0 && more) read_users(nxt);
       }
       if (!alive) break;
-      if (more) stage_rows(nxt);
       if (!__all_sync(0xffffffffu, bar_wait(bar(BW_PVDONE), (T - 1) & 1, cta_abort, a.d_error, 22300)))
         break;
       tc_fence_after();
@@ -614,35 +645,39 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
         }
         // O in the layout of the scores: rows g8 and g8 + 8, columns 8 k + 2 qd and the next, i.e.
         // the dims of the same numbers with their last two bits xor'ed with the group's number
+        uint8_t* dst[2];
+        bool on[2], last[2];
+        float inv[2];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {                // (registers: O is read once per row of the lane)
-          const int i = g8 + 8 * e, row = warp * 16 + i;
-          const int query = __shfl_sync(0xffffffffu, cur.user.query, i);
-          const int slot = __shfl_sync(0xffffffffu, cur.user.slot, i);
-          const float l = e ? l_hi : l_lo, ref = e ? ref_hi : ref_lo;
+        for (int e = 0; e < 2; ++e) {
+          const int row = warp * 16 + g8 + 8 * e, slot = cur.user[e].slot;
           const int head = cur.head0 + row % G;
-          const float inv = slot < 0 ? 1.f / l : 1.f;
-          const size_t prow = (size_t)(slot + cur.add) * HQ + head;
-          __nv_bfloat16* const out = (__nv_bfloat16*)a.out + ((size_t)query * HQ + head) * kDim;
-          float* const part = a.part_o + prow * kDim;
+          on[e] = row < R;
+          last[e] = slot < 0;
+          inv[e] = last[e] ? 1.f / (e ? l_hi : l_lo) : 1.f;
+          const size_t prow = (size_t)((last[e] ? 0 : slot) + cur.add) * HQ + head;
+          dst[e] = last[e] ? (uint8_t*)a.out + ((size_t)cur.user[e].query * HQ + head) * (kDim * 2)
+                           : (uint8_t*)(a.part_o + prow * kDim);
+          if (on[e] && !last[e] && qd == 0)
+            a.part_ml[prow] = e ? make_float2(ref_hi, l_hi) : make_float2(ref_lo, l_lo);
+        }
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {              // dims 64 c ..
-            uint32_t o[32];
-            TMEM_LD_16x256((tm_o + 64u * c) | lane_sel, o);
-            tmem_wait_ld();
-            if (row < R) {
+        for (int GG = 0; GG < 4; ++GG) {             // columns n, n + 1 hold dims n ^ GG, (n + 1) ^ GG
+          uint32_t o[16];
+          TMEM_LD_16x256_32((tm_o + 32u * GG) | lane_sel, o);
+          tmem_wait_ld();
 #pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                const int GG = 2 * c + (k >> 2);     // columns n, n + 1 hold dims n ^ GG, (n + 1) ^ GG
-                const int n = 64 * c + 8 * k + ((2 * qd) ^ (GG & 2));
-                const float x = __uint_as_float(o[4 * k + 2 * e + (GG & 1)]) * inv;
-                const float y = __uint_as_float(o[4 * k + 2 * e + 1 - (GG & 1)]) * inv;
-                if (slot < 0) *(uint32_t*)(out + n) = pack2(x, y);
-                else *(float2*)(part + n) = make_float2(x, y);
+          for (int e = 0; e < 2; ++e)
+            if (on[e]) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const int n = 32 * GG + 8 * k + ((2 * qd) ^ (GG & 2));
+                const float x = __uint_as_float(o[4 * k + 2 * e + (GG & 1)]) * inv[e];
+                const float y = __uint_as_float(o[4 * k + 2 * e + 1 - (GG & 1)]) * inv[e];
+                if (last[e]) *(uint32_t*)(dst[e] + 2 * n) = pack2(x, y);
+                else *(float2*)(dst[e] + 4 * n) = make_float2(x, y);
               }
             }
-          }
-          if (row < R && slot >= 0 && qd == 0) a.part_ml[prow] = make_float2(ref, l);
         }
       }
       tc_fence_before();
