@@ -587,37 +587,42 @@ attn_q4_kernel(const AttnArgs a, const Q4Units units) {
   pdl_wait();                        // "this grid has completed" implies the one before it has
 }
 
-// End of a verification, one warp per (candidate, head): the candidates it sees, read straight from
-// the 4-bit pool, and the partial results of the committed tokens before them, folded into the
-// output.  The halves of the warp take the set bits of the mask in turn (a candidate of a tree
-// sees few others), and the partial results too; lane c of a half holds dims 8 c .. 8 c + 7.  What
-// it reads first depends on nothing the attention kernels write, so it may start before them.
+// End of a verification, one warp per candidate and kHeads heads of one kv head: the candidates it
+// sees, read straight from the 4-bit pool, and the partial results of the committed tokens before
+// them, folded into the output.  The halves of the warp take the set bits of the mask in turn (a
+// candidate of a tree sees few others), and the partial results too; lane c of a half holds dims
+// 8 c .. 8 c + 7.  What it reads first depends on nothing the attention kernels write, so it may
+// start before them.  Turning the rows into numbers is what costs: heads that share them share it.
+template <int kHeads>
 __global__ void __launch_bounds__(128) q4_verify_finish_kernel(const AttnArgs a,
                                                                const VerifyDesc* __restrict__ descs) {
   const VerifyDesc d = descs[blockIdx.x];
   const int G = a.shape.group, HQ = a.shape.num_q_heads, HKV = a.shape.num_kv_heads;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int half = lane >> 4, c = lane & 15;
-  const int head = blockIdx.y * 4 + warp;
-  if (head >= HQ) return;
-  const int kvh = head / G;
+  const int head0 = (blockIdx.y * 4 + warp) * kHeads;
+  if (head0 >= HQ) return;
+  const int kvh = head0 / G;
   const int32_t* table = a.d_tables + (size_t)d.row * a.shape.table_stride;
-  float qf[8], o[8];
-  {
-    const uint4 qv = __ldg((const uint4*)a.q + ((size_t)d.query * HQ + head) * 16 + c);
+  float qf[kHeads][8], o[kHeads][8], m[kHeads], l[kHeads];   // m, l of this half
+#pragma unroll
+  for (int h = 0; h < kHeads; ++h) {
+    const uint4 qv = __ldg((const uint4*)a.q + ((size_t)d.query * HQ + head0 + h) * 16 + c);
     const uint32_t w[4] = {qv.x, qv.y, qv.z, qv.w};
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-      qf[2 * x] = bf16_lo(w[x]) * a.scale_log2e;
-      qf[2 * x + 1] = bf16_hi(w[x]) * a.scale_log2e;
-      o[2 * x] = o[2 * x + 1] = 0.f;
+      qf[h][2 * x] = bf16_lo(w[x]) * a.scale_log2e;
+      qf[h][2 * x + 1] = bf16_hi(w[x]) * a.scale_log2e;
+      o[h][2 * x] = o[h][2 * x + 1] = 0.f;
     }
+    m[h] = -INFINITY;
+    l[h] = 0.f;
   }
-  float m = -INFINITY, l = 0.f;                      // of this half
   uint64_t left = d.mask;
   while (left) {
     // two candidates per half at a time
-    float t[2], vf[2][8];
+    constexpr int kSums = 2 * kHeads;                // sum n * kHeads + h: candidate n, head h
+    float t[kSums], vf[2][8];
     bool on[2];
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
@@ -628,7 +633,8 @@ __global__ void __launch_bounds__(128) q4_verify_finish_kernel(const AttnArgs a,
       const bool two = left != 0;
       left &= left - 1;
       on[n] = half ? two : any;
-      t[n] = 0.f;
+#pragma unroll
+      for (int h = 0; h < kHeads; ++h) t[n * kHeads + h] = 0.f;
 #pragma unroll
       for (int x = 0; x < 8; ++x) vf[n][x] = 0.f;
       if (on[n]) {
@@ -638,73 +644,99 @@ __global__ void __launch_bounds__(128) q4_verify_finish_kernel(const AttnArgs a,
         q4_load8_k((const uint8_t*)a.k_pool + tile, pos & (kBlock - 1), c, kf);
         q4_load8_v((const uint8_t*)a.v_pool + tile, pos & (kBlock - 1), c, vf[n]);
 #pragma unroll
-        for (int x = 0; x < 8; ++x) t[n] = fmaf(qf[x], kf[x], t[n]);
+        for (int h = 0; h < kHeads; ++h)
+#pragma unroll
+          for (int x = 0; x < 8; ++x) t[n * kHeads + h] = fmaf(qf[h][x], kf[x], t[n * kHeads + h]);
       }
     }
+    // sums over the 16 lanes: each step halves the sums a lane carries, then lane i 16 / kSums has i
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
+    for (int x = 8, left_of = kSums; x; x >>= 1) {
+      left_of >>= 1;
+      if (left_of) {
 #pragma unroll
-      for (int x = 8; x; x >>= 1) t[n] += __shfl_xor_sync(0xffffffffu, t[n], x);
-      if (!on[n]) t[n] = -INFINITY;
+        for (int i = 0; i < kSums / 2; ++i)
+          if (i < left_of) {
+            const bool up = c & x;
+            const float give = up ? t[i] : t[i + left_of], keep = up ? t[i + left_of] : t[i];
+            t[i] = keep + __shfl_xor_sync(0xffffffffu, give, x);
+          }
+      } else {
+        t[0] += __shfl_xor_sync(0xffffffffu, t[0], x);
+      }
     }
-    const float mn = fmaxf(m, fmaxf(t[0], t[1]));
-    const float corr = m == -INFINITY ? 0.f : ex2(m - mn);
-    const float p0 = on[0] ? ex2(t[0] - mn) : 0.f, p1 = on[1] ? ex2(t[1] - mn) : 0.f;
-    m = mn;
-    l = fmaf(l, corr, p0 + p1);
+    const float own = t[0];
 #pragma unroll
-    for (int x = 0; x < 8; ++x) o[x] = fmaf(p0, vf[0][x], fmaf(p1, vf[1][x], o[x] * corr));
+    for (int i = 0; i < kSums; ++i) {
+      t[i] = __shfl_sync(0xffffffffu, own, i * (16 / kSums), 16);
+      if (!on[i / kHeads]) t[i] = -INFINITY;
+    }
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h) {
+      const float t0 = t[h], t1 = t[kHeads + h];
+      const float mn = fmaxf(m[h], fmaxf(t0, t1));
+      const float corr = m[h] == -INFINITY ? 0.f : ex2(m[h] - mn);
+      const float p0 = on[0] ? ex2(t0 - mn) : 0.f, p1 = on[1] ? ex2(t1 - mn) : 0.f;
+      m[h] = mn;
+      l[h] = fmaf(l[h], corr, p0 + p1);
+#pragma unroll
+      for (int x = 0; x < 8; ++x) o[h][x] = fmaf(p0, vf[0][x], fmaf(p1, vf[1][x], o[h][x] * corr));
+    }
   }
   pdl_wait();                                        // partial results of the attention kernels
-  for (int j0 = half; j0 < d.parts; j0 += 8) {       // four per half at a time
-    float2 ml[4];
-    float4 x0[4], x1[4];
-    float mn = m;
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      const int j = j0 + 2 * n;
-      ml[n] = make_float2(-INFINITY, 0.f);
-      x0[n] = x1[n] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (j < d.parts) {
-        const size_t prow = (size_t)(d.slot - d.parts + j) * HQ + head;
-        ml[n] = a.part_ml[prow];
-        const float4* src = (const float4*)(a.part_o + prow * kDim) + 2 * c;
-        x0[n] = src[0];
-        x1[n] = src[1];
+  for (int h = 0; h < kHeads; ++h) {
+    const int head = head0 + h;
+    for (int j0 = half; j0 < d.parts; j0 += 8) {     // four per half at a time
+      float2 ml[4];
+      float4 x0[4], x1[4];
+      float mn = m[h];
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const int j = j0 + 2 * n;
+        ml[n] = make_float2(-INFINITY, 0.f);
+        x0[n] = x1[n] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (j < d.parts) {
+          const size_t prow = (size_t)(d.slot - d.parts + j) * HQ + head;
+          ml[n] = a.part_ml[prow];
+          const float4* src = (const float4*)(a.part_o + prow * kDim) + 2 * c;
+          x0[n] = src[0];
+          x1[n] = src[1];
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < 4; ++n) mn = fmaxf(mn, ml[n].x);
+      const float corr = m[h] == -INFINITY ? 0.f : ex2(m[h] - mn);
+      m[h] = mn;
+      l[h] *= corr;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) o[h][x] *= corr;
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const float w = ml[n].x == -INFINITY ? 0.f : ex2(ml[n].x - mn);
+        l[h] = fmaf(ml[n].y, w, l[h]);
+        o[h][0] = fmaf(x0[n].x, w, o[h][0]); o[h][1] = fmaf(x0[n].y, w, o[h][1]);
+        o[h][2] = fmaf(x0[n].z, w, o[h][2]); o[h][3] = fmaf(x0[n].w, w, o[h][3]);
+        o[h][4] = fmaf(x1[n].x, w, o[h][4]); o[h][5] = fmaf(x1[n].y, w, o[h][5]);
+        o[h][6] = fmaf(x1[n].z, w, o[h][6]); o[h][7] = fmaf(x1[n].w, w, o[h][7]);
       }
     }
+    __syncwarp();
+    const float M = fmaxf(m[h], __shfl_xor_sync(0xffffffffu, m[h], 16));
+    const float f = m[h] == -INFINITY ? 0.f : ex2(m[h] - M);   // (a half may have seen nothing)
+    l[h] *= f;
+    l[h] += __shfl_xor_sync(0xffffffffu, l[h], 16);
 #pragma unroll
-    for (int n = 0; n < 4; ++n) mn = fmaxf(mn, ml[n].x);
-    const float corr = m == -INFINITY ? 0.f : ex2(m - mn);
-    m = mn;
-    l *= corr;
-#pragma unroll
-    for (int x = 0; x < 8; ++x) o[x] *= corr;
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      const float w = ml[n].x == -INFINITY ? 0.f : ex2(ml[n].x - mn);
-      l = fmaf(ml[n].y, w, l);
-      o[0] = fmaf(x0[n].x, w, o[0]); o[1] = fmaf(x0[n].y, w, o[1]);
-      o[2] = fmaf(x0[n].z, w, o[2]); o[3] = fmaf(x0[n].w, w, o[3]);
-      o[4] = fmaf(x1[n].x, w, o[4]); o[5] = fmaf(x1[n].y, w, o[5]);
-      o[6] = fmaf(x1[n].z, w, o[6]); o[7] = fmaf(x1[n].w, w, o[7]);
+    for (int x = 0; x < 8; ++x) {
+      o[h][x] *= f;
+      o[h][x] += __shfl_xor_sync(0xffffffffu, o[h][x], 16);
     }
+    const float inv = 1.f / l[h];                    // (a candidate sees itself)
+    if (half == 0)
+      *((uint4*)((__nv_bfloat16*)a.out + ((size_t)d.query * HQ + head) * kDim) + c) =
+          make_uint4(pack2(o[h][0] * inv, o[h][1] * inv), pack2(o[h][2] * inv, o[h][3] * inv),
+                     pack2(o[h][4] * inv, o[h][5] * inv), pack2(o[h][6] * inv, o[h][7] * inv));
   }
-  __syncwarp();
-  const float M = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-  const float f = m == -INFINITY ? 0.f : ex2(m - M);   // (a half may have seen nothing)
-  l *= f;
-  l += __shfl_xor_sync(0xffffffffu, l, 16);
-#pragma unroll
-  for (int x = 0; x < 8; ++x) {
-    o[x] *= f;
-    o[x] += __shfl_xor_sync(0xffffffffu, o[x], 16);
-  }
-  const float inv = 1.f / l;                         // (a candidate sees itself)
-  if (half == 0)
-    *((uint4*)((__nv_bfloat16*)a.out + ((size_t)d.query * HQ + head) * kDim) + c) =
-        make_uint4(pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv),
-                   pack2(o[4] * inv, o[5] * inv), pack2(o[6] * inv, o[7] * inv));
 }
 
 // out = sum_j o_j 2^(m_j - M) / sum_j l_j 2^(m_j - M) over the partial results of one (query, head).
@@ -813,8 +845,12 @@ cudaError_t launch_attention_q4(const AttnArgs& a, const Q4Items& it, cudaStream
 cudaError_t launch_q4_verify_finish(const AttnArgs& a, const VerifyDesc* d_desc, int n_desc,
                                     cudaStream_t st) {
   if (n_desc <= 0) return cudaSuccess;
-  return launch_kernel(q4_verify_finish_kernel, dim3(n_desc, (a.shape.num_q_heads + 3) / 4), dim3(128), 0,
-                       st, a.pdl != 0, a, d_desc);
+  // Heads of one warp, two where two share a kv head: 2496 candidates x 32 heads take 57 us, with one
+  // head 72, with four (122 registers) 64.
+  const int heads = a.shape.group % 2 == 0 ? 2 : 1;
+  auto* kernel = heads == 2 ? q4_verify_finish_kernel<2> : q4_verify_finish_kernel<1>;
+  return launch_kernel(kernel, dim3(n_desc, (a.shape.num_q_heads + 4 * heads - 1) / (4 * heads)),
+                       dim3(128), 0, st, a.pdl != 0, a, d_desc);
 }
 
 }  // namespace apar
