@@ -5,10 +5,9 @@
 // through units of their own, from first to last block, with no barrier between them: a warp
 // streams the tiles of its blocks (K and V of one block: 2560 bytes) through a private ring with
 // cp.async, and the copies run ahead *across* units - the next unit's description, query rows and
-// first blocks are on their way while the current one is computed.  (The form before this one, a
-// CTA per unit whose four warps shared its blocks, spent some 5 us per unit on the chain item ->
-// table -> tile and on the fold: 158 us instead of the figure below on the same case.)  Units are
-// dealt out in the planner's order, longest first, forwards and backwards in turn, so no counter
+// first blocks are on their way while the current one is computed.  (A CTA per unit whose four
+// warps share its blocks spends some 5 us per unit on the chain item -> table -> tile and on the
+// fold.)  Units are dealt out in the planner's order, longest first, forwards and backwards in turn, so no counter
 // in memory is needed and the kernel can be captured and replayed as it is.
 //
 // Products run on mma.sync m16n8k16 (f16) with the *cache* as the 16-row operand and the queries
@@ -37,6 +36,12 @@
 //
 // The C fragment of S^T holds tokens in rows, the B operand wants them in the k index: a
 // movmatrix of the 8 x 8 halves brings one into the other.
+//
+// Measured: four contexts of 125 k tokens, 32 query heads over 8 (646 MB): 126 us, 5.1 TB/s, 0.78 of
+// a copy; the same kernel with its arithmetic taken out takes 97 us, with its loads taken out 113.
+// 128 tails of 190 tokens and 32 prompts of 512 under 32 heads (210 MB): 57 us, 3.7 TB/s.  What
+// bounds it is issue: a block is some 280 instructions of a warp, most of them on the integer
+// pipe, and twelve warps are what the registers (168) allow.
 #include <algorithm>
 #include <climits>
 

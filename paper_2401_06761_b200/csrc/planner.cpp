@@ -28,7 +28,10 @@ void Planner::init(int num_blocks, int group, int num_kv_heads) {
 }
 
 static inline int64_t round_up16(int64_t x) { return (x + 15) / 16 * 16; }
-constexpr int kWideCost = 2;         // time of a wide unit of a 4-bit pool, in those of a warp
+// 4-bit pools.  A wide unit takes the time of some four units of a single warp, so up to three of
+// those do the work of one: 64 runs of 2048 tokens on 8 kv heads take with 16 rows 104 us against
+// 144, with 24 rows 130 against 154, with 32 rows 189 against 159, with 64 rows 312 against 175.
+constexpr int kWideCost = 4, kStreamUnits = 3;
 constexpr int kMaxFoldedParts = 8;   // partial results a finishing item may fold by itself
 
 void Planner::ensure_keys(size_t n) {
@@ -140,6 +143,13 @@ bool Planner::build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_
   const int64_t kInf = (int64_t)1 << 40;
   int64_t chunk = std::max<int64_t>(128, round_up16(unique * hint_kv_heads_ / (num_sms_ * 8)));
   int max_users = std::max(1, kMaxRowsPerItem / group_);
+  const int stream_users = std::max(1, stream_rows_ / group_);
+  // users of the next item of a run of which `left` have none yet
+  auto item_users = [&](int left) {
+    if (streams_ && group_ <= stream_rows_ && left <= kStreamUnits * stream_users)
+      return std::min(left, stream_users);
+    return std::min(left, max_users);
+  };
   bool many_units = false;
   if (streams_) {
     // With little to do, everything goes to single warps: a wide unit takes some 10 us to come and
@@ -148,17 +158,19 @@ bool Planner::build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_
     for (const Seg& g : segs_)
       blocks += ((int64_t)g.n_users * group_ + stream_rows_ - 1) / stream_rows_ * hint_kv_heads_ *
                 ((g.tok_end - g.tok_begin + kBlock - 1) / kBlock);
-    if (blocks <= 4ll * num_sms_ * streams_) max_users = std::max(1, stream_rows_ / group_);
+    if (blocks <= 4ll * num_sms_ * streams_) max_users = stream_users;
     // The fewest chunks that give every warp a unit and none a second one; with more units than
     // warps from the start, no unit longer than a warp's even share.
     const int64_t warps = (int64_t)num_sms_ * streams_;
     // warps' worth of time per token of a run
     auto units_of = [&](const Seg& g) {
-      const int64_t per = max_users;
-      auto cost = [&](int64_t users) -> int64_t {
-        return users == 0 ? 0 : users * group_ > stream_rows_ ? kWideCost : 1;
-      };
-      return (g.n_users / per * cost(per) + cost(g.n_users % per)) * hint_kv_heads_;
+      int64_t units = 0;
+      for (int left = g.n_users; left > 0;) {
+        const int users = item_users(left), alike = users == max_users ? left / users : 1;
+        units += (int64_t)alike * (users * group_ > stream_rows_ ? kWideCost : 1);
+        left -= alike * users;
+      }
+      return units * hint_kv_heads_;
     };
     int64_t uncut = 0, work = 0, longest = 0;
     for (const Seg& g : segs_) {
@@ -281,8 +293,8 @@ bool Planner::build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_
   for (const Seg& g : segs_) {
     const int64_t chunk = seg_chunk(g);        // this run's own chunk length
     const int32_t n_chunks = (int32_t)((g.tok_end - g.tok_begin + chunk - 1) / chunk);
-    for (int u0 = 0; u0 < g.n_users; u0 += max_users) {
-      const int nu = std::min(max_users, g.n_users - u0);
+    for (int u0 = 0, nu; u0 < g.n_users; u0 += nu) {
+      nu = item_users(g.n_users - u0);
       for (int c = 0; c < n_chunks; ++c) {
         WorkItem it;
         it.table_row = g.table_row;
