@@ -436,6 +436,23 @@ def test_more_units_than_one_round(hq, hk, requests, children):
     p.close()
 
 
+@pytest.mark.parametrize("children", [6, 7, 18, 22, 23])
+def test_runs_whose_rows_fill_wide_units_and_leave_a_rest(children):
+    """24, 28, 64 + 8, 64 + 24 and 64 + 28 rows on a shared prompt, with work enough for wide units."""
+    hq, hk, requests, held = 64, 16, 6, 401
+    p = Kv4Pair(hq, hk, num_blocks=1024, max_threads=256, max_blocks=32)
+    roots = p.new_threads(requests)
+    p.append(roots, [held] * requests, rows(held * requests, hk, 191), rows(held * requests, hk, 192))
+    kids = p.fork([r for r in roots for _ in range(children)])
+    n = len(kids)
+    p.append(kids, [2] * n, rows(2 * n, hk, 193), rows(2 * n, hk, 194))
+    q = rows(n, hq, 195)
+    got = p.sess.attention(kids, q)
+    some = [i for i in range(n) if i % children in (0, 1, 15, 16, 17, 21, children - 1)][:2 * children]
+    check(got[some], *p.expected([kids[i] for i in some], q[some], p.sess.sm_scale))
+    p.close()
+
+
 def test_one_long_chain_on_one_kv_head():
     """More chunks than partial-result rows: the chunks grow until they fit."""
     p = Kv4Pair(4, 1, num_blocks=20000, max_threads=4, max_blocks=20000)
