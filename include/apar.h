@@ -444,8 +444,10 @@ typedef struct {
  *   positions [device] int32 [n]
  *   q, q_out  [device] bf16, head h of token i at q + i * q_stride + h * 128 elements; a stride of
  *             0 means contiguous rows (num_q_heads * 128); k, k_out likewise
- *   q_out == q with equal strides rotates in place; any other overlap of an input with its own
- *   output is refused.  num_q_heads or num_kv_heads may be 0 (that side's pointers are ignored).
+ *   q_out == q with equal strides rotates in place; any other overlap of an input's address range
+ *   with its own output's is refused.  The rows of one side's output must not overlap the rows of
+ *   the other side (rows of both that lie in turn in one array are fine).  num_q_heads or
+ *   num_kv_heads may be 0 (that side's pointers are ignored).
  * Rows on 16-byte boundaries (and rotary_dim a multiple of 16 in the half layout) take a vectorised
  * kernel, others an element-wise one.  No context, no workspace; can be captured in a graph.
  * Errors: INVALID_ARG, UNSUPPORTED (head_dim), CUDA (read it with cudaGetLastError). */

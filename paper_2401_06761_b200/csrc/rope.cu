@@ -242,7 +242,7 @@ extern "C" apar_status apar_rope(const apar_rope_config* cfg, int32_t n, const i
   }
   const int64_t total_heads = (int64_t)num_q_heads + num_kv_heads;
   if (n == 0 || total_heads == 0) return APAR_OK;
-  if (!positions) return APAR_ERR_INVALID_ARG;
+  if (!positions || ((uintptr_t)positions & 3)) return APAR_ERR_INVALID_ARG;
   if (total_heads > 65536) return APAR_ERR_INVALID_ARG;
   // Several tokens to a CTA once there are enough of them to fill the machine that way.
   const int tokens = n >= 4096 ? kMaxTokens : 1;

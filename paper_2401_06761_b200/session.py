@@ -33,13 +33,16 @@ class Rope:
         n = q.shape[0]
         assert positions.dtype == torch.int32 and positions.is_contiguous() and positions.is_cuda
         assert positions.shape == (n,)
+        here = torch.cuda.current_device()             # (the launch goes to its current stream)
+        assert positions.get_device() == here
         outs, sides = [], []
         for x in (q, k):
             if x is None:
                 outs.append(None)
                 sides += [0, 0, 0, 0, 0]
                 continue
-            assert x.is_cuda and x.dtype == torch.bfloat16 and x.dim() == 3 and x.shape[0] == n
+            assert x.get_device() == here and x.dtype == torch.bfloat16
+            assert x.dim() == 3 and x.shape[0] == n
             assert x.shape[2] == self.cfg.head_dim
             assert x.stride(2) == 1 and (x.shape[1] == 1 or x.stride(1) == x.shape[2])
             out = x if inplace else torch.empty(x.shape, dtype=x.dtype, device=x.device)

@@ -89,6 +89,7 @@ def test_rope_arguments_refused():
     refused("UNSUPPORTED", B.make_rope_config(head_dim=64, rotary_dim=64), 1, p, 1, p, 0, p, 0, 0, 0, 0, 0, 0)
     refused("INVALID_ARG", cfg, -1, p, 1, p, 0, p, 0, 0, 0, 0, 0, 0)
     refused("INVALID_ARG", cfg, 1, 0, 1, p, 0, p, 0, 0, 0, 0, 0, 0)                # no positions
+    refused("INVALID_ARG", cfg, 1, p + 2, 1, p, 0, p, 0, 0, 0, 0, 0, 0)            # positions off 4 bytes
     refused("INVALID_ARG", cfg, 1, p, 1, 0, 0, p, 0, 0, 0, 0, 0, 0)                # no q
     refused("INVALID_ARG", cfg, 1, p, 0, 0, 0, 0, 0, 2, p, 0, 0, 0)                # no k_out
     refused("INVALID_ARG", cfg, 4, p, 2, p, 255, 2 * p, 0, 0, 0, 0, 0, 0)          # stride below a row
