@@ -453,6 +453,18 @@ def test_runs_whose_rows_fill_wide_units_and_leave_a_rest(children):
     p.close()
 
 
+@pytest.mark.parametrize("hq,hk", WIDTHS)
+def test_a_thread_listed_several_times(hq, hk):
+    p = Kv4Pair(hq, hk)
+    t, u = p.new_threads(2)
+    p.append([t, u], [70, 33], rows(103, hk, 201), rows(103, hk, 202))
+    p.check_attention([t, u, t, t, u] * 3, rows(15, hq, 203))
+    (c,) = p.fork([t])
+    p.append([c], [1], rows(1, hk, 204), rows(1, hk, 205))
+    p.check_attention([c, t, c], rows(3, hq, 206))
+    p.close()
+
+
 def test_one_long_chain_on_one_kv_head():
     """More chunks than partial-result rows: the chunks grow until they fit."""
     p = Kv4Pair(4, 1, num_blocks=20000, max_threads=4, max_blocks=20000)
