@@ -692,12 +692,12 @@ __global__ void __launch_bounds__(128) q4_verify_finish_kernel(const AttnArgs a,
 #pragma unroll
   for (int h = 0; h < kHeads; ++h) {
     const int head = head0 + h;
-    for (int j0 = half; j0 < d.parts; j0 += 8) {     // four per half at a time
-      float2 ml[4];
-      float4 x0[4], x1[4];
+    for (int j0 = half; j0 < d.parts; j0 += 4) {     // two per half at a time
+      float2 ml[2];
+      float4 x0[2], x1[2];
       float mn = m[h];
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
+      for (int n = 0; n < 2; ++n) {
         const int j = j0 + 2 * n;
         ml[n] = make_float2(-INFINITY, 0.f);
         x0[n] = x1[n] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -710,14 +710,14 @@ __global__ void __launch_bounds__(128) q4_verify_finish_kernel(const AttnArgs a,
         }
       }
 #pragma unroll
-      for (int n = 0; n < 4; ++n) mn = fmaxf(mn, ml[n].x);
+      for (int n = 0; n < 2; ++n) mn = fmaxf(mn, ml[n].x);
       const float corr = m[h] == -INFINITY ? 0.f : ex2(m[h] - mn);
       m[h] = mn;
       l[h] *= corr;
 #pragma unroll
       for (int x = 0; x < 8; ++x) o[h][x] *= corr;
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
+      for (int n = 0; n < 2; ++n) {
         const float w = ml[n].x == -INFINITY ? 0.f : ex2(ml[n].x - mn);
         l[h] = fmaf(ml[n].y, w, l[h]);
         o[h][0] = fmaf(x0[n].x, w, o[h][0]); o[h][1] = fmaf(x0[n].y, w, o[h][1]);
@@ -745,9 +745,9 @@ __global__ void __launch_bounds__(128) q4_verify_finish_kernel(const AttnArgs a,
 }
 
 // out = sum_j o_j 2^(m_j - M) / sum_j l_j 2^(m_j - M) over the partial results of one (query, head).
-// kWarpsPerRow warps share a row's parts (1: four rows to a CTA); (m, l) and o of up to eight parts
+// kWarpsPerRow warps share a row's parts (1: four rows to a CTA); (m, l) and o of kRound parts a warp
 // are requested together, so that a row of few parts costs one trip to memory.
-template <int kWarpsPerRow>
+template <int kWarpsPerRow, int kRound>
 __global__ void __launch_bounds__(128) q4_merge_kernel(const AttnArgs a,
                                                        const MergeRef* __restrict__ merges) {
   __shared__ float sm_m[4], sm_l[4];
@@ -760,11 +760,11 @@ __global__ void __launch_bounds__(128) q4_merge_kernel(const AttnArgs a,
   if (head >= HQ) return;                            // (whole warps, and only where rows are warps)
   float M = -INFINITY, L = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int j0 = kWarpsPerRow == 1 ? 0 : warp; j0 < mr.n; j0 += 8 * kWarpsPerRow) {
-    float2 ml[8];
-    float4 o[8];
+  for (int j0 = kWarpsPerRow == 1 ? 0 : warp; j0 < mr.n; j0 += kRound * kWarpsPerRow) {
+    float2 ml[kRound];
+    float4 o[kRound];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < kRound; ++k) {
       const int j = j0 + k * kWarpsPerRow;
       ml[k] = make_float2(-INFINITY, 0.f);
       o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -776,13 +776,13 @@ __global__ void __launch_bounds__(128) q4_merge_kernel(const AttnArgs a,
     }
     float m = M;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) m = fmaxf(m, ml[k].x);
+    for (int k = 0; k < kRound; ++k) m = fmaxf(m, ml[k].x);
     const float f = M == -INFINITY ? 0.f : ex2(M - m);
     M = m;
     L *= f;
     acc.x *= f; acc.y *= f; acc.z *= f; acc.w *= f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < kRound; ++k) {
       const float w = ml[k].x == -INFINITY ? 0.f : ex2(ml[k].x - m);
       L = fmaf(ml[k].y, w, L);
       acc.x = fmaf(o[k].x, w, acc.x); acc.y = fmaf(o[k].y, w, acc.y);
@@ -820,11 +820,13 @@ cudaError_t launch_q4_merge(const AttnArgs& a, const MergeRef* d_merge, int n_me
                             cudaStream_t st) {
   if (n_merge <= 0) return cudaSuccess;
   const int HQ = a.shape.num_q_heads;
-  // One warp takes a row unless the parts of some row need more than one round of its loads.
-  if (max_parts <= 8)
-    return launch_kernel(q4_merge_kernel<1>, dim3(n_merge, (HQ + 3) / 4), dim3(128), 0, st, a.pdl != 0,
-                         a, d_merge);
-  return launch_kernel(q4_merge_kernel<4>, dim3(n_merge, HQ), dim3(128), 0, st, a.pdl != 0, a, d_merge);
+  // One warp takes a row unless the parts of some row need more than one round of its loads; rounds of
+  // eight are mostly empty slots where no row has more than two.
+  if (max_parts <= 8) {
+    auto* kernel = max_parts <= 2 ? q4_merge_kernel<1, 2> : q4_merge_kernel<1, 8>;
+    return launch_kernel(kernel, dim3(n_merge, (HQ + 3) / 4), dim3(128), 0, st, a.pdl != 0, a, d_merge);
+  }
+  return launch_kernel(q4_merge_kernel<4, 8>, dim3(n_merge, HQ), dim3(128), 0, st, a.pdl != 0, a, d_merge);
 }
 
 cudaError_t launch_attention_q4(const AttnArgs& a, const Q4Items& it, cudaStream_t st) {
