@@ -7,6 +7,7 @@ library has not been built, importing this module raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 import struct
 
@@ -134,6 +135,11 @@ for _name, (_res, _args) in _SIGS.items():
 EXPORTS = tuple(_SIGS)
 
 
+@functools.lru_cache(256)
+def _packer(n):
+    return struct.Struct(f"{n}i")
+
+
 def _arr(xs):
     if isinstance(xs, tuple) and len(xs) == 2 and isinstance(xs[1], int):
         return xs          # already marshalled by int32_array()
@@ -141,7 +147,7 @@ def _arr(xs):
         xs = xs if isinstance(xs, (list, tuple)) else list(xs)
         n = len(xs)
         try:                           # (several times as fast as numpy for short lists)
-            raw = struct.pack(f"{max(n, 1)}i", *(xs or (0,)))
+            raw = _packer(max(n, 1)).pack(*(xs or (0,)))
         except struct.error:           # not plain ints of 32 bits: numpy's conversions and errors
             raw = np.fromiter(xs, dtype=np.int32).tobytes()
         return (C.c_int32 * max(n, 1)).from_buffer_copy(raw), n

@@ -29,9 +29,9 @@
 // common exit where TMEM is released.
 //
 // Measured: 64 prompts of 2048 tokens, 64 rows on each of 8 kv heads (34 GFLOP, 168 MB): 139 us;
-// 2496 candidates of 96 threads, 32 heads over 8: 195 us.  A tile takes a CTA some 3600 cycles, of
+// 2496 candidates of 96 threads, 40 or 64 rows, 32 heads over 8: 175 us.  A tile takes a CTA some 3600 cycles, of
 // which a converter warp is busy 2500, a softmax warp 2300 and the MMA warp 1500.  No single unit
-// is full: issue slots 48 %, shared memory 36 %, tensor pipe 20 %; the roles wait for one another,
+// is full: issue slots 50 %, shared memory 46 %, tensor pipe 25 %; the roles wait for one another,
 // and 18 warps of different code miss the instruction cache (a fifth of the stalls).
 #include <algorithm>
 #include <climits>

@@ -4,6 +4,7 @@ from __future__ import annotations
 
 import math
 
+import numpy as np
 import torch
 
 from . import binding as B
@@ -193,7 +194,9 @@ class PagedSession:
 
     def read_kv(self, tids, begin, count, layer: int = 0):
         """Rows begin[i] .. begin[i] + count[i] - 1 of each thread's chain, as bf16 (k, v)."""
-        shape = (sum(count), self.shape.num_kv_heads, self.shape.head_dim)
+        count = B.int32_array(count)
+        rows = int(np.frombuffer(count[0], np.int32, count[1]).sum(dtype=np.int64))
+        shape = (rows, self.shape.num_kv_heads, self.shape.head_dim)
         k = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
         v = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
         B.apar_read_kv(self.ctx, layer, tids, begin, count, k.data_ptr(), v.data_ptr(),
