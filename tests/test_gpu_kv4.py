@@ -348,8 +348,9 @@ def test_decode_steps_with_rotary_positions_over_layers_and_forks():
         p.close()
 
 
-def test_captured_step_replays():
-    hq, hk, n = 8, 2, 5
+@pytest.mark.parametrize("hq,hk", WIDTHS)
+def test_captured_step_replays(hq, hk):
+    n = 5
     p = Kv4Pair(hq, hk, num_blocks=64)
     tids = p.new_threads(n)
     k, v = rows(18 * n, hk, 101), rows(18 * n, hk, 102)
