@@ -46,7 +46,7 @@ class Rope:
             assert x.dim() == 3 and x.shape[0] == n
             assert x.shape[2] == self.cfg.head_dim
             assert x.stride(2) == 1 and (x.shape[1] == 1 or x.stride(1) == x.shape[2])
-            out = x if inplace else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            out = x if inplace else torch.empty_like(x, memory_format=torch.contiguous_format)
             stride = x.stride(0) if n > 1 else 0       # (0: contiguous)
             outs.append(out)
             sides += [x.shape[1], x.data_ptr(), stride, out.data_ptr(), stride if inplace else 0]
@@ -110,7 +110,8 @@ class PagedSession:
 
     @staticmethod
     def _stream() -> int:
-        return torch.cuda.current_stream().cuda_stream
+        # (torch.cuda.current_stream().cuda_stream without its 3 us of wrapping)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
     # the replay protocol of synth.build_forest
     def new_threads(self, n):
