@@ -21,7 +21,7 @@
 //              P = 2^(x - ref) in f16, its sum less the token's factor in 32 bits, P to shared memory
 //              as an operand.  The reference follows score and size of V together and moves
 //              lazily, as in attn_q4.cu.  (With a thread per row - M 128, P in tensor memory -
-//              every thread reads every token's constants: 212 us instead of 150.)
+//              every thread reads every token's constants, a quarter of the shared-memory cycles.)
 // K', V' and S are double-buffered; P is not, for want of shared memory.  Both operands and the
 // weights are rounded to 11 bits (K' and V' of values far below their maximum to 2^-18 of it),
 // against eight of the output.
