@@ -24,10 +24,14 @@
 //                   the group; the powers of two are part of the softmax scale.  The second sum is
 //                   one more product: lo_j is a bf16 number, and qsum_j the sum of three, so
 //                   that four groups fill a k of 16.  Scores are exact to 32 bits.
-//   O^T += V^T P^T  A = V codes, 16 dims x 16 tokens.  B = P s_j, one operand per group, rounded
-//                   once to f16: it is below 2^16 by the choice of reference, and 11 bits against
-//                   bf16's eight keep the result as good as 32-bit arithmetic rounded to bf16.
-//                   The offsets lo_j are summed in 32 bits on the side, once per group and row.
+//   O^T += V^T P^T  A = V codes less 7.5, 16 dims x 16 tokens (one fused multiply-add a pair, exact).
+//                   B = P s_j, one operand per group, rounded once to f16: it is below 2^16 by the
+//                   choice of reference.  The middles lo_j + 7.5 s_j are summed in 32 bits on the
+//                   side, once per group and row.  Codes as they lie, 0..15, would make of both sums
+//                   numbers that grow with the length and cancel: over 32768 tokens of equal
+//                   weight what the tensor core cuts off its sums, always the same way, and
+//                   the rounding of one and the same weight came to 1.8 % of the result.  Less
+//                   their middle they leave 0.16 %, the output's own rounding.
 // The reference subtracted in the exponent is the running maximum of score + log2(largest
 // scale of the token's V row), not of the score: P s_j is then bounded whatever the scales are,
 // and f16's narrow exponent is spent on the largest terms of the sum.  It moves lazily (kSlack), and
@@ -37,11 +41,11 @@
 // The C fragment of S^T holds tokens in rows, the B operand wants them in the k index: a
 // movmatrix of the 8 x 8 halves brings one into the other.
 //
-// Measured: four contexts of 125 k tokens, 32 query heads over 8 (646 MB): 126 us, 5.1 TB/s, 0.78 of
-// a copy; the same kernel with its arithmetic taken out takes 97 us, with its loads taken out 113.
-// 128 tails of 190 tokens and 32 prompts of 512 under 32 heads (210 MB): 57 us, 3.7 TB/s.  What
-// bounds it is issue: a block is some 280 instructions of a warp, most of them on the integer
-// pipe, and twelve warps are what the registers (168) allow.
+// Measured: four contexts of 125 k tokens, 32 query heads over 8 (646 MB): 133 us, 4.9 TB/s, 0.74 of
+// a copy (129 before the codes went less their middle; then, with the arithmetic taken out, 97 us, and
+// with the loads taken out 113).  128 tails of 190 tokens and 32 prompts of 512 under 32 heads
+// (210 MB): 59 us, 3.6 TB/s.  What bounds it is issue: a block is some 320 instructions of a warp, most
+// of them on the integer pipe, and twelve warps are what the registers (168) allow.
 #include <algorithm>
 #include <climits>
 
@@ -68,13 +72,17 @@ constexpr int kOffQ = kWarps * kDepth * kSlot;       // the next unit's query ro
 constexpr int kOffHdr = kOffQ + kWarps * kRows * kDim * 2;
 constexpr int kSmemQ4 = kOffHdr + kWarps * kHdrs * kHdrInts * 4;
 static_assert(kSmemQ4 <= 227 * 1024, "shared memory");
-constexpr float kHeadroom = 6.f;                     // largest weight when the reference is set: 2^6
-constexpr float kSlack = 14.f;                       // and when it has to move: 2^14 (times 2^1.1)
+constexpr float kHeadroom = 12.f;                    // largest weight when the reference is set: 2^12
+constexpr float kSlack = 15.5f;                      // and when it has to move: 2^15.5 (times 2^0.1)
 constexpr float kNoRef = -3e38f;                      // of a row that has seen nothing (finite: a
                                                      // masked score less this is still -inf)
 constexpr float kCodeUnit = 1.f / 16777216.f;        // what a code of 1 counts as in a product: 2^-24
 constexpr uint32_t kEven = 0x000f000fu;             // nibbles 0 and 4 of a word: f16 pair c * 2^-24
 constexpr uint32_t kOdd = 0x00f000f0u;              // nibbles 1 and 5: c * 2^-20
+constexpr uint32_t kUpEven = 0x78007800u, kUpOdd = 0x68006800u;   // f16 pairs 2^15 and 2^11: bring
+                                                     // c * 2^-24 and c * 2^-20 to c * 2^-9
+constexpr uint32_t kLessMiddle = 0xa380a380u;        // f16 pair -7.5 * 2^-9
+constexpr float kValueUnit = 512.f;                  // 2^9
 constexpr float kMinScaleLog2 = -60.f;               // V scales below 2^-60 count as 2^-60
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
@@ -101,6 +109,10 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   __half2 h = __floats2half2_rn(lo, hi);
   return *(uint32_t*)&h;
+}
+__device__ __forceinline__ uint32_t fma_f16(uint32_t a, uint32_t b, uint32_t c) {
+  __half2 r = __hfma2(*(__half2*)&a, *(__half2*)&b, *(__half2*)&c);
+  return *(uint32_t*)&r;
 }
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -402,21 +414,23 @@ __device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Units& u
       l[0] += x[0] + x[2];
       l[1] += x[1] + x[3];
     };
-    // the B operand of group j, and the offsets' share
+    // the B operand of group j, and the middles' share
     auto weights_b = [&](uint32_t z0, uint32_t z1, const float (&p)[4], int j, uint32_t& b0,
                          uint32_t& b1) {
       const float sa = bf16_lo(z0), sb = bf16_lo(z1);
       b0 = transpose8x8(pack_f16(p[0] * sa, p[1] * sa));
       b1 = transpose8x8(pack_f16(p[2] * sb, p[3] * sb));
-      const float la = bf16_hi(z0), lb = bf16_hi(z1);
+      const float la = fmaf(7.5f, sa, bf16_hi(z0)), lb = fmaf(7.5f, sb, bf16_hi(z1));
       lsum[j][0] = fmaf(p[0], la, fmaf(p[2], lb, lsum[j][0]));
       lsum[j][1] = fmaf(p[1], la, fmaf(p[3], lb, lsum[j][1]));
     };
     auto accumulate = [&](uint32_t xl, uint32_t xh, uint32_t b0, uint32_t b1, float (&d0)[4],
                           float (&d1)[4]) {
       const uint32_t hl = xl >> 8, hh = xh >> 8;
-      mma_f16(d0, xl & kEven, xl & kOdd, xh & kEven, xh & kOdd, b0, b1);
-      mma_f16(d1, hl & kEven, hl & kOdd, hh & kEven, hh & kOdd, b0, b1);
+      auto even = [](uint32_t w) { return fma_f16(w & kEven, kUpEven, kLessMiddle); };
+      auto odd = [](uint32_t w) { return fma_f16(w & kOdd, kUpOdd, kLessMiddle); };
+      mma_f16(d0, even(xl), odd(xl), even(xh), odd(xh), b0, b1);
+      mma_f16(d1, even(hl), odd(hl), even(hh), odd(hh), b0, b1);
     };
     auto k_words = [&](uint32_t kt, uint4& w0, uint4& w1) {
       w0 = lds128(kt + g * kQ4RowBytes + q * 16);
@@ -558,17 +572,16 @@ __device__ __forceinline__ void stream_units(const AttnArgs& a, const Q4Units& u
     for (int e = 0; e < 2; ++e) {
       const int r = 2 * q + e;
       if (r >= rows) continue;
-      constexpr float kLow = 1.f / kCodeUnit, kHigh = kLow / 16.f;   // (odd nibbles counted 16 times)
       const int head = h[H_KVH] * G + r % G;
       const int query = h[H_QUERY + r], slot = h[H_SLOT + r];
       const float inv = slot < 0 ? 1.f / l[e] : 1.f;
       const size_t prow = (size_t)(slot + h[H_ADD]) * HQ + head;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float4 v = make_float4(fmaf(o[2 * j][e], kLow, lsum[j][e]) * inv,
-                                     fmaf(o[2 * j][2 + e], kHigh, lsum[j][e]) * inv,
-                                     fmaf(o[2 * j + 1][e], kLow, lsum[j][e]) * inv,
-                                     fmaf(o[2 * j + 1][2 + e], kHigh, lsum[j][e]) * inv);
+        const float4 v = make_float4(fmaf(o[2 * j][e], kValueUnit, lsum[j][e]) * inv,
+                                     fmaf(o[2 * j][2 + e], kValueUnit, lsum[j][e]) * inv,
+                                     fmaf(o[2 * j + 1][e], kValueUnit, lsum[j][e]) * inv,
+                                     fmaf(o[2 * j + 1][2 + e], kValueUnit, lsum[j][e]) * inv);
         if (slot < 0)
           *(uint2*)((__nv_bfloat16*)a.out + ((size_t)query * HQ + head) * kDim + 32 * j + 4 * g) =
               make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
