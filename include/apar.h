@@ -148,9 +148,14 @@ apar_status apar_destroy(apar_ctx* ctx);
  *   Bytes.  80 per row (64 of codes, then {s, lo} of each group as two bf16) instead of 256;
  *   each pool is [num_layers][num_blocks][num_kv_heads][16 rows][80 bytes].  The order of the
  *   codes inside a row is the library's own; apar_read_kv gives the rows as numbers.
- *   Attention reads q and writes out as bf16, sums in 32 bits and rounds the weights to 11
- *   bits after they are scaled: results are as exact as 32-bit arithmetic on the values above
- *   rounded to bf16.  A NaN row makes NaN of the outputs that see it, and only of those.
+ *   Attention reads q and writes out as bf16.  Scores, the softmax's sums and the results are summed
+ *   in 32 bits; q and the values of K enter the scores unrounded (a query's dims below 2^-38 of its
+ *   largest count as 0; the scales of a K row's groups keep all their digits down to 2^-12 of the
+ *   largest of that row).  Rounded to 11 bits are the weights, after they are scaled (each then
+ *   multiplies a value or its distance from the middle of its group), and in runs of tokens that
+ *   more than eight query rows share V's values.  All of it is less than the rounding of the result
+ *   to bf16 (measured up to 400 000 tokens), for groups of a V row down to 2^-20 of the row's
+ *   largest.  A NaN row makes NaN of the outputs that see it, and only of those.
  * All calls of this header work on such a context, except apar_tree_prefill_attention, which
  * returns APAR_ERR_UNSUPPORTED (apar_tree_prefix_attention serves runs of up to max_threads
  * queries).  Device row pointers (q, out, k_new, v_new) must be 16-byte aligned: otherwise

@@ -8,31 +8,44 @@
 // walked in tiles of 64 tokens; two persistent CTAs per SM take units in the planner's order, forwards
 // and backwards in turn, and every role runs on from one unit into the next (a CTA per unit spent
 // some 6 us on each: 92 of 178 us of a case whose roles did nothing else):
-//   warps 4-7  one block of the tile each: its 4-bit K and V tiles arrive through a private cp.async
-//              ring, a tile ahead, and leave as f16 operands.  K' = K 2^-(E + 8) with E the
-//              exponent of the block's largest value, V' = V 2^-(F + 8) with F that of the token's,
-//              so that f16's range is never an issue; a code enters the conversion as the
-//              subnormal number it is in place (c * 2^-24, or * 2^-20 a nibble up), one fused
-//              multiply-add per pair of values.  At a unit's first tile they also stage its query
-//              rows, 16 each.  One fence and one arrival per tile cover all of it (separate ones
-//              for K', V' and Q: 148 us instead of 139).
-//   warp 8     issues S = Q K'^T (M 64, N 64, K 128) and, one tile behind, O += P V' (M 64, N 128, K 64).
-//   warps 0-3  16 rows each, a row's scores spread over a quad: x = S u 2^(E + 8) + F + 8,
+//   warps 4-7  one block of the tile each: its 4-bit K and V tiles arrive by cp.async while the tile
+//              before is converted, and leave as f16 operands.
+//              K' = s (c - 8) 2^-e, e from the token's largest scale: eight bits of s times at
+//              most three of c - 8, so exact for scales down to 2^-12 of that one, and beyond it
+//              good to 2^-20 of it.  A code enters as the subnormal number c * 2^-20, brought to
+//              the second nibble of its 16 bits; one fused multiply-add per pair of values.
+//              What is left of a key, lo + 8 s of each group, meets the query's sum over the group
+//              in one more product: lo and 8 s in f16 (exact too) against that sum as two f16
+//              numbers, which makes a k of 16.  Scores are then as good as 32-bit sums, whatever
+//              the keys have in common.  (Keys rounded to 11 bits with their offsets inside, under one
+//              exponent per block, made errors of the exponent: 2.6 times the output's rounding
+//              where two channels had offsets of 16, seventy times at 200.)
+//              V' = V 2^(13 - F), F the exponent of the token's largest value, rounded to 11 bits:
+//              normal numbers down to 2^-27 of that.  (Scaled to 2^-8, as the codes as they
+//              lie in the word would have it, a group 2^10 below the row's largest lost its digits.)
+//              Here a code enters as 1024 + c, or 1024 + 16 c a nibble up, less the constant.
+//              At a unit's first tile they also stage its query rows, 16 each.  One fence and one
+//              arrival per tile cover all of it (separate ones for K', V' and Q: 148 us instead of
+//              139).
+//   warp 8     issues S = Q K'^T (M 64, N 64, K 128 + 16) and, one tile behind, O += P V' (M 64, N 128,
+//              K 64).
+//   warps 0-3  16 rows each, a row's scores spread over a quad: x = S u 2^e + F - 13,
 //              P = 2^(x - ref) in f16, its sum less the token's factor in 32 bits, P to shared memory
 //              as an operand.  The reference follows score and size of V together and moves
 //              lazily, as in attn_q4.cu.  (With a thread per row - M 128, P in tensor memory -
 //              every thread reads every token's constants, a quarter of the shared-memory cycles.)
-// K', V' and S are double-buffered; P is not, for want of shared memory.  Both operands and the
-// weights are rounded to 11 bits (K' and V' of values far below their maximum to 2^-18 of it),
-// against eight of the output.
+// K', V' and S are double-buffered; P is not, for want of shared memory.  Weights and V' are rounded
+// to 11 bits, against eight of the output.
 // All waits are bounded; a wait that gives up raises the error word and every role unwinds to the
 // common exit where TMEM is released.
 //
-// Measured: 64 prompts of 2048 tokens, 64 rows on each of 8 kv heads (34 GFLOP, 168 MB): 139 us;
-// 2496 candidates of 96 threads, 40 or 64 rows, 32 heads over 8: 175 us.  A tile takes a CTA some 3600 cycles, of
-// which a converter warp is busy 2500, a softmax warp 2300 and the MMA warp 1500.  No single unit
-// is full: issue slots 50 %, shared memory 46 %, tensor pipe 25 %; the roles wait for one another,
-// and 18 warps of different code miss the instruction cache (a fifth of the stalls).
+// Measured: 64 prompts of 2048 tokens, 64 rows on each of 8 kv heads (34 GFLOP, 168 MB): 155 us;
+// 2496 candidates of 96 threads, 40 or 64 rows, 32 heads over 8: 193 us.  With keys rounded to 11 bits
+// and V scaled to 2^-8 it was 139 and 172: V's codes by way of 1024 + c cost 8 us of each, the exact
+// keys the rest.  (Then a tile took a CTA some 3600 cycles, of which a converter warp was busy 2500,
+// a softmax warp 2300 and the MMA warp 1500; the converters' share is what grew.)  No single unit
+// is full: the roles wait for one another, and 18 warps of different code miss the instruction
+// cache (a fifth of the stalls).
 #include <algorithm>
 #include <climits>
 
@@ -52,26 +65,38 @@ constexpr int kTok = 64;                             // tokens of a tile
 constexpr int kConv = 4, kSoftmax = 4;               // warps
 constexpr int kThreads = 32 * (kSoftmax + kConv + 1);
 constexpr int kBlk = 2 * kQ4TileBytes;               // K and V of one block, as stored
-constexpr int kDepthW = 2;                           // blocks of a converter's ring
 constexpr int kHalfOp = 64 * 128;                    // 64 rows x 64 dims f16, 128-byte swizzle
 constexpr int kOpBytes = 2 * kHalfOp;                // K' or V' of a tile, or Q
 constexpr int kOffK = kOpBytes;
 constexpr int kOffVw = kOffK + 2 * kOpBytes;
 constexpr int kOffP = kOffVw + 2 * kOpBytes;         // P: 64 rows x 64 tokens f16
-constexpr int kOffRaw = kOffP + kHalfOp;
-constexpr int kOffTok = kOffRaw + kConv * kDepthW * kBlk;     // [2] F + 8 and 2^-(F + 8) of 64 tokens
-constexpr int kOffKb = kOffTok + 2 * 2 * kTok * 4;            // [2][4] 2^(E + 8)
-constexpr int kOffRow = kOffKb + 2 * 4 * 4;                   // [4 units][64] the rows' factors
+constexpr int kCoreBytes = 64 * 16;                  // 64 rows x 8 f16, no swizzle: 8 rows to 128 bytes
+constexpr int kMidBytes = 2 * kCoreBytes;            // lo, 8 s of a tile's tokens, or the rows' sums
+constexpr int kOffQmid = kOffP + kHalfOp;
+constexpr int kOffKmid = kOffQmid + kMidBytes;
+constexpr int kOffRaw = kOffKmid + 2 * kMidBytes;
+constexpr int kOffTok = kOffRaw + kConv * kBlk;      // [2] F - 13, 2^(13 - F), 2^(e - 8) of 64 tokens
+constexpr int kTokc = 3 * kTok;
+constexpr int kOffRow = kOffTok + 2 * kTokc * 4;              // [4 units][64] the rows' factors
 constexpr int kOffBarW = kOffRow + 4 * 64 * 4;
 enum { BW_FULL = 0, BW_KEMPTY = 2, BW_VEMPTY = 4, BW_SFULL = 6, BW_PFULL = 8, BW_PVDONE = 9,
        BW_ODONE = 10, BW_TOTAL = 11 };
 constexpr int kSmemWide = kOffBarW + 8 * BW_TOTAL + 16;
 static_assert(2 * (kSmemWide + 1024) <= 228 * 1024, "two CTAs per SM");
 constexpr int kTmemColsW = 256;                      // S at 0 and 64, O at 128
-constexpr float kHeadroomW = 6.f, kSlackW = 14.f;    // as in attn_q4.cu: weights 2^6 .. 2^14
+constexpr float kHeadroomW = 6.f, kSlackW = 15.5f;   // as in attn_q4.cu, but set to 2^6: V' has taken the
+                                                     // sizes of the groups on itself, and moving O
+                                                     // costs more here (with 2^12 the candidates
+                                                     // took 201 us instead of 190)
 constexpr float kNoRefW = -3e38f;
-constexpr int kLift = 8;                             // operands stay below 2^(1 - kLift)
+constexpr int kLiftV = 13;                           // exponent of the largest values of V'
+constexpr int kDropK = 5;                            // e less the exponent of the largest scale: that one
+                                                     // times 2^20 (for the codes) is then below 2^16
+constexpr int kLiftMid = 7;                          // lo and 8 s stand that much above K', sums below
+constexpr int kStepK = 8;                            // of e, carried by the rows' factors (range)
 constexpr uint32_t kEvenW = 0x000f000fu, kOddW = 0x00f000f0u;
+constexpr uint32_t kSixteenth = 0x2c002c00u;         // f16 1/16 twice
+constexpr int kMinExpV = -60;                        // V rows below 2^-60 count as of that size
 
 // D fp32, A and B f16, both K-major.
 __host__ __device__ constexpr uint32_t instr_desc_f16(int n, int m) {
@@ -89,11 +114,26 @@ __device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
   __half2 r = __hmul2(*(__half2*)&a, *(__half2*)&b);
   return *(uint32_t*)&r;
 }
-constexpr uint32_t kSixteenth = 0x2c002c00u;         // f16 1/16 twice
+__device__ __forceinline__ uint32_t hadd2(uint32_t a, uint32_t b) {
+  __half2 r = __hadd2(*(__half2*)&a, *(__half2*)&b);
+  return *(uint32_t*)&r;
+}
+// The f16 pairs c of nibbles 0 and 4 of a word, and of nibbles 1 and 5; exact.
+__device__ __forceinline__ uint32_t codes_even(uint32_t w) {
+  return hadd2((w & kEvenW) | 0x64006400u, 0xe400e400u);               // less 1024
+}
+__device__ __forceinline__ uint32_t codes_odd(uint32_t w) {
+  return hfma2((w & kOddW) | 0x64006400u, kSixteenth, 0xd400d400u);    // a sixteenth, less 64
+}
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
-// exponent of a non-negative number, kept away from the ends of the range
-__device__ __forceinline__ int exponent_of(float x) {
-  return min(110, max(-100, (int)(__float_as_uint(x) >> 23) - 127));
+// exponent of a non-negative number, kept away from the low end of the range
+__device__ __forceinline__ int exponent_of(float x, int lowest) {
+  return min(127, max(lowest, (int)(__float_as_uint(x) >> 23) - 127));
+}
+// Descriptor of a K-major operand without swizzle whose second eight k lie kCoreBytes on.
+__device__ __forceinline__ uint64_t core_desc(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(kCoreBytes >> 4) << 16) |
+         ((uint64_t)(128 >> 4) << 32) | (1ull << 46);
 }
 // largest magnitude a group can stand for
 __device__ __forceinline__ float group_top(uint32_t sl) {
@@ -196,10 +236,11 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
   } else if (warp >= kSoftmax && warp < kSoftmax + kConv) {
     // ---------------------------------------------------------------- converters
     const int cw = warp - kSoftmax;
-    const uint32_t raw = base + kOffRaw + cw * kDepthW * kBlk;
-    // the loads run kDepthW - 1 tiles ahead, into the next units too
+    const uint32_t raw = base + kOffRaw + cw * kBlk;
+    // the loads run a tile ahead, into the next units too: a tile's block is asked for once the
+    // one before is in registers, and has all of its conversion to arrive in
     Unit lu = {0, 0, 0, 0, 0}, nu = my_units ? describe(0) : lu;   // the loads' unit; the one after it
-    int l_pass = -1, l_t = 0, l_slot = 0, l_bid = 0;
+    int l_pass = -1, l_t = 0, l_bid = 0;
     const int32_t* l_tab = nullptr;
     auto load_tile = [&]() {                         // this warp's block of the next tile, if any
       if (l_t == lu.n_tiles && l_pass + 1 < my_units) {
@@ -215,7 +256,7 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
           const size_t tile = ((size_t)l_bid * HKV + lu.kvh) * kQ4TileBytes + lane * 16;
           const uint8_t* kt = (const uint8_t*)a.k_pool + tile;
           const uint8_t* vt = (const uint8_t*)a.v_pool + tile - kQ4TileBytes;
-          const uint32_t dst = raw + l_slot * kBlk + lane * 16;
+          const uint32_t dst = raw + lane * 16;
           cp16(dst, kt);
           cp16(dst + 512, kt + 512);
           cp16(dst + 1024, (lane < 16 ? kt : vt) + 1024);
@@ -226,12 +267,9 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
         const int nb = l_t * kConv + cw;
         if (nb * kBlock < lu.n_tok) l_bid = l_tab[nb];         // (arrives while a tile is converted)
       }
-      l_slot = l_slot == kDepthW - 1 ? 0 : l_slot + 1;
-      asm volatile("cp.async.commit_group;" ::: "memory");
     };
-#pragma unroll 1
-    for (int i = 0; i < kDepthW - 1; ++i) load_tile();
-    int T = 0, slot = 0;                             // tiles of all units
+    load_tile();
+    int T = 0;                                       // tiles of all units
     // The query rows of the unit whose first tile is T into the operand, in f16 under a power of two
     // of their own: this warp's 16, a lane four pieces of rows lane / 4 and lane / 4 + 8.  (By these
     // warps, which have the time: the softmax warps spent 6000 cycles on it between two units.)
@@ -266,18 +304,37 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
         const int lift = min(126, 14 + 127 - (int)(top >> 7));
         const float f = pow2(lift);
+        float sum[4];                                // over dims 32 j .. 32 j + 31
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int c = qd + 4 * j;
           const uint32_t w[4] = {v[e][j].x, v[e][j].y, v[e][j].z, v[e][j].w};
           uint32_t h[4];
+          sum[j] = 0.f;
 #pragma unroll
-          for (int p = 0; p < 4; ++p) h[p] = f16x2(bf16_lo(w[p]) * f, bf16_hi(w[p]) * f);
+          for (int p = 0; p < 4; ++p) {
+            const float e0 = bf16_lo(w[p]) * f, e1 = bf16_hi(w[p]) * f;
+            sum[j] += e0 + e1;
+            h[p] = f16x2(e0, e1);
+          }
+          sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 1);
+          sum[j] += __shfl_xor_sync(0xffffffffu, sum[j], 2);
+          sum[j] *= 1.f / (1 << kLiftMid);
           *(uint4*)(bp + (c >> 3) * kHalfOp + r * 128 + (((c & 7) ^ (r & 7)) << 4)) =
               make_uint4(h[0], h[1], h[2], h[3]);
         }
+        if (qd < 2) {                                // the sums to 11 bits, and what that leaves
+          float part[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float first = __half2float(__float2half_rn(sum[j]));
+            part[j] = qd ? sum[j] - first : first;
+          }
+          const uint32_t p01 = f16x2(part[0], part[1]), p23 = f16x2(part[2], part[3]);
+          *(uint4*)(bp + kOffQmid + qd * kCoreBytes + r * 16) = make_uint4(p01, p23, p01, p23);
+        }
         // (the softmax warps read them at the unit's first tile: four units on they have)
-        if (qd == 0) ((float*)(bp + kOffRow))[(pass & 3) * 64 + r] = a.scale_log2e * pow2(-lift);
+        if (qd == 0) ((float*)(bp + kOffRow))[(pass & 3) * 64 + r] = a.scale_log2e * pow2(kStepK - lift);
       }
       return true;
     };
@@ -286,12 +343,11 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
     for (int pass = 0; pass < my_units && ok; ++pass) {
       const Unit cu = describe(pass);                // (in the L1 cache by now)
 #pragma unroll 1
-    for (int t = 0; t < cu.n_tiles; ++t, ++T, slot = slot == kDepthW - 1 ? 0 : slot + 1) {
+    for (int t = 0; t < cu.n_tiles; ++t, ++T) {
       const int b = T & 1;
-      asm volatile("cp.async.wait_group %0;" ::"n"(kDepthW - 2) : "memory");
+      asm volatile("cp.async.wait_all;" ::: "memory");
       __syncwarp();
-      load_tile();
-      const uint8_t* kt = bp + (raw - base) + slot * kBlk;
+      const uint8_t* kt = bp + (raw - base);
       const uint8_t* vt = kt + kQ4TileBytes;
       const int nv = cu.n_tok - (t * kConv + cw) * kBlock;   // tokens of the block that count
 
@@ -317,36 +373,25 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
       if (2 * pair >= nv) se = 0u;
       if (2 * pair + 1 >= nv) so = 0u;
       const uint32_t sl[4] = {sc.x, sc.y, sc.z, sc.w};
-      float top = fmaxf(fmaxf(group_top(sl[0]), group_top(sl[1])),
-                        fmaxf(group_top(sl[2]), group_top(sl[3])));
       float te = group_top(se), to = group_top(so);
 #pragma unroll
-      for (int d = 1; d < 16; d <<= 1) {
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-        if (d <= 2) {
-          te = fmaxf(te, __shfl_xor_sync(0xffffffffu, te, d));
-          to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, d));
-        }
+      for (int d = 1; d <= 2; d <<= 1) {
+        te = fmaxf(te, __shfl_xor_sync(0xffffffffu, te, d));
+        to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, d));
       }
-      const int ek = exponent_of(top) + kLift;
-      const int ee = exponent_of(te) + kLift, eo = exponent_of(to) + kLift;
-      uint32_t v1[4], v16[4], vl[4];                         // of the four pairs
-      {
-        const float de = pow2(-ee), dn = pow2(-eo);
-        const float s0 = bf16_lo(se) * (de * 16777216.f), s1 = bf16_lo(so) * (dn * 16777216.f);
-        const uint32_t x1 = f16x2(s0, s1);
-        const uint32_t xl = f16x2(bf16_hi(se) * de, bf16_hi(so) * dn);
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {                        // from the lanes that made them
-          const int from = 8 * pg + GG + 4 * ((p & 1) + 2 * (p & 2));    // pair token_at(8 pg + 2 p) / 2
-          v1[p] = __shfl_sync(0xffffffffu, x1, from);
-          vl[p] = __shfl_sync(0xffffffffu, xl, from);
-          v16[p] = hmul2(v1[p], kSixteenth);
-        }
-      }
+      // the token's largest scale; and lo has to stay below 2^16 where all groups are flat
+      const float s_top = fmaxf(fmaxf(bf16_lo(sl[0]), bf16_lo(sl[1])),
+                                fmaxf(bf16_lo(sl[2]), bf16_lo(sl[3])));
+      const float lo_top = fmaxf(fmaxf(fabsf(bf16_hi(sl[0])), fabsf(bf16_hi(sl[1]))),
+                                 fmaxf(fabsf(bf16_hi(sl[2])), fabsf(bf16_hi(sl[3]))));
+      const int ek = max(min(exponent_of(s_top, -100), 124) + kDropK, exponent_of(lo_top, -100) + kLiftMid - 14);
+      const int ee = exponent_of(te, kMinExpV) - kLiftV, eo = exponent_of(to, kMinExpV) - kLiftV;
+      const float de = pow2(-ee), dn = pow2(-eo);
+      const uint32_t x1 = f16x2(bf16_lo(se) * de, bf16_lo(so) * dn);
+      const uint32_t xl = f16x2(bf16_hi(se) * de, bf16_hi(so) * dn);
       // ---- K
       {
-        const float down = pow2(-ek), up = down * 16777216.f;
+        const float up = pow2(20 - ek);
         if (T >= 2 && !__all_sync(0xffffffffu, bar_wait(bar(BW_KEMPTY + b), ((T >> 1) - 1) & 1, cta_abort,
                                                         a.d_error, 23000))) {
           ok = false;
@@ -359,35 +404,52 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
         const uint32_t piece = (uint32_t)((2 * h) ^ (r & 7)) << 4;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float s = bf16_lo(sl[j]) * up, lo = bf16_hi(sl[j]) * down;
-          const uint32_t s1 = f16x2(s, s), s16 = hmul2(s1, kSixteenth), lo2 = f16x2(lo, lo);
+          const float s = bf16_lo(sl[j]) * up;
+          const uint32_t s1 = f16x2(s, s), m8 = hmul2(s1, 0x80808080u);   // (-8 * 2^-20 as an f16 number)
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            const uint32_t kw = x ? w1[j] : w0[j], kh = kw >> 8;
+            const uint32_t kw = x ? w1[j] : w0[j];
             *(uint4*)(dst + (j >> 1) * kHalfOp + (piece ^ ((4 * (j & 1) + x) << 4))) =
-                make_uint4(hfma2(kw & kEvenW, s1, lo2), hfma2(kw & kOddW, s16, lo2),
-                           hfma2(kh & kEvenW, s1, lo2), hfma2(kh & kOddW, s16, lo2));
+                make_uint4(hfma2((kw << 4) & kOddW, s1, m8), hfma2(kw & kOddW, s1, m8),
+                           hfma2((kw >> 4) & kOddW, s1, m8), hfma2((kw >> 8) & kOddW, s1, m8));
           }
         }
+        // lo and 8 s of the four groups, for either half of the query's sums
+        const float dm = pow2(kLiftMid - ek), d8 = pow2(kLiftMid + 3 - ek);
+        *(uint4*)(bp + kOffKmid + b * kMidBytes + h * kCoreBytes + r * 16) =
+            make_uint4(f16x2(bf16_hi(sl[0]) * dm, bf16_hi(sl[1]) * dm),
+                       f16x2(bf16_hi(sl[2]) * dm, bf16_hi(sl[3]) * dm),
+                       f16x2(bf16_lo(sl[0]) * d8, bf16_lo(sl[1]) * d8),
+                       f16x2(bf16_lo(sl[2]) * d8, bf16_lo(sl[3]) * d8));
       }
       if (t == 0 && !stage_rows(pass)) {
         ok = false;
         break;
       }
+      __syncwarp();                                          // (the raw tile has been read by all)
+      load_tile();
       // ---- V
       {
+        uint32_t v1[4], vl[4];                               // of the four pairs, from the lanes
+#pragma unroll                                               // that made them
+        for (int p = 0; p < 4; ++p) {
+          const int from = 8 * pg + GG + 4 * ((p & 1) + 2 * (p & 2));    // pair token_at(8 pg + 2 p) / 2
+          v1[p] = __shfl_sync(0xffffffffu, x1, from);
+          vl[p] = __shfl_sync(0xffffffffu, xl, from);
+        }
         if (T >= 2 && !__all_sync(0xffffffffu, bar_wait(bar(BW_VEMPTY + b), ((T >> 1) - 1) & 1,
                                                         cta_abort, a.d_error, 23200))) {
           ok = false;
           break;
         }
         if (g4 == 0) {                                       // (a pair stays together)
-          float* tokc = (float*)(bp + kOffTok) + b * 2 * kTok + cw * kBlock + token_at(2 * pair);
+          float* tokc = (float*)(bp + kOffTok) + b * kTokc + cw * kBlock + token_at(2 * pair);
           const bool e_on = 2 * pair < nv, o_on = 2 * pair + 1 < nv;
           *(float2*)tokc = make_float2(e_on ? (float)ee : -INFINITY, o_on ? (float)eo : -INFINITY);
           *(float2*)(tokc + kTok) = make_float2(e_on ? pow2(-ee) : 0.f, o_on ? pow2(-eo) : 0.f);
         }
-        if (lane == 0) ((float*)(bp + kOffKb))[b * 4 + cw] = pow2(ek);
+        if (h == 0)
+          ((float*)(bp + kOffTok))[b * kTokc + 2 * kTok + cw * kBlock + pos] = pow2(ek - kStepK);
         // operand row of word 4 g + G, dim e: d = 32 G + 4 g + (e ^ G), piece 2 cw + pg at its
         // place xor d % 8
         const int d0 = 32 * GG + 4 * ((lane & 15) >> 2), at = (2 * cw + pg) ^ (d0 & 4);
@@ -398,10 +460,10 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
 #pragma unroll
           for (int p = 0; p < 4; ++p) {
             const uint32_t x = w[i][p], xh = x >> 8;
-            out[0][p] = hfma2(x & kEvenW, v1[p], vl[p]);
-            out[1][p] = hfma2(x & kOddW, v16[p], vl[p]);
-            out[2][p] = hfma2(xh & kEvenW, v1[p], vl[p]);
-            out[3][p] = hfma2(xh & kOddW, v16[p], vl[p]);
+            out[0][p] = hfma2(codes_even(x), v1[p], vl[p]);
+            out[1][p] = hfma2(codes_odd(x), v1[p], vl[p]);
+            out[2][p] = hfma2(codes_even(xh), v1[p], vl[p]);
+            out[3][p] = hfma2(codes_odd(xh), v1[p], vl[p]);
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -423,6 +485,7 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
     constexpr unsigned kAll = 0xffffffffu;
     // (addresses stay below 2^18: adding to the address field, in 16 bytes, carries nowhere)
     const uint64_t desc_q = smem_desc(base, 16, 1024), desc_p = smem_desc(base + kOffP, 16, 1024);
+    const uint64_t desc_qm = core_desc(base + kOffQmid);
     int T = 0, due = -1;                             // tiles so far; the tile whose P V is due
     bool due_first = false, ok = true;
     int due_pass = 0;
@@ -467,6 +530,7 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
             const uint32_t off = (ks >> 2) * kHalfOp + (ks & 3) * 32;
             umma_bf16(tmem + 64u * b, desc_q + (off >> 4), desc_k + (off >> 4), kIdescQK, ks > 0);
           }
+          umma_bf16(tmem + 64u * b, desc_qm, core_desc(base + kOffKmid + b * kMidBytes), kIdescQK, 1);
           umma_commit(bar(BW_SFULL + b));
           umma_commit(bar(BW_KEMPTY + b));
         }
@@ -544,9 +608,7 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
         if (!idle) {
           uint32_t sr[32];
           TMEM_LD_16x256((tmem + 64u * b) | lane_sel, sr);
-          const float* tokc = (const float*)(bp + kOffTok) + b * 2 * kTok + 2 * qd;
-          const float4 kb = *(const float4*)((const float*)(bp + kOffKb) + b * 4);
-          const float kbs[4] = {kb.x, kb.y, kb.z, kb.w};
+          const float* tokc = (const float*)(bp + kOffTok) + b * kTokc + 2 * qd;
           float2 f[8];
 #pragma unroll
           for (int k = 0; k < 8; ++k) f[k] = *(const float2*)(tokc + 8 * k);
@@ -554,11 +616,11 @@ attn_q4_wide_kernel(const AttnArgs a, int n_units) {
           float m_lo = -INFINITY, m_hi = -INFINITY;
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
-            const float s_lo = u_lo * kbs[k >> 1], s_hi = u_hi * kbs[k >> 1];
-            const float x0 = fmaf(__uint_as_float(sr[4 * k]), s_lo, f[k].x);
-            const float x1 = fmaf(__uint_as_float(sr[4 * k + 1]), s_lo, f[k].y);
-            const float x2 = fmaf(__uint_as_float(sr[4 * k + 2]), s_hi, f[k].x);
-            const float x3 = fmaf(__uint_as_float(sr[4 * k + 3]), s_hi, f[k].y);
+            const float2 e = *(const float2*)(tokc + 2 * kTok + 8 * k);
+            const float x0 = fmaf(__uint_as_float(sr[4 * k]), u_lo * e.x, f[k].x);
+            const float x1 = fmaf(__uint_as_float(sr[4 * k + 1]), u_lo * e.y, f[k].y);
+            const float x2 = fmaf(__uint_as_float(sr[4 * k + 2]), u_hi * e.x, f[k].x);
+            const float x3 = fmaf(__uint_as_float(sr[4 * k + 3]), u_hi * e.y, f[k].y);
             m_lo = fmaxf(m_lo, fmaxf(x0, x1));
             m_hi = fmaxf(m_hi, fmaxf(x2, x3));
             sr[4 * k] = __float_as_uint(x0);
