@@ -23,12 +23,22 @@ def pool_requirements(spec: ForestSpec, slack: float = 0.05):
 class Rope:
     """Rotary positions of a model: the parameters of apar_rope_config, applied by calling.
 
-    q [n][heads][128] and k (or None) are bf16 and may be views with any stride between tokens;
-    positions is int32 [n].  Returns rotated (q, k): new contiguous tensors, or the inputs
-    themselves with inplace=True."""
+    q [n][heads][128] and k (or None) are bf16 and may be views with any stride between tokens
+    (rows that overlap are refused; one row expanded to all tokens is copied out first, and refused
+    in place); positions is int32 [n].  Returns rotated (q, k): new contiguous tensors, or the
+    inputs themselves with inplace=True."""
 
     def __init__(self, **params):
         self.cfg = B.make_rope_config(**params)
+
+    @staticmethod
+    def _rows(x: torch.Tensor, inplace: bool) -> torch.Tensor:
+        # (apar_rope takes a stride of 0 for contiguous rows)
+        if x.shape[0] > 1 and x.stride(0) == 0:
+            if inplace:
+                raise ValueError("the tokens of an expanded tensor share one row: not in place")
+            x = x.contiguous()
+        return x
 
     def __call__(self, q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, inplace=False):
         n = q.shape[0]
@@ -46,6 +56,7 @@ class Rope:
             assert x.dim() == 3 and x.shape[0] == n
             assert x.shape[2] == self.cfg.head_dim
             assert x.stride(2) == 1 and (x.shape[1] == 1 or x.stride(1) == x.shape[2])
+            x = self._rows(x, inplace)
             out = x if inplace else torch.empty_like(x, memory_format=torch.contiguous_format)
             stride = x.stride(0) if n > 1 else 0       # (0: contiguous)
             outs.append(out)

@@ -144,3 +144,19 @@ def test_captured_in_a_graph():
         torch.cuda.synchronize()
         _check(out, x, pos - 1, 128, "half")
     assert int(pos[0]) == 3
+
+
+def test_one_row_expanded_to_all_tokens():
+    x = torch.randn(1, 3, 128, device="cuda").to(torch.bfloat16)
+    pos = torch.arange(7, dtype=torch.int32, device="cuda")
+    many, before = x.expand(7, 3, 128), x.clone()
+    rope = Rope()
+    q, k = rope(many, many[:, :1], pos)
+    _check(q, many, pos, 128, "half")
+    assert torch.equal(k, q[:, :1])
+    with pytest.raises(ValueError):
+        rope(many, None, pos, inplace=True)
+    with pytest.raises(B.AparError):                           # rows that overlap
+        rope(torch.zeros(20 * 128, dtype=torch.bfloat16, device="cuda").as_strided((7, 3, 128), (128, 128, 1)),
+             None, pos)
+    assert torch.equal(x, before)

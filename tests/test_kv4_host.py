@@ -128,3 +128,18 @@ def test_ancestor_masks_may_be_negative(monkeypatch):
     B.apar_tree_verify_attention(None, [0], [2], [1, 2**64 - 1], 0, 0, 1.0)
     B.apar_tree_verify_attention(None, [0], [2], [1, -1], 0, 0, 1.0)
     assert seen == [[1, 2**64 - 1]] * 2
+
+
+def test_rows_of_an_expanded_tensor():
+    """Rope hands apar_rope rows that exist: a stride of 0 between tokens would mean contiguous rows."""
+    import torch
+    from paper_2401_06761_b200.session import Rope
+    one = torch.arange(256).reshape(1, 2, 128).to(torch.bfloat16)
+    many = one.expand(5, 2, 128)
+    rows = Rope._rows(many, False)
+    assert rows.stride(0) == 256 and torch.equal(rows, many)
+    with pytest.raises(ValueError):
+        Rope._rows(many, True)
+    fused = torch.zeros(5, 6, 128, dtype=torch.bfloat16)[:, 1:3]
+    for x in (fused, one, many[:1], many[:0]):                 # as they are
+        assert Rope._rows(x, False) is x and Rope._rows(x, True) is x
