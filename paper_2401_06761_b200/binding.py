@@ -19,6 +19,7 @@ if not os.path.exists(_LIB_PATH):
 lib = C.CDLL(_LIB_PATH)
 
 APAR_OK = 0
+APAR_ERR_INVALID_ARG = -1
 STATUS = {0: "OK", -1: "INVALID_ARG", -2: "BAD_THREAD", -3: "NO_BLOCKS", -4: "NO_THREADS",
           -5: "TABLE_FULL", -6: "EMPTY_CONTEXT", -7: "WORKSPACE_TOO_SMALL", -8: "CUDA",
           -9: "UNSUPPORTED"}
@@ -287,8 +288,10 @@ def apar_note_step_replay(ctx):
 
 def apar_read_kv(ctx, layer: int, tid, begin, count, k_out: int, v_out: int, stream=0):
     tids, n = _arr(tid)
-    begins, _ = _arr(begin)
-    counts, _ = _arr(count)
+    begins, n_begin = _arr(begin)
+    counts, n_count = _arr(count)
+    if n_begin != n or n_count != n:   # (the library takes n entries of each)
+        raise AparError(APAR_ERR_INVALID_ARG)
     _check(lib.apar_read_kv(ctx, layer, n, tids, begins, counts, k_out, v_out, stream))
 
 

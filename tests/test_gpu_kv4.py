@@ -509,3 +509,16 @@ def test_refusals():
     with pytest.raises(B.AparError):
         B.apar_create_kv(sess.cfg, 2)
     sess.close()
+
+
+def test_read_kv_refuses_lists_of_different_lengths_and_negative_counts():
+    sess = PagedSession(LayerShape(4, 2), 16, 4, 4, kv_format="q4")
+    t, u = sess.new_threads(2)
+    k = rows(10, 2, 221)
+    sess.append([t, u], [5, 5], k, k)
+    for args in (([t, u], [0], [5, 5]), ([t, u], [0, 0], [5]), ([t], [0, 0], [5, 5]), ([t, u], [0, 0], [5, -1]),
+                 ([t, u], [0, 0], [-5, -5])):
+        with pytest.raises(B.AparError) as e:
+            sess.read_kv(*args)
+        assert e.value.code == "INVALID_ARG"
+    sess.close()

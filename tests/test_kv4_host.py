@@ -143,3 +143,15 @@ def test_rows_of_an_expanded_tensor():
     fused = torch.zeros(5, 6, 128, dtype=torch.bfloat16)[:, 1:3]
     for x in (fused, one, many[:1], many[:0]):                 # as they are
         assert Rope._rows(x, False) is x and Rope._rows(x, True) is x
+
+
+def test_read_kv_takes_lists_of_one_length():
+    ctx = B.apar_create_host_only(B.make_config(100, 8, 2, 4, 10))
+    t, u = B.apar_new_threads(ctx, 2)
+    B.apar_append_kv(ctx, [t, u], [5, 5], 0, 0)
+    for tids, begin, count in (([t, u], [0], [5, 5]), ([t, u], [0, 0], [5]), ([t], [0, 0], [5]),
+                               ([t], [0], [5, 5]), ([t], [], [])):
+        with pytest.raises(B.AparError) as e:
+            B.apar_read_kv(ctx, 0, tids, begin, count, 256, 256)
+        assert e.value.code == "INVALID_ARG"
+    B.apar_destroy(ctx)
