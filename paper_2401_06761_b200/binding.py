@@ -157,6 +157,14 @@ def _arr(xs):
     return buf, int(a.size)
 
 
+def _arr_for(n, xs):
+    """The array of a list that has an entry for each of n threads (the library reads that many)."""
+    buf, m = _arr(xs)
+    if m < n:
+        raise AparError(APAR_ERR_INVALID_ARG)
+    return buf
+
+
 def _check(status: int):
     if status != APAR_OK:
         raise AparError(status)
@@ -216,7 +224,7 @@ def apar_fork(ctx, parent_tid, stream=0):
 
 def apar_append_kv(ctx, tid, n_tok, k_new: int, v_new: int, stream=0):
     tids, n = _arr(tid)
-    counts = _arr(n_tok)[0] if n_tok is not None else None
+    counts = _arr_for(n, n_tok) if n_tok is not None else None
     _check(lib.apar_append_kv(ctx, n, tids, counts, k_new, v_new, stream))
 
 
@@ -227,7 +235,7 @@ def apar_tree_decode_attention(ctx, tid, q: int, out: int, sm_scale: float, stre
 
 def apar_tree_prefix_attention(ctx, tid, attend_len, q: int, out: int, sm_scale: float, stream=0):
     tids, n = _arr(tid)
-    lens, _ = _arr(attend_len)
+    lens = _arr_for(n, attend_len)
     _check(lib.apar_tree_prefix_attention(ctx, n, tids, lens, q, out, sm_scale, stream))
 
 
@@ -235,7 +243,9 @@ def apar_tree_verify_attention(ctx, tid, n_cand, anc_mask, q: int, out: int, sm_
                                stream=0):
     """anc_mask: one Python int (uint64 bit mask) per candidate, all threads' candidates in order."""
     tids, n = _arr(tid)
-    cands, _ = _arr(n_cand)
+    cands = _arr_for(n, n_cand)
+    if len(anc_mask) < sum(cands[:n]):
+        raise AparError(APAR_ERR_INVALID_ARG)
     m = max(len(anc_mask), 1)
     try:
         masks = (C.c_uint64 * m).from_buffer_copy(struct.pack(f"{m}Q", *(anc_mask or (0,))))
@@ -247,8 +257,8 @@ def apar_tree_verify_attention(ctx, tid, n_cand, anc_mask, q: int, out: int, sm_
 def apar_accept_candidates(ctx, tid, n_cand, keep, stream=0):
     """keep: per thread, the list of candidate indices that stay (increasing)."""
     tids, n = _arr(tid)
-    cands, _ = _arr(n_cand)
-    counts, _ = _arr([len(k) for k in keep])
+    cands = _arr_for(n, n_cand)
+    counts = _arr_for(n, [len(k) for k in keep])
     flat, _ = _arr([x for k in keep for x in k])
     _check(lib.apar_accept_candidates(ctx, n, tids, cands, counts, flat, stream))
 
@@ -256,8 +266,7 @@ def apar_accept_candidates(ctx, tid, n_cand, keep, stream=0):
 def apar_tree_prefill_attention(ctx, layer: int, tid, q_begin, q_count, q: int, out: int,
                                 sm_scale: float, stream=0):
     tids, n = _arr(tid)
-    begins, _ = _arr(q_begin)
-    counts, _ = _arr(q_count)
+    begins, counts = _arr_for(n, q_begin), _arr_for(n, q_count)
     _check(lib.apar_tree_prefill_attention(ctx, layer, n, tids, begins, counts, q, out, sm_scale,
                                            stream))
 
@@ -317,7 +326,7 @@ def apar_tree_decode_attention_tables(cfg, block_tables, ctx_lens, q: int, out: 
                                       sm_scale: float, stream=0):
     """block_tables: n rows, each padded by the caller to cfg.max_blocks_per_thread ints."""
     lens, n = _arr(ctx_lens)
-    flat, _ = _arr(x for row in block_tables for x in row)
+    flat = _arr_for(n * cfg.max_blocks_per_thread, [x for row in block_tables for x in row])
     _check(lib.apar_tree_decode_attention_tables(C.byref(cfg), n, flat, lens, q, out,
                                                  sm_scale, stream))
 

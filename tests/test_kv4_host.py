@@ -155,3 +155,39 @@ def test_read_kv_takes_lists_of_one_length():
             B.apar_read_kv(ctx, 0, tids, begin, count, 256, 256)
         assert e.value.code == "INVALID_ARG"
     B.apar_destroy(ctx)
+
+
+def test_lists_shorter_than_the_threads_they_go_with(monkeypatch):
+    """Refused before the library would read past them; what is as long or longer goes through."""
+    calls = []
+
+    class Lib:
+        def __getattr__(self, name):
+            if name == "apar_status_string":
+                return lambda status: b""
+            return lambda *args: calls.append(name) or 0
+    monkeypatch.setattr(B, "lib", Lib())
+    cfg = B.make_config(100, 8, 2, 4, 3)
+
+    def refused(f, *args):
+        before = len(calls)
+        with pytest.raises(B.AparError) as e:
+            f(*args)
+        assert e.value.code == "INVALID_ARG" and len(calls) == before
+    refused(B.apar_append_kv, None, [1, 2], [3], 0, 0)
+    refused(B.apar_tree_prefix_attention, None, [1, 2], [3], 0, 0, 1.0)
+    refused(B.apar_tree_verify_attention, None, [1, 2], [1], [1, 1], 0, 0, 1.0)
+    refused(B.apar_tree_verify_attention, None, [1, 2], [1, 2], [1, 1], 0, 0, 1.0)
+    refused(B.apar_accept_candidates, None, [1, 2], [1], [[0], [0]])
+    refused(B.apar_accept_candidates, None, [1, 2], [1, 1], [[0]])
+    refused(B.apar_tree_prefill_attention, None, 0, [1, 2], [0], [1, 1], 0, 0, 1.0)
+    refused(B.apar_tree_prefill_attention, None, 0, [1, 2], [0, 0], [1], 0, 0, 1.0)
+    refused(B.apar_tree_decode_attention_tables, cfg, [[0, 1, 2], [0, 1]], [16, 16], 0, 0, 1.0)
+    B.apar_append_kv(None, [1, 2], None, 0, 0)
+    B.apar_append_kv(None, [1, 2], [3, 4, 5], 0, 0)
+    B.apar_tree_prefix_attention(None, [1, 2], [3, 4], 0, 0, 1.0)
+    B.apar_tree_verify_attention(None, [1, 2], [1, 2], [1, 1, 3], 0, 0, 1.0)
+    B.apar_accept_candidates(None, [1, 2], [1, 1], [[0], []])
+    B.apar_tree_prefill_attention(None, 0, [1, 2], [0, 0], [1, 1], 0, 0, 1.0)
+    B.apar_tree_decode_attention_tables(cfg, [[0, 1, 2], [0, 1, 2]], [16, 16], 0, 0, 1.0)
+    assert len(calls) == 7
