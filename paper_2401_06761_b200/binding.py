@@ -241,14 +241,14 @@ def apar_tree_prefix_attention(ctx, tid, attend_len, q: int, out: int, sm_scale:
 
 def apar_tree_verify_attention(ctx, tid, n_cand, anc_mask, q: int, out: int, sm_scale: float,
                                stream=0):
-    """anc_mask: one Python int (uint64 bit mask) per candidate, all threads' candidates in order."""
+    """anc_mask: a sequence of ints (uint64 bit masks), one per candidate, all threads' in order."""
     tids, n = _arr(tid)
     cands = _arr_for(n, n_cand)
     if len(anc_mask) < sum(cands[:n]):
         raise AparError(APAR_ERR_INVALID_ARG)
     m = max(len(anc_mask), 1)
     try:
-        masks = (C.c_uint64 * m).from_buffer_copy(struct.pack(f"{m}Q", *(anc_mask or (0,))))
+        masks = (C.c_uint64 * m).from_buffer_copy(struct.pack(f"{m}Q", *(anc_mask if len(anc_mask) else (0,))))
     except struct.error:               # (a negative int stands for its 64 low bits)
         masks = (C.c_uint64 * m)(*anc_mask)
     _check(lib.apar_tree_verify_attention(ctx, n, tids, cands, masks, q, out, sm_scale, stream))

@@ -191,3 +191,23 @@ def test_lists_shorter_than_the_threads_they_go_with(monkeypatch):
     B.apar_tree_prefill_attention(None, 0, [1, 2], [0, 0], [1, 1], 0, 0, 1.0)
     B.apar_tree_decode_attention_tables(cfg, [[0, 1, 2], [0, 1, 2]], [16, 16], 0, 0, 1.0)
     assert len(calls) == 7
+
+
+def test_ancestor_masks_in_arrays(monkeypatch):
+    import torch
+    seen = []
+
+    class Lib:
+        @staticmethod
+        def apar_tree_verify_attention(ctx, n, tids, cands, masks, q, out, scale, stream):
+            seen.append(list(masks))
+            return 0
+    monkeypatch.setattr(B, "lib", Lib)
+    for masks in (np.array([1, 3], np.uint64), np.array([1, 3]), torch.tensor([1, 3]), (1, 3), [np.uint64(1), 3]):
+        B.apar_tree_verify_attention(None, [0], [2], masks, 0, 0, 1.0)
+    assert seen == [[1, 3]] * 5
+    for masks in (np.array([1, -1]), torch.tensor([1, -1])):   # (negative: the 64 low bits)
+        B.apar_tree_verify_attention(None, [0], [2], masks, 0, 0, 1.0)
+    assert seen[5:] == [[1, 2**64 - 1]] * 2
+    for masks in (np.array([], np.uint64), torch.tensor([], dtype=torch.int64), []):
+        B.apar_tree_verify_attention(None, [], [], masks, 0, 0, 1.0)
