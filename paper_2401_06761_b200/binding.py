@@ -149,7 +149,7 @@ def _arr(xs):
         n = len(xs)
         try:                           # (several times as fast as numpy for short lists)
             raw = _packer(max(n, 1)).pack(*(xs or (0,)))
-        except struct.error:           # not plain ints of 32 bits: numpy's conversions and errors
+        except (struct.error, TypeError):   # not plain 32-bit ints: numpy's conversions and errors
             raw = np.fromiter(xs, dtype=np.int32).tobytes()
         return (C.c_int32 * max(n, 1)).from_buffer_copy(raw), n
     a = np.ascontiguousarray(xs.astype(np.int32, copy=False))

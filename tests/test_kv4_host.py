@@ -211,3 +211,10 @@ def test_ancestor_masks_in_arrays(monkeypatch):
     assert seen[5:] == [[1, 2**64 - 1]] * 2
     for masks in (np.array([], np.uint64), torch.tensor([], dtype=torch.int64), []):
         B.apar_tree_verify_attention(None, [], [], masks, 0, 0, 1.0)
+
+
+def test_argument_lists_of_tensors():
+    import torch
+    for xs in ([torch.tensor(3.0), torch.tensor(-1)], [torch.tensor([3]), -1], torch.tensor([3, -1])):
+        buf, n = B._arr(xs)
+        assert n == 2 and list(buf) == [3, -1]
