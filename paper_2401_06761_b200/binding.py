@@ -142,7 +142,7 @@ def _packer(n):
 
 
 def _arr(xs):
-    if isinstance(xs, tuple) and len(xs) == 2 and isinstance(xs[1], int):
+    if isinstance(xs, tuple) and len(xs) == 2 and isinstance(xs[0], C.Array):
         return xs          # already marshalled by int32_array()
     if not isinstance(xs, np.ndarray):
         xs = xs if isinstance(xs, (list, tuple)) else list(xs)

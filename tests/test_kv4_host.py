@@ -218,3 +218,11 @@ def test_argument_lists_of_tensors():
     for xs in ([torch.tensor(3.0), torch.tensor(-1)], [torch.tensor([3]), -1], torch.tensor([3, -1])):
         buf, n = B._arr(xs)
         assert n == 2 and list(buf) == [3, -1]
+
+
+def test_argument_lists_that_are_pairs():
+    """A tuple of two ints is a list of two; what int32_array made goes through as it is."""
+    buf, n = B._arr((5, 7))
+    assert n == 2 and list(buf) == [5, 7]
+    made = B.int32_array([5, 7, 9])
+    assert B._arr(made) is made
