@@ -46,7 +46,7 @@ class Rope:
         assert positions.shape == (n,)
         here = torch.cuda.current_device()             # (the launch goes to its current stream)
         assert positions.get_device() == here
-        outs, sides = [], []
+        outs, sides, held = [], [], []                 # (held: copies live until the launch)
         for x in (q, k):
             if x is None:
                 outs.append(None)
@@ -57,6 +57,7 @@ class Rope:
             assert x.shape[2] == self.cfg.head_dim
             assert x.stride(2) == 1 and (x.shape[1] == 1 or x.stride(1) == x.shape[2])
             x = self._rows(x, inplace)
+            held.append(x)
             out = x if inplace else torch.empty_like(x, memory_format=torch.contiguous_format)
             stride = x.stride(0) if n > 1 else 0       # (0: contiguous)
             outs.append(out)
