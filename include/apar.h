@@ -175,7 +175,7 @@ apar_status apar_create_kv(const apar_config* cfg /*[host]*/, int32_t kv_format,
 /* Reads rows of the cache back as bf16 (4-bit rows: lo + s * c, rounded once): for entry i the
  * rows of thread tid[i] at chain positions begin[i] .. begin[i] + count[i] - 1 of pool layer
  * `layer`, entries one after the other.  A thread may be listed several times, count 0 is allowed.
- *   k_out, v_out [device] bf16 [sum count][num_kv_heads][128], 16-byte aligned.
+ *   k_out, v_out [device] bf16 [sum count][num_kv_heads][128], 16-byte aligned (NULL where the sum is 0).
  * Works on both formats.  Uses the staging buffers, so it cannot be captured.
  * Errors: INVALID_ARG (also rows outside a thread, a misaligned output, a capturing stream),
  * BAD_THREAD, UNSUPPORTED (host-only context), CUDA. */

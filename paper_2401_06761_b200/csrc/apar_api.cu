@@ -1479,8 +1479,7 @@ apar_status apar_read_kv(apar_ctx* c, int32_t layer, int32_t n, const int32_t* t
                          const int32_t* begin, const int32_t* count, void* k_out, void* v_out,
                          void* cuda_stream) {
   if (!c || n < 0 || layer < 0 || layer >= c->num_layers ||
-      (n > 0 && (!tid || !begin || !count || !k_out || !v_out)) ||
-      (((uintptr_t)k_out | (uintptr_t)v_out) & 15))
+      (n > 0 && (!tid || !begin || !count)))
     return APAR_ERR_INVALID_ARG;
   if (c->host_only) return APAR_ERR_UNSUPPORTED;
   cudaStream_t st = (cudaStream_t)cuda_stream;
@@ -1492,7 +1491,8 @@ apar_status apar_read_kv(apar_ctx* c, int32_t layer, int32_t n, const int32_t* t
       return APAR_ERR_INVALID_ARG;
     rows += count[i];
   }
-  if (rows == 0) return APAR_OK;
+  if (rows == 0) return APAR_OK;        // (the outputs may then be empty, without an address)
+  if (!k_out || !v_out || (((uintptr_t)k_out | (uintptr_t)v_out) & 15)) return APAR_ERR_INVALID_ARG;
   {
     // the list of rows goes through the staging buffers, which a captured call may not use
     cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;

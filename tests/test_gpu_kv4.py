@@ -522,3 +522,35 @@ def test_read_kv_refuses_lists_of_different_lengths_and_negative_counts():
             sess.read_kv(*args)
         assert e.value.code == "INVALID_ARG"
     sess.close()
+
+
+@pytest.mark.parametrize("fmt", ["q4", "bf16"])
+def test_read_kv_of_no_rows(fmt):
+    sess = PagedSession(LayerShape(4, 2), 16, 4, 4, kv_format=fmt)
+    t, u = sess.new_threads(2)
+    k = rows(5, 2, 231)
+    sess.append([t], [5], k, k)
+    for args in (([], [], []), ([t], [5], [0]), ([u, t], [0, 2], [0, 0])):
+        gk, gv = sess.read_kv(*args)
+        assert gk.shape == gv.shape == (0, 2, 128)
+    for args in (([t], [6], [0]), ([t], [0], [6])):
+        with pytest.raises(B.AparError):
+            sess.read_kv(*args)
+    with pytest.raises(B.AparError):
+        B.apar_read_kv(sess.ctx, 0, [t], [0], [1], 0, 0)
+    sess.close()
+
+
+@pytest.mark.parametrize("fmt", ["q4", "bf16"])
+def test_read_kv_of_more_rows_than_one_upload_lists(fmt):
+    """2^18 rows go to a launch; the next one begins inside an entry."""
+    sess = PagedSession(LayerShape(1, 1), 160, 4, 140, kv_format=fmt)
+    (t,) = sess.new_threads(1)
+    n, times = 2000, 140
+    k, v = rows(n, 1, 232), rows(n, 1, 233)
+    sess.append([t], [n], k, v)
+    gk, gv = sess.read_kv([t] * times, [0] * times, [n] * times)
+    for got, x in ((gk, k), (gv, v)):
+        want = torch.from_numpy(_expect_rows(x)).to(torch.bfloat16).cuda() if fmt == "q4" else x
+        assert torch.equal(got.view(times, n, 1, 128), want.expand(times, n, 1, 128))
+    sess.close()
