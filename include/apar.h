@@ -455,7 +455,8 @@ typedef struct {
  *   num_kv_heads may be 0 (that side's pointers are ignored).
  * Rows on 16-byte boundaries (and rotary_dim a multiple of 16 in the half layout) take a vectorised
  * kernel, others an element-wise one.  No context, no workspace; can be captured in a graph.
- * Errors: INVALID_ARG, UNSUPPORTED (head_dim), CUDA (read it with cudaGetLastError). */
+ * Errors: INVALID_ARG, UNSUPPORTED (head_dim), CUDA (of this call's own launch;
+ * apar_last_cuda_error(NULL) gives its code). */
 apar_status apar_rope(const apar_rope_config* cfg /*[host]*/, int32_t n,
                       const int32_t* positions /*[device]*/, int32_t num_q_heads,
                       const void* q /*[device]*/, int64_t q_stride, void* q_out /*[device]*/,
@@ -542,7 +543,7 @@ apar_status apar_debug_plan_threads(apar_ctx* ctx, int32_t n, const int32_t* tid
  *   src   [device] 16-byte aligned, caller-owned, not modified
  *   sink  [device] 8-byte aligned word, caller-owned; its old value is xor-ed into, not cleared
  * Returns APAR_ERR_INVALID_ARG for NULL or misaligned pointers, APAR_ERR_CUDA if the launch
- * failed (no context, so the CUDA error is read with cudaGetLastError by the caller). */
+ * failed (no context: apar_last_cuda_error(NULL) gives the CUDA error). */
 apar_status apar_stream_read(const void* src, size_t bytes, void* sink, void* cuda_stream);
 
 /* Measurement aid (the paper has no counterpart): from now on every attention call of this
@@ -553,7 +554,9 @@ apar_status apar_stream_read(const void* src, size_t bytes, void* sink, void* cu
  * it off.  Errors: INVALID_ARG if only one of the two is NULL. */
 apar_status apar_set_timing_events(apar_ctx* ctx, void* start, void* stop);
 
-/* cudaError_t value of the most recent failing CUDA call of this context (0 if none). */
+/* cudaError_t value of the most recent failing CUDA call of this context (0 if none).  NULL: of the
+ * calling thread's most recent apar_rope or apar_stream_read that returned APAR_ERR_CUDA.  (The
+ * library has a CUDA runtime of its own; the caller's cudaGetLastError knows nothing of it.) */
 int32_t     apar_last_cuda_error(apar_ctx* ctx);
 const char* apar_status_string(apar_status s);
 

@@ -737,7 +737,11 @@ apar_status create_impl(const apar_config* cfg, bool external, bool host_only, i
   return APAR_OK;
 }
 
+thread_local int32_t t_last_cuda = 0;   // of calls without a context
+
 }  // namespace
+
+void apar::note_cuda_error(cudaError_t e) { t_last_cuda = (int32_t)e; }
 
 extern "C" {
 
@@ -1850,11 +1854,17 @@ apar_status apar_stream_read(const void* src, size_t bytes, void* sink, void* st
       (reinterpret_cast<uintptr_t>(sink) & 7))
     return APAR_ERR_INVALID_ARG;
   int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms <= 0)
+  cudaError_t found = cudaGetDevice(&dev);
+  if (found == cudaSuccess)
+    found = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (found != cudaSuccess || sms <= 0) {
+    note_cuda_error(found);
     return APAR_ERR_CUDA;
-  return launch_stream_read(src, bytes, sink, sms, (cudaStream_t)stream) == cudaSuccess
-             ? APAR_OK : APAR_ERR_CUDA;
+  }
+  const cudaError_t e = launch_stream_read(src, bytes, sink, sms, (cudaStream_t)stream);
+  if (e == cudaSuccess) return APAR_OK;
+  note_cuda_error(e);
+  return APAR_ERR_CUDA;
 }
 
 apar_status apar_set_timing_events(apar_ctx* c, void* start, void* stop) {
@@ -1864,7 +1874,7 @@ apar_status apar_set_timing_events(apar_ctx* c, void* start, void* stop) {
   return APAR_OK;
 }
 
-int32_t apar_last_cuda_error(apar_ctx* c) { return c ? c->last_cuda : 0; }
+int32_t apar_last_cuda_error(apar_ctx* c) { return c ? c->last_cuda : t_last_cuda; }
 
 const char* apar_status_string(apar_status s) {
   switch (s) {

@@ -119,6 +119,9 @@ inline cudaError_t launch_kernel(void (*kernel)(KArgs...), dim3 grid, dim3 block
 }
 #endif
 
+// Keeps the error of a call without a context for apar_last_cuda_error(NULL) on this thread.
+void note_cuda_error(cudaError_t e);
+
 // ---- kernel launchers (kernels.cu); all enqueue on `st` and return cudaGetLastError() ----
 cudaError_t launch_cow_copy(void* k_pool, void* v_pool, const CowCopy* d_copies, int n,
                             int num_kv_heads, cudaStream_t st);

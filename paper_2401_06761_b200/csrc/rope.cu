@@ -247,9 +247,10 @@ extern "C" apar_status apar_rope(const apar_rope_config* cfg, int32_t n, const i
   // Several tokens to a CTA once there are enough of them to fill the machine that way.
   const int tokens = n >= 4096 ? kMaxTokens : 1;
   const unsigned grid = (unsigned)((n + (int64_t)tokens - 1) / tokens);
-  if (vec)
-    rope_vec_kernel<<<grid, kRopeThreads, 0, (cudaStream_t)cuda_stream>>>(a, tokens);
-  else
-    rope_any_kernel<<<grid, kRopeThreads, 0, (cudaStream_t)cuda_stream>>>(a, tokens);
-  return cudaGetLastError() == cudaSuccess ? APAR_OK : APAR_ERR_CUDA;
+  // (the launch's own status: an error that an earlier call left is neither taken for it nor lost)
+  const cudaError_t e = launch_kernel(vec ? rope_vec_kernel : rope_any_kernel, dim3(grid),
+                                      dim3(kRopeThreads), 0, (cudaStream_t)cuda_stream, false, a, tokens);
+  if (e == cudaSuccess) return APAR_OK;
+  note_cuda_error(e);
+  return APAR_ERR_CUDA;
 }

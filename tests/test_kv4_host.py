@@ -226,3 +226,27 @@ def test_argument_lists_that_are_pairs():
     assert n == 2 and list(buf) == [5, 7]
     made = B.int32_array([5, 7, 9])
     assert B._arr(made) is made
+
+
+def test_a_failed_launch_without_a_context_leaves_its_code():
+    """In a process that sees no device: every call fails before anything is launched, and the code
+    can be read afterwards, once more after a second call too."""
+    import os
+    import subprocess
+    import sys
+    code = """
+from paper_2401_06761_b200 import binding as B
+assert B.apar_last_cuda_error(None) == 0
+for call in (lambda: B.apar_rope(B.make_rope_config(), 1, 4096, 1, 4096, 0, 8192, 0, 0, 0, 0, 0, 0),
+             lambda: B.apar_stream_read(4096, 16, 8192)) * 2:
+    try:
+        call()
+        raise SystemExit(2)
+    except B.AparError as e:
+        assert e.code == "CUDA", e.code
+    assert B.apar_last_cuda_error(None) != 0
+"""
+    env = dict(os.environ, CUDA_VISIBLE_DEVICES="")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", code], env=env, cwd=root, capture_output=True, text=True)
+    assert done.returncode == 0, done.stderr
