@@ -11,6 +11,11 @@ from . import binding as B
 from .synth import ForestSpec, LayerShape
 
 
+# torch.cuda.current_stream().cuda_stream without its 3 us of wrapping; not part of torch's public
+# interface, so that its absence must not matter
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def pool_requirements(spec: ForestSpec, slack: float = 0.05):
     """(num_blocks, max_threads, max_blocks_per_thread) that hold `spec`."""
     bs = spec.shape.block_size
@@ -122,8 +127,9 @@ class PagedSession:
 
     @staticmethod
     def _stream() -> int:
-        # (torch.cuda.current_stream().cuda_stream without its 3 us of wrapping)
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        if _raw_stream is None:
+            return torch.cuda.current_stream().cuda_stream
+        return _raw_stream(torch.cuda.current_device())
 
     # the replay protocol of synth.build_forest
     def new_threads(self, n):

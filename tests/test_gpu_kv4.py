@@ -554,3 +554,13 @@ def test_read_kv_of_more_rows_than_one_upload_lists(fmt):
         want = torch.from_numpy(_expect_rows(x)).to(torch.bfloat16).cuda() if fmt == "q4" else x
         assert torch.equal(got.view(times, n, 1, 128), want.expand(times, n, 1, 128))
     sess.close()
+
+
+def test_the_current_stream_with_and_without_the_short_way(monkeypatch):
+    from paper_2401_06761_b200 import session
+    for short in (session._raw_stream, None):
+        monkeypatch.setattr(session, "_raw_stream", short)
+        stream = torch.cuda.Stream()
+        assert PagedSession._stream() == torch.cuda.current_stream().cuda_stream
+        with torch.cuda.stream(stream):
+            assert PagedSession._stream() == stream.cuda_stream
