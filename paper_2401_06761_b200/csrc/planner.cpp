@@ -29,8 +29,14 @@ void Planner::init(int num_blocks, int group, int num_kv_heads) {
 
 static inline int64_t round_up16(int64_t x) { return (x + 15) / 16 * 16; }
 // 4-bit pools.  A wide unit takes the time of some four units of a single warp, so up to three of
-// those do the work of one: 64 runs of 2048 tokens on 8 kv heads take with 16 rows 104 us against
-// 144, with 24 rows 130 against 154, with 32 rows 189 against 159, with 64 rows 312 against 175.
+// those do the work of one (kStreamUnits).  Measured on 1.2 M tokens times kv heads, with 4, 8 and 32
+// kv heads alike, in runs of 512 / 2048 / 8192 tokens, by single warps against as a wide unit:
+//   16 rows 142 / 112 / 108 us against 222 / 157 / 142    32 rows 228 / 200 / 194 against 241 / 167 / 151
+//   24 rows 171 / 138 / 173 us against 226 / 161 / 151    64 rows 448 / 359 / 372 against 294 / 181 / 226
+// kWideCost weighs units against each other when runs are cut.  Four, six and eight were measured on
+// 40 trees: all within 3 % of one another, except where a few runs of 8192 tokens and more make about
+// as many units as the machine takes at once; there a cut more or less decides, and four took
+// between 0.53 and 1.5 times what six did, with no rule to it.
 constexpr int kWideCost = 4, kStreamUnits = 3;
 constexpr int kMaxFoldedParts = 8;   // partial results a finishing item may fold by itself
 
@@ -153,7 +159,9 @@ bool Planner::build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_
   bool many_units = false;
   if (streams_) {
     // With little to do, everything goes to single warps: a wide unit takes some 10 us to come and
-    // go, in which a warp does about four blocks.
+    // go.  64 rows on runs of 128 / 1024 tokens, all by warps against the wide kernel for its share:
+    // 19 / 20 us against 32 / 32 with four blocks a warp, 30 / 24 against 40 / 34 with eight, 50 / 38
+    // against 56 / 38 with sixteen, 83 / 62 against 79 / 52 with 32.
     int64_t blocks = 0;
     for (const Seg& g : segs_)
       blocks += ((int64_t)g.n_users * group_ + stream_rows_ - 1) / stream_rows_ * hint_kv_heads_ *
