@@ -214,7 +214,8 @@ class PagedSession:
     def read_kv(self, tids, begin, count, layer: int = 0):
         """Rows begin[i] .. begin[i] + count[i] - 1 of each thread's chain, as bf16 (k, v)."""
         count = B.int32_array(count)
-        rows = int(np.frombuffer(count[0], np.int32, count[1]).clip(0).sum(dtype=np.int64))
+        # (negative counts are the library's to refuse)
+        rows = max(0, int(np.frombuffer(count[0], np.int32, count[1]).sum(dtype=np.int64)))
         shape = (rows, self.shape.num_kv_heads, self.shape.head_dim)
         k = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
         v = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
