@@ -45,7 +45,7 @@
 // keys the rest.  (Then a tile took a CTA some 3600 cycles, of which a converter warp was busy 2500,
 // a softmax warp 2300 and the MMA warp 1500; the converters' share is what grew.)  No single unit
 // is full: the roles wait for one another, and 18 warps of different code miss the instruction
-// cache (a fifth of the stalls).
+// cache (a sixth of the stalls).
 #include <algorithm>
 #include <climits>
 
