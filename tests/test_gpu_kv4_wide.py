@@ -20,7 +20,7 @@ def _candidate_tree(rng, n):
 
 
 def _check_candidates(p, root, got, parents, k, v, q):
-    """Each candidate is a thread of its own in the checker, forked from its parent candidate."""
+    """Each candidate is a thread of its own in the oracle, forked from its parent candidate."""
     node = []
     for j, par in enumerate(parents):
         src = root if par < 0 else node[par]
