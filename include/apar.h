@@ -150,11 +150,12 @@ apar_status apar_destroy(apar_ctx* ctx);
  *   codes inside a row is the library's own; apar_read_kv gives the rows as numbers.
  *   Attention reads q and writes out as bf16.  Scores, the softmax's sums and the results are summed
  *   in 32 bits; q and the values of K enter the scores unrounded (a query's dims lose digits below
- *   2^-27 of its largest, the scales of a K row's groups below 2^-12 of the row's largest scale).  Rounded to 11 bits are the weights, after they are scaled (each then
- *   multiplies a value or its distance from the middle of its group), and in runs of tokens that
- *   more than eight query rows share V's values.  All of it is less than the rounding of the result
- *   to bf16 (measured up to 400 000 tokens), for groups of a V row down to 2^-20 of the row's
- *   largest.  A NaN row makes NaN of the outputs that see it, and only of those.
+ *   2^-27 of its largest, the scales of a K row's groups below 2^-12 of the row's largest scale).
+ *   Rounded to 11 bits are the weights, after they are scaled (each then multiplies a value or its
+ *   distance from the middle of its group), and in runs of tokens that more than eight query
+ *   rows share V's values.  All of it is less than the rounding of the result to bf16 (measured
+ *   up to 400 000 tokens), for groups of a V row down to 2^-20 of the row's largest.  A NaN row
+ *   makes NaN of the outputs that see it, and only of those.
  * All calls of this header work on such a context, except apar_tree_prefill_attention, which
  * returns APAR_ERR_UNSUPPORTED (apar_tree_prefix_attention serves runs of up to max_threads
  * queries).  Device row pointers (q, out, k_new, v_new) must be 16-byte aligned: otherwise
