@@ -464,6 +464,49 @@ apar_status apar_rope(const apar_rope_config* cfg /*[host]*/, int32_t n,
                       int64_t k_stride, void* k_out /*[device]*/, int64_t k_out_stride,
                       void* cuda_stream);
 
+/* Beam search's selection (the paper has no counterpart: its threads sample greedily).  A sequence
+ * is decoded by num_beams beams; a pair (b, v) of a beam and a token has the value
+ *     score[b] + x[b][v] - log sum_u exp(x[b][u]),      x the beam's row of logits.
+ * Chosen are the num_select pairs of the highest values over all beams and the whole vocabulary,
+ * highest first; of equal values the lower beam's, then the lower token.  Values are compared in 64
+ * bits; each sum of exponentials is taken in 32. */
+enum {
+  APAR_LOGITS_BF16 = 0,
+  APAR_LOGITS_F16 = 1,
+  APAR_LOGITS_F32 = 2
+};
+typedef struct {
+  int32_t vocab;        /* tokens, 1 .. 2^28 - 1                                                  */
+  int32_t num_beams;    /* beams of a sequence, 1 .. 64                                           */
+  int32_t num_select;   /* pairs to choose per sequence, 1 .. 64                                  */
+  int32_t logits_type;  /* APAR_LOGITS_*                                                          */
+  int32_t eos;          /* the token a finished beam goes on with; -1: none (no finished beams)   */
+  int32_t reserved;
+} apar_beam_config;
+/* Bytes of device scratch apar_beam_select needs for n_seq sequences; 0 for a bad configuration. */
+size_t apar_beam_workspace_bytes(const apar_beam_config* cfg /*[host]*/, int32_t n_seq);
+/* Chooses for n_seq sequences.
+ *   logits [device] row of beam b of sequence i at logits + i * seq_stride + b * beam_stride elements
+ *          (strides of 0 mean contiguous rows); rows may begin on any element
+ *   scores [device] float [n_seq][num_beams].  A beam whose score is not finite has no pairs (the
+ *          unused beams of a search's first step have the score -inf), nor has one whose logits hold
+ *          a NaN or +inf or are all -inf, and a token whose logit is -inf is never chosen.
+ *   finished [device] uint8 [n_seq][num_beams] or NULL: a beam whose entry is not 0 has a single pair,
+ *          (b, eos) with its own score; its logits are not looked at
+ *   out_score [device] float [n_seq][num_select], out_beam and out_token [device] int32, likewise.
+ *          Where pairs run out: -inf, -1, -1.
+ *   workspace [device] 256-byte aligned, its old contents do not matter; calls that may run at the
+ *          same time need one each.
+ * No context; can be captured in a graph.
+ * Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, CUDA (apar_last_cuda_error(NULL) gives its code). */
+apar_status apar_beam_select(const apar_beam_config* cfg /*[host]*/, int32_t n_seq,
+                             const void* logits /*[device]*/, int64_t seq_stride,
+                             int64_t beam_stride, const float* scores /*[device]*/,
+                             const uint8_t* finished /*[device] or NULL*/,
+                             float* out_score /*[device]*/, int32_t* out_beam /*[device]*/,
+                             int32_t* out_token /*[device]*/, void* workspace /*[device]*/,
+                             size_t workspace_bytes, void* cuda_stream);
+
 /* Paragraph tree of Algorithm 1 (host only): which slice of which sequence belongs where in the
  * final text.  apar_paragraph_root makes thread tid (a prompt sequence, already holding its
  * prompt) the root: its node starts at the thread's current length.  From then on every
@@ -555,7 +598,7 @@ apar_status apar_stream_read(const void* src, size_t bytes, void* sink, void* cu
 apar_status apar_set_timing_events(apar_ctx* ctx, void* start, void* stop);
 
 /* cudaError_t value of the most recent failing CUDA call of this context (0 if none).  NULL: of the
- * calling thread's most recent apar_rope or apar_stream_read that returned APAR_ERR_CUDA.  (The
+ * calling thread's most recent apar_rope, apar_beam_select or apar_stream_read that returned APAR_ERR_CUDA.  (The
  * library has a CUDA runtime of its own; the caller's cudaGetLastError knows nothing of it.) */
 int32_t     apar_last_cuda_error(apar_ctx* ctx);
 const char* apar_status_string(apar_status s);

@@ -48,9 +48,15 @@ class apar_rope_config(C.Structure):
                 ("high", C.c_double), ("attn_scale", C.c_double)]
 
 
+class apar_beam_config(C.Structure):
+    _fields_ = [("vocab", C.c_int32), ("num_beams", C.c_int32), ("num_select", C.c_int32),
+                ("logits_type", C.c_int32), ("eos", C.c_int32), ("reserved", C.c_int32)]
+
+
 KV_FORMATS = {"bf16": 0, "q4": 1}
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 ROPE_SCALINGS = {"none": 0, "linear": 1, "bands": 2, "yarn": 3}
+LOGITS_TYPES = {"bfloat16": 0, "float16": 1, "float32": 2}
 
 
 class apar_stats(C.Structure):
@@ -80,6 +86,10 @@ _SIGS = {
     "apar_rope": (C.c_int32, [C.POINTER(apar_rope_config), C.c_int32, C.c_void_p, C.c_int32,
                               C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p,
                               C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]),
+    "apar_beam_workspace_bytes": (C.c_size_t, [C.POINTER(apar_beam_config), C.c_int32]),
+    "apar_beam_select": (C.c_int32, [C.POINTER(apar_beam_config), C.c_int32, C.c_void_p, C.c_int64,
+                                     C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                     C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "apar_destroy": (C.c_int32, [_ctx]),
     "apar_new_threads": (C.c_int32, [_ctx, C.c_int32, _i32p]),
     "apar_fork": (C.c_int32, [_ctx, C.c_int32, _i32p, _i32p, C.c_void_p]),
@@ -315,6 +325,23 @@ def apar_rope(cfg: apar_rope_config, n: int, positions: int, num_q_heads: int, q
               k_stride: int, k_out: int, k_out_stride: int, stream=0):
     _check(lib.apar_rope(C.byref(cfg), n, positions, num_q_heads, q, q_stride, q_out, q_out_stride,
                          num_kv_heads, k, k_stride, k_out, k_out_stride, stream))
+
+
+def make_beam_config(vocab, num_beams, num_select, logits_type="bfloat16", eos=None):
+    return apar_beam_config(vocab, num_beams, num_select, LOGITS_TYPES[logits_type],
+                            -1 if eos is None else eos, 0)
+
+
+def apar_beam_workspace_bytes(cfg: apar_beam_config, n_seq: int) -> int:
+    return lib.apar_beam_workspace_bytes(C.byref(cfg), n_seq)
+
+
+def apar_beam_select(cfg: apar_beam_config, n_seq: int, logits: int, seq_stride: int,
+                     beam_stride: int, scores: int, finished: int, out_score: int, out_beam: int,
+                     out_token: int, workspace: int, workspace_bytes: int, stream=0):
+    _check(lib.apar_beam_select(C.byref(cfg), n_seq, logits, seq_stride, beam_stride, scores,
+                                finished or None, out_score, out_beam, out_token, workspace,
+                                workspace_bytes, stream))
 
 
 def apar_release(ctx, tid):

@@ -71,6 +71,43 @@ class Rope:
         return tuple(outs)
 
 
+class BeamSelect:
+    """Beam search's selection: the parameters of apar_beam_config, applied by calling.
+
+    logits [n][beams][vocab] is bf16, f16 or f32 and may be a view with any strides of its first two
+    dims; scores is f32 [n][beams]; finished is None or a bool or uint8 tensor [n][beams] (then eos is
+    needed).  Returns (scores f32, beams int32, tokens int32), each [n][select], best first."""
+
+    def __init__(self, beams: int, vocab: int, select: int, eos=None):
+        self.beams, self.vocab, self.select = beams, vocab, select
+        self.cfgs = {t: B.make_beam_config(vocab, beams, select, str(t).rpartition(".")[2], eos)
+                     for t in (torch.bfloat16, torch.float16, torch.float32)}
+        self._bytes = {}                               # scratch by number of sequences
+
+    def __call__(self, logits: torch.Tensor, scores: torch.Tensor, finished: torch.Tensor = None):
+        n = logits.shape[0]
+        here = torch.cuda.current_device()             # (the launches go to its current stream)
+        assert logits.shape == (n, self.beams, self.vocab) and logits.dtype in self.cfgs
+        assert scores.shape == (n, self.beams) and scores.dtype == torch.float32
+        assert logits.get_device() == here and scores.get_device() == here and scores.is_contiguous()
+        if finished is not None:
+            assert finished.shape == (n, self.beams) and finished.dtype in (torch.bool, torch.uint8)
+            assert finished.get_device() == here and finished.is_contiguous()
+        if (self.vocab > 1 and logits.stride(2) != 1) or 0 in logits.stride()[:2]:
+            logits = logits.contiguous()               # (a stride of 0 stands for contiguous rows)
+        cfg = self.cfgs[logits.dtype]
+        if n not in self._bytes:
+            self._bytes[n] = B.apar_beam_workspace_bytes(cfg, n)
+        held = torch.empty(self._bytes[n], dtype=torch.uint8, device=logits.device)
+        best = torch.empty((n, self.select), dtype=torch.float32, device=logits.device)
+        beams, tokens = torch.empty((2, n, self.select), dtype=torch.int32, device=logits.device)
+        B.apar_beam_select(cfg, n, logits.data_ptr(), logits.stride(0), logits.stride(1),
+                           scores.data_ptr(), 0 if finished is None else finished.data_ptr(),
+                           best.data_ptr(), beams.data_ptr(), tokens.data_ptr(), held.data_ptr(),
+                           self._bytes[n], PagedSession._stream())
+        return best, beams, tokens
+
+
 class PagedSession:
     def __init__(self, shape: LayerShape, num_blocks: int, max_threads: int,
                  max_blocks_per_thread: int, device="cuda", poison: bool = False,
