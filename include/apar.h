@@ -129,7 +129,8 @@ size_t apar_workspace_bytes(const apar_config* cfg /*[host]*/);
 apar_status apar_create(const apar_config* cfg /*[host]*/, apar_ctx** out /*[host]*/);
 /* The same bookkeeping without a device (the paper has no counterpart): k_pool, v_pool and
  * workspace are ignored, no CUDA call is made, nothing is ever launched.  apar_new_threads,
- * apar_fork, apar_append_kv (row pointers may be NULL), apar_release, the paragraph calls and
+ * apar_fork, apar_append_kv (row pointers may be NULL), apar_release, apar_reorder, apar_evict (which
+ * needs no weights here), the paragraph calls and
  * all introspection work as documented and hand out the same ids as a device context would;
  * every attention call and apar_decode_step return APAR_ERR_UNSUPPORTED.  For schedulers that
  * want to try an admission decision (will this fork or append fit?) on a copy of the state,
@@ -463,6 +464,79 @@ apar_status apar_rope(const apar_rope_config* cfg /*[host]*/, int32_t n,
                       int64_t q_out_stride, int32_t num_kv_heads, const void* k /*[device]*/,
                       int64_t k_stride, void* k_out /*[device]*/, int64_t k_out_stride,
                       void* cuda_stream);
+
+/* Threads go on from other threads' chains (the paper has no counterpart: beam search reorders its
+ * beams after every selection).  After the call thread tid[i] holds the chain that source_tid[i]
+ * held before it, for all i at once; ids stay as they are.  Sources need not be listed themselves;
+ * one that is not keeps its chain.  Full blocks are shared as after apar_fork.  A chain's partial
+ * last block stays with the chain's own thread if that goes on with it or is not listed, else
+ * with the first entry that goes on with the chain; every other one gets a copy of its rows.  A
+ * chain that no thread goes on with is given back as by apar_release.  Entries with tid[i] ==
+ * source_tid[i] cost nothing.  Blocks for copies are taken in index order, before any is given back.
+ * tids distinct; not for threads of a paragraph tree.  A call that copies cannot be captured.
+ * apar_append_kv_layer does not replay an append that came before it.
+ * Errors: BAD_THREAD, INVALID_ARG, NO_BLOCKS (needs one block per copy), WORKSPACE_TOO_SMALL, CUDA. */
+apar_status apar_reorder(apar_ctx* ctx, int32_t n, const int32_t* tid /*[host]*/,
+                         const int32_t* source_tid /*[host]*/, void* cuda_stream);
+
+/* Accumulated attention weights (the paper has no counterpart; schedulers that keep a cache small
+ * drop the rows that attention hardly looks at).  With memory attached a context holds a float per
+ * cached row, layer and kv head, which lies with the row's block: an appended row starts at 0, a row
+ * that a fork, apar_reorder or apar_accept_candidates copies or moves takes its weight along, and
+ * threads that share a block share its rows' weights.  bf16 pools only: UNSUPPORTED otherwise.
+ *   Bytes: the weights, float [num_layers][num_blocks][num_kv_heads][16], then areas of the
+ *   library's own.  The caller owns the memory and may read and write the weights on the context's
+ *   stream; those of rows that are cached when it is attached are what the memory holds. */
+size_t apar_weights_bytes(const apar_config* cfg /*[host]*/);
+/* memory [device] 256-byte aligned, or NULL to detach.
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE_TOO_SMALL. */
+apar_status apar_attach_weights(apar_ctx* ctx, void* memory /*[device] or NULL*/, size_t bytes);
+/* From now on every attention call of this context also writes lse [device] float
+ * [queries][num_q_heads]: the natural logarithm of each row's softmax denominator, sum over the keys
+ * it sees of exp(sm_scale * <q, k>).  NULL turns it off.  bf16 pools only.  Results are unchanged.
+ * Errors: INVALID_ARG, UNSUPPORTED. */
+apar_status apar_set_lse_output(apar_ctx* ctx, float* lse /*[device] or NULL*/);
+/* Adds the weights of the most recent decode attention (apar_tree_decode_attention, apar_decode_step,
+ * their layer forms, or apar_tree_prefix_attention): for every key that one of its queries saw, and
+ * every kv head,
+ *     w (+)= sum over those queries and the heads of the group of exp(sm_scale * <q, k> - lse).
+ * K is read once for all queries that share it, V not at all.  replace != 0: the sum takes the place of
+ * the old weight (of the keys seen; others keep theirs).  Sums are in 32 bits in a fixed order.
+ *   q [device] bf16 [n][num_q_heads][128], 16-byte aligned, lse [device] float [n][num_q_heads]: of that
+ *   call and layer, its queries in its order.
+ * The first call after an attention call that made a plan of its own uploads one too; others launch
+ * one kernel and can be captured.
+ * Errors: INVALID_ARG (also: no memory attached, bookkeeping since that attention call, a
+ * verification, an upload while the stream is capturing), UNSUPPORTED, WORKSPACE_TOO_SMALL, CUDA. */
+apar_status apar_add_weights(apar_ctx* ctx, int32_t layer, const void* q /*[device]*/,
+                             const float* lse /*[device]*/, float sm_scale, int32_t replace,
+                             void* cuda_stream);
+/* Weights of rows begin[i] .. begin[i] + count[i] - 1 of thread tid[i]'s chain, entries one after the
+ * other: out [device] float [sum count][num_kv_heads].  A thread may be listed several times.
+ * Uses the staging buffers, so it cannot be captured.
+ * Errors: INVALID_ARG, BAD_THREAD, UNSUPPORTED, CUDA. */
+apar_status apar_read_weights(apar_ctx* ctx, int32_t layer, int32_t n, const int32_t* tid /*[host]*/,
+                              const int32_t* begin /*[host]*/, const int32_t* count /*[host]*/,
+                              float* out /*[device]*/, void* cuda_stream);
+/* Eviction by accumulated weight.  Of the rows begin[i] .. end[i] - 1 of thread tid[i]'s chain keep[i]
+ * stay, in every layer and for every kv head on its own: those with the largest weights (a NaN counts
+ * as the largest; of equal weights the earlier row).  They become rows begin[i] .. begin[i] +
+ * keep[i] - 1, K, V and weight: a row that lies there already stays where it is, the others take the
+ * free places in order.  (Attention does not depend on the order of keys; positions are in the keys.)
+ * Rows from end[i] on follow them, in their blocks; the thread is end - begin - keep rows shorter.
+ *   begin[i] is a multiple of 16.  If rows follow, so are end[i] and keep[i].
+ *   Blocks shared by several threads: threads listed with the same blocks (and then the same begin,
+ *   end and keep) share the kept rows afterwards; keep has to be a multiple of 16 for them.  Where a
+ *   thread that is not listed holds one of the blocks, the kept rows are copied to new blocks, and the
+ *   stretch has to end with the thread; that thread keeps all of its rows.  Otherwise rows move
+ *   inside the stretch, and blocks left over are given back in table order.
+ * tids distinct; not for threads of a paragraph tree.  Uses the staging buffers, so it cannot be
+ * captured.  apar_append_kv_layer does not replay an append that came before it.
+ * Errors: INVALID_ARG (also: no memory attached), BAD_THREAD, NO_BLOCKS, UNSUPPORTED,
+ * WORKSPACE_TOO_SMALL, CUDA. */
+apar_status apar_evict(apar_ctx* ctx, int32_t n, const int32_t* tid /*[host]*/,
+                       const int32_t* begin /*[host]*/, const int32_t* end /*[host]*/,
+                       const int32_t* keep /*[host]*/, void* cuda_stream);
 
 /* Beam search's selection (the paper has no counterpart: its threads sample greedily).  A sequence
  * is decoded by num_beams beams; a pair (b, v) of a beam and a token has the value

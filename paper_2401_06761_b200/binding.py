@@ -86,6 +86,15 @@ _SIGS = {
     "apar_rope": (C.c_int32, [C.POINTER(apar_rope_config), C.c_int32, C.c_void_p, C.c_int32,
                               C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p,
                               C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]),
+    "apar_reorder": (C.c_int32, [_ctx, C.c_int32, _i32p, _i32p, C.c_void_p]),
+    "apar_weights_bytes": (C.c_size_t, [_cfgp]),
+    "apar_attach_weights": (C.c_int32, [_ctx, C.c_void_p, C.c_size_t]),
+    "apar_set_lse_output": (C.c_int32, [_ctx, C.c_void_p]),
+    "apar_add_weights": (C.c_int32, [_ctx, C.c_int32, C.c_void_p, C.c_void_p, C.c_float, C.c_int32,
+                                     C.c_void_p]),
+    "apar_read_weights": (C.c_int32, [_ctx, C.c_int32, C.c_int32, _i32p, _i32p, _i32p, C.c_void_p,
+                                      C.c_void_p]),
+    "apar_evict": (C.c_int32, [_ctx, C.c_int32, _i32p, _i32p, _i32p, _i32p, C.c_void_p]),
     "apar_beam_workspace_bytes": (C.c_size_t, [C.POINTER(apar_beam_config), C.c_int32]),
     "apar_beam_select": (C.c_int32, [C.POINTER(apar_beam_config), C.c_int32, C.c_void_p, C.c_int64,
                                      C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
@@ -325,6 +334,46 @@ def apar_rope(cfg: apar_rope_config, n: int, positions: int, num_q_heads: int, q
               k_stride: int, k_out: int, k_out_stride: int, stream=0):
     _check(lib.apar_rope(C.byref(cfg), n, positions, num_q_heads, q, q_stride, q_out, q_out_stride,
                          num_kv_heads, k, k_stride, k_out, k_out_stride, stream))
+
+
+def _lists(tid, *others):
+    """(n, arrays): lists that have exactly one entry for each thread."""
+    tids, n = _arr(tid)
+    out = [tids]
+    for xs in others:
+        buf, m = _arr(xs)
+        if m != n:
+            raise AparError(APAR_ERR_INVALID_ARG)
+        out.append(buf)
+    return (n, *out)
+
+
+def apar_reorder(ctx, tid, source_tid, stream=0):
+    _check(lib.apar_reorder(ctx, *_lists(tid, source_tid), stream))
+
+
+def apar_weights_bytes(cfg: apar_config) -> int:
+    return lib.apar_weights_bytes(C.byref(cfg))
+
+
+def apar_attach_weights(ctx, memory: int, nbytes: int):
+    _check(lib.apar_attach_weights(ctx, memory or None, nbytes))
+
+
+def apar_set_lse_output(ctx, lse: int):
+    _check(lib.apar_set_lse_output(ctx, lse or None))
+
+
+def apar_add_weights(ctx, layer: int, q: int, lse: int, sm_scale: float, replace: bool, stream=0):
+    _check(lib.apar_add_weights(ctx, layer, q, lse, sm_scale, int(bool(replace)), stream))
+
+
+def apar_read_weights(ctx, layer: int, tid, begin, count, out: int, stream=0):
+    _check(lib.apar_read_weights(ctx, layer, *_lists(tid, begin, count), out, stream))
+
+
+def apar_evict(ctx, tid, begin, end, keep, stream=0):
+    _check(lib.apar_evict(ctx, *_lists(tid, begin, end, keep), stream))
 
 
 def make_beam_config(vocab, num_beams, num_select, logits_type="bfloat16", eos=None):

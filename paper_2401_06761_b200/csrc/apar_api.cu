@@ -71,6 +71,26 @@ Layout make_layout(const apar_config* c) {
   return L;
 }
 
+struct WeightsLayout {     // partition of the memory of apar_attach_weights
+  size_t moves, counts, units, users, total;
+  int64_t unit_cap, user_cap;
+};
+
+WeightsLayout make_weights_layout(const apar_config* c) {
+  WeightsLayout L;
+  const size_t rows = (size_t)std::max(1, c->num_layers) * c->num_blocks * c->num_kv_heads * kBlock;
+  size_t off = align_up(rows * sizeof(float), 256);
+  auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes, 256); return o; };
+  L.moves = take(rows * sizeof(int2));                  // (no more rows stay than there are)
+  L.counts = take((size_t)c->max_threads * std::max(1, c->num_layers) * c->num_kv_heads * 4);
+  L.unit_cap = c->num_blocks;                           // (no block is in two units)
+  L.user_cap = (int64_t)c->max_threads * 16 + 4096;
+  L.units = take((size_t)L.unit_cap * sizeof(KeyUnit));
+  L.users = take((size_t)L.user_cap * sizeof(KeyUser));
+  L.total = off;
+  return L;
+}
+
 struct ThreadRec {
   int32_t tid = -1;       // -1: slot free
   int32_t len = 0;
@@ -148,6 +168,14 @@ struct apar_ctx {
   bool track_runs = true;                     // false: tables were filled in directly
   bool plan_by_runs = true;                   // APAR_PLANNER=tables (testing): walk block ids
   cudaEvent_t time_start = nullptr, time_stop = nullptr;   // caller's events around the kernels
+  float* lse_out = nullptr;                   // caller's array for the softmax's log denominators
+  // ---- accumulated weights (apar_attach_weights)
+  char* weights = nullptr;                    // [num_layers][num_blocks][num_kv_heads][16] floats, then
+  WeightsLayout wlay;                         // the areas below
+  struct Seen { int32_t slot, lim; };         // queries of the last attention call; lim < 0: whole chain
+  std::vector<Seen> seen;
+  bool seen_valid = false, key_plan_valid = false;   // (they describe / the units on the device are of)
+  int32_t n_key_units = 0;                           // that call
   // thread list of the most recent apar_decode_step; its table rows are resident on the device
   std::vector<int32_t> step_tids, step_slots, tmp_slots;
   bool step_valid = false;
@@ -160,6 +188,7 @@ struct apar_ctx {
 
   int32_t* row(int slot) { return tables.data() + (size_t)slot * cfg.max_blocks_per_thread; }
   char* ws(size_t off) { return (char*)cfg.workspace + off; }
+  size_t layer_weights() const { return (size_t)cfg.num_blocks * cfg.num_kv_heads * kBlock; }
 };
 
 namespace {
@@ -385,6 +414,7 @@ apar_status launch_plan(apar_ctx* c, int layer, const void* q, void* out, float 
   a.part_ml = (float2*)c->ws(c->lay.part_ml);
   a.shape = c->shape;
   a.scale_log2e = sm_scale * 1.4426950408889634f;
+  a.lse = c->lse_out;
   if (!c->q4) {
     a.tm_k = &c->tm_k[layer];
     a.tm_v = &c->tm_v[layer];
@@ -509,6 +539,12 @@ apar_status run_attention(apar_ctx* c, int n, const int32_t* qslots, const int32
 
   const bool cacheable = tids != nullptr && !has_dups && !qlens;
   bool reuse = cacheable && plan_reusable(c, n, tids, attended);
+  if (c->weights && !(reuse && c->seen_valid)) {        // (a reused plan is of the same queries)
+    c->seen.resize(n);
+    for (int i = 0; i < n; ++i) c->seen[i] = {qslots[i], qlens ? qlens[i] : -1};
+    c->seen_valid = !verify;
+    c->key_plan_valid = false;
+  }
   c->last.attn_plan_host_us = 0;
   if (!tables_in_sync) c->last.attn_upload_bytes = 0;   // (else the caller's uploads count too)
   if (!reuse) {
@@ -633,6 +669,115 @@ apar_status run_attention(apar_ctx* c, int n, const int32_t* qslots, const int32
   c->last.attn_vec_items = p.n_vec;
   c->last.attn_mma_items = p.n_mma;
   return APAR_OK;
+}
+
+// New rows have received no weight yet, a copied row what its original has (every layer at once).
+apar_status clear_weights(apar_ctx* c, const int32_t* d_slots, int n_rows, cudaStream_t st) {
+  if (!c->weights || n_rows <= 0) return APAR_OK;
+  APAR_CUDA(c, launch_weights_clear((float*)c->weights, c->layer_weights(), c->num_layers, d_slots,
+                                    n_rows, c->cfg.num_kv_heads, st));
+  ++c->kernels_total;
+  return APAR_OK;
+}
+apar_status copy_weights(apar_ctx* c, const CowCopy* d_copies, int n, cudaStream_t st) {
+  if (!c->weights) return APAR_OK;
+  APAR_CUDA(c, launch_weights_cow((float*)c->weights, c->layer_weights(), c->num_layers, d_copies, n,
+                                  c->cfg.num_kv_heads, st));
+  ++c->kernels_total;
+  return APAR_OK;
+}
+
+// Calls that use the staging buffers cannot be captured.
+apar_status refuse_capture(apar_ctx* c, cudaStream_t st) {
+  cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+  APAR_CUDA(c, cudaStreamIsCapturing(st, &cap));
+  return cap == cudaStreamCaptureStatusNone ? APAR_OK : APAR_ERR_INVALID_ARG;
+}
+
+apar_status upload(apar_ctx* c, const void* src, size_t bytes, char* dst, cudaStream_t st) {
+  size_t done = 0;
+  while (done < bytes) {
+    Staging* s;
+    apar_status rc = acquire(c, &s);
+    if (rc) return rc;
+    const size_t chunk = std::min(bytes - done, c->ring_bytes);
+    memcpy(s->host, (const char*)src + done, chunk);
+    rc = send(c, s, dst + done, chunk, st);
+    if (rc) return rc;
+    done += chunk;
+  }
+  return APAR_OK;
+}
+
+// Cuts the runs into units of at most `chunk` keys, longest first, and sends both lists.
+apar_status send_key_plan(apar_ctx* c, const std::vector<KeyRun>& runs, const std::vector<KeyUser>& users,
+                          int chunk, std::vector<KeyUnit>* units, cudaStream_t st) {
+  units->clear();
+  for (const KeyRun& r : runs) {
+    const bool open = r.tok_end < 0;
+    const int end = open ? r.tok_begin - r.tok_end - 1 : r.tok_end;
+    for (int t = r.tok_begin; t < end; t += chunk) {
+      const bool last = t + chunk >= end;
+      units->push_back(KeyUnit{r.table_row, t, last && open ? -(end - t) - 1 : std::min(end, t + chunk),
+                               r.user_begin, r.n_users, {0, 0, 0}});
+    }
+  }
+  if ((int64_t)units->size() > c->wlay.unit_cap || (int64_t)users.size() > c->wlay.user_cap)
+    return APAR_ERR_WORKSPACE_TOO_SMALL;
+  auto cost = [](const KeyUnit& u) {
+    const int64_t keys = u.tok_end < 0 ? -u.tok_end - 1 : u.tok_end - u.tok_begin;
+    return keys * (1 + u.n_users);
+  };
+  std::stable_sort(units->begin(), units->end(),
+                   [&](const KeyUnit& a, const KeyUnit& b) { return cost(a) > cost(b); });
+  apar_status rc = upload(c, units->data(), units->size() * sizeof(KeyUnit), c->weights + c->wlay.units, st);
+  if (rc == APAR_OK)
+    rc = upload(c, users.data(), users.size() * sizeof(KeyUser), c->weights + c->wlay.users, st);
+  return rc;
+}
+
+KeyArgs key_args(apar_ctx* c, int layer, const void* q, const float* lse, float sm_scale, int replace) {
+  KeyArgs a;
+  a.q = q;
+  a.lse = lse;
+  a.k_pool = (const char*)c->cfg.k_pool + (size_t)layer * c->layer_bytes;
+  a.weights = (float*)c->weights + (size_t)layer * c->layer_weights();
+  a.d_tables = (const int32_t*)c->ws(c->lay.tables);
+  a.d_lens = (const int32_t*)c->ws(c->lay.lens);
+  a.units = (const KeyUnit*)(c->weights + c->wlay.units);
+  a.users = (const KeyUser*)(c->weights + c->wlay.users);
+  a.shape = c->shape;
+  a.scale_log2e = sm_scale * 1.4426950408889634f;
+  a.replace = replace != 0;
+  a.num_sms = c->num_sms;
+  return a;
+}
+
+// Every thread that lists group `gid` lists it as two groups from now on, cut at table position `pos`
+// (all see it at the same positions).  Nothing happens where `pos` is an end of the group.
+void split_group(apar_ctx* c, int32_t gid, int32_t pos) {
+  int32_t rest = -1;
+  for (std::vector<BlockRun>& rs : c->runs)
+    for (size_t k = 0; k < rs.size(); ++k) {
+      if (rs[k].gid != gid) continue;
+      const int32_t first = pos - rs[k].pos;
+      if (first <= 0 || first >= rs[k].n) return;
+      if (rest < 0) {
+        rest = new_gid(c);
+        c->gid_ref[rest] = c->gid_ref[gid];
+      }
+      const BlockRun second{rest, pos, rs[k].n - first};
+      rs[k].n = first;
+      rs.insert(rs.begin() + k + 1, second);
+      break;
+    }
+}
+void split_groups_of(apar_ctx* c, int slot, int32_t pos) {
+  for (const BlockRun& r : c->runs[slot])
+    if (r.pos < pos && pos < r.pos + r.n) {
+      split_group(c, r.gid, pos);
+      return;
+    }
 }
 
 apar_status create_impl(const apar_config* cfg, bool external, bool host_only, int32_t kv_format,
@@ -859,6 +1004,7 @@ apar_status apar_fork(apar_ctx* c, int32_t n, const int32_t* parent_tid, int32_t
                         c->cfg.num_kv_heads, st));
       ++c->kernels_total;
     }
+    return copy_weights(c, (const CowCopy*)d_stage, nc, st);
   }
   return APAR_OK;
 }
@@ -908,10 +1054,11 @@ apar_status apar_append_kv(apar_ctx* c, int32_t n, const int32_t* tid, const int
     APAR_CUDA(c, scatter(c->cfg.k_pool, c->cfg.v_pool, k_new, v_new, (const int32_t*)d_stage,
                          first_row, (int)filled, c->cfg.num_kv_heads, st));
     ++c->kernels_total;
+    rc = clear_weights(c, (const int32_t*)d_stage, (int)filled, st);
     first_row += (int64_t)filled;
     filled = 0;
     stg = nullptr;
-    return APAR_OK;
+    return rc;
   };
   for (int i = 0; i < n; ++i) {
     const int s = slot_of(c, tid[i]);
@@ -1074,6 +1221,8 @@ apar_status apar_decode_step(apar_ctx* c, int32_t n, const int32_t* tid, const v
   APAR_CUDA(c, scatter(c->cfg.k_pool, c->cfg.v_pool, k_new, v_new,
                        (const int32_t*)c->ws(c->lay.slot_map), 0, n, c->cfg.num_kv_heads, st));
   c->kernels_total += 2;
+  rc = clear_weights(c, (const int32_t*)c->ws(c->lay.slot_map), n, st);
+  if (rc) return rc;
   return run_attention(c, n, sl, tid, false, q, out, sm_scale, st, nullptr, true);
 }
 
@@ -1299,6 +1448,13 @@ apar_status apar_accept_candidates(apar_ctx* c, int32_t n, const int32_t* tid,
                         c->cfg.num_kv_heads, st));
       ++c->kernels_total;
     }
+    if (c->weights) {
+      APAR_CUDA(c, launch_weights_move((float*)c->weights, c->layer_weights(), c->num_layers,
+                                       (const RowMove*)d_stage,
+                                       (const int32_t*)(d_stage + (size_t)n_moves * sizeof(RowMove)),
+                                       (int)ng, c->cfg.num_kv_heads, st));
+      ++c->kernels_total;
+    }
   }
   return APAR_OK;
 }
@@ -1378,6 +1534,7 @@ apar_status apar_tree_prefill_attention(apar_ctx* c, int32_t layer, int32_t n,
   a.part_ml = nullptr;
   a.shape = c->shape;
   a.scale_log2e = sm_scale * 1.4426950408889634f;
+  a.lse = c->lse_out;
   a.tm_k = &c->tm_k[layer];
   a.tm_v = &c->tm_v[layer];
   a.d_error = (int*)c->ws(c->lay.err);
@@ -1533,6 +1690,401 @@ apar_status apar_read_kv(apar_ctx* c, int32_t layer, int32_t n, const int32_t* t
     ++c->kernels_total;
     first_row += filled;
   }
+  return APAR_OK;
+}
+
+apar_status apar_reorder(apar_ctx* c, int32_t n, const int32_t* tid, const int32_t* source_tid,
+                         void* cuda_stream) {
+  if (!c || n < 0 || (n > 0 && (!tid || !source_tid))) return APAR_ERR_INVALID_ARG;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  for (int i = 0; i < n; ++i)
+    if (slot_of(c, tid[i]) < 0 || slot_of(c, source_tid[i]) < 0) return APAR_ERR_BAD_THREAD;
+  const uint32_t mk = next_mark(c);
+  for (int i = 0; i < n; ++i) {
+    const int s = slot_of(c, tid[i]);
+    if (c->mark[s] == mk || c->cur_node[tid[i]] >= 0 || c->cur_node[source_tid[i]] >= 0)
+      return APAR_ERR_INVALID_ARG;
+    c->mark[s] = mk;
+  }
+  // Every chain that somebody goes on with keeps its table row: with its own thread if that goes on
+  // with it or is not listed, else with the first thread that does ("heir").  The other threads
+  // become forks of it in the rows of the chains that nobody goes on with.
+  std::vector<int32_t> row_of(n, -1);            // table row each listed thread has afterwards
+  std::vector<int32_t> dropped, heir(c->slots.size(), -1);
+  for (int i = 0; i < n; ++i)
+    if (tid[i] == source_tid[i]) heir[slot_of(c, tid[i])] = row_of[i] = slot_of(c, tid[i]);
+  for (int i = 0; i < n; ++i) {
+    const int p = slot_of(c, source_tid[i]);
+    if (c->mark[p] == mk && heir[p] < 0) heir[p] = row_of[i] = p;
+  }
+  int64_t need = 0, forks = 0;
+  for (int i = 0; i < n; ++i) {
+    if (heir[slot_of(c, tid[i])] < 0) dropped.push_back(slot_of(c, tid[i]));
+    if (row_of[i] >= 0) continue;
+    ++forks;
+    if (c->slots[slot_of(c, source_tid[i])].len % kBlock) ++need;
+  }
+  bool same = forks == 0;
+  for (int i = 0; i < n && same; ++i) same = tid[i] == source_tid[i];
+  if (same) return APAR_OK;
+  if (need > (int64_t)c->free_stack.size()) return APAR_ERR_NO_BLOCKS;
+  if ((size_t)need * sizeof(CowCopy) > c->lay.stage_cap) return APAR_ERR_WORKSPACE_TOO_SMALL;
+  Staging* stg = nullptr;
+  if (need && !c->host_only) {
+    apar_status rc = refuse_capture(c, st);
+    if (rc) return rc;
+    rc = acquire(c, &stg);
+    if (rc) return rc;
+  }
+  CowCopy* copies = stg ? (CowCopy*)stg->host : nullptr;
+  // what the dropped rows held, to be given back at the end
+  std::vector<std::vector<int32_t>> old_blocks(dropped.size());
+  std::vector<BlockRun> old_runs;
+  for (size_t d = 0; d < dropped.size(); ++d) {
+    const int s = dropped[d];
+    old_blocks[d].assign(c->row(s), c->row(s) + c->slots[s].n_blocks);
+    old_runs.insert(old_runs.end(), c->runs[s].begin(), c->runs[s].end());
+    c->runs[s].clear();
+    c->own_open[s] = 0;
+  }
+  int nc = 0;
+  size_t used = 0;
+  for (int i = 0; i < n; ++i) {
+    if (row_of[i] >= 0) continue;
+    const int ps = slot_of(c, source_tid[i]), cs = dropped[used++];
+    const int32_t L = c->slots[ps].len, full = L / kBlock, r = L % kBlock;
+    ThreadRec& ch = c->slots[cs];
+    int32_t* ct = c->row(cs);
+    const int32_t* pt = c->row(ps);
+    for (int b = 0; b < full; ++b) {
+      ct[b] = pt[b];
+      ++c->refcnt[pt[b]];
+    }
+    ch.n_blocks = full;
+    run_fork(c, ps, cs, full);
+    if (r) {
+      const int32_t dst = alloc_block(c);
+      if (copies) copies[nc] = CowCopy{pt[full], dst, r, 0};
+      ++nc;
+      ct[full] = dst;
+      ch.n_blocks = full + 1;
+      run_add_block(c, cs, full);
+    }
+    ch.len = L;
+    ch.synced = 0;
+    ch.dev_len = -1;
+    row_of[i] = cs;
+  }
+  for (int i = 0; i < n; ++i) {
+    c->tid_slot[tid[i]] = row_of[i];
+    c->slots[row_of[i]].tid = tid[i];
+  }
+  for (const std::vector<int32_t>& blocks : old_blocks)
+    for (int32_t b : blocks)
+      if (--c->refcnt[b] == 0) c->free_stack.push_back(b);
+  for (const BlockRun& r : old_runs)
+    if (--c->gid_ref[r.gid] == 0) c->gid_free.push_back(r.gid);
+  ++c->struct_epoch;
+  ++c->book_seq;
+  ++c->mod_seq;
+  ++c->life_seq;
+  c->last_append_rows = -1;
+  if (nc && !c->host_only) {
+    char* d_stage = c->ws(c->lay.stage);
+    apar_status rc = send(c, stg, d_stage, (size_t)nc * sizeof(CowCopy), st);
+    if (rc) return rc;
+    for (int l = 0; l < c->num_layers; ++l) {
+      auto copy = c->q4 ? launch_q4_cow_copy : launch_cow_copy;
+      APAR_CUDA(c, copy((char*)c->cfg.k_pool + l * c->layer_bytes,
+                        (char*)c->cfg.v_pool + l * c->layer_bytes, (const CowCopy*)d_stage, nc,
+                        c->cfg.num_kv_heads, st));
+      ++c->kernels_total;
+    }
+    return copy_weights(c, (const CowCopy*)d_stage, nc, st);
+  }
+  return APAR_OK;
+}
+
+size_t apar_weights_bytes(const apar_config* cfg) {
+  return supported(cfg) ? make_weights_layout(cfg).total : 0;
+}
+
+apar_status apar_attach_weights(apar_ctx* c, void* memory, size_t bytes) {
+  if (!c || ((uintptr_t)memory & 255)) return APAR_ERR_INVALID_ARG;
+  if (c->host_only || c->q4) return APAR_ERR_UNSUPPORTED;
+  c->wlay = make_weights_layout(&c->cfg);
+  if (memory && bytes < c->wlay.total) return APAR_ERR_WORKSPACE_TOO_SMALL;
+  c->weights = (char*)memory;
+  c->seen_valid = c->key_plan_valid = false;
+  return APAR_OK;
+}
+
+apar_status apar_set_lse_output(apar_ctx* c, float* lse) {
+  if (!c || ((uintptr_t)lse & 3)) return APAR_ERR_INVALID_ARG;
+  if (c->host_only || c->q4) return APAR_ERR_UNSUPPORTED;
+  c->lse_out = lse;
+  return APAR_OK;
+}
+
+apar_status apar_add_weights(apar_ctx* c, int32_t layer, const void* q, const float* lse,
+                             float sm_scale, int32_t replace, void* cuda_stream) {
+  if (!c || layer < 0 || layer >= c->num_layers || !q || !lse || ((uintptr_t)q & 15) ||
+      ((uintptr_t)lse & 3))
+    return APAR_ERR_INVALID_ARG;
+  if (c->host_only || c->q4) return APAR_ERR_UNSUPPORTED;
+  // the queries are those of the most recent attention call, whose tables the device still holds
+  if (!c->weights || !c->seen_valid || c->attn_book_seq != c->book_seq) return APAR_ERR_INVALID_ARG;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  if (!c->key_plan_valid) {
+    apar_status rc = refuse_capture(c, st);
+    if (rc) return rc;
+    std::vector<KeyQuery> qs(c->seen.size());
+    for (size_t i = 0; i < qs.size(); ++i) {
+      const auto& x = c->seen[i];
+      const bool whole = x.lim < 0;
+      qs[i] = KeyQuery{c->row(x.slot), x.slot, whole ? c->slots[x.slot].len : x.lim, whole,
+                       KeyUser{(int32_t)i, whole ? INT32_MAX : x.lim, 1, 0}};
+    }
+    std::vector<KeyRun> runs;
+    std::vector<KeyUser> users;
+    if (!c->planner.key_runs(qs.data(), (int)qs.size(), &runs, &users)) return APAR_ERR_INVALID_ARG;
+    // units of even length, some four to a warp of the machine where there is that much
+    int64_t keys = 0;
+    for (const KeyRun& r : runs) keys += r.tok_end < 0 ? -r.tok_end - 1 : r.tok_end - r.tok_begin;
+    const int64_t share = keys * c->cfg.num_kv_heads / ((int64_t)c->num_sms * 64);
+    int64_t chunk = std::min<int64_t>(1024, std::max<int64_t>(64, (share + 15) / 16 * 16));
+    std::vector<KeyUnit> units;
+    rc = send_key_plan(c, runs, users, (int)chunk, &units, st);
+    if (rc) return rc;
+    c->n_key_units = (int32_t)units.size();
+    c->key_plan_valid = true;
+  }
+  APAR_CUDA(c, launch_key_weights(key_args(c, layer, q, lse, sm_scale, replace), c->n_key_units, st));
+  ++c->kernels_total;
+  return APAR_OK;
+}
+
+apar_status apar_read_weights(apar_ctx* c, int32_t layer, int32_t n, const int32_t* tid,
+                              const int32_t* begin, const int32_t* count, float* out,
+                              void* cuda_stream) {
+  if (!c || n < 0 || layer < 0 || layer >= c->num_layers || (n > 0 && (!tid || !begin || !count)))
+    return APAR_ERR_INVALID_ARG;
+  if (c->host_only || c->q4) return APAR_ERR_UNSUPPORTED;
+  if (!c->weights) return APAR_ERR_INVALID_ARG;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  std::vector<int32_t> slots(n);
+  std::vector<RowRange> ranges;
+  int64_t rows = 0;
+  for (int i = 0; i < n; ++i) {
+    const int s = slot_of(c, tid[i]);
+    if (s < 0) return APAR_ERR_BAD_THREAD;
+    if (begin[i] < 0 || count[i] < 0 || (int64_t)begin[i] + count[i] > c->slots[s].len)
+      return APAR_ERR_INVALID_ARG;
+    slots[i] = s;
+    if (count[i]) ranges.push_back(RowRange{s, begin[i], count[i], 0, rows});
+    rows += count[i];
+  }
+  if (rows == 0) return APAR_OK;
+  if (!out || ((uintptr_t)out & 3)) return APAR_ERR_INVALID_ARG;
+  apar_status rc = refuse_capture(c, st);
+  if (rc) return rc;
+  rc = sync_device_tables(c, slots.data(), n, st);
+  if (rc) return rc;
+  const size_t per_pass = c->lay.stage_cap / sizeof(RowRange);
+  for (size_t i = 0; i < ranges.size(); i += per_pass) {
+    const int m = (int)std::min(per_pass, ranges.size() - i);
+    int max_count = 0;
+    for (int j = 0; j < m; ++j) max_count = std::max(max_count, ranges[i + j].count);
+    char* d_stage = c->ws(c->lay.stage);
+    rc = upload(c, ranges.data() + i, (size_t)m * sizeof(RowRange), d_stage, st);
+    if (rc) return rc;
+    APAR_CUDA(c, launch_weights_read((const float*)c->weights + (size_t)layer * c->layer_weights(),
+                                     (const int32_t*)c->ws(c->lay.tables), c->cfg.max_blocks_per_thread,
+                                     (const RowRange*)d_stage, m, max_count, c->cfg.num_kv_heads, out, st));
+    ++c->kernels_total;
+  }
+  return APAR_OK;
+}
+
+apar_status apar_evict(apar_ctx* c, int32_t n, const int32_t* tid, const int32_t* begin,
+                       const int32_t* end, const int32_t* keep, void* cuda_stream) {
+  if (!c || n < 0 || (n > 0 && (!tid || !begin || !end || !keep))) return APAR_ERR_INVALID_ARG;
+  if (c->q4) return APAR_ERR_UNSUPPORTED;
+  if (!c->weights && !c->host_only) return APAR_ERR_INVALID_ARG;   // (the bookkeeping needs none)
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  for (int i = 0; i < n; ++i)
+    if (slot_of(c, tid[i]) < 0) return APAR_ERR_BAD_THREAD;
+  const uint32_t mk = next_mark(c);
+  for (int i = 0; i < n; ++i) {
+    const int s = slot_of(c, tid[i]);
+    const int32_t len = c->slots[s].len;
+    if (c->mark[s] == mk || c->cur_node[tid[i]] >= 0) return APAR_ERR_INVALID_ARG;
+    c->mark[s] = mk;
+    if (begin[i] < 0 || begin[i] % kBlock || end[i] < begin[i] || end[i] > len || keep[i] < 0 ||
+        keep[i] > end[i] - begin[i])
+      return APAR_ERR_INVALID_ARG;
+    // rows behind the stretch stay in their blocks
+    if (end[i] < len && (end[i] % kBlock || keep[i] % kBlock)) return APAR_ERR_INVALID_ARG;
+  }
+  // Stretches: threads that list the same blocks share one.
+  struct Stretch { int32_t first, members, in_place, new_blocks; };
+  std::vector<Stretch> st_list;
+  std::vector<int32_t> stretch_of(n, -1), owner;         // owner: by block, 1 + stretch
+  auto blocks_of = [](int32_t rows) { return (rows + kBlock - 1) / kBlock; };
+  owner.assign(c->cfg.num_blocks, 0);
+  for (int i = 0; i < n; ++i) {
+    if (keep[i] == end[i] - begin[i]) continue;          // nothing goes
+    const int32_t* tab = c->row(slot_of(c, tid[i]));
+    const int b0 = begin[i] / kBlock, b1 = blocks_of(end[i]);
+    const int32_t o = owner[tab[b0]];
+    if (o) {
+      const int f = st_list[o - 1].first;
+      const int32_t* ftab = c->row(slot_of(c, tid[f]));
+      if (begin[f] != begin[i] || end[f] != end[i] || keep[f] != keep[i] ||
+          memcmp(ftab + b0, tab + b0, (size_t)(b1 - b0) * 4))
+        return APAR_ERR_INVALID_ARG;
+      ++st_list[o - 1].members;
+      stretch_of[i] = o - 1;
+      continue;
+    }
+    for (int b = b0; b < b1; ++b) {
+      if (owner[tab[b]]) return APAR_ERR_INVALID_ARG;    // overlaps another stretch in part
+      owner[tab[b]] = (int32_t)st_list.size() + 1;
+    }
+    stretch_of[i] = (int32_t)st_list.size();
+    st_list.push_back(Stretch{i, 1, 1, 0});
+  }
+  int64_t need = 0;
+  for (Stretch& x : st_list) {
+    const int f = x.first;
+    const int32_t* tab = c->row(slot_of(c, tid[f]));
+    for (int b = begin[f] / kBlock; b < blocks_of(end[f]); ++b)
+      if (c->refcnt[tab[b]] != x.members) x.in_place = 0;
+    if (x.members > 1 && keep[f] % kBlock) return APAR_ERR_INVALID_ARG;   // a partial block is one thread's
+    if (!x.in_place) {
+      x.new_blocks = blocks_of(keep[f]);
+      need += x.new_blocks;
+    }
+  }
+  for (int i = 0; i < n; ++i)                            // others hold the blocks: the rest may not shift
+    if (stretch_of[i] >= 0 && !st_list[stretch_of[i]].in_place && end[i] != c->slots[slot_of(c, tid[i])].len)
+      return APAR_ERR_INVALID_ARG;
+  if (st_list.empty()) return APAR_OK;
+  if (need > (int64_t)c->free_stack.size()) return APAR_ERR_NO_BLOCKS;
+  const size_t b_entries = st_list.size() * sizeof(EvictEntry);
+  if (b_entries + (size_t)need * 4 > c->lay.stage_cap) return APAR_ERR_WORKSPACE_TOO_SMALL;
+  std::vector<int32_t> slots;
+  for (const Stretch& x : st_list) slots.push_back(slot_of(c, tid[x.first]));
+  apar_status rc = APAR_OK;
+  Staging* stg = nullptr;
+  if (!c->host_only) {
+    rc = refuse_capture(c, st);
+    if (rc == APAR_OK) rc = sync_device_tables(c, slots.data(), (int)slots.size(), st);
+    if (rc == APAR_OK) rc = acquire(c, &stg);
+    if (rc) return rc;
+  }
+  std::vector<EvictEntry> entries;
+  std::vector<int32_t> dst;
+  const int lh = c->num_layers * c->cfg.num_kv_heads;
+  int32_t max_rows = 0;
+  int64_t list = 0;
+  std::vector<int32_t> dst_of(st_list.size(), 0);
+  for (size_t k = 0; k < st_list.size(); ++k) {
+    const Stretch& x = st_list[k];
+    const int f = x.first, rows = end[f] - begin[f];
+    dst_of[k] = (int32_t)dst.size();
+    for (int b = 0; b < x.new_blocks; ++b) dst.push_back(alloc_block(c));
+    if (keep[f] == 0) continue;
+    const int32_t cap = x.in_place ? std::min(keep[f], rows - keep[f]) : keep[f];
+    entries.push_back(EvictEntry{slots[k], begin[f], rows, keep[f], x.in_place, dst_of[k], cap, 0, list});
+    list += (int64_t)cap * lh;
+    max_rows = std::max(max_rows, cap);
+  }
+  // ---- tables, groups and lengths
+  for (int i = 0; i < n; ++i) {
+    if (stretch_of[i] < 0) continue;
+    const Stretch& x = st_list[stretch_of[i]];
+    const int s = slot_of(c, tid[i]);
+    ThreadRec& t = c->slots[s];
+    int32_t* tab = c->row(s);
+    const int b0 = begin[i] / kBlock, b1 = blocks_of(end[i]), kb = blocks_of(keep[i]);
+    std::vector<BlockRun>& rs = c->runs[s];
+    const bool first = i == x.first;
+    if (c->track_runs) {
+      if (first) {                                       // (for every thread that lists the blocks)
+        split_groups_of(c, s, b0);
+        if (x.in_place) {
+          split_groups_of(c, s, b0 + kb);
+          split_groups_of(c, s, b1);
+        }
+      }
+      const int32_t gone0 = x.in_place ? b0 + kb : b0;
+      size_t w = 0;
+      for (size_t k = 0; k < rs.size(); ++k) {
+        if (rs[k].pos >= gone0 && rs[k].pos < b1) {
+          if (--c->gid_ref[rs[k].gid] == 0) c->gid_free.push_back(rs[k].gid);
+          if (k + 1 == rs.size()) c->own_open[s] = 0;
+          continue;
+        }
+        rs[w] = rs[k];
+        if (rs[w].pos >= b1) rs[w].pos -= b1 - gone0;
+        ++w;
+      }
+      rs.resize(w);
+    }
+    const int32_t nb_old = t.n_blocks;
+    std::vector<int32_t> gone(tab + (x.in_place ? b0 + kb : b0), tab + b1);
+    if (!x.in_place)
+      for (int b = 0; b < kb; ++b) tab[b0 + b] = dst[dst_of[stretch_of[i]] + b];
+    for (int b = b1; b < nb_old; ++b) tab[b - b1 + b0 + kb] = tab[b];
+    if (!x.in_place && !first)
+      for (int b = 0; b < kb; ++b) ++c->refcnt[tab[b0 + b]];
+    for (int32_t b : gone)
+      if (--c->refcnt[b] == 0) c->free_stack.push_back(b);
+    t.n_blocks = nb_old - (b1 - b0) + kb;
+    t.len -= end[i] - begin[i] - keep[i];
+    t.synced = std::min(t.synced, b0);
+    t.dev_len = -1;
+    if (c->track_runs) {
+      if (!x.in_place && kb) {
+        // the new blocks: one group of all threads of the stretch, one thread's its own
+        if (first) {
+          rs.push_back(BlockRun{new_gid(c), b0, kb});
+          c->gid_ref[rs.back().gid] = x.members;
+        } else {
+          rs.push_back(BlockRun{c->runs[slot_of(c, tid[x.first])].back().gid, b0, kb});
+        }
+        c->own_open[s] = x.members == 1;
+      }
+      if (t.len % kBlock) c->own_open[s] = 1;            // (its last block is nobody else's)
+    }
+  }
+  ++c->struct_epoch;
+  ++c->book_seq;
+  ++c->mod_seq;
+  c->last_append_rows = -1;
+  if (entries.empty() || c->host_only) return APAR_OK;
+  const size_t b_used = entries.size() * sizeof(EvictEntry);
+  memcpy(stg->host, entries.data(), b_used);
+  memcpy(stg->host + b_used, dst.data(), dst.size() * 4);
+  char* d_stage = c->ws(c->lay.stage);
+  rc = send(c, stg, d_stage, b_used + dst.size() * 4, st);
+  if (rc) return rc;
+  EvictArgs a;
+  a.entries = (const EvictEntry*)d_stage;
+  a.dst_blocks = (const int32_t*)(d_stage + b_used);
+  a.d_tables = (const int32_t*)c->ws(c->lay.tables);
+  a.table_stride = c->cfg.max_blocks_per_thread;
+  a.num_kv_heads = c->cfg.num_kv_heads;
+  a.k_pool = c->cfg.k_pool;
+  a.v_pool = c->cfg.v_pool;
+  a.weights = (float*)c->weights;
+  a.layer_bytes = c->layer_bytes;
+  a.layer_floats = c->layer_weights();
+  a.moves = (int2*)(c->weights + c->wlay.moves);
+  a.counts = (int32_t*)(c->weights + c->wlay.counts);
+  APAR_CUDA(c, launch_evict(a, (int)entries.size(), c->num_layers, max_rows, st));
+  c->kernels_total += 2;
   return APAR_OK;
 }
 

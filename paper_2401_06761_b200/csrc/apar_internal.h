@@ -102,6 +102,11 @@ __device__ __forceinline__ void pdl_launch_dependents() {
 }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
+// Natural log of sum exp, of a sum l relative to 2^m.
+__device__ __forceinline__ float lse_of(float m, float l) {
+  return l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : l == 0.f ? -INFINITY : l;   // (l: a NaN)
+}
+
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_kernel(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem,
                                  cudaStream_t st, bool pdl, Args&&... args) {
@@ -158,6 +163,8 @@ struct AttnArgs {
   int* part_flag = nullptr;
   Shape shape;
   float scale_log2e;                  // sm_scale * log2(e)
+  float* lse = nullptr;               // [n][num_q_heads] or nullptr: whoever writes a row of out also
+                                      // writes the log of its softmax denominator (not 4-bit pools)
   const CUtensorMap* tm_k = nullptr;  // [host] TMA descriptors of the pools (tensor-core path)
   const CUtensorMap* tm_v = nullptr;
   int* d_error = nullptr;             // [device] set to 1 when a bounded wait gave up
@@ -246,6 +253,70 @@ cudaError_t launch_q4_merge(const AttnArgs& a, const MergeRef* d_merge, int n_me
 cudaError_t launch_q4_verify_finish(const AttnArgs& a, const VerifyDesc* d_desc, int n_desc,
                                     cudaStream_t st);
 
+// ---- accumulated weights and eviction (weights.cu) ----
+// A run of keys and the queries that see it.  Units of one call share no key.
+struct KeyUnit {
+  int32_t table_row, tok_begin, tok_end;   // tok_end < 0: the current length of table_row
+  int32_t user_begin, n_users;
+  int32_t pad[3];
+};
+struct KeyUser {
+  int32_t query;                 // the (first) query
+  int32_t lim;                   // keys before this position are seen (by the first query)
+  int32_t count, pad;            // consecutive queries; each sees one key more than the one before
+};
+struct KeyArgs {
+  const void* q;
+  const float* lse;
+  const void* k_pool;            // (of the layer, as the next)
+  float* weights;                // [num_blocks][num_kv_heads][16]
+  const int32_t* d_tables;
+  const int32_t* d_lens;
+  const KeyUnit* units;
+  const KeyUser* users;
+  Shape shape;
+  float scale_log2e;
+  int replace;                   // 1: the keys' old weights do not count
+  int num_sms;
+};
+struct RowRange {
+  int32_t table_row, begin, count, pad;
+  int64_t first;                 // row of the output
+};
+// One stretch of rows out of which `keep` stay.  The moves of (layer, kv head) i are entries
+// list_begin + i * list_rows onward of the list: {from, to}, rows of the stretch.
+struct EvictEntry {
+  int32_t table_row, begin, n, keep;
+  int32_t in_place;              // 0: kept rows are copied to the blocks dst_blocks[dst_begin ..]
+  int32_t dst_begin, list_rows, pad;
+  int64_t list_begin;
+};
+struct EvictArgs {
+  const EvictEntry* entries;
+  const int32_t* dst_blocks;
+  const int32_t* d_tables;
+  int32_t table_stride, num_kv_heads;
+  void* k_pool;
+  void* v_pool;
+  float* weights;
+  size_t layer_bytes, layer_floats;
+  int2* moves;
+  int32_t* counts;               // [entries][layers * kv heads]
+};
+cudaError_t launch_weights_clear(float* w, size_t layer_floats, int num_layers, const int32_t* d_slots,
+                                 int n_rows, int num_kv_heads, cudaStream_t st);
+cudaError_t launch_weights_cow(float* w, size_t layer_floats, int num_layers, const CowCopy* d_copies,
+                               int n, int num_kv_heads, cudaStream_t st);
+cudaError_t launch_weights_move(float* w, size_t layer_floats, int num_layers, const RowMove* d_moves,
+                                const int32_t* d_group_begin, int n_groups, int num_kv_heads,
+                                cudaStream_t st);
+cudaError_t launch_key_weights(const KeyArgs& a, int n_units, cudaStream_t st);
+cudaError_t launch_weights_read(const float* w, const int32_t* d_tables, int table_stride,
+                                const RowRange* d_ranges, int n, int max_count, int num_kv_heads,
+                                float* out, cudaStream_t st);
+// max_rows: rows the entry that moves most may move.
+cudaError_t launch_evict(const EvictArgs& a, int n, int num_layers, int max_rows, cudaStream_t st);
+
 // ---- planner (planner.cpp) ----
 // A run of consecutive table positions whose blocks are held by the same set of threads
 // ("group"): blocks become shared only through fork, so the host keeps, per thread, its table
@@ -290,8 +361,24 @@ struct Plan {
   int32_t chunk_tokens = 0;
 };
 
+// Runs of keys for accumulated weights: each block of the queries' chains in exactly one run, with
+// all queries that see any of it.
+struct KeyQuery {
+  const int32_t* table;   // host block ids of the query's thread
+  int32_t table_row;
+  int32_t len;            // tokens whose blocks belong to the call
+  bool open;              // they are the thread's whole chain, which may grow while the plan is in use
+  KeyUser user;
+};
+struct KeyRun {
+  int32_t table_row, tok_begin, tok_end;   // tok_end < 0: open, the planned length folded as in WorkItem
+  int32_t user_begin, n_users;
+};
+
 class Planner {
  public:
+  // Returns false if two queries' tables disagree (tables that do not come from forks).
+  bool key_runs(const KeyQuery* q, int n, std::vector<KeyRun>* runs, std::vector<KeyUser>* users);
   void init(int num_blocks, int group, int num_kv_heads);
   // open_tails: the last chunk of a private tail run gets tok_end < 0 (resolved on the device
   // from the length array), so the plan stays valid while threads only grow.

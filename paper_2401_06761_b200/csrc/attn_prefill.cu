@@ -660,6 +660,7 @@ attn_prefill_kernel(const __grid_constant__ CUtensorMap tm_k,
       tc_fence_after();
       {
         const float inv = 1.f / l;
+        if (a.lse && out_row >= 0) a.lse[out_row] = lse_of(ref, l);
         uint4* dst = (uint4*)((__nv_bfloat16*)a.out + out_row * kDim);
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) {

@@ -501,6 +501,7 @@ attn_umma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
           }
         }
         if (mine && ur.slot >= 0) a.part_ml[prow] = make_float2(ref, l);
+        else if (mine && a.lse) a.lse[(size_t)ur.query * HQ + head] = lse_of(ref, l);
       }
       // O has been read: the next head's first P V may overwrite it
       tc_fence_before();
@@ -1087,6 +1088,7 @@ attn_umma_persist_kernel(const __grid_constant__ CUtensorMap tm_k,
           }
         }
         if (mine && ur.slot >= 0) a.part_ml[prow] = make_float2(ref, l);
+        else if (mine && a.lse) a.lse[(size_t)ur.query * HQ + head] = lse_of(ref, l);
       }
       // O has been read and this unit's description is no longer needed by this warp
       tc_fence_before();

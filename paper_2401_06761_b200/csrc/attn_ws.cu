@@ -282,6 +282,7 @@ attn_ws_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
         }
         if (ur.slot < 0 || fin_count(it) > 0) {
           const float inv = 1.f / L;
+          if (a.lse && tq == 0) a.lse[(size_t)ur.query * HQ + head] = lse_of(M, L);
           uint32_t* dst = (uint32_t*)a.out + ((size_t)ur.query * HQ + head) * 64 + tq;
 #pragma unroll
           for (int j = 0; j < 16; ++j)
@@ -669,6 +670,7 @@ attn_ws_persist_kernel(const __grid_constant__ CUtensorMap tm_k,
         }
         if (ur.slot < 0 || cur.fin_n > 0) {
           const float inv = 1.f / L;
+          if (a.lse && tq == 0) a.lse[(size_t)ur.query * HQ + head] = lse_of(M, L);
           uint32_t* dst = (uint32_t*)a.out + ((size_t)ur.query * HQ + head) * 64 + tq;
 #pragma unroll
           for (int j = 0; j < 16; ++j)

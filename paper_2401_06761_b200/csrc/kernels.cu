@@ -289,6 +289,7 @@ __global__ void __launch_bounds__(128) attn_vec_kernel(const AttnArgs a, int ite
           // an empty range (no tokens at all) has L = 0: its output is defined as zero
           ((__nv_bfloat16*)a.out)[((size_t)ur.query * HQ + head) * kDim + t] =
               __float2bfloat16_rn(L > 0.f ? O / L : 0.f);
+          if (a.lse && t == 0) a.lse[(size_t)ur.query * HQ + head] = lse_of(M, L);
         } else {
           const size_t prow = (size_t)(ur.slot + it.slot_add) * HQ + head;
           a.part_o[prow * kDim + t] = O;
@@ -420,6 +421,7 @@ __global__ void __launch_bounds__(128) attn_vec_heads_kernel(const AttnArgs a, i
         packed.x = *(uint32_t*)&p0; packed.y = *(uint32_t*)&p1;
         packed.z = *(uint32_t*)&p2; packed.w = *(uint32_t*)&p3;
         ((uint4*)((__nv_bfloat16*)a.out + ((size_t)ur.query * HQ + h) * kDim))[c] = packed;
+        if (a.lse && c == 0) a.lse[(size_t)ur.query * HQ + h] = lse_of(m, l);
       } else {
         const size_t prow = (size_t)(ur.slot + it.slot_add) * HQ + h;
         float4* dst = (float4*)(a.part_o + prow * kDim) + 2 * c;
@@ -523,6 +525,7 @@ __global__ void __launch_bounds__(128) verify_tail_kernel(const AttnArgs a,
         packed.x = *(uint32_t*)&p0; packed.y = *(uint32_t*)&p1;
         packed.z = *(uint32_t*)&p2; packed.w = *(uint32_t*)&p3;
         ((uint4*)((__nv_bfloat16*)a.out + ((size_t)d.query * HQ + head) * kDim))[c] = packed;
+        if (a.lse && c == 0) a.lse[(size_t)d.query * HQ + head] = lse_of(m, l);
       } else {
         const size_t prow = (size_t)d.slot * HQ + head;
         float4* dst = (float4*)(a.part_o + prow * kDim) + 2 * c;
@@ -673,6 +676,7 @@ __global__ void __launch_bounds__(128) merge_kernel(const AttnArgs a,
   packed.x = *(uint32_t*)&lo;
   packed.y = *(uint32_t*)&hi;
   ((uint2*)((__nv_bfloat16*)a.out + ((size_t)mr.query * HQ + head) * kDim))[lane] = packed;
+  if (a.lse && lane == 0) a.lse[(size_t)mr.query * HQ + head] = lse_of(M, L);
 }
 
 cudaError_t launch_merge(const AttnArgs& a, const MergeRef* d_merge, int n_merge, cudaStream_t st) {

@@ -379,4 +379,59 @@ bool Planner::build(const PlanQuery* q, int n, int64_t slot_capacity, bool open_
   return true;
 }
 
+bool Planner::key_runs(const KeyQuery* q, int n, std::vector<KeyRun>* runs,
+                       std::vector<KeyUser>* users) {
+  if (++epoch_ == 0) {
+    std::fill(stamp_.begin(), stamp_.end(), 0u);
+    epoch_ = 1;
+  }
+  // how many queries list each block; the sets are nested along a chain, so consecutive blocks
+  // listed equally often are listed by the same queries
+  for (int i = 0; i < n; ++i)
+    for (int e = 0; e < (q[i].len + kBlock - 1) / kBlock; ++e) {
+      const int32_t b = q[i].table[e];
+      if (stamp_[b] != epoch_) {
+        stamp_[b] = epoch_;
+        cnt_[b] = 0;
+        seg_of_[b] = -1;
+      }
+      ++cnt_[b];
+    }
+  runs->clear();
+  seg_users_.clear();
+  for (int i = 0; i < n; ++i) {
+    const int ne = (q[i].len + kBlock - 1) / kBlock;
+    for (int e0 = 0, e1; e0 < ne; e0 = e1) {
+      const int32_t b0 = q[i].table[e0];
+      for (e1 = e0 + 1; e1 < ne && cnt_[q[i].table[e1]] == cnt_[b0]; ++e1) {}
+      if (seg_of_[b0] < 0) {
+        seg_of_[b0] = (int32_t)runs->size();
+        runs->push_back(KeyRun{q[i].table_row, e0 * kBlock, e1 * kBlock, 0, 0});
+      }
+      KeyRun& r = (*runs)[seg_of_[b0]];
+      if (r.tok_begin != e0 * kBlock || (r.tok_end < 0 ? -r.tok_end - 1 : r.tok_end - r.tok_begin) !=
+                                            (e1 - e0) * kBlock)
+        return false;
+      // the end of a thread's chain: nobody else lists its last block, or only after a fork at a full
+      // block, where a row more would open a block of its own (and a new plan)
+      if (e1 == ne && q[i].open && r.tok_end >= 0 && r.table_row == q[i].table_row)
+        r.tok_end = -(r.tok_end - r.tok_begin) - 1;
+      ++r.n_users;
+      seg_users_.push_back(SegUser{seg_of_[b0], i, 0});
+    }
+  }
+  int32_t at = 0;
+  for (KeyRun& r : *runs) {
+    r.user_begin = at;
+    at += r.n_users;
+    r.n_users = 0;
+  }
+  users->resize(at);
+  for (const SegUser& su : seg_users_) {
+    KeyRun& r = (*runs)[su.seg];
+    (*users)[r.user_begin + r.n_users++] = q[su.query].user;
+  }
+  return true;
+}
+
 }  // namespace apar

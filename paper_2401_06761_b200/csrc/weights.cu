@@ -1,0 +1,386 @@
+// Accumulated attention weights of cached keys, and eviction by them.
+//
+// A float per (layer, block, kv head, row) lies beside the K and V pools, in the same order: how much
+// weight the key has received so far, summed over queries and the heads of a group,
+//     w[key] (+)= sum_{query, head} exp(scale <q, k> - lse[query, head]),
+// where lse is the log of the softmax's denominator that the attention call has written.  So one pass
+// over K is enough, V is not read, and no maximum or sum has to be found first.
+#include <algorithm>
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include "apar_internal.h"
+#include "ptx.cuh"
+
+namespace apar {
+namespace {
+
+constexpr unsigned kAll = 0xffffffffu;
+
+// ------------------------------------------------------------------ rows that come, move and are copied
+__global__ void __launch_bounds__(256) weights_clear_kernel(float* __restrict__ w, size_t layer_floats,
+                                                            const int32_t* __restrict__ slots,
+                                                            int n_rows, int num_kv_heads) {
+  const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  if (i >= (int64_t)n_rows * num_kv_heads) return;
+  const int slot = slots[i / num_kv_heads], h = (int)(i % num_kv_heads);
+  w[blockIdx.y * layer_floats + ((size_t)(slot >> 4) * num_kv_heads + h) * kBlock + (slot & 15)] = 0.f;
+}
+
+__global__ void __launch_bounds__(128) weights_cow_kernel(float* __restrict__ w, size_t layer_floats,
+                                                          const CowCopy* __restrict__ copies,
+                                                          int num_kv_heads) {
+  const CowCopy c = copies[blockIdx.x];
+  float* p = w + blockIdx.y * layer_floats;
+  for (int i = threadIdx.x; i < num_kv_heads * kBlock; i += blockDim.x)
+    if ((i & 15) < c.rows)
+      p[(size_t)c.dst_block * num_kv_heads * kBlock + i] = p[(size_t)c.src_block * num_kv_heads * kBlock + i];
+}
+
+// A group is at most 64 rows whose sources and destinations may overlap: all are read, then written.
+__global__ void __launch_bounds__(64) weights_move_kernel(float* __restrict__ w, size_t layer_floats,
+                                                          const RowMove* __restrict__ moves,
+                                                          const int32_t* __restrict__ group_begin,
+                                                          int num_kv_heads) {
+  const int m = group_begin[blockIdx.x] + threadIdx.x, h = blockIdx.y;
+  float* p = w + blockIdx.z * layer_floats;
+  const bool on = m < group_begin[blockIdx.x + 1];
+  auto at = [&](int slot) {
+    return ((size_t)(slot >> 4) * num_kv_heads + h) * kBlock + (slot & 15);
+  };
+  float v = 0.f;
+  if (on) v = p[at(moves[m].src_slot)];
+  __syncthreads();
+  if (on) p[at(moves[m].dst_slot)] = v;
+}
+
+// ------------------------------------------------------------------ one query per thread
+// A unit is a run of keys and the queries that see it; no key belongs to two units, so a unit adds
+// to its keys' weights without atomics and in a fixed order.  One warp takes a unit and a kv head:
+// sixteen keys at a time are the A operand of mma.m16n8k16, eight rows (query, head of the group) the
+// B operand.  The contraction may take the dims in any order as long as both operands take the same:
+// a lane loads sixteen consecutive bytes of its key's row, which hold its share of two products, so K
+// comes straight from memory into registers.
+__device__ __forceinline__ uint4 ld_k(const uint4* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+                                         uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9},"
+      " {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+constexpr int kKeyWarps = 8;
+
+__global__ void __launch_bounds__(kKeyWarps * 32, 2) key_weights_kernel(const KeyArgs a, int n_units) {
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int G = a.shape.group, HQ = a.shape.num_q_heads, HKV = a.shape.num_kv_heads;
+  const int stride = gridDim.x * kKeyWarps;
+  for (int64_t u = (int64_t)blockIdx.x * kKeyWarps + (threadIdx.x >> 5); u < (int64_t)n_units * HKV; u += stride) {
+    const KeyUnit it = a.units[u / HKV];
+    const int h = (int)(u % HKV);
+    const int32_t* table = a.d_tables + (size_t)it.table_row * a.shape.table_stride;
+    const int end = it.tok_end < 0 ? a.d_lens[it.table_row] : it.tok_end;
+    const int rows = it.n_users * G;
+    if (it.tok_begin >= end) continue;
+    for (int r0 = 0; r0 < rows; r0 += 8) {
+      // this lane's part of the rows: row r0 + g as an operand, rows r0 + 2 t and + 1 as results
+      uint4 q[4];
+      const int r = r0 + g;
+      if (r < rows) {
+        const int query = a.users[it.user_begin + r / G].query;
+        const uint4* src = (const uint4*)((const __nv_bfloat16*)a.q + ((size_t)query * HQ + h * G + r % G) * kDim);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) q[w] = __ldg(src + 4 * w + t);
+      } else {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) q[w] = make_uint4(0u, 0u, 0u, 0u);
+      }
+      float ref[2];
+      int see[2];                                // keys before this one are seen
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int rr = r0 + 2 * t + e;
+        ref[e] = 0.f;
+        see[e] = 0;
+        if (rr < rows) {
+          const KeyUser user = a.users[it.user_begin + rr / G];
+          ref[e] = __ldg(a.lse + (size_t)user.query * HQ + h * G + rr % G) * 1.4426950408889634f;
+          see[e] = min(user.lim, end);
+        }
+      }
+      uint4 k[8];
+      auto fetch = [&](int tok) {
+        const uint4* src = (const uint4*)((const uint8_t*)a.k_pool +
+                                          ((size_t)table[tok >> 4] * HKV + h) * kTileBytes) + g * 16 + t;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          k[w] = ld_k(src + 4 * w);
+          k[4 + w] = ld_k(src + 128 + 4 * w);
+        }
+      };
+      fetch(it.tok_begin);
+      for (int tok = it.tok_begin; tok < end; tok += kBlock) {
+        float d[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          mma16816(d, k[w].x, k[4 + w].x, k[w].y, k[4 + w].y, q[w].x, q[w].y);
+          mma16816(d, k[w].z, k[4 + w].z, k[w].w, k[4 + w].w, q[w].z, q[w].w);
+        }
+        const int block = table[tok >> 4];
+        if (tok + kBlock < end) fetch(tok + kBlock);
+        // keys tok + g (d[0], d[1]) and tok + g + 8 (d[2], d[3]); a key that a row does not see may
+        // hold any bits
+        float lo = 0.f, hi = 0.f;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          if (tok + g < see[e]) lo += ex2(fmaf(d[e], a.scale_log2e, -ref[e]));
+          if (tok + g + 8 < see[e]) hi += ex2(fmaf(d[2 + e], a.scale_log2e, -ref[e]));
+        }
+        lo += __shfl_xor_sync(kAll, lo, 1);
+        hi += __shfl_xor_sync(kAll, hi, 1);
+        lo += __shfl_xor_sync(kAll, lo, 2);
+        hi += __shfl_xor_sync(kAll, hi, 2);
+        if (t < 2) {
+          const int row = g + 8 * t;
+          float* w = a.weights + ((size_t)block * HKV + h) * kBlock + row;
+          const float add = t ? hi : lo;
+          if (tok + row < end) *w = a.replace && r0 == 0 ? add : *w + add;
+        }
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------ read back
+__global__ void __launch_bounds__(256) weights_read_kernel(const float* __restrict__ w,
+                                                           const int32_t* __restrict__ tables, int stride,
+                                                           const RowRange* __restrict__ ranges,
+                                                           int num_kv_heads, float* __restrict__ out) {
+  const RowRange r = ranges[blockIdx.y];
+  const int64_t n = (int64_t)r.count * num_kv_heads;
+  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
+    const int pos = r.begin + (int)(i / num_kv_heads), h = (int)(i % num_kv_heads);
+    const int block = tables[(size_t)r.table_row * stride + (pos >> 4)];
+    out[r.first * num_kv_heads + i] = w[((size_t)block * num_kv_heads + h) * kBlock + (pos & 15)];
+  }
+}
+
+// ------------------------------------------------------------------ eviction: which rows
+// One CTA per (stretch, layer, kv head).  The keep-th largest weight is found eight bits at a time from
+// histograms; a second pass in order of the rows tells which rows equal to it are early enough, and
+// numbers the rows that move and the places they move to.
+__device__ __forceinline__ uint32_t weight_key(float x) {      // larger weight, larger key; a NaN on top
+  const uint32_t b = __float_as_uint(x + 0.f);
+  return x != x ? 0xffffffffu : b ^ (uint32_t)((int32_t)b >> 31 | 0x80000000);
+}
+
+constexpr int kPickThreads = 512;
+
+__global__ void __launch_bounds__(kPickThreads) evict_pick_kernel(const EvictArgs a) {
+  __shared__ uint32_t hist[256];
+  __shared__ uint32_t s_prefix, s_left;
+  __shared__ int s_scan[3][kPickThreads / 32];
+  const EvictEntry en = a.entries[blockIdx.x];
+  const int heads = a.num_kv_heads, lh = blockIdx.y, l = lh / heads, h = lh % heads;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const float* w = a.weights + (size_t)l * a.layer_floats;
+  const int32_t* table = a.d_tables + (size_t)en.table_row * a.table_stride + en.begin / kBlock;
+  int2* list = a.moves + en.list_begin + (size_t)lh * en.list_rows;
+  auto key_at = [&](int i) {
+    return weight_key(w[((size_t)table[i >> 4] * heads + h) * kBlock + (i & 15)]);
+  };
+  uint32_t prefix = 0, left = en.keep;           // the left-th largest key that starts with prefix
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    for (int i = threadIdx.x; i < 256; i += kPickThreads) hist[i] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < en.n; i += kPickThreads) {
+      const uint32_t k = key_at(i);
+      if (shift == 24 || k >> (shift + 8) == prefix) atomicAdd(&hist[k >> shift & 255], 1u);
+    }
+    __syncthreads();
+    if (warp == 0) {
+      // lane i looks after bins 255 - 8 i downwards
+      uint32_t sum = 0;
+      for (int j = 0; j < 8; ++j) sum += hist[255 - 8 * lane - j];
+      uint32_t upto = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o *= 2) {
+        const uint32_t x = __shfl_up_sync(kAll, upto, o);
+        if (lane >= o) upto += x;
+      }
+      uint32_t above = upto - sum;
+      if (above < left && left <= upto) {
+        int bin = 255 - 8 * lane;
+        while (above + hist[bin] < left) above += hist[bin--];
+        s_prefix = prefix << 8 | bin;
+        s_left = left - above;
+      }
+    }
+    __syncthreads();
+    prefix = s_prefix;
+    left = s_left;
+  }
+  // rows above `prefix` are kept, and the first `left` rows equal to it
+  int n_equal = 0, n_move = 0, n_hole = 0;
+  for (int i0 = 0; i0 < en.n; i0 += kPickThreads) {
+    const int i = i0 + threadIdx.x;
+    const uint32_t k = i < en.n ? key_at(i) : 0;
+    const bool equal = i < en.n && k == prefix;
+    unsigned who = __ballot_sync(kAll, equal);
+    if (lane == 0) s_scan[0][warp] = __popc(who);
+    __syncthreads();
+    int before = n_equal + __popc(who & ((1u << lane) - 1)), total = 0;
+    for (int x = 0; x < kPickThreads / 32; ++x) {
+      if (x < warp) before += s_scan[0][x];
+      total += s_scan[0][x];
+    }
+    n_equal += total;
+    const bool kept = i < en.n && (k > prefix || (equal && before < (int)left));
+    const bool move = kept && i >= en.keep, hole = !kept && i < en.keep;
+    const unsigned wm = __ballot_sync(kAll, move), wh = __ballot_sync(kAll, hole);
+    if (lane == 0) {
+      s_scan[1][warp] = __popc(wm);
+      s_scan[2][warp] = __popc(wh);
+    }
+    __syncthreads();
+    int m = n_move + __popc(wm & ((1u << lane) - 1)), o = n_hole + __popc(wh & ((1u << lane) - 1));
+    for (int x = 0; x < kPickThreads / 32; ++x) {
+      if (x < warp) {
+        m += s_scan[1][x];
+        o += s_scan[2][x];
+      }
+      n_move += s_scan[1][x];
+      n_hole += s_scan[2][x];
+    }
+    if (move) list[m].x = i;
+    if (hole) list[o].y = i;
+    __syncthreads();
+  }
+  // out of place the rows that stay are copied as well, behind those that move
+  if (!en.in_place) {
+    int n_stay = n_move;
+    n_equal = 0;
+    for (int i0 = 0; i0 < en.keep; i0 += kPickThreads) {
+      const int i = i0 + threadIdx.x;
+      const uint32_t k = i < en.n ? key_at(i) : 0;
+      const bool equal = i < en.n && k == prefix;
+      const unsigned who = __ballot_sync(kAll, equal);
+      if (lane == 0) s_scan[0][warp] = __popc(who);
+      __syncthreads();
+      int before = n_equal + __popc(who & ((1u << lane) - 1));
+      for (int x = 0; x < kPickThreads / 32; ++x) {
+        if (x < warp) before += s_scan[0][x];
+        n_equal += s_scan[0][x];
+      }
+      const bool stay = i < en.keep && i < en.n && (k > prefix || (equal && before < (int)left));
+      const unsigned ws = __ballot_sync(kAll, stay);
+      if (lane == 0) s_scan[1][warp] = __popc(ws);
+      __syncthreads();
+      int m = n_stay + __popc(ws & ((1u << lane) - 1));
+      for (int x = 0; x < kPickThreads / 32; ++x) {
+        if (x < warp) m += s_scan[1][x];
+        n_stay += s_scan[1][x];
+      }
+      if (stay) list[m] = make_int2(i, i);
+      __syncthreads();
+    }
+    n_move = n_stay;
+  }
+  if (threadIdx.x == 0) a.counts[(size_t)blockIdx.x * gridDim.y + lh] = n_move;
+}
+
+// ------------------------------------------------------------------ eviction: the rows move
+// Half a warp per row: 256 bytes of K, 256 of V, and the weight.  Sources lie behind `keep` and
+// destinations before it, or in other blocks: no move reads what another writes.
+__global__ void __launch_bounds__(256) evict_move_kernel(const EvictArgs a) {
+  const EvictEntry en = a.entries[blockIdx.z];
+  const int heads = a.num_kv_heads, lh = blockIdx.y, l = lh / heads, h = lh % heads;
+  const int n = a.counts[(size_t)blockIdx.z * gridDim.y + lh], c = threadIdx.x & 15;
+  const int2* list = a.moves + en.list_begin + (size_t)lh * en.list_rows;
+  const int32_t* from = a.d_tables + (size_t)en.table_row * a.table_stride + en.begin / kBlock;
+  const int32_t* to = en.in_place ? from : a.dst_blocks + en.dst_begin;
+  uint4* k = (uint4*)((char*)a.k_pool + (size_t)l * a.layer_bytes);
+  uint4* v = (uint4*)((char*)a.v_pool + (size_t)l * a.layer_bytes);
+  float* w = a.weights + (size_t)l * a.layer_floats;
+  for (int m = blockIdx.x * 16 + (threadIdx.x >> 4); m < n; m += gridDim.x * 16) {
+    const int2 mv = list[m];
+    const size_t src = ((size_t)from[mv.x >> 4] * heads + h) * kBlock + (mv.x & 15);
+    const size_t dst = ((size_t)to[mv.y >> 4] * heads + h) * kBlock + (mv.y & 15);
+    const uint4 x = k[src * 16 + c], y = v[src * 16 + c];
+    k[dst * 16 + c] = x;
+    v[dst * 16 + c] = y;
+    if (c == 0) w[dst] = w[src];
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_weights_clear(float* w, size_t layer_floats, int num_layers, const int32_t* d_slots,
+                                 int n_rows, int num_kv_heads, cudaStream_t st) {
+  if (n_rows <= 0) return cudaSuccess;
+  const unsigned grid = (unsigned)(((int64_t)n_rows * num_kv_heads + 255) / 256);
+  return launch_kernel(weights_clear_kernel, dim3(grid, num_layers), dim3(256), 0, st, false, w,
+                       layer_floats, d_slots, n_rows, num_kv_heads);
+}
+
+cudaError_t launch_weights_cow(float* w, size_t layer_floats, int num_layers, const CowCopy* d_copies,
+                               int n, int num_kv_heads, cudaStream_t st) {
+  if (n <= 0) return cudaSuccess;
+  return launch_kernel(weights_cow_kernel, dim3(n, num_layers), dim3(128), 0, st, false, w,
+                       layer_floats, d_copies, num_kv_heads);
+}
+
+cudaError_t launch_weights_move(float* w, size_t layer_floats, int num_layers, const RowMove* d_moves,
+                                const int32_t* d_group_begin, int n_groups, int num_kv_heads,
+                                cudaStream_t st) {
+  if (n_groups <= 0) return cudaSuccess;
+  return launch_kernel(weights_move_kernel, dim3(n_groups, num_kv_heads, num_layers), dim3(64), 0, st,
+                       false, w, layer_floats, d_moves, d_group_begin, num_kv_heads);
+}
+
+cudaError_t launch_key_weights(const KeyArgs& a, int n_units, cudaStream_t st) {
+  if (n_units <= 0) return cudaSuccess;
+  const int64_t warps = (int64_t)n_units * a.shape.num_kv_heads;
+  const int grid = (int)std::min<int64_t>((warps + kKeyWarps - 1) / kKeyWarps, 2 * a.num_sms);
+  return launch_kernel(key_weights_kernel, dim3(grid), dim3(kKeyWarps * 32), 0, st, false, a, n_units);
+}
+
+cudaError_t launch_weights_read(const float* w, const int32_t* d_tables, int table_stride,
+                                const RowRange* d_ranges, int n, int max_count, int num_kv_heads,
+                                float* out, cudaStream_t st) {
+  if (n <= 0 || max_count <= 0) return cudaSuccess;
+  const unsigned grid = (unsigned)std::min<int64_t>(((int64_t)max_count * num_kv_heads + 255) / 256, 4096);
+  for (int i = 0; i < n; i += 65535) {                 // (the grid's limit)
+    const cudaError_t e = launch_kernel(weights_read_kernel, dim3(grid, std::min(n - i, 65535)), dim3(256),
+                                        0, st, false, w, d_tables, table_stride, d_ranges + i,
+                                        num_kv_heads, out);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+cudaError_t launch_evict(const EvictArgs& a, int n, int num_layers, int max_rows, cudaStream_t st) {
+  if (n <= 0) return cudaSuccess;
+  const int lh = num_layers * a.num_kv_heads;
+  cudaError_t e = launch_kernel(evict_pick_kernel, dim3(n, lh), dim3(kPickThreads), 0, st, false, a);
+  if (e != cudaSuccess || max_rows <= 0) return e;
+  const unsigned grid = (unsigned)std::min((max_rows + 15) / 16, 1024);
+  EvictArgs part = a;
+  for (int i = 0; i < n && e == cudaSuccess; i += 65535) {   // (the grid's limit)
+    part.entries = a.entries + i;
+    part.counts = a.counts + (size_t)i * lh;
+    e = launch_kernel(evict_move_kernel, dim3(grid, lh, std::min(n - i, 65535)), dim3(256), 0, st, false,
+                      part);
+  }
+  return e;
+}
+
+}  // namespace apar

@@ -111,7 +111,7 @@ class BeamSelect:
 class PagedSession:
     def __init__(self, shape: LayerShape, num_blocks: int, max_threads: int,
                  max_blocks_per_thread: int, device="cuda", poison: bool = False,
-                 num_layers: int = 1, kv_format: str = "bf16"):
+                 num_layers: int = 1, kv_format: str = "bf16", weights: bool = False):
         if not torch.cuda.is_available():
             raise RuntimeError("the APAR library needs a CUDA device; there is no CPU path")
         self.shape, self.device = shape, torch.device(device)
@@ -143,6 +143,15 @@ class PagedSession:
         self.ctx = (B.apar_create(cfg) if kv_format == "bf16" else
                     B.apar_create_kv(cfg, B.KV_FORMATS[kv_format]))
         self.sm_scale = 1.0 / math.sqrt(shape.head_dim)
+        # accumulated weight of every cached row: [layers][blocks][kv heads][16]
+        self.weights = None
+        if weights:
+            nbytes = B.apar_weights_bytes(cfg)
+            self._weights_memory = torch.zeros(nbytes, dtype=torch.uint8, device=device)
+            rows = num_layers * num_blocks * shape.num_kv_heads * shape.block_size
+            self.weights = self._weights_memory[:4 * rows].view(torch.float32).view(
+                num_layers, num_blocks, shape.num_kv_heads, shape.block_size)
+            B.apar_attach_weights(self.ctx, self._weights_memory.data_ptr(), nbytes)
 
     @classmethod
     def for_spec(cls, spec: ForestSpec, device="cuda", poison=False, extra_blocks=0,
@@ -168,6 +177,18 @@ class PagedSession:
             return torch.cuda.current_stream().cuda_stream
         return _raw_stream(torch.cuda.current_device())
 
+    def _attend(self, lse, q, call, *args):
+        """One attention call, which also writes lse [queries][heads] if one is given."""
+        if lse is None:
+            return call(self.ctx, *args)
+        assert lse.is_cuda and lse.is_contiguous() and lse.dtype == torch.float32
+        assert lse.shape == q.shape[:2]
+        B.apar_set_lse_output(self.ctx, lse.data_ptr())
+        try:
+            return call(self.ctx, *args)
+        finally:
+            B.apar_set_lse_output(self.ctx, 0)
+
     # the replay protocol of synth.build_forest
     def new_threads(self, n):
         return B.apar_new_threads(self.ctx, n)
@@ -182,32 +203,34 @@ class PagedSession:
         B.apar_append_kv(self.ctx, tids, counts, k_rows.data_ptr(), v_rows.data_ptr(),
                          self._stream())
 
-    def attention(self, tids, q: torch.Tensor, out: torch.Tensor = None, sm_scale=None):
+    def attention(self, tids, q: torch.Tensor, out: torch.Tensor = None, sm_scale=None, lse=None):
+        """lse (here and below): a float tensor [n][heads] that takes the log of each row's softmax
+        denominator, for add_weights."""
         assert q.is_cuda and q.is_contiguous() and q.dtype == torch.bfloat16
         if out is None:
             out = torch.empty_like(q)
-        B.apar_tree_decode_attention(self.ctx, tids, q.data_ptr(), out.data_ptr(),
-                                     self.sm_scale if sm_scale is None else sm_scale,
-                                     self._stream())
+        self._attend(lse, q, B.apar_tree_decode_attention, tids, q.data_ptr(),
+                     out.data_ptr(), self.sm_scale if sm_scale is None else sm_scale,
+                     self._stream())
         return out
 
     def decode_step(self, tids, k_rows: torch.Tensor, v_rows: torch.Tensor, q: torch.Tensor,
-                    out: torch.Tensor = None, sm_scale=None):
+                    out: torch.Tensor = None, sm_scale=None, lse=None):
         assert k_rows.is_cuda and k_rows.is_contiguous() and v_rows.is_contiguous()
         assert q.is_cuda and q.is_contiguous() and q.dtype == torch.bfloat16
         if out is None:
             out = torch.empty_like(q)
-        B.apar_decode_step(self.ctx, tids, k_rows.data_ptr(), v_rows.data_ptr(), q.data_ptr(),
-                           out.data_ptr(), self.sm_scale if sm_scale is None else sm_scale,
-                           self._stream())
+        self._attend(lse, q, B.apar_decode_step, tids, k_rows.data_ptr(), v_rows.data_ptr(),
+                     q.data_ptr(), out.data_ptr(), self.sm_scale if sm_scale is None else
+                     sm_scale, self._stream())
         return out
 
-    def prefix_attention(self, tids, attend_len, q: torch.Tensor, sm_scale=None):
+    def prefix_attention(self, tids, attend_len, q: torch.Tensor, sm_scale=None, lse=None):
         assert q.is_cuda and q.is_contiguous() and q.dtype == torch.bfloat16
         out = torch.empty_like(q)
-        B.apar_tree_prefix_attention(self.ctx, tids, attend_len, q.data_ptr(), out.data_ptr(),
-                                     self.sm_scale if sm_scale is None else sm_scale,
-                                     self._stream())
+        self._attend(lse, q, B.apar_tree_prefix_attention, tids, attend_len, q.data_ptr(),
+                     out.data_ptr(), self.sm_scale if sm_scale is None else sm_scale,
+                     self._stream())
         return out
 
     def verify_attention(self, tids, n_cand, anc_mask, q: torch.Tensor, sm_scale=None):
@@ -223,14 +246,13 @@ class PagedSession:
         B.apar_accept_candidates(self.ctx, tids, n_cand, keep, self._stream())
 
     def prefill_attention(self, tids, q_begin, q_count, q: torch.Tensor, out: torch.Tensor = None,
-                          layer: int = 0, sm_scale=None):
+                          layer: int = 0, sm_scale=None, lse=None):
         assert q.is_cuda and q.is_contiguous() and q.dtype == torch.bfloat16
         if out is None:
             out = torch.empty_like(q)
-        B.apar_tree_prefill_attention(self.ctx, layer, tids, q_begin, q_count, q.data_ptr(),
-                                      out.data_ptr(),
-                                      self.sm_scale if sm_scale is None else sm_scale,
-                                      self._stream())
+        self._attend(lse, q, B.apar_tree_prefill_attention, layer, tids, q_begin, q_count,
+                     q.data_ptr(), out.data_ptr(), self.sm_scale if sm_scale is None else
+                     sm_scale, self._stream())
         return out
 
     def append_layer(self, layer: int, k_rows: torch.Tensor, v_rows: torch.Tensor):
@@ -239,13 +261,13 @@ class PagedSession:
                                self._stream())
 
     def attention_layer(self, layer: int, q: torch.Tensor, out: torch.Tensor = None,
-                        sm_scale=None):
+                        sm_scale=None, lse=None):
         assert q.is_cuda and q.is_contiguous() and q.dtype == torch.bfloat16
         if out is None:
             out = torch.empty_like(q)
-        B.apar_tree_decode_attention_layer(self.ctx, layer, q.data_ptr(), out.data_ptr(),
-                                           self.sm_scale if sm_scale is None else sm_scale,
-                                           self._stream())
+        self._attend(lse, q, B.apar_tree_decode_attention_layer, layer, q.data_ptr(),
+                     out.data_ptr(), self.sm_scale if sm_scale is None else sm_scale,
+                     self._stream())
         return out
 
     def read_kv(self, tids, begin, count, layer: int = 0):
@@ -259,6 +281,33 @@ class PagedSession:
         B.apar_read_kv(self.ctx, layer, tids, begin, count, k.data_ptr(), v.data_ptr(),
                        self._stream())
         return k, v
+
+    def reorder(self, tids, sources):
+        """Thread tids[i] goes on with the chain that sources[i] held (beam search)."""
+        B.apar_reorder(self.ctx, tids, sources, self._stream())
+
+    def add_weights(self, q: torch.Tensor, lse: torch.Tensor, layer: int = 0, sm_scale=None,
+                    replace: bool = False):
+        """Adds to each cached row the weight that the queries of the most recent decode attention
+        gave it: q and lse are that call's (of this layer)."""
+        assert q.is_cuda and q.is_contiguous() and q.dtype == torch.bfloat16
+        assert lse.is_cuda and lse.is_contiguous() and lse.dtype == torch.float32
+        assert lse.shape == q.shape[:2]
+        B.apar_add_weights(self.ctx, layer, q.data_ptr(), lse.data_ptr(),
+                           self.sm_scale if sm_scale is None else sm_scale, replace, self._stream())
+
+    def read_weights(self, tids, begin, count, layer: int = 0):
+        """Weights [rows][kv heads] of rows begin[i] .. begin[i] + count[i] - 1 of each chain."""
+        count = B.int32_array(count)
+        rows = max(0, int(np.frombuffer(count[0], np.int32, count[1]).sum(dtype=np.int64)))
+        out = torch.empty((rows, self.shape.num_kv_heads), dtype=torch.float32, device=self.device)
+        B.apar_read_weights(self.ctx, layer, tids, begin, count, out.data_ptr(), self._stream())
+        return out
+
+    def evict(self, tids, begin, end, keep):
+        """Of rows begin[i] .. end[i] - 1 of each chain only the keep[i] heaviest stay, per layer and
+        kv head."""
+        B.apar_evict(self.ctx, tids, begin, end, keep, self._stream())
 
     def release(self, tids):
         B.apar_release(self.ctx, tids)
