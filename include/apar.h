@@ -511,6 +511,18 @@ apar_status apar_set_lse_output(apar_ctx* ctx, float* lse /*[device] or NULL*/);
 apar_status apar_add_weights(apar_ctx* ctx, int32_t layer, const void* q /*[device]*/,
                              const float* lse /*[device]*/, float sm_scale, int32_t replace,
                              void* cuda_stream);
+/* The same for runs of consecutive queries, as apar_tree_prefill_attention takes them: segment i is
+ * the tokens of thread tid[i] at chain positions q_begin[i] .. q_begin[i] + q_count[i] - 1, and the
+ * query at position p sees positions 0 .. p.  q and lse [sum q_count][num_q_heads]([128]), segments in
+ * order, as that call took and wrote them; a part of its queries will do (a window of the last ones,
+ * say).  replace != 0: weights of rows 0 .. q_begin[i] + q_count[i] - 1 of each chain are replaced.
+ * A plan is made and uploaded, so it cannot be captured.
+ * Errors: INVALID_ARG (also a range outside the thread, no memory attached), BAD_THREAD, UNSUPPORTED,
+ * WORKSPACE_TOO_SMALL, CUDA. */
+apar_status apar_add_weights_prefill(apar_ctx* ctx, int32_t layer, int32_t n, const int32_t* tid /*[host]*/,
+                                     const int32_t* q_begin /*[host]*/, const int32_t* q_count /*[host]*/,
+                                     const void* q /*[device]*/, const float* lse /*[device]*/,
+                                     float sm_scale, int32_t replace, void* cuda_stream);
 /* Weights of rows begin[i] .. begin[i] + count[i] - 1 of thread tid[i]'s chain, entries one after the
  * other: out [device] float [sum count][num_kv_heads].  A thread may be listed several times.
  * Uses the staging buffers, so it cannot be captured.

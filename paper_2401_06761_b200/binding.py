@@ -92,6 +92,9 @@ _SIGS = {
     "apar_set_lse_output": (C.c_int32, [_ctx, C.c_void_p]),
     "apar_add_weights": (C.c_int32, [_ctx, C.c_int32, C.c_void_p, C.c_void_p, C.c_float, C.c_int32,
                                      C.c_void_p]),
+    "apar_add_weights_prefill": (C.c_int32, [_ctx, C.c_int32, C.c_int32, _i32p, _i32p, _i32p,
+                                             C.c_void_p, C.c_void_p, C.c_float, C.c_int32,
+                                             C.c_void_p]),
     "apar_read_weights": (C.c_int32, [_ctx, C.c_int32, C.c_int32, _i32p, _i32p, _i32p, C.c_void_p,
                                       C.c_void_p]),
     "apar_evict": (C.c_int32, [_ctx, C.c_int32, _i32p, _i32p, _i32p, _i32p, C.c_void_p]),
@@ -366,6 +369,12 @@ def apar_set_lse_output(ctx, lse: int):
 
 def apar_add_weights(ctx, layer: int, q: int, lse: int, sm_scale: float, replace: bool, stream=0):
     _check(lib.apar_add_weights(ctx, layer, q, lse, sm_scale, int(bool(replace)), stream))
+
+
+def apar_add_weights_prefill(ctx, layer: int, tid, q_begin, q_count, q: int, lse: int,
+                             sm_scale: float, replace: bool, stream=0):
+    _check(lib.apar_add_weights_prefill(ctx, layer, *_lists(tid, q_begin, q_count), q, lse, sm_scale,
+                                        int(bool(replace)), stream))
 
 
 def apar_read_weights(ctx, layer: int, tid, begin, count, out: int, stream=0):

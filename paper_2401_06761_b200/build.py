@@ -10,7 +10,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libapar.so")
 SOURCES = ["apar_api.cu", "planner.cpp", "kernels.cu", "attn_umma.cu", "attn_prefill.cu", "attn_ws.cu", "attn_static.cu", "tensor_maps.cu",
            "kv4.cu", "attn_q4.cu", "attn_q4_wide.cu",
-           "rope.cu", "beam.cu", "weights.cu"]
+           "rope.cu", "beam.cu", "weights.cu", "weights_prompt.cu"]
 HEADERS = ["apar_internal.h", "ptx.cuh", "tcgen05.cuh", "kv4.cuh", os.path.join("..", "..", "include", "apar.h")]
 
 

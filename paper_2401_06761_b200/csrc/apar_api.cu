@@ -713,23 +713,31 @@ apar_status upload(apar_ctx* c, const void* src, size_t bytes, char* dst, cudaSt
 apar_status send_key_plan(apar_ctx* c, const std::vector<KeyRun>& runs, const std::vector<KeyUser>& users,
                           int chunk, std::vector<KeyUnit>* units, cudaStream_t st) {
   units->clear();
-  for (const KeyRun& r : runs) {
-    const bool open = r.tok_end < 0;
-    const int end = open ? r.tok_begin - r.tok_end - 1 : r.tok_end;
-    for (int t = r.tok_begin; t < end; t += chunk) {
-      const bool last = t + chunk >= end;
-      units->push_back(KeyUnit{r.table_row, t, last && open ? -(end - t) - 1 : std::min(end, t + chunk),
+  for (const KeyRun& r : runs)
+    for (int t = r.tok_begin; t < r.tok_end; t += chunk) {
+      const bool last = t + chunk >= r.tok_end;
+      units->push_back(KeyUnit{r.table_row, t, last && r.open ? -(r.tok_end - t) - 1 : std::min(r.tok_end, t + chunk),
                                r.user_begin, r.n_users, {0, 0, 0}});
     }
-  }
   if ((int64_t)units->size() > c->wlay.unit_cap || (int64_t)users.size() > c->wlay.user_cap)
     return APAR_ERR_WORKSPACE_TOO_SMALL;
-  auto cost = [](const KeyUnit& u) {
-    const int64_t keys = u.tok_end < 0 ? -u.tok_end - 1 : u.tok_end - u.tok_begin;
-    return keys * (1 + u.n_users);
-  };
-  std::stable_sort(units->begin(), units->end(),
-                   [&](const KeyUnit& a, const KeyUnit& b) { return cost(a) > cost(b); });
+  // (queries that see the unit's keys, or all but a few of them)
+  std::vector<int64_t> cost(units->size());
+  std::vector<int32_t> order(units->size());
+  for (size_t i = 0; i < units->size(); ++i) {
+    const KeyUnit& u = (*units)[i];
+    int64_t queries = 0;
+    for (int x = 0; x < u.n_users; ++x) {
+      const KeyUser& user = users[u.user_begin + x];
+      queries += user.count - (user.count > 1 ? std::max(0, std::min(user.count, u.tok_begin - user.lim)) : 0);
+    }
+    cost[i] = (u.tok_end < 0 ? -u.tok_end - 1 : u.tok_end - u.tok_begin) * (1 + queries);
+    order[i] = (int32_t)i;
+  }
+  std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return cost[a] > cost[b]; });
+  std::vector<KeyUnit> sorted(units->size());
+  for (size_t i = 0; i < order.size(); ++i) sorted[i] = (*units)[order[i]];
+  units->swap(sorted);
   apar_status rc = upload(c, units->data(), units->size() * sizeof(KeyUnit), c->weights + c->wlay.units, st);
   if (rc == APAR_OK)
     rc = upload(c, users.data(), users.size() * sizeof(KeyUser), c->weights + c->wlay.users, st);
@@ -750,6 +758,7 @@ KeyArgs key_args(apar_ctx* c, int layer, const void* q, const float* lse, float 
   a.scale_log2e = sm_scale * 1.4426950408889634f;
   a.replace = replace != 0;
   a.num_sms = c->num_sms;
+  a.d_error = (int*)c->ws(c->lay.err);
   return a;
 }
 
@@ -1850,7 +1859,7 @@ apar_status apar_add_weights(apar_ctx* c, int32_t layer, const void* q, const fl
     if (!c->planner.key_runs(qs.data(), (int)qs.size(), &runs, &users)) return APAR_ERR_INVALID_ARG;
     // units of even length, some four to a warp of the machine where there is that much
     int64_t keys = 0;
-    for (const KeyRun& r : runs) keys += r.tok_end < 0 ? -r.tok_end - 1 : r.tok_end - r.tok_begin;
+    for (const KeyRun& r : runs) keys += r.tok_end - r.tok_begin;
     const int64_t share = keys * c->cfg.num_kv_heads / ((int64_t)c->num_sms * 64);
     int64_t chunk = std::min<int64_t>(1024, std::max<int64_t>(64, (share + 15) / 16 * 16));
     std::vector<KeyUnit> units;
@@ -1860,6 +1869,50 @@ apar_status apar_add_weights(apar_ctx* c, int32_t layer, const void* q, const fl
     c->key_plan_valid = true;
   }
   APAR_CUDA(c, launch_key_weights(key_args(c, layer, q, lse, sm_scale, replace), c->n_key_units, st));
+  ++c->kernels_total;
+  return APAR_OK;
+}
+
+apar_status apar_add_weights_prefill(apar_ctx* c, int32_t layer, int32_t n, const int32_t* tid,
+                                     const int32_t* q_begin, const int32_t* q_count, const void* q,
+                                     const float* lse, float sm_scale, int32_t replace,
+                                     void* cuda_stream) {
+  if (!c || n < 0 || layer < 0 || layer >= c->num_layers ||
+      (n > 0 && (!tid || !q_begin || !q_count || !q || !lse)) || ((uintptr_t)q & 15) || ((uintptr_t)lse & 3))
+    return APAR_ERR_INVALID_ARG;
+  if (c->host_only || c->q4) return APAR_ERR_UNSUPPORTED;
+  if (!c->weights) return APAR_ERR_INVALID_ARG;
+  if (n == 0) return APAR_OK;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  std::vector<int32_t> slots(n);
+  std::vector<KeyQuery> qs(n);
+  int64_t total_q = 0;
+  for (int i = 0; i < n; ++i) {
+    const int s = slot_of(c, tid[i]);
+    if (s < 0) return APAR_ERR_BAD_THREAD;
+    if (q_begin[i] < 0 || q_count[i] < 1 || (int64_t)q_begin[i] + q_count[i] > c->slots[s].len)
+      return APAR_ERR_INVALID_ARG;
+    slots[i] = s;
+    qs[i] = KeyQuery{c->row(s), s, q_begin[i] + q_count[i], false,
+                     KeyUser{(int32_t)total_q, q_begin[i], q_count[i], 0}};
+    total_q += q_count[i];
+    if (total_q > INT32_MAX) return APAR_ERR_INVALID_ARG;
+  }
+  apar_status rc = refuse_capture(c, st);
+  if (rc) return rc;
+  CUtensorMap tm_q;
+  if (make_query_tensor_map(q, total_q, c->shape.num_q_heads, c->shape.group, &tm_q) != 0)
+    return APAR_ERR_INVALID_ARG;
+  std::vector<KeyRun> runs;
+  std::vector<KeyUser> users;
+  std::vector<KeyUnit> units;
+  if (!c->planner.key_runs(qs.data(), n, &runs, &users)) return APAR_ERR_INVALID_ARG;
+  c->key_plan_valid = false;                             // (this plan takes the place of the other's)
+  rc = send_key_plan(c, runs, users, kPromptUnit, &units, st);
+  if (rc == APAR_OK) rc = sync_device_tables(c, slots.data(), n, st);
+  if (rc) return rc;
+  APAR_CUDA(c, launch_prompt_weights(key_args(c, layer, q, lse, sm_scale, replace), &c->tm_k[layer], &tm_q,
+                                     (int)units.size(), st));
   ++c->kernels_total;
   return APAR_OK;
 }

@@ -262,8 +262,9 @@ struct KeyUnit {
 };
 struct KeyUser {
   int32_t query;                 // the (first) query
-  int32_t lim;                   // keys before this position are seen (by the first query)
-  int32_t count, pad;            // consecutive queries; each sees one key more than the one before
+  int32_t lim;                   // one query: keys before this position are seen; a run of queries: the
+                                 // first one's position, the last key that it sees
+  int32_t count, pad;            // queries of the run
 };
 struct KeyArgs {
   const void* q;
@@ -278,6 +279,7 @@ struct KeyArgs {
   float scale_log2e;
   int replace;                   // 1: the keys' old weights do not count
   int num_sms;
+  int* d_error;                  // set when a bounded wait gave up
 };
 struct RowRange {
   int32_t table_row, begin, count, pad;
@@ -311,6 +313,11 @@ cudaError_t launch_weights_move(float* w, size_t layer_floats, int num_layers, c
                                 const int32_t* d_group_begin, int n_groups, int num_kv_heads,
                                 cudaStream_t st);
 cudaError_t launch_key_weights(const KeyArgs& a, int n_units, cudaStream_t st);
+// Units of at most 256 keys, closed; a user is a run of queries, the first at position lim.  tm_q as in
+// launch_attention_prefill.
+constexpr int kPromptUnit = 256;
+cudaError_t launch_prompt_weights(const KeyArgs& a, const CUtensorMap* tm_k, const CUtensorMap* tm_q,
+                                  int n_units, cudaStream_t st);
 cudaError_t launch_weights_read(const float* w, const int32_t* d_tables, int table_stride,
                                 const RowRange* d_ranges, int n, int max_count, int num_kv_heads,
                                 float* out, cudaStream_t st);
@@ -371,7 +378,9 @@ struct KeyQuery {
   KeyUser user;
 };
 struct KeyRun {
-  int32_t table_row, tok_begin, tok_end;   // tok_end < 0: open, the planned length folded as in WorkItem
+  int32_t table_row, tok_begin, tok_end;   // tok_end: past the last key that any of the queries sees
+  int32_t n_blocks;
+  bool open;                               // ends with the thread, wherever that is by then
   int32_t user_begin, n_users;
 };
 

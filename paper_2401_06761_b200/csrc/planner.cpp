@@ -406,16 +406,14 @@ bool Planner::key_runs(const KeyQuery* q, int n, std::vector<KeyRun>* runs,
       for (e1 = e0 + 1; e1 < ne && cnt_[q[i].table[e1]] == cnt_[b0]; ++e1) {}
       if (seg_of_[b0] < 0) {
         seg_of_[b0] = (int32_t)runs->size();
-        runs->push_back(KeyRun{q[i].table_row, e0 * kBlock, e1 * kBlock, 0, 0});
+        runs->push_back(KeyRun{q[i].table_row, e0 * kBlock, e0 * kBlock, e1 - e0, false, 0, 0});
       }
       KeyRun& r = (*runs)[seg_of_[b0]];
-      if (r.tok_begin != e0 * kBlock || (r.tok_end < 0 ? -r.tok_end - 1 : r.tok_end - r.tok_begin) !=
-                                            (e1 - e0) * kBlock)
-        return false;
+      if (r.tok_begin != e0 * kBlock || r.n_blocks != e1 - e0) return false;
+      r.tok_end = std::max(r.tok_end, std::min(e1 * kBlock, q[i].len));
       // the end of a thread's chain: nobody else lists its last block, or only after a fork at a full
       // block, where a row more would open a block of its own (and a new plan)
-      if (e1 == ne && q[i].open && r.tok_end >= 0 && r.table_row == q[i].table_row)
-        r.tok_end = -(r.tok_end - r.tok_begin) - 1;
+      if (e1 == ne && q[i].open && r.table_row == q[i].table_row) r.open = true;
       ++r.n_users;
       seg_users_.push_back(SegUser{seg_of_[b0], i, 0});
     }

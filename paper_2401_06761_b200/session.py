@@ -296,6 +296,16 @@ class PagedSession:
         B.apar_add_weights(self.ctx, layer, q.data_ptr(), lse.data_ptr(),
                            self.sm_scale if sm_scale is None else sm_scale, replace, self._stream())
 
+    def add_weights_prefill(self, tids, q_begin, q_count, q: torch.Tensor, lse: torch.Tensor,
+                            layer: int = 0, sm_scale=None, replace: bool = False):
+        """The same for runs of queries, as prefill_attention takes them."""
+        assert q.is_cuda and q.is_contiguous() and q.dtype == torch.bfloat16
+        assert lse.is_cuda and lse.is_contiguous() and lse.dtype == torch.float32
+        assert lse.shape == q.shape[:2] and q.shape[0] == sum(q_count)
+        B.apar_add_weights_prefill(self.ctx, layer, tids, q_begin, q_count, q.data_ptr(),
+                                   lse.data_ptr(), self.sm_scale if sm_scale is None else sm_scale,
+                                   replace, self._stream())
+
     def read_weights(self, tids, begin, count, layer: int = 0):
         """Weights [rows][kv heads] of rows begin[i] .. begin[i] + count[i] - 1 of each chain."""
         count = B.int32_array(count)

@@ -341,6 +341,107 @@ def test_reorder_moves_chains():
             assert np.abs(out[i].double().cpu().numpy() - np.einsum("hn,hnd->hd", p, v)).max() <= 2e-2
 
 
+def add_segments(f, segments, q, layer=0, replace=False):
+    """The definition for runs of queries (thread, first, count); returns lse and the bound."""
+    qq = q.double().cpu().numpy()
+    if replace:
+        for t, b, c in segments:
+            for x in f.names[t][:b + c]:
+                f.w[x][layer] = 0
+    lse, size, at = [], 1.0, 0
+    for t, b, c in segments:
+        k = np.stack([f.k[x][layer] for x in f.names[t][:b + c]], 1)
+        k = np.repeat(k, f.hq // f.hk, 0)
+        s = SCALE * np.einsum("qhd,hnd->hqn", qq[at:at + c], k)
+        s[:, np.arange(b + c)[None, :] > b + np.arange(c)[:, None]] = -np.inf
+        l = np.logaddexp.reduce(s, 2)
+        p = np.exp(s - l[..., None]).sum(1).reshape(f.hk, -1, b + c).sum(1)
+        for j, x in enumerate(f.names[t][:b + c]):
+            f.w[x][layer] += p[:, j]
+        lse.append(l.T)
+        big = SCALE * np.einsum("qhd,hnd->hqn", np.abs(qq[at:at + c]), np.abs(k)).max()
+        size, at = max(size, big, np.abs(l).max()), at + c
+    return np.concatenate(lse), size * 24 * 2.0 ** -23 + 2.0 ** -20
+
+
+@pytest.mark.parametrize("hq,hk", HEADS + [(5, 1)])
+def test_weights_of_prompts(hq, hk):
+    f, tids = small_forest(hq, hk, layers=2, prompt=301)
+    n = [len(f.names[t]) for t in tids]
+    # whole prompts; children from their own first row on; windows, one query, the same thread twice
+    segments = [(tids[0], 0, n[0]), (tids[1], 0, n[1])]
+    segments += [(t, 301, m - 301) for t, m in zip(tids[2:5], n[2:5])]
+    segments += [(tids[6], n[6] - 3, 3), (tids[5], n[5] - 1, 1), (tids[0], 100, 7), (tids[0], 0, 1)]
+    q = rows(sum(c for _, _, c in segments), hq, 21)
+    ids, begin, count = (list(x) for x in zip(*segments))
+    for layer in (0, 1):
+        lse = torch.empty(q.shape[:2], device="cuda")
+        f.s.prefill_attention(ids, begin, count, q, layer=layer, lse=lse)
+        want, rel = add_segments(f, segments, q, layer)
+        assert np.abs(lse.cpu().numpy() - want).max() <= rel
+        f.s.add_weights_prefill(ids, begin, count, q, lse, layer=layer)
+        f.check_weights(tids, rel, layer)
+        some = segments[2:4]
+        part = q[n[0] + n[1]:][:sum(c for _, _, c in some)].contiguous()
+        lse2 = lse[n[0] + n[1]:][:len(part)].contiguous()
+        f.s.add_weights_prefill(*(list(x) for x in zip(*some)), part, lse2, layer=layer, replace=True)
+        add_segments(f, some, part, layer, replace=True)
+        f.check_weights(tids, rel, layer)
+    assert B.apar_get_stats(f.s.ctx)["device_wait_timeouts"] == 0
+
+
+@pytest.mark.parametrize("n,count", [(1, 1), (16, 16), (17, 17), (128, 128), (129, 2), (256, 256),
+                                     (257, 257), (400, 130), (1025, 1025), (2000, 1), (2000, 33)])
+@pytest.mark.parametrize("hq,hk", [(8, 1), (2, 2)])
+def test_weights_of_prompts_of_many_lengths(n, count, hq, hk):
+    f = Forest(hq, hk)
+    (t,) = f.new(1)
+    f.append([t], [n])
+    q = rows(count, hq, n)
+    segments = [(t, n - count, count)]
+    lse = torch.empty(count, hq, device="cuda")
+    f.s.prefill_attention([t], [n - count], [count], q, lse=lse)
+    _, rel = add_segments(f, segments, q)
+    f.s.add_weights_prefill([t], [n - count], [count], q, lse)
+    f.check_weights([t], rel)
+    # a decode step's weights after it: each has a plan of its own
+    q1, lse1 = rows(1, hq, n + 1), torch.empty(1, hq, device="cuda")
+    f.s.attention([t], q1, lse=lse1)
+    f.s.add_weights(q1, lse1)
+    f.s.add_weights_prefill([t], [n - count], [count], q, lse)
+    f.s.add_weights(q1, lse1)
+    f.add([t], q1)
+    f.add([t], q1)
+    add_segments(f, segments, q)
+    f.check_weights([t], rel)
+    assert B.apar_get_stats(f.s.ctx)["device_wait_timeouts"] == 0
+
+
+def test_weights_of_prompts_in_many_units():
+    """More units than CTAs, of different lengths; the same bits every time; the sum of a query's
+    weights is the number of heads of a group."""
+    s = PagedSession(LayerShape(32, 8), 1500, 16, 200, weights=True)
+    tids = s.new_threads(9)
+    n = [2100, 1, 700, 1999, 64, 333, 16, 2500, 1300]
+    s.append(tids, n, rows(sum(n), 8, 1, 2.0), rows(sum(n), 8, 2))
+    q = rows(sum(n), 32, 3)
+    lse = torch.empty(sum(n), 32, device="cuda")
+    zero = [0] * 9
+    s.prefill_attention(tids, zero, n, q, lse=lse)
+    s.add_weights_prefill(tids, zero, n, q, lse)
+    first = s.read_weights(tids, zero, n)
+    at = 0
+    for m in n:
+        total = first[at:at + m].double().sum(0).cpu().numpy()
+        # every weight within 1e-4 of its own (scores are below 2^6 here; see Forest.add)
+        assert np.abs(total - 4 * m).max() <= 4 * m * 1e-4
+        at += m
+    for _ in range(3):
+        s.add_weights_prefill(tids, zero, n, q, lse, replace=True)
+        assert torch.equal(s.read_weights(tids, zero, n), first)
+    assert B.apar_get_stats(s.ctx)["device_wait_timeouts"] == 0
+
+
 def place(w, keep):
     """Rows that stay, by place, of weights w [n]: NaN first, then by weight, ties to the earlier."""
     key = [(not math.isnan(x), 0 if math.isnan(x) else -x, i) for i, x in enumerate(w)]
@@ -535,6 +636,14 @@ def test_refusals():
     refused("BAD_THREAD", s.read_weights, [999], [0], [1])
     refused("INVALID_ARG", s.read_weights, [tids[0]], [0], [1], layer=1)
     assert s.read_weights([tids[0]], [3], [0]).shape == (0, 2)
+    m = len(f.names[tids[0]])
+    for begin, count in ((0, 0), (-1, 2), (m, 1), (m - 1, 2)):
+        refused("INVALID_ARG", B.apar_add_weights_prefill, s.ctx, 0, [tids[0]], [begin], [count],
+                q.data_ptr(), lse.data_ptr(), 1.0, False)
+    refused("BAD_THREAD", B.apar_add_weights_prefill, s.ctx, 0, [999], [0], [1], q.data_ptr(),
+            lse.data_ptr(), 1.0, False)
+    refused("INVALID_ARG", B.apar_add_weights_prefill, s.ctx, 0, [tids[0]], [0], [1],
+            q.data_ptr() + 2, lse.data_ptr(), 1.0, False)
     refused("INVALID_ARG", B.apar_attach_weights, s.ctx, s._weights_memory.data_ptr() + 16, 1 << 40)
     refused("WORKSPACE_TOO_SMALL", B.apar_attach_weights, s.ctx, s._weights_memory.data_ptr(), 1024)
     B.apar_attach_weights(s.ctx, 0, 0)
