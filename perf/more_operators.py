@@ -305,13 +305,21 @@ def prepare(case, seed):
                         case["prompt"] + max(e - b for _, b, e in threads))
         tids = _forked(sess, prompts, threads, k, k)
         sess.attention(tids, q)               # (the step whose weights are summed)
-        # each row once: a prompt through the first of its threads
+        # each row once: a prompt through the first of its threads; and behind all of them what the other
+        # threads' copies of a prompt's last, partial block have received
         where = {}
         for t, (r, b, e) in zip(tids, threads):
             if case["prompt"]:
                 where.setdefault(prompts[r][0], (t, 0, case["prompt"]))
             where[b] = (t, case["prompt"], e - b)
         rows = [where[at] for at in sorted(where)]
+        part = case["prompt"] % 16
+        state["copied"] = None
+        if part and case["children"] > 1:
+            for c in range(1, case["children"]):
+                rows += [(t, case["prompt"] - part, part) for t in tids[c::case["children"]]]
+            state["copied"] = torch.cat([torch.arange(e - part, e) for _, e in prompts]).cuda()
+            state["total"] = total
         state.update(sess=sess, tids=[x[0] for x in rows], begin=[x[1] for x in rows],
                      count=[x[2] for x in rows])
         return state
@@ -402,7 +410,12 @@ def run(state):
     if kind == "weights":
         if own:
             state["sess"].add_weights(state["q"], state["lse"], replace=True)
-            return state["sess"].read_weights(state["tids"], state["begin"], state["count"])
+            w = state["sess"].read_weights(state["tids"], state["begin"], state["count"])
+            if state["copied"] is None:
+                return w
+            w, copies = w[:state["total"]], w[state["total"]:]
+            w[state["copied"]] += copies.view(-1, len(state["copied"]), w.shape[1]).sum(0)
+            return w
         return _plain_weights(state)
     if kind == "prompt":
         if own:
