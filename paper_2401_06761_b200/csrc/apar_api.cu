@@ -342,7 +342,7 @@ apar_status sync_device_tables(apar_ctx* c, const int32_t* slots, int n, cudaStr
     int32_t* pairs = (int32_t*)(s->host + (size_t)max_entries * sizeof(TableDelta));
     int32_t* data = pairs + 2 * (size_t)max_entries;
     const size_t data_cap = (cap - ((char*)data - s->host)) / 4;
-    int nd = 0, np = 0;
+    int nd = 0, np = 0, longest = 0;
     size_t used = 0;
     const uint32_t mk = next_mark(c);
     for (; i < n; ++i) {
@@ -356,6 +356,7 @@ apar_status sync_device_tables(apar_ctx* c, const int32_t* slots, int n, cudaStr
         deltas[nd++] = TableDelta{slots[i], t.synced, need, (int32_t)used};
         memcpy(data + used, c->row(slots[i]) + t.synced, (size_t)need * 4);
         used += need;
+        longest = std::max(longest, need);
         t.synced = t.n_blocks;
       }
       if (t.dev_len != t.len) {
@@ -386,7 +387,7 @@ apar_status sync_device_tables(apar_ctx* c, const int32_t* slots, int n, cudaStr
     APAR_CUDA(c, launch_sync((int32_t*)c->ws(c->lay.tables), c->cfg.max_blocks_per_thread,
                              (int32_t*)c->ws(c->lay.lens), (const TableDelta*)src,
                              (const int32_t*)(src + off_data), nd,
-                             (const int32_t*)(src + off_pairs), np, st));
+                             (const int32_t*)(src + off_pairs), np, longest, st));
     if (s->mapped) {
       rc = send(c, s, nullptr, 0, st);      // nothing to copy: only marks the buffer in flight
       if (rc) return rc;
@@ -2039,7 +2040,7 @@ apar_status apar_evict(apar_ctx* c, int32_t n, const int32_t* tid, const int32_t
   std::vector<EvictEntry> entries;
   std::vector<int32_t> dst;
   const int lh = c->num_layers * c->cfg.num_kv_heads;
-  int32_t max_rows = 0;
+  int32_t max_rows = 0, max_len = 0;
   int64_t list = 0;
   std::vector<int32_t> dst_of(st_list.size(), 0);
   for (size_t k = 0; k < st_list.size(); ++k) {
@@ -2052,6 +2053,7 @@ apar_status apar_evict(apar_ctx* c, int32_t n, const int32_t* tid, const int32_t
     entries.push_back(EvictEntry{slots[k], begin[f], rows, keep[f], x.in_place, dst_of[k], cap, 0, list});
     list += (int64_t)cap * lh;
     max_rows = std::max(max_rows, cap);
+    max_len = std::max(max_len, rows);
   }
   // ---- tables, groups and lengths
   for (int i = 0; i < n; ++i) {
@@ -2136,7 +2138,7 @@ apar_status apar_evict(apar_ctx* c, int32_t n, const int32_t* tid, const int32_t
   a.layer_floats = c->layer_weights();
   a.moves = (int2*)(c->weights + c->wlay.moves);
   a.counts = (int32_t*)(c->weights + c->wlay.counts);
-  APAR_CUDA(c, launch_evict(a, (int)entries.size(), c->num_layers, max_rows, st));
+  APAR_CUDA(c, launch_evict(a, (int)entries.size(), c->num_layers, max_len, max_rows, st));
   c->kernels_total += 2;
   return APAR_OK;
 }

@@ -140,10 +140,11 @@ cudaError_t launch_stream_read(const void* src, size_t bytes, void* sink, int nu
 cudaError_t launch_append(void* k_pool, void* v_pool, const void* k_new, const void* v_new,
                           const int32_t* d_slots, int64_t first_row, int n_rows,
                           int num_kv_heads, cudaStream_t st);
-// Applies table deltas and (row, length) pairs to the device copies in one launch.
+// Applies table deltas and (row, length) pairs to the device copies in one launch; max_count: entries
+// of the longest delta.
 cudaError_t launch_sync(int32_t* d_tables, int table_stride, int32_t* d_lens,
                         const TableDelta* d_deltas, const int32_t* d_data, int n_deltas,
-                        const int32_t* d_len_pairs, int n_pairs, cudaStream_t st);
+                        const int32_t* d_len_pairs, int n_pairs, int max_count, cudaStream_t st);
 
 // One decode step on the device: lens[row] += 1 for the n rows in d_step_rows, slot of each new
 // row into d_slot_map; d_pairs (int4: list position, row, table position, block id) are the
@@ -321,8 +322,9 @@ cudaError_t launch_prompt_weights(const KeyArgs& a, const CUtensorMap* tm_k, con
 cudaError_t launch_weights_read(const float* w, const int32_t* d_tables, int table_stride,
                                 const RowRange* d_ranges, int n, int max_count, int num_kv_heads,
                                 float* out, cudaStream_t st);
-// max_rows: rows the entry that moves most may move.
-cudaError_t launch_evict(const EvictArgs& a, int n, int num_layers, int max_rows, cudaStream_t st);
+// max_len: rows of the longest stretch; max_rows: rows the entry that moves most may move.
+cudaError_t launch_evict(const EvictArgs& a, int n, int num_layers, int max_len, int max_rows,
+                         cudaStream_t st);
 
 // ---- planner (planner.cpp) ----
 // A run of consecutive table positions whose blocks are held by the same set of threads

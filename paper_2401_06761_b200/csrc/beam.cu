@@ -5,16 +5,17 @@
 // enough: it keeps, per piece of a row, the num_select largest logits and the piece's maximum and sum
 // of exponentials, and a second small kernel puts the pieces of a sequence's rows together.
 //
-// beam_scan_kernel   one CTA of eight warps per piece; the warps run on their own.  A warp reads 256
-//     consecutive elements at a time, eight per lane, and compares them with a threshold that at least
-//     num_select of its elements are above or equal to; the few that pass go into a buffer of 128 in
-//     shared memory, which is sorted and cut back to num_select when it fills up, and the threshold
-//     rises.  The first threshold is the num_select-th largest of the maxima of 64 groups of sixteen
-//     elements.  A key is (ordered bits of the logit, complement of the token): of equal logits the
-//     lower token is kept.
-// beam_pick_kernel   one warp per sequence: each lane looks after the heads of some of the sorted
-//     lists, num_select rounds of a maximum over the warp.  Scores of different beams are compared in
-//     64 bits: their difference goes through two log-sum-exps, and 32 bits would round it.
+// beam_scan_kernel   one CTA per piece, which reads up to 16384 elements into registers, 64 to a
+//     thread, all loads on their way at once.  A threshold that at least num_select elements reach comes
+//     from the threads' maxima: with j = num_select / 8 rounded up, the least of the eight warps' j-th
+//     largest.  The few elements that reach it (some two to three times num_select) are collected in shared
+//     memory and put in order by counting, for each, how many are larger.  A key is (ordered bits of
+//     the logit, complement of the token): of equal logits the lower token is kept.  Where more than
+//     512 elements reach the threshold (many equal ones) the warps go over the piece again with
+//     buffers that they sort and cut back as they fill.
+// beam_pick_kernel   one CTA per sequence, the same way over the pieces' lists.  Values of different
+//     beams are compared in 64 bits: their difference goes through two log-sum-exps, and 32 bits would
+//     round it.
 #include <algorithm>
 #include <climits>
 
@@ -29,8 +30,11 @@
 namespace apar {
 namespace {
 
-constexpr int kWarps = 8;                     // of a scanning CTA
-constexpr int kBuf = 128;                     // keys a warp holds
+constexpr int kWarps = 8, kThreads = 32 * kWarps;
+constexpr int kGroups = 8;                    // groups of eight elements a thread holds
+constexpr int kChunk = kThreads * kGroups;    // groups a CTA holds
+constexpr int kCand = 512;                    // elements that may reach a threshold
+constexpr int kBuf = 128;                     // keys a warp holds where more do
 constexpr int kMaxSelect = 64, kMaxBeams = 64;
 constexpr int kMaxPieces = 16;                // of a row
 constexpr int kMaxLists = 128;                // pieces of a sequence's rows
@@ -42,7 +46,8 @@ __device__ __forceinline__ uint32_t ordered(float x) {   // (-0 counts as 0)
   const uint32_t b = __float_as_uint(x + 0.f);
   return b ^ (uint32_t)((int32_t)b >> 31 | 0x80000000);
 }
-__device__ __forceinline__ float unordered(uint32_t o) {
+__device__ __forceinline__ float unordered(uint32_t o) {   // (what is below -inf counts as that)
+  if (o < 0x007fffffu) return -INFINITY;
   return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
 }
 
@@ -108,37 +113,6 @@ __device__ __forceinline__ void load_group(const T* row, int vocab, int off, int
   }
 }
 
-// Sorts N keys, element N / 32 * lane + i in v[i], largest first.
-template <int N, typename T>
-__device__ __forceinline__ void warp_sort(T (&v)[N / 32], int lane) {
-  constexpr int P = N / 32;
-#pragma unroll
-  for (int size = 2; size <= N; size *= 2) {
-#pragma unroll
-    for (int d = size / 2; d > 0; d /= 2) {
-      if (d >= P) {
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-          const T o = __shfl_xor_sync(kAll, v[i], d / P);
-          const int at = lane * P + i;
-          const bool big = ((at & d) == 0) == ((at & size) == 0);   // keeps the larger of the two
-          v[i] = (o > v[i]) == big ? o : v[i];
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-          if (i & d) continue;
-          const bool down = ((lane * P + i) & size) == 0;
-          const T a = v[i], b = v[i | d];
-          const bool swap = (b > a) == down;
-          v[i] = swap ? b : a;
-          v[i | d] = swap ? a : b;
-        }
-      }
-    }
-  }
-}
-
 struct BeamArgs {
   const void* logits;
   int64_t seq_stride, beam_stride;   // elements
@@ -152,191 +126,282 @@ struct BeamArgs {
   int32_t *out_beam, *out_token;
 };
 
-// What a warp knows of its part of a row.
-struct Held {
-  u64* buf;                          // kBuf keys in shared memory
-  int n = 0;                         // of them in use
-  float tau = -INFINITY;             // smaller elements are of no interest,
-  u64 last = 0;                      // nor keys below this one
-  float m = -INFINITY, l = 0.f;      // of this lane's elements
-};
+// A value that at least `select` of the CTA's threads' maxima (as ordered integers) reach: the least of
+// the j-th largest of the first `full` warps, all of whose threads have something.  The least there is
+// where those warps are too few.  *most receives the largest of all.  `sh`: 2 * kWarps words.
+__device__ __forceinline__ uint32_t threshold(uint32_t mine, int select, int full, uint32_t* sh,
+                                              uint32_t* most) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint32_t rest = mine, top = __reduce_max_sync(kAll, mine);
+  if (lane == 0) sh[warp] = top;
+  full = min(full, kWarps);
+  if (full * 32 < select) full = 0;
+  for (int j = full ? (select + full - 1) / full : 0; j > 1; --j) {
+    // (one of those that hold the largest steps back)
+    if (lane == __ffs(__ballot_sync(kAll, rest == top)) - 1) rest = 0;
+    top = __reduce_max_sync(kAll, rest);
+  }
+  if (lane == 0) sh[kWarps + warp] = top;
+  __syncthreads();
+  uint32_t least = 0xffffffffu, m = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    m = max(m, sh[w]);
+    if (w < full) least = min(least, sh[kWarps + w]);
+  }
+  *most = m;
+  return full ? least : 0;
+}
 
-__device__ __forceinline__ void cut_back(Held& h, int select, int lane) {
+// ------------------------------------------------------------------ pieces with many equal elements
+__device__ __forceinline__ void warp_sort(u64 (&v)[kBuf / 32], int lane) {   // largest first
+  constexpr int P = kBuf / 32;
+#pragma unroll 1
+  for (int size = 2; size <= kBuf; size *= 2) {
+#pragma unroll 1
+    for (int d = size / 2; d >= P; d /= 2) {
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const u64 o = __shfl_xor_sync(kAll, v[i], d / P);
+        const int at = lane * P + i;
+        const bool big = ((at & d) == 0) == ((at & size) == 0);   // keeps the larger of the two
+        v[i] = (o > v[i]) == big ? o : v[i];
+      }
+    }
+#pragma unroll
+    for (int d = P / 2; d > 0; d /= 2) {
+      if (d >= size) continue;
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        if (i & d) continue;
+        const bool down = ((lane * P + i) & size) == 0;
+        const u64 a = v[i], b = v[i | d];
+        const bool swap = (b > a) == down;
+        v[i] = swap ? b : a;
+        v[i | d] = swap ? a : b;
+      }
+    }
+  }
+}
+
+// Cuts a warp's buffer of n keys back to its `select` largest, sorted; returns how many there are.
+__device__ __noinline__ int cut_back(u64* buf, int n, int select) {
+  const int lane = threadIdx.x & 31;
   u64 v[kBuf / 32];
 #pragma unroll
   for (int i = 0; i < kBuf / 32; ++i) {
     const int at = lane * (kBuf / 32) + i;
-    v[i] = at < h.n ? h.buf[at] : 0ull;
+    v[i] = at < n ? buf[at] : 0ull;
   }
   __syncwarp();
-  warp_sort<kBuf>(v, lane);
+  warp_sort(v, lane);
 #pragma unroll
-  for (int i = 0; i < kBuf / 32; ++i) h.buf[lane * (kBuf / 32) + i] = v[i];
+  for (int i = 0; i < kBuf / 32; ++i) buf[lane * (kBuf / 32) + i] = v[i];
   __syncwarp();
-  if (h.n >= select) {
-    h.n = select;
-    h.last = h.buf[select - 1];
-    h.tau = unordered((uint32_t)(h.last >> 32));
-  }
+  return min(n, select);
 }
 
-// One element per lane; -inf where a lane has none.
-__device__ __forceinline__ void offer(Held& h, float x, int token, int select, int lane) {
-  const u64 key = (u64)ordered(x) << 32 | (uint32_t)~token;
-  auto wanted = [&] { return x >= h.tau && x > -INFINITY && key > h.last; };   // (a NaN is not)
-  unsigned who = __ballot_sync(kAll, wanted());
-  if (who == 0) return;
-  if (h.n + 32 > kBuf) {                       // (more than num_select are held: cut back to that many)
-    cut_back(h, select, lane);
-    who = __ballot_sync(kAll, wanted());
+// The `select` largest of the groups [g0, g1) that reach tau, one warp; sorted into buf, their number
+// returned.
+template <typename T>
+__device__ int scan_again(const T* row, int vocab, int off, int g0, int g1, float tau, int select,
+                          u64* buf) {
+  const int lane = threadIdx.x & 31;
+  int n = 0;
+  u64 last = 0;                                // keys below this one are of no use
+  for (int g = g0; g < g1; g += 32) {
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = -INFINITY;
+    if (g + lane < g1) load_group(row, vocab, off, g + lane, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const u64 key = (u64)ordered(x[e]) << 32 | (uint32_t)~((g + lane) * 8 + e);
+      const bool in = x[e] >= tau && x[e] > -INFINITY;     // (a NaN is not)
+      unsigned who = __ballot_sync(kAll, in && key > last);
+      if (who == 0) continue;
+      if (n + 32 > kBuf) {                     // (more than num_select are held)
+        n = cut_back(buf, n, select);
+        last = buf[n - 1];
+        who = __ballot_sync(kAll, in && key > last);
+      }
+      if (who >> lane & 1) buf[n + __popc(who & ((1u << lane) - 1))] = key;
+      n += __popc(who);
+      __syncwarp();
+    }
   }
-  if (who >> lane & 1) h.buf[h.n + __popc(who & ((1u << lane) - 1))] = key;
-  h.n += __popc(who);
-  __syncwarp();
+  return cut_back(buf, n, select);
 }
+
+// ------------------------------------------------------------------ pieces of rows
+union ScanKeys {
+  u64 cand[kCand];
+  u64 bufs[kWarps][kBuf];
+};
 
 template <typename T>
-__global__ void __launch_bounds__(kWarps * 32) beam_scan_kernel(const BeamArgs a) {
-  __shared__ u64 bufs[kWarps][kBuf];
-  __shared__ int counts[kWarps];
-  __shared__ float2 sums[kWarps];
+__global__ void __launch_bounds__(kThreads, 2) beam_scan_kernel(const BeamArgs a) {
+  __shared__ ScanKeys sh;
+  __shared__ u64 held[kMaxSelect];             // the largest so far, in order
+  __shared__ uint32_t tops[2 * kWarps];
+  __shared__ float sums[kWarps];
+  __shared__ int counts[kWarps], n_cand;
   pdl_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int row = blockIdx.x / a.pieces, piece = blockIdx.x % a.pieces;
   const int seq = row / a.beams, beam = row % a.beams;
   const T* x = (const T*)a.logits + seq * a.seq_stride + beam * a.beam_stride;
-  Held h;
-  h.buf = bufs[warp];
-  const bool skip = a.finished && a.finished[row];   // (has its one continuation, see the other kernel)
-  if (!skip) {
-    const int off = (int)((uintptr_t)x & 15) / (int)sizeof(T);
-    const int groups = (a.vocab + 7) / 8;
-    const int per_piece = (groups + a.pieces - 1) / a.pieces;
-    const int per_warp = ((per_piece + kWarps - 1) / kWarps + 31) / 32 * 32;
-    const int end = min(groups, (piece + 1) * per_piece);
-    const int g0 = piece * per_piece + warp * per_warp, g1 = min(end, g0 + per_warp);
-    bool first = true;
-    for (int g = g0; g < g1; g += 128) {       // up to four groups a lane in flight
-      float v[4][8];
+  const int off = (int)((uintptr_t)x & 15) / (int)sizeof(T);
+  const int groups = (a.vocab + 7) / 8, per_piece = (groups + a.pieces - 1) / a.pieces;
+  const int end = min(groups, (piece + 1) * per_piece);
+  const bool skip = a.finished && a.finished[row];     // (has its one continuation, see the other kernel)
+  int n_held = 0;
+  float m = -INFINITY, l = 0.f;
+  for (int c0 = skip ? end : piece * per_piece; c0 < end; c0 += kChunk) {
+    float v[kGroups][8];
+    float mine = -INFINITY;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int at = g + 32 * u + lane;
-        if (at < g1) {
-          load_group(x, a.vocab, off, at, v[u]);
-        } else {
+    for (int u = 0; u < kGroups; ++u) {
+      const int at = c0 + u * kThreads + threadIdx.x;
+      if (at < end) {
+        load_group(x, a.vocab, off, at, v[u]);
+      } else {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[u][e] = -INFINITY;
-        }
-      }
-      if (first) {
-        // each group is half of what the lane holds
-        uint32_t top[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          float t = v[2 * k][0];
-#pragma unroll
-          for (int u = 2 * k; u < 2 * k + 2; ++u)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) t = fmaxf(t, v[u][e]);
-          top[k] = ordered(t == t ? t : -INFINITY);
-        }
-        warp_sort<64>(top, lane);
-        const int at = a.select - 1;           // (at least num_select elements are not below that one)
-        const uint32_t t0 = __shfl_sync(kAll, top[0], at >> 1), t1 = __shfl_sync(kAll, top[1], at >> 1);
-        h.tau = fmaxf(h.tau, unordered(at & 1 ? t1 : t0));
-        first = false;
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        float top = v[u][0];
-#pragma unroll
-        for (int e = 1; e < 8; ++e) top = fmaxf(top, v[u][e]);
-        if (top > h.m) {
-          h.l *= ex2((h.m - top) * kLog2e);
-          h.m = top;
-        }
-        // (x - m before the factor: rounding m log2 e would be the same error in every term)
-        const float ref = h.m == -INFINITY ? 0.f : h.m;
-        float part = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) part += ex2((v[u][e] - ref) * kLog2e);
-        h.l += part;
-        if (__any_sync(kAll, top >= h.tau)) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            offer(h, v[u][e], (g + 32 * u + lane) * 8 + e, a.select, lane);
-        }
+        for (int e = 0; e < 8; ++e) v[u][e] = -INFINITY;
       }
     }
-    cut_back(h, a.select, lane);
-    h.n = min(h.n, a.select);
+#pragma unroll
+    for (int u = 0; u < kGroups; ++u)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) mine = fmaxf(mine, v[u][e]);
+    if (threadIdx.x == 0) n_cand = n_held;
+    if ((int)threadIdx.x < n_held) sh.cand[threadIdx.x] = held[threadIdx.x];
+    uint32_t most;
+    float tau = unordered(threshold(ordered(mine == mine ? mine : -INFINITY), a.select,
+                                    min(end - c0, kChunk) / 32, tops, &most));
+    if (n_held == a.select) tau = fmaxf(tau, unordered((uint32_t)(held[n_held - 1] >> 32)));
+    // (x - max before the factor: rounding max log2 e would be the same error in every term)
+    const float ref = unordered(most) == -INFINITY ? 0.f : unordered(most);
+    float part = 0.f;
+#pragma unroll
+    for (int u = 0; u < kGroups; ++u) {
+      float p[2] = {0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e & 1] += ex2((v[u][e] - ref) * kLog2e);
+      part += p[0] + p[1];
+    }
+    if (mine >= tau && mine > -INFINITY) {
+#pragma unroll
+      for (int u = 0; u < kGroups; ++u)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (v[u][e] >= tau && v[u][e] > -INFINITY) {
+            const int i = atomicAdd(&n_cand, 1);
+            const uint32_t token = (c0 + u * kThreads + threadIdx.x) * 8 + e;
+            if (i < kCand) sh.cand[i] = (u64)ordered(v[u][e]) << 32 | ~token;
+          }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(kAll, part, o);
+    if (lane == 0) sums[warp] = part;
+    __syncthreads();
+    // maximum and sum so far
+    {
+      float s = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) s += sums[w];
+      const float top = fmaxf(m, unordered(most));
+      const float r = top == -INFINITY ? 0.f : top;
+      l = l * ex2((m - r) * kLog2e) + s * ex2((ref - r) * kLog2e);
+      m = top;
+    }
+    const int n = n_cand;
+    if (n <= kCand) {
+      // (each thread one or two of them; their order in the list does not matter)
+      for (int i = threadIdx.x; i < n; i += kThreads) {
+        const u64 key = sh.cand[i];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += sh.cand[j] > key;
+        if (rank < a.select) held[rank] = key;
+      }
+      n_held = min(n, a.select);
+      __syncthreads();
+    } else {
+      const int per_warp = (kChunk + kWarps - 1) / kWarps, first = c0 + warp * per_warp;
+      const int found = scan_again(x, a.vocab, off, first, min(min(end, c0 + kChunk), first + per_warp), tau,
+                                   a.select, sh.bufs[warp]);
+      if (lane == 0) counts[warp] = found;
+      __syncthreads();
+      // the warps' sorted lists and what is held become one list
+      u64 merged[kMaxSelect / 32] = {0ull, 0ull};
+      int n_new = 0;
+      if (warp == 0) {
+        const u64* list = lane < kWarps ? sh.bufs[lane] : held;
+        int at = 0, have = lane < kWarps ? counts[lane] : lane == kWarps ? n_held : 0;
+        for (int k = 0; k < a.select; ++k) {
+          const u64 head = at < have ? list[at] : 0ull;
+          u64 best = head;
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(kAll, best, o));
+          if (best == 0) break;
+          if (head == best) ++at;
+          if (lane == (k & 31)) merged[k >> 5] = best;
+          ++n_new;
+        }
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < kMaxSelect / 32; ++k) held[32 * k + lane] = merged[k];
+        if (lane == 0) n_cand = n_new;
+      }
+      __syncthreads();
+      n_held = n_cand;
+      __syncthreads();
+    }
   }
-  // maximum and sum of the warp
-  float m = h.m;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kAll, m, o));
-  float l = h.m == -INFINITY ? h.l : h.l * ex2((h.m - m) * kLog2e);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(kAll, l, o);
-  if (lane == 0) {
-    counts[warp] = h.n;
-    sums[warp] = make_float2(m, l);
-  }
-  __syncthreads();
-  if (warp != 0) return;
-  // the warps' sorted lists become one
-  const int mine = lane < kWarps ? lane : 0;
-  int at = 0, n = lane < kWarps ? counts[mine] : 0;
-  u64* out = a.keys + (size_t)blockIdx.x * a.select;
-  for (int k = 0; k < a.select; ++k) {
-    const u64 head = at < n ? bufs[mine][at] : 0ull;
-    u64 best = head;
-#pragma unroll
-    for (int o = kWarps / 2; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(kAll, best, o));
-    if (best != 0 && head == best) ++at;
-    if (lane == 0) out[k] = best;
-  }
-  float2 s = sums[mine];
-  float M = s.x;
-#pragma unroll
-  for (int o = kWarps / 2; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(kAll, M, o));
-  float L = s.x == -INFINITY ? s.y : s.y * ex2((s.x - M) * kLog2e);
-#pragma unroll
-  for (int o = kWarps / 2; o > 0; o >>= 1) L += __shfl_xor_sync(kAll, L, o);
-  if (lane == 0) a.stats[blockIdx.x] = make_float2(M, L);
+  if ((int)threadIdx.x < a.select)
+    a.keys[(size_t)blockIdx.x * a.select + threadIdx.x] = (int)threadIdx.x < n_held ? held[threadIdx.x] : 0ull;
+  if (threadIdx.x == 0) a.stats[blockIdx.x] = make_float2(m, l);
 }
 
+// ------------------------------------------------------------------ sequences
 // A pair's place in the order: larger value first, then lower beam, then lower token.
 struct Pair {
   double value;
-  uint32_t beam, token;
+  u64 at;                                      // beam << 32 | token
 };
 __device__ __forceinline__ bool before(const Pair& a, const Pair& b) {
-  if (a.value != b.value) return a.value > b.value;
-  return a.beam != b.beam ? a.beam < b.beam : a.token < b.token;
+  return a.value != b.value ? a.value > b.value : a.at < b.at;
 }
 
-__global__ void __launch_bounds__(32) beam_pick_kernel(const BeamArgs a) {
-  extern __shared__ u64 lists[];                       // [beams * pieces][select]
-  __shared__ double base[kMaxBeams];                   // score - lse; NaN: the beam has no pairs
-  const int lane = threadIdx.x, seq = blockIdx.x, n_lists = a.beams * a.pieces;
-  pdl_wait();                                          // (the scan has written its lists)
-  const u64* src = a.keys + (size_t)seq * n_lists * a.select;
-  for (int i = lane; i < n_lists * a.select; i += 32) lists[i] = src[i];
-  for (int b = lane; b < a.beams; b += 32) {
-    const int row = seq * a.beams + b;
+__global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
+  __shared__ Pair cand[kCand];
+  __shared__ double base[kMaxBeams];           // score - lse; NaN: the beam has no pairs
+  __shared__ float2 stats[kMaxLists];
+  __shared__ uint8_t over[kMaxBeams];
+  __shared__ uint32_t tops[2 * kWarps];
+  __shared__ Pair picks[kWarps];
+  __shared__ int n_cand;
+  const int seq = blockIdx.x, n_lists = a.beams * a.pieces, n_all = n_lists * a.select;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  pdl_wait();                                  // (the scan has written its lists)
+  if (threadIdx.x == 0) n_cand = 0;
+  for (int i = threadIdx.x; i < n_lists; i += kThreads) stats[i] = a.stats[(size_t)seq * n_lists + i];
+  __syncthreads();
+  if ((int)threadIdx.x < a.beams) {
+    const int b = threadIdx.x, row = seq * a.beams + b;
     const float score = a.scores[row];
+    over[b] = a.finished && a.finished[row];
     double to = NAN;
-    if (score - score == 0.f) {                        // finite
-      if (a.finished && a.finished[row]) {
+    if (score - score == 0.f) {                // finite
+      if (over[b]) {
         to = score;
       } else {
         float M = -INFINITY;
-        for (int p = 0; p < a.pieces; ++p) M = fmaxf(M, a.stats[row * a.pieces + p].x);
+        for (int p = 0; p < a.pieces; ++p) M = fmaxf(M, stats[b * a.pieces + p].x);
         double L = 0.0;
         for (int p = 0; p < a.pieces; ++p) {
-          const float2 s = a.stats[row * a.pieces + p];
-          L += s.x == -INFINITY ? (double)s.y : (double)s.y * exp((double)s.x - (double)M);
+          const float2 s = stats[b * a.pieces + p];
+          L += s.x == M || s.x == -INFINITY ? (double)s.y : (double)s.y * exp((double)s.x - (double)M);
         }
         const double lse = (double)M + log(L);
         if (lse - lse == 0.0) to = (double)score - lse;
@@ -344,65 +409,82 @@ __global__ void __launch_bounds__(32) beam_pick_kernel(const BeamArgs a) {
     }
     base[b] = to;
   }
-  __syncwarp();
-  // this lane's lists are lane, lane + 32, ...; at[j] is how far list j has been used
-  int at[kMaxLists / 32];
-#pragma unroll
-  for (int j = 0; j < kMaxLists / 32; ++j) at[j] = 0;
-  for (int k = 0; k < a.select; ++k) {
-    Pair best{-INFINITY, 0xffffffffu, 0xffffffffu};
-    int from = -1;
-#pragma unroll
-    for (int j = 0; j < kMaxLists / 32; ++j) {
-      const int list = lane + 32 * j;
-      if (list >= n_lists || at[j] >= a.select) continue;
-      const uint32_t b = list / a.pieces;
-      const double to = base[b];
-      Pair p;
-      p.beam = b;
-      if (a.finished && a.finished[seq * a.beams + b]) {
-        if (at[j] > 0 || list % a.pieces) continue;
-        p.value = to;
-        p.token = (uint32_t)a.eos;
-      } else {
-        const u64 key = lists[list * a.select + at[j]];
-        if (key == 0) continue;
-        p.value = to + (double)unordered((uint32_t)(key >> 32));
-        p.token = ~(uint32_t)key;
-      }
-      if (!(p.value > -INFINITY)) continue;            // (NaN: the beam has no pairs)
-      if (from < 0 || before(p, best)) {
-        best = p;
-        from = j;
-      }
+  __syncthreads();
+  // pair i of the lists; a value that is not above -inf: none
+  const u64* keys = a.keys + (size_t)seq * n_all;
+  auto pair_of = [&](int i) {
+    const int list = i / a.select, b = list / a.pieces;
+    if (over[b]) return Pair{i % (a.pieces * a.select) ? -INFINITY : base[b], (u64)b << 32 | (uint32_t)a.eos};
+    const u64 key = keys[i];
+    return Pair{key ? base[b] + (double)unordered((uint32_t)(key >> 32)) : -INFINITY,
+                (u64)b << 32 | (uint32_t)~(uint32_t)key};
+  };
+  float mine = -INFINITY;
+  for (int i = threadIdx.x; i < n_all; i += kThreads) {
+    const double x = pair_of(i).value;
+    if (x > -INFINITY) mine = fmaxf(mine, __double2float_rn(x));
+  }
+  uint32_t most;
+  const float tau = unordered(threshold(ordered(mine), a.select, n_all / 32, tops, &most));
+  for (int i = threadIdx.x; i < n_all; i += kThreads) {
+    const Pair p = pair_of(i);
+    if (p.value > -INFINITY && __double2float_rn(p.value) >= tau) {   // (rounding keeps the order)
+      const int at = atomicAdd(&n_cand, 1);
+      if (at < kCand) cand[at] = p;
     }
-    Pair w = best;
+  }
+  __syncthreads();
+  const int n = n_cand;
+  float* out_score = a.out_score + (size_t)seq * a.select;
+  int32_t* out_beam = a.out_beam + (size_t)seq * a.select;
+  int32_t* out_token = a.out_token + (size_t)seq * a.select;
+  auto put = [&](int k, const Pair& p) {       // (values are rounded once, here)
+    out_score[k] = (float)p.value;
+    out_beam[k] = (int32_t)(p.at >> 32);
+    out_token[k] = (int32_t)p.at;
+  };
+  const Pair none{-INFINITY, ~0ull};
+  if (n <= kCand) {
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+      const Pair p = cand[i];
+      int rank = 0;
+      for (int j = 0; j < n; ++j) rank += before(cand[j], p);
+      if (rank < a.select) put(rank, p);
+    }
+    if ((int)threadIdx.x >= n && (int)threadIdx.x < a.select) put(threadIdx.x, none);
+    return;
+  }
+  // many equal values: one pair after the other, each the first behind the one before
+  Pair last{INFINITY, 0};
+  for (int k = 0; k < a.select; ++k) {
+    Pair best = none;
+    for (int i = threadIdx.x; i < n_all; i += kThreads) {
+      const Pair p = pair_of(i);
+      if (p.value > -INFINITY && before(last, p) && before(p, best)) best = p;
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-      Pair x;
-      x.value = __shfl_xor_sync(kAll, w.value, o);
-      x.beam = __shfl_xor_sync(kAll, w.beam, o);
-      x.token = __shfl_xor_sync(kAll, w.token, o);
-      if (before(x, w)) w = x;
+      const Pair x{__shfl_xor_sync(kAll, best.value, o), __shfl_xor_sync(kAll, best.at, o)};
+      if (before(x, best)) best = x;
     }
+    if (lane == 0) picks[warp] = best;
+    __syncthreads();
 #pragma unroll
-    for (int j = 0; j < kMaxLists / 32; ++j)
-      if (j == from && best.beam == w.beam && best.token == w.token) ++at[j];
-    if (lane == 0) {
-      const size_t o = (size_t)seq * a.select + k;
-      a.out_score[o] = (float)w.value;                 // (rounded once; -inf where pairs ran out)
-      a.out_beam[o] = (int32_t)w.beam;
-      a.out_token[o] = (int32_t)w.token;
-    }
+    for (int w = 0; w < kWarps; ++w)
+      if (before(picks[w], best)) best = picks[w];
+    last = best;
+    if (threadIdx.x == 0) put(k, best);
+    __syncthreads();
   }
 }
 
-// Pieces of a row: enough CTAs to fill the machine twice over where there are few rows, none shorter
-// than 2048 elements.
+// Pieces of a row: what a CTA's registers hold, and more of them where there are few rows, to fill the
+// machine twice over, none shorter than 2048 elements.
 int pieces_of(const apar_beam_config* c, int32_t n_seq) {
   const int64_t rows = (int64_t)n_seq * c->num_beams;
-  int64_t p = std::min<int64_t>({kMaxPieces, (2 * 148 + rows - 1) / rows, (c->vocab + 2047) / 2048,
-                                 kMaxLists / c->num_beams});
+  const int64_t fit = (c->vocab + 8 * kChunk - 1) / (8 * kChunk);
+  int64_t p = std::min<int64_t>((2 * 148 + rows - 1) / rows, (c->vocab + 2047) / 2048);
+  p = std::min<int64_t>({std::max(p, fit), kMaxPieces, kMaxLists / c->num_beams});
   return (int)std::max<int64_t>(1, p);
 }
 
@@ -465,13 +547,8 @@ extern "C" apar_status apar_beam_select(const apar_beam_config* cfg, int32_t n_s
   auto scan = cfg->logits_type == APAR_LOGITS_F32   ? beam_scan_kernel<float>
               : cfg->logits_type == APAR_LOGITS_F16 ? beam_scan_kernel<__half>
                                                     : beam_scan_kernel<__nv_bfloat16>;
-  const size_t smem = (size_t)a.beams * a.pieces * a.select * sizeof(u64);
-  cudaError_t e = cudaSuccess;
-  if (smem > 48 * 1024)
-    e = cudaFuncSetAttribute(beam_pick_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             kMaxLists * kMaxSelect * (int)sizeof(u64));
-  if (e == cudaSuccess) e = launch_kernel(scan, dim3(lists), dim3(kWarps * 32), 0, st, false, a);
-  if (e == cudaSuccess) e = launch_kernel(beam_pick_kernel, dim3(n_seq), dim3(32), smem, st, true, a);
+  cudaError_t e = launch_kernel(scan, dim3(lists), dim3(kThreads), 0, st, false, a);
+  if (e == cudaSuccess) e = launch_kernel(beam_pick_kernel, dim3(n_seq), dim3(kThreads), 0, st, true, a);
   if (e != cudaSuccess) {
     note_cuda_error(e);
     return APAR_ERR_CUDA;

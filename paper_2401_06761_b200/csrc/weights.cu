@@ -160,31 +160,230 @@ __global__ void __launch_bounds__(kKeyWarps * 32, 2) key_weights_kernel(const Ke
 }
 
 // ------------------------------------------------------------------ read back
+// One warp per block: its weights are one contiguous piece of the pool, and so are its rows of the output.
 __global__ void __launch_bounds__(256) weights_read_kernel(const float* __restrict__ w,
                                                            const int32_t* __restrict__ tables, int stride,
                                                            const RowRange* __restrict__ ranges,
                                                            int num_kv_heads, float* __restrict__ out) {
   const RowRange r = ranges[blockIdx.y];
-  const int64_t n = (int64_t)r.count * num_kv_heads;
-  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
-    const int pos = r.begin + (int)(i / num_kv_heads), h = (int)(i % num_kv_heads);
-    const int block = tables[(size_t)r.table_row * stride + (pos >> 4)];
-    out[r.first * num_kv_heads + i] = w[((size_t)block * num_kv_heads + h) * kBlock + (pos & 15)];
+  const int lane = threadIdx.x & 31, last = (r.begin + r.count - 1) / kBlock;
+  for (int b = r.begin / kBlock + blockIdx.x * 8 + (threadIdx.x >> 5); b <= last; b += gridDim.x * 8) {
+    const float* src = w + (size_t)tables[(size_t)r.table_row * stride + b] * num_kv_heads * kBlock;
+    const int p0 = max(r.begin, b * kBlock), p1 = min(r.begin + r.count, b * kBlock + kBlock);
+    float* dst = out + (r.first + p0 - r.begin) * num_kv_heads;
+    for (int i = lane; i < (p1 - p0) * num_kv_heads; i += 32)
+      dst[i] = src[(i % num_kv_heads) * kBlock + (p0 & 15) + i / num_kv_heads];
   }
 }
 
 // ------------------------------------------------------------------ eviction: which rows
-// One CTA per (stretch, layer, kv head).  The keep-th largest weight is found eight bits at a time from
-// histograms; a second pass in order of the rows tells which rows equal to it are early enough, and
-// numbers the rows that move and the places they move to.
+// A cluster of one to eight CTAs per (stretch, layer, kv head), each with a contiguous part of the rows,
+// whose weights it reads once and keeps in registers as ordered integers.  The keep-th largest is
+// found eleven bits at a time (three rounds): every CTA counts its part in shared memory and reads the
+// others' counts there.  Rows above it are kept, and of the rows equal to it the first few.  Ranks (which
+// of the equal rows, which of the rows that move, which of the places they move to) come from counts per
+// warp and sixteen rows of a thread, added up once over the CTA and once over the cluster.
 __device__ __forceinline__ uint32_t weight_key(float x) {      // larger weight, larger key; a NaN on top
   const uint32_t b = __float_as_uint(x + 0.f);
   return x != x ? 0xffffffffu : b ^ (uint32_t)((int32_t)b >> 31 | 0x80000000);
 }
 
-constexpr int kPickThreads = 512;
+constexpr int kPickThreads = 512, kPickWarps = kPickThreads / 32;
+constexpr int kPickKeys = 32;                                  // a thread holds at most
+constexpr int kPickRows = kPickThreads * kPickKeys;            // a CTA holds at most
+constexpr int kPickCluster = 8;
+constexpr int kBins = 2048;
 
-__global__ void __launch_bounds__(kPickThreads) evict_pick_kernel(const EvictArgs a) {
+struct __align__(16) PickShared {
+  uint32_t hist[kBins];
+  uint32_t warp_sum[kPickWarps];
+  uint32_t prefix, left;
+  int before[3][kPickKeys * kPickWarps];   // rows of a kind before those of (key, warp), in the CTA
+  int total[3];                            // in the CTA
+};
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {               // (all CTAs of a cluster run at the same time)
+  asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;" ::: "memory");
+}
+// What lies at `p` in the shared memory of CTA `rank`.
+__device__ __forceinline__ uint32_t ld_peer(const void* p, uint32_t rank) {
+  uint32_t a, v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(s32(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint4 ld_peer4(const void* p, uint32_t rank) {
+  uint32_t a;
+  uint4 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(s32(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.u32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
+
+// sh.before[kind][..] holds counts per (key, warp) and becomes how many rows of that kind come earlier
+// in the stretch; returns the number of all of them.
+__device__ int ranks_of(PickShared& sh, int kind, int used, uint32_t n_cta, uint32_t me) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int mine = (int)threadIdx.x < used * kPickWarps ? sh.before[kind][threadIdx.x] : 0;
+  int upto = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o *= 2) {
+    const int x = __shfl_up_sync(kAll, upto, o);
+    if (lane >= o) upto += x;
+  }
+  if (lane == 31) sh.warp_sum[warp] = upto;
+  __syncthreads();
+  int base = 0, total = 0;
+  for (int x = 0; x < kPickWarps; ++x) {
+    if (x < warp) base += sh.warp_sum[x];
+    total += sh.warp_sum[x];
+  }
+  if (threadIdx.x == 0) sh.total[kind] = total;
+  int all = total;
+  if (n_cta > 1) {
+    cluster_sync();
+    const int t = (uint32_t)lane < n_cta ? (int)ld_peer(&sh.total[kind], lane) : 0;   // (a lane per CTA)
+    base += __reduce_add_sync(kAll, (uint32_t)lane < me ? t : 0);
+    all = __reduce_add_sync(kAll, t);
+  }
+  if ((int)threadIdx.x < used * kPickWarps) sh.before[kind][threadIdx.x] = base + upto - mine;
+  __syncthreads();
+  return all;
+}
+
+template <int kKeys>                             // rows of a thread: few where that is enough, for more CTAs an SM
+__global__ void __launch_bounds__(kPickThreads, kKeys <= 4 ? 4 : 1)
+evict_pick_kernel(const EvictArgs a, int n_cta) {
+  __shared__ PickShared sh;
+  const uint32_t me = n_cta > 1 ? cluster_rank() : 0;
+  const int entry = blockIdx.x / n_cta;
+  const EvictEntry en = a.entries[entry];
+  const int heads = a.num_kv_heads, lh = blockIdx.y, l = lh / heads, h = lh % heads;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const float* w = a.weights + (size_t)l * a.layer_floats;
+  const int32_t* table = a.d_tables + (size_t)en.table_row * a.table_stride + en.begin / kBlock;
+  int2* list = a.moves + en.list_begin + (size_t)lh * en.list_rows;
+  // this CTA's rows, r0 .. r0 + n - 1; thread t holds rows t, t + 512, ... of them
+  const int per = (en.n + n_cta * kPickThreads - 1) / (n_cta * kPickThreads) * kPickThreads;
+  const int r0 = min(en.n, (int)me * per), n = min(en.n - r0, per);
+  const int used = (n + kPickThreads - 1) / kPickThreads;
+  uint32_t key[kKeys];
+#pragma unroll
+  for (int k = 0; k < kKeys; ++k) {
+    key[k] = 0;
+    const int i = r0 + k * kPickThreads + threadIdx.x;
+    if (k < used && i < r0 + n)
+      key[k] = weight_key(w[((size_t)table[i >> 4] * heads + h) * kBlock + (i & 15)]);
+  }
+  uint32_t prefix = 0, left = en.keep;           // the left-th largest of the keys that start with prefix
+  for (int round = 0; round < 3; ++round) {
+    const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, bits = round == 2 ? 10 : 11;
+    for (int i = threadIdx.x; i < kBins; i += kPickThreads) sh.hist[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kKeys; ++k) {
+      if (k >= used) break;
+      if (k * kPickThreads + (int)threadIdx.x < n && (round == 0 || key[k] >> (shift + bits) == prefix))
+        atomicAdd(&sh.hist[key[k] >> shift & ((1u << bits) - 1)], 1u);
+    }
+    __syncthreads();
+    if (n_cta > 1) cluster_sync();
+    // thread t looks after four bins, from the top down
+    const int top = kBins - 1 - 4 * threadIdx.x;
+    uint4 part[kPickCluster];
+#pragma unroll
+    for (int r = 0; r < kPickCluster; ++r)       // (all on their way at once)
+      part[r] = r == 0 && n_cta == 1 ? *(const uint4*)&sh.hist[top - 3]
+                : r < n_cta          ? ld_peer4(&sh.hist[top - 3], r)
+                                     : make_uint4(0u, 0u, 0u, 0u);
+    uint32_t c[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int r = 0; r < kPickCluster; ++r) {
+      c[0] += part[r].w;
+      c[1] += part[r].z;
+      c[2] += part[r].y;
+      c[3] += part[r].x;
+    }
+    const uint32_t sum = c[0] + c[1] + c[2] + c[3];
+    uint32_t upto = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const uint32_t x = __shfl_up_sync(kAll, upto, o);
+      if (lane >= o) upto += x;
+    }
+    if (lane == 31) sh.warp_sum[warp] = upto;
+    __syncthreads();
+    for (int x = 0; x < warp; ++x) upto += sh.warp_sum[x];
+    uint32_t above = upto - sum;
+    if (above < left && left <= upto) {
+      int j = 0;
+      while (j < 3 && above + c[j] < left) above += c[j++];
+      sh.prefix = prefix << bits | (uint32_t)(top - j);
+      sh.left = left - above;
+    }
+    __syncthreads();
+    prefix = sh.prefix;
+    left = sh.left;
+    if (n_cta > 1) cluster_sync();               // (the counts have been read: they may be cleared)
+  }
+  // ---- which rows are kept, and where they go
+#pragma unroll
+  for (int k = 0; k < kKeys; ++k) {
+    if (k >= used) break;
+    const unsigned who = __ballot_sync(kAll, k * kPickThreads + (int)threadIdx.x < n && key[k] == prefix);
+    if (lane == 0) sh.before[0][k * kPickWarps + warp] = __popc(who);
+  }
+  __syncthreads();
+  ranks_of(sh, 0, used, n_cta, me);
+  uint32_t kept = 0;                             // bit k: row k of this thread
+#pragma unroll
+  for (int k = 0; k < kKeys; ++k) {
+    if (k >= used) break;
+    const int at = k * kPickThreads + threadIdx.x, i = r0 + at;
+    const bool equal = at < n && key[k] == prefix;
+    const unsigned who = __ballot_sync(kAll, equal);
+    const int rank = sh.before[0][k * kPickWarps + warp] + __popc(who & ((1u << lane) - 1));
+    const bool keep = at < n && (key[k] > prefix || (equal && rank < (int)left));
+    if (keep) kept |= 1u << k;
+    const unsigned move = __ballot_sync(kAll, keep && i >= en.keep);
+    const unsigned hole = __ballot_sync(kAll, at < n && !keep && i < en.keep);
+    if (lane == 0) {
+      sh.before[1][k * kPickWarps + warp] = __popc(move);
+      sh.before[2][k * kPickWarps + warp] = __popc(hole);
+    }
+  }
+  __syncthreads();
+  const int n_move = ranks_of(sh, 1, used, n_cta, me);
+  ranks_of(sh, 2, used, n_cta, me);
+#pragma unroll
+  for (int k = 0; k < kKeys; ++k) {
+    if (k >= used) break;
+    const int at = k * kPickThreads + threadIdx.x, i = r0 + at;
+    const bool keep = kept >> k & 1, move = keep && i >= en.keep;
+    const bool hole = at < n && !keep && i < en.keep;
+    const unsigned wm = __ballot_sync(kAll, move), wh = __ballot_sync(kAll, hole);
+    const unsigned lower = (1u << lane) - 1;
+    const int holes = sh.before[2][k * kPickWarps + warp] + __popc(wh & lower);
+    if (move) list[sh.before[1][k * kPickWarps + warp] + __popc(wm & lower)].x = i;
+    if (hole) list[holes].y = i;
+    // out of place the rows that stay are copied as well, behind those that move: the row's place
+    // less the free places before it
+    if (!en.in_place && keep && !move) list[n_move + i - holes] = make_int2(i, i);
+  }
+  if (threadIdx.x == 0 && me == 0)
+    a.counts[(size_t)entry * gridDim.y + lh] = en.in_place ? n_move : en.keep;
+  if (n_cta > 1) cluster_sync();                 // (nobody leaves while its counts are being read)
+}
+
+// The same for stretches that the registers of a cluster do not hold: one CTA, eight bits at a time,
+// the weights read again for every round and for the ranks.
+__global__ void __launch_bounds__(kPickThreads) evict_pick_long_kernel(const EvictArgs a) {
   __shared__ uint32_t hist[256];
   __shared__ uint32_t s_prefix, s_left;
   __shared__ int s_scan[3][kPickThreads / 32];
@@ -357,7 +556,7 @@ cudaError_t launch_weights_read(const float* w, const int32_t* d_tables, int tab
                                 const RowRange* d_ranges, int n, int max_count, int num_kv_heads,
                                 float* out, cudaStream_t st) {
   if (n <= 0 || max_count <= 0) return cudaSuccess;
-  const unsigned grid = (unsigned)std::min<int64_t>(((int64_t)max_count * num_kv_heads + 255) / 256, 4096);
+  const unsigned grid = (unsigned)std::min(max_count / (kBlock * 8) + 1, 1024);
   for (int i = 0; i < n; i += 65535) {                 // (the grid's limit)
     const cudaError_t e = launch_kernel(weights_read_kernel, dim3(grid, std::min(n - i, 65535)), dim3(256),
                                         0, st, false, w, d_tables, table_stride, d_ranges + i,
@@ -367,10 +566,27 @@ cudaError_t launch_weights_read(const float* w, const int32_t* d_tables, int tab
   return cudaSuccess;
 }
 
-cudaError_t launch_evict(const EvictArgs& a, int n, int num_layers, int max_rows, cudaStream_t st) {
+cudaError_t launch_evict(const EvictArgs& a, int n, int num_layers, int max_len, int max_rows,
+                         cudaStream_t st) {
   if (n <= 0) return cudaSuccess;
   const int lh = num_layers * a.num_kv_heads;
-  cudaError_t e = launch_kernel(evict_pick_kernel, dim3(n, lh), dim3(kPickThreads), 0, st, false, a);
+  // CTAs per stretch: as many as it takes to hold the longest stretch in registers
+  int n_cta = 1;
+  while (n_cta < kPickCluster && max_len > n_cta * kPickRows) n_cta *= 2;
+  auto pick = max_len <= kPickThreads * 4 ? evict_pick_kernel<4> : evict_pick_kernel<kPickKeys>;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(n * n_cta, lh);
+  cfg.blockDim = dim3(kPickThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = n_cta;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = n_cta > 1 ? 1 : 0;
+  cudaError_t e = max_len <= kPickCluster * kPickRows
+                      ? cudaLaunchKernelEx(&cfg, pick, a, n_cta)
+                      : launch_kernel(evict_pick_long_kernel, dim3(n, lh), dim3(kPickThreads), 0, st, false, a);
   if (e != cudaSuccess || max_rows <= 0) return e;
   const unsigned grid = (unsigned)std::min((max_rows + 15) / 16, 1024);
   EvictArgs part = a;

@@ -543,16 +543,21 @@ def test_eviction_of_several_threads_shared_and_copied(hq, hk):
     B.apar_check_invariants(f.s.ctx)
 
 
-def test_eviction_of_a_long_stretch():
-    f = Forest(4, 1, blocks=4500, per_thread=4400, poison=False)
+@pytest.mark.parametrize("n", [16384, 16400, 33000, 70000, 131072, 140001])
+def test_eviction_of_a_long_stretch(n):
+    f = Forest(4, 1, blocks=13000, per_thread=8800, poison=False)
     (t,) = f.new(1)
-    n = 70000
     k, v = rows(n, 1, 1), rows(n, 1, 2)
     f.s.append([t], [n], k, v)
-    w = some_weights(np.random.default_rng(3), "plain", 1, n, 1)
+    w = some_weights(np.random.default_rng(3), "plain" if n % 16 else "few", 1, n, 1)
     set_weights(f, t, w)
-    f.s.evict([t], [0], [n], [30011])
-    check_evicted(f, t, w, [k], [v], 0, n, 30011)
+    keep = n * 3 // 7
+    (c,) = f.s.fork([t])
+    f.s.evict([c], [16], [n], [keep])                    # copied: the parent keeps its rows
+    check_evicted(f, c, w, [k], [v], 16, n, keep)
+    f.s.release([c])
+    f.s.evict([t], [0], [n], [keep])
+    check_evicted(f, t, w, [k], [v], 0, n, keep)
 
 
 def test_beam_search_with_a_bounded_cache():
