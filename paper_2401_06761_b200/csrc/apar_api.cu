@@ -24,6 +24,7 @@ constexpr int kFewQueries = 768;      // up to here single-row items go to the w
 constexpr int kSlotsPerThread = 6;    // partial-result rows provisioned per live thread
 constexpr int kMinSlots = 1184;       // and never fewer than this (8 per SM of a 148-SM part), so
                                       // that a few very long threads still spread over the machine
+constexpr int kKeyUnitsPerSm = 40;    // units an SM gets of a call for accumulated weights
 constexpr int kSlotMapRows = 262144;  // new-row slots of the last append kept for other layers
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
@@ -175,7 +176,7 @@ struct apar_ctx {
   struct Seen { int32_t slot, lim; };         // queries of the last attention call; lim < 0: whole chain
   std::vector<Seen> seen;
   bool seen_valid = false, key_plan_valid = false;   // (they describe / the units on the device are of)
-  int32_t n_key_units = 0;                           // that call
+  int32_t n_key_units[3] = {0, 0, 0};                // that call; by class
   // thread list of the most recent apar_decode_step; its table rows are resident on the device
   std::vector<int32_t> step_tids, step_slots, tmp_slots;
   bool step_valid = false;
@@ -710,9 +711,10 @@ apar_status upload(apar_ctx* c, const void* src, size_t bytes, char* dst, cudaSt
   return APAR_OK;
 }
 
-// Cuts the runs into units of at most `chunk` keys, longest first, and sends both lists.
+// Cuts the runs into units of at most `chunk` keys, longest first (by_class: the widest class first), and
+// sends both lists.
 apar_status send_key_plan(apar_ctx* c, const std::vector<KeyRun>& runs, const std::vector<KeyUser>& users,
-                          int chunk, std::vector<KeyUnit>* units, cudaStream_t st) {
+                          int chunk, bool by_class, std::vector<KeyUnit>* units, cudaStream_t st) {
   units->clear();
   for (const KeyRun& r : runs)
     for (int t = r.tok_begin; t < r.tok_end; t += chunk) {
@@ -735,7 +737,10 @@ apar_status send_key_plan(apar_ctx* c, const std::vector<KeyRun>& runs, const st
     cost[i] = (u.tok_end < 0 ? -u.tok_end - 1 : u.tok_end - u.tok_begin) * (1 + queries);
     order[i] = (int32_t)i;
   }
-  std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) { return cost[a] > cost[b]; });
+  auto cls = [&](int32_t i) { return by_class ? key_class((*units)[i].n_users * c->shape.group) : 0; };
+  std::stable_sort(order.begin(), order.end(), [&](int32_t a, int32_t b) {
+    return cls(a) != cls(b) ? cls(a) > cls(b) : cost[a] > cost[b];
+  });
   std::vector<KeyUnit> sorted(units->size());
   for (size_t i = 0; i < order.size(); ++i) sorted[i] = (*units)[order[i]];
   units->swap(sorted);
@@ -1858,15 +1863,16 @@ apar_status apar_add_weights(apar_ctx* c, int32_t layer, const void* q, const fl
     std::vector<KeyRun> runs;
     std::vector<KeyUser> users;
     if (!c->planner.key_runs(qs.data(), (int)qs.size(), &runs, &users)) return APAR_ERR_INVALID_ARG;
-    // units of even length, some four to a warp of the machine where there is that much
+    // units of even length, some three to a warp of the machine where there is that much
     int64_t keys = 0;
     for (const KeyRun& r : runs) keys += r.tok_end - r.tok_begin;
-    const int64_t share = keys * c->cfg.num_kv_heads / ((int64_t)c->num_sms * 64);
-    int64_t chunk = std::min<int64_t>(1024, std::max<int64_t>(64, (share + 15) / 16 * 16));
+    const int64_t share = keys * c->cfg.num_kv_heads / ((int64_t)c->num_sms * kKeyUnitsPerSm);
+    const int64_t chunk = std::min<int64_t>(1024, std::max<int64_t>(64, (share + 15) / 16 * 16));
     std::vector<KeyUnit> units;
-    rc = send_key_plan(c, runs, users, (int)chunk, &units, st);
+    rc = send_key_plan(c, runs, users, (int)chunk, true, &units, st);
     if (rc) return rc;
-    c->n_key_units = (int32_t)units.size();
+    for (int32_t& n : c->n_key_units) n = 0;
+    for (const KeyUnit& u : units) ++c->n_key_units[key_class(u.n_users * c->shape.group)];
     c->key_plan_valid = true;
   }
   APAR_CUDA(c, launch_key_weights(key_args(c, layer, q, lse, sm_scale, replace), c->n_key_units, st));
@@ -1909,7 +1915,7 @@ apar_status apar_add_weights_prefill(apar_ctx* c, int32_t layer, int32_t n, cons
   std::vector<KeyUnit> units;
   if (!c->planner.key_runs(qs.data(), n, &runs, &users)) return APAR_ERR_INVALID_ARG;
   c->key_plan_valid = false;                             // (this plan takes the place of the other's)
-  rc = send_key_plan(c, runs, users, kPromptUnit, &units, st);
+  rc = send_key_plan(c, runs, users, kPromptUnit, false, &units, st);
   if (rc == APAR_OK) rc = sync_device_tables(c, slots.data(), n, st);
   if (rc) return rc;
   APAR_CUDA(c, launch_prompt_weights(key_args(c, layer, q, lse, sm_scale, replace), &c->tm_k[layer], &tm_q,

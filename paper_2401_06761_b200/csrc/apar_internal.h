@@ -313,7 +313,9 @@ cudaError_t launch_weights_cow(float* w, size_t layer_floats, int num_layers, co
 cudaError_t launch_weights_move(float* w, size_t layer_floats, int num_layers, const RowMove* d_moves,
                                 const int32_t* d_group_begin, int n_groups, int num_kv_heads,
                                 cudaStream_t st);
-cudaError_t launch_key_weights(const KeyArgs& a, int n_units, cudaStream_t st);
+// Units in three classes, the widest first in the list: n_units[i] of key_class i.
+inline int key_class(int rows) { return rows <= 8 ? 0 : rows <= 16 ? 1 : 2; }
+cudaError_t launch_key_weights(KeyArgs a, const int32_t (&n_units)[3], cudaStream_t st);
 // Units of at most 256 keys, closed; a user is a run of queries, the first at position lim.  tm_q as in
 // launch_attention_prefill.
 constexpr int kPromptUnit = 256;

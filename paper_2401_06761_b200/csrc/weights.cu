@@ -62,6 +62,11 @@ __global__ void __launch_bounds__(64) weights_move_kernel(float* __restrict__ w,
 // B operand.  The contraction may take the dims in any order as long as both operands take the same:
 // a lane loads sixteen consecutive bytes of its key's row, which hold its share of two products, so K
 // comes straight from memory into registers.
+// K is read once for up to 8 * NT rows, whose queries stay in registers; units of more than 32 go over their
+// keys again, in the L2 cache.  Units of up to 8, 16 and more rows have a launch each (in one kernel
+// the three would share the widest one's registers); a launch may start before the one before it is done.
+// kAhead blocks of keys are on their way while one is worked on: it takes some 48 KB an SM in flight to
+// keep HBM busy.
 __device__ __forceinline__ uint4 ld_k(const uint4* p) {
   uint4 v;
   asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
@@ -77,12 +82,114 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-constexpr int kKeyWarps = 8;
+constexpr int kKeyWarps = 4;                     // per CTA
 
-__global__ void __launch_bounds__(kKeyWarps * 32, 2) key_weights_kernel(const KeyArgs a, int n_units) {
+// Rows r0 .. r0 + 8 NT - 1 of the unit against its keys [begin, end) of kv head h.
+template <int NT, int kAhead>
+__device__ __forceinline__ void key_rows(const KeyArgs& a, const KeyUnit& it, const int32_t* table, int h,
+                                         int end, int rows, int r0, bool replace) {
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int G = a.shape.group, HQ = a.shape.num_q_heads, HKV = a.shape.num_kv_heads;
-  const int stride = gridDim.x * kKeyWarps;
+  const int n_blk = (end - it.tok_begin + kBlock - 1) / kBlock;
+  const int32_t* ids = table + it.tok_begin / kBlock;
+  // block ids of 32 blocks at a time, lane b's being block b's
+  int id = lane < n_blk ? ids[lane] : 0, id_next = 32 + lane < n_blk ? ids[32 + lane] : 0;
+  const uint8_t* k_base = (const uint8_t*)a.k_pool + (size_t)h * kTileBytes + g * 256 + t * 16;
+  uint4 k[kAhead][8];
+  auto fetch = [&](uint4 (&dst)[8], int block) {
+    const uint4* src = (const uint4*)(k_base + (size_t)block * HKV * kTileBytes);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      dst[w] = ld_k(src + 4 * w);
+      dst[4 + w] = ld_k(src + 128 + 4 * w);
+    }
+  };
+#pragma unroll
+  for (int x = 0; x < kAhead; ++x)
+    if (x < n_blk) fetch(k[x], __shfl_sync(kAll, id, x));
+  // this lane's part of the rows: rows 8 i + g as operands, 8 i + 2 t and + 1 as results
+  uint4 q[NT][4];
+  float ref[NT][2];
+  int see[NT][2];                                // keys before this one are seen
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    const int r = r0 + 8 * i + g;
+    if (r < rows) {
+      const int query = a.users[it.user_begin + r / G].query;
+      const uint4* src = (const uint4*)((const __nv_bfloat16*)a.q + ((size_t)query * HQ + h * G + r % G) * kDim);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) q[i][w] = __ldg(src + 4 * w + t);
+    } else {
+#pragma unroll
+      for (int w = 0; w < 4; ++w) q[i][w] = make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int rr = r0 + 8 * i + 2 * t + e;
+      ref[i][e] = 0.f;
+      see[i][e] = 0;
+      if (rr < rows) {
+        const KeyUser user = a.users[it.user_begin + rr / G];
+        ref[i][e] = __ldg(a.lse + (size_t)user.query * HQ + h * G + rr % G) * 1.4426950408889634f;
+        see[i][e] = min(user.lim, end);
+      }
+    }
+  }
+  for (int b0 = 0; b0 < n_blk; b0 += kAhead) {
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {           // (unrolled: each block in registers of its own)
+      const int b = b0 + x;
+      if (b >= n_blk) break;
+      if (b > 0 && (b & 31) == 0) {
+        id = id_next;
+        id_next = b + 32 + lane < n_blk ? ids[b + 32 + lane] : 0;
+      }
+      const int block = __shfl_sync(kAll, id, b & 31);
+      float d[NT][4];
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        d[i][0] = d[i][1] = d[i][2] = d[i][3] = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          mma16816(d[i], k[x][w].x, k[x][4 + w].x, k[x][w].y, k[x][4 + w].y, q[i][w].x, q[i][w].y);
+          mma16816(d[i], k[x][w].z, k[x][4 + w].z, k[x][w].w, k[x][4 + w].w, q[i][w].z, q[i][w].w);
+        }
+      }
+      const int nb = b + kAhead;
+      if (nb < n_blk) {
+        const int from = (nb & 31) < (b & 31) ? id_next : id;   // (already of the next 32?)
+        fetch(k[x], __shfl_sync(kAll, from, nb & 31));
+      }
+      // keys tok + g (d[0], d[1]) and tok + g + 8 (d[2], d[3]); a key that a row does not see may
+      // hold any bits
+      const int tok = it.tok_begin + b * kBlock;
+      float lo = 0.f, hi = 0.f;
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          if (tok + g < see[i][e]) lo += ex2(fmaf(d[i][e], a.scale_log2e, -ref[i][e]));
+          if (tok + g + 8 < see[i][e]) hi += ex2(fmaf(d[i][2 + e], a.scale_log2e, -ref[i][e]));
+        }
+      lo += __shfl_xor_sync(kAll, lo, 1);
+      hi += __shfl_xor_sync(kAll, hi, 1);
+      lo += __shfl_xor_sync(kAll, lo, 2);
+      hi += __shfl_xor_sync(kAll, hi, 2);
+      if (t < 2) {
+        const int row = g + 8 * t;
+        float* w = a.weights + ((size_t)block * HKV + h) * kBlock + row;
+        const float add = t ? hi : lo;
+        if (tok + row < end) *w = replace ? add : *w + add;
+      }
+    }
+  }
+}
+
+template <int NT, int kAhead, int kCtas>
+__global__ void __launch_bounds__(kKeyWarps * 32, kCtas) key_weights_kernel(const KeyArgs a, int n_units) {
+  const int G = a.shape.group, HKV = a.shape.num_kv_heads;
+  const int64_t stride = (int64_t)gridDim.x * kKeyWarps;
+  pdl_launch_dependents();
   for (int64_t u = (int64_t)blockIdx.x * kKeyWarps + (threadIdx.x >> 5); u < (int64_t)n_units * HKV; u += stride) {
     const KeyUnit it = a.units[u / HKV];
     const int h = (int)(u % HKV);
@@ -90,73 +197,10 @@ __global__ void __launch_bounds__(kKeyWarps * 32, 2) key_weights_kernel(const Ke
     const int end = it.tok_end < 0 ? a.d_lens[it.table_row] : it.tok_end;
     const int rows = it.n_users * G;
     if (it.tok_begin >= end) continue;
-    for (int r0 = 0; r0 < rows; r0 += 8) {
-      // this lane's part of the rows: row r0 + g as an operand, rows r0 + 2 t and + 1 as results
-      uint4 q[4];
-      const int r = r0 + g;
-      if (r < rows) {
-        const int query = a.users[it.user_begin + r / G].query;
-        const uint4* src = (const uint4*)((const __nv_bfloat16*)a.q + ((size_t)query * HQ + h * G + r % G) * kDim);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) q[w] = __ldg(src + 4 * w + t);
-      } else {
-#pragma unroll
-        for (int w = 0; w < 4; ++w) q[w] = make_uint4(0u, 0u, 0u, 0u);
-      }
-      float ref[2];
-      int see[2];                                // keys before this one are seen
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int rr = r0 + 2 * t + e;
-        ref[e] = 0.f;
-        see[e] = 0;
-        if (rr < rows) {
-          const KeyUser user = a.users[it.user_begin + rr / G];
-          ref[e] = __ldg(a.lse + (size_t)user.query * HQ + h * G + rr % G) * 1.4426950408889634f;
-          see[e] = min(user.lim, end);
-        }
-      }
-      uint4 k[8];
-      auto fetch = [&](int tok) {
-        const uint4* src = (const uint4*)((const uint8_t*)a.k_pool +
-                                          ((size_t)table[tok >> 4] * HKV + h) * kTileBytes) + g * 16 + t;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          k[w] = ld_k(src + 4 * w);
-          k[4 + w] = ld_k(src + 128 + 4 * w);
-        }
-      };
-      fetch(it.tok_begin);
-      for (int tok = it.tok_begin; tok < end; tok += kBlock) {
-        float d[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          mma16816(d, k[w].x, k[4 + w].x, k[w].y, k[4 + w].y, q[w].x, q[w].y);
-          mma16816(d, k[w].z, k[4 + w].z, k[w].w, k[4 + w].w, q[w].z, q[w].w);
-        }
-        const int block = table[tok >> 4];
-        if (tok + kBlock < end) fetch(tok + kBlock);
-        // keys tok + g (d[0], d[1]) and tok + g + 8 (d[2], d[3]); a key that a row does not see may
-        // hold any bits
-        float lo = 0.f, hi = 0.f;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          if (tok + g < see[e]) lo += ex2(fmaf(d[e], a.scale_log2e, -ref[e]));
-          if (tok + g + 8 < see[e]) hi += ex2(fmaf(d[2 + e], a.scale_log2e, -ref[e]));
-        }
-        lo += __shfl_xor_sync(kAll, lo, 1);
-        hi += __shfl_xor_sync(kAll, hi, 1);
-        lo += __shfl_xor_sync(kAll, lo, 2);
-        hi += __shfl_xor_sync(kAll, hi, 2);
-        if (t < 2) {
-          const int row = g + 8 * t;
-          float* w = a.weights + ((size_t)block * HKV + h) * kBlock + row;
-          const float add = t ? hi : lo;
-          if (tok + row < end) *w = a.replace && r0 == 0 ? add : *w + add;
-        }
-      }
-    }
+    for (int r0 = 0; r0 < rows; r0 += 8 * NT)
+      key_rows<NT, kAhead>(a, it, table, h, end, rows, r0, a.replace && r0 == 0);
   }
+  pdl_wait();                                    // (done means that the launches before it are, too)
 }
 
 // ------------------------------------------------------------------ read back
@@ -545,11 +589,21 @@ cudaError_t launch_weights_move(float* w, size_t layer_floats, int num_layers, c
                        false, w, layer_floats, d_moves, d_group_begin, num_kv_heads);
 }
 
-cudaError_t launch_key_weights(const KeyArgs& a, int n_units, cudaStream_t st) {
-  if (n_units <= 0) return cudaSuccess;
-  const int64_t warps = (int64_t)n_units * a.shape.num_kv_heads;
-  const int grid = (int)std::min<int64_t>((warps + kKeyWarps - 1) / kKeyWarps, 2 * a.num_sms);
-  return launch_kernel(key_weights_kernel, dim3(grid), dim3(kKeyWarps * 32), 0, st, false, a, n_units);
+cudaError_t launch_key_weights(KeyArgs a, const int32_t (&n_units)[3], cudaStream_t st) {
+  cudaError_t e = cudaSuccess;
+  bool first = true;
+  auto launch = [&](auto kernel, int n, int ctas) {
+    if (n <= 0 || e != cudaSuccess) return;
+    const int64_t warps = (int64_t)n * a.shape.num_kv_heads;
+    const int grid = (int)std::min<int64_t>((warps + kKeyWarps - 1) / kKeyWarps, (int64_t)ctas * a.num_sms);
+    e = launch_kernel(kernel, dim3(grid), dim3(kKeyWarps * 32), 0, st, !first, a, n);
+    a.units += n;
+    first = false;
+  };
+  launch(key_weights_kernel<4, 1, 3>, n_units[2], 3);
+  launch(key_weights_kernel<2, 2, 3>, n_units[1], 3);
+  launch(key_weights_kernel<1, 2, 4>, n_units[0], 4);
+  return e;
 }
 
 cudaError_t launch_weights_read(const float* w, const int32_t* d_tables, int table_stride,

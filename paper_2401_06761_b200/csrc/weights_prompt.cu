@@ -5,11 +5,17 @@
 // owns a key (its TMEM lane), goes over the queries in the columns and adds up
 //     exp2(c s - log2 e * lse[column])
 // in a register: no shuffles, no atomics, nothing but one number per key leaves the SM.
-//   warps 0-3, 4-7  own keys 0..127 and 128..255 of the unit, each with two S buffers of 128 columns.
-//   warp 8          reads the unit list, copies K tiles (double-buffered, 64 KiB a unit) and query
-//                   tiles (128 / group tokens times the group's heads; three in flight) by TMA, and puts
-//                   each query tile's log-sum-exps and a description beside it.
-//   warp 9          issues the products (lane 0): per query tile and half of the keys M 128, N 128, K 128.
+//   warps 0-15      four to a quarter: half of the unit's keys (two S buffers of 128 columns each), half
+//                   of the columns.  At a unit's end the first half of the columns writes its sums, and
+//                   the second adds its own to them.
+//   warp 16         copies, by TMA, K tiles (double-buffered, 64 KiB a unit) and query tiles (128 / group
+//                   tokens times the group's heads; three in flight).
+//   warp 17         puts each query tile's log-sum-exps and a description into a ring of five.
+//   warps 18, 19    issue the products (lane 0), one for each half of the keys: M 128, N 128, K 128 per query
+//                   tile.
+// Each of these four does one small thing per tile: next to warps that keep the SM busy a single warp gets an
+// instruction in every ten cycles or so and a look at a barrier takes it 250, and a tile's sums take 2000.
+// (One warp that copied and described, and one that issued both products, took 3200 a tile.)
 // 256 keys to a unit, so that a query tile is read from L2 once for twice the keys.  Units are dealt out
 // longest first, forwards and backwards in turn.  All waits are bounded, as in the attention kernels.
 #include <algorithm>
@@ -32,9 +38,13 @@ constexpr int kUnitB = 2 * kTileB;
 constexpr int kQStages = 3;
 constexpr int kOffQ = 2 * kUnitB;
 constexpr int kOffLse = kOffQ + kQStages * kTileB;
-constexpr int kOffDesc = kOffLse + kQStages * kKeys * 4;
-constexpr int kOffBar = kOffDesc + kQStages * 32;
-constexpr int kSmem = kOffBar + 256 + 1024;
+constexpr int kLStages = 5;
+constexpr int kOffDesc = kOffLse + kLStages * kKeys * 4;
+constexpr int kOffFlags = kOffDesc + kLStages * 32;
+constexpr int kOffBar = kOffFlags + 16;
+constexpr int kSmem = kOffBar + 288;
+constexpr int kSumWarps = 16;
+constexpr int kWarps = kSumWarps + 4;
 static_assert(kSmem <= 227 * 1024, "shared memory");
 
 struct TileDesc {
@@ -42,32 +52,107 @@ struct TileDesc {
   int32_t pos;                   // position of the first
   int32_t tok_begin, end;        // the unit's keys
   int32_t table_row, kvh;
-  int32_t flags;                 // 1: the unit's first tile, 2: its last
+  int32_t flags;                 // F_*
   int32_t pad;
 };
 static_assert(sizeof(TileDesc) == 32, "description");
+// What the issuers need of it: a word beside each stage of the ring of query tiles.
+enum { F_FIRST = 1, F_LAST = 2, F_BOTH = 4, F_END = 8 };
 
 enum { B_KFULL = 0, B_KEMPTY = 2, B_QFULL = 4, B_QEMPTY = B_QFULL + kQStages,
-       B_SFULL = B_QEMPTY + kQStages,            // [half][buffer]
-       B_SEMPTY = B_SFULL + 4, B_TOTAL = B_SEMPTY + 4 };
-static_assert(8 * B_TOTAL + 16 <= 256, "barrier area");
+       B_LFULL = B_QEMPTY + kQStages, B_LEMPTY = B_LFULL + kLStages,   // log-sum-exps and description
+       B_SFULL = B_LEMPTY + kLStages,            // [half][buffer]
+       B_SEMPTY = B_SFULL + 4,
+       B_WFULL = B_SEMPTY + 4, B_WEMPTY = B_WFULL + 2,   // [half]: the first columns' sums are written
+       B_TOTAL = B_WEMPTY + 2 };
+static_assert(8 * B_TOTAL + 16 <= 256 + 32, "barrier area");
+
+// ---- two numbers at a time
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair(float lo, float hi) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpair(f32x2 v, float& lo, float& hi) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 
 // Units in the order they are dealt out: CTA b's i-th.
 __device__ __forceinline__ int64_t dealt(int64_t i) {
   return i * gridDim.x + (i & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
 }
 
-__global__ void __launch_bounds__(320, 1)
+// The units of a CTA in their order.  Descriptions are asked for two units ahead, a unit's first user and
+// its block ids (lane b: of block b / 2) one unit ahead.
+struct UnitWalk {
+  const KeyArgs& a;
+  const int64_t total;
+  const int b;
+  int64_t i = 0;                                 // units looked at so far
+  KeyUnit it, it1, it2;                          // the current one, the next, the one after that
+  KeyUser user, user1;
+  int h, h1, h2, bid, bid1;
+  bool more, more1, more2;
+
+  __device__ UnitWalk(const KeyArgs& args, int64_t n, int lane) : a(args), total(n), b(lane >> 1) {
+    look();
+    fetch();
+    look();
+    step();
+  }
+  __device__ void look() {
+    more2 = false;
+    while (i * gridDim.x < total && !more2) {
+      const int64_t u = dealt(i++);
+      if (u >= total) continue;
+      it2 = a.units[u / a.shape.num_kv_heads];
+      h2 = (int)(u % a.shape.num_kv_heads);
+      more2 = true;
+    }
+  }
+  __device__ void fetch() {
+    more1 = more2;
+    if (!more1) return;
+    it1 = it2;
+    h1 = h2;
+    user1 = a.users[it1.user_begin];
+    bid1 = b < (it1.tok_end - it1.tok_begin + kBlock - 1) / kBlock
+               ? a.d_tables[(size_t)it1.table_row * a.shape.table_stride + it1.tok_begin / kBlock + b] : 0;
+  }
+  __device__ void step() {
+    more = more1;
+    if (!more) return;
+    it = it1;
+    user = user1;
+    h = h1;
+    bid = bid1;
+    fetch();
+    look();
+  }
+};
+
+__global__ void __launch_bounds__(kWarps * 32, 1)
 prompt_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_q,
                       const KeyArgs a, int n_units) {
-  extern __shared__ uint8_t smem_raw[];
-  const uint32_t base = (s32(smem_raw) + 1023u) & ~1023u;
-  uint8_t* bp = smem_raw + (base - s32(smem_raw));
+  extern __shared__ __align__(1024) uint8_t bp[];
+  const uint32_t base = s32(bp);
   auto bar = [&](int i) { return base + kOffBar + 8u * i; };
   volatile int* cta_abort = (volatile int*)(bp + kOffBar + 8 * B_TOTAL);
   volatile uint32_t* tmem_slot = (volatile uint32_t*)(bp + kOffBar + 8 * B_TOTAL + 8);
   TileDesc* descs = (TileDesc*)(bp + kOffDesc);
   float* lses = (float*)(bp + kOffLse);
+  volatile int* q_flags = (volatile int*)(bp + kOffFlags);
   const int G = a.shape.group, HQ = a.shape.num_q_heads, HKV = a.shape.num_kv_heads;
   const int T = kKeys / G;                       // tokens of a query tile
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -75,19 +160,29 @@ prompt_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
 
   if (threadIdx.x == 0) {
     *cta_abort = *(volatile int*)a.d_error;      // an earlier kernel gave up: do not pile up
+    if (base & 1023) {                           // (the swizzle counts from 1024-byte boundaries)
+      *cta_abort = 1;
+      atomicCAS(a.d_error, 0, 25000);
+    }
     asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)&tm_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)&tm_q) : "memory");
     for (int b = 0; b < 2; ++b) {
       bar_init(bar(B_KFULL + b), 1);
-      bar_init(bar(B_KEMPTY + b), 1);
+      bar_init(bar(B_KEMPTY + b), 2);            // both issuers
+      bar_init(bar(B_WFULL + b), 4);
+      bar_init(bar(B_WEMPTY + b), 4);
     }
     for (int s = 0; s < kQStages; ++s) {
       bar_init(bar(B_QFULL + s), 1);
-      bar_init(bar(B_QEMPTY + s), 9);            // the products' end, and eight warps
+      bar_init(bar(B_QEMPTY + s), 2);
+    }
+    for (int s = 0; s < kLStages; ++s) {
+      bar_init(bar(B_LFULL + s), 1);
+      bar_init(bar(B_LEMPTY + s), kSumWarps);
     }
     for (int s = 0; s < 4; ++s) {
       bar_init(bar(B_SFULL + s), 1);
-      bar_init(bar(B_SEMPTY + s), 4);
+      bar_init(bar(B_SEMPTY + s), kSumWarps / 2);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -95,7 +190,7 @@ prompt_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
   for (int i = threadIdx.x; i < kQStages * kTileB / 16; i += blockDim.x)
     *(uint4*)(bp + kOffQ + 16 * i) = make_uint4(0u, 0u, 0u, 0u);
   fence_async_smem();
-  if (warp == 9) {
+  if (warp == kSumWarps + 2) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
                  ::"r"(s32((const void*)tmem_slot)), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -108,72 +203,55 @@ prompt_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
   const int64_t total = (int64_t)n_units * HKV;
 
   if (dead) {
-  } else if (warp == 8) {
+  } else if (warp == kSumWarps) {
     // ---------------------------------------------------------------- copies
-    int off[4];                                  // this lane's rows of a tile, in the lse array
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = lane + 32 * i;
-      off[i] = r < T * G ? r / G * HQ + r % G : -1;
-    }
     int g = 0, ku = 0;                           // query tiles and units so far
     bool ok = true;
-    for (int64_t i = 0; ok && i * gridDim.x < total; ++i) {
-      const int64_t u = dealt(i);
-      if (u >= total) continue;
-      const KeyUnit it = a.units[u / HKV];
-      const int h = (int)(u % HKV), n_blk = (it.tok_end - it.tok_begin + kBlock - 1) / kBlock;
-      const int32_t* table = a.d_tables + (size_t)it.table_row * a.shape.table_stride + it.tok_begin / kBlock;
-      const int bid = (lane >> 1) < n_blk ? table[lane >> 1] : 0;
-      bool first = true;
-      for (int x = 0; ok && x < it.n_users; ++x) {
-        const KeyUser user = a.users[it.user_begin + x];
-        for (int j = max(0, it.tok_begin - user.lim); j < user.count; j += T, ++g) {
-          const int st = g % kQStages, n_tok = min(T, user.count - j), q0 = user.query + j;
-          float l[4];                            // (on its way while the stage is waited for)
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            l[k] = off[k] >= 0 && lane + 32 * k < n_tok * G ? __ldg(a.lse + (int64_t)q0 * HQ + h * G + off[k])
-                                                            : INFINITY;
-          if (g >= kQStages)
-            ok = bar_wait(bar(B_QEMPTY + st), (g / kQStages - 1) & 1, cta_abort, a.d_error, 22000);
-          if (first && ku >= 2)
-            ok = ok && bar_wait(bar(B_KEMPTY + (ku & 1)), ((ku >> 1) - 1) & 1, cta_abort, a.d_error, 22100);
-          ok = __all_sync(kAll, ok);
-          if (!ok) break;
-          if (first) {
-            if (lane == 0) bar_expect_tx(bar(B_KFULL + (ku & 1)), (uint32_t)n_blk * kTileBytes);
-            __syncwarp();
-            // block b of the unit: 16 rows of its half of the keys, in two pieces of 64 dims
-            const uint32_t dst = base + (ku & 1) * kUnitB + (lane & 1) * kHalf;
-            const int b = lane >> 1;
-            if (b < n_blk)
-              tma_2d(dst + (b >> 3) * kTileB + (b & 7) * (kBlock * 128), &tm_k, (lane & 1) * 64,
-                     (bid * HKV + h) * kBlock, bar(B_KFULL + (ku & 1)));
+    const uint32_t q_bytes = 2u * T * G * 128u;
+    for (UnitWalk u(a, total, lane); ok && u.more; u.step(), ++ku) {
+      const int n_blk = (u.it.tok_end - u.it.tok_begin + kBlock - 1) / kBlock, kf = bar(B_KFULL + (ku & 1));
+      if (ku >= 2)
+        ok = __all_sync(kAll, bar_wait(bar(B_KEMPTY + (ku & 1)), ((ku >> 1) - 1) & 1, cta_abort, a.d_error,
+                                       22100));
+      if (!ok) break;
+      if (lane == 0) bar_expect_tx(kf, (uint32_t)n_blk * kTileBytes);
+      __syncwarp();
+      // block b of the unit: 16 rows of its half of the keys, in two pieces of 64 dims
+      if (u.b < n_blk)
+        tma_2d(base + (ku & 1) * kUnitB + (u.b >> 3) * kTileB + (lane & 1) * kHalf + (u.b & 7) * (kBlock * 128),
+               &tm_k, (lane & 1) * 64, (u.bid * HKV + u.h) * kBlock, kf);
+      int flags = F_FIRST | (n_blk * kBlock > kKeys ? F_BOTH : 0);
+      KeyUser user = u.user;
+      for (int x = 0; ok; user = a.users[u.it.user_begin + x]) {
+        const int end = user.query + user.count;
+        ++x;
+        for (int q0 = user.query + max(0, u.it.tok_begin - user.lim); q0 < end; q0 += T, ++g) {
+          const int st = g % kQStages;
+          if (g >= kQStages &&
+              !__all_sync(kAll, bar_wait(bar(B_QEMPTY + st), (g / kQStages - 1) & 1, cta_abort, a.d_error,
+                                         22000))) {
+            ok = false;
+            break;
           }
-#pragma unroll
-          for (int k = 0; k < 4; ++k) lses[st * kKeys + lane + 32 * k] = l[k] * 1.4426950408889634f;
+          if (x == u.it.n_users && q0 + T >= end) flags |= F_LAST;
           if (lane == 0) {
-            const bool last = x == it.n_users - 1 && j + T >= user.count;
-            descs[st] = TileDesc{n_tok, user.lim + j, it.tok_begin, it.tok_end, it.table_row, h,
-                                 (first ? 1 : 0) | (last ? 2 : 0), 0};
+            q_flags[st] = flags;
+            bar_expect_tx(bar(B_QFULL + st), q_bytes);
           }
-          __syncwarp();
-          if (lane == 0) bar_expect_tx(bar(B_QFULL + st), 2u * T * G * 128u);
+          flags &= ~F_FIRST;
           __syncwarp();
           if (lane < 2)
-            tma_3d(base + kOffQ + st * kTileB + lane * kHalf, &tm_q, lane * 64, h * G, q0, bar(B_QFULL + st));
-          first = false;
+            tma_3d(base + kOffQ + st * kTileB + lane * kHalf, &tm_q, lane * 64, u.h * G, q0, bar(B_QFULL + st));
         }
+        if (x == u.it.n_users) break;
       }
-      if (!first) ++ku;
     }
+    const int st = g % kQStages;
     if (ok && g >= kQStages)
-      ok = __all_sync(kAll, bar_wait(bar(B_QEMPTY + g % kQStages), (g / kQStages - 1) & 1, cta_abort,
-                                     a.d_error, 22200));
+      ok = __all_sync(kAll, bar_wait(bar(B_QEMPTY + st), (g / kQStages - 1) & 1, cta_abort, a.d_error, 22400));
     if (ok && lane == 0) {
-      descs[g % kQStages].n_tok = 0;
-      bar_arrive(bar(B_QFULL + g % kQStages));
+      q_flags[st] = F_END;
+      bar_arrive(bar(B_QFULL + st));
     }
     // after a wait that gave up: the copies in flight are waited for (with a limit of their own)
     if (*cta_abort && lane == 0) {
@@ -182,26 +260,78 @@ prompt_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
       for (int x = max(0, ku - 1); x <= ku; ++x)
         for (uint32_t i = 0; i < kSpin && !bar_try(bar(B_KFULL + (x & 1)), (x >> 1) & 1); ++i) {}
     }
-  } else if (warp == 9) {
+  } else if (warp == kSumWarps + 1) {
+    // ---------------------------------------------------------------- log-sum-exps, descriptions
+    const float* src[4];                         // this lane's rows of a tile that begins with query 0, head 0
+    int row_of[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = lane + 32 * i;
+      row_of[i] = r < T * G ? r : 1 << 30;
+      src[i] = a.lse + (r < T * G ? r / G * HQ + r % G : 0);
+    }
+    int g = 0;
+    bool ok = true;
+    for (UnitWalk u(a, total, lane); ok && u.more; u.step()) {
+      KeyUser user = u.user;
+      for (int x = 0; ok; user = a.users[u.it.user_begin + x]) {
+        ++x;
+        int j = max(0, u.it.tok_begin - user.lim);
+        int64_t at = (int64_t)(user.query + j) * HQ + u.h * G;
+        float l[4];
+        auto ask = [&](int n) {                  // a tile of n tokens
+#pragma unroll
+          for (int k = 0; k < 4; ++k) l[k] = row_of[k] < n * G ? __ldg(src[k] + at) : INFINITY;
+        };
+        ask(min(T, user.count - j));
+        for (; j < user.count; j += T, ++g) {
+          const int ls = g % kLStages;
+          if (g >= kLStages &&
+              !__all_sync(kAll, bar_wait(bar(B_LEMPTY + ls), (g / kLStages - 1) & 1, cta_abort, a.d_error,
+                                         22300))) {
+            ok = false;
+            break;
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k) lses[ls * kKeys + lane + 32 * k] = l[k] * -1.4426950408889634f;
+          if (lane == 0)
+            descs[ls] = TileDesc{min(T, user.count - j), user.lim + j, u.it.tok_begin, u.it.tok_end,
+                                 u.it.table_row, u.h, x == u.it.n_users && j + T >= user.count ? F_LAST : 0, 0};
+          __syncwarp();
+          if (lane == 0) bar_arrive(bar(B_LFULL + ls));
+          at += (int64_t)T * HQ;
+          ask(min(T, user.count - j - T));       // (of no tokens behind the last tile)
+        }
+        if (x == u.it.n_users) break;
+      }
+    }
+    const int ls = g % kLStages;
+    if (ok && g >= kLStages)
+      ok = __all_sync(kAll, bar_wait(bar(B_LEMPTY + ls), (g / kLStages - 1) & 1, cta_abort, a.d_error, 22200));
+    if (ok && lane == 0) {
+      descs[ls].n_tok = 0;
+      bar_arrive(bar(B_LFULL + ls));
+    }
+  } else if (warp > kSumWarps + 1) {
     // ---------------------------------------------------------------- products
     constexpr uint32_t kIdesc = instr_desc(128, false, 128);
-    int ku = 0, cnt[2] = {0, 0};
+    const int w = warp - kSumWarps - 2;
+    int ku = 0, cnt = 0;
+    bool seen = false;                           // the tile was there at the last look
     for (int g = 0;; ++g) {
-      const int st = g % kQStages;
-      if (!__all_sync(kAll, bar_wait(bar(B_QFULL + st), (g / kQStages) & 1, cta_abort, a.d_error, 23000)))
+      const int st = g % kQStages, sb = cnt & 1;
+      if (!__all_sync(kAll, seen) &&
+          !__all_sync(kAll, bar_wait(bar(B_QFULL + st), (g / kQStages) & 1, cta_abort, a.d_error, 23000)))
         break;
-      const TileDesc d = descs[st];
-      if (d.n_tok == 0) break;
-      bool ok = true;
-      if (d.flags & 1)
-        ok = bar_wait(bar(B_KFULL + (ku & 1)), (ku >> 1) & 1, cta_abort, a.d_error, 23100);
-      const int halves = d.end - d.tok_begin > kKeys ? 2 : 1;
-      for (int w = 0; w < halves && ok; ++w) {
-        const int sb = cnt[w] & 1;
-        if (cnt[w] >= 2)
-          ok = bar_wait(bar(B_SEMPTY + 2 * w + sb), ((cnt[w] >> 1) - 1) & 1, cta_abort, a.d_error, 23200);
-        ok = __all_sync(kAll, ok);
-        if (!ok) break;
+      const int flags = q_flags[st];
+      if (flags & F_END) break;
+      if (w == 0 || (flags & F_BOTH)) {
+        bool ok = true;
+        if (flags & F_FIRST)
+          ok = bar_wait(bar(B_KFULL + (ku & 1)), (ku >> 1) & 1, cta_abort, a.d_error, 23100);
+        if (cnt >= 2)
+          ok = ok && bar_wait(bar(B_SEMPTY + 2 * w + sb), ((cnt >> 1) - 1) & 1, cta_abort, a.d_error, 23200);
+        if (!__all_sync(kAll, ok)) break;
         tc_fence_after();
         if (lane == 0) {
           const uint64_t kd = smem_desc(base + (ku & 1) * kUnitB + w * kTileB, 16, 1024);
@@ -212,88 +342,112 @@ prompt_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
             umma_bf16(tmem + 256u * w + 128u * sb, kd + at, qd + at, kIdesc, ks > 0);
           }
           umma_commit(bar(B_SFULL + 2 * w + sb));
+          umma_commit(bar(B_QEMPTY + st));
+          if (flags & F_LAST) umma_commit(bar(B_KEMPTY + (ku & 1)));
         }
-        ++cnt[w];
+        ++cnt;
+      } else if (lane == 0) {                    // (nothing of this half in the unit)
+        bar_arrive(bar(B_QEMPTY + st));
+        if (flags & F_LAST) bar_arrive(bar(B_KEMPTY + (ku & 1)));
       }
-      if (!__all_sync(kAll, ok)) break;
-      if (lane == 0) {
-        umma_commit(bar(B_QEMPTY + st));
-        if (d.flags & 2) umma_commit(bar(B_KEMPTY + (ku & 1)));
-      }
-      if (d.flags & 2) ++ku;
+      if (flags & F_LAST) ++ku;
       __syncwarp();
+      seen = bar_test(bar(B_QFULL + (g + 1) % kQStages), ((g + 1) / kQStages) & 1);
     }
   } else {
     // ---------------------------------------------------------------- sums
-    const int w = warp >> 2, row = (warp & 3) * 32 + lane;     // the key's row of its half: its TMEM lane
-    const uint32_t lane_sel = (uint32_t)((warp & 3) * 32) << 16;
+    const int w = warp >> 3, ch = warp >> 2 & 1;   // half of the keys, half of the columns
+    const int row = (warp & 3) * 32 + lane;        // the key's row of its half: its TMEM lane
+    const uint32_t ts = (tmem + 256u * w + 64u * ch) | (uint32_t)((warp & 3) * 32) << 16;
     const float c = a.scale_log2e;
-    float acc[4] = {0.f, 0.f, 0.f, 0.f};
-    int cnt = 0;
+    const f32x2 c2 = pair(c, c);
+    f32x2 acc[2] = {0ull, 0ull};
+    int cnt = 0, parts = 0;                        // S buffers taken, units written
     for (int g = 0;; ++g) {
-      const int st = g % kQStages;
-      if (!__all_sync(kAll, bar_wait(bar(B_QFULL + st), (g / kQStages) & 1, cta_abort, a.d_error, 24000)))
+      const int ls = g % kLStages;
+      if (!__all_sync(kAll, bar_wait(bar(B_LFULL + ls), (g / kLStages) & 1, cta_abort, a.d_error, 24000)))
         break;
-      const TileDesc d = descs[st];
+      const TileDesc d = descs[ls];
       if (d.n_tok == 0) break;
       const int key = d.tok_begin + kKeys * w + row;
-      if (d.tok_begin + kKeys * w < d.end) {     // (the unit reaches into this half)
+      const bool used = d.tok_begin + kKeys * w < d.end;       // (the unit reaches into this half)
+      if (used) {
         const int sb = cnt & 1;
         if (!__all_sync(kAll, bar_wait(bar(B_SFULL + 2 * w + sb), (cnt >> 1) & 1, cta_abort, a.d_error,
                                        24100)))
           break;
         ++cnt;
         tc_fence_after();
-        const uint32_t ts = (tmem + 256u * w + 128u * sb) | lane_sel;
-        const float* lse = lses + st * kKeys;
-        // the key is seen by columns lo .. hi - 1: by the tokens from its own position on
-        const int lo = max(0, key - d.pos) * G, hi = d.n_tok * G;
-        const bool all = __all_sync(kAll, lo == 0 && d.n_tok == T);
-        for (int q4 = 0; q4 < 4; ++q4) {
-          uint32_t s[32];
-          TMEM_LD_32(ts + 32u * q4, s, 0);
-          tmem_wait_ld();
-          if (q4 == 3) {                         // all of it is in registers
+        uint32_t s[64];
+        TMEM_LD_32(ts + 128u * sb, s, 0);
+        tmem_wait_ld();
+        // the key is seen by columns lo .. hi - 1, by the tokens from its own position on; a whole tile but
+        // for zero rows behind its last token, whose log-sum-exp is infinite
+        const int lo = max(0, key - d.pos) * G - 64 * ch, hi = d.n_tok * G - 64 * ch;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          if (q == 0) {
+            TMEM_LD_32(ts + 128u * sb + 32u, s, 32);
+          } else {
+            tmem_wait_ld();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) bar_arrive(bar(B_SEMPTY + 2 * w + sb));
           }
-          if (all) {
+          const float* lse = lses + ls * kKeys + 64 * ch + 32 * q;     // (times - log2 e)
+          if (__all_sync(kAll, lo <= 32 * q && (hi >= 32 * q + 32 || d.n_tok == T))) {
 #pragma unroll
-            for (int j = 0; j < 32; j += 4) {
-              const float4 l = *(const float4*)(lse + 32 * q4 + j);
-              acc[0] += ex2(fmaf(__uint_as_float(s[j]), c, -l.x));
-              acc[1] += ex2(fmaf(__uint_as_float(s[j + 1]), c, -l.y));
-              acc[2] += ex2(fmaf(__uint_as_float(s[j + 2]), c, -l.z));
-              acc[3] += ex2(fmaf(__uint_as_float(s[j + 3]), c, -l.w));
+            for (int j = 0; j < 16; ++j) {
+              const f32x2 l = *(const f32x2*)(lse + 2 * j);
+              const f32x2 x = fma2(pair(__uint_as_float(s[32 * q + 2 * j]), __uint_as_float(s[32 * q + 2 * j + 1])),
+                                   c2, l);
+              float e0, e1;
+              unpair(x, e0, e1);
+              acc[j & 1] = add2(acc[j & 1], pair(ex2(e0), ex2(e1)));
             }
-          } else {
+          } else if (!__all_sync(kAll, lo >= 32 * q + 32 || hi <= 32 * q)) {
+            float part[2] = {0.f, 0.f};
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
-              const int col = 32 * q4 + j;
-              const float p = ex2(fmaf(__uint_as_float(s[j]), c, -lse[col]));
-              if (col >= lo && col < hi) acc[j & 3] += p;
+              const float p = ex2(fmaf(__uint_as_float(s[32 * q + j]), c, lse[j]));
+              if (32 * q + j >= lo && 32 * q + j < hi) part[j & 1] += p;
             }
+            acc[1] = add2(acc[1], pair(part[0], part[1]));
           }
         }
       }
       __syncwarp();
-      if (lane == 0) bar_arrive(bar(B_QEMPTY + st));
-      if (d.flags & 2) {
+      if (lane == 0) bar_arrive(bar(B_LEMPTY + ls));
+      if ((d.flags & F_LAST) && used) {
+        float sum, more;
+        unpair(add2(acc[0], acc[1]), sum, more);
+        sum += more;
+        float* out = nullptr;
         if (key < d.end) {
           const int block = a.d_tables[(size_t)d.table_row * a.shape.table_stride + (key >> 4)];
-          float* out = a.weights + ((size_t)block * HKV + d.kvh) * kBlock + (key & 15);
-          const float sum = (acc[0] + acc[1]) + (acc[2] + acc[3]);
-          *out = a.replace ? sum : *out + sum;
+          out = a.weights + ((size_t)block * HKV + d.kvh) * kBlock + (key & 15);
         }
-        acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
+        if (ch == 0) {
+          if (out) *out = a.replace ? sum : *out + sum;
+          if (parts > 0 && !__all_sync(kAll, bar_wait(bar(B_WEMPTY + w), (parts - 1) & 1, cta_abort,
+                                                      a.d_error, 24200)))
+            break;
+          __syncwarp();
+          if (lane == 0) bar_arrive(bar(B_WFULL + w));
+        } else {
+          if (!__all_sync(kAll, bar_wait(bar(B_WFULL + w), parts & 1, cta_abort, a.d_error, 24300))) break;
+          if (lane == 0) bar_arrive(bar(B_WEMPTY + w));
+          if (out) *out += sum;
+        }
+        ++parts;
+        acc[0] = acc[1] = 0ull;
       }
     }
   }
   // ---- common exit: every role arrives here, then the allocating warp frees TMEM
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == kSumWarps + 2) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
   }
@@ -308,7 +462,7 @@ cudaError_t launch_prompt_weights(const KeyArgs& a, const CUtensorMap* tm_k, con
                                              cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
   if (e != cudaSuccess) return e;
   const int grid = (int)std::min<int64_t>((int64_t)n_units * a.shape.num_kv_heads, a.num_sms);
-  return launch_kernel(prompt_weights_kernel, dim3(grid), dim3(320), kSmem, st, false, *tm_k, *tm_q, a, n_units);
+  return launch_kernel(prompt_weights_kernel, dim3(grid), dim3(kWarps * 32), kSmem, st, false, *tm_k, *tm_q, a, n_units);
 }
 
 }  // namespace apar
