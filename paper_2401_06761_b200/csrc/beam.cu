@@ -5,8 +5,10 @@
 // enough: it keeps, per piece of a row, the num_select largest logits and the piece's maximum and sum
 // of exponentials, and a second small kernel puts the pieces of a sequence's rows together.
 //
-// beam_scan_kernel   one CTA per piece, which reads up to 16384 elements into registers, 64 to a
-//     thread, all loads on their way at once.  A threshold that at least num_select elements reach comes
+// beam_scan_kernel   one CTA per piece, which reads up to 12288 (f32) or 16384 (16-bit) elements into
+//     registers, all loads on their way at once.  A thread's words are 1 KiB apart, so that loads are
+//     whole lines wherever a row begins, and the order of the sums depends on the token alone: equal rows
+//     tie exactly.  A threshold that at least num_select elements reach comes
 //     from the threads' maxima: with j = num_select / 8 rounded up, the least of the eight warps' j-th
 //     largest.  The few elements that reach it (some two to three times num_select) are collected in shared
 //     memory and put in order by counting, for each, how many are larger.  A key is (ordered bits of
@@ -31,8 +33,6 @@ namespace apar {
 namespace {
 
 constexpr int kWarps = 8, kThreads = 32 * kWarps;
-constexpr int kGroups = 8;                    // groups of eight elements a thread holds
-constexpr int kChunk = kThreads * kGroups;    // groups a CTA holds
 constexpr int kCand = 512;                    // elements that may reach a threshold
 constexpr int kBuf = 128;                     // keys a warp holds where more do
 constexpr int kMaxSelect = 64, kMaxBeams = 64;
@@ -51,66 +51,52 @@ __device__ __forceinline__ float unordered(uint32_t o) {   // (what is below -in
   return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
 }
 
+// A row's elements as words: one f32, or two 16-bit ones.
 __device__ __forceinline__ float number(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float number(__half x) { return __half2float(x); }
 __device__ __forceinline__ float number(float x) { return x; }
-
-__device__ __forceinline__ void numbers(const uint32_t* w, const __nv_bfloat16*, float (&x)[8]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ void numbers(const uint32_t* w, const __half*, float (&x)[8]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 f = __half22float2(*(const __half2*)&w[i]);
-    x[2 * i] = f.x;
-    x[2 * i + 1] = f.y;
-  }
-}
-__device__ __forceinline__ void numbers(const uint32_t* w, const float*, float (&x)[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
-}
-
-// Elements 8 at .. 8 at + 7 of a row; -inf past its end.  Groups are counted from the row's first
-// element wherever that lies, so that two equal rows are summed in the same order and tie exactly:
-// a row that begins off a 16-byte boundary (`off` elements behind one) is read in the aligned pieces
-// that cover the group, which are then shifted into place.
 template <typename T>
-__device__ __forceinline__ void load_group(const T* row, int vocab, int off, int at, float (&x)[8]) {
-  constexpr int kWords = 2 * (int)sizeof(T);           // of a group
-  constexpr int kPiece = 16 / (int)sizeof(T);          // elements of 16 bytes
-  const T* p = row + (int64_t)at * 8;
-  if (off == 0 && at * 8 + 8 <= vocab) {
-    uint32_t w[kWords];
-#pragma unroll
-    for (int i = 0; i < kWords / 4; ++i) *(uint4*)(w + 4 * i) = __ldg((const uint4*)p + i);
-    numbers(w, row, x);
-  } else if (off != 0 && at > 0 && at * 8 + 8 + kPiece - off <= vocab) {
-    uint32_t w[kWords + 4];                            // (all of it inside the row)
-#pragma unroll
-    for (int i = 0; i < kWords / 4 + 1; ++i) *(uint4*)(w + 4 * i) = __ldg((const uint4*)(p - off) + i);
-    const int words = sizeof(T) == 4 ? off : off >> 1;
-    if (words & 2) {
-#pragma unroll
-      for (int i = 0; i < kWords + 2; ++i) w[i] = w[i + 2];
-    }
-    if (words & 1) {
-#pragma unroll
-      for (int i = 0; i < kWords + 1; ++i) w[i] = w[i + 1];
-    }
-    if (sizeof(T) == 2 && (off & 1)) {
-#pragma unroll
-      for (int i = 0; i < kWords; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
-    }
-    numbers(w, row, x);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = at * 8 + e < vocab ? number(__ldg(p + e)) : -INFINITY;
+struct Words;
+template <>
+struct Words<float> {
+  static constexpr int kPer = 1, kHeld = 48;           // elements of a word, words a thread holds
+  static constexpr uint32_t kNone = 0xff800000u;       // -inf
+  static __device__ __forceinline__ void numbers(uint32_t w, float (&x)[1]) { x[0] = __uint_as_float(w); }
+};
+template <>
+struct Words<__nv_bfloat16> {
+  static constexpr int kPer = 2, kHeld = 32;
+  static constexpr uint32_t kNone = 0xff80ff80u;
+  static __device__ __forceinline__ void numbers(uint32_t w, float (&x)[2]) {
+    x[0] = __uint_as_float(w << 16);
+    x[1] = __uint_as_float(w & 0xffff0000u);
   }
+};
+template <>
+struct Words<__half> {
+  static constexpr int kPer = 2, kHeld = 32;
+  static constexpr uint32_t kNone = 0xfc00fc00u;
+  static __device__ __forceinline__ void numbers(uint32_t w, float (&x)[2]) {
+    const float2 f = __half22float2(*(const __half2*)&w);
+    x[0] = f.x;
+    x[1] = f.y;
+  }
+};
+// Word `at` of a row of n elements; what lies past its end is -inf.  `odd`: the row's words are not aligned.
+__device__ __forceinline__ uint32_t load_word(const float* row, int n, bool, int at) {
+  return at < n ? __float_as_uint(__ldg(row + at)) : Words<float>::kNone;
+}
+template <typename T>
+__device__ __forceinline__ uint32_t load_word(const T* row, int n, bool odd, int at) {
+  uint32_t w = Words<T>::kNone;
+  if (2 * at + 1 < n) {
+    if (!odd) return __ldg((const uint32_t*)row + at);
+    const uint16_t* p = (const uint16_t*)row + 2 * at;
+    w = (uint32_t)__ldg(p) | (uint32_t)__ldg(p + 1) << 16;
+  } else if (2 * at < n) {
+    w = (w & 0xffff0000u) | __ldg((const uint16_t*)row + 2 * at);
+  }
+  return w;
 }
 
 struct BeamArgs {
@@ -201,34 +187,27 @@ __device__ __noinline__ int cut_back(u64* buf, int n, int select) {
   return min(n, select);
 }
 
-// The `select` largest of the groups [g0, g1) that reach tau, one warp; sorted into buf, their number
+// The `select` largest of the elements [e0, e1) that reach tau, one warp; sorted into buf, their number
 // returned.
 template <typename T>
-__device__ int scan_again(const T* row, int vocab, int off, int g0, int g1, float tau, int select,
-                          u64* buf) {
+__device__ int scan_again(const T* row, int e0, int e1, float tau, int select, u64* buf) {
   const int lane = threadIdx.x & 31;
   int n = 0;
   u64 last = 0;                                // keys below this one are of no use
-  for (int g = g0; g < g1; g += 32) {
-    float x[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = -INFINITY;
-    if (g + lane < g1) load_group(row, vocab, off, g + lane, x);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const u64 key = (u64)ordered(x[e]) << 32 | (uint32_t)~((g + lane) * 8 + e);
-      const bool in = x[e] >= tau && x[e] > -INFINITY;     // (a NaN is not)
-      unsigned who = __ballot_sync(kAll, in && key > last);
-      if (who == 0) continue;
-      if (n + 32 > kBuf) {                     // (more than num_select are held)
-        n = cut_back(buf, n, select);
-        last = buf[n - 1];
-        who = __ballot_sync(kAll, in && key > last);
-      }
-      if (who >> lane & 1) buf[n + __popc(who & ((1u << lane) - 1))] = key;
-      n += __popc(who);
-      __syncwarp();
+  for (int e = e0; e < e1; e += 32) {
+    const float x = e + lane < e1 ? number(row[e + lane]) : -INFINITY;
+    const u64 key = (u64)ordered(x) << 32 | (uint32_t)~(e + lane);
+    const bool in = x >= tau && x > -INFINITY;             // (a NaN is not)
+    unsigned who = __ballot_sync(kAll, in && key > last);
+    if (who == 0) continue;
+    if (n + 32 > kBuf) {                       // (more than num_select are held)
+      n = cut_back(buf, n, select);
+      last = buf[n - 1];
+      who = __ballot_sync(kAll, in && key > last);
     }
+    if (who >> lane & 1) buf[n + __popc(who & ((1u << lane) - 1))] = key;
+    n += __popc(who);
+    __syncwarp();
   }
   return cut_back(buf, n, select);
 }
@@ -240,7 +219,9 @@ union ScanKeys {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 2) beam_scan_kernel(const BeamArgs a) {
+__global__ void __launch_bounds__(kThreads, 3) beam_scan_kernel(const BeamArgs a) {
+  using W = Words<T>;
+  constexpr int kPer = W::kPer, kHeld = W::kHeld, kChunk = kThreads * kHeld;   // words of a CTA
   __shared__ ScanKeys sh;
   __shared__ u64 held[kMaxSelect];             // the largest so far, in order
   __shared__ uint32_t tops[2 * kWarps];
@@ -251,69 +232,82 @@ __global__ void __launch_bounds__(kThreads, 2) beam_scan_kernel(const BeamArgs a
   const int row = blockIdx.x / a.pieces, piece = blockIdx.x % a.pieces;
   const int seq = row / a.beams, beam = row % a.beams;
   const T* x = (const T*)a.logits + seq * a.seq_stride + beam * a.beam_stride;
-  const int off = (int)((uintptr_t)x & 15) / (int)sizeof(T);
-  const int groups = (a.vocab + 7) / 8, per_piece = (groups + a.pieces - 1) / a.pieces;
-  const int end = min(groups, (piece + 1) * per_piece);
+  const bool odd = (uintptr_t)x & 3;
+  const int words = (a.vocab + kPer - 1) / kPer, per_piece = (words + a.pieces - 1) / a.pieces;
+  const int end = min(words, (piece + 1) * per_piece);
   const bool skip = a.finished && a.finished[row];     // (has its one continuation, see the other kernel)
   int n_held = 0;
   float m = -INFINITY, l = 0.f;
   for (int c0 = skip ? end : piece * per_piece; c0 < end; c0 += kChunk) {
-    float v[kGroups][8];
+    const int n_in = min(a.vocab, end * kPer);         // elements before this one are the piece's
+    uint32_t v[kHeld];
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) v[k] = load_word(x, n_in, odd, c0 + k * kThreads + threadIdx.x);
     float mine = -INFINITY;
 #pragma unroll
-    for (int u = 0; u < kGroups; ++u) {
-      const int at = c0 + u * kThreads + threadIdx.x;
-      if (at < end) {
-        load_group(x, a.vocab, off, at, v[u]);
-      } else {
+    for (int k = 0; k < kHeld; ++k) {
+      float e[kPer];
+      W::numbers(v[k], e);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[u][e] = -INFINITY;
-      }
+      for (int i = 0; i < kPer; ++i) mine = fmaxf(mine, e[i]);
     }
-#pragma unroll
-    for (int u = 0; u < kGroups; ++u)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) mine = fmaxf(mine, v[u][e]);
     if (threadIdx.x == 0) n_cand = n_held;
     if ((int)threadIdx.x < n_held) sh.cand[threadIdx.x] = held[threadIdx.x];
     uint32_t most;
-    float tau = unordered(threshold(ordered(mine == mine ? mine : -INFINITY), a.select,
-                                    min(end - c0, kChunk) / 32, tops, &most));
+    float tau = unordered(threshold(ordered(mine), a.select, min(end - c0, kChunk) / 32, tops, &most));
     if (n_held == a.select) tau = fmaxf(tau, unordered((uint32_t)(held[n_held - 1] >> 32)));
-    // (x - max before the factor: rounding max log2 e would be the same error in every term)
-    const float ref = unordered(most) == -INFINITY ? 0.f : unordered(most);
-    float part = 0.f;
+    // 2^(x log2 e - ref), ref being max log2 e; what rounding that product takes off every exponent is
+    // put back into the sum
+    const float top = unordered(most);
+    const bool finite = top - top == 0.f;
+    const float ref = top == -INFINITY ? 0.f : top * kLog2e;
+    float part[2] = {0.f, 0.f};
 #pragma unroll
-    for (int u = 0; u < kGroups; ++u) {
-      float p[2] = {0.f, 0.f};
+    for (int k = 0; k < kHeld; ++k) {
+      float e[kPer];
+      W::numbers(v[k], e);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) p[e & 1] += ex2((v[u][e] - ref) * kLog2e);
-      part += p[0] + p[1];
+      for (int i = 0; i < kPer; ++i) part[(k + i) & 1] += ex2(fmaf(e[i], kLog2e, -ref));
     }
+    // The few elements that reach the threshold: bits first, then a loop that reads them again (a copy
+    // of what to do with one for each word a thread holds would be 600 instructions to fetch).
     if (mine >= tau && mine > -INFINITY) {
+      u64 hits = 0;
 #pragma unroll
-      for (int u = 0; u < kGroups; ++u)
+      for (int k = 0; k < kHeld; ++k) {
+        float e[kPer];
+        W::numbers(v[k], e);
+        bool any = false;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (v[u][e] >= tau && v[u][e] > -INFINITY) {
-            const int i = atomicAdd(&n_cand, 1);
-            const uint32_t token = (c0 + u * kThreads + threadIdx.x) * 8 + e;
-            if (i < kCand) sh.cand[i] = (u64)ordered(v[u][e]) << 32 | ~token;
+        for (int i = 0; i < kPer; ++i) any = any || e[i] >= tau;
+        if (any) hits |= 1ull << k;
+      }
+      for (; hits; hits &= hits - 1) {
+        const uint32_t token = (c0 + (__ffsll(hits) - 1) * kThreads + threadIdx.x) * kPer;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          const float e = (int)token + i < n_in ? number(x[token + i]) : -INFINITY;
+          if (e >= tau && e > -INFINITY) {
+            const int at = atomicAdd(&n_cand, 1);
+            if (at < kCand) sh.cand[at] = (u64)ordered(e) << 32 | ~(token + i);
           }
+        }
+      }
     }
+    float sum = part[0] + part[1];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(kAll, part, o);
-    if (lane == 0) sums[warp] = part;
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
+    if (lane == 0) sums[warp] = sum;
     __syncthreads();
     // maximum and sum so far
     {
       float s = 0.f;
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) s += sums[w];
-      const float top = fmaxf(m, unordered(most));
-      const float r = top == -INFINITY ? 0.f : top;
-      l = l * ex2((m - r) * kLog2e) + s * ex2((ref - r) * kLog2e);
-      m = top;
+      if (finite) s *= ex2(fmaf(-kLog2e, top, ref));
+      const float both = fmaxf(m, top), r = both == -INFINITY ? 0.f : both;
+      l = l * ex2((m - r) * kLog2e) + s * (top == -INFINITY ? 1.f : ex2((top - r) * kLog2e));
+      m = both;
     }
     const int n = n_cand;
     if (n <= kCand) {
@@ -327,9 +321,8 @@ __global__ void __launch_bounds__(kThreads, 2) beam_scan_kernel(const BeamArgs a
       n_held = min(n, a.select);
       __syncthreads();
     } else {
-      const int per_warp = (kChunk + kWarps - 1) / kWarps, first = c0 + warp * per_warp;
-      const int found = scan_again(x, a.vocab, off, first, min(min(end, c0 + kChunk), first + per_warp), tau,
-                                   a.select, sh.bufs[warp]);
+      const int per_warp = kChunk / kWarps * kPer, first = c0 * kPer + warp * per_warp;
+      const int found = scan_again(x, first, min(n_in, first + per_warp), tau, a.select, sh.bufs[warp]);
       if (lane == 0) counts[warp] = found;
       __syncthreads();
       // the warps' sorted lists and what is held become one list
@@ -384,16 +377,20 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
   const int seq = blockIdx.x, n_lists = a.beams * a.pieces, n_all = n_lists * a.select;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_wait();                                  // (the scan has written its lists)
+  // (everything that is needed first is asked for at once)
+  const u64* keys = a.keys + (size_t)seq * n_all;
+  const u64 key0 = (int)threadIdx.x < n_all ? keys[threadIdx.x] : 0ull;
+  const int b = threadIdx.x, row = seq * a.beams + b;
+  const float score = b < a.beams ? a.scores[row] : 0.f;
+  const bool done = b < a.beams && a.finished && a.finished[row];
   if (threadIdx.x == 0) n_cand = 0;
   for (int i = threadIdx.x; i < n_lists; i += kThreads) stats[i] = a.stats[(size_t)seq * n_lists + i];
   __syncthreads();
-  if ((int)threadIdx.x < a.beams) {
-    const int b = threadIdx.x, row = seq * a.beams + b;
-    const float score = a.scores[row];
-    over[b] = a.finished && a.finished[row];
+  if (b < a.beams) {
+    over[b] = done;
     double to = NAN;
     if (score - score == 0.f) {                // finite
-      if (over[b]) {
+      if (done) {
         to = score;
       } else {
         float M = -INFINITY;
@@ -411,11 +408,10 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
   }
   __syncthreads();
   // pair i of the lists; a value that is not above -inf: none
-  const u64* keys = a.keys + (size_t)seq * n_all;
   auto pair_of = [&](int i) {
     const int list = i / a.select, b = list / a.pieces;
     if (over[b]) return Pair{i % (a.pieces * a.select) ? -INFINITY : base[b], (u64)b << 32 | (uint32_t)a.eos};
-    const u64 key = keys[i];
+    const u64 key = i < kThreads ? key0 : keys[i];   // (every thread asks for i = its own first)
     return Pair{key ? base[b] + (double)unordered((uint32_t)(key >> 32)) : -INFINITY,
                 (u64)b << 32 | (uint32_t)~(uint32_t)key};
   };
@@ -482,7 +478,8 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
 // machine twice over, none shorter than 2048 elements.
 int pieces_of(const apar_beam_config* c, int32_t n_seq) {
   const int64_t rows = (int64_t)n_seq * c->num_beams;
-  const int64_t fit = (c->vocab + 8 * kChunk - 1) / (8 * kChunk);
+  const int64_t held = kThreads * (c->logits_type == APAR_LOGITS_F32 ? Words<float>::kHeld : 2 * Words<__half>::kHeld);
+  const int64_t fit = (c->vocab + held - 1) / held;
   int64_t p = std::min<int64_t>((2 * 148 + rows - 1) / rows, (c->vocab + 2047) / 2048);
   p = std::min<int64_t>({std::max(p, fit), kMaxPieces, kMaxLists / c->num_beams});
   return (int)std::max<int64_t>(1, p);
