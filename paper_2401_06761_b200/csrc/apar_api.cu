@@ -673,7 +673,7 @@ apar_status run_attention(apar_ctx* c, int n, const int32_t* qslots, const int32
   return APAR_OK;
 }
 
-// New rows have received no weight yet, a copied row what its original has (every layer at once).
+// New rows have received no weight yet (every layer at once).
 apar_status clear_weights(apar_ctx* c, const int32_t* d_slots, int n_rows, cudaStream_t st) {
   if (!c->weights || n_rows <= 0) return APAR_OK;
   APAR_CUDA(c, launch_weights_clear((float*)c->weights, c->layer_weights(), c->num_layers, d_slots,
@@ -681,10 +681,20 @@ apar_status clear_weights(apar_ctx* c, const int32_t* d_slots, int n_rows, cudaS
   ++c->kernels_total;
   return APAR_OK;
 }
-apar_status copy_weights(apar_ctx* c, const CowCopy* d_copies, int n, cudaStream_t st) {
-  if (!c->weights) return APAR_OK;
-  APAR_CUDA(c, launch_weights_cow((float*)c->weights, c->layer_weights(), c->num_layers, d_copies, n,
-                                  c->cfg.num_kv_heads, st));
+// Copies partial blocks, in every layer, their weights along with the rows.
+apar_status copy_rows(apar_ctx* c, const CowCopy* d_copies, int n, cudaStream_t st) {
+  if (c->q4) {
+    for (int l = 0; l < c->num_layers; ++l) {
+      APAR_CUDA(c, launch_q4_cow_copy((char*)c->cfg.k_pool + l * c->layer_bytes,
+                                      (char*)c->cfg.v_pool + l * c->layer_bytes, d_copies, n,
+                                      c->cfg.num_kv_heads, st));
+      ++c->kernels_total;
+    }
+    return APAR_OK;
+  }
+  APAR_CUDA(c, launch_cow_copy(c->cfg.k_pool, c->cfg.v_pool, c->num_layers,
+                               (size_t)c->cfg.num_blocks * c->cfg.num_kv_heads, (float*)c->weights,
+                               d_copies, n, c->cfg.num_kv_heads, st));
   ++c->kernels_total;
   return APAR_OK;
 }
@@ -1012,14 +1022,7 @@ apar_status apar_fork(apar_ctx* c, int32_t n, const int32_t* parent_tid, int32_t
     char* d_stage = c->ws(c->lay.stage);
     apar_status rc = send(c, stg, d_stage, (size_t)nc * sizeof(CowCopy), st);
     if (rc) return rc;
-    for (int l = 0; l < c->num_layers; ++l) {
-      auto copy = c->q4 ? launch_q4_cow_copy : launch_cow_copy;
-      APAR_CUDA(c, copy((char*)c->cfg.k_pool + l * c->layer_bytes,
-                        (char*)c->cfg.v_pool + l * c->layer_bytes, (const CowCopy*)d_stage, nc,
-                        c->cfg.num_kv_heads, st));
-      ++c->kernels_total;
-    }
-    return copy_weights(c, (const CowCopy*)d_stage, nc, st);
+    return copy_rows(c, (const CowCopy*)d_stage, nc, st);
   }
   return APAR_OK;
 }
@@ -1808,14 +1811,7 @@ apar_status apar_reorder(apar_ctx* c, int32_t n, const int32_t* tid, const int32
     char* d_stage = c->ws(c->lay.stage);
     apar_status rc = send(c, stg, d_stage, (size_t)nc * sizeof(CowCopy), st);
     if (rc) return rc;
-    for (int l = 0; l < c->num_layers; ++l) {
-      auto copy = c->q4 ? launch_q4_cow_copy : launch_cow_copy;
-      APAR_CUDA(c, copy((char*)c->cfg.k_pool + l * c->layer_bytes,
-                        (char*)c->cfg.v_pool + l * c->layer_bytes, (const CowCopy*)d_stage, nc,
-                        c->cfg.num_kv_heads, st));
-      ++c->kernels_total;
-    }
-    return copy_weights(c, (const CowCopy*)d_stage, nc, st);
+    return copy_rows(c, (const CowCopy*)d_stage, nc, st);
   }
   return APAR_OK;
 }

@@ -128,8 +128,10 @@ inline cudaError_t launch_kernel(void (*kernel)(KArgs...), dim3 grid, dim3 block
 void note_cuda_error(cudaError_t e);
 
 // ---- kernel launchers (kernels.cu); all enqueue on `st` and return cudaGetLastError() ----
-cudaError_t launch_cow_copy(void* k_pool, void* v_pool, const CowCopy* d_copies, int n,
-                            int num_kv_heads, cudaStream_t st);
+// All layers at once; layer_tiles: (block, kv head) tiles of a layer.  weights may be NULL.
+cudaError_t launch_cow_copy(void* k_pool, void* v_pool, int num_layers, size_t layer_tiles,
+                            float* weights, const CowCopy* d_copies, int n, int num_kv_heads,
+                            cudaStream_t st);
 // dst[0..bytes) = src_mapped[0..bytes) read by the SMs; src_mapped is the device alias of a
 // pinned, mapped host buffer; bytes is a multiple of 4.
 cudaError_t launch_stage_copy(void* dst, const void* src_mapped, size_t bytes, cudaStream_t st);
@@ -218,7 +220,7 @@ cudaError_t launch_row_moves(void* k_pool, void* v_pool, const RowMove* d_moves,
 cudaError_t launch_merge(const AttnArgs& a, const MergeRef* d_merge, int n_merge, cudaStream_t st);
 
 // ---- pools held in 4 bits (kv4.cu, attn_q4.cu; layout in kv4.cuh) ----
-// The same jobs as launch_append, launch_cow_copy and launch_row_moves above.
+// The same jobs as launch_append, launch_cow_copy (one layer) and launch_row_moves above.
 cudaError_t launch_q4_append(void* k_pool, void* v_pool, const void* k_new, const void* v_new,
                              const int32_t* d_slots, int64_t first_row, int n_rows,
                              int num_kv_heads, cudaStream_t st);
@@ -308,8 +310,6 @@ struct EvictArgs {
 };
 cudaError_t launch_weights_clear(float* w, size_t layer_floats, int num_layers, const int32_t* d_slots,
                                  int n_rows, int num_kv_heads, cudaStream_t st);
-cudaError_t launch_weights_cow(float* w, size_t layer_floats, int num_layers, const CowCopy* d_copies,
-                               int n, int num_kv_heads, cudaStream_t st);
 cudaError_t launch_weights_move(float* w, size_t layer_floats, int num_layers, const RowMove* d_moves,
                                 const int32_t* d_group_begin, int n_groups, int num_kv_heads,
                                 cudaStream_t st);

@@ -369,7 +369,7 @@ __device__ __forceinline__ bool before(const Pair& a, const Pair& b) {
 __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
   __shared__ Pair cand[kCand];
   __shared__ double base[kMaxBeams];           // score - lse; NaN: the beam has no pairs
-  __shared__ float2 stats[kMaxLists];
+  __shared__ float2 stats[kMaxLists], terms[kMaxLists];
   __shared__ uint8_t over[kMaxBeams];
   __shared__ uint32_t tops[2 * kWarps];
   __shared__ Pair picks[kWarps];
@@ -384,7 +384,18 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
   const float score = b < a.beams ? a.scores[row] : 0.f;
   const bool done = b < a.beams && a.finished && a.finished[row];
   if (threadIdx.x == 0) n_cand = 0;
-  for (int i = threadIdx.x; i < n_lists; i += kThreads) stats[i] = a.stats[(size_t)seq * n_lists + i];
+  // (n_lists <= kMaxLists < kThreads)
+  float2 mine_s = make_float2(-INFINITY, 0.f);
+  if (b < n_lists) stats[b] = mine_s = a.stats[(size_t)seq * n_lists + b];
+  __syncthreads();
+  if (b < n_lists) {
+    const int first = b / a.pieces * a.pieces;
+    float M = -INFINITY;
+    for (int p = first; p < first + a.pieces; ++p) M = fmaxf(M, stats[p].x);
+    // the piece's sum relative to the row's maximum
+    terms[b] = make_float2(M, mine_s.x == M || mine_s.x == -INFINITY ? mine_s.y
+                                                                     : mine_s.y * ex2((mine_s.x - M) * kLog2e));
+  }
   __syncthreads();
   if (b < a.beams) {
     over[b] = done;
@@ -393,14 +404,9 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
       if (done) {
         to = score;
       } else {
-        float M = -INFINITY;
-        for (int p = 0; p < a.pieces; ++p) M = fmaxf(M, stats[b * a.pieces + p].x);
         double L = 0.0;
-        for (int p = 0; p < a.pieces; ++p) {
-          const float2 s = stats[b * a.pieces + p];
-          L += s.x == M || s.x == -INFINITY ? (double)s.y : (double)s.y * exp((double)s.x - (double)M);
-        }
-        const double lse = (double)M + log(L);
+        for (int p = 0; p < a.pieces; ++p) L += terms[b * a.pieces + p].y;
+        const double lse = terms[b * a.pieces].x + log(L);
         if (lse - lse == 0.0) to = (double)score - lse;
       }
     }

@@ -11,26 +11,38 @@
 namespace apar {
 
 // ------------------------------------------------------------------ fork: copy r rows
-// One CTA per (copy, kv head, K|V): the r valid rows of a (block, head) tile are r * 256
-// contiguous bytes.
+// One CTA per (copy, kv head, layer and K|V): the r valid rows of a (block, head) tile are r * 256
+// contiguous bytes.  Where accumulated weights are kept, the rows' weights go along.
 __global__ void __launch_bounds__(128) cow_copy_kernel(uint4* __restrict__ k_pool,
-                                                       uint4* __restrict__ v_pool,
+                                                       uint4* __restrict__ v_pool, size_t layer_tiles,
+                                                       float* __restrict__ weights,
                                                        const CowCopy* __restrict__ copies,
                                                        int num_kv_heads) {
   const CowCopy c = copies[blockIdx.x];
-  uint4* pool = blockIdx.z ? v_pool : k_pool;
+  uint4* pool = blockIdx.z & 1 ? v_pool : k_pool;
   const size_t tile = kTileBytes / 16;
-  const uint4* src = pool + ((size_t)c.src_block * num_kv_heads + blockIdx.y) * tile;
-  uint4* dst = pool + ((size_t)c.dst_block * num_kv_heads + blockIdx.y) * tile;
+  const size_t layer = (blockIdx.z >> 1) * layer_tiles;
+  const size_t from = layer + (size_t)c.src_block * num_kv_heads + blockIdx.y;
+  const size_t to = layer + (size_t)c.dst_block * num_kv_heads + blockIdx.y;
+  const uint4* src = pool + from * tile;
+  uint4* dst = pool + to * tile;
   const int n = c.rows * (kDim * 2 / 16);
   for (int i = threadIdx.x; i < n; i += blockDim.x) dst[i] = src[i];
+  if (weights && !(blockIdx.z & 1) && (int)threadIdx.x < c.rows)
+    weights[to * kBlock + threadIdx.x] = weights[from * kBlock + threadIdx.x];
 }
 
-cudaError_t launch_cow_copy(void* k_pool, void* v_pool, const CowCopy* d_copies, int n,
-                            int num_kv_heads, cudaStream_t st) {
+cudaError_t launch_cow_copy(void* k_pool, void* v_pool, int num_layers, size_t layer_tiles,
+                            float* weights, const CowCopy* d_copies, int n, int num_kv_heads,
+                            cudaStream_t st) {
   if (n <= 0) return cudaSuccess;
-  cow_copy_kernel<<<dim3(n, num_kv_heads, 2), 128, 0, st>>>((uint4*)k_pool, (uint4*)v_pool,
-                                                            d_copies, num_kv_heads);
+  for (int l = 0; l < num_layers; l += 32767) {          // (the grid's limit)
+    const int layers = std::min(num_layers - l, 32767);
+    const size_t off = (size_t)l * layer_tiles;
+    cow_copy_kernel<<<dim3(n, num_kv_heads, 2 * layers), 128, 0, st>>>(
+        (uint4*)k_pool + off * (kTileBytes / 16), (uint4*)v_pool + off * (kTileBytes / 16), layer_tiles,
+        weights ? weights + off * kBlock : nullptr, d_copies, num_kv_heads);
+  }
   return cudaGetLastError();
 }
 

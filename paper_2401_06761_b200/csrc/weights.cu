@@ -18,7 +18,7 @@ namespace {
 
 constexpr unsigned kAll = 0xffffffffu;
 
-// ------------------------------------------------------------------ rows that come, move and are copied
+// ------------------------------------------------------------------ rows that come and move
 __global__ void __launch_bounds__(256) weights_clear_kernel(float* __restrict__ w, size_t layer_floats,
                                                             const int32_t* __restrict__ slots,
                                                             int n_rows, int num_kv_heads) {
@@ -26,16 +26,6 @@ __global__ void __launch_bounds__(256) weights_clear_kernel(float* __restrict__ 
   if (i >= (int64_t)n_rows * num_kv_heads) return;
   const int slot = slots[i / num_kv_heads], h = (int)(i % num_kv_heads);
   w[blockIdx.y * layer_floats + ((size_t)(slot >> 4) * num_kv_heads + h) * kBlock + (slot & 15)] = 0.f;
-}
-
-__global__ void __launch_bounds__(128) weights_cow_kernel(float* __restrict__ w, size_t layer_floats,
-                                                          const CowCopy* __restrict__ copies,
-                                                          int num_kv_heads) {
-  const CowCopy c = copies[blockIdx.x];
-  float* p = w + blockIdx.y * layer_floats;
-  for (int i = threadIdx.x; i < num_kv_heads * kBlock; i += blockDim.x)
-    if ((i & 15) < c.rows)
-      p[(size_t)c.dst_block * num_kv_heads * kBlock + i] = p[(size_t)c.src_block * num_kv_heads * kBlock + i];
 }
 
 // A group is at most 64 rows whose sources and destinations may overlap: all are read, then written.
@@ -572,13 +562,6 @@ cudaError_t launch_weights_clear(float* w, size_t layer_floats, int num_layers, 
   const unsigned grid = (unsigned)(((int64_t)n_rows * num_kv_heads + 255) / 256);
   return launch_kernel(weights_clear_kernel, dim3(grid, num_layers), dim3(256), 0, st, false, w,
                        layer_floats, d_slots, n_rows, num_kv_heads);
-}
-
-cudaError_t launch_weights_cow(float* w, size_t layer_floats, int num_layers, const CowCopy* d_copies,
-                               int n, int num_kv_heads, cudaStream_t st) {
-  if (n <= 0) return cudaSuccess;
-  return launch_kernel(weights_cow_kernel, dim3(n, num_layers), dim3(128), 0, st, false, w,
-                       layer_floats, d_copies, num_kv_heads);
 }
 
 cudaError_t launch_weights_move(float* w, size_t layer_floats, int num_layers, const RowMove* d_moves,

@@ -82,7 +82,7 @@ class BeamSelect:
         self.beams, self.vocab, self.select = beams, vocab, select
         self.cfgs = {t: B.make_beam_config(vocab, beams, select, str(t).rpartition(".")[2], eos)
                      for t in (torch.bfloat16, torch.float16, torch.float32)}
-        self._bytes = {}                               # scratch by number of sequences
+        self._bytes = {}                               # scratch by number of sequences and type
 
     def __call__(self, logits: torch.Tensor, scores: torch.Tensor, finished: torch.Tensor = None):
         n = logits.shape[0]
@@ -93,18 +93,22 @@ class BeamSelect:
         if finished is not None:
             assert finished.shape == (n, self.beams) and finished.dtype in (torch.bool, torch.uint8)
             assert finished.get_device() == here and finished.is_contiguous()
-        if (self.vocab > 1 and logits.stride(2) != 1) or 0 in logits.stride()[:2]:
+        by_seq, by_beam, by_token = logits.stride()
+        if (by_token != 1 and self.vocab > 1) or by_seq == 0 or by_beam == 0:
             logits = logits.contiguous()               # (a stride of 0 stands for contiguous rows)
+            by_seq, by_beam, _ = logits.stride()
         cfg = self.cfgs[logits.dtype]
-        if n not in self._bytes:
-            self._bytes[n] = B.apar_beam_workspace_bytes(cfg, n)
-        held = torch.empty(self._bytes[n], dtype=torch.uint8, device=logits.device)
+        nbytes = self._bytes.get((n, logits.dtype))
+        if nbytes is None:
+            nbytes = self._bytes[n, logits.dtype] = B.apar_beam_workspace_bytes(cfg, n)
+        held = torch.empty(nbytes, dtype=torch.uint8, device=logits.device)
         best = torch.empty((n, self.select), dtype=torch.float32, device=logits.device)
-        beams, tokens = torch.empty((2, n, self.select), dtype=torch.int32, device=logits.device)
-        B.apar_beam_select(cfg, n, logits.data_ptr(), logits.stride(0), logits.stride(1),
-                           scores.data_ptr(), 0 if finished is None else finished.data_ptr(),
-                           best.data_ptr(), beams.data_ptr(), tokens.data_ptr(), held.data_ptr(),
-                           self._bytes[n], PagedSession._stream())
+        beams = torch.empty((n, self.select), dtype=torch.int32, device=logits.device)
+        tokens = torch.empty_like(beams)
+        B.apar_beam_select(cfg, n, logits.data_ptr(), by_seq, by_beam, scores.data_ptr(),
+                           0 if finished is None else finished.data_ptr(), best.data_ptr(),
+                           beams.data_ptr(), tokens.data_ptr(), held.data_ptr(), nbytes,
+                           PagedSession._stream())
         return best, beams, tokens
 
 
