@@ -222,19 +222,40 @@ __device__ __forceinline__ uint32_t weight_key(float x) {      // larger weight,
   return x != x ? 0xffffffffu : b ^ (uint32_t)((int32_t)b >> 31 | 0x80000000);
 }
 
-constexpr int kPickThreads = 512, kPickWarps = kPickThreads / 32;
-constexpr int kPickKeys = 32;                                  // a thread holds at most
-constexpr int kPickRows = kPickThreads * kPickKeys;            // a CTA holds at most
+// Threads of a CTA and rows a thread holds: a stretch of up to 2048 rows takes eight warps (every warp adds
+// up counts of its own), a longer one 32 warps and, from 16384 rows on, a cluster.
+constexpr int kPickFew = 256, kPickFewKeys = 8;
+constexpr int kPickMany = 1024, kPickManyKeys = 16;
+constexpr int kPickRows = kPickMany * kPickManyKeys;           // a CTA holds at most
 constexpr int kPickCluster = 8;
 constexpr int kBins = 2048;
 
+template <int kThreads, int kKeys>
 struct __align__(16) PickShared {
+  static constexpr int kWarps = kThreads / 32;
   uint32_t hist[kBins];
-  uint32_t warp_sum[kPickWarps];
+  uint32_t warp_sum[32];
   uint32_t prefix, left;
-  int before[3][kPickKeys * kPickWarps];   // rows of a kind before those of (key, warp), in the CTA
+  int before[3][kKeys * kWarps];           // rows of a kind before those of (key, warp), in the CTA
   int total[3];                            // in the CTA
 };
+
+// Sum of the values of the threads before this one; *all: of all threads.
+template <int kThreads>
+__device__ __forceinline__ uint32_t sum_before(uint32_t mine, uint32_t* warp_sum, uint32_t* all) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint32_t upto = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o *= 2) {
+    const uint32_t x = __shfl_up_sync(kAll, upto, o);
+    if (lane >= o) upto += x;
+  }
+  if (lane == 31) warp_sum[warp] = upto;
+  __syncthreads();
+  const uint32_t w = lane < kThreads / 32 ? warp_sum[lane] : 0;
+  *all = __reduce_add_sync(kAll, w);
+  return __reduce_add_sync(kAll, lane < warp ? w : 0) + upto - mine;
+}
 
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -251,50 +272,41 @@ __device__ __forceinline__ uint32_t ld_peer(const void* p, uint32_t rank) {
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
   return v;
 }
-__device__ __forceinline__ uint4 ld_peer4(const void* p, uint32_t rank) {
+__device__ __forceinline__ uint2 ld_peer2(const void* p, uint32_t rank) {
   uint32_t a;
-  uint4 v;
+  uint2 v;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(s32(p)), "r"(rank));
-  asm volatile("ld.shared::cluster.v4.u32 {%0,%1,%2,%3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  asm volatile("ld.shared::cluster.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
   return v;
 }
 
 // sh.before[kind][..] holds counts per (key, warp) and becomes how many rows of that kind come earlier
 // in the stretch; returns the number of all of them.
-__device__ int ranks_of(PickShared& sh, int kind, int used, uint32_t n_cta, uint32_t me) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int mine = (int)threadIdx.x < used * kPickWarps ? sh.before[kind][threadIdx.x] : 0;
-  int upto = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o *= 2) {
-    const int x = __shfl_up_sync(kAll, upto, o);
-    if (lane >= o) upto += x;
-  }
-  if (lane == 31) sh.warp_sum[warp] = upto;
-  __syncthreads();
-  int base = 0, total = 0;
-  for (int x = 0; x < kPickWarps; ++x) {
-    if (x < warp) base += sh.warp_sum[x];
-    total += sh.warp_sum[x];
-  }
-  if (threadIdx.x == 0) sh.total[kind] = total;
-  int all = total;
+template <int kThreads, int kKeys>
+__device__ int ranks_of(PickShared<kThreads, kKeys>& sh, int kind, int used, uint32_t n_cta, uint32_t me) {
+  constexpr int kWarps = kThreads / 32;
+  static_assert(kKeys * kWarps <= kThreads, "a thread for each count");
+  const int lane = threadIdx.x & 31;
+  const bool on = (int)threadIdx.x < used * kWarps;
+  uint32_t all;
+  uint32_t base = sum_before<kThreads>(on ? sh.before[kind][threadIdx.x] : 0, sh.warp_sum, &all);
   if (n_cta > 1) {
+    if (threadIdx.x == 0) sh.total[kind] = (int)all;
     cluster_sync();
-    const int t = (uint32_t)lane < n_cta ? (int)ld_peer(&sh.total[kind], lane) : 0;   // (a lane per CTA)
+    const uint32_t t = (uint32_t)lane < n_cta ? ld_peer(&sh.total[kind], lane) : 0;   // (a lane per CTA)
     base += __reduce_add_sync(kAll, (uint32_t)lane < me ? t : 0);
     all = __reduce_add_sync(kAll, t);
   }
-  if ((int)threadIdx.x < used * kPickWarps) sh.before[kind][threadIdx.x] = base + upto - mine;
+  if (on) sh.before[kind][threadIdx.x] = (int)base;
   __syncthreads();
-  return all;
+  return (int)all;
 }
 
-template <int kKeys>                             // rows of a thread: few where that is enough, for more CTAs an SM
-__global__ void __launch_bounds__(kPickThreads, kKeys <= 4 ? 4 : 1)
+template <int kThreads, int kKeys>
+__global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 6 : 1)
 evict_pick_kernel(const EvictArgs a, int n_cta) {
-  __shared__ PickShared sh;
+  constexpr int kWarps = kThreads / 32, kPerThread = kBins / kThreads;
+  __shared__ PickShared<kThreads, kKeys> sh;
   const uint32_t me = n_cta > 1 ? cluster_rank() : 0;
   const int entry = blockIdx.x / n_cta;
   const EvictEntry en = a.entries[entry];
@@ -303,63 +315,65 @@ evict_pick_kernel(const EvictArgs a, int n_cta) {
   const float* w = a.weights + (size_t)l * a.layer_floats;
   const int32_t* table = a.d_tables + (size_t)en.table_row * a.table_stride + en.begin / kBlock;
   int2* list = a.moves + en.list_begin + (size_t)lh * en.list_rows;
-  // this CTA's rows, r0 .. r0 + n - 1; thread t holds rows t, t + 512, ... of them
-  const int per = (en.n + n_cta * kPickThreads - 1) / (n_cta * kPickThreads) * kPickThreads;
+  // this CTA's rows, r0 .. r0 + n - 1; thread t holds rows t, t + kThreads, ... of them
+  const int per = (en.n + n_cta * kThreads - 1) / (n_cta * kThreads) * kThreads;
   const int r0 = min(en.n, (int)me * per), n = min(en.n - r0, per);
-  const int used = (n + kPickThreads - 1) / kPickThreads;
+  const int used = (n + kThreads - 1) / kThreads;
   uint32_t key[kKeys];
 #pragma unroll
   for (int k = 0; k < kKeys; ++k) {
     key[k] = 0;
-    const int i = r0 + k * kPickThreads + threadIdx.x;
+    const int i = r0 + k * kThreads + threadIdx.x;
     if (k < used && i < r0 + n)
       key[k] = weight_key(w[((size_t)table[i >> 4] * heads + h) * kBlock + (i & 15)]);
   }
   uint32_t prefix = 0, left = en.keep;           // the left-th largest of the keys that start with prefix
   for (int round = 0; round < 3; ++round) {
     const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, bits = round == 2 ? 10 : 11;
-    for (int i = threadIdx.x; i < kBins; i += kPickThreads) sh.hist[i] = 0;
+    for (int i = threadIdx.x; i < kBins; i += kThreads) sh.hist[i] = 0;
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < kKeys; ++k) {
       if (k >= used) break;
-      if (k * kPickThreads + (int)threadIdx.x < n && (round == 0 || key[k] >> (shift + bits) == prefix))
+      if (k * kThreads + (int)threadIdx.x < n && (round == 0 || key[k] >> (shift + bits) == prefix))
         atomicAdd(&sh.hist[key[k] >> shift & ((1u << bits) - 1)], 1u);
     }
     __syncthreads();
     if (n_cta > 1) cluster_sync();
-    // thread t looks after four bins, from the top down
-    const int top = kBins - 1 - 4 * threadIdx.x;
-    uint4 part[kPickCluster];
+    // a thread looks after a few neighbouring bins, the first one after the highest
+    const int top = kBins - 1 - kPerThread * threadIdx.x;
+    uint32_t c[kPerThread], sum = 0;               // c[0]: the highest
+    if (n_cta == 1) {
 #pragma unroll
-    for (int r = 0; r < kPickCluster; ++r)       // (all on their way at once)
-      part[r] = r == 0 && n_cta == 1 ? *(const uint4*)&sh.hist[top - 3]
-                : r < n_cta          ? ld_peer4(&sh.hist[top - 3], r)
-                                     : make_uint4(0u, 0u, 0u, 0u);
-    uint32_t c[4] = {0, 0, 0, 0};
+      for (int j = 0; j < kPerThread; ++j) c[j] = sh.hist[top - j];
+    } else {
+      uint2 part[kPickCluster];
 #pragma unroll
-    for (int r = 0; r < kPickCluster; ++r) {
-      c[0] += part[r].w;
-      c[1] += part[r].z;
-      c[2] += part[r].y;
-      c[3] += part[r].x;
+      for (int j = 0; j < kPerThread; j += 2) {
+#pragma unroll
+        for (int r = 0; r < kPickCluster; ++r)     // (all on their way at once)
+          part[r] = r < n_cta ? ld_peer2(&sh.hist[top - j - 1], r) : make_uint2(0u, 0u);
+        c[j] = c[j + 1] = 0;
+#pragma unroll
+        for (int r = 0; r < kPickCluster; ++r) {
+          c[j] += part[r].y;
+          c[j + 1] += part[r].x;
+        }
+      }
     }
-    const uint32_t sum = c[0] + c[1] + c[2] + c[3];
-    uint32_t upto = sum;
 #pragma unroll
-    for (int o = 1; o < 32; o *= 2) {
-      const uint32_t x = __shfl_up_sync(kAll, upto, o);
-      if (lane >= o) upto += x;
-    }
-    if (lane == 31) sh.warp_sum[warp] = upto;
-    __syncthreads();
-    for (int x = 0; x < warp; ++x) upto += sh.warp_sum[x];
-    uint32_t above = upto - sum;
-    if (above < left && left <= upto) {
-      int j = 0;
-      while (j < 3 && above + c[j] < left) above += c[j++];
-      sh.prefix = prefix << bits | (uint32_t)(top - j);
-      sh.left = left - above;
+    for (int j = 0; j < kPerThread; ++j) sum += c[j];
+    uint32_t all;
+    uint32_t above = sum_before<kThreads>(sum, sh.warp_sum, &all);
+    if (above < left && left <= above + sum) {
+#pragma unroll
+      for (int j = 0; j < kPerThread; ++j) {
+        if (above < left && left <= above + c[j]) {
+          sh.prefix = prefix << bits | (uint32_t)(top - j);
+          sh.left = left - above;
+        }
+        above += c[j];
+      }
     }
     __syncthreads();
     prefix = sh.prefix;
@@ -370,8 +384,8 @@ evict_pick_kernel(const EvictArgs a, int n_cta) {
 #pragma unroll
   for (int k = 0; k < kKeys; ++k) {
     if (k >= used) break;
-    const unsigned who = __ballot_sync(kAll, k * kPickThreads + (int)threadIdx.x < n && key[k] == prefix);
-    if (lane == 0) sh.before[0][k * kPickWarps + warp] = __popc(who);
+    const unsigned who = __ballot_sync(kAll, k * kThreads + (int)threadIdx.x < n && key[k] == prefix);
+    if (lane == 0) sh.before[0][k * kWarps + warp] = __popc(who);
   }
   __syncthreads();
   ranks_of(sh, 0, used, n_cta, me);
@@ -379,17 +393,17 @@ evict_pick_kernel(const EvictArgs a, int n_cta) {
 #pragma unroll
   for (int k = 0; k < kKeys; ++k) {
     if (k >= used) break;
-    const int at = k * kPickThreads + threadIdx.x, i = r0 + at;
+    const int at = k * kThreads + threadIdx.x, i = r0 + at;
     const bool equal = at < n && key[k] == prefix;
     const unsigned who = __ballot_sync(kAll, equal);
-    const int rank = sh.before[0][k * kPickWarps + warp] + __popc(who & ((1u << lane) - 1));
+    const int rank = sh.before[0][k * kWarps + warp] + __popc(who & ((1u << lane) - 1));
     const bool keep = at < n && (key[k] > prefix || (equal && rank < (int)left));
     if (keep) kept |= 1u << k;
     const unsigned move = __ballot_sync(kAll, keep && i >= en.keep);
     const unsigned hole = __ballot_sync(kAll, at < n && !keep && i < en.keep);
     if (lane == 0) {
-      sh.before[1][k * kPickWarps + warp] = __popc(move);
-      sh.before[2][k * kPickWarps + warp] = __popc(hole);
+      sh.before[1][k * kWarps + warp] = __popc(move);
+      sh.before[2][k * kWarps + warp] = __popc(hole);
     }
   }
   __syncthreads();
@@ -398,13 +412,13 @@ evict_pick_kernel(const EvictArgs a, int n_cta) {
 #pragma unroll
   for (int k = 0; k < kKeys; ++k) {
     if (k >= used) break;
-    const int at = k * kPickThreads + threadIdx.x, i = r0 + at;
+    const int at = k * kThreads + threadIdx.x, i = r0 + at;
     const bool keep = kept >> k & 1, move = keep && i >= en.keep;
     const bool hole = at < n && !keep && i < en.keep;
     const unsigned wm = __ballot_sync(kAll, move), wh = __ballot_sync(kAll, hole);
     const unsigned lower = (1u << lane) - 1;
-    const int holes = sh.before[2][k * kPickWarps + warp] + __popc(wh & lower);
-    if (move) list[sh.before[1][k * kPickWarps + warp] + __popc(wm & lower)].x = i;
+    const int holes = sh.before[2][k * kWarps + warp] + __popc(wh & lower);
+    if (move) list[sh.before[1][k * kWarps + warp] + __popc(wm & lower)].x = i;
     if (hole) list[holes].y = i;
     // out of place the rows that stay are copied as well, behind those that move: the row's place
     // less the free places before it
@@ -417,6 +431,7 @@ evict_pick_kernel(const EvictArgs a, int n_cta) {
 
 // The same for stretches that the registers of a cluster do not hold: one CTA, eight bits at a time,
 // the weights read again for every round and for the ranks.
+constexpr int kPickThreads = 512;
 __global__ void __launch_bounds__(kPickThreads) evict_pick_long_kernel(const EvictArgs a) {
   __shared__ uint32_t hist[256];
   __shared__ uint32_t s_prefix, s_left;
@@ -607,23 +622,28 @@ cudaError_t launch_evict(const EvictArgs& a, int n, int num_layers, int max_len,
                          cudaStream_t st) {
   if (n <= 0) return cudaSuccess;
   const int lh = num_layers * a.num_kv_heads;
-  // CTAs per stretch: as many as it takes to hold the longest stretch in registers
-  int n_cta = 1;
-  while (n_cta < kPickCluster && max_len > n_cta * kPickRows) n_cta *= 2;
-  auto pick = max_len <= kPickThreads * 4 ? evict_pick_kernel<4> : evict_pick_kernel<kPickKeys>;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(n * n_cta, lh);
-  cfg.blockDim = dim3(kPickThreads);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = n_cta;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = n_cta > 1 ? 1 : 0;
-  cudaError_t e = max_len <= kPickCluster * kPickRows
-                      ? cudaLaunchKernelEx(&cfg, pick, a, n_cta)
-                      : launch_kernel(evict_pick_long_kernel, dim3(n, lh), dim3(kPickThreads), 0, st, false, a);
+  cudaError_t e;
+  if (max_len <= kPickFew * kPickFewKeys) {
+    e = launch_kernel(evict_pick_kernel<kPickFew, kPickFewKeys>, dim3(n, lh), dim3(kPickFew), 0, st, false, a, 1);
+  } else if (max_len <= kPickCluster * kPickRows) {
+    // CTAs per stretch: as many as it takes to hold the longest stretch in registers, or to give a
+    // thread no more than four rows
+    int n_cta = 1;
+    while (n_cta < kPickCluster && max_len > n_cta * kPickMany * 4) n_cta *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(n * n_cta, lh);
+    cfg.blockDim = dim3(kPickMany);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = n_cta;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = n_cta > 1 ? 1 : 0;
+    e = cudaLaunchKernelEx(&cfg, evict_pick_kernel<kPickMany, kPickManyKeys>, a, n_cta);
+  } else {
+    e = launch_kernel(evict_pick_long_kernel, dim3(n, lh), dim3(kPickThreads), 0, st, false, a);
+  }
   if (e != cudaSuccess || max_rows <= 0) return e;
   const unsigned grid = (unsigned)std::min((max_rows + 15) / 16, 1024);
   EvictArgs part = a;
