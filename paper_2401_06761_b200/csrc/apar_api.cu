@@ -730,19 +730,22 @@ apar_status send_key_plan(apar_ctx* c, const std::vector<KeyRun>& runs, const st
     for (int t = r.tok_begin; t < r.tok_end; t += chunk) {
       const bool last = t + chunk >= r.tok_end;
       units->push_back(KeyUnit{r.table_row, t, last && r.open ? -(r.tok_end - t) - 1 : std::min(r.tok_end, t + chunk),
-                               r.user_begin, r.n_users, {0, 0, 0}});
+                               r.user_begin, r.n_users, 0, {0, 0}});
     }
   if ((int64_t)units->size() > c->wlay.unit_cap || (int64_t)users.size() > c->wlay.user_cap)
     return APAR_ERR_WORKSPACE_TOO_SMALL;
   // (queries that see the unit's keys, or all but a few of them)
   std::vector<int64_t> cost(units->size());
   std::vector<int32_t> order(units->size());
+  const int per_tile = 128 / c->shape.group;
   for (size_t i = 0; i < units->size(); ++i) {
-    const KeyUnit& u = (*units)[i];
+    KeyUnit& u = (*units)[i];
     int64_t queries = 0;
     for (int x = 0; x < u.n_users; ++x) {
       const KeyUser& user = users[u.user_begin + x];
-      queries += user.count - (user.count > 1 ? std::max(0, std::min(user.count, u.tok_begin - user.lim)) : 0);
+      const int seeing = user.count - (by_class ? 0 : std::max(0, u.tok_begin - user.lim));
+      queries += seeing;
+      u.n_tiles += (seeing + per_tile - 1) / per_tile;
     }
     cost[i] = (u.tok_end < 0 ? -u.tok_end - 1 : u.tok_end - u.tok_begin) * (1 + queries);
     order[i] = (int32_t)i;

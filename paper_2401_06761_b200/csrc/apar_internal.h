@@ -261,7 +261,8 @@ cudaError_t launch_q4_verify_finish(const AttnArgs& a, const VerifyDesc* d_desc,
 struct KeyUnit {
   int32_t table_row, tok_begin, tok_end;   // tok_end < 0: the current length of table_row
   int32_t user_begin, n_users;
-  int32_t pad[3];
+  int32_t n_tiles;                         // (prompts) tiles of 128 / group queries that see some of it
+  int32_t pad[2];
 };
 struct KeyUser {
   int32_t query;                 // the (first) query

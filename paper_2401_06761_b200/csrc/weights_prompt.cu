@@ -5,9 +5,11 @@
 // owns a key (its TMEM lane), goes over the queries in the columns and adds up
 //     exp2(c s - log2 e * lse[column])
 // in a register: no shuffles, no atomics, nothing but one number per key leaves the SM.
-//   warps 0-15      four to a quarter: half of the unit's keys (two S buffers of 128 columns each), half
-//                   of the columns.  At a unit's end the first half of the columns writes its sums, and
-//                   the second adds its own to them.
+//   warps 0-15      eight to a half of the unit's keys, which has two S buffers of 128 columns: four take the
+//                   even query tiles and four the odd ones, all columns of a tile.  So the barriers and the
+//                   first scores' way from TMEM (1400 cycles a tile) pass while the other four have the
+//                   special-function unit (1000 cycles a tile and half).  At a unit's end those that
+//                   had its first tile write their sums and the others add theirs.
 //   warp 16         copies, by TMA, K tiles (double-buffered, 64 KiB a unit) and query tiles (128 / group
 //                   tokens times the group's heads; three in flight).
 //   warp 17         puts each query tile's log-sum-exps and a description into a ring of five.
@@ -52,18 +54,19 @@ struct TileDesc {
   int32_t pos;                   // position of the first
   int32_t tok_begin, end;        // the unit's keys
   int32_t table_row, kvh;
-  int32_t flags;                 // F_*
-  int32_t pad;
+  int32_t t, n_tiles;            // tile of the unit, and how many it has
 };
 static_assert(sizeof(TileDesc) == 32, "description");
 // What the issuers need of it: a word beside each stage of the ring of query tiles.
-enum { F_FIRST = 1, F_LAST = 2, F_BOTH = 4, F_END = 8 };
+enum { F_FIRST = 1, F_LAST = 2,  // tile of the unit
+       F_BOTH = 4,               // the unit reaches into both halves of the keys
+       F_END = 8 };
 
 enum { B_KFULL = 0, B_KEMPTY = 2, B_QFULL = 4, B_QEMPTY = B_QFULL + kQStages,
        B_LFULL = B_QEMPTY + kQStages, B_LEMPTY = B_LFULL + kLStages,   // log-sum-exps and description
        B_SFULL = B_LEMPTY + kLStages,            // [half][buffer]
        B_SEMPTY = B_SFULL + 4,
-       B_WFULL = B_SEMPTY + 4, B_WEMPTY = B_WFULL + 2,   // [half]: the first columns' sums are written
+       B_WFULL = B_SEMPTY + 4, B_WEMPTY = B_WFULL + 2,   // [half]: the first tile's warps have written
        B_TOTAL = B_WEMPTY + 2 };
 static_assert(8 * B_TOTAL + 16 <= 256 + 32, "barrier area");
 
@@ -178,11 +181,11 @@ prompt_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
     }
     for (int s = 0; s < kLStages; ++s) {
       bar_init(bar(B_LFULL + s), 1);
-      bar_init(bar(B_LEMPTY + s), kSumWarps);
+      bar_init(bar(B_LEMPTY + s), kSumWarps / 2);
     }
     for (int s = 0; s < 4; ++s) {
       bar_init(bar(B_SFULL + s), 1);
-      bar_init(bar(B_SEMPTY + s), kSumWarps / 2);
+      bar_init(bar(B_SEMPTY + s), kSumWarps / 4);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -274,6 +277,7 @@ prompt_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
     bool ok = true;
     for (UnitWalk u(a, total, lane); ok && u.more; u.step()) {
       KeyUser user = u.user;
+      int t = 0;
       for (int x = 0; ok; user = a.users[u.it.user_begin + x]) {
         ++x;
         int j = max(0, u.it.tok_begin - user.lim);
@@ -296,7 +300,8 @@ prompt_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
           for (int k = 0; k < 4; ++k) lses[ls * kKeys + lane + 32 * k] = l[k] * -1.4426950408889634f;
           if (lane == 0)
             descs[ls] = TileDesc{min(T, user.count - j), user.lim + j, u.it.tok_begin, u.it.tok_end,
-                                 u.it.table_row, u.h, x == u.it.n_users && j + T >= user.count ? F_LAST : 0, 0};
+                                 u.it.table_row, u.h, t, u.it.n_tiles};
+          ++t;
           __syncwarp();
           if (lane == 0) bar_arrive(bar(B_LFULL + ls));
           at += (int64_t)T * HQ;
@@ -305,21 +310,23 @@ prompt_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
         if (x == u.it.n_users) break;
       }
     }
-    const int ls = g % kLStages;
-    if (ok && g >= kLStages)
-      ok = __all_sync(kAll, bar_wait(bar(B_LEMPTY + ls), (g / kLStages - 1) & 1, cta_abort, a.d_error, 22200));
-    if (ok && lane == 0) {
-      descs[ls].n_tok = 0;
-      bar_arrive(bar(B_LFULL + ls));
+    for (int x = 0; x < 2 && ok; ++x, ++g) {     // (one for each of the two that take turns)
+      const int ls = g % kLStages;
+      if (g >= kLStages)
+        ok = __all_sync(kAll, bar_wait(bar(B_LEMPTY + ls), (g / kLStages - 1) & 1, cta_abort, a.d_error, 22200));
+      if (ok && lane == 0) {
+        descs[ls].n_tok = 0;
+        bar_arrive(bar(B_LFULL + ls));
+      }
     }
   } else if (warp > kSumWarps + 1) {
     // ---------------------------------------------------------------- products
     constexpr uint32_t kIdesc = instr_desc(128, false, 128);
     const int w = warp - kSumWarps - 2;
-    int ku = 0, cnt = 0;
+    int ku = 0, cnt[2] = {0, 0};                 // units; products of each buffer
     bool seen = false;                           // the tile was there at the last look
     for (int g = 0;; ++g) {
-      const int st = g % kQStages, sb = cnt & 1;
+      const int st = g % kQStages, sb = g & 1;
       if (!__all_sync(kAll, seen) &&
           !__all_sync(kAll, bar_wait(bar(B_QFULL + st), (g / kQStages) & 1, cta_abort, a.d_error, 23000)))
         break;
@@ -329,8 +336,9 @@ prompt_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
         bool ok = true;
         if (flags & F_FIRST)
           ok = bar_wait(bar(B_KFULL + (ku & 1)), (ku >> 1) & 1, cta_abort, a.d_error, 23100);
-        if (cnt >= 2)
-          ok = ok && bar_wait(bar(B_SEMPTY + 2 * w + sb), ((cnt >> 1) - 1) & 1, cta_abort, a.d_error, 23200);
+        const int n = sb ? cnt[1]++ : cnt[0]++;
+        if (n > 0)
+          ok = ok && bar_wait(bar(B_SEMPTY + 2 * w + sb), (n - 1) & 1, cta_abort, a.d_error, 23200);
         if (!__all_sync(kAll, ok)) break;
         tc_fence_after();
         if (lane == 0) {
@@ -345,7 +353,6 @@ prompt_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
           umma_commit(bar(B_QEMPTY + st));
           if (flags & F_LAST) umma_commit(bar(B_KEMPTY + (ku & 1)));
         }
-        ++cnt;
       } else if (lane == 0) {                    // (nothing of this half in the unit)
         bar_arrive(bar(B_QEMPTY + st));
         if (flags & F_LAST) bar_arrive(bar(B_KEMPTY + (ku & 1)));
@@ -356,14 +363,35 @@ prompt_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
     }
   } else {
     // ---------------------------------------------------------------- sums
-    const int w = warp >> 3, ch = warp >> 2 & 1;   // half of the keys, half of the columns
+    const int w = warp >> 3, turn = warp >> 2 & 1;   // half of the keys; even or odd tiles
     const int row = (warp & 3) * 32 + lane;        // the key's row of its half: its TMEM lane
-    const uint32_t ts = (tmem + 256u * w + 64u * ch) | (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t ts = (tmem + 256u * w + 128u * turn) | (uint32_t)((warp & 3) * 32) << 16;
     const float c = a.scale_log2e;
     const f32x2 c2 = pair(c, c);
     f32x2 acc[2] = {0ull, 0ull};
-    int cnt = 0, parts = 0;                        // S buffers taken, units written
-    for (int g = 0;; ++g) {
+    int cnt = 0, parts = 0;                        // times scores were taken, units of more than a tile
+    // Adds up 32 columns, of which lo .. hi - 1 see the key.
+    auto add = [&](const uint32_t (&s)[32], const float* lse, int lo, int hi) {
+      if (__all_sync(kAll, lo <= 0 && hi >= 32)) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const f32x2 l = *(const f32x2*)(lse + 2 * j);                // (times - log2 e)
+          const f32x2 x = fma2(pair(__uint_as_float(s[2 * j]), __uint_as_float(s[2 * j + 1])), c2, l);
+          float e0, e1;
+          unpair(x, e0, e1);
+          acc[j & 1] = add2(acc[j & 1], pair(ex2(e0), ex2(e1)));
+        }
+      } else if (!__all_sync(kAll, lo >= 32 || hi <= 0)) {
+        float part[2] = {0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          const float p = ex2(fmaf(__uint_as_float(s[j]), c, lse[j]));
+          if (j >= lo && j < hi) part[j & 1] += p;
+        }
+        acc[1] = add2(acc[1], pair(part[0], part[1]));
+      }
+    };
+    for (int g = turn;; g += 2) {
       const int ls = g % kLStages;
       if (!__all_sync(kAll, bar_wait(bar(B_LFULL + ls), (g / kLStages) & 1, cta_abort, a.d_error, 24000)))
         break;
@@ -372,53 +400,34 @@ prompt_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
       const int key = d.tok_begin + kKeys * w + row;
       const bool used = d.tok_begin + kKeys * w < d.end;       // (the unit reaches into this half)
       if (used) {
-        const int sb = cnt & 1;
-        if (!__all_sync(kAll, bar_wait(bar(B_SFULL + 2 * w + sb), (cnt >> 1) & 1, cta_abort, a.d_error,
-                                       24100)))
+        if (!__all_sync(kAll, bar_wait(bar(B_SFULL + 2 * w + turn), cnt & 1, cta_abort, a.d_error, 24100)))
           break;
         ++cnt;
         tc_fence_after();
-        uint32_t s[64];
-        TMEM_LD_32(ts + 128u * sb, s, 0);
+        uint32_t s0[32], s1[32];
+        TMEM_LD_32(ts, s0, 0);
+        // by the tokens from the key's own position on; a whole tile but for zero rows behind its last
+        // token, whose log-sum-exp is infinite
+        const int lo = max(0, key - d.pos) * G, hi = d.n_tok == T ? kKeys : d.n_tok * G;
+        const float* lse = lses + ls * kKeys;
         tmem_wait_ld();
-        // the key is seen by columns lo .. hi - 1, by the tokens from its own position on; a whole tile but
-        // for zero rows behind its last token, whose log-sum-exp is infinite
-        const int lo = max(0, key - d.pos) * G - 64 * ch, hi = d.n_tok * G - 64 * ch;
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          if (q == 0) {
-            TMEM_LD_32(ts + 128u * sb + 32u, s, 32);
-          } else {
-            tmem_wait_ld();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(bar(B_SEMPTY + 2 * w + sb));
-          }
-          const float* lse = lses + ls * kKeys + 64 * ch + 32 * q;     // (times - log2 e)
-          if (__all_sync(kAll, lo <= 32 * q && (hi >= 32 * q + 32 || d.n_tok == T))) {
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              const f32x2 l = *(const f32x2*)(lse + 2 * j);
-              const f32x2 x = fma2(pair(__uint_as_float(s[32 * q + 2 * j]), __uint_as_float(s[32 * q + 2 * j + 1])),
-                                   c2, l);
-              float e0, e1;
-              unpair(x, e0, e1);
-              acc[j & 1] = add2(acc[j & 1], pair(ex2(e0), ex2(e1)));
-            }
-          } else if (!__all_sync(kAll, lo >= 32 * q + 32 || hi <= 32 * q)) {
-            float part[2] = {0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              const float p = ex2(fmaf(__uint_as_float(s[32 * q + j]), c, lse[j]));
-              if (32 * q + j >= lo && 32 * q + j < hi) part[j & 1] += p;
-            }
-            acc[1] = add2(acc[1], pair(part[0], part[1]));
-          }
-        }
+        TMEM_LD_32(ts + 32u, s1, 0);
+        add(s0, lse, lo, hi);
+        tmem_wait_ld();
+        TMEM_LD_32(ts + 64u, s0, 0);
+        add(s1, lse + 32, lo - 32, hi - 32);
+        tmem_wait_ld();
+        TMEM_LD_32(ts + 96u, s1, 0);
+        add(s0, lse + 64, lo - 64, hi - 64);
+        tmem_wait_ld();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(bar(B_SEMPTY + 2 * w + turn));
+        add(s1, lse + 96, lo - 96, hi - 96);
       }
       __syncwarp();
       if (lane == 0) bar_arrive(bar(B_LEMPTY + ls));
-      if ((d.flags & F_LAST) && used) {
+      if (used && d.t + 2 >= d.n_tiles) {          // the last one of the unit for these warps
         float sum, more;
         unpair(add2(acc[0], acc[1]), sum, more);
         sum += more;
@@ -427,19 +436,21 @@ prompt_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
           const int block = a.d_tables[(size_t)d.table_row * a.shape.table_stride + (key >> 4)];
           out = a.weights + ((size_t)block * HKV + d.kvh) * kBlock + (key & 15);
         }
-        if (ch == 0) {
+        if (!(d.t & 1)) {
           if (out) *out = a.replace ? sum : *out + sum;
-          if (parts > 0 && !__all_sync(kAll, bar_wait(bar(B_WEMPTY + w), (parts - 1) & 1, cta_abort,
-                                                      a.d_error, 24200)))
-            break;
-          __syncwarp();
-          if (lane == 0) bar_arrive(bar(B_WFULL + w));
+          if (d.n_tiles > 1) {
+            if (parts > 0 && !__all_sync(kAll, bar_wait(bar(B_WEMPTY + w), (parts - 1) & 1, cta_abort,
+                                                        a.d_error, 24200)))
+              break;
+            __syncwarp();
+            if (lane == 0) bar_arrive(bar(B_WFULL + w));
+          }
         } else {
           if (!__all_sync(kAll, bar_wait(bar(B_WFULL + w), parts & 1, cta_abort, a.d_error, 24300))) break;
           if (lane == 0) bar_arrive(bar(B_WEMPTY + w));
           if (out) *out += sum;
         }
-        ++parts;
+        parts += d.n_tiles > 1;
         acc[0] = acc[1] = 0ull;
       }
     }
