@@ -6,9 +6,9 @@
 // of exponentials, and a second small kernel puts the pieces of a sequence's rows together.
 //
 // beam_scan_kernel   one CTA per piece, which reads up to 12288 (f32) or 16384 (16-bit) elements into
-//     registers, all loads on their way at once.  A thread's words are 1 KiB apart, so that loads are
-//     whole lines wherever a row begins, and the order of the sums depends on the token alone: equal rows
-//     tie exactly.  A threshold that at least num_select elements reach comes
+//     registers, all loads on their way at once, sixteen bytes each where a row begins on such a
+//     boundary.  Which thread holds which element, and so the order of the sums, depends on the
+//     element alone: equal rows tie exactly.  A threshold that at least num_select elements reach comes
 //     from the threads' maxima: with j = num_select / 8 rounded up, the least of the eight warps' j-th
 //     largest.  The few elements that reach it (some two to three times num_select) are collected in shared
 //     memory and put in order by counting, for each, how many are larger.  A key is (ordered bits of
@@ -51,52 +51,85 @@ __device__ __forceinline__ float unordered(uint32_t o) {   // (what is below -in
   return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
 }
 
-// A row's elements as words: one f32, or two 16-bit ones.
+// A row's elements in packs of sixteen bytes.
 __device__ __forceinline__ float number(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float number(__half x) { return __half2float(x); }
 __device__ __forceinline__ float number(float x) { return x; }
 template <typename T>
-struct Words;
+struct Packs;
 template <>
-struct Words<float> {
-  static constexpr int kPer = 1, kHeld = 48;           // elements of a word, words a thread holds
+struct Packs<float> {
+  static constexpr int kPer = 4, kHeld = 12;           // elements of a pack, packs a thread holds
   static constexpr uint32_t kNone = 0xff800000u;       // -inf
-  static __device__ __forceinline__ void numbers(uint32_t w, float (&x)[1]) { x[0] = __uint_as_float(w); }
+  static __device__ __forceinline__ void numbers(uint4 w, float (&x)[4]) {
+    x[0] = __uint_as_float(w.x);
+    x[1] = __uint_as_float(w.y);
+    x[2] = __uint_as_float(w.z);
+    x[3] = __uint_as_float(w.w);
+  }
 };
 template <>
-struct Words<__nv_bfloat16> {
-  static constexpr int kPer = 2, kHeld = 32;
+struct Packs<__nv_bfloat16> {
+  static constexpr int kPer = 8, kHeld = 8;
   static constexpr uint32_t kNone = 0xff80ff80u;
-  static __device__ __forceinline__ void numbers(uint32_t w, float (&x)[2]) {
-    x[0] = __uint_as_float(w << 16);
-    x[1] = __uint_as_float(w & 0xffff0000u);
+  static __device__ __forceinline__ void numbers(uint4 w, float (&x)[8]) {
+    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(v[i] << 16);
+      x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+    }
   }
 };
 template <>
-struct Words<__half> {
-  static constexpr int kPer = 2, kHeld = 32;
+struct Packs<__half> {
+  static constexpr int kPer = 8, kHeld = 8;
   static constexpr uint32_t kNone = 0xfc00fc00u;
-  static __device__ __forceinline__ void numbers(uint32_t w, float (&x)[2]) {
-    const float2 f = __half22float2(*(const __half2*)&w);
-    x[0] = f.x;
-    x[1] = f.y;
+  static __device__ __forceinline__ void numbers(uint4 w, float (&x)[8]) {
+    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = __half22float2(*(const __half2*)&v[i]);
+      x[2 * i] = f.x;
+      x[2 * i + 1] = f.y;
+    }
   }
 };
-// Word `at` of a row of n elements; what lies past its end is -inf.  `odd`: the row's words are not aligned.
-__device__ __forceinline__ uint32_t load_word(const float* row, int n, bool, int at) {
-  return at < n ? __float_as_uint(__ldg(row + at)) : Words<float>::kNone;
-}
-template <typename T>
-__device__ __forceinline__ uint32_t load_word(const T* row, int n, bool odd, int at) {
-  uint32_t w = Words<T>::kNone;
-  if (2 * at + 1 < n) {
-    if (!odd) return __ldg((const uint32_t*)row + at);
-    const uint16_t* p = (const uint16_t*)row + 2 * at;
-    w = (uint32_t)__ldg(p) | (uint32_t)__ldg(p + 1) << 16;
-  } else if (2 * at < n) {
-    w = (w & 0xffff0000u) | __ldg((const uint16_t*)row + 2 * at);
+// A whole pack from an address on a boundary of kAlign bytes.
+template <int kAlign>
+__device__ __forceinline__ uint4 load_pack(const void* p) {
+  if constexpr (kAlign == 16) {
+    return __ldg((const uint4*)p);
+  } else {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = kAlign == 4 ? __ldg((const uint32_t*)p + i)
+                         : (uint32_t)__ldg((const uint16_t*)p + 2 * i) |
+                               (uint32_t)__ldg((const uint16_t*)p + 2 * i + 1) << 16;
+    return make_uint4(w[0], w[1], w[2], w[3]);
   }
-  return w;
+}
+// This thread's packs at0, at0 + kThreads, ... of the n elements of a row; what lies past them is -inf.
+template <typename T, int kAlign>
+__device__ __forceinline__ void load_packs(uint4 (&v)[Packs<T>::kHeld], const T* row, int n, int at0) {
+  constexpr int kPer = Packs<T>::kPer;
+#pragma unroll
+  for (int k = 0; k < Packs<T>::kHeld; ++k) {
+    const int at = at0 + k * kThreads;
+    v[k] = make_uint4(Packs<T>::kNone, Packs<T>::kNone, Packs<T>::kNone, Packs<T>::kNone);
+    if ((at + 1) * kPer <= n) v[k] = load_pack<kAlign>(row + (int64_t)at * kPer);
+  }
+  const int last = n / kPer, k_last = (last - at0) / kThreads;     // the pack that the row's end cuts
+  if (n % kPer && last >= at0 && (last - at0) % kThreads == 0) {
+    alignas(16) T x[kPer];
+    const uint32_t none = Packs<T>::kNone;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) x[i] = last * kPer + i < n ? row[last * kPer + i] : *(const T*)&none;
+#pragma unroll
+    for (int k = 0; k < Packs<T>::kHeld; ++k)
+      if (k == k_last) v[k] = *(const uint4*)x;
+  }
 }
 
 struct BeamArgs {
@@ -220,8 +253,8 @@ union ScanKeys {
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 3) beam_scan_kernel(const BeamArgs a) {
-  using W = Words<T>;
-  constexpr int kPer = W::kPer, kHeld = W::kHeld, kChunk = kThreads * kHeld;   // words of a CTA
+  using W = Packs<T>;
+  constexpr int kPer = W::kPer, kHeld = W::kHeld, kChunk = kThreads * kHeld;   // packs of a CTA
   __shared__ ScanKeys sh;
   __shared__ u64 held[kMaxSelect];             // the largest so far, in order
   __shared__ uint32_t tops[2 * kWarps];
@@ -232,17 +265,17 @@ __global__ void __launch_bounds__(kThreads, 3) beam_scan_kernel(const BeamArgs a
   const int row = blockIdx.x / a.pieces, piece = blockIdx.x % a.pieces;
   const int seq = row / a.beams, beam = row % a.beams;
   const T* x = (const T*)a.logits + seq * a.seq_stride + beam * a.beam_stride;
-  const bool odd = (uintptr_t)x & 3;
-  const int words = (a.vocab + kPer - 1) / kPer, per_piece = (words + a.pieces - 1) / a.pieces;
-  const int end = min(words, (piece + 1) * per_piece);
+  const int packs = (a.vocab + kPer - 1) / kPer, per_piece = (packs + a.pieces - 1) / a.pieces;
+  const int end = min(packs, (piece + 1) * per_piece);
   const bool skip = a.finished && a.finished[row];     // (has its one continuation, see the other kernel)
   int n_held = 0;
   float m = -INFINITY, l = 0.f;
   for (int c0 = skip ? end : piece * per_piece; c0 < end; c0 += kChunk) {
     const int n_in = min(a.vocab, end * kPer);         // elements before this one are the piece's
-    uint32_t v[kHeld];
-#pragma unroll
-    for (int k = 0; k < kHeld; ++k) v[k] = load_word(x, n_in, odd, c0 + k * kThreads + threadIdx.x);
+    uint4 v[kHeld];
+    if (((uintptr_t)x & 15) == 0) load_packs<T, 16>(v, x, n_in, c0 + threadIdx.x);
+    else if (sizeof(T) == 4 || ((uintptr_t)x & 3) == 0) load_packs<T, 4>(v, x, n_in, c0 + threadIdx.x);
+    else load_packs<T, 2>(v, x, n_in, c0 + threadIdx.x);
     float mine = -INFINITY;
 #pragma unroll
     for (int k = 0; k < kHeld; ++k) {
@@ -267,12 +300,12 @@ __global__ void __launch_bounds__(kThreads, 3) beam_scan_kernel(const BeamArgs a
       float e[kPer];
       W::numbers(v[k], e);
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) part[(k + i) & 1] += ex2(fmaf(e[i], kLog2e, -ref));
+      for (int i = 0; i < kPer; ++i) part[i & 1] += ex2(fmaf(e[i], kLog2e, -ref));
     }
-    // The few elements that reach the threshold: bits first, then a loop that reads them again (a copy
-    // of what to do with one for each word a thread holds would be 600 instructions to fetch).
+    // The few elements that reach the threshold: their packs' bits first, then a loop that reads them again
+    // (what to do with one, once for each that a thread holds, would be 600 instructions to fetch).
     if (mine >= tau && mine > -INFINITY) {
-      u64 hits = 0;
+      uint32_t hits = 0;
 #pragma unroll
       for (int k = 0; k < kHeld; ++k) {
         float e[kPer];
@@ -280,10 +313,10 @@ __global__ void __launch_bounds__(kThreads, 3) beam_scan_kernel(const BeamArgs a
         bool any = false;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) any = any || e[i] >= tau;
-        if (any) hits |= 1ull << k;
+        if (any) hits |= 1u << k;
       }
       for (; hits; hits &= hits - 1) {
-        const uint32_t token = (c0 + (__ffsll(hits) - 1) * kThreads + threadIdx.x) * kPer;
+        const uint32_t token = (c0 + (__ffs(hits) - 1) * kThreads + threadIdx.x) * kPer;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
           const float e = (int)token + i < n_in ? number(x[token + i]) : -INFINITY;
@@ -484,7 +517,8 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
 // machine twice over, none shorter than 2048 elements.
 int pieces_of(const apar_beam_config* c, int32_t n_seq) {
   const int64_t rows = (int64_t)n_seq * c->num_beams;
-  const int64_t held = kThreads * (c->logits_type == APAR_LOGITS_F32 ? Words<float>::kHeld : 2 * Words<__half>::kHeld);
+  const int64_t held = kThreads * (c->logits_type == APAR_LOGITS_F32 ? Packs<float>::kHeld * Packs<float>::kPer
+                                                                     : Packs<__half>::kHeld * Packs<__half>::kPer);
   const int64_t fit = (c->vocab + held - 1) / held;
   int64_t p = std::min<int64_t>((2 * 148 + rows - 1) / rows, (c->vocab + 2047) / 2048);
   p = std::min<int64_t>({std::max(p, fit), kMaxPieces, kMaxLists / c->num_beams});
