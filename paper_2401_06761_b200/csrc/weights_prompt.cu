@@ -44,7 +44,7 @@ constexpr int kLStages = 5;
 constexpr int kOffDesc = kOffLse + kLStages * kKeys * 4;
 constexpr int kOffFlags = kOffDesc + kLStages * 32;
 constexpr int kOffBar = kOffFlags + 16;
-constexpr int kSmem = kOffBar + 288;
+constexpr int kSmem = kOffBar + 320;
 constexpr int kSumWarps = 16;
 constexpr int kWarps = kSumWarps + 4;
 static_assert(kSmem <= 227 * 1024, "shared memory");
@@ -66,9 +66,9 @@ enum { B_KFULL = 0, B_KEMPTY = 2, B_QFULL = 4, B_QEMPTY = B_QFULL + kQStages,
        B_LFULL = B_QEMPTY + kQStages, B_LEMPTY = B_LFULL + kLStages,   // log-sum-exps and description
        B_SFULL = B_LEMPTY + kLStages,            // [half][buffer]
        B_SEMPTY = B_SFULL + 4,
-       B_WFULL = B_SEMPTY + 4, B_WEMPTY = B_WFULL + 2,   // [half]: the first tile's warps have written
-       B_TOTAL = B_WEMPTY + 2 };
-static_assert(8 * B_TOTAL + 16 <= 256 + 32, "barrier area");
+       B_WFULL = B_SEMPTY + 4, B_WEMPTY = B_WFULL + 4,   // [half][turn of the first tile's warps]: they have
+       B_TOTAL = B_WEMPTY + 4 };                         // written; the others have seen that
+static_assert(8 * B_TOTAL + 16 <= 320, "barrier area");
 
 // ---- two numbers at a time
 typedef unsigned long long f32x2;
@@ -89,6 +89,19 @@ __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
   f32x2 r;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
+}
+
+// Waits for the loads from TMEM into r.  Naming the registers keeps what is done with them behind the wait:
+// to the compiler they have their values from the load on.
+__device__ __forceinline__ void wait_scores(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]),
+                 "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]),
+                 "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]),
+                 "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
+                 "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]),
+                 "+r"(r[31])
+               :: "memory");
 }
 
 // Units in the order they are dealt out: CTA b's i-th.
@@ -172,6 +185,8 @@ prompt_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
     for (int b = 0; b < 2; ++b) {
       bar_init(bar(B_KFULL + b), 1);
       bar_init(bar(B_KEMPTY + b), 2);            // both issuers
+    }
+    for (int b = 0; b < 4; ++b) {
       bar_init(bar(B_WFULL + b), 4);
       bar_init(bar(B_WEMPTY + b), 4);
     }
@@ -369,7 +384,10 @@ prompt_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
     const float c = a.scale_log2e;
     const f32x2 c2 = pair(c, c);
     f32x2 acc[2] = {0ull, 0ull};
-    int cnt = 0, parts = 0;                        // times scores were taken, units of more than a tile
+    int cnt = 0;                                   // times scores were taken
+    // units of more than a tile whose first these warps had, or had not.  (Each has barriers of its own: a
+    // warp may not wait for a phase before the one before it, which it has not seen, is complete.)
+    int firsts = 0, seconds = 0;
     // Adds up 32 columns, of which lo .. hi - 1 see the key.
     auto add = [&](const uint32_t (&s)[32], const float* lse, int lo, int hi) {
       if (__all_sync(kAll, lo <= 0 && hi >= 32)) {
@@ -410,16 +428,16 @@ prompt_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
         // token, whose log-sum-exp is infinite
         const int lo = max(0, key - d.pos) * G, hi = d.n_tok == T ? kKeys : d.n_tok * G;
         const float* lse = lses + ls * kKeys;
-        tmem_wait_ld();
+        wait_scores(s0);
         TMEM_LD_32(ts + 32u, s1, 0);
         add(s0, lse, lo, hi);
-        tmem_wait_ld();
+        wait_scores(s1);
         TMEM_LD_32(ts + 64u, s0, 0);
         add(s1, lse + 32, lo - 32, hi - 32);
-        tmem_wait_ld();
+        wait_scores(s0);
         TMEM_LD_32(ts + 96u, s1, 0);
         add(s0, lse + 64, lo - 64, hi - 64);
-        tmem_wait_ld();
+        wait_scores(s1);
         tc_fence_before();
         __syncwarp();
         if (lane == 0) bar_arrive(bar(B_SEMPTY + 2 * w + turn));
@@ -437,20 +455,23 @@ prompt_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
           out = a.weights + ((size_t)block * HKV + d.kvh) * kBlock + (key & 15);
         }
         if (!(d.t & 1)) {
+          const int full = B_WFULL + 2 * w + turn, empty = B_WEMPTY + 2 * w + turn;
           if (out) *out = a.replace ? sum : *out + sum;
           if (d.n_tiles > 1) {
-            if (parts > 0 && !__all_sync(kAll, bar_wait(bar(B_WEMPTY + w), (parts - 1) & 1, cta_abort,
-                                                        a.d_error, 24200)))
+            if (firsts > 0 &&
+                !__all_sync(kAll, bar_wait(bar(empty), (firsts - 1) & 1, cta_abort, a.d_error, 24200)))
               break;
             __syncwarp();
-            if (lane == 0) bar_arrive(bar(B_WFULL + w));
+            if (lane == 0) bar_arrive(bar(full));
+            ++firsts;
           }
         } else {
-          if (!__all_sync(kAll, bar_wait(bar(B_WFULL + w), parts & 1, cta_abort, a.d_error, 24300))) break;
-          if (lane == 0) bar_arrive(bar(B_WEMPTY + w));
+          const int full = B_WFULL + 2 * w + (turn ^ 1), empty = B_WEMPTY + 2 * w + (turn ^ 1);
+          if (!__all_sync(kAll, bar_wait(bar(full), seconds & 1, cta_abort, a.d_error, 24300))) break;
+          if (lane == 0) bar_arrive(bar(empty));
           if (out) *out += sum;
+          ++seconds;
         }
-        parts += d.n_tiles > 1;
         acc[0] = acc[1] = 0ull;
       }
     }

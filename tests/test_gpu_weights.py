@@ -442,6 +442,27 @@ def test_weights_of_prompts_in_many_units():
     assert B.apar_get_stats(s.ctx)["device_wait_timeouts"] == 0
 
 
+@pytest.mark.parametrize("hq,hk", [(32, 32), (32, 8)])
+def test_weights_of_prompts_have_the_same_bits_in_many_runs(hq, hk):
+    """Units with even and odd numbers of query tiles after each other, many of them per CTA."""
+    s = PagedSession(LayerShape(hq, hk), 1100, 16, 200, weights=True)
+    n = [2040, 1910, 1777, 1650, 2001, 1523, 1999, 1801]
+    tids = s.new_threads(8)
+    s.append(tids, n, rows(sum(n), hk, 1), rows(sum(n), hk, 2))
+    q = rows(sum(n), hq, 3)
+    lse = torch.empty(sum(n), hq, device="cuda")
+    zero = [0] * 8
+    s.prefill_attention(tids, zero, n, q, lse=lse)
+    s.add_weights_prefill(tids, zero, n, q, lse, replace=True)
+    first = s.read_weights(tids, zero, n)
+    wrong = torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(300):
+        s.add_weights_prefill(tids, zero, n, q, lse, replace=True)
+        wrong += (s.read_weights(tids, zero, n) != first).sum()
+    assert wrong.item() == 0
+    assert B.apar_get_stats(s.ctx)["device_wait_timeouts"] == 0
+
+
 def place(w, keep):
     """Rows that stay, by place, of weights w [n]: NaN first, then by weight, ties to the earlier."""
     key = [(not math.isnan(x), 0 if math.isnan(x) else -x, i) for i, x in enumerate(w)]
