@@ -73,8 +73,8 @@ Layout make_layout(const apar_config* c) {
 }
 
 struct WeightsLayout {     // partition of the memory of apar_attach_weights
-  size_t moves, counts, units, users, total;
-  int64_t unit_cap, user_cap;
+  size_t moves, counts, plan, total;
+  size_t plan_bytes;       // units, then users
 };
 
 WeightsLayout make_weights_layout(const apar_config* c) {
@@ -84,10 +84,10 @@ WeightsLayout make_weights_layout(const apar_config* c) {
   auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes, 256); return o; };
   L.moves = take(rows * sizeof(int2));                  // (no more rows stay than there are)
   L.counts = take((size_t)c->max_threads * std::max(1, c->num_layers) * c->num_kv_heads * 4);
-  L.unit_cap = c->num_blocks;                           // (no block is in two units)
-  L.user_cap = (int64_t)c->max_threads * 16 + 4096;
-  L.units = take((size_t)L.unit_cap * sizeof(KeyUnit));
-  L.users = take((size_t)L.user_cap * sizeof(KeyUser));
+  // (no block is in two units; a thread is a user of as many runs as its chain has forks)
+  L.plan_bytes = (size_t)c->num_blocks * sizeof(KeyUnit) +
+                 ((size_t)c->max_threads * 16 + 4096) * sizeof(KeyUser);
+  L.plan = take(L.plan_bytes);
   L.total = off;
   return L;
 }
@@ -177,6 +177,7 @@ struct apar_ctx {
   std::vector<Seen> seen;
   bool seen_valid = false, key_plan_valid = false;   // (they describe / the units on the device are of)
   int32_t n_key_units[3] = {0, 0, 0};                // that call; by class
+  size_t key_users_at = 0;                           // where the users begin in the plan's area
   // thread list of the most recent apar_decode_step; its table rows are resident on the device
   std::vector<int32_t> step_tids, step_slots, tmp_slots;
   bool step_valid = false;
@@ -732,8 +733,8 @@ apar_status send_key_plan(apar_ctx* c, const std::vector<KeyRun>& runs, const st
       units->push_back(KeyUnit{r.table_row, t, last && r.open ? -(r.tok_end - t) - 1 : std::min(r.tok_end, t + chunk),
                                r.user_begin, r.n_users, 0, {0, 0}});
     }
-  if ((int64_t)units->size() > c->wlay.unit_cap || (int64_t)users.size() > c->wlay.user_cap)
-    return APAR_ERR_WORKSPACE_TOO_SMALL;
+  const size_t b_units = units->size() * sizeof(KeyUnit), b_users = users.size() * sizeof(KeyUser);
+  if (b_units + b_users > c->wlay.plan_bytes) return APAR_ERR_WORKSPACE_TOO_SMALL;
   // (queries that see the unit's keys, or all but a few of them)
   std::vector<int64_t> cost(units->size());
   std::vector<int32_t> order(units->size());
@@ -757,10 +758,11 @@ apar_status send_key_plan(apar_ctx* c, const std::vector<KeyRun>& runs, const st
   std::vector<KeyUnit> sorted(units->size());
   for (size_t i = 0; i < order.size(); ++i) sorted[i] = (*units)[order[i]];
   units->swap(sorted);
-  apar_status rc = upload(c, units->data(), units->size() * sizeof(KeyUnit), c->weights + c->wlay.units, st);
-  if (rc == APAR_OK)
-    rc = upload(c, users.data(), users.size() * sizeof(KeyUser), c->weights + c->wlay.users, st);
-  return rc;
+  std::vector<char> plan(b_units + b_users);
+  memcpy(plan.data(), units->data(), b_units);
+  memcpy(plan.data() + b_units, users.data(), b_users);
+  c->key_users_at = b_units;
+  return upload(c, plan.data(), plan.size(), c->weights + c->wlay.plan, st);
 }
 
 KeyArgs key_args(apar_ctx* c, int layer, const void* q, const float* lse, float sm_scale, int replace) {
@@ -771,8 +773,8 @@ KeyArgs key_args(apar_ctx* c, int layer, const void* q, const float* lse, float 
   a.weights = (float*)c->weights + (size_t)layer * c->layer_weights();
   a.d_tables = (const int32_t*)c->ws(c->lay.tables);
   a.d_lens = (const int32_t*)c->ws(c->lay.lens);
-  a.units = (const KeyUnit*)(c->weights + c->wlay.units);
-  a.users = (const KeyUser*)(c->weights + c->wlay.users);
+  a.units = (const KeyUnit*)(c->weights + c->wlay.plan);
+  a.users = (const KeyUser*)(c->weights + c->wlay.plan + c->key_users_at);
   a.shape = c->shape;
   a.scale_log2e = sm_scale * 1.4426950408889634f;
   a.replace = replace != 0;
@@ -1949,17 +1951,25 @@ apar_status apar_read_weights(apar_ctx* c, int32_t layer, int32_t n, const int32
   if (rc) return rc;
   rc = sync_device_tables(c, slots.data(), n, st);
   if (rc) return rc;
-  const size_t per_pass = c->lay.stage_cap / sizeof(RowRange);
+  const float* w = (const float*)c->weights + (size_t)layer * c->layer_weights();
+  const int32_t* tables = (const int32_t*)c->ws(c->lay.tables);
+  // (a few ranges travel with the launch, more of them through the staging area)
+  const size_t per_pass = ranges.size() <= RowRanges::kMax ? RowRanges::kMax : c->lay.stage_cap / sizeof(RowRange);
   for (size_t i = 0; i < ranges.size(); i += per_pass) {
     const int m = (int)std::min(per_pass, ranges.size() - i);
     int max_count = 0;
     for (int j = 0; j < m; ++j) max_count = std::max(max_count, ranges[i + j].count);
-    char* d_stage = c->ws(c->lay.stage);
-    rc = upload(c, ranges.data() + i, (size_t)m * sizeof(RowRange), d_stage, st);
-    if (rc) return rc;
-    APAR_CUDA(c, launch_weights_read((const float*)c->weights + (size_t)layer * c->layer_weights(),
-                                     (const int32_t*)c->ws(c->lay.tables), c->cfg.max_blocks_per_thread,
-                                     (const RowRange*)d_stage, m, max_count, c->cfg.num_kv_heads, out, st));
+    RowRanges few;
+    const RowRange* many = nullptr;
+    if (per_pass == RowRanges::kMax) {
+      memcpy(few.r, ranges.data(), (size_t)m * sizeof(RowRange));
+    } else {
+      many = (const RowRange*)c->ws(c->lay.stage);
+      rc = upload(c, ranges.data() + i, (size_t)m * sizeof(RowRange), c->ws(c->lay.stage), st);
+      if (rc) return rc;
+    }
+    APAR_CUDA(c, launch_weights_read(w, tables, c->cfg.max_blocks_per_thread, few, many, m, max_count,
+                                     c->cfg.num_kv_heads, out, st));
     ++c->kernels_total;
   }
   return APAR_OK;

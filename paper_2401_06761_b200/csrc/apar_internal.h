@@ -289,6 +289,10 @@ struct RowRange {
   int32_t table_row, begin, count, pad;
   int64_t first;                 // row of the output
 };
+struct RowRanges {               // (as a kernel's argument)
+  static constexpr int kMax = 32;
+  RowRange r[kMax];
+};
 // One stretch of rows out of which `keep` stay.  The moves of (layer, kv head) i are entries
 // list_begin + i * list_rows onward of the list: {from, to}, rows of the stretch.
 struct EvictEntry {
@@ -322,9 +326,10 @@ cudaError_t launch_key_weights(KeyArgs a, const int32_t (&n_units)[3], cudaStrea
 constexpr int kPromptUnit = 256;
 cudaError_t launch_prompt_weights(const KeyArgs& a, const CUtensorMap* tm_k, const CUtensorMap* tm_q,
                                   int n_units, cudaStream_t st);
+// n ranges at `many` (device), or where that is NULL the first n of `few`.
 cudaError_t launch_weights_read(const float* w, const int32_t* d_tables, int table_stride,
-                                const RowRange* d_ranges, int n, int max_count, int num_kv_heads,
-                                float* out, cudaStream_t st);
+                                const RowRanges& few, const RowRange* many, int n, int max_count,
+                                int num_kv_heads, float* out, cudaStream_t st);
 // max_len: rows of the longest stretch; max_rows: rows the entry that moves most may move.
 cudaError_t launch_evict(const EvictArgs& a, int n, int num_layers, int max_len, int max_rows,
                          cudaStream_t st);

@@ -197,9 +197,10 @@ __global__ void __launch_bounds__(kKeyWarps * 32, kCtas) key_weights_kernel(cons
 // One warp per block: its weights are one contiguous piece of the pool, and so are its rows of the output.
 __global__ void __launch_bounds__(256) weights_read_kernel(const float* __restrict__ w,
                                                            const int32_t* __restrict__ tables, int stride,
-                                                           const RowRange* __restrict__ ranges,
+                                                           const __grid_constant__ RowRanges few,
+                                                           const RowRange* __restrict__ many,
                                                            int num_kv_heads, float* __restrict__ out) {
-  const RowRange r = ranges[blockIdx.y];
+  const RowRange r = many ? many[blockIdx.y] : few.r[blockIdx.y];
   const int lane = threadIdx.x & 31, last = (r.begin + r.count - 1) / kBlock;
   for (int b = r.begin / kBlock + blockIdx.x * 8 + (threadIdx.x >> 5); b <= last; b += gridDim.x * 8) {
     const float* src = w + (size_t)tables[(size_t)r.table_row * stride + b] * num_kv_heads * kBlock;
@@ -605,14 +606,14 @@ cudaError_t launch_key_weights(KeyArgs a, const int32_t (&n_units)[3], cudaStrea
 }
 
 cudaError_t launch_weights_read(const float* w, const int32_t* d_tables, int table_stride,
-                                const RowRange* d_ranges, int n, int max_count, int num_kv_heads,
-                                float* out, cudaStream_t st) {
+                                const RowRanges& few, const RowRange* many, int n, int max_count,
+                                int num_kv_heads, float* out, cudaStream_t st) {
   if (n <= 0 || max_count <= 0) return cudaSuccess;
   const unsigned grid = (unsigned)std::min(max_count / (kBlock * 8) + 1, 1024);
   for (int i = 0; i < n; i += 65535) {                 // (the grid's limit)
     const cudaError_t e = launch_kernel(weights_read_kernel, dim3(grid, std::min(n - i, 65535)), dim3(256),
-                                        0, st, false, w, d_tables, table_stride, d_ranges + i,
-                                        num_kv_heads, out);
+                                        0, st, false, w, d_tables, table_stride, few,
+                                        many ? many + i : nullptr, num_kv_heads, out);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;

@@ -312,9 +312,9 @@ class PagedSession:
 
     def read_weights(self, tids, begin, count, layer: int = 0):
         """Weights [rows][kv heads] of rows begin[i] .. begin[i] + count[i] - 1 of each chain."""
-        count = B.int32_array(count)
-        rows = max(0, int(np.frombuffer(count[0], np.int32, count[1]).sum(dtype=np.int64)))
-        out = torch.empty((rows, self.shape.num_kv_heads), dtype=torch.float32, device=self.device)
+        # (negative counts are the library's to refuse)
+        out = torch.empty((max(0, int(sum(count))), self.shape.num_kv_heads), dtype=torch.float32,
+                          device=self.device)
         B.apar_read_weights(self.ctx, layer, tids, begin, count, out.data_ptr(), self._stream())
         return out
 
