@@ -465,6 +465,8 @@ apar_status apar_rope(const apar_rope_config* cfg /*[host]*/, int32_t n,
                       int64_t k_stride, void* k_out /*[device]*/, int64_t k_out_stride,
                       void* cuda_stream);
 
+/* (The calls from here to apar_evict return INVALID_ARG, too, where the host's memory runs out.) */
+
 /* Threads go on from other threads' chains (the paper has no counterpart: beam search reorders its
  * beams after every selection).  After the call thread tid[i] holds the chain that source_tid[i]
  * held before it, for all i at once; ids stay as they are.  Sources need not be listed themselves;
@@ -504,8 +506,9 @@ apar_status apar_set_lse_output(apar_ctx* ctx, float* lse /*[device] or NULL*/);
  * the old weight (of the keys seen; others keep theirs).  Sums are in 32 bits in a fixed order.
  *   q [device] bf16 [n][num_q_heads][128], 16-byte aligned, lse [device] float [n][num_q_heads]: of that
  *   call and layer, its queries in its order.
- * The first call after an attention call that made a plan of its own uploads one too; others launch
- * one kernel and can be captured.
+ * The first call after an attention call that made a plan of its own uploads one too; others only
+ * launch kernels and can be captured.  A captured call follows the plan that the most recent
+ * uncaptured one left on the device.
  * Errors: INVALID_ARG (also: no memory attached, bookkeeping since that attention call, a
  * verification, an upload while the stream is capturing), UNSUPPORTED, WORKSPACE_TOO_SMALL, CUDA. */
 apar_status apar_add_weights(apar_ctx* ctx, int32_t layer, const void* q /*[device]*/,

@@ -73,8 +73,8 @@ Layout make_layout(const apar_config* c) {
 }
 
 struct WeightsLayout {     // partition of the memory of apar_attach_weights
-  size_t moves, counts, plan, total;
-  size_t plan_bytes;       // units, then users
+  size_t moves, counts, plan, prompt_plan, total;
+  size_t plan_bytes;       // of each: a KeyPlan, units, users
 };
 
 WeightsLayout make_weights_layout(const apar_config* c) {
@@ -85,9 +85,10 @@ WeightsLayout make_weights_layout(const apar_config* c) {
   L.moves = take(rows * sizeof(int2));                  // (no more rows stay than there are)
   L.counts = take((size_t)c->max_threads * std::max(1, c->num_layers) * c->num_kv_heads * 4);
   // (no block is in two units; a thread is a user of as many runs as its chain has forks)
-  L.plan_bytes = (size_t)c->num_blocks * sizeof(KeyUnit) +
+  L.plan_bytes = ((size_t)c->num_blocks + 1) * sizeof(KeyUnit) +
                  ((size_t)c->max_threads * 16 + 4096) * sizeof(KeyUser);
   L.plan = take(L.plan_bytes);
+  L.prompt_plan = take(L.plan_bytes);
   L.total = off;
   return L;
 }
@@ -176,8 +177,7 @@ struct apar_ctx {
   struct Seen { int32_t slot, lim; };         // queries of the last attention call; lim < 0: whole chain
   std::vector<Seen> seen;
   bool seen_valid = false, key_plan_valid = false;   // (they describe / the units on the device are of)
-  int32_t n_key_units[3] = {0, 0, 0};                // that call; by class
-  size_t key_users_at = 0;                           // where the users begin in the plan's area
+  KeyPlan key_plan = {};                             // that call
   // thread list of the most recent apar_decode_step; its table rows are resident on the device
   std::vector<int32_t> step_tids, step_slots, tmp_slots;
   bool step_valid = false;
@@ -722,11 +722,11 @@ apar_status upload(apar_ctx* c, const void* src, size_t bytes, char* dst, cudaSt
   return APAR_OK;
 }
 
-// Cuts the runs into units of at most `chunk` keys, longest first (by_class: the widest class first), and
-// sends both lists.
+// Cuts the runs into units of at most `chunk` keys, longest first (of a decode step: the widest class
+// first), and sends the plan.
 apar_status send_key_plan(apar_ctx* c, const std::vector<KeyRun>& runs, const std::vector<KeyUser>& users,
-                          int chunk, bool by_class, std::vector<KeyUnit>* units, cudaStream_t st) {
-  units->clear();
+                          int chunk, bool by_class, KeyPlan* plan, cudaStream_t st) {
+  std::vector<KeyUnit> unit_list, *units = &unit_list;
   for (const KeyRun& r : runs)
     for (int t = r.tok_begin; t < r.tok_end; t += chunk) {
       const bool last = t + chunk >= r.tok_end;
@@ -734,7 +734,7 @@ apar_status send_key_plan(apar_ctx* c, const std::vector<KeyRun>& runs, const st
                                r.user_begin, r.n_users, 0, {0, 0}});
     }
   const size_t b_units = units->size() * sizeof(KeyUnit), b_users = users.size() * sizeof(KeyUser);
-  if (b_units + b_users > c->wlay.plan_bytes) return APAR_ERR_WORKSPACE_TOO_SMALL;
+  if (sizeof(KeyUnit) + b_units + b_users > c->wlay.plan_bytes) return APAR_ERR_WORKSPACE_TOO_SMALL;
   // (queries that see the unit's keys, or all but a few of them)
   std::vector<int64_t> cost(units->size());
   std::vector<int32_t> order(units->size());
@@ -758,14 +758,17 @@ apar_status send_key_plan(apar_ctx* c, const std::vector<KeyRun>& runs, const st
   std::vector<KeyUnit> sorted(units->size());
   for (size_t i = 0; i < order.size(); ++i) sorted[i] = (*units)[order[i]];
   units->swap(sorted);
-  std::vector<char> plan(b_units + b_users);
-  memcpy(plan.data(), units->data(), b_units);
-  memcpy(plan.data() + b_units, users.data(), b_users);
-  c->key_users_at = b_units;
-  return upload(c, plan.data(), plan.size(), c->weights + c->wlay.plan, st);
+  *plan = KeyPlan{{0, 0, 0}, (int32_t)users.size()};
+  for (int32_t i = 0; i < (int32_t)units->size(); ++i) ++plan->n_units[cls(i)];   // (whatever their order)
+  std::vector<char> bytes(sizeof(KeyUnit) + b_units + b_users, 0);
+  memcpy(bytes.data(), plan, sizeof(*plan));
+  memcpy(bytes.data() + sizeof(KeyUnit), units->data(), b_units);
+  memcpy(bytes.data() + sizeof(KeyUnit) + b_units, users.data(), b_users);
+  return upload(c, bytes.data(), bytes.size(), c->weights + (by_class ? c->wlay.plan : c->wlay.prompt_plan), st);
 }
 
-KeyArgs key_args(apar_ctx* c, int layer, const void* q, const float* lse, float sm_scale, int replace) {
+KeyArgs key_args(apar_ctx* c, size_t plan, int layer, const void* q, const float* lse, float sm_scale,
+                 int replace) {
   KeyArgs a;
   a.q = q;
   a.lse = lse;
@@ -773,8 +776,7 @@ KeyArgs key_args(apar_ctx* c, int layer, const void* q, const float* lse, float 
   a.weights = (float*)c->weights + (size_t)layer * c->layer_weights();
   a.d_tables = (const int32_t*)c->ws(c->lay.tables);
   a.d_lens = (const int32_t*)c->ws(c->lay.lens);
-  a.units = (const KeyUnit*)(c->weights + c->wlay.plan);
-  a.users = (const KeyUser*)(c->weights + c->wlay.plan + c->key_users_at);
+  a.plan = (const KeyPlan*)(c->weights + plan);
   a.shape = c->shape;
   a.scale_log2e = sm_scale * 1.4426950408889634f;
   a.replace = replace != 0;
@@ -1717,7 +1719,7 @@ apar_status apar_read_kv(apar_ctx* c, int32_t layer, int32_t n, const int32_t* t
 }
 
 apar_status apar_reorder(apar_ctx* c, int32_t n, const int32_t* tid, const int32_t* source_tid,
-                         void* cuda_stream) {
+                         void* cuda_stream) try {
   if (!c || n < 0 || (n > 0 && (!tid || !source_tid))) return APAR_ERR_INVALID_ARG;
   cudaStream_t st = (cudaStream_t)cuda_stream;
   for (int i = 0; i < n; ++i)
@@ -1819,6 +1821,8 @@ apar_status apar_reorder(apar_ctx* c, int32_t n, const int32_t* tid, const int32
     return copy_rows(c, (const CowCopy*)d_stage, nc, st);
   }
   return APAR_OK;
+} catch (...) {               // (the host's memory)
+  return APAR_ERR_INVALID_ARG;
 }
 
 size_t apar_weights_bytes(const apar_config* cfg) {
@@ -1843,7 +1847,7 @@ apar_status apar_set_lse_output(apar_ctx* c, float* lse) {
 }
 
 apar_status apar_add_weights(apar_ctx* c, int32_t layer, const void* q, const float* lse,
-                             float sm_scale, int32_t replace, void* cuda_stream) {
+                             float sm_scale, int32_t replace, void* cuda_stream) try {
   if (!c || layer < 0 || layer >= c->num_layers || !q || !lse || ((uintptr_t)q & 15) ||
       ((uintptr_t)lse & 3))
     return APAR_ERR_INVALID_ARG;
@@ -1869,22 +1873,24 @@ apar_status apar_add_weights(apar_ctx* c, int32_t layer, const void* q, const fl
     for (const KeyRun& r : runs) keys += r.tok_end - r.tok_begin;
     const int64_t share = keys * c->cfg.num_kv_heads / ((int64_t)c->num_sms * kKeyUnitsPerSm);
     const int64_t chunk = std::min<int64_t>(1024, std::max<int64_t>(64, (share + 15) / 16 * 16));
-    std::vector<KeyUnit> units;
-    rc = send_key_plan(c, runs, users, (int)chunk, true, &units, st);
+    rc = send_key_plan(c, runs, users, (int)chunk, true, &c->key_plan, st);
     if (rc) return rc;
-    for (int32_t& n : c->n_key_units) n = 0;
-    for (const KeyUnit& u : units) ++c->n_key_units[key_class(u.n_users * c->shape.group)];
     c->key_plan_valid = true;
   }
-  APAR_CUDA(c, launch_key_weights(key_args(c, layer, q, lse, sm_scale, replace), c->n_key_units, st));
+  cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+  APAR_CUDA(c, cudaStreamIsCapturing(st, &cap));
+  APAR_CUDA(c, launch_key_weights(key_args(c, c->wlay.plan, layer, q, lse, sm_scale, replace),
+                                  c->key_plan.n_units, cap != cudaStreamCaptureStatusNone, st));
   ++c->kernels_total;
   return APAR_OK;
+} catch (...) {               // (the host's memory)
+  return APAR_ERR_INVALID_ARG;
 }
 
 apar_status apar_add_weights_prefill(apar_ctx* c, int32_t layer, int32_t n, const int32_t* tid,
                                      const int32_t* q_begin, const int32_t* q_count, const void* q,
                                      const float* lse, float sm_scale, int32_t replace,
-                                     void* cuda_stream) {
+                                     void* cuda_stream) try {
   if (!c || n < 0 || layer < 0 || layer >= c->num_layers ||
       (n > 0 && (!tid || !q_begin || !q_count || !q || !lse)) || ((uintptr_t)q & 15) || ((uintptr_t)lse & 3))
     return APAR_ERR_INVALID_ARG;
@@ -1913,21 +1919,22 @@ apar_status apar_add_weights_prefill(apar_ctx* c, int32_t layer, int32_t n, cons
     return APAR_ERR_INVALID_ARG;
   std::vector<KeyRun> runs;
   std::vector<KeyUser> users;
-  std::vector<KeyUnit> units;
+  KeyPlan plan;
   if (!c->planner.key_runs(qs.data(), n, &runs, &users)) return APAR_ERR_INVALID_ARG;
-  c->key_plan_valid = false;                             // (this plan takes the place of the other's)
-  rc = send_key_plan(c, runs, users, kPromptUnit, false, &units, st);
+  rc = send_key_plan(c, runs, users, kPromptUnit, false, &plan, st);
   if (rc == APAR_OK) rc = sync_device_tables(c, slots.data(), n, st);
   if (rc) return rc;
-  APAR_CUDA(c, launch_prompt_weights(key_args(c, layer, q, lse, sm_scale, replace), &c->tm_k[layer], &tm_q,
-                                     (int)units.size(), st));
+  APAR_CUDA(c, launch_prompt_weights(key_args(c, c->wlay.prompt_plan, layer, q, lse, sm_scale, replace),
+                                     &c->tm_k[layer], &tm_q, plan.n_units[0], st));
   ++c->kernels_total;
   return APAR_OK;
+} catch (...) {               // (the host's memory)
+  return APAR_ERR_INVALID_ARG;
 }
 
 apar_status apar_read_weights(apar_ctx* c, int32_t layer, int32_t n, const int32_t* tid,
                               const int32_t* begin, const int32_t* count, float* out,
-                              void* cuda_stream) {
+                              void* cuda_stream) try {
   if (!c || n < 0 || layer < 0 || layer >= c->num_layers || (n > 0 && (!tid || !begin || !count)))
     return APAR_ERR_INVALID_ARG;
   if (c->host_only || c->q4) return APAR_ERR_UNSUPPORTED;
@@ -1973,10 +1980,12 @@ apar_status apar_read_weights(apar_ctx* c, int32_t layer, int32_t n, const int32
     ++c->kernels_total;
   }
   return APAR_OK;
+} catch (...) {               // (the host's memory)
+  return APAR_ERR_INVALID_ARG;
 }
 
 apar_status apar_evict(apar_ctx* c, int32_t n, const int32_t* tid, const int32_t* begin,
-                       const int32_t* end, const int32_t* keep, void* cuda_stream) {
+                       const int32_t* end, const int32_t* keep, void* cuda_stream) try {
   if (!c || n < 0 || (n > 0 && (!tid || !begin || !end || !keep))) return APAR_ERR_INVALID_ARG;
   if (c->q4) return APAR_ERR_UNSUPPORTED;
   if (!c->weights && !c->host_only) return APAR_ERR_INVALID_ARG;   // (the bookkeeping needs none)
@@ -2156,6 +2165,8 @@ apar_status apar_evict(apar_ctx* c, int32_t n, const int32_t* tid, const int32_t
   APAR_CUDA(c, launch_evict(a, (int)entries.size(), c->num_layers, max_len, max_rows, st));
   c->kernels_total += 2;
   return APAR_OK;
+} catch (...) {               // (the host's memory)
+  return APAR_ERR_INVALID_ARG;
 }
 
 apar_status apar_release(apar_ctx* c, int32_t n, const int32_t* tid) {

@@ -270,6 +270,18 @@ struct KeyUser {
                                  // first one's position, the last key that it sees
   int32_t count, pad;            // queries of the run
 };
+// What the kernels find at the beginning of a plan.  Read on the device, so that a captured launch that is
+// replayed follows the plan that lies there then.
+struct KeyPlan {
+  int32_t n_units[3];            // by key_class, which are in the list from the last one on; a prompt's plan
+                                 // has them all in the first
+  int32_t n_users;
+  __host__ __device__ const KeyUnit* units() const { return (const KeyUnit*)(this + 2); }
+  __host__ __device__ const KeyUser* users() const {
+    return (const KeyUser*)(units() + n_units[0] + n_units[1] + n_units[2]);
+  }
+};
+static_assert(2 * sizeof(KeyPlan) == sizeof(KeyUnit), "alignment");
 struct KeyArgs {
   const void* q;
   const float* lse;
@@ -277,8 +289,7 @@ struct KeyArgs {
   float* weights;                // [num_blocks][num_kv_heads][16]
   const int32_t* d_tables;
   const int32_t* d_lens;
-  const KeyUnit* units;
-  const KeyUser* users;
+  const KeyPlan* plan;
   Shape shape;
   float scale_log2e;
   int replace;                   // 1: the keys' old weights do not count
@@ -318,9 +329,10 @@ cudaError_t launch_weights_clear(float* w, size_t layer_floats, int num_layers, 
 cudaError_t launch_weights_move(float* w, size_t layer_floats, int num_layers, const RowMove* d_moves,
                                 const int32_t* d_group_begin, int n_groups, int num_kv_heads,
                                 cudaStream_t st);
-// Units in three classes, the widest first in the list: n_units[i] of key_class i.
+// n_units: of the plan as the host knows it, for the size of the grids.  all: launch all classes, as a
+// captured call has to that may be replayed with another plan.
 inline int key_class(int rows) { return rows <= 8 ? 0 : rows <= 16 ? 1 : 2; }
-cudaError_t launch_key_weights(KeyArgs a, const int32_t (&n_units)[3], cudaStream_t st);
+cudaError_t launch_key_weights(const KeyArgs& a, const int32_t (&n_units)[3], bool all, cudaStream_t st);
 // Units of at most 256 keys, closed; a user is a run of queries, the first at position lim.  tm_q as in
 // launch_attention_prefill.
 constexpr int kPromptUnit = 256;

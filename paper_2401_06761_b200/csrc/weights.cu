@@ -76,8 +76,9 @@ constexpr int kKeyWarps = 4;                     // per CTA
 
 // Rows r0 .. r0 + 8 NT - 1 of the unit against its keys [begin, end) of kv head h.
 template <int NT, int kAhead>
-__device__ __forceinline__ void key_rows(const KeyArgs& a, const KeyUnit& it, const int32_t* table, int h,
-                                         int end, int rows, int r0, bool replace) {
+__device__ __forceinline__ void key_rows(const KeyArgs& a, const KeyUnit& it, const KeyUser* users,
+                                         const int32_t* table, int h, int end, int rows, int r0,
+                                         bool replace) {
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int G = a.shape.group, HQ = a.shape.num_q_heads, HKV = a.shape.num_kv_heads;
   const int n_blk = (end - it.tok_begin + kBlock - 1) / kBlock;
@@ -105,7 +106,7 @@ __device__ __forceinline__ void key_rows(const KeyArgs& a, const KeyUnit& it, co
   for (int i = 0; i < NT; ++i) {
     const int r = r0 + 8 * i + g;
     if (r < rows) {
-      const int query = a.users[it.user_begin + r / G].query;
+      const int query = users[it.user_begin + r / G].query;
       const uint4* src = (const uint4*)((const __nv_bfloat16*)a.q + ((size_t)query * HQ + h * G + r % G) * kDim);
 #pragma unroll
       for (int w = 0; w < 4; ++w) q[i][w] = __ldg(src + 4 * w + t);
@@ -119,7 +120,7 @@ __device__ __forceinline__ void key_rows(const KeyArgs& a, const KeyUnit& it, co
       ref[i][e] = 0.f;
       see[i][e] = 0;
       if (rr < rows) {
-        const KeyUser user = a.users[it.user_begin + rr / G];
+        const KeyUser user = users[it.user_begin + rr / G];
         ref[i][e] = __ldg(a.lse + (size_t)user.query * HQ + h * G + rr % G) * 1.4426950408889634f;
         see[i][e] = min(user.lim, end);
       }
@@ -176,19 +177,25 @@ __device__ __forceinline__ void key_rows(const KeyArgs& a, const KeyUnit& it, co
 }
 
 template <int NT, int kAhead, int kCtas>
-__global__ void __launch_bounds__(kKeyWarps * 32, kCtas) key_weights_kernel(const KeyArgs a, int n_units) {
+__global__ void __launch_bounds__(kKeyWarps * 32, kCtas) key_weights_kernel(const KeyArgs a) {
+  constexpr int kClass = NT == 1 ? 0 : NT == 2 ? 1 : 2;
   const int G = a.shape.group, HKV = a.shape.num_kv_heads;
   const int64_t stride = (int64_t)gridDim.x * kKeyWarps;
   pdl_launch_dependents();
-  for (int64_t u = (int64_t)blockIdx.x * kKeyWarps + (threadIdx.x >> 5); u < (int64_t)n_units * HKV; u += stride) {
-    const KeyUnit it = a.units[u / HKV];
+  const KeyUnit* units = a.plan->units();
+  const KeyUser* users = a.plan->users();
+#pragma unroll
+  for (int c = 2; c > kClass; --c) units += a.plan->n_units[c];
+  const int64_t total = (int64_t)a.plan->n_units[kClass] * HKV;
+  for (int64_t u = (int64_t)blockIdx.x * kKeyWarps + (threadIdx.x >> 5); u < total; u += stride) {
+    const KeyUnit it = units[u / HKV];
     const int h = (int)(u % HKV);
     const int32_t* table = a.d_tables + (size_t)it.table_row * a.shape.table_stride;
     const int end = it.tok_end < 0 ? a.d_lens[it.table_row] : it.tok_end;
     const int rows = it.n_users * G;
     if (it.tok_begin >= end) continue;
     for (int r0 = 0; r0 < rows; r0 += 8 * NT)
-      key_rows<NT, kAhead>(a, it, table, h, end, rows, r0, a.replace && r0 == 0);
+      key_rows<NT, kAhead>(a, it, users, table, h, end, rows, r0, a.replace && r0 == 0);
   }
   pdl_wait();                                    // (done means that the launches before it are, too)
 }
@@ -588,15 +595,14 @@ cudaError_t launch_weights_move(float* w, size_t layer_floats, int num_layers, c
                        false, w, layer_floats, d_moves, d_group_begin, num_kv_heads);
 }
 
-cudaError_t launch_key_weights(KeyArgs a, const int32_t (&n_units)[3], cudaStream_t st) {
+cudaError_t launch_key_weights(const KeyArgs& a, const int32_t (&n_units)[3], bool all, cudaStream_t st) {
   cudaError_t e = cudaSuccess;
   bool first = true;
   auto launch = [&](auto kernel, int n, int ctas) {
-    if (n <= 0 || e != cudaSuccess) return;
-    const int64_t warps = (int64_t)n * a.shape.num_kv_heads;
-    const int grid = (int)std::min<int64_t>((warps + kKeyWarps - 1) / kKeyWarps, (int64_t)ctas * a.num_sms);
-    e = launch_kernel(kernel, dim3(grid), dim3(kKeyWarps * 32), 0, st, !first, a, n);
-    a.units += n;
+    if ((n <= 0 && !all) || e != cudaSuccess) return;
+    const int64_t ctas_full = (int64_t)ctas * a.num_sms, warps = (int64_t)n * a.shape.num_kv_heads;
+    const int grid = (int)(all ? ctas_full : std::min<int64_t>((warps + kKeyWarps - 1) / kKeyWarps, ctas_full));
+    e = launch_kernel(kernel, dim3(grid), dim3(kKeyWarps * 32), 0, st, !first, a);
     first = false;
   };
   launch(key_weights_kernel<4, 1, 3>, n_units[2], 3);

@@ -115,13 +115,16 @@ struct UnitWalk {
   const KeyArgs& a;
   const int64_t total;
   const int b;
+  const KeyUnit* units;
+  const KeyUser* users;
   int64_t i = 0;                                 // units looked at so far
   KeyUnit it, it1, it2;                          // the current one, the next, the one after that
   KeyUser user, user1;
   int h, h1, h2, bid, bid1;
   bool more, more1, more2;
 
-  __device__ UnitWalk(const KeyArgs& args, int64_t n, int lane) : a(args), total(n), b(lane >> 1) {
+  __device__ UnitWalk(const KeyArgs& args, int64_t n, int lane)
+      : a(args), total(n), b(lane >> 1), units(args.plan->units()), users(args.plan->users()) {
     look();
     fetch();
     look();
@@ -132,7 +135,7 @@ struct UnitWalk {
     while (i * gridDim.x < total && !more2) {
       const int64_t u = dealt(i++);
       if (u >= total) continue;
-      it2 = a.units[u / a.shape.num_kv_heads];
+      it2 = units[u / a.shape.num_kv_heads];
       h2 = (int)(u % a.shape.num_kv_heads);
       more2 = true;
     }
@@ -142,7 +145,7 @@ struct UnitWalk {
     if (!more1) return;
     it1 = it2;
     h1 = h2;
-    user1 = a.users[it1.user_begin];
+    user1 = users[it1.user_begin];
     bid1 = b < (it1.tok_end - it1.tok_begin + kBlock - 1) / kBlock
                ? a.d_tables[(size_t)it1.table_row * a.shape.table_stride + it1.tok_begin / kBlock + b] : 0;
   }
@@ -240,7 +243,7 @@ prompt_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                &tm_k, (lane & 1) * 64, (u.bid * HKV + u.h) * kBlock, kf);
       int flags = F_FIRST | (n_blk * kBlock > kKeys ? F_BOTH : 0);
       KeyUser user = u.user;
-      for (int x = 0; ok; user = a.users[u.it.user_begin + x]) {
+      for (int x = 0; ok; user = u.users[u.it.user_begin + x]) {
         const int end = user.query + user.count;
         ++x;
         for (int q0 = user.query + max(0, u.it.tok_begin - user.lim); q0 < end; q0 += T, ++g) {
@@ -293,7 +296,7 @@ prompt_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
     for (UnitWalk u(a, total, lane); ok && u.more; u.step()) {
       KeyUser user = u.user;
       int t = 0;
-      for (int x = 0; ok; user = a.users[u.it.user_begin + x]) {
+      for (int x = 0; ok; user = u.users[u.it.user_begin + x]) {
         ++x;
         int j = max(0, u.it.tok_begin - user.lim);
         int64_t at = (int64_t)(user.query + j) * HQ + u.h * G;

@@ -312,8 +312,13 @@ class PagedSession:
 
     def read_weights(self, tids, begin, count, layer: int = 0):
         """Weights [rows][kv heads] of rows begin[i] .. begin[i] + count[i] - 1 of each chain."""
+        if not isinstance(count, list):
+            count = B.int32_array(count)
+            rows = int(np.frombuffer(count[0], np.int32, count[1]).sum(dtype=np.int64))
+        else:
+            rows = int(sum(count))
         # (negative counts are the library's to refuse)
-        out = torch.empty((max(0, int(sum(count))), self.shape.num_kv_heads), dtype=torch.float32,
+        out = torch.empty((max(0, rows), self.shape.num_kv_heads), dtype=torch.float32,
                           device=self.device)
         B.apar_read_weights(self.ctx, layer, tids, begin, count, out.data_ptr(), self._stream())
         return out

@@ -296,6 +296,60 @@ def test_captured_step_with_weights():
     f.check_weights(tids, rel)
 
 
+def test_replays_between_other_plans():
+    """A captured step with weights is replayed after a prompt's weights and after another step's plan of
+    the same threads took the place of the captured one's."""
+    f, tids = small_forest(8, 2)
+    f.append(tids, [16 - len(f.names[t]) % 16 + 1 for t in tids])
+    q = rows(len(tids), 8, 50)
+    k, v = rows(len(tids), 2, 51), rows(len(tids), 2, 52)
+    lse, out = torch.empty(len(tids), 8, device="cuda"), torch.empty_like(q)
+
+    def step():
+        f.s.decode_step(tids, k, v, q, out=out, lse=lse)
+        f.s.add_weights(q, lse)
+
+    def follow():
+        host = k.double().cpu().numpy(), v.double().cpu().numpy()
+        for i, t in enumerate(tids):
+            f.names[t].append(f.n)
+            f.k[f.n], f.v[f.n], f.w[f.n] = host[0][i][None], host[1][i][None], np.zeros((1, 2))
+            f.n += 1
+        return f.add(tids, q)[1]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+        follow()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            step()
+        g.replay()
+        rel = follow()
+        n = len(f.names[tids[0]])
+        p, pl = rows(20, 8, 60), torch.empty(20, 8, device="cuda")
+        # (the lse of a thread's last rows, without an attention call in between, from its definition)
+        want, _ = add_segments(f, [(tids[0], n - 20, 20)], p)
+        pl.copy_(torch.from_numpy(want).float())
+        f.s.add_weights_prefill([tids[0]], [n - 20], [20], p, pl)
+        B.apar_note_step_replay(f.s.ctx)
+        g.replay()
+        follow()
+        some = tids[:3]
+        q3, lse3 = rows(3, 8, 70), torch.empty(3, 8, device="cuda")
+        f.s.attention(some, q3, lse=lse3)
+        f.s.add_weights(q3, lse3)
+        f.add(some, q3)
+        with pytest.raises(B.AparError):                 # (the plan is another's)
+            B.apar_note_step_replay(f.s.ctx)
+        f.s.attention(tids, q, lse=lse)
+        f.s.add_weights(q, lse)
+        rel = max(rel, f.add(tids, q)[1])
+        side.synchronize()
+    f.check_weights(tids, 2 * rel)                       # (lse rounded once more)
+
+
 def test_rows_that_move_take_their_weights_along():
     f, tids = small_forest(8, 2)
     t = tids[4]
