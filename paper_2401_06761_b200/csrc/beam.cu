@@ -404,7 +404,7 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
   __shared__ double base[kMaxBeams];           // score - lse; NaN: the beam has no pairs
   __shared__ float2 stats[kMaxLists], terms[kMaxLists];
   __shared__ uint8_t over[kMaxBeams];
-  __shared__ uint32_t tops[2 * kWarps];
+  __shared__ uint32_t tops[kWarps];
   __shared__ Pair picks[kWarps];
   __shared__ int n_cand;
   const int seq = blockIdx.x, n_lists = a.beams * a.pieces, n_all = n_lists * a.select;
@@ -459,8 +459,33 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
     const double x = pair_of(i).value;
     if (x > -INFINITY) mine = fmaxf(mine, __double2float_rn(x));
   }
-  uint32_t most;
-  const float tau = unordered(threshold(ordered(mine), a.select, n_all / 32, tops, &most));
+  // A threshold that at least num_select of the threads' maxima reach, and hardly more: down from the
+  // largest in growing steps, then halving the last one.  (Beams differ too much for what serves above.)
+  const uint32_t most_here = __reduce_max_sync(kAll, ordered(mine));
+  if (lane == 0) tops[warp] = most_here;
+  __syncthreads();
+  uint32_t most = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) most = max(most, tops[w]);
+  float tau = unordered(most), above = tau, width = 1.f;
+  int reach = 0;
+  while (reach < a.select && tau > -3e38f) {
+    above = tau;
+    tau = unordered(most) - width;
+    width *= 4.f;
+    reach = __syncthreads_count(mine >= tau);
+  }
+  if (reach < a.select) tau = -INFINITY;
+  for (int i = 0; i < 8 && reach > a.select + a.select / 2 + 8; ++i) {
+    const float mid = 0.5f * (tau + above);
+    const int n = __syncthreads_count(mine >= mid);
+    if (n >= a.select) {
+      tau = mid;
+      reach = n;
+    } else {
+      above = mid;
+    }
+  }
   for (int i = threadIdx.x; i < n_all; i += kThreads) {
     const Pair p = pair_of(i);
     if (p.value > -INFINITY && __double2float_rn(p.value) >= tau) {   // (rounding keeps the order)
