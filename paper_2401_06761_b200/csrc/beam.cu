@@ -5,19 +5,27 @@
 // enough: it keeps, per piece of a row, the num_select largest logits and the piece's maximum and sum
 // of exponentials, and a second small kernel puts the pieces of a sequence's rows together.
 //
-// beam_scan_kernel   one CTA per piece, which reads up to 12288 (f32) or 16384 (16-bit) elements into
+// beam_scan_kernel   one CTA per piece, which reads 8192 (f32) or 16384 (16-bit) elements at a time into
 //     registers, all loads on their way at once, sixteen bytes each where a row begins on such a
 //     boundary.  Which thread holds which element, and so the order of the sums, depends on the
 //     element alone: equal rows tie exactly.  A threshold that at least num_select elements reach comes
 //     from the threads' maxima: with j = num_select / 8 rounded up, the least of the eight warps' j-th
-//     largest.  The few elements that reach it (some two to three times num_select) are collected in shared
-//     memory and put in order by counting, for each, how many are larger.  A key is (ordered bits of
-//     the logit, complement of the token): of equal logits the lower token is kept.  Where more than
+//     largest.  The few elements that reach it (some two to three times num_select; the exact
+//     num_select-th largest of the maxima leaves fewer, but takes longer than it saves) are collected in
+//     shared memory and put in order by counting, for each, how many are larger.  A key is (ordered bits
+//     of the logit, complement of the token): of equal logits the lower token is kept.  Where more than
 //     512 elements reach the threshold (many equal ones) the warps go over the piece again with
 //     buffers that they sort and cut back as they fill.
-// beam_pick_kernel   one CTA per sequence, the same way over the pieces' lists.  Values of different
-//     beams are compared in 64 bits: their difference goes through two log-sum-exps, and 32 bits would
-//     round it.
+// beam_pick_kernel   one CTA per sequence: a threshold by halving (the beams' scores differ too much for
+//     the one above), and the few pairs that reach it ordered by counting.  Values of different beams are
+//     compared in 64 bits: their difference goes through two log-sum-exps, and 32 bits would round it.
+//
+// Bound: 4 bytes per f32 logit, one product and one special-function operation for each.  2048 rows of
+// 32003 f32 logits, a fifth of them finished (208 MB read): scan 55 us, 3.8 TB/s; without the exponentials
+// it takes 6 us less, without collecting and ordering 18: what is left is the waits between a CTA's steps,
+// which four CTAs of an SM cover in part.  (Tried: the next piece's copies into shared memory meanwhile, 73;
+// into registers, 58 with 64 of them a thread; into L2, no change.)  128 rows of 131072 bf16 logits: 14 us,
+// 2.4 TB/s, two and a half rounds of CTAs.  4 rows of 32000: 5 us, then 5 for the pick.
 #include <algorithm>
 #include <climits>
 
@@ -42,6 +50,23 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr unsigned kAll = 0xffffffffu;
 typedef unsigned long long u64;
 
+__device__ __forceinline__ u64 pair_of(float a, float b) {
+  return (u64)__float_as_uint(b) << 32 | __float_as_uint(a);
+}
+__device__ __forceinline__ float2 parts_of(u64 p) {
+  return make_float2(__uint_as_float((uint32_t)p), __uint_as_float((uint32_t)(p >> 32)));
+}
+__device__ __forceinline__ u64 fma2(u64 a, u64 b, u64 c) {
+  u64 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ u64 add2(u64 a, u64 b) {
+  u64 d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
 __device__ __forceinline__ uint32_t ordered(float x) {   // (-0 counts as 0)
   const uint32_t b = __float_as_uint(x + 0.f);
   return b ^ (uint32_t)((int32_t)b >> 31 | 0x80000000);
@@ -51,7 +76,8 @@ __device__ __forceinline__ float unordered(uint32_t o) {   // (what is below -in
   return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
 }
 
-// A row's elements in packs of sixteen bytes.
+// A row's elements in packs of sixteen bytes.  (f32: 12 packs of a thread and 3 CTAs 55 us where 8 and 4 take
+// 54; 16-bit: 4 packs and 4 CTAs 21 us where 8 and 3 take 14.)
 __device__ __forceinline__ float number(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float number(__half x) { return __half2float(x); }
 __device__ __forceinline__ float number(float x) { return x; }
@@ -59,7 +85,7 @@ template <typename T>
 struct Packs;
 template <>
 struct Packs<float> {
-  static constexpr int kPer = 4, kHeld = 12;           // elements of a pack, packs a thread holds
+  static constexpr int kPer = 4, kHeld = 8, kCtas = 4; // a pack's elements, a thread's packs, CTAs of an SM
   static constexpr uint32_t kNone = 0xff800000u;       // -inf
   static __device__ __forceinline__ void numbers(uint4 w, float (&x)[4]) {
     x[0] = __uint_as_float(w.x);
@@ -70,7 +96,7 @@ struct Packs<float> {
 };
 template <>
 struct Packs<__nv_bfloat16> {
-  static constexpr int kPer = 8, kHeld = 8;
+  static constexpr int kPer = 8, kHeld = 8, kCtas = 3;
   static constexpr uint32_t kNone = 0xff80ff80u;
   static __device__ __forceinline__ void numbers(uint4 w, float (&x)[8]) {
     const uint32_t v[4] = {w.x, w.y, w.z, w.w};
@@ -83,7 +109,7 @@ struct Packs<__nv_bfloat16> {
 };
 template <>
 struct Packs<__half> {
-  static constexpr int kPer = 8, kHeld = 8;
+  static constexpr int kPer = 8, kHeld = 8, kCtas = 3;
   static constexpr uint32_t kNone = 0xfc00fc00u;
   static __device__ __forceinline__ void numbers(uint4 w, float (&x)[8]) {
     const uint32_t v[4] = {w.x, w.y, w.z, w.w};
@@ -95,6 +121,17 @@ struct Packs<__half> {
     }
   }
 };
+__device__ __forceinline__ float max3(float a, float b, float c) {   // (a NaN counts as less than everything)
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+template <int N>
+__device__ __forceinline__ float largest(float m, const float (&x)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += 2) m = max3(m, x[i], x[i + 1]);
+  return m;
+}
 // A whole pack from an address on a boundary of kAlign bytes.
 template <int kAlign>
 __device__ __forceinline__ uint4 load_pack(const void* p) {
@@ -252,14 +289,15 @@ union ScanKeys {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 3) beam_scan_kernel(const BeamArgs a) {
+__global__ void __launch_bounds__(kThreads, Packs<T>::kCtas) beam_scan_kernel(const BeamArgs a) {
   using W = Packs<T>;
   constexpr int kPer = W::kPer, kHeld = W::kHeld, kChunk = kThreads * kHeld;   // packs of a CTA
   __shared__ ScanKeys sh;
   __shared__ u64 held[kMaxSelect];             // the largest so far, in order
   __shared__ uint32_t tops[2 * kWarps];
   __shared__ float sums[kWarps];
-  __shared__ int counts[kWarps], n_cand;
+  __shared__ int counts[kWarps], n_cand, n_hit;
+  __shared__ uint8_t hit[kThreads];            // threads with something that reaches the threshold
   pdl_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int row = blockIdx.x / a.pieces, piece = blockIdx.x % a.pieces;
@@ -281,53 +319,35 @@ __global__ void __launch_bounds__(kThreads, 3) beam_scan_kernel(const BeamArgs a
     for (int k = 0; k < kHeld; ++k) {
       float e[kPer];
       W::numbers(v[k], e);
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) mine = fmaxf(mine, e[i]);
+      mine = largest(mine, e);
     }
-    if (threadIdx.x == 0) n_cand = n_held;
+    if (threadIdx.x == 0) {
+      n_cand = n_held;
+      n_hit = 0;
+    }
     if ((int)threadIdx.x < n_held) sh.cand[threadIdx.x] = held[threadIdx.x];
     uint32_t most;
     float tau = unordered(threshold(ordered(mine), a.select, min(end - c0, kChunk) / 32, tops, &most));
     if (n_held == a.select) tau = fmaxf(tau, unordered((uint32_t)(held[n_held - 1] >> 32)));
+    if (mine >= tau && mine > -INFINITY) hit[atomicAdd(&n_hit, 1)] = (uint8_t)threadIdx.x;
     // 2^(x log2 e - ref), ref being max log2 e; what rounding that product takes off every exponent is
     // put back into the sum
     const float top = unordered(most);
     const bool finite = top - top == 0.f;
     const float ref = top == -INFINITY ? 0.f : top * kLog2e;
-    float part[2] = {0.f, 0.f};
+    u64 part = 0;                              // two sums
+    const u64 scale = pair_of(kLog2e, kLog2e), less = pair_of(-ref, -ref);
 #pragma unroll
     for (int k = 0; k < kHeld; ++k) {
       float e[kPer];
       W::numbers(v[k], e);
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) part[i & 1] += ex2(fmaf(e[i], kLog2e, -ref));
-    }
-    // The few elements that reach the threshold: their packs' bits first, then a loop that reads them again
-    // (what to do with one, once for each that a thread holds, would be 600 instructions to fetch).
-    if (mine >= tau && mine > -INFINITY) {
-      uint32_t hits = 0;
-#pragma unroll
-      for (int k = 0; k < kHeld; ++k) {
-        float e[kPer];
-        W::numbers(v[k], e);
-        bool any = false;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) any = any || e[i] >= tau;
-        if (any) hits |= 1u << k;
-      }
-      for (; hits; hits &= hits - 1) {
-        const uint32_t token = (c0 + (__ffs(hits) - 1) * kThreads + threadIdx.x) * kPer;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          const float e = (int)token + i < n_in ? number(x[token + i]) : -INFINITY;
-          if (e >= tau && e > -INFINITY) {
-            const int at = atomicAdd(&n_cand, 1);
-            if (at < kCand) sh.cand[at] = (u64)ordered(e) << 32 | ~(token + i);
-          }
-        }
+      for (int i = 0; i < kPer; i += 2) {
+        const float2 p = parts_of(fma2(pair_of(e[i], e[i + 1]), scale, less));
+        part = add2(part, pair_of(ex2(p.x), ex2(p.y)));
       }
     }
-    float sum = part[0] + part[1];
+    float sum = parts_of(part).x + parts_of(part).y;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
     if (lane == 0) sums[warp] = sum;
@@ -342,14 +362,42 @@ __global__ void __launch_bounds__(kThreads, 3) beam_scan_kernel(const BeamArgs a
       l = l * ex2((m - r) * kLog2e) + s * (top == -INFINITY ? 1.f : ex2((top - r) * kLog2e));
       m = both;
     }
+    // The few elements that reach the threshold: the hit threads' packs are read again, each by a thread of
+    // its own.  (Looked for by the threads that hold them, they take longer than all the exponentials.)
+    for (int i = threadIdx.x, n = n_hit * kHeld; i < n; i += kThreads) {
+      const int at = c0 + i % kHeld * kThreads + hit[i / kHeld];
+      if (at * kPer >= n_in) continue;
+      float e[kPer];
+      if (((uintptr_t)x & 15) == 0 && (at + 1) * kPer <= n_in) {
+        W::numbers(load_pack<16>(x + (int64_t)at * kPer), e);
+      } else {
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) e[k] = at * kPer + k < n_in ? number(x[at * kPer + k]) : -INFINITY;
+      }
+      if (!(largest(-INFINITY, e) >= tau)) continue;
+      int slot = 0;
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) slot += e[k] >= tau && e[k] > -INFINITY;
+      slot = atomicAdd(&n_cand, slot);
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) {
+        if (!(e[k] >= tau && e[k] > -INFINITY)) continue;
+        if (slot < kCand) sh.cand[slot] = (u64)ordered(e[k]) << 32 | (uint32_t)~(at * kPer + k);
+        ++slot;
+      }
+    }
+    __syncthreads();
     const int n = n_cand;
     if (n <= kCand) {
-      // (each thread one or two of them; their order in the list does not matter)
-      for (int i = threadIdx.x; i < n; i += kThreads) {
-        const u64 key = sh.cand[i];
+      // (four threads to each of them; their order in the list does not matter)
+      for (int i0 = 0; i0 < n; i0 += kThreads / 4) {
+        const int i = i0 + threadIdx.x / 4;
+        const u64 key = i < n ? sh.cand[i] : 0ull;
         int rank = 0;
-        for (int j = 0; j < n; ++j) rank += sh.cand[j] > key;
-        if (rank < a.select) held[rank] = key;
+        for (int j = threadIdx.x & 3; j < n; j += 4) rank += sh.cand[j] > key;
+        rank += __shfl_xor_sync(kAll, rank, 1);
+        rank += __shfl_xor_sync(kAll, rank, 2);
+        if (i < n && rank < a.select) held[rank] = key;
       }
       n_held = min(n, a.select);
       __syncthreads();
@@ -447,7 +495,7 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
   }
   __syncthreads();
   // pair i of the lists; a value that is not above -inf: none
-  auto pair_of = [&](int i) {
+  auto entry = [&](int i) {
     const int list = i / a.select, b = list / a.pieces;
     if (over[b]) return Pair{i % (a.pieces * a.select) ? -INFINITY : base[b], (u64)b << 32 | (uint32_t)a.eos};
     const u64 key = i < kThreads ? key0 : keys[i];   // (every thread asks for i = its own first)
@@ -456,7 +504,7 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
   };
   float mine = -INFINITY;
   for (int i = threadIdx.x; i < n_all; i += kThreads) {
-    const double x = pair_of(i).value;
+    const double x = entry(i).value;
     if (x > -INFINITY) mine = fmaxf(mine, __double2float_rn(x));
   }
   // A threshold that at least num_select of the threads' maxima reach, and hardly more: down from the
@@ -487,7 +535,7 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
     }
   }
   for (int i = threadIdx.x; i < n_all; i += kThreads) {
-    const Pair p = pair_of(i);
+    const Pair p = entry(i);
     if (p.value > -INFINITY && __double2float_rn(p.value) >= tau) {   // (rounding keeps the order)
       const int at = atomicAdd(&n_cand, 1);
       if (at < kCand) cand[at] = p;
@@ -519,7 +567,7 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
   for (int k = 0; k < a.select; ++k) {
     Pair best = none;
     for (int i = threadIdx.x; i < n_all; i += kThreads) {
-      const Pair p = pair_of(i);
+      const Pair p = entry(i);
       if (p.value > -INFINITY && before(last, p) && before(p, best)) best = p;
     }
 #pragma unroll
@@ -538,16 +586,19 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
   }
 }
 
-// Pieces of a row: what a CTA's registers hold, and more of them where there are few rows, to fill the
-// machine twice over, none shorter than 2048 elements.
+// Pieces of a row.  Few rows are cut to fill the machine twice over, no piece shorter than 2048 elements;
+// more rows into pieces that a CTA's registers hold, as long as that gives no more than four rounds of CTAs:
+// a piece that takes several rounds of loads collects fewer candidates, but waits for each (32 x 4 rows of
+// 131072, 16-bit: 8 pieces 14.2 us, 3 pieces 15.4; 256 x 8 of 32003, f32: 3 pieces 63 us, one 56).
 int pieces_of(const apar_beam_config* c, int32_t n_seq) {
   const int64_t rows = (int64_t)n_seq * c->num_beams;
-  const int64_t held = kThreads * (c->logits_type == APAR_LOGITS_F32 ? Packs<float>::kHeld * Packs<float>::kPer
-                                                                     : Packs<__half>::kHeld * Packs<__half>::kPer);
-  const int64_t fit = (c->vocab + held - 1) / held;
-  int64_t p = std::min<int64_t>((2 * 148 + rows - 1) / rows, (c->vocab + 2047) / 2048);
-  p = std::min<int64_t>({std::max(p, fit), kMaxPieces, kMaxLists / c->num_beams});
-  return (int)std::max<int64_t>(1, p);
+  const bool f32 = c->logits_type == APAR_LOGITS_F32;
+  const int64_t held = kThreads * (f32 ? Packs<float>::kHeld * Packs<float>::kPer
+                                       : Packs<__half>::kHeld * Packs<__half>::kPer);
+  const int64_t round = 148 * (f32 ? Packs<float>::kCtas : Packs<__half>::kCtas);
+  const int64_t few = std::min<int64_t>((2 * 148 + rows - 1) / rows, (c->vocab + 2047) / 2048);
+  const int64_t fit = std::min<int64_t>((4 * round + rows - 1) / rows, (c->vocab + held - 1) / held);
+  return (int)std::min<int64_t>({std::max(few, fit), kMaxPieces, kMaxLists / c->num_beams});
 }
 
 bool valid(const apar_beam_config* c, int32_t n_seq) {
