@@ -127,6 +127,8 @@ struct apar_ctx {
   apar_stats last = {};
   std::vector<uint32_t> mark;          // per slot, duplicate detection
   uint32_t mark_epoch = 0;
+  std::vector<uint64_t> block_stretch;       // of apar_evict
+  uint32_t stretch_epoch = 0;
   // ---- staging
   Staging ring[kRing];
   size_t ring_bytes = 0;
@@ -1687,35 +1689,47 @@ apar_status apar_read_kv(apar_ctx* c, int32_t layer, int32_t n, const int32_t* t
   }
   const char* kp = (const char*)c->cfg.k_pool + (size_t)layer * c->layer_bytes;
   const char* vp = (const char*)c->cfg.v_pool + (size_t)layer * c->layer_bytes;
+  // Pieces of blocks: a few of them travel with the launch, more of them through the staging area.
+  ReadPieces few;
+  ReadPiece* list = few.p;
+  Staging* stg = nullptr;
   char* d_stage = c->ws(c->lay.stage);
-  const int64_t cap_rows = (int64_t)(c->lay.stage_cap / 4);
-  int64_t first_row = 0;
-  int i = 0;
-  int32_t done = 0;                     // rows of entry i already listed
-  while (first_row < rows) {
-    Staging* stg;
-    apar_status rc = acquire(c, &stg);
-    if (rc) return rc;
-    int32_t* list = (int32_t*)stg->host;
-    int64_t filled = 0;
-    while (i < n && filled < cap_rows) {
-      const int32_t* tab = c->row(slot_of(c, tid[i]));
-      for (; done < count[i] && filled < cap_rows; ++done) {
-        const int32_t pos = begin[i] + done;
-        list[filled++] = tab[pos / kBlock] * kBlock + pos % kBlock;
-      }
-      if (done < count[i]) break;
-      ++i;
-      done = 0;
+  const int cap = (int)std::min<size_t>(c->lay.stage_cap / sizeof(ReadPiece), 1 << 20);
+  int64_t out = 0;
+  int filled = 0;
+  auto flush = [&]() -> apar_status {
+    if (stg) {
+      apar_status rc = send(c, stg, d_stage, (size_t)filled * sizeof(ReadPiece), st);
+      if (rc) return rc;
     }
-    rc = send(c, stg, d_stage, (size_t)filled * 4, st);
-    if (rc) return rc;
-    APAR_CUDA(c, launch_read_rows(c->q4, kp, vp, k_out, v_out, (const int32_t*)d_stage, first_row,
-                                  (int)filled, c->cfg.num_kv_heads, st));
+    APAR_CUDA(c, launch_read_rows(c->q4, kp, vp, k_out, v_out, few, stg ? (const ReadPiece*)d_stage : nullptr,
+                                  filled, c->cfg.num_kv_heads, st));
     ++c->kernels_total;
-    first_row += filled;
+    stg = nullptr;
+    filled = 0;
+    return APAR_OK;
+  };
+  for (int i = 0; i < n; ++i) {
+    const int32_t* tab = c->row(slot_of(c, tid[i]));
+    for (int32_t pos = begin[i], end = begin[i] + count[i]; pos < end;) {
+      if (filled == ReadPieces::kMax && !stg) {
+        apar_status rc = acquire(c, &stg);
+        if (rc) return rc;
+        list = (ReadPiece*)stg->host;
+        memcpy(list, few.p, sizeof(few.p));
+      }
+      const int row = pos % kBlock, take = std::min(kBlock - row, end - pos);
+      list[filled++] = ReadPiece{tab[pos / kBlock], (int16_t)row, (int16_t)take, out};
+      pos += take;
+      out += take;
+      if (stg && filled == cap) {
+        apar_status rc = flush();
+        if (rc) return rc;
+        list = few.p;
+      }
+    }
   }
-  return APAR_OK;
+  return filled ? flush() : APAR_OK;
 }
 
 apar_status apar_reorder(apar_ctx* c, int32_t n, const int32_t* tid, const int32_t* source_tid,
@@ -1825,13 +1839,18 @@ apar_status apar_reorder(apar_ctx* c, int32_t n, const int32_t* tid, const int32
   return APAR_ERR_INVALID_ARG;
 }
 
+static bool weights_fit(const apar_config* cfg) {        // (layers x kv heads: a dimension of a grid)
+  return (int64_t)std::max(1, cfg->num_layers) * cfg->num_kv_heads <= 65535;
+}
+
 size_t apar_weights_bytes(const apar_config* cfg) {
-  return supported(cfg) ? make_weights_layout(cfg).total : 0;
+  return supported(cfg) && weights_fit(cfg) ? make_weights_layout(cfg).total : 0;
 }
 
 apar_status apar_attach_weights(apar_ctx* c, void* memory, size_t bytes) {
   if (!c || ((uintptr_t)memory & 255)) return APAR_ERR_INVALID_ARG;
   if (c->host_only || c->q4) return APAR_ERR_UNSUPPORTED;
+  if (!weights_fit(&c->cfg)) return APAR_ERR_UNSUPPORTED;
   c->wlay = make_weights_layout(&c->cfg);
   if (memory && bytes < c->wlay.total) return APAR_ERR_WORKSPACE_TOO_SMALL;
   c->weights = (char*)memory;
@@ -2007,14 +2026,20 @@ apar_status apar_evict(apar_ctx* c, int32_t n, const int32_t* tid, const int32_t
   // Stretches: threads that list the same blocks share one.
   struct Stretch { int32_t first, members, in_place, new_blocks; };
   std::vector<Stretch> st_list;
-  std::vector<int32_t> stretch_of(n, -1), owner;         // owner: by block, 1 + stretch
+  std::vector<int32_t> stretch_of(n, -1);
   auto blocks_of = [](int32_t rows) { return (rows + kBlock - 1) / kBlock; };
-  owner.assign(c->cfg.num_blocks, 0);
+  // by block, the call that looked at it last and 1 + the stretch that it is of
+  if (c->block_stretch.empty()) c->block_stretch.resize(c->cfg.num_blocks, 0);
+  ++c->stretch_epoch;
+  auto owner = [&](int32_t block) -> int32_t {
+    const uint64_t x = c->block_stretch[block];
+    return x >> 32 == c->stretch_epoch ? (int32_t)(uint32_t)x : 0;
+  };
   for (int i = 0; i < n; ++i) {
     if (keep[i] == end[i] - begin[i]) continue;          // nothing goes
     const int32_t* tab = c->row(slot_of(c, tid[i]));
     const int b0 = begin[i] / kBlock, b1 = blocks_of(end[i]);
-    const int32_t o = owner[tab[b0]];
+    const int32_t o = owner(tab[b0]);
     if (o) {
       const int f = st_list[o - 1].first;
       const int32_t* ftab = c->row(slot_of(c, tid[f]));
@@ -2025,9 +2050,9 @@ apar_status apar_evict(apar_ctx* c, int32_t n, const int32_t* tid, const int32_t
       stretch_of[i] = o - 1;
       continue;
     }
-    for (int b = b0; b < b1; ++b) {
-      if (owner[tab[b]]) return APAR_ERR_INVALID_ARG;    // overlaps another stretch in part
-      owner[tab[b]] = (int32_t)st_list.size() + 1;
+    for (int b = b0; b < b1 && n > 1; ++b) {             // (a thread's own blocks differ)
+      if (owner(tab[b])) return APAR_ERR_INVALID_ARG;    // overlaps another stretch in part
+      c->block_stretch[tab[b]] = (uint64_t)c->stretch_epoch << 32 | (st_list.size() + 1);
     }
     stretch_of[i] = (int32_t)st_list.size();
     st_list.push_back(Stretch{i, 1, 1, 0});
@@ -2036,8 +2061,8 @@ apar_status apar_evict(apar_ctx* c, int32_t n, const int32_t* tid, const int32_t
   for (Stretch& x : st_list) {
     const int f = x.first;
     const int32_t* tab = c->row(slot_of(c, tid[f]));
-    for (int b = begin[f] / kBlock; b < blocks_of(end[f]); ++b)
-      if (c->refcnt[tab[b]] != x.members) x.in_place = 0;
+    for (int b = begin[f] / kBlock; b < blocks_of(end[f]) && x.in_place; ++b)
+      x.in_place = c->refcnt[tab[b]] == x.members;
     if (x.members > 1 && keep[f] % kBlock) return APAR_ERR_INVALID_ARG;   // a partial block is one thread's
     if (!x.in_place) {
       x.new_blocks = blocks_of(keep[f]);
@@ -2049,8 +2074,10 @@ apar_status apar_evict(apar_ctx* c, int32_t n, const int32_t* tid, const int32_t
       return APAR_ERR_INVALID_ARG;
   if (st_list.empty()) return APAR_OK;
   if (need > (int64_t)c->free_stack.size()) return APAR_ERR_NO_BLOCKS;
+  // (few stretches and new blocks travel with the launches, more of them through the staging area)
+  const bool few_go = st_list.size() <= EvictFew::kEntries && need <= EvictFew::kBlocks;
   const size_t b_entries = st_list.size() * sizeof(EvictEntry);
-  if (b_entries + (size_t)need * 4 > c->lay.stage_cap) return APAR_ERR_WORKSPACE_TOO_SMALL;
+  if (!few_go && b_entries + (size_t)need * 4 > c->lay.stage_cap) return APAR_ERR_WORKSPACE_TOO_SMALL;
   std::vector<int32_t> slots;
   for (const Stretch& x : st_list) slots.push_back(slot_of(c, tid[x.first]));
   apar_status rc = APAR_OK;
@@ -2058,7 +2085,7 @@ apar_status apar_evict(apar_ctx* c, int32_t n, const int32_t* tid, const int32_t
   if (!c->host_only) {
     rc = refuse_capture(c, st);
     if (rc == APAR_OK) rc = sync_device_tables(c, slots.data(), (int)slots.size(), st);
-    if (rc == APAR_OK) rc = acquire(c, &stg);
+    if (rc == APAR_OK && !few_go) rc = acquire(c, &stg);
     if (rc) return rc;
   }
   std::vector<EvictEntry> entries;
@@ -2112,14 +2139,13 @@ apar_status apar_evict(apar_ctx* c, int32_t n, const int32_t* tid, const int32_t
       rs.resize(w);
     }
     const int32_t nb_old = t.n_blocks;
-    std::vector<int32_t> gone(tab + (x.in_place ? b0 + kb : b0), tab + b1);
+    for (int b = x.in_place ? b0 + kb : b0; b < b1; ++b)
+      if (--c->refcnt[tab[b]] == 0) c->free_stack.push_back(tab[b]);
     if (!x.in_place)
       for (int b = 0; b < kb; ++b) tab[b0 + b] = dst[dst_of[stretch_of[i]] + b];
     for (int b = b1; b < nb_old; ++b) tab[b - b1 + b0 + kb] = tab[b];
     if (!x.in_place && !first)
       for (int b = 0; b < kb; ++b) ++c->refcnt[tab[b0 + b]];
-    for (int32_t b : gone)
-      if (--c->refcnt[b] == 0) c->free_stack.push_back(b);
     t.n_blocks = nb_old - (b1 - b0) + kb;
     t.len -= end[i] - begin[i] - keep[i];
     t.synced = std::min(t.synced, b0);
@@ -2144,14 +2170,22 @@ apar_status apar_evict(apar_ctx* c, int32_t n, const int32_t* tid, const int32_t
   c->last_append_rows = -1;
   if (entries.empty() || c->host_only) return APAR_OK;
   const size_t b_used = entries.size() * sizeof(EvictEntry);
-  memcpy(stg->host, entries.data(), b_used);
-  memcpy(stg->host + b_used, dst.data(), dst.size() * 4);
-  char* d_stage = c->ws(c->lay.stage);
-  rc = send(c, stg, d_stage, b_used + dst.size() * 4, st);
-  if (rc) return rc;
   EvictArgs a;
-  a.entries = (const EvictEntry*)d_stage;
-  a.dst_blocks = (const int32_t*)(d_stage + b_used);
+  EvictFew few;
+  a.entries = nullptr;
+  a.dst_blocks = nullptr;
+  if (few_go) {
+    memcpy(few.entries, entries.data(), b_used);
+    if (!dst.empty()) memcpy(few.dst_blocks, dst.data(), dst.size() * 4);
+  } else {
+    memcpy(stg->host, entries.data(), b_used);
+    if (!dst.empty()) memcpy(stg->host + b_used, dst.data(), dst.size() * 4);
+    char* d_stage = c->ws(c->lay.stage);
+    rc = send(c, stg, d_stage, b_used + dst.size() * 4, st);
+    if (rc) return rc;
+    a.entries = (const EvictEntry*)d_stage;
+    a.dst_blocks = (const int32_t*)(d_stage + b_used);
+  }
   a.d_tables = (const int32_t*)c->ws(c->lay.tables);
   a.table_stride = c->cfg.max_blocks_per_thread;
   a.num_kv_heads = c->cfg.num_kv_heads;
@@ -2162,7 +2196,7 @@ apar_status apar_evict(apar_ctx* c, int32_t n, const int32_t* tid, const int32_t
   a.layer_floats = c->layer_weights();
   a.moves = (int2*)(c->weights + c->wlay.moves);
   a.counts = (int32_t*)(c->weights + c->wlay.counts);
-  APAR_CUDA(c, launch_evict(a, (int)entries.size(), c->num_layers, max_len, max_rows, st));
+  APAR_CUDA(c, launch_evict(a, few, (int)entries.size(), c->num_layers, max_len, max_rows, st));
   c->kernels_total += 2;
   return APAR_OK;
 } catch (...) {               // (the host's memory)

@@ -229,9 +229,19 @@ cudaError_t launch_q4_cow_copy(void* k_pool, void* v_pool, const CowCopy* d_copi
 cudaError_t launch_q4_row_moves(void* k_pool, void* v_pool, const RowMove* d_moves,
                                 const int32_t* d_group_begin, int n_groups, int num_kv_heads,
                                 cudaStream_t st);
-// Rows d_slots[0..n_rows) of a pool as bf16, to rows first_row.. of k_out and v_out.
+// Rows row .. row + count - 1 of a block, read to rows out .. of the output.
+struct ReadPiece {
+  int32_t block;
+  int16_t row, count;
+  int64_t out;
+};
+struct ReadPieces {              // (as a kernel's argument)
+  static constexpr int kMax = 128;
+  ReadPiece p[kMax];
+};
+// n pieces of a pool as bf16; at `many` (device), or where that is NULL the first n of `few`.
 cudaError_t launch_read_rows(bool q4, const void* k_pool, const void* v_pool, void* k_out,
-                             void* v_out, const int32_t* d_slots, int64_t first_row, int n_rows,
+                             void* v_out, const ReadPieces& few, const ReadPiece* many, int n,
                              int num_kv_heads, cudaStream_t st);
 // The items of a plan made with mma_min_rows = 1, reordered by width: n_wide with more than kQ4Rows
 // rows (tcgen05 kernel), n_mid, n_narrow with at most kQ4NarrowRows (both warp-stream kernel).
@@ -312,8 +322,13 @@ struct EvictEntry {
   int32_t dst_begin, list_rows, pad;
   int64_t list_begin;
 };
+struct EvictFew {                // (as a kernel's argument)
+  static constexpr int kEntries = 8, kBlocks = 640;
+  EvictEntry entries[kEntries];
+  int32_t dst_blocks[kBlocks];
+};
 struct EvictArgs {
-  const EvictEntry* entries;
+  const EvictEntry* entries;     // NULL: entries and blocks are those of an EvictFew
   const int32_t* dst_blocks;
   const int32_t* d_tables;
   int32_t table_stride, num_kv_heads;
@@ -343,8 +358,8 @@ cudaError_t launch_weights_read(const float* w, const int32_t* d_tables, int tab
                                 const RowRanges& few, const RowRange* many, int n, int max_count,
                                 int num_kv_heads, float* out, cudaStream_t st);
 // max_len: rows of the longest stretch; max_rows: rows the entry that moves most may move.
-cudaError_t launch_evict(const EvictArgs& a, int n, int num_layers, int max_len, int max_rows,
-                         cudaStream_t st);
+cudaError_t launch_evict(const EvictArgs& a, const EvictFew& few, int n, int num_layers, int max_len,
+                         int max_rows, cudaStream_t st);
 
 // ---- planner (planner.cpp) ----
 // A run of consecutive table positions whose blocks are held by the same set of threads

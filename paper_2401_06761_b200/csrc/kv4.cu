@@ -194,31 +194,31 @@ __global__ void __launch_bounds__(256) q4_row_move_kernel(uint8_t* __restrict__ 
 }
 
 // ------------------------------------------------------------------ rows read back as bf16
-// One thread per sixteen dims of a row; blockIdx.y selects K or V.  A 4-bit row reads as
-// bf16(lo + s * c), the sum taken in 32 bits and rounded once more to the output's type.
+// One thread per sixteen dims of a row; blockIdx.y selects K or V, blockIdx.z which 32 of a piece's
+// (row, head) pairs.  A 4-bit row reads as bf16(lo + s * c), the sum taken in 32 bits and rounded once
+// more to the output's type.
 template <bool kQ4>
 __global__ void __launch_bounds__(256) read_rows_kernel(const uint8_t* __restrict__ k_pool,
                                                         const uint8_t* __restrict__ v_pool,
                                                         uint4* __restrict__ k_out,
                                                         uint4* __restrict__ v_out,
-                                                        const int32_t* __restrict__ slots,
-                                                        long long first_row, int n_rows,
+                                                        const __grid_constant__ ReadPieces few,
+                                                        const ReadPiece* __restrict__ many,
                                                         int num_kv_heads) {
-  const uint32_t rh = blockIdx.x * (blockDim.x / 8) + (threadIdx.x >> 3);   // (row, head) < 2^31
-  if (rh >= (uint32_t)n_rows * (uint32_t)num_kv_heads) return;
+  const ReadPiece p = many ? many[blockIdx.x] : few.p[blockIdx.x];
+  const int rh = blockIdx.z * (blockDim.x / 8) + (threadIdx.x >> 3);
+  if (rh >= p.count * num_kv_heads) return;
   const int c = threadIdx.x & 7;
-  const int r = (int)(rh / (uint32_t)num_kv_heads);
-  const int h = (int)(rh - (uint32_t)r * (uint32_t)num_kv_heads);
-  const int slot = slots[r];
-  const size_t tile = (size_t)(slot >> 4) * num_kv_heads + h;
+  const int r = rh / num_kv_heads, h = rh - r * num_kv_heads, row = p.row + r;
+  const size_t tile = (size_t)p.block * num_kv_heads + h;
   const uint8_t* pool = blockIdx.y ? v_pool : k_pool;
   uint4 out[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     if (kQ4) {
       float f[8];
-      if (blockIdx.y) q4_load8_v(pool + tile * kQ4TileBytes, slot & 15, 2 * c + i, f);
-      else q4_load8_k(pool + tile * kQ4TileBytes, slot & 15, 2 * c + i, f);
+      if (blockIdx.y) q4_load8_v(pool + tile * kQ4TileBytes, row, 2 * c + i, f);
+      else q4_load8_k(pool + tile * kQ4TileBytes, row, 2 * c + i, f);
       uint32_t w[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -227,10 +227,10 @@ __global__ void __launch_bounds__(256) read_rows_kernel(const uint8_t* __restric
       }
       out[i] = make_uint4(w[0], w[1], w[2], w[3]);
     } else {
-      out[i] = ((const uint4*)pool)[(tile * kBlock + (slot & 15)) * 16 + 2 * c + i];
+      out[i] = ((const uint4*)pool)[(tile * kBlock + row) * 16 + 2 * c + i];
     }
   }
-  uint4* dst = (blockIdx.y ? v_out : k_out) + (first_row * num_kv_heads + rh) * 16 + 2 * c;
+  uint4* dst = (blockIdx.y ? v_out : k_out) + (p.out * num_kv_heads + rh) * 16 + 2 * c;
   dst[0] = out[0];
   dst[1] = out[1];
 }
@@ -266,14 +266,13 @@ cudaError_t launch_q4_row_moves(void* k_pool, void* v_pool, const RowMove* d_mov
 }
 
 cudaError_t launch_read_rows(bool q4, const void* k_pool, const void* v_pool, void* k_out,
-                             void* v_out, const int32_t* d_slots, int64_t first_row, int n_rows,
+                             void* v_out, const ReadPieces& few, const ReadPiece* many, int n,
                              int num_kv_heads, cudaStream_t st) {
-  if (n_rows <= 0) return cudaSuccess;
-  const long long total = (long long)n_rows * num_kv_heads * 8;
-  const dim3 grid((unsigned)((total + 255) / 256), 2);
+  if (n <= 0) return cudaSuccess;
+  const dim3 grid(n, 2, (kBlock * num_kv_heads + 31) / 32);
   auto kernel = q4 ? read_rows_kernel<true> : read_rows_kernel<false>;
   kernel<<<grid, 256, 0, st>>>((const uint8_t*)k_pool, (const uint8_t*)v_pool, (uint4*)k_out,
-                               (uint4*)v_out, d_slots, (long long)first_row, n_rows, num_kv_heads);
+                               (uint4*)v_out, few, many, num_kv_heads);
   return cudaGetLastError();
 }
 

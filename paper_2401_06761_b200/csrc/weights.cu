@@ -312,12 +312,13 @@ __device__ int ranks_of(PickShared<kThreads, kKeys>& sh, int kind, int used, uin
 
 template <int kThreads, int kKeys>
 __global__ void __launch_bounds__(kThreads, kThreads <= 256 ? 6 : 1)
-evict_pick_kernel(const EvictArgs a, int n_cta) {
+evict_pick_kernel(const EvictArgs a, const __grid_constant__ EvictFew few, int n_cta) {
   constexpr int kWarps = kThreads / 32, kPerThread = kBins / kThreads;
   __shared__ PickShared<kThreads, kKeys> sh;
+  pdl_launch_dependents();
   const uint32_t me = n_cta > 1 ? cluster_rank() : 0;
   const int entry = blockIdx.x / n_cta;
-  const EvictEntry en = a.entries[entry];
+  const EvictEntry en = a.entries ? a.entries[entry] : few.entries[entry];
   const int heads = a.num_kv_heads, lh = blockIdx.y, l = lh / heads, h = lh % heads;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const float* w = a.weights + (size_t)l * a.layer_floats;
@@ -440,11 +441,13 @@ evict_pick_kernel(const EvictArgs a, int n_cta) {
 // The same for stretches that the registers of a cluster do not hold: one CTA, eight bits at a time,
 // the weights read again for every round and for the ranks.
 constexpr int kPickThreads = 512;
-__global__ void __launch_bounds__(kPickThreads) evict_pick_long_kernel(const EvictArgs a) {
+__global__ void __launch_bounds__(kPickThreads) evict_pick_long_kernel(const EvictArgs a,
+                                                                       const __grid_constant__ EvictFew few) {
   __shared__ uint32_t hist[256];
   __shared__ uint32_t s_prefix, s_left;
   __shared__ int s_scan[3][kPickThreads / 32];
-  const EvictEntry en = a.entries[blockIdx.x];
+  pdl_launch_dependents();
+  const EvictEntry en = a.entries ? a.entries[blockIdx.x] : few.entries[blockIdx.x];
   const int heads = a.num_kv_heads, lh = blockIdx.y, l = lh / heads, h = lh % heads;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const float* w = a.weights + (size_t)l * a.layer_floats;
@@ -554,26 +557,43 @@ __global__ void __launch_bounds__(kPickThreads) evict_pick_long_kernel(const Evi
 }
 
 // ------------------------------------------------------------------ eviction: the rows move
-// Half a warp per row: 256 bytes of K, 256 of V, and the weight.  Sources lie behind `keep` and
-// destinations before it, or in other blocks: no move reads what another writes.
-__global__ void __launch_bounds__(256) evict_move_kernel(const EvictArgs a) {
-  const EvictEntry en = a.entries[blockIdx.z];
+// Half a warp per row, four rows at a time: 256 bytes of K, 256 of V, and the weight.  Sources lie behind
+// `keep` and destinations before it, or in other blocks: no move reads what another writes.
+constexpr int kMoveRows = 4;
+__global__ void __launch_bounds__(256) evict_move_kernel(const EvictArgs a, const __grid_constant__ EvictFew few) {
+  const EvictEntry en = a.entries ? a.entries[blockIdx.z] : few.entries[blockIdx.z];
   const int heads = a.num_kv_heads, lh = blockIdx.y, l = lh / heads, h = lh % heads;
-  const int n = a.counts[(size_t)blockIdx.z * gridDim.y + lh], c = threadIdx.x & 15;
   const int2* list = a.moves + en.list_begin + (size_t)lh * en.list_rows;
   const int32_t* from = a.d_tables + (size_t)en.table_row * a.table_stride + en.begin / kBlock;
-  const int32_t* to = en.in_place ? from : a.dst_blocks + en.dst_begin;
+  const int32_t* to = en.in_place ? from : (a.entries ? a.dst_blocks : few.dst_blocks) + en.dst_begin;
   uint4* k = (uint4*)((char*)a.k_pool + (size_t)l * a.layer_bytes);
   uint4* v = (uint4*)((char*)a.v_pool + (size_t)l * a.layer_bytes);
   float* w = a.weights + (size_t)l * a.layer_floats;
-  for (int m = blockIdx.x * 16 + (threadIdx.x >> 4); m < n; m += gridDim.x * 16) {
-    const int2 mv = list[m];
-    const size_t src = ((size_t)from[mv.x >> 4] * heads + h) * kBlock + (mv.x & 15);
-    const size_t dst = ((size_t)to[mv.y >> 4] * heads + h) * kBlock + (mv.y & 15);
-    const uint4 x = k[src * 16 + c], y = v[src * 16 + c];
-    k[dst * 16 + c] = x;
-    v[dst * 16 + c] = y;
-    if (c == 0) w[dst] = w[src];
+  pdl_wait();                                  // (the list is written)
+  const int n = a.counts[(size_t)blockIdx.z * gridDim.y + lh], c = threadIdx.x & 15;
+  for (int m0 = blockIdx.x * 16 * kMoveRows + (threadIdx.x >> 4); m0 < n; m0 += gridDim.x * 16 * kMoveRows) {
+    size_t src[kMoveRows], dst[kMoveRows];
+    uint4 x[kMoveRows], y[kMoveRows];
+    float z[kMoveRows];
+#pragma unroll
+    for (int r = 0; r < kMoveRows; ++r) {
+      const int2 mv = list[min(m0 + 16 * r, n - 1)];
+      src[r] = ((size_t)from[mv.x >> 4] * heads + h) * kBlock + (mv.x & 15);
+      dst[r] = ((size_t)to[mv.y >> 4] * heads + h) * kBlock + (mv.y & 15);
+    }
+#pragma unroll
+    for (int r = 0; r < kMoveRows; ++r) {
+      x[r] = k[src[r] * 16 + c];
+      y[r] = v[src[r] * 16 + c];
+      if (c == 0) z[r] = w[src[r]];
+    }
+#pragma unroll
+    for (int r = 0; r < kMoveRows; ++r) {
+      if (m0 + 16 * r >= n) break;
+      k[dst[r] * 16 + c] = x[r];
+      v[dst[r] * 16 + c] = y[r];
+      if (c == 0) w[dst[r]] = z[r];
+    }
   }
 }
 
@@ -625,13 +645,14 @@ cudaError_t launch_weights_read(const float* w, const int32_t* d_tables, int tab
   return cudaSuccess;
 }
 
-cudaError_t launch_evict(const EvictArgs& a, int n, int num_layers, int max_len, int max_rows,
-                         cudaStream_t st) {
+cudaError_t launch_evict(const EvictArgs& a, const EvictFew& few, int n, int num_layers, int max_len,
+                         int max_rows, cudaStream_t st) {
   if (n <= 0) return cudaSuccess;
   const int lh = num_layers * a.num_kv_heads;
   cudaError_t e;
   if (max_len <= kPickFew * kPickFewKeys) {
-    e = launch_kernel(evict_pick_kernel<kPickFew, kPickFewKeys>, dim3(n, lh), dim3(kPickFew), 0, st, false, a, 1);
+    e = launch_kernel(evict_pick_kernel<kPickFew, kPickFewKeys>, dim3(n, lh), dim3(kPickFew), 0, st, false, a,
+                      few, 1);
   } else if (max_len <= kPickCluster * kPickRows) {
     // CTAs per stretch: as many as it takes to hold the longest stretch in registers, or to give a
     // thread no more than four rows
@@ -647,18 +668,18 @@ cudaError_t launch_evict(const EvictArgs& a, int n, int num_layers, int max_len,
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = n_cta > 1 ? 1 : 0;
-    e = cudaLaunchKernelEx(&cfg, evict_pick_kernel<kPickMany, kPickManyKeys>, a, n_cta);
+    e = cudaLaunchKernelEx(&cfg, evict_pick_kernel<kPickMany, kPickManyKeys>, a, few, n_cta);
   } else {
-    e = launch_kernel(evict_pick_long_kernel, dim3(n, lh), dim3(kPickThreads), 0, st, false, a);
+    e = launch_kernel(evict_pick_long_kernel, dim3(n, lh), dim3(kPickThreads), 0, st, false, a, few);
   }
   if (e != cudaSuccess || max_rows <= 0) return e;
-  const unsigned grid = (unsigned)std::min((max_rows + 15) / 16, 1024);
+  const unsigned grid = (unsigned)std::min((max_rows + 16 * kMoveRows - 1) / (16 * kMoveRows), 1024);
   EvictArgs part = a;
   for (int i = 0; i < n && e == cudaSuccess; i += 65535) {   // (the grid's limit)
-    part.entries = a.entries + i;
+    if (a.entries) part.entries = a.entries + i;
     part.counts = a.counts + (size_t)i * lh;
-    e = launch_kernel(evict_move_kernel, dim3(grid, lh, std::min(n - i, 65535)), dim3(256), 0, st, false,
-                      part);
+    e = launch_kernel(evict_move_kernel, dim3(grid, lh, std::min(n - i, 65535)), dim3(256), 0, st, i == 0,
+                      part, few);
   }
   return e;
 }

@@ -101,10 +101,10 @@ class BeamSelect:
         nbytes = self._bytes.get((n, logits.dtype))
         if nbytes is None:
             nbytes = self._bytes[n, logits.dtype] = B.apar_beam_workspace_bytes(cfg, n)
-        held = torch.empty(nbytes, dtype=torch.uint8, device=logits.device)
-        best = torch.empty((n, self.select), dtype=torch.float32, device=logits.device)
-        beams = torch.empty((n, self.select), dtype=torch.int32, device=logits.device)
-        tokens = torch.empty_like(beams)
+        held = scores.new_empty((nbytes + 3) // 4)
+        best = scores.new_empty((n, self.select))
+        beams = best.new_empty((n, self.select), dtype=torch.int32)
+        tokens = beams.new_empty((n, self.select))
         B.apar_beam_select(cfg, n, logits.data_ptr(), by_seq, by_beam, scores.data_ptr(),
                            0 if finished is None else finished.data_ptr(), best.data_ptr(),
                            beams.data_ptr(), tokens.data_ptr(), held.data_ptr(), nbytes,
@@ -274,14 +274,20 @@ class PagedSession:
                      self._stream())
         return out
 
+    @staticmethod
+    def _counts(count):
+        """Counts as the library takes them, and their total (negative ones are the library's to refuse)."""
+        count = B.int32_array(count)
+        buf, n = count
+        rows = sum(buf[:n]) if n <= 64 else int(np.frombuffer(buf, np.int32, n).sum(dtype=np.int64))
+        return count, max(0, rows)
+
     def read_kv(self, tids, begin, count, layer: int = 0):
         """Rows begin[i] .. begin[i] + count[i] - 1 of each thread's chain, as bf16 (k, v)."""
-        count = B.int32_array(count)
-        # (negative counts are the library's to refuse)
-        rows = max(0, int(np.frombuffer(count[0], np.int32, count[1]).sum(dtype=np.int64)))
-        shape = (rows, self.shape.num_kv_heads, self.shape.head_dim)
-        k = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
-        v = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+        count, rows = self._counts(count)
+        k = self.workspace.new_empty((rows, self.shape.num_kv_heads, self.shape.head_dim),
+                                     dtype=torch.bfloat16)
+        v = torch.empty_like(k)
         B.apar_read_kv(self.ctx, layer, tids, begin, count, k.data_ptr(), v.data_ptr(),
                        self._stream())
         return k, v
@@ -312,14 +318,8 @@ class PagedSession:
 
     def read_weights(self, tids, begin, count, layer: int = 0):
         """Weights [rows][kv heads] of rows begin[i] .. begin[i] + count[i] - 1 of each chain."""
-        if not isinstance(count, list):
-            count = B.int32_array(count)
-            rows = int(np.frombuffer(count[0], np.int32, count[1]).sum(dtype=np.int64))
-        else:
-            rows = int(sum(count))
-        # (negative counts are the library's to refuse)
-        out = torch.empty((max(0, rows), self.shape.num_kv_heads), dtype=torch.float32,
-                          device=self.device)
+        count, rows = self._counts(count)
+        out = self.workspace.new_empty((rows, self.shape.num_kv_heads), dtype=torch.float32)
         B.apar_read_weights(self.ctx, layer, tids, begin, count, out.data_ptr(), self._stream())
         return out
 
