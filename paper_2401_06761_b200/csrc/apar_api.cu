@@ -24,7 +24,6 @@ constexpr int kFewQueries = 768;      // up to here single-row items go to the w
 constexpr int kSlotsPerThread = 6;    // partial-result rows provisioned per live thread
 constexpr int kMinSlots = 1184;       // and never fewer than this (8 per SM of a 148-SM part), so
                                       // that a few very long threads still spread over the machine
-constexpr int kKeyUnitsPerSm = 40;    // units an SM gets of a call for accumulated weights
 constexpr int kSlotMapRows = 262144;  // new-row slots of the last append kept for other layers
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
@@ -724,17 +723,43 @@ apar_status upload(apar_ctx* c, const void* src, size_t bytes, char* dst, cudaSt
   return APAR_OK;
 }
 
-// Cuts the runs into units of at most `chunk` keys, longest first (of a decode step: the widest class
-// first), and sends the plan.
-apar_status send_key_plan(apar_ctx* c, const std::vector<KeyRun>& runs, const std::vector<KeyUser>& users,
-                          int chunk, bool by_class, KeyPlan* plan, cudaStream_t st) {
-  std::vector<KeyUnit> unit_list, *units = &unit_list;
+// Keys of a class's units: the least for which there is a unit for every warp of the machine, but not more,
+// or where 1024 keys to a unit leave more than that, for every warp as many.  (64 x 3 forks of 2400 keys, 32
+// heads on 8, units for 10, 12, 20 and 40 warps of an SM, which has 12: 68, 93, 72 and 78 us.)
+int key_chunk(const apar_ctx* c, const std::vector<KeyRun>& runs, int cls) {
+  constexpr int kMost = 1024;
+  int64_t keys = 0, n = 0;
   for (const KeyRun& r : runs)
+    if (key_class(r.n_users * c->shape.group) == cls) keys += r.tok_end - r.tok_begin, ++n;
+  const int64_t heads = c->cfg.num_kv_heads, warps = (int64_t)c->num_sms * kKeyWarpsPerSm[cls];
+  const int64_t rounds = std::max((keys * heads + warps * kMost - 1) / (warps * kMost), (n * heads + warps - 1) / warps);
+  if (rounds == 0) return kMost;
+  int64_t chunk = std::max<int64_t>(64, (keys * heads / (warps * rounds) + 15) / 16 * 16);
+  for (; chunk < kMost; chunk += std::max<int64_t>(16, chunk / 256 * 16)) {
+    int64_t units = 0;
+    for (const KeyRun& r : runs)
+      if (key_class(r.n_users * c->shape.group) == cls) units += (r.tok_end - r.tok_begin + chunk - 1) / chunk;
+    if (units * heads <= warps * rounds) break;
+  }
+  return (int)std::min<int64_t>(chunk, kMost);
+}
+
+// Cuts the runs into units of at most `chunk` keys (of a decode step: by class), longest first (of a decode
+// step: the widest class first), and sends the plan.
+apar_status send_key_plan(apar_ctx* c, const std::vector<KeyRun>& runs, const std::vector<KeyUser>& users,
+                          const int (&chunks)[3], bool by_class, KeyPlan* plan, cudaStream_t st) {
+  std::vector<KeyUnit> unit_list, *units = &unit_list;
+  for (const KeyRun& r : runs) {
+    // (even parts: a short rest would be a unit like the others, with little to do)
+    const int most = chunks[by_class ? key_class(r.n_users * c->shape.group) : 0];
+    const int len = r.tok_end - r.tok_begin, parts = (len + most - 1) / most;
+    const int chunk = by_class ? ((len + parts - 1) / parts + kBlock - 1) / kBlock * kBlock : most;
     for (int t = r.tok_begin; t < r.tok_end; t += chunk) {
       const bool last = t + chunk >= r.tok_end;
       units->push_back(KeyUnit{r.table_row, t, last && r.open ? -(r.tok_end - t) - 1 : std::min(r.tok_end, t + chunk),
                                r.user_begin, r.n_users, 0, {0, 0}});
     }
+  }
   const size_t b_units = units->size() * sizeof(KeyUnit), b_users = users.size() * sizeof(KeyUser);
   if (sizeof(KeyUnit) + b_units + b_users > c->wlay.plan_bytes) return APAR_ERR_WORKSPACE_TOO_SMALL;
   // (queries that see the unit's keys, or all but a few of them)
@@ -1887,12 +1912,9 @@ apar_status apar_add_weights(apar_ctx* c, int32_t layer, const void* q, const fl
     std::vector<KeyRun> runs;
     std::vector<KeyUser> users;
     if (!c->planner.key_runs(qs.data(), (int)qs.size(), &runs, &users)) return APAR_ERR_INVALID_ARG;
-    // units of even length, some three to a warp of the machine where there is that much
-    int64_t keys = 0;
-    for (const KeyRun& r : runs) keys += r.tok_end - r.tok_begin;
-    const int64_t share = keys * c->cfg.num_kv_heads / ((int64_t)c->num_sms * kKeyUnitsPerSm);
-    const int64_t chunk = std::min<int64_t>(1024, std::max<int64_t>(64, (share + 15) / 16 * 16));
-    rc = send_key_plan(c, runs, users, (int)chunk, true, &c->key_plan, st);
+    int chunks[3];
+    for (int x = 0; x < 3; ++x) chunks[x] = key_chunk(c, runs, x);
+    rc = send_key_plan(c, runs, users, chunks, true, &c->key_plan, st);
     if (rc) return rc;
     c->key_plan_valid = true;
   }
@@ -1940,7 +1962,7 @@ apar_status apar_add_weights_prefill(apar_ctx* c, int32_t layer, int32_t n, cons
   std::vector<KeyUser> users;
   KeyPlan plan;
   if (!c->planner.key_runs(qs.data(), n, &runs, &users)) return APAR_ERR_INVALID_ARG;
-  rc = send_key_plan(c, runs, users, kPromptUnit, false, &plan, st);
+  rc = send_key_plan(c, runs, users, {kPromptUnit, 0, 0}, false, &plan, st);
   if (rc == APAR_OK) rc = sync_device_tables(c, slots.data(), n, st);
   if (rc) return rc;
   APAR_CUDA(c, launch_prompt_weights(key_args(c, c->wlay.prompt_plan, layer, q, lse, sm_scale, replace),

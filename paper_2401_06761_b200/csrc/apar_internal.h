@@ -347,6 +347,7 @@ cudaError_t launch_weights_move(float* w, size_t layer_floats, int num_layers, c
 // n_units: of the plan as the host knows it, for the size of the grids.  all: launch all classes, as a
 // captured call has to that may be replayed with another plan.
 inline int key_class(int rows) { return rows <= 8 ? 0 : rows <= 16 ? 1 : 2; }
+constexpr int kKeyWarpsPerSm[3] = {16, 12, 12};
 cudaError_t launch_key_weights(const KeyArgs& a, const int32_t (&n_units)[3], bool all, cudaStream_t st);
 // Units of at most 256 keys, closed; a user is a run of queries, the first at position lim.  tm_q as in
 // launch_attention_prefill.

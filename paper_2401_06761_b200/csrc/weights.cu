@@ -54,9 +54,12 @@ __global__ void __launch_bounds__(64) weights_move_kernel(float* __restrict__ w,
 // comes straight from memory into registers.
 // K is read once for up to 8 * NT rows, whose queries stay in registers; units of more than 32 go over their
 // keys again, in the L2 cache.  Units of up to 8, 16 and more rows have a launch each (in one kernel
-// the three would share the widest one's registers); a launch may start before the one before it is done.
-// kAhead blocks of keys are on their way while one is worked on: it takes some 48 KB an SM in flight to
-// keep HBM busy.
+// the three share the widest one's registers; with one of 8 rows, K is read again for every 8: 64 prompts
+// of 2400 keys and 3 forks each, 32 heads on 8, 117 us, now 68); a launch may start before the one before
+// it is done.  kAhead blocks of keys are on their way while one is worked on: it takes some 48 KB an SM in
+// flight to keep HBM busy.
+// Bound by HBM: those 64 x 2400 keys are 315 MB, 4.6 TB/s; 256 threads with 2400 keys of their own are 1.26 GB
+// and take 215 us, 5.8 TB/s.
 __device__ __forceinline__ uint4 ld_k(const uint4* p) {
   uint4 v;
   asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
@@ -224,14 +227,19 @@ __global__ void __launch_bounds__(256) weights_read_kernel(const float* __restri
 // found eleven bits at a time (three rounds): every CTA counts its part in shared memory and reads the
 // others' counts there.  Rows above it are kept, and of the rows equal to it the first few.  Ranks (which
 // of the equal rows, which of the rows that move, which of the places they move to) come from counts per
-// warp and sixteen rows of a thread, added up once over the CTA and once over the cluster.
+// warp and row of a thread, added up once over the CTA and once over the cluster.
+// Bound by its steps one after the other, some 20 barriers: 32 x 8 stretches of 2048 rows (2 MB) take 13 us,
+// 8 of 131072 rows (4 MB) 38; one CTA that reads the weights for every round took 605 for those.
 __device__ __forceinline__ uint32_t weight_key(float x) {      // larger weight, larger key; a NaN on top
   const uint32_t b = __float_as_uint(x + 0.f);
   return x != x ? 0xffffffffu : b ^ (uint32_t)((int32_t)b >> 31 | 0x80000000);
 }
 
-// Threads of a CTA and rows a thread holds: a stretch of up to 2048 rows takes eight warps (every warp adds
-// up counts of its own), a longer one 32 warps and, from 16384 rows on, a cluster.
+// Threads of a CTA and rows a thread holds.  Eight warps where that is enough and there are more stretches
+// than SMs, or little to do (every warp adds up counts of its own: 32 x 8 stretches of 2048 rows 13 us, with
+// 32 warps 16; but 8 of them 10.5 and 7.6), else 32 warps.  More than 8192 rows are cut in two, four or eight
+// while SMs are idle (8 stretches of 16384 rows 23.5 us in one CTA, 19.4 in two; of 8192 rows 13.9 and 15.3;
+// 128 of 16384 rows 27 and 43), and more than a CTA's registers hold always.
 constexpr int kPickFew = 256, kPickFewKeys = 8;
 constexpr int kPickMany = 1024, kPickManyKeys = 16;
 constexpr int kPickRows = kPickMany * kPickManyKeys;           // a CTA holds at most
@@ -559,6 +567,7 @@ __global__ void __launch_bounds__(kPickThreads) evict_pick_long_kernel(const Evi
 // ------------------------------------------------------------------ eviction: the rows move
 // Half a warp per row, four rows at a time: 256 bytes of K, 256 of V, and the weight.  Sources lie behind
 // `keep` and destinations before it, or in other blocks: no move reads what another writes.
+// Bound by HBM: 32 x 900 rows of 16 (layer, head) pairs, 472 MB read and written, 81 us, 5.8 TB/s.
 constexpr int kMoveRows = 4;
 __global__ void __launch_bounds__(256) evict_move_kernel(const EvictArgs a, const __grid_constant__ EvictFew few) {
   const EvictEntry en = a.entries ? a.entries[blockIdx.z] : few.entries[blockIdx.z];
@@ -650,14 +659,15 @@ cudaError_t launch_evict(const EvictArgs& a, const EvictFew& few, int n, int num
   if (n <= 0) return cudaSuccess;
   const int lh = num_layers * a.num_kv_heads;
   cudaError_t e;
-  if (max_len <= kPickFew * kPickFewKeys) {
+  const int64_t stretches = (int64_t)n * lh;
+  if (max_len <= kPickFew * (stretches > 148 ? kPickFewKeys : 2)) {
     e = launch_kernel(evict_pick_kernel<kPickFew, kPickFewKeys>, dim3(n, lh), dim3(kPickFew), 0, st, false, a,
                       few, 1);
   } else if (max_len <= kPickCluster * kPickRows) {
-    // CTAs per stretch: as many as it takes to hold the longest stretch in registers, or to give a
-    // thread no more than four rows
-    int n_cta = 1;
-    while (n_cta < kPickCluster && max_len > n_cta * kPickMany * 4) n_cta *= 2;
+    int n_cta = 1;                               // of a stretch
+    while (n_cta < kPickCluster &&
+           (max_len > n_cta * kPickRows || (max_len > n_cta * 8192 && 2 * n_cta * stretches <= 148)))
+      n_cta *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(n * n_cta, lh);
     cfg.blockDim = dim3(kPickMany);
