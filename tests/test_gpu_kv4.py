@@ -556,6 +556,27 @@ def test_read_kv_of_more_rows_than_one_upload_lists(fmt):
     sess.close()
 
 
+@pytest.mark.parametrize("fmt", ["q4", "bf16"])
+def test_read_kv_of_more_pieces_than_one_upload_lists(fmt):
+    """2^16 pieces of blocks go to a launch; the next one begins inside an entry.  129 of them are
+    one more than travel with the launch itself."""
+    sess = PagedSession(LayerShape(1, 1), 160, 4, 140, kv_format=fmt)
+    (t,) = sess.new_threads(1)
+    n, times = 1500, 705
+    k, v = rows(n, 1, 232), rows(n, 1, 233)
+    sess.append([t], [n], k, v)
+    want = [torch.from_numpy(_expect_rows(x)).to(torch.bfloat16).cuda() if fmt == "q4" else x for x in (k, v)]
+    got = sess.read_kv([t] * times, [5] * times, [n - 7] * times)
+    for g, w in zip(got, want):
+        assert torch.equal(g.view(times, n - 7, 1, 128), w[5:n - 2].expand(times, n - 7, 1, 128))
+    for m in (127, 128, 129):                            # one row each, any order, the same row twice
+        at = [(37 * i) % n for i in range(m - 1)] + [0]
+        got = sess.read_kv([t] * m, at, [1] * m)
+        for g, w in zip(got, want):
+            assert torch.equal(g, w[at])
+    sess.close()
+
+
 def test_the_current_stream_with_and_without_the_short_way(monkeypatch):
     from paper_2401_06761_b200 import session
     for short in (session._raw_stream, None):

@@ -635,6 +635,46 @@ def test_eviction_of_a_long_stretch(n):
     check_evicted(f, t, w, [k], [v], 0, n, keep)
 
 
+@pytest.mark.parametrize("n_threads,n,keep,hk", [
+    (1, 512, 200, 2), (1, 513, 200, 2), (1, 2048, 2047, 1), (1, 2049, 30, 1), (1, 8192, 5000, 2),
+    (1, 8193, 8000, 2), (8, 300, 200, 2), (9, 300, 200, 2), (1, 10241, 10240, 1), (1, 10257, 10256, 1),
+    (40, 600, 333, 4), (40, 2048, 100, 4)])
+def test_eviction_of_stretches_that_are_few_and_many(n_threads, n, keep, hk):
+    f = Forest(2 * hk, hk, blocks=n_threads * 2 * (n // 16 + 2) + 64, threads=2 * n_threads + 8,
+               per_thread=n // 16 + 8, poison=False)
+    tids = f.new(n_threads)
+    k, v = rows(n * n_threads, hk, 1), rows(n * n_threads, hk, 2)
+    f.s.append(tids, [n] * n_threads, k, v)
+    ws = []
+    for i, t in enumerate(tids):
+        kind = KINDS[i % len(KINDS)] if n_threads > 1 else "few"
+        ws.append(some_weights(np.random.default_rng(i), kind, 1, n, hk))
+        set_weights(f, t, ws[-1])
+    kids = f.s.fork(tids)
+    for who in (kids, tids):                             # copied, then in place
+        f.s.evict(who, [0] * n_threads, [n] * n_threads, [keep] * n_threads)
+        B.apar_check_invariants(f.s.ctx)
+        for i, t in enumerate(who):
+            check_evicted(f, t, ws[i], [k[i * n:i * n + n]], [v[i * n:i * n + n]], 0, n, keep)
+        if who is kids:
+            f.s.release(kids)
+
+
+@pytest.mark.parametrize("hq,hk,n_threads,prompt,kids", [
+    (8, 1, 1, 1025, 0), (8, 1, 3, 2100, 0), (8, 1, 1, 5000, 1), (4, 1, 2, 700, 9), (32, 32, 6, 130, 1)])
+def test_weights_of_runs_cut_into_even_units(hq, hk, n_threads, prompt, kids):
+    f = Forest(hq, hk, blocks=2000, per_thread=400)
+    tids = f.new(n_threads)
+    f.append(tids, [prompt + 37 * i for i in range(n_threads)])
+    if kids:
+        tids = tids + f.fork(tids * kids)
+    q, lse = rows(len(tids), hq, 3), torch.empty(len(tids), hq, device="cuda")
+    f.s.attention(tids, q, lse=lse)
+    f.s.add_weights(q, lse)
+    _, rel = f.add(tids, q)
+    f.check_weights(tids, rel)
+
+
 def test_beam_search_with_a_bounded_cache():
     """Selection, reordering, decode steps with weights and evictions, as they are used together:
     the library's threads against plain lists of rows."""
