@@ -732,7 +732,8 @@ int key_chunk(const apar_ctx* c, const std::vector<KeyRun>& runs, int cls) {
   for (const KeyRun& r : runs)
     if (key_class(r.n_users * c->shape.group) == cls) keys += r.tok_end - r.tok_begin, ++n;
   const int64_t heads = c->cfg.num_kv_heads, warps = (int64_t)c->num_sms * kKeyWarpsPerSm[cls];
-  const int64_t rounds = std::max((keys * heads + warps * kMost - 1) / (warps * kMost), (n * heads + warps - 1) / warps);
+  const int64_t rounds = std::max((keys * heads + warps * kMost - 1) / (warps * kMost),
+                                  (n * heads + warps - 1) / warps);
   if (rounds == 0) return kMost;
   int64_t chunk = std::max<int64_t>(64, (keys * heads / (warps * rounds) + 15) / 16 * 16);
   for (; chunk < kMost; chunk += std::max<int64_t>(16, chunk / 256 * 16)) {
@@ -752,12 +753,12 @@ apar_status send_key_plan(apar_ctx* c, const std::vector<KeyRun>& runs, const st
   for (const KeyRun& r : runs) {
     // (even parts: a short rest would be a unit like the others, with little to do)
     const int most = chunks[by_class ? key_class(r.n_users * c->shape.group) : 0];
-    const int len = r.tok_end - r.tok_begin, parts = (len + most - 1) / most;
+    const int len = r.tok_end - r.tok_begin, parts = std::max(1, (len + most - 1) / most);
     const int chunk = by_class ? ((len + parts - 1) / parts + kBlock - 1) / kBlock * kBlock : most;
     for (int t = r.tok_begin; t < r.tok_end; t += chunk) {
       const bool last = t + chunk >= r.tok_end;
-      units->push_back(KeyUnit{r.table_row, t, last && r.open ? -(r.tok_end - t) - 1 : std::min(r.tok_end, t + chunk),
-                               r.user_begin, r.n_users, 0, {0, 0}});
+      const int end = last && r.open ? -(r.tok_end - t) - 1 : std::min(r.tok_end, t + chunk);
+      units->push_back(KeyUnit{r.table_row, t, end, r.user_begin, r.n_users, 0, {0, 0}});
     }
   }
   const size_t b_units = units->size() * sizeof(KeyUnit), b_users = users.size() * sizeof(KeyUser);
@@ -1727,8 +1728,9 @@ apar_status apar_read_kv(apar_ctx* c, int32_t layer, int32_t n, const int32_t* t
       apar_status rc = send(c, stg, d_stage, (size_t)filled * sizeof(ReadPiece), st);
       if (rc) return rc;
     }
-    APAR_CUDA(c, launch_read_rows(c->q4, kp, vp, k_out, v_out, few, stg ? (const ReadPiece*)d_stage : nullptr,
-                                  filled, c->cfg.num_kv_heads, st));
+    const ReadPiece* many = stg ? (const ReadPiece*)d_stage : nullptr;
+    APAR_CUDA(c, launch_read_rows(c->q4, kp, vp, k_out, v_out, few, many, filled,
+                                  c->cfg.num_kv_heads, st));
     ++c->kernels_total;
     stg = nullptr;
     filled = 0;

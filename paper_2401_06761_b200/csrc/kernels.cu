@@ -90,7 +90,8 @@ __global__ void __launch_bounds__(128) sync_kernel(int32_t* __restrict__ tables,
     const TableDelta d = deltas[blockIdx.x];
     int32_t* dst = tables + (size_t)d.row * stride + d.pos;
     const int32_t* src = data + d.data_off;
-    // (a long row - a fork of a long thread - by several CTAs: each word crosses PCIe on its own time)
+    // (a long row - a fork of a long thread - by several CTAs: each word crosses PCIe on its own time; 8188
+    // words by one CTA some 80 us, by sixteen 8)
     for (int i = blockIdx.y * blockDim.x + threadIdx.x; i < d.count; i += gridDim.y * blockDim.x)
       dst[i] = src[i];
   } else if (blockIdx.y == 0) {
@@ -104,8 +105,9 @@ cudaError_t launch_sync(int32_t* d_tables, int table_stride, int32_t* d_lens,
                         const int32_t* d_len_pairs, int n_pairs, int max_count, cudaStream_t st) {
   const int grid = n_deltas + (n_pairs + 127) / 128;
   if (grid <= 0) return cudaSuccess;
-  sync_kernel<<<dim3(grid, max_count > 512 ? (max_count + 511) / 512 : 1), 128, 0, st>>>(d_tables, table_stride, d_lens, d_deltas, d_data, n_deltas,
-                                    d_len_pairs, n_pairs);
+  const unsigned parts = std::max(1, (max_count + 511) / 512);
+  sync_kernel<<<dim3(grid, parts), 128, 0, st>>>(d_tables, table_stride, d_lens, d_deltas, d_data, n_deltas,
+                                                 d_len_pairs, n_pairs);
   return cudaGetLastError();
 }
 
