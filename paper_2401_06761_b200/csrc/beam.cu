@@ -5,27 +5,28 @@
 // enough: it keeps, per piece of a row, the num_select largest logits and the piece's maximum and sum
 // of exponentials, and a second small kernel puts the pieces of a sequence's rows together.
 //
-// beam_scan_kernel   one CTA per piece, which reads 8192 (f32) or 16384 (16-bit) elements at a time into
-//     registers, all loads on their way at once, sixteen bytes each where a row begins on such a
-//     boundary.  Which thread holds which element, and so the order of the sums, depends on the
-//     element alone: equal rows tie exactly.  A threshold that at least num_select elements reach comes
-//     from the threads' maxima: with j = num_select / 8 rounded up, the least of the eight warps' j-th
-//     largest.  The few elements that reach it (some two to three times num_select; the exact
-//     num_select-th largest of the maxima leaves fewer, but takes longer than it saves) are collected in
-//     shared memory and put in order by counting, for each, how many are larger.  A key is (ordered bits
-//     of the logit, complement of the token): of equal logits the lower token is kept.  Where more than
-//     512 elements reach the threshold (many equal ones) the warps go over the piece again with
-//     buffers that they sort and cut back as they fill.
+// beam_scan_kernel   one CTA per piece of a row.  A thread goes over its elements a step of 16 at a time,
+//     sixteen bytes to a load where the row begins on such a boundary, the next step's on their way
+//     meanwhile, and keeps the largest, the sum of 2^((x - it) log2 e) and, in shared memory, each step's
+//     largest.  Which thread holds which element, and so the order of the sums, depends on the element
+//     alone: equal rows tie exactly.  A threshold that at least num_select elements reach comes from the
+//     threads' maxima: with j = num_select / 8 rounded up, the least of the eight warps' j-th largest.
+//     The steps that reach it (some two to three times num_select; the exact num_select-th largest of the
+//     maxima leaves fewer, but takes longer than it saves) are read again, the elements that do collected
+//     and put in order by counting, for each, how many are larger.  A key is (ordered bits of the logit,
+//     complement of the token): of equal logits the lower token is kept.  Where more than 512 elements
+//     reach the threshold (many equal ones) the warps go over the piece again with buffers that they
+//     sort and cut back as they fill.
 // beam_pick_kernel   one CTA per sequence: a threshold by halving (the beams' scores differ too much for
 //     the one above), and the few pairs that reach it ordered by counting.  Values of different beams are
 //     compared in 64 bits: their difference goes through two log-sum-exps, and 32 bits would round it.
 //
-// Bound: 4 bytes per f32 logit, one product and one special-function operation for each.  2048 rows of
-// 32003 f32 logits, a fifth of them finished (208 MB read): scan 55 us, 3.8 TB/s; without the exponentials
-// it takes 6 us less, without collecting and ordering 18: what is left is the waits between a CTA's steps,
-// which four CTAs of an SM cover in part.  (Tried: the next piece's copies into shared memory meanwhile, 73;
-// into registers, 58 with 64 of them a thread; into L2, no change.)  128 rows of 131072 bf16 logits: 14 us,
-// 2.4 TB/s, two and a half rounds of CTAs.  4 rows of 32000: 5 us, then 5 for the pick.
+// Bound: HBM, 4 bytes per f32 logit, and one special-function operation for each.  2048 rows of 32003 f32
+// logits, a fifth of them finished (208 MB read): scan 50 us, 4.2 TB/s; 10 of them are the end of a piece
+// (threshold, collecting, ordering), a chain of short steps that the SM's other CTAs cover in part.  128 rows
+// of 131072 bf16 logits: 13.5 us, 2.5 TB/s.  4 rows of 32000: 4 us, then 5 for the pick; with
+// 64 beams and 64 pairs of 16 sequences the pick takes 35.  (Tried: the next
+// step's copies into shared memory meanwhile, and whole pieces in registers until the end: 73 and 55 us.)
 #include <algorithm>
 #include <climits>
 
@@ -56,9 +57,9 @@ __device__ __forceinline__ u64 pair_of(float a, float b) {
 __device__ __forceinline__ float2 parts_of(u64 p) {
   return make_float2(__uint_as_float((uint32_t)p), __uint_as_float((uint32_t)(p >> 32)));
 }
-__device__ __forceinline__ u64 fma2(u64 a, u64 b, u64 c) {
+__device__ __forceinline__ u64 mul2(u64 a, u64 b) {
   u64 d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
 __device__ __forceinline__ u64 add2(u64 a, u64 b) {
@@ -76,8 +77,8 @@ __device__ __forceinline__ float unordered(uint32_t o) {   // (what is below -in
   return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
 }
 
-// A row's elements in packs of sixteen bytes.  (f32: 12 packs of a thread and 3 CTAs 55 us where 8 and 4 take
-// 54; 16-bit: 4 packs and 4 CTAs 21 us where 8 and 3 take 14.)
+// A row's elements in packs of sixteen bytes.  (f32: 2 packs a step and 6 CTAs of an SM 54 us, 3 and 5 54,
+// 4 and 4 50; 16-bit: 1 and 6 20 us, 2 and 5 13.4, 4 and 3 15.)
 __device__ __forceinline__ float number(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float number(__half x) { return __half2float(x); }
 __device__ __forceinline__ float number(float x) { return x; }
@@ -85,7 +86,7 @@ template <typename T>
 struct Packs;
 template <>
 struct Packs<float> {
-  static constexpr int kPer = 4, kHeld = 8, kCtas = 4; // a pack's elements, a thread's packs, CTAs of an SM
+  static constexpr int kPer = 4, kHeld = 4, kCtas = 4; // a pack's elements, packs of a step, CTAs of an SM
   static constexpr uint32_t kNone = 0xff800000u;       // -inf
   static __device__ __forceinline__ void numbers(uint4 w, float (&x)[4]) {
     x[0] = __uint_as_float(w.x);
@@ -96,7 +97,7 @@ struct Packs<float> {
 };
 template <>
 struct Packs<__nv_bfloat16> {
-  static constexpr int kPer = 8, kHeld = 8, kCtas = 3;
+  static constexpr int kPer = 8, kHeld = 2, kCtas = 5;
   static constexpr uint32_t kNone = 0xff80ff80u;
   static __device__ __forceinline__ void numbers(uint4 w, float (&x)[8]) {
     const uint32_t v[4] = {w.x, w.y, w.z, w.w};
@@ -109,7 +110,7 @@ struct Packs<__nv_bfloat16> {
 };
 template <>
 struct Packs<__half> {
-  static constexpr int kPer = 8, kHeld = 8, kCtas = 3;
+  static constexpr int kPer = 8, kHeld = 2, kCtas = 5;
   static constexpr uint32_t kNone = 0xfc00fc00u;
   static __device__ __forceinline__ void numbers(uint4 w, float (&x)[8]) {
     const uint32_t v[4] = {w.x, w.y, w.z, w.w};
@@ -283,6 +284,7 @@ __device__ int scan_again(const T* row, int e0, int e1, float tau, int select, u
 }
 
 // ------------------------------------------------------------------ pieces of rows
+constexpr int kSlots = 16;
 union ScanKeys {
   u64 cand[kCand];
   u64 bufs[kWarps][kBuf];
@@ -291,150 +293,160 @@ union ScanKeys {
 template <typename T>
 __global__ void __launch_bounds__(kThreads, Packs<T>::kCtas) beam_scan_kernel(const BeamArgs a) {
   using W = Packs<T>;
-  constexpr int kPer = W::kPer, kHeld = W::kHeld, kChunk = kThreads * kHeld;   // packs of a CTA
+  constexpr int kPer = W::kPer, kHeld = W::kHeld, kChunk = kThreads * kHeld;   // packs of a round
   __shared__ ScanKeys sh;
-  __shared__ u64 held[kMaxSelect];             // the largest so far, in order
   __shared__ uint32_t tops[2 * kWarps];
   __shared__ float sums[kWarps];
   __shared__ int counts[kWarps], n_cand, n_hit;
-  __shared__ uint8_t hit[kThreads];            // threads with something that reaches the threshold
+  __shared__ float peaks[kSlots][kThreads];    // largest of so many steps of a thread
+  __shared__ uint16_t hit[kCand];              // (slot, thread) that has something that reaches the threshold
   pdl_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int row = blockIdx.x / a.pieces, piece = blockIdx.x % a.pieces;
   const int seq = row / a.beams, beam = row % a.beams;
   const T* x = (const T*)a.logits + seq * a.seq_stride + beam * a.beam_stride;
   const int packs = (a.vocab + kPer - 1) / kPer, per_piece = (packs + a.pieces - 1) / a.pieces;
-  const int end = min(packs, (piece + 1) * per_piece);
-  const bool skip = a.finished && a.finished[row];     // (has its one continuation, see the other kernel)
-  int n_held = 0;
-  float m = -INFINITY, l = 0.f;
-  for (int c0 = skip ? end : piece * per_piece; c0 < end; c0 += kChunk) {
-    const int n_in = min(a.vocab, end * kPer);         // elements before this one are the piece's
-    uint4 v[kHeld];
+  const int begin = piece * per_piece, end = min(packs, begin + per_piece);
+  const int n_in = min(a.vocab, end * kPer);   // elements before this one are the piece's
+  u64* keys = a.keys + (size_t)blockIdx.x * a.select;
+  if (begin >= end || (a.finished && a.finished[row])) {   // (has its one continuation, see the other kernel)
+    if ((int)threadIdx.x < a.select) keys[threadIdx.x] = 0ull;
+    if (threadIdx.x == 0) a.stats[blockIdx.x] = make_float2(-INFINITY, 0.f);
+    return;
+  }
+  if (threadIdx.x == 0) n_cand = n_hit = 0;
+  // ---- this thread's elements: the largest, and the sum of 2^((x - it) log2 e).  (The difference first: no
+  // logit is too large or, as the lowest number of its type, too small for it.)
+  float mine = -INFINITY;
+  u64 part = 0;                                // two sums
+  const u64 scale = pair_of(kLog2e, kLog2e);
+  auto load = [&](uint4 (&v)[kHeld], int c0) {
     if (((uintptr_t)x & 15) == 0) load_packs<T, 16>(v, x, n_in, c0 + threadIdx.x);
     else if (sizeof(T) == 4 || ((uintptr_t)x & 3) == 0) load_packs<T, 4>(v, x, n_in, c0 + threadIdx.x);
     else load_packs<T, 2>(v, x, n_in, c0 + threadIdx.x);
-    float mine = -INFINITY;
+  };
+  const int steps = (end - begin + kChunk - 1) / kChunk, of_slot = (steps + kSlots - 1) / kSlots;
+  int slot = 0, left = of_slot;
+  float peak = -INFINITY;
+  auto add = [&](const uint4 (&v)[kHeld]) {
 #pragma unroll
     for (int k = 0; k < kHeld; ++k) {
       float e[kPer];
       W::numbers(v[k], e);
-      mine = largest(mine, e);
+      peak = largest(peak, e);
     }
-    if (threadIdx.x == 0) {
-      n_cand = n_held;
-      n_hit = 0;
+    const float now = fmaxf(mine, peak);
+    if (--left == 0) {
+      peaks[slot++][threadIdx.x] = peak;
+      peak = -INFINITY;
+      left = of_slot;
     }
-    if ((int)threadIdx.x < n_held) sh.cand[threadIdx.x] = held[threadIdx.x];
-    uint32_t most;
-    float tau = unordered(threshold(ordered(mine), a.select, min(end - c0, kChunk) / 32, tops, &most));
-    if (n_held == a.select) tau = fmaxf(tau, unordered((uint32_t)(held[n_held - 1] >> 32)));
-    if (mine >= tau && mine > -INFINITY) hit[atomicAdd(&n_hit, 1)] = (uint8_t)threadIdx.x;
-    // 2^(x log2 e - ref), ref being max log2 e; what rounding that product takes off every exponent is
-    // put back into the sum
-    const float top = unordered(most);
-    const bool finite = top - top == 0.f;
-    const float ref = top == -INFINITY ? 0.f : top * kLog2e;
-    u64 part = 0;                              // two sums
-    const u64 scale = pair_of(kLog2e, kLog2e), less = pair_of(-ref, -ref);
+    const float less = mine == -INFINITY ? 0.f : ex2((mine - now) * kLog2e);
+    part = mul2(part, pair_of(less, less));
+    mine = now;
+    const float from = now == -INFINITY ? 0.f : now;
+    const u64 minus = pair_of(-from, -from);
 #pragma unroll
     for (int k = 0; k < kHeld; ++k) {
       float e[kPer];
       W::numbers(v[k], e);
 #pragma unroll
       for (int i = 0; i < kPer; i += 2) {
-        const float2 p = parts_of(fma2(pair_of(e[i], e[i + 1]), scale, less));
+        const float2 p = parts_of(mul2(add2(pair_of(e[i], e[i + 1]), minus), scale));
         part = add2(part, pair_of(ex2(p.x), ex2(p.y)));
       }
     }
-    float sum = parts_of(part).x + parts_of(part).y;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
-    if (lane == 0) sums[warp] = sum;
-    __syncthreads();
-    // maximum and sum so far
-    {
-      float s = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) s += sums[w];
-      if (finite) s *= ex2(fmaf(-kLog2e, top, ref));
-      const float both = fmaxf(m, top), r = both == -INFINITY ? 0.f : both;
-      l = l * ex2((m - r) * kLog2e) + s * (top == -INFINITY ? 1.f : ex2((top - r) * kLog2e));
-      m = both;
-    }
-    // The few elements that reach the threshold: the hit threads' packs are read again, each by a thread of
-    // its own.  (Looked for by the threads that hold them, they take longer than all the exponentials.)
-    for (int i = threadIdx.x, n = n_hit * kHeld; i < n; i += kThreads) {
-      const int at = c0 + i % kHeld * kThreads + hit[i / kHeld];
-      if (at * kPer >= n_in) continue;
-      float e[kPer];
-      if (((uintptr_t)x & 15) == 0 && (at + 1) * kPer <= n_in) {
-        W::numbers(load_pack<16>(x + (int64_t)at * kPer), e);
-      } else {
-#pragma unroll
-        for (int k = 0; k < kPer; ++k) e[k] = at * kPer + k < n_in ? number(x[at * kPer + k]) : -INFINITY;
+  };
+  uint4 v0[kHeld], v1[kHeld];                  // one on its way while the other is added
+  load(v0, begin);
+#pragma unroll 1
+  for (int c0 = begin; c0 < end; c0 += 2 * kChunk) {
+    if (c0 + kChunk < end) load(v1, c0 + kChunk);
+    add(v0);
+    if (c0 + kChunk >= end) break;
+    if (c0 + 2 * kChunk < end) load(v0, c0 + 2 * kChunk);
+    add(v1);
+  }
+  if (left != of_slot) peaks[slot++][threadIdx.x] = peak;
+  // ---- the threads together
+  uint32_t most;
+  const float tau = unordered(threshold(ordered(mine), a.select, (end - begin) / 32, tops, &most));
+  if (mine >= tau && mine > -INFINITY)
+    for (int k = 0; k < slot; ++k)
+      if (peaks[k][threadIdx.x] >= tau && peaks[k][threadIdx.x] > -INFINITY) {
+        const int at = atomicAdd(&n_hit, 1);
+        if (at < kCand) hit[at] = (uint16_t)(k * kThreads + threadIdx.x);
       }
-      if (!(largest(-INFINITY, e) >= tau)) continue;
-      int slot = 0;
+  const float top = unordered(most);
+  float sum = parts_of(part).x + parts_of(part).y;
+  if (mine != top) sum *= ex2((mine - top) * kLog2e);
 #pragma unroll
-      for (int k = 0; k < kPer; ++k) slot += e[k] >= tau && e[k] > -INFINITY;
-      slot = atomicAdd(&n_cand, slot);
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
+  if (lane == 0) sums[warp] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    float s = 0.f;
 #pragma unroll
-      for (int k = 0; k < kPer; ++k) {
-        if (!(e[k] >= tau && e[k] > -INFINITY)) continue;
-        if (slot < kCand) sh.cand[slot] = (u64)ordered(e[k]) << 32 | (uint32_t)~(at * kPer + k);
-        ++slot;
-      }
-    }
-    __syncthreads();
-    const int n = n_cand;
-    if (n <= kCand) {
-      // (four threads to each of them; their order in the list does not matter)
-      for (int i0 = 0; i0 < n; i0 += kThreads / 4) {
-        const int i = i0 + threadIdx.x / 4;
-        const u64 key = i < n ? sh.cand[i] : 0ull;
-        int rank = 0;
-        for (int j = threadIdx.x & 3; j < n; j += 4) rank += sh.cand[j] > key;
-        rank += __shfl_xor_sync(kAll, rank, 1);
-        rank += __shfl_xor_sync(kAll, rank, 2);
-        if (i < n && rank < a.select) held[rank] = key;
-      }
-      n_held = min(n, a.select);
-      __syncthreads();
+    for (int w = 0; w < kWarps; ++w) s += sums[w];
+    a.stats[blockIdx.x] = make_float2(top, s);
+  }
+  // The few elements that reach the threshold: where there is one, the packs are read again, by a thread each.
+  // (Looked for by the threads that hold them, they take longer than all the exponentials.)
+  const int n_again = n_hit, of_hit = of_slot * kHeld;
+  for (int i = threadIdx.x; i < n_again * of_hit && n_again <= kCand; i += kThreads) {
+    const int t = i / of_hit, h = hit[t];
+    const int at = begin + (h / kThreads * of_hit + i - t * of_hit) * kThreads + h % kThreads;
+    if (at >= end) continue;
+    float e[kPer];
+    if (((uintptr_t)x & 15) == 0 && (at + 1) * kPer <= n_in) {
+      W::numbers(load_pack<16>(x + (int64_t)at * kPer), e);
     } else {
-      const int per_warp = kChunk / kWarps * kPer, first = c0 * kPer + warp * per_warp;
-      const int found = scan_again(x, first, min(n_in, first + per_warp), tau, a.select, sh.bufs[warp]);
-      if (lane == 0) counts[warp] = found;
-      __syncthreads();
-      // the warps' sorted lists and what is held become one list
-      u64 merged[kMaxSelect / 32] = {0ull, 0ull};
-      int n_new = 0;
-      if (warp == 0) {
-        const u64* list = lane < kWarps ? sh.bufs[lane] : held;
-        int at = 0, have = lane < kWarps ? counts[lane] : lane == kWarps ? n_held : 0;
-        for (int k = 0; k < a.select; ++k) {
-          const u64 head = at < have ? list[at] : 0ull;
-          u64 best = head;
 #pragma unroll
-          for (int o = 16; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(kAll, best, o));
-          if (best == 0) break;
-          if (head == best) ++at;
-          if (lane == (k & 31)) merged[k >> 5] = best;
-          ++n_new;
-        }
-        __syncwarp();
+      for (int k = 0; k < kPer; ++k) e[k] = at * kPer + k < n_in ? number(x[at * kPer + k]) : -INFINITY;
+    }
+    if (!(largest(-INFINITY, e) >= tau)) continue;
+    int put = 0;
 #pragma unroll
-        for (int k = 0; k < kMaxSelect / 32; ++k) held[32 * k + lane] = merged[k];
-        if (lane == 0) n_cand = n_new;
-      }
-      __syncthreads();
-      n_held = n_cand;
-      __syncthreads();
+    for (int k = 0; k < kPer; ++k) put += e[k] >= tau && e[k] > -INFINITY;
+    put = atomicAdd(&n_cand, put);
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      if (!(e[k] >= tau && e[k] > -INFINITY)) continue;
+      if (put < kCand) sh.cand[put] = (u64)ordered(e[k]) << 32 | (uint32_t)~(at * kPer + k);
+      ++put;
     }
   }
-  if ((int)threadIdx.x < a.select)
-    a.keys[(size_t)blockIdx.x * a.select + threadIdx.x] = (int)threadIdx.x < n_held ? held[threadIdx.x] : 0ull;
-  if (threadIdx.x == 0) a.stats[blockIdx.x] = make_float2(m, l);
+  __syncthreads();
+  const int n = n_cand;
+  if (n <= kCand && n_again <= kCand) {
+    // (four threads to each of them; their order in the list does not matter)
+    for (int i0 = 0; i0 < n; i0 += kThreads / 4) {
+      const int i = i0 + threadIdx.x / 4;
+      const u64 key = i < n ? sh.cand[i] : 0ull;
+      int rank = 0;
+      for (int j = threadIdx.x & 3; j < n; j += 4) rank += sh.cand[j] > key;
+      rank += __shfl_xor_sync(kAll, rank, 1);
+      rank += __shfl_xor_sync(kAll, rank, 2);
+      if (i < n && rank < a.select && (threadIdx.x & 3) == 0) keys[rank] = key;
+    }
+    if ((int)threadIdx.x >= n && (int)threadIdx.x < a.select) keys[threadIdx.x] = 0ull;
+    return;
+  }
+  const int per_warp = ((end - begin + kWarps - 1) / kWarps) * kPer, first = begin * kPer + warp * per_warp;
+  const int found = scan_again(x, min(n_in, first), min(n_in, first + per_warp), tau, a.select, sh.bufs[warp]);
+  if (lane == 0) counts[warp] = found;
+  __syncthreads();
+  if (warp != 0) return;
+  // the warps' sorted lists become one
+  int at = 0, have = lane < kWarps ? counts[lane] : 0;
+  for (int k = 0; k < a.select; ++k) {
+    const u64 head = at < have ? sh.bufs[lane & (kWarps - 1)][at] : 0ull;
+    u64 most_of = head;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) most_of = max(most_of, __shfl_xor_sync(kAll, most_of, o));
+    if (head == most_of) ++at;
+    if (lane == 0) keys[k] = most_of;
+  }
 }
 
 // ------------------------------------------------------------------ sequences
@@ -449,7 +461,7 @@ __device__ __forceinline__ bool before(const Pair& a, const Pair& b) {
 
 __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
   __shared__ Pair cand[kCand];
-  __shared__ double base[kMaxBeams];           // score - lse; NaN: the beam has no pairs
+  __shared__ double base[kMaxBeams];           // score - (lse - largest logit); NaN: the beam has no pairs
   __shared__ float2 stats[kMaxLists], terms[kMaxLists];
   __shared__ uint8_t over[kMaxBeams];
   __shared__ uint32_t tops[kWarps];
@@ -459,8 +471,10 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_wait();                                  // (the scan has written its lists)
   // (everything that is needed first is asked for at once)
-  const u64* keys = a.keys + (size_t)seq * n_all;
-  const u64 key0 = (int)threadIdx.x < n_all ? keys[threadIdx.x] : 0ull;
+  // Pair i is the i / n_lists-th of list i mod n_lists: a thread that looks at several has them of few lists,
+  // where they fall off, and not the first ones of many.
+  auto place = [&](int i) { return (size_t)(seq * n_lists + i % n_lists) * a.select + i / n_lists; };
+  const u64 key0 = (int)threadIdx.x < n_all ? a.keys[place(threadIdx.x)] : 0ull;
   const int b = threadIdx.x, row = seq * a.beams + b;
   const float score = b < a.beams ? a.scores[row] : 0.f;
   const bool done = b < a.beams && a.finished && a.finished[row];
@@ -487,8 +501,8 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
       } else {
         double L = 0.0;
         for (int p = 0; p < a.pieces; ++p) L += terms[b * a.pieces + p].y;
-        const double lse = terms[b * a.pieces].x + log(L);
-        if (lse - lse == 0.0) to = (double)score - lse;
+        const double M = terms[b * a.pieces].x, rest = log(L);
+        if (M - M == 0.0 && rest - rest == 0.0) to = (double)score - rest;
       }
     }
     base[b] = to;
@@ -496,10 +510,12 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
   __syncthreads();
   // pair i of the lists; a value that is not above -inf: none
   auto entry = [&](int i) {
-    const int list = i / a.select, b = list / a.pieces;
-    if (over[b]) return Pair{i % (a.pieces * a.select) ? -INFINITY : base[b], (u64)b << 32 | (uint32_t)a.eos};
-    const u64 key = i < kThreads ? key0 : keys[i];   // (every thread asks for i = its own first)
-    return Pair{key ? base[b] + (double)unordered((uint32_t)(key >> 32)) : -INFINITY,
+    const int list = i % n_lists, b = list / a.pieces;
+    if (over[b])
+      return Pair{i >= n_lists || list % a.pieces ? -INFINITY : base[b], (u64)b << 32 | (uint32_t)a.eos};
+    const u64 key = i < kThreads ? key0 : a.keys[place(i)];   // (every thread asks for i = its own first)
+    const double less = (double)unordered((uint32_t)(key >> 32)) - (double)terms[b * a.pieces].x;
+    return Pair{key ? base[b] + less : -INFINITY,
                 (u64)b << 32 | (uint32_t)~(uint32_t)key};
   };
   float mine = -INFINITY;
@@ -587,17 +603,16 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
 }
 
 // Pieces of a row.  Few rows are cut to fill the machine twice over, no piece shorter than 2048 elements;
-// more rows into pieces that a CTA's registers hold, as long as that gives no more than four rounds of CTAs:
-// a piece that takes several rounds of loads collects fewer candidates, but waits for each (32 x 4 rows of
-// 131072, 16-bit: 8 pieces 14.2 us, 3 pieces 15.4; 256 x 8 of 32003, f32: 3 pieces 63 us, one 56).
+// more rows into pieces of no less than 8192 (f32) or 16384, as long as that gives no more than two rounds of
+// CTAs: the end of a piece costs as much as some thousand elements (256 x 8 rows of 32003, f32, in 1, 2 and 4
+// pieces: 50, 57 and 67 us).
 int pieces_of(const apar_beam_config* c, int32_t n_seq) {
   const int64_t rows = (int64_t)n_seq * c->num_beams;
   const bool f32 = c->logits_type == APAR_LOGITS_F32;
-  const int64_t held = kThreads * (f32 ? Packs<float>::kHeld * Packs<float>::kPer
-                                       : Packs<__half>::kHeld * Packs<__half>::kPer);
+  const int64_t held = f32 ? 8192 : 16384;
   const int64_t round = 148 * (f32 ? Packs<float>::kCtas : Packs<__half>::kCtas);
   const int64_t few = std::min<int64_t>((2 * 148 + rows - 1) / rows, (c->vocab + 2047) / 2048);
-  const int64_t fit = std::min<int64_t>((4 * round + rows - 1) / rows, (c->vocab + held - 1) / held);
+  const int64_t fit = std::min<int64_t>((2 * round + rows - 1) / rows, (c->vocab + held - 1) / held);
   return (int)std::min<int64_t>({std::max(few, fit), kMaxPieces, kMaxLists / c->num_beams});
 }
 

@@ -131,6 +131,52 @@ def test_large_and_small_logits():
     check(x, s * 1e-3, 3)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+def test_masks_of_the_lowest_and_logits_of_the_largest_value(dtype):
+    """A row whose logits all lie at the type's lowest value is as good as one of zeros."""
+    low, high = torch.finfo(dtype).min, torch.finfo(dtype).max
+    x, s, _ = random_inputs(5, 2, 9000, dtype, 11)
+    x[0, :, 40:] = low                                   # most of a row, whole threads of it
+    x[1, 0] = low
+    x[2, 1] = high
+    x[3, 0, :4500], x[3, 0, 4500:] = low, high
+    x[4, 1] = low
+    x[4, 1, 8999] = 0
+    x = x.contiguous()
+    best, beam, token = (t.cpu().numpy() for t in BeamSelect(2, 9000, 12)(x, s))
+    d = x.double().cpu().numpy()
+    less = d - d.max(-1, keepdims=True)                  # (before anything else: it is exact)
+    value = s.double().cpu().numpy()[..., None] + (less - np.log(np.exp(less).sum(-1, keepdims=True)))
+    value = value.reshape(5, -1)
+    for i in range(5):
+        order = np.lexsort((np.arange(18000), -value[i]))[:12]
+        want = value[i][order]
+        tol = LSE_TOL + np.abs(want) * 2.0 ** -24
+        assert np.all(np.abs(best[i] - want) <= tol), (i, best[i], want)
+        flat = beam[i].astype(np.int64) * 9000 + token[i]
+        assert np.all(np.abs(value[i][flat] - want) <= 2 * tol) and len(set(flat.tolist())) == 12
+        for b in range(2):                               # equal logits: the lower token first
+            mine = token[i][beam[i] == b]
+            ref = np.lexsort((np.arange(9000), -d[i, b]))[:len(mine)]
+            assert np.array_equal(mine, ref), (i, b, mine, ref)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+def test_many_rows_whose_pieces_take_several_rounds(dtype):
+    x, s, g = random_inputs(225, 8, 17003, dtype, 12, pad=5)
+    x[3, :, 11:13000] = 1.0                              # more equal ones than are collected
+    x[3] = x[3].clamp(max=1.0)
+    x[4] = 0.0
+    done = torch.rand(225, 8, generator=g, device="cuda") < 0.2
+    check(x[:40], s[:40], 16, done[:40].contiguous(), eos=3)
+    sel = BeamSelect(8, 17003, 16, 3)
+    whole = sel(x, s, done)
+    for i in range(0, 225, 45):                          # few rows are cut into pieces, many are not
+        part = sel(x[i:i + 45], s[i:i + 45], done[i:i + 45])
+        assert all(torch.equal(u[i:i + 45], v) for u, v in zip(whole[1:], part[1:]))
+        assert torch.allclose(whole[0][i:i + 45], part[0], rtol=2.0 ** -23, atol=2 * LSE_TOL)
+
+
 def test_strided_views_and_other_streams():
     x, s, _ = random_inputs(4, 3, 1000, torch.float16, 6)
     swapped = x.transpose(0, 1).contiguous().transpose(0, 1)       # beams outermost in memory
