@@ -24,9 +24,9 @@
 // Bound: HBM, 4 bytes per f32 logit, and one special-function operation for each.  2048 rows of 32003 f32
 // logits, a fifth of them finished (208 MB read): scan 50 us, 4.2 TB/s; 10 of them are the end of a piece
 // (threshold, collecting, ordering), a chain of short steps that the SM's other CTAs cover in part.  128 rows
-// of 131072 bf16 logits: 13.5 us, 2.5 TB/s.  4 rows of 32000: 4 us, then 5 for the pick; with
-// 64 beams and 64 pairs of 16 sequences the pick takes 35.  (Tried: the next
-// step's copies into shared memory meanwhile, and whole pieces in registers until the end: 73 and 55 us.)
+// of 131072 bf16 logits: 13.5 us, 2.5 TB/s.  4 rows of 32000: 4 us, then 5 for the pick; that of 64 pairs for
+// 16 sequences of 64 beams takes 35.  (Tried: the next step's copies into shared memory meanwhile, and whole
+// pieces in registers until the end: 73 and 55 us.)
 #include <algorithm>
 #include <climits>
 
