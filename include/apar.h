@@ -485,7 +485,8 @@ apar_status apar_reorder(apar_ctx* ctx, int32_t n, const int32_t* tid /*[host]*/
  * drop the rows that attention hardly looks at).  With memory attached a context holds a float per
  * cached row, layer and kv head, which lies with the row's block: an appended row starts at 0, a row
  * that a fork, apar_reorder or apar_accept_candidates copies or moves takes its weight along, and
- * threads that share a block share its rows' weights.  bf16 pools only: UNSUPPORTED otherwise.
+ * threads that share a block share its rows' weights.  bf16 pools only, and no more than 65535 layers
+ * times kv heads: UNSUPPORTED otherwise.
  *   Bytes: the weights, float [num_layers][num_blocks][num_kv_heads][16], then areas of the
  *   library's own.  The caller owns the memory and may read and write the weights on the context's
  *   stream; those of rows that are cached when it is attached are what the memory holds. */
