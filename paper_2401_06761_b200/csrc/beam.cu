@@ -464,17 +464,22 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
   __shared__ double base[kMaxBeams];           // score - (lse - largest logit); NaN: the beam has no pairs
   __shared__ float2 stats[kMaxLists], terms[kMaxLists];
   __shared__ uint8_t over[kMaxBeams];
+  __shared__ float vals[kMaxLists * kMaxSelect];   // rounded; a thread's own
   __shared__ uint32_t tops[kWarps];
+  __shared__ int counts[2][kWarps], n_cand;
   __shared__ Pair picks[kWarps];
-  __shared__ int n_cand;
   const int seq = blockIdx.x, n_lists = a.beams * a.pieces, n_all = n_lists * a.select;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_wait();                                  // (the scan has written its lists)
   // (everything that is needed first is asked for at once)
-  // Pair i is the i / n_lists-th of list i mod n_lists: a thread that looks at several has them of few lists,
-  // where they fall off, and not the first ones of many.
-  auto place = [&](int i) { return (size_t)(seq * n_lists + i % n_lists) * a.select + i / n_lists; };
-  const u64 key0 = (int)threadIdx.x < n_all ? a.keys[place(threadIdx.x)] : 0ull;
+  const u64* keys = a.keys + (size_t)seq * n_all;
+  constexpr int kAhead = 4;
+  u64 ahead[kAhead];
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) {
+    const int i = threadIdx.x + k * kThreads;
+    ahead[k] = i < n_all ? keys[i] : 0ull;
+  }
   const int b = threadIdx.x, row = seq * a.beams + b;
   const float score = b < a.beams ? a.scores[row] : 0.f;
   const bool done = b < a.beams && a.finished && a.finished[row];
@@ -509,40 +514,66 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
   }
   __syncthreads();
   // pair i of the lists; a value that is not above -inf: none
-  auto entry = [&](int i) {
-    const int list = i % n_lists, b = list / a.pieces;
+  const float by_select = 1.f / a.select, by_pieces = 1.f / a.pieces;   // (i < 2^13: the quotients are exact)
+  auto entry = [&](int i, u64 key) {
+    const int list = (int)((i + 0.5f) * by_select), b = (int)((list + 0.5f) * by_pieces);
     if (over[b])
-      return Pair{i >= n_lists || list % a.pieces ? -INFINITY : base[b], (u64)b << 32 | (uint32_t)a.eos};
-    const u64 key = i < kThreads ? key0 : a.keys[place(i)];   // (every thread asks for i = its own first)
+      return Pair{i == b * a.pieces * a.select ? base[b] : -INFINITY, (u64)b << 32 | (uint32_t)a.eos};
     const double less = (double)unordered((uint32_t)(key >> 32)) - (double)terms[b * a.pieces].x;
-    return Pair{key ? base[b] + less : -INFINITY,
-                (u64)b << 32 | (uint32_t)~(uint32_t)key};
+    return Pair{key ? base[b] + less : -INFINITY, (u64)b << 32 | (uint32_t)~(uint32_t)key};
   };
   float mine = -INFINITY;
-  for (int i = threadIdx.x; i < n_all; i += kThreads) {
-    const double x = entry(i).value;
-    if (x > -INFINITY) mine = fmaxf(mine, __double2float_rn(x));
+  for (int i0 = threadIdx.x; i0 < n_all; i0 += kAhead * kThreads) {
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int i = i0 + k * kThreads;
+      if (i >= n_all) break;
+      const double x = entry(i, ahead[k]).value;
+      const float r = x > -INFINITY ? __double2float_rn(x) : -INFINITY;   // (rounding keeps the order)
+      vals[i] = r;
+      mine = fmaxf(mine, r);
+    }
+    if (n_all <= kAhead * kThreads) break;     // (they stay where they are)
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int i = i0 + (k + kAhead) * kThreads;
+      ahead[k] = i < n_all ? keys[i] : 0ull;
+    }
   }
-  // A threshold that at least num_select of the threads' maxima reach, and hardly more: down from the
-  // largest in growing steps, then halving the last one.  (Beams differ too much for what serves above.)
+  // A threshold that at least num_select pairs reach, and hardly more: down from the largest in growing
+  // steps, then halving the last one.  (Beams differ too much for what serves above.)
   const uint32_t most_here = __reduce_max_sync(kAll, ordered(mine));
   if (lane == 0) tops[warp] = most_here;
   __syncthreads();
   uint32_t most = 0;
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) most = max(most, tops[w]);
+  int turn = 0;
+  auto count = [&](float t) {                  // pairs that reach t
+    if (n_all <= kThreads) return __syncthreads_count(mine >= t);
+    int c = 0;
+    for (int i = threadIdx.x; i < n_all; i += kThreads) c += vals[i] >= t;
+    c = __reduce_add_sync(kAll, c);
+    if (lane == 0) counts[turn][warp] = c;
+    __syncthreads();
+    c = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) c += counts[turn][w];
+    turn ^= 1;
+    return c;
+  };
   float tau = unordered(most), above = tau, width = 1.f;
   int reach = 0;
   while (reach < a.select && tau > -3e38f) {
     above = tau;
     tau = unordered(most) - width;
     width *= 4.f;
-    reach = __syncthreads_count(mine >= tau);
+    reach = count(tau);
   }
   if (reach < a.select) tau = -INFINITY;
-  for (int i = 0; i < 8 && reach > a.select + a.select / 2 + 8; ++i) {
+  for (int i = 0; i < 16 && reach > 2 * a.select + 32; ++i) {
     const float mid = 0.5f * (tau + above);
-    const int n = __syncthreads_count(mine >= mid);
+    const int n = count(mid);
     if (n >= a.select) {
       tau = mid;
       reach = n;
@@ -550,12 +581,19 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
       above = mid;
     }
   }
-  for (int i = threadIdx.x; i < n_all; i += kThreads) {
-    const Pair p = entry(i);
-    if (p.value > -INFINITY && __double2float_rn(p.value) >= tau) {   // (rounding keeps the order)
-      const int at = atomicAdd(&n_cand, 1);
-      if (at < kCand) cand[at] = p;
+  auto offer = [&](int i, u64 key) {
+    const int at = atomicAdd(&n_cand, 1);
+    if (at < kCand) cand[at] = entry(i, key);
+  };
+  if (n_all <= kAhead * kThreads) {
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int i = threadIdx.x + k * kThreads;
+      if (i < n_all && vals[i] >= tau && vals[i] > -INFINITY) offer(i, ahead[k]);
     }
+  } else {
+    for (int i = threadIdx.x; i < n_all; i += kThreads)
+      if (vals[i] >= tau && vals[i] > -INFINITY) offer(i, keys[i]);
   }
   __syncthreads();
   const int n = n_cand;
@@ -583,8 +621,9 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
   for (int k = 0; k < a.select; ++k) {
     Pair best = none;
     for (int i = threadIdx.x; i < n_all; i += kThreads) {
-      const Pair p = entry(i);
-      if (p.value > -INFINITY && before(last, p) && before(p, best)) best = p;
+      if (!(vals[i] >= tau && vals[i] > -INFINITY)) continue;
+      const Pair p = entry(i, keys[i]);
+      if (before(last, p) && before(p, best)) best = p;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {

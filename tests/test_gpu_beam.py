@@ -177,6 +177,13 @@ def test_many_rows_whose_pieces_take_several_rounds(dtype):
         assert torch.allclose(whole[0][i:i + 45], part[0], rtol=2.0 ** -23, atol=2 * LSE_TOL)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("beams,vocab,spread", [(32, 10000, 1.0), (64, 3000, 30.0), (16, 20000, 0.0), (64, 9000, 0.1)])
+def test_wide_beams_of_different_scores(beams, vocab, spread, dtype):
+    x, s, _ = random_inputs(3, beams, vocab, dtype, beams)
+    check(x, s * spread, 64)
+
+
 def test_strided_views_and_other_streams():
     x, s, _ = random_inputs(4, 3, 1000, torch.float16, 6)
     swapped = x.transpose(0, 1).contiguous().transpose(0, 1)       # beams outermost in memory
