@@ -17,6 +17,7 @@
 //     complement of the token): of equal logits the lower token is kept.  Where more than 512 elements
 //     reach the threshold (many equal ones) the warps go over the piece again with buffers that they
 //     sort and cut back as they fill.
+// beam_rows_kernel   the same for many short rows, a warp each.
 // beam_pick_kernel   one CTA per sequence: a threshold by halving (the beams' scores differ too much for
 //     the one above), and the few pairs that reach it ordered by counting.  Values of different beams are
 //     compared in 64 bits: their difference goes through two log-sum-exps, and 32 bits would round it.
@@ -148,26 +149,33 @@ __device__ __forceinline__ uint4 load_pack(const void* p) {
     return make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
-// This thread's packs at0, at0 + kThreads, ... of the n elements of a row; what lies past them is -inf.
-template <typename T, int kAlign>
-__device__ __forceinline__ void load_packs(uint4 (&v)[Packs<T>::kHeld], const T* row, int n, int at0) {
+// This thread's packs at0, at0 + kStride, ... of the n elements of a row; what lies past them is -inf.
+template <typename T, int kAlign, int kStride, int kN>
+__device__ __forceinline__ void load_packs(uint4 (&v)[kN], const T* row, int n, int at0) {
   constexpr int kPer = Packs<T>::kPer;
 #pragma unroll
-  for (int k = 0; k < Packs<T>::kHeld; ++k) {
-    const int at = at0 + k * kThreads;
+  for (int k = 0; k < kN; ++k) {
+    const int at = at0 + k * kStride;
     v[k] = make_uint4(Packs<T>::kNone, Packs<T>::kNone, Packs<T>::kNone, Packs<T>::kNone);
     if ((at + 1) * kPer <= n) v[k] = load_pack<kAlign>(row + (int64_t)at * kPer);
   }
-  const int last = n / kPer, k_last = (last - at0) / kThreads;     // the pack that the row's end cuts
-  if (n % kPer && last >= at0 && (last - at0) % kThreads == 0) {
+  const int last = n / kPer, k_last = (last - at0) / kStride;     // the pack that the row's end cuts
+  if (n % kPer && last >= at0 && (last - at0) % kStride == 0) {
     alignas(16) T x[kPer];
     const uint32_t none = Packs<T>::kNone;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) x[i] = last * kPer + i < n ? row[last * kPer + i] : *(const T*)&none;
 #pragma unroll
-    for (int k = 0; k < Packs<T>::kHeld; ++k)
+    for (int k = 0; k < kN; ++k)
       if (k == k_last) v[k] = *(const uint4*)x;
   }
+}
+// (whatever the row's alignment)
+template <typename T, int kStride, int kN>
+__device__ __forceinline__ void load_packs(uint4 (&v)[kN], const T* row, int n, int at0) {
+  if (((uintptr_t)row & 15) == 0) load_packs<T, 16, kStride>(v, row, n, at0);
+  else if (sizeof(T) == 4 || ((uintptr_t)row & 3) == 0) load_packs<T, 4, kStride>(v, row, n, at0);
+  else load_packs<T, 2, kStride>(v, row, n, at0);
 }
 
 struct BeamArgs {
@@ -320,11 +328,7 @@ __global__ void __launch_bounds__(kThreads, Packs<T>::kCtas) beam_scan_kernel(co
   float mine = -INFINITY;
   u64 part = 0;                                // two sums
   const u64 scale = pair_of(kLog2e, kLog2e);
-  auto load = [&](uint4 (&v)[kHeld], int c0) {
-    if (((uintptr_t)x & 15) == 0) load_packs<T, 16>(v, x, n_in, c0 + threadIdx.x);
-    else if (sizeof(T) == 4 || ((uintptr_t)x & 3) == 0) load_packs<T, 4>(v, x, n_in, c0 + threadIdx.x);
-    else load_packs<T, 2>(v, x, n_in, c0 + threadIdx.x);
-  };
+  auto load = [&](uint4 (&v)[kHeld], int c0) { load_packs<T, kThreads>(v, x, n_in, c0 + threadIdx.x); };
   const int steps = (end - begin + kChunk - 1) / kChunk, of_slot = (steps + kSlots - 1) / kSlots;
   int slot = 0, left = of_slot;
   float peak = -INFINITY;
@@ -447,6 +451,126 @@ __global__ void __launch_bounds__(kThreads, Packs<T>::kCtas) beam_scan_kernel(co
     if (head == most_of) ++at;
     if (lane == 0) keys[k] = most_of;
   }
+}
+
+// ------------------------------------------------------------------ short rows
+// A warp to a row of up to 2048 elements, which it holds in registers.  The threshold by halving, counting
+// elements: no waits between warps, and few candidates even where half of a row's elements is asked for.  Taken
+// where there are more rows than CTAs of the other kernel run at a time (64000 rows of 1000, 32 pairs, f32: 184
+// us and 542, 64 pairs, bf16: 248 and 855; 16000 of 1500: 52 and 121; 800 of 2048: 7.9 and 8.9; but 256 of
+// 2000: 8.4 and 6.3, one: 8.9 and 6.5).  Bound by instruction issue.
+constexpr int kShort = 2048, kShortRows = 4 * 148;
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 2) beam_rows_kernel(const BeamArgs a) {
+  using W = Packs<T>;
+  constexpr int kPer = W::kPer, kN = kShort / kPer / 32;
+  __shared__ u64 bufs[kWarps][kBuf];
+  pdl_launch_dependents();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x * kWarps + warp;
+  if (row >= a.n_seq * a.beams) return;
+  const int seq = row / a.beams, beam = row % a.beams;
+  u64* keys = a.keys + (size_t)row * a.select;
+  if (a.finished && a.finished[row]) {
+    for (int i = lane; i < a.select; i += 32) keys[i] = 0ull;
+    if (lane == 0) a.stats[row] = make_float2(-INFINITY, 0.f);
+    return;
+  }
+  const T* x = (const T*)a.logits + seq * a.seq_stride + beam * a.beam_stride;
+  uint4 v[kN];
+  load_packs<T, 32>(v, x, a.vocab, lane);
+  const int used = (a.vocab + 32 * kPer - 1) / (32 * kPer);   // packs of a lane
+  float mine = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < kN; ++k) {
+    float e[kPer];
+    W::numbers(v[k], e);
+    mine = largest(mine, e);
+  }
+  const float top = unordered(__reduce_max_sync(kAll, ordered(mine)));
+  const float from = top == -INFINITY ? 0.f : top;
+  const u64 minus = pair_of(-from, -from), scale = pair_of(kLog2e, kLog2e);
+  u64 part = 0;
+#pragma unroll
+  for (int k = 0; k < kN; ++k) {
+    if (k >= used) break;
+    float e[kPer];
+    W::numbers(v[k], e);
+#pragma unroll
+    for (int i = 0; i < kPer; i += 2) {
+      const float2 p = parts_of(mul2(add2(pair_of(e[i], e[i + 1]), minus), scale));
+      part = add2(part, pair_of(ex2(p.x), ex2(p.y)));
+    }
+  }
+  float sum = parts_of(part).x + parts_of(part).y;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
+  if (lane == 0) a.stats[row] = make_float2(top, sum);
+  // elements of this lane that reach t (and are above -inf)
+  auto here = [&](float t) {
+    int c = 0;
+#pragma unroll
+    for (int k = 0; k < kN; ++k) {
+      if (k >= used) break;
+      float e[kPer];
+      W::numbers(v[k], e);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) c += e[i] >= t;
+    }
+    return c;
+  };
+  float tau = top, above = top, width = 1.f;
+  int reach = 0;
+  while (reach < a.select && tau > -3e38f) {
+    above = tau;
+    tau = top - width;
+    width *= 4.f;
+    reach = __reduce_add_sync(kAll, here(tau));
+  }
+  if (reach < a.select) reach = __reduce_add_sync(kAll, here(tau = -3.4028235e38f));
+  for (int i = 0; i < 24 && reach > min(kBuf, 2 * a.select + 16); ++i) {
+    const float mid = 0.5f * tau + 0.5f * above;
+    const int n = __reduce_add_sync(kAll, here(mid));
+    if (n >= a.select) {
+      tau = mid;
+      reach = n;
+    } else {
+      above = mid;
+    }
+  }
+  u64* buf = bufs[warp];
+  if (reach > kBuf) {                          // many equal ones
+    const int n = scan_again(x, 0, a.vocab, tau, a.select, buf);
+    for (int i = lane; i < a.select; i += 32) keys[i] = i < n ? buf[i] : 0ull;
+    return;
+  }
+  int at = here(tau);
+  {
+    const int c = at;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const int up = __shfl_up_sync(kAll, at, o);
+      if (lane >= o) at += up;
+    }
+    at -= c;
+  }
+#pragma unroll
+  for (int k = 0; k < kN; ++k) {
+    if (k >= used) break;
+    float e[kPer];
+    W::numbers(v[k], e);
+    if (!(largest(-INFINITY, e) >= tau)) continue;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (e[i] >= tau) buf[at++] = (u64)ordered(e[i]) << 32 | (uint32_t)~((k * 32 + lane) * kPer + i);
+  }
+  __syncwarp();
+  for (int i = lane; i < reach; i += 32) {
+    const u64 key = buf[i];
+    int rank = 0;
+    for (int j = 0; j < reach; ++j) rank += buf[j] > key;
+    if (rank < a.select) keys[rank] = key;
+  }
+  for (int i = reach + lane; i < a.select; i += 32) keys[i] = 0ull;
 }
 
 // ------------------------------------------------------------------ sequences
@@ -714,7 +838,15 @@ extern "C" apar_status apar_beam_select(const apar_beam_config* cfg, int32_t n_s
   auto scan = cfg->logits_type == APAR_LOGITS_F32   ? beam_scan_kernel<float>
               : cfg->logits_type == APAR_LOGITS_F16 ? beam_scan_kernel<__half>
                                                     : beam_scan_kernel<__nv_bfloat16>;
-  cudaError_t e = launch_kernel(scan, dim3(lists), dim3(kThreads), 0, st, false, a);
+  cudaError_t e;
+  if (a.vocab <= kShort && lists > kShortRows) {   // (rows of one piece)
+    auto rows = cfg->logits_type == APAR_LOGITS_F32   ? beam_rows_kernel<float>
+                : cfg->logits_type == APAR_LOGITS_F16 ? beam_rows_kernel<__half>
+                                                      : beam_rows_kernel<__nv_bfloat16>;
+    e = launch_kernel(rows, dim3((lists + kWarps - 1) / kWarps), dim3(kThreads), 0, st, false, a);
+  } else {
+    e = launch_kernel(scan, dim3(lists), dim3(kThreads), 0, st, false, a);
+  }
   if (e == cudaSuccess) e = launch_kernel(beam_pick_kernel, dim3(n_seq), dim3(kThreads), 0, st, true, a);
   if (e != cudaSuccess) {
     note_cuda_error(e);

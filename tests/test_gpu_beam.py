@@ -184,6 +184,34 @@ def test_wide_beams_of_different_scores(beams, vocab, spread, dtype):
     check(x, s * spread, 64)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("n,beams,vocab,select,pad", [
+    (300, 2, 1, 1, 0), (200, 3, 33, 4, 1), (150, 4, 257, 64, 0), (100, 8, 1000, 64, 3), (80, 8, 2047, 16, 2),
+    (600, 1, 2048, 64, 0), (40, 16, 2048, 32, 8)])
+def test_many_short_rows(n, beams, vocab, select, pad, dtype):
+    x, s, g = random_inputs(n, beams, vocab, dtype, n + vocab, pad)
+    check(x, s, select)
+    low = torch.finfo(dtype).min
+    x = x.clone()
+    x[0] = 1.0                                           # equal ones
+    x[1, 0] = low
+    x[2, :, vocab // 2:] = -float("inf")
+    x[3, 0] = -float("inf")
+    x[4, 0, -1] = float("nan")
+    x[5, 0, 0] = float("inf")
+    x[6, :, ::2] = low
+    done = torch.rand(n, beams, generator=g, device="cuda") < 0.3
+    done[:7] = False
+    sel = BeamSelect(beams, vocab, select, 0)
+    many = sel(x, s, done)
+    for i in (0, 2, 3, 4, 5, 6, 7, n - 1):               # one sequence's rows take the other way
+        one = sel(x[i:i + 1], s[i:i + 1], done[i:i + 1])
+        assert all(torch.equal(u[i:i + 1], v) for u, v in zip(many[1:], one[1:])), i
+        assert torch.allclose(many[0][i:i + 1], one[0], rtol=2.0 ** -23, atol=2 * LSE_TOL)
+    rows_ok = [i for i in range(n) if i not in (1, 6)][:60]
+    check(x[rows_ok].contiguous(), s[rows_ok].contiguous(), select, done[rows_ok].contiguous(), eos=0)
+
+
 def test_strided_views_and_other_streams():
     x, s, _ = random_inputs(4, 3, 1000, torch.float16, 6)
     swapped = x.transpose(0, 1).contiguous().transpose(0, 1)       # beams outermost in memory
