@@ -735,14 +735,17 @@ int key_chunk(const apar_ctx* c, const std::vector<KeyRun>& runs, int cls) {
   const int64_t rounds = std::max((keys * heads + warps * kMost - 1) / (warps * kMost),
                                   (n * heads + warps - 1) / warps);
   if (rounds == 0) return kMost;
-  int64_t chunk = std::max<int64_t>(64, (keys * heads / (warps * rounds) + 15) / 16 * 16);
-  for (; chunk < kMost; chunk += std::max<int64_t>(16, chunk / 256 * 16)) {
+  // (fewer units, the longer they are: by halving, in steps of 16)
+  int64_t least = std::max<int64_t>(4, (keys * heads / (warps * rounds) + 15) / 16), most = kMost / 16;
+  while (least < most) {
+    const int64_t mid = (least + most) / 2, chunk = 16 * mid;
     int64_t units = 0;
     for (const KeyRun& r : runs)
       if (key_class(r.n_users * c->shape.group) == cls) units += (r.tok_end - r.tok_begin + chunk - 1) / chunk;
-    if (units * heads <= warps * rounds) break;
+    if (units * heads <= warps * rounds) most = mid;
+    else least = mid + 1;
   }
-  return (int)std::min<int64_t>(chunk, kMost);
+  return (int)(16 * std::min<int64_t>(least, kMost / 16));
 }
 
 // Cuts the runs into units of at most `chunk` keys (of a decode step: by class), longest first (of a decode
@@ -1925,7 +1928,7 @@ apar_status apar_add_weights(apar_ctx* c, int32_t layer, const void* q, const fl
   APAR_CUDA(c, cudaStreamIsCapturing(st, &cap));
   APAR_CUDA(c, launch_key_weights(key_args(c, c->wlay.plan, layer, q, lse, sm_scale, replace),
                                   c->key_plan.n_units, cap != cudaStreamCaptureStatusNone, st));
-  ++c->kernels_total;
+  for (int n : c->key_plan.n_units) c->kernels_total += n > 0 || cap != cudaStreamCaptureStatusNone;
   return APAR_OK;
 } catch (...) {               // (the host's memory)
   return APAR_ERR_INVALID_ARG;
