@@ -57,7 +57,8 @@ __global__ void __launch_bounds__(64) weights_move_kernel(float* __restrict__ w,
 // the three share the widest one's registers; with one of 8 rows, K is read again for every 8: 64 prompts
 // of 2400 keys and 3 forks each, 32 heads on 8, 117 us, now 68); a launch may start before the one before
 // it is done.  kAhead blocks of keys are on their way while one is worked on: it takes some 48 KB an SM in
-// flight to keep HBM busy.
+// flight to keep HBM busy.  (Of 32 rows with one block ahead and three CTAs, two and two, or 64 rows with one and
+// two: 64 prompts of 1024 under 16 threads each 73, 77 and 72 us; 16 of 3000 under 8 34, 36 and 48.)
 // Bound by HBM: those 64 x 2400 keys are 315 MB, 4.6 TB/s; 256 threads with 2400 keys of their own are 1.26 GB
 // and take 215 us, 5.8 TB/s.
 __device__ __forceinline__ uint4 ld_k(const uint4* p) {
