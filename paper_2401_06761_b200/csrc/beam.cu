@@ -456,8 +456,8 @@ __global__ void __launch_bounds__(kThreads, Packs<T>::kCtas) beam_scan_kernel(co
 // ------------------------------------------------------------------ short rows
 // A warp to a row of up to 2048 elements, which it holds in registers.  The threshold by halving, counting
 // elements: no waits between warps, and few candidates even where half of a row's elements is asked for.  Taken
-// where there are more rows than CTAs of the other kernel run at a time (64000 rows of 1000, 32 pairs, f32: 184
-// us and 542, 64 pairs, bf16: 248 and 855; 16000 of 1500: 52 and 121; 800 of 2048: 7.9 and 8.9; but 256 of
+// where there are more rows than CTAs of the other kernel run at a time (64000 rows of 1000, 32 pairs, f32: 195
+// us and 542, 64 pairs, bf16: 259 and 855; 16000 of 1500: 45 and 121; 800 of 2048: 6.8 and 8.9; but 256 of
 // 2000: 8.4 and 6.3, one: 8.9 and 6.5).  Bound by instruction issue.
 constexpr int kShort = 2048, kShortRows = 4 * 148;
 template <typename T>
@@ -518,15 +518,28 @@ __global__ void __launch_bounds__(kThreads, 2) beam_rows_kernel(const BeamArgs a
     }
     return c;
   };
-  float tau = top, above = top, width = 1.f;
+  float tau = -INFINITY, above = top;
   int reach = 0;
-  while (reach < a.select && tau > -3e38f) {
-    above = tau;
-    tau = top - width;
-    width *= 4.f;
-    reach = __reduce_add_sync(kAll, here(tau));
+  if (a.select <= 16) {
+    // the num_select-th largest of the lanes' maxima: at least as many elements reach it (16000 rows of 1500, 16
+    // pairs: 45 us, without this 52; but with 32 pairs of 64000 rows 209 and 184)
+    uint32_t rest = ordered(mine), t = 0;
+    for (int j = 0; j < a.select; ++j) {
+      t = __reduce_max_sync(kAll, rest);
+      if (lane == __ffs(__ballot_sync(kAll, rest == t)) - 1) rest = 0;
+    }
+    tau = unordered(t);
   }
-  if (reach < a.select) reach = __reduce_add_sync(kAll, here(tau = -3.4028235e38f));
+  if (tau == -INFINITY) {                      // (or there are not so many: down from the largest)
+    tau = top;
+    for (float width = 1.f; reach < a.select && tau > -3e38f; width *= 4.f) {
+      above = tau;
+      tau = top - width;
+      reach = __reduce_add_sync(kAll, here(tau));
+    }
+    if (reach < a.select) tau = -3.4028235e38f;
+  }
+  reach = __reduce_add_sync(kAll, here(tau));
   for (int i = 0; i < 24 && reach > min(kBuf, 2 * a.select + 16); ++i) {
     const float mid = 0.5f * tau + 0.5f * above;
     const int n = __reduce_add_sync(kAll, here(mid));
