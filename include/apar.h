@@ -304,7 +304,8 @@ apar_status apar_tree_prefill_attention(apar_ctx* ctx, int32_t layer, int32_t n,
  *     per call; a larger call cannot be replayed (APAR_ERR_WORKSPACE_TOO_SMALL).
  *   apar_tree_decode_attention_layer: same queries, in the same order, as in that attention
  *     call (which itself ran on layer 0).  Fails with APAR_ERR_INVALID_ARG if any bookkeeping
- *     call (new_threads, fork, append, release) came after it.
+ *     call (new_threads, fork, append, release, reorder, evict) or apar_tree_prefill_attention came
+ *     after it.
  * apar_fork copies the partial block in every layer.
  * Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, CUDA. */
 apar_status apar_append_kv_layer(apar_ctx* ctx, int32_t layer, const void* k_new /*[device]*/,
@@ -510,8 +511,9 @@ apar_status apar_set_lse_output(apar_ctx* ctx, float* lse /*[device] or NULL*/);
  * The first call after an attention call that made a plan of its own uploads one too; others only
  * launch kernels and can be captured.  A captured call follows the plan that the most recent
  * uncaptured one left on the device.
- * Errors: INVALID_ARG (also: no memory attached, bookkeeping since that attention call, a
- * verification, an upload while the stream is capturing), UNSUPPORTED, WORKSPACE_TOO_SMALL, CUDA. */
+ * Errors: INVALID_ARG (also: no memory attached, bookkeeping or apar_tree_prefill_attention since
+ * that attention call, a verification, an upload while the stream is capturing), UNSUPPORTED,
+ * WORKSPACE_TOO_SMALL, CUDA. */
 apar_status apar_add_weights(apar_ctx* ctx, int32_t layer, const void* q /*[device]*/,
                              const float* lse /*[device]*/, float sm_scale, int32_t replace,
                              void* cuda_stream);

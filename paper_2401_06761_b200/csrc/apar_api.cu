@@ -134,7 +134,7 @@ struct apar_ctx {
   int ring_next = 0, ring_n = kRing;   // buffers in use (a one-call context needs few)
   // ---- planning
   Planner planner;
-  Plan plan;
+  Plan plan, next_plan;                 // next_plan: being made, for a call that may still be refused
   std::vector<PlanQuery> pq;
   std::vector<int32_t> plan_tids;
   uint64_t struct_epoch = 1, plan_epoch = 0;
@@ -537,20 +537,16 @@ apar_status run_attention(apar_ctx* c, int n, const int32_t* qslots, const int32
                           bool has_dups, const void* q, void* out, float sm_scale,
                           cudaStream_t st, const int32_t* qlens = nullptr,
                           bool tables_in_sync = false, std::vector<VerifyDesc>* verify = nullptr) {
-  c->last.attn_kernels = 0;
   int64_t attended = 0;
   for (int i = 0; i < n; ++i) attended += qlens ? qlens[i] : c->slots[qslots[i]].len;
 
   const bool cacheable = tids != nullptr && !has_dups && !qlens;
   bool reuse = cacheable && plan_reusable(c, n, tids, attended);
-  if (c->weights && !(reuse && c->seen_valid)) {        // (a reused plan is of the same queries)
-    c->seen.resize(n);
-    for (int i = 0; i < n; ++i) c->seen[i] = {qslots[i], qlens ? qlens[i] : -1};
-    c->seen_valid = !verify;
-    c->key_plan_valid = false;
-  }
-  c->last.attn_plan_host_us = 0;
-  if (!tables_in_sync) c->last.attn_upload_bytes = 0;   // (else the caller's uploads count too)
+  // Until nothing can refuse the call any more it leaves what the call before it left: that one's plan, which
+  // layer calls, replays and apar_add_weights follow.
+  int64_t plan_host_us = 0;
+  int min_rows = c->plan_min_rows;
+  Q4Items q4_items;
   if (!reuse) {
     const auto t_plan = std::chrono::steady_clock::now();
     c->pq.clear();
@@ -573,37 +569,45 @@ apar_status run_attention(apar_ctx* c, int n, const int32_t* qslots, const int32
       if (c->q4 && verify) pq.first_query = i;
       c->pq.push_back(pq);
     }
-    c->plan_verify_n = 0;
     // Single-row items (no GQA group, private tail): the vector kernel keeps up to 16 CTAs per
     // SM in flight and wins when there are many of them; with few, the warp-stream kernel's
     // deeper per-warp rings do better (measured crossover near 900 queries).
-    c->plan_min_rows = c->mma_min_rows;
-    if (c->auto_path && c->shape.group == 1 && n <= kFewQueries) c->plan_min_rows = 1;
+    min_rows = c->mma_min_rows;
+    if (c->auto_path && c->shape.group == 1 && n <= kFewQueries) min_rows = 1;
     // finishing items land in the single-row vector kernel or the warp-stream kernel
-    const bool fuse_final = c->use_ws && c->plan_min_rows <= 2 && !verify && !c->q4;
-    if (!c->planner.build(c->pq.data(), (int)c->pq.size(), c->lay.slot_capacity, cacheable, c->plan_min_rows,
-                          fuse_final, &c->plan, by_runs))
+    const bool fuse_final = c->use_ws && min_rows <= 2 && !verify && !c->q4;
+    Plan& plan = c->next_plan;
+    if (!c->planner.build(c->pq.data(), (int)c->pq.size(), c->lay.slot_capacity, cacheable, min_rows,
+                          fuse_final, &plan, by_runs))
       return APAR_ERR_WORKSPACE_TOO_SMALL;
-    if ((int64_t)c->plan.users.size() > c->lay.entry_capacity ||
-        (int64_t)c->plan.items.size() > c->lay.entry_capacity)
+    if ((int64_t)plan.users.size() > c->lay.entry_capacity ||
+        (int64_t)plan.items.size() > c->lay.entry_capacity)
       return APAR_ERR_WORKSPACE_TOO_SMALL;
+    if (verify && (size_t)n * sizeof(VerifyDesc) > c->ring_bytes) return APAR_ERR_WORKSPACE_TOO_SMALL;
     if (c->q4) {
-      std::vector<WorkItem>& items = c->plan.items;
+      std::vector<WorkItem>& items = plan.items;
       auto rows = [&](const WorkItem& w) { return w.n_users * c->shape.group; };
       const auto mid = std::stable_partition(
           items.begin(), items.end(), [&](const WorkItem& w) { return rows(w) > kQ4Rows; });
       const auto narrow = std::stable_partition(
           mid, items.end(), [&](const WorkItem& w) { return rows(w) > kQ4NarrowRows; });
-      c->q4_items = Q4Items();
-      c->q4_items.n_wide = (int32_t)(mid - items.begin());
-      c->q4_items.n_mid = (int32_t)(narrow - mid);
-      c->q4_items.n_narrow = (int32_t)(items.end() - narrow);
-      for (const MergeRef& m : c->plan.merges)
-        c->q4_items.max_parts = std::max(c->q4_items.max_parts, m.n);
+      q4_items.n_wide = (int32_t)(mid - items.begin());
+      q4_items.n_mid = (int32_t)(narrow - mid);
+      q4_items.n_narrow = (int32_t)(items.end() - narrow);
+      for (const MergeRef& m : plan.merges) q4_items.max_parts = std::max(q4_items.max_parts, m.n);
     }
-    c->last.attn_plan_host_us = std::chrono::duration_cast<std::chrono::microseconds>(
-                                    std::chrono::steady_clock::now() - t_plan).count();
+    plan_host_us = std::chrono::duration_cast<std::chrono::microseconds>(
+                       std::chrono::steady_clock::now() - t_plan).count();
+    std::swap(c->plan, c->next_plan);
+    c->plan_epoch = 0;                    // (of the plan before)
+    c->plan_verify_n = 0;
+    c->plan_min_rows = min_rows;
+    c->q4_items = q4_items;
   }
+  c->attn_book_seq = 0;
+  c->last.attn_kernels = 0;
+  c->last.attn_plan_host_us = plan_host_us;
+  if (!tables_in_sync) c->last.attn_upload_bytes = 0;   // (else the caller's uploads count too)
   apar_status rc = tables_in_sync ? APAR_OK : sync_device_tables(c, qslots, n, st);
   if (rc) return rc;
 
@@ -632,7 +636,6 @@ apar_status run_attention(apar_ctx* c, int n, const int32_t* qslots, const int32
     }
     if (verify) {
       // every candidate's descriptor learns where its partial result goes
-      if ((size_t)n * sizeof(VerifyDesc) > c->ring_bytes) return APAR_ERR_WORKSPACE_TOO_SMALL;
       for (int i = 0; i < n; ++i) (*verify)[i].slot = p.extra_slot[i];
       for (const MergeRef& m : p.merges) (*verify)[m.query].parts = m.n - 1;
       Staging* s;
@@ -649,8 +652,6 @@ apar_status run_attention(apar_ctx* c, int n, const int32_t* qslots, const int32
       c->plan_epoch = c->struct_epoch;
       c->plan_attended = attended;
       c->plan_age = 0;
-    } else {
-      c->plan_epoch = 0;
     }
   } else {
     ++c->plan_age;
@@ -662,6 +663,12 @@ apar_status run_attention(apar_ctx* c, int n, const int32_t* qslots, const int32
   if (rc) return rc;
   if (c->time_stop) APAR_CUDA(c, cudaEventRecord(c->time_stop, st));
   c->attn_book_seq = c->book_seq;
+  if (c->weights && !(reuse && c->seen_valid)) {        // (a reused plan is of the same queries)
+    c->seen.resize(n);
+    for (int i = 0; i < n; ++i) c->seen[i] = {qslots[i], qlens ? qlens[i] : -1};
+    c->seen_valid = !verify;
+    c->key_plan_valid = false;
+  }
   c->kernels_total += launches;
   c->last.attn_kernels += launches;
   c->last.attn_threads = n;
@@ -1538,6 +1545,9 @@ apar_status apar_tree_prefill_attention(apar_ctx* c, int32_t layer, int32_t n,
     attended += (int64_t)q_count[i] * q_begin[i] + (int64_t)q_count[i] * (q_count[i] + 1) / 2;
   }
   if (total_q > INT32_MAX) return APAR_ERR_INVALID_ARG;
+  CUtensorMap tm_q;
+  if (make_query_tensor_map(q, total_q, c->shape.num_q_heads, c->shape.group, &tm_q) != 0)
+    return APAR_ERR_INVALID_ARG;        // (a query array that is not 16-byte aligned)
   apar_status rc = sync_device_tables(c, seg_slot.data(), n, st);
   if (rc) return rc;
   c->attn_book_seq = 0;                 // layer replays of a decode plan need a decode call
@@ -1596,9 +1606,6 @@ apar_status apar_tree_prefill_attention(apar_ctx* c, int32_t layer, int32_t n,
   a.d_error = (int*)c->ws(c->lay.err);
   a.num_sms = c->num_sms;
   a.d_ticket = (int*)c->ws(c->lay.ticket);
-  CUtensorMap tm_q;
-  if (make_query_tensor_map(q, total_q, c->shape.num_q_heads, G, &tm_q) != 0)
-    return APAR_ERR_INVALID_ARG;        // (a query array that is not 16-byte aligned)
 
   auto upload = [&](const void* src, size_t bytes, char* dst) -> apar_status {
     size_t done = 0;
@@ -1878,15 +1885,18 @@ size_t apar_weights_bytes(const apar_config* cfg) {
   return supported(cfg) && weights_fit(cfg) ? make_weights_layout(cfg).total : 0;
 }
 
-apar_status apar_attach_weights(apar_ctx* c, void* memory, size_t bytes) {
+apar_status apar_attach_weights(apar_ctx* c, void* memory, size_t bytes) try {
   if (!c || ((uintptr_t)memory & 255)) return APAR_ERR_INVALID_ARG;
   if (c->host_only || c->q4) return APAR_ERR_UNSUPPORTED;
   if (!weights_fit(&c->cfg)) return APAR_ERR_UNSUPPORTED;
   c->wlay = make_weights_layout(&c->cfg);
   if (memory && bytes < c->wlay.total) return APAR_ERR_WORKSPACE_TOO_SMALL;
+  if (memory) c->seen.reserve(c->cfg.max_threads);       // (queries of a call)
   c->weights = (char*)memory;
   c->seen_valid = c->key_plan_valid = false;
   return APAR_OK;
+} catch (...) {               // (the host's memory)
+  return APAR_ERR_INVALID_ARG;
 }
 
 apar_status apar_set_lse_output(apar_ctx* c, float* lse) {

@@ -811,3 +811,53 @@ def test_calls_while_capturing_are_refused():
     assert codes == ["INVALID_ARG"] * 3
     B.apar_check_invariants(f.s.ctx)
     f.check_rows(tids)
+
+
+def test_a_refused_attention_call_leaves_the_one_before_it():
+    """Queries of so many lengths that their partial results do not fit are refused; the weights, the layer
+    calls and the plan of the call before are then still there."""
+    f = Forest(8, 2, layers=2)
+    (a, b) = f.new(2)
+    f.append([a, b], [64 * 16, 40])
+    tids = f.fork([a, a]) + [b]
+    q = [rows(3, 8, 40 + l) for l in range(2)]
+    lse = [torch.empty(3, 8, device="cuda") for _ in range(2)]
+    plain = f.s.attention(tids, q[0], lse=lse[0])
+    plain1 = f.s.attention_layer(1, q[1], lse=lse[1])
+
+    def refused():
+        many = rows(64, 8, 44)
+        before = B.apar_get_stats(f.s.ctx)
+        with pytest.raises(B.AparError) as e:
+            f.s.prefix_attention([a] * 64, [16 * (i + 1) for i in range(64)], many)
+        assert e.value.code == "WORKSPACE_TOO_SMALL"
+        with pytest.raises(B.AparError) as e:            # (a prompt's queries that begin between boundaries)
+            B.apar_tree_prefill_attention(f.s.ctx, 0, [a], [0], [4], many.data_ptr() + 2, many.data_ptr(), SCALE)
+        assert e.value.code == "INVALID_ARG"
+        assert B.apar_get_stats(f.s.ctx) == before
+
+    refused()
+    f.s.add_weights(q[0], lse[0])                        # (its plan is made after the refusal)
+    rel = f.add(tids, q[0])[1]
+    refused()
+    f.s.add_weights(q[1], lse[1], layer=1)               # (and was there before it)
+    rel = max(rel, f.add(tids, q[1], 1)[1])
+    assert torch.equal(f.s.attention_layer(1, q[1]), plain1)
+    refused()
+    assert torch.equal(f.s.attention(tids, q[0]), plain)
+    for l in range(2):
+        f.check_weights([*tids, a], rel, l)
+    assert f.s.stats()["device_wait_timeouts"] == 0
+
+
+def test_prompt_attention_ends_what_weights_can_be_added():
+    f, tids = small_forest(8, 2)
+    q, lse = rows(len(tids), 8, 1), torch.empty(len(tids), 8, device="cuda")
+    f.s.attention(tids, q, lse=lse)
+    f.s.prefill_attention([tids[0]], [0], [4], rows(4, 8, 2))
+    with pytest.raises(B.AparError) as e:
+        f.s.add_weights(q, lse)
+    assert e.value.code == "INVALID_ARG"
+    f.s.attention(tids, q, lse=lse)
+    f.s.add_weights(q, lse)
+    f.check_weights(tids, f.add(tids, q)[1])
