@@ -108,6 +108,30 @@ __device__ __forceinline__ void wait_scores(uint32_t (&r)[32]) {
                :: "memory");
 }
 
+// Of `issued` copies through a ring of so many stages, the oldest that may still be in flight: a stage is only
+// filled again once its copy has been consumed.
+__host__ __device__ constexpr int oldest_in_flight(int issued, int stages) {
+  return issued > stages ? issued - stages : 0;
+}
+// Checked when this is compiled: whichever of those copies have not landed yet, waits for the parities of copies
+// oldest_in_flight .. issued - 1, in order, wait for each of them, and none waits for a copy nobody asked for.
+constexpr bool drain_waits_for_all(int stages) {
+  for (int issued = 0; issued < 4 * stages; ++issued)
+    for (unsigned missing = 0; missing < 1u << stages; ++missing) {   // bit of a stage: its last copy is on its way
+      unsigned left = missing;
+      for (int x = oldest_in_flight(issued, stages); x < issued; ++x) {
+        const int s = x % stages, filled = (issued - 1 - s) / stages + 1;
+        const int phase = filled - (left >> s & 1);                   // phases that the barrier has completed
+        const bool through = phase > 0 ? (phase - 1) % 2 == x / stages % 2 : x / stages % 2 == 1;
+        if (!through && !(left >> s & 1)) return false;               // (would run into its limit)
+        if (!through) left &= ~(1u << s);
+      }
+      if (left & ((1u << (issued < stages ? issued : stages)) - 1)) return false;
+    }
+  return true;
+}
+static_assert(drain_waits_for_all(2) && drain_waits_for_all(kQStages), "copies in flight at a give-up");
+
 // Units in the order they are dealt out: CTA b's i-th.
 __device__ __forceinline__ int64_t dealt(int64_t i) {
   return i * gridDim.x + (i & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
@@ -278,11 +302,13 @@ prompt_weights_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
       q_flags[st] = F_END;
       bar_arrive(bar(B_QFULL + st));
     }
-    // after a wait that gave up: the copies in flight are waited for (with a limit of their own)
+    // After a wait that gave up: the copies in flight are waited for (with a limit of their own).  On every way
+    // here query tiles 0 .. g - 1 and units 0 .. ku - 1 have been asked for, and no others; the end's word (ok)
+    // takes a stage as a tile does.
     if (*cta_abort && lane == 0) {
-      for (int x = max(0, g - kQStages); x < g; ++x)
+      for (int x = oldest_in_flight(ok ? g + 1 : g, kQStages); x < g; ++x)
         for (uint32_t i = 0; i < kSpin && !bar_try(bar(B_QFULL + x % kQStages), (x / kQStages) & 1); ++i) {}
-      for (int x = max(0, ku - 1); x <= ku; ++x)
+      for (int x = oldest_in_flight(ku, 2); x < ku; ++x)
         for (uint32_t i = 0; i < kSpin && !bar_try(bar(B_KFULL + (x & 1)), (x >> 1) & 1); ++i) {}
     }
   } else if (warp == kSumWarps + 1) {
