@@ -652,6 +652,8 @@ apar_status run_attention(apar_ctx* c, int n, const int32_t* qslots, const int32
       c->plan_epoch = c->struct_epoch;
       c->plan_attended = attended;
       c->plan_age = 0;
+    } else {
+      c->plan_tids.clear();               // (what lies on the device is no plan of a step)
     }
   } else {
     ++c->plan_age;

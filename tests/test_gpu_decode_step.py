@@ -253,3 +253,27 @@ def test_whole_step_of_all_layers_replayed_from_a_cuda_graph(hq, hkv):
         B.apar_note_step_replay(sess.ctx)
     assert sess.stats()["device_wait_timeouts"] == 0
     sess.close()
+
+
+def test_no_replay_after_attention_of_other_queries():
+    """A captured step follows the plan on the device.  One of prefixes, or of a thread listed twice, is not
+    the step's: a replay is refused until a call of the step's own list has made its plan again."""
+    from paper_2401_06761_b200 import binding as B
+    from paper_2401_06761_b200.session import PagedSession
+    shape = synth.LayerShape(8, 2)
+    sess = PagedSession(shape, 64, 8, 16, poison=True)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    tids = sess.new_threads(3)
+    sess.append(tids, [17, 18, 20], _rand((55, 2, 128), g), _rand((55, 2, 128), g))
+    k, v, q = _rand((3, 2, 128), g), _rand((3, 2, 128), g), _rand((3, 8, 128), g)
+    sess.decode_step(tids, k, v, q)
+    B.apar_note_step_replay(sess.ctx)                    # (nothing is replayed here: the host's side alone)
+    for other in (lambda: sess.prefix_attention(tids, [3, 4, 5], q),
+                  lambda: sess.attention([tids[0], tids[0], tids[1]], q)):
+        other()
+        with pytest.raises(B.AparError) as e:
+            B.apar_note_step_replay(sess.ctx)
+        assert e.value.code == "INVALID_ARG"
+        sess.attention(tids, q)
+        B.apar_note_step_replay(sess.ctx)
+    sess.close()
