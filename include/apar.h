@@ -346,7 +346,8 @@ apar_status apar_steps_before_new_block(apar_ctx* ctx, int32_t* steps_out /*[hos
 /* Host side of one replay of a captured apar_decode_step: every thread of the list is one token
  * longer, exactly what the replayed kernels do on the device.  Launches nothing.
  * Errors: INVALID_ARG if the step list or the plan is no longer the captured one (any
- * bookkeeping call since), or if a thread of the list would start a new block - make an
+ * bookkeeping call since, attention of other queries), if apar_add_weights has been captured on this
+ * context and none that was not has followed the attention call that made the plan, or if a thread of the list would start a new block - make an
  * ordinary apar_decode_step then, and capture again afterwards if block ids matter to the
  * graph (they do not: the captured kernels read tables and lengths from the device). */
 apar_status apar_note_step_replay(apar_ctx* ctx);
@@ -492,7 +493,8 @@ apar_status apar_reorder(apar_ctx* ctx, int32_t n, const int32_t* tid /*[host]*/
  *   library's own.  The caller owns the memory and may read and write the weights on the context's
  *   stream; those of rows that are cached when it is attached are what the memory holds. */
 size_t apar_weights_bytes(const apar_config* cfg /*[host]*/);
-/* memory [device] 256-byte aligned, or NULL to detach.
+/* memory [device] 256-byte aligned, or NULL to detach.  Graphs with calls below that were captured before may not be
+ * replayed after it.
  * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE_TOO_SMALL. */
 apar_status apar_attach_weights(apar_ctx* ctx, void* memory /*[device] or NULL*/, size_t bytes);
 /* From now on every attention call of this context also writes lse [device] float
@@ -510,7 +512,7 @@ apar_status apar_set_lse_output(apar_ctx* ctx, float* lse /*[device] or NULL*/);
  *   call and layer, its queries in its order.
  * The first call after an attention call that made a plan of its own uploads one too; others only
  * launch kernels and can be captured.  A captured call follows the plan that the most recent
- * uncaptured one left on the device.
+ * uncaptured one left on the device; apar_note_step_replay refuses where that is of other queries.
  * Errors: INVALID_ARG (also: no memory attached, bookkeeping or apar_tree_prefill_attention since
  * that attention call, a verification, an upload while the stream is capturing), UNSUPPORTED,
  * WORKSPACE_TOO_SMALL, CUDA. */

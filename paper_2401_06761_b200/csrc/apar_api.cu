@@ -179,6 +179,7 @@ struct apar_ctx {
   std::vector<Seen> seen;
   bool seen_valid = false, key_plan_valid = false;   // (they describe / the units on the device are of)
   KeyPlan key_plan = {};                             // that call
+  bool key_captured = false;                         // a graph follows the units on the device
   // thread list of the most recent apar_decode_step; its table rows are resident on the device
   std::vector<int32_t> step_tids, step_slots, tmp_slots;
   bool step_valid = false;
@@ -1308,7 +1309,7 @@ apar_status apar_note_step_replay(apar_ctx* c) {
   // the device-resident plan and step list must be the ones the replayed kernels were
   // captured with, and no thread may need a block (the captured step carries none)
   if (!step_list_current(c) || c->attn_book_seq != c->book_seq || c->plan.items.empty() ||
-      c->plan_tids != c->step_tids)
+      c->plan_tids != c->step_tids || (c->key_captured && !c->key_plan_valid))
     return APAR_ERR_INVALID_ARG;
   for (int32_t s : c->step_slots)
     if ((c->slots[s].len & (kBlock - 1)) == 0) return APAR_ERR_INVALID_ARG;
@@ -1895,7 +1896,7 @@ apar_status apar_attach_weights(apar_ctx* c, void* memory, size_t bytes) try {
   if (memory && bytes < c->wlay.total) return APAR_ERR_WORKSPACE_TOO_SMALL;
   if (memory) c->seen.reserve(c->cfg.max_threads);       // (queries of a call)
   c->weights = (char*)memory;
-  c->seen_valid = c->key_plan_valid = false;
+  c->seen_valid = c->key_plan_valid = c->key_captured = false;   // (graphs of the old memory end with it)
   return APAR_OK;
 } catch (...) {               // (the host's memory)
   return APAR_ERR_INVALID_ARG;
@@ -1940,6 +1941,7 @@ apar_status apar_add_weights(apar_ctx* c, int32_t layer, const void* q, const fl
   APAR_CUDA(c, cudaStreamIsCapturing(st, &cap));
   APAR_CUDA(c, launch_key_weights(key_args(c, c->wlay.plan, layer, q, lse, sm_scale, replace),
                                   c->key_plan.n_units, cap != cudaStreamCaptureStatusNone, st));
+  c->key_captured |= cap != cudaStreamCaptureStatusNone;
   for (int n : c->key_plan.n_units) c->kernels_total += n > 0 || cap != cudaStreamCaptureStatusNone;
   return APAR_OK;
 } catch (...) {               // (the host's memory)

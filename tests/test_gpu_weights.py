@@ -861,3 +861,43 @@ def test_prompt_attention_ends_what_weights_can_be_added():
     f.s.attention(tids, q, lse=lse)
     f.s.add_weights(q, lse)
     f.check_weights(tids, f.add(tids, q)[1])
+
+
+def test_no_replay_over_other_queries_weights():
+    """A captured apar_add_weights follows the units on the device: while those are another call's (whose
+    queries may be more than the captured call has), no replay is announced."""
+    f, tids = small_forest(8, 2)
+    f.append(tids, [16 - len(f.names[t]) % 16 + 1 for t in tids])
+    some = tids[:2]
+    q, k = rows(2, 8, 50), rows(2, 2, 51)
+    lse, out = torch.empty(2, 8, device="cuda"), torch.empty_like(q)
+    all_q, all_lse = rows(len(tids), 8, 52), torch.empty(len(tids), 8, device="cuda")
+
+    def step():
+        f.s.decode_step(some, k, k, q, out=out, lse=lse)
+        f.s.add_weights(q, lse)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            step()
+        g.replay()
+        B.apar_note_step_replay(f.s.ctx)
+        g.replay()
+        f.s.attention(tids, all_q, lse=all_lse)
+        f.s.add_weights(all_q, all_lse)
+        f.s.attention(some, q, lse=lse)                  # the step's plan again, but not its weights'
+        with pytest.raises(B.AparError) as e:
+            B.apar_note_step_replay(f.s.ctx)
+        assert e.value.code == "INVALID_ARG"
+        f.s.add_weights(q, lse)
+        B.apar_note_step_replay(f.s.ctx)
+        g.replay()
+        side.synchronize()
+    # of every query each kv head's weights sum up to its heads: four steps and an attention call of two
+    # threads, one call of all (a weight is off by less than 1e-4 of itself, see Forest.add)
+    total = f.s.weights[0].nan_to_num(0).double().sum((0, 2)).cpu().numpy()
+    assert np.abs(total - 4 * (5 * 2 + len(tids))).max() <= 4 * (10 + len(tids)) * 1e-4
