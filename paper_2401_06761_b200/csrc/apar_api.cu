@@ -274,6 +274,17 @@ int32_t alloc_block(apar_ctx* c) {
   return b;
 }
 
+// Room for `most` entries, so that adding up to there cannot run out of memory.
+template <typename T>
+void make_room(std::vector<T>& v, size_t most) {
+  if (v.capacity() < most) v.reserve(std::max(most, 2 * v.capacity()));
+}
+// Room for so many more groups, in use or given back.
+void make_room_for_groups(apar_ctx* c, size_t more) {
+  make_room(c->gid_ref, c->gid_ref.size() + more);
+  make_room(c->gid_free, c->gid_ref.size() + more);
+}
+
 int32_t new_gid(apar_ctx* c) {
   int32_t g;
   if (!c->gid_free.empty()) {
@@ -827,23 +838,39 @@ KeyArgs key_args(apar_ctx* c, size_t plan, int layer, const void* q, const float
 }
 
 // Every thread that lists group `gid` lists it as two groups from now on, cut at table position `pos`
-// (all see it at the same positions).  Nothing happens where `pos` is an end of the group.
+// (all see it at the same positions).  Nothing happens where `pos` is an end of the group, nor, but for the
+// exception, where memory runs out; there is room for a group more.
 void split_group(apar_ctx* c, int32_t gid, int32_t pos) {
   int32_t rest = -1;
-  for (std::vector<BlockRun>& rs : c->runs)
-    for (size_t k = 0; k < rs.size(); ++k) {
-      if (rs[k].gid != gid) continue;
-      const int32_t first = pos - rs[k].pos;
-      if (first <= 0 || first >= rs[k].n) return;
-      if (rest < 0) {
-        rest = new_gid(c);
-        c->gid_ref[rest] = c->gid_ref[gid];
+  try {
+    for (std::vector<BlockRun>& rs : c->runs)
+      for (size_t k = 0; k < rs.size(); ++k) {
+        if (rs[k].gid != gid) continue;
+        const int32_t first = pos - rs[k].pos;
+        if (first <= 0 || first >= rs[k].n) return;
+        make_room(rs, rs.size() + 1);
+        if (rest < 0) {
+          rest = new_gid(c);
+          c->gid_ref[rest] = c->gid_ref[gid];
+        }
+        const BlockRun second{rest, pos, rs[k].n - first};
+        rs[k].n = first;
+        rs.insert(rs.begin() + k + 1, second);
+        break;
       }
-      const BlockRun second{rest, pos, rs[k].n - first};
-      rs[k].n = first;
-      rs.insert(rs.begin() + k + 1, second);
-      break;
-    }
+  } catch (...) {
+    if (rest < 0) throw;
+    for (std::vector<BlockRun>& rs : c->runs)
+      for (size_t k = 1; k < rs.size(); ++k) {
+        if (rs[k].gid != rest) continue;
+        rs[k - 1].n += rs[k].n;
+        rs.erase(rs.begin() + k);
+        break;
+      }
+    c->gid_ref[rest] = 0;
+    c->gid_free.push_back(rest);
+    throw;
+  }
 }
 void split_groups_of(apar_ctx* c, int slot, int32_t pos) {
   for (const BlockRun& r : c->runs[slot])
@@ -1809,6 +1836,23 @@ apar_status apar_reorder(apar_ctx* c, int32_t n, const int32_t* tid, const int32
   if (same) return APAR_OK;
   if (need > (int64_t)c->free_stack.size()) return APAR_ERR_NO_BLOCKS;
   if ((size_t)need * sizeof(CowCopy) > c->lay.stage_cap) return APAR_ERR_WORKSPACE_TOO_SMALL;
+  // what the dropped rows held, to be given back at the end
+  std::vector<std::vector<int32_t>> old_blocks(dropped.size());
+  std::vector<BlockRun> old_runs;
+  for (size_t d = 0; d < dropped.size(); ++d) {
+    const int s = dropped[d];
+    old_blocks[d].assign(c->row(s), c->row(s) + c->slots[s].n_blocks);
+    old_runs.insert(old_runs.end(), c->runs[s].begin(), c->runs[s].end());
+  }
+  // (a fork may cut its source's last group in two, and opens a group of its own)
+  make_room_for_groups(c, 2 * (size_t)forks);
+  size_t used = 0;
+  for (int i = 0; i < n; ++i) {
+    if (row_of[i] >= 0) continue;
+    std::vector<BlockRun>& from = c->runs[slot_of(c, source_tid[i])];
+    make_room(from, from.size() + 1);
+    make_room(c->runs[dropped[used++]], from.size() + 2);
+  }
   Staging* stg = nullptr;
   if (need && !c->host_only) {
     apar_status rc = refuse_capture(c, st);
@@ -1817,18 +1861,13 @@ apar_status apar_reorder(apar_ctx* c, int32_t n, const int32_t* tid, const int32
     if (rc) return rc;
   }
   CowCopy* copies = stg ? (CowCopy*)stg->host : nullptr;
-  // what the dropped rows held, to be given back at the end
-  std::vector<std::vector<int32_t>> old_blocks(dropped.size());
-  std::vector<BlockRun> old_runs;
-  for (size_t d = 0; d < dropped.size(); ++d) {
-    const int s = dropped[d];
-    old_blocks[d].assign(c->row(s), c->row(s) + c->slots[s].n_blocks);
-    old_runs.insert(old_runs.end(), c->runs[s].begin(), c->runs[s].end());
+  // ---- from here on nothing runs out of memory
+  for (int s : dropped) {
     c->runs[s].clear();
     c->own_open[s] = 0;
   }
   int nc = 0;
-  size_t used = 0;
+  used = 0;
   for (int i = 0; i < n; ++i) {
     if (row_of[i] >= 0) continue;
     const int ps = slot_of(c, source_tid[i]), cs = dropped[used++];
@@ -2125,19 +2164,38 @@ apar_status apar_evict(apar_ctx* c, int32_t n, const int32_t* tid, const int32_t
   std::vector<int32_t> slots;
   for (const Stretch& x : st_list) slots.push_back(slot_of(c, tid[x.first]));
   apar_status rc = APAR_OK;
+  if (!c->host_only && (rc = refuse_capture(c, st))) return rc;
+  std::vector<EvictEntry> entries;
+  std::vector<int32_t> dst, dst_of(st_list.size(), 0);
+  entries.reserve(st_list.size());
+  dst.reserve((size_t)need);
+  if (c->track_runs) {
+    // groups end where the stretches do, for every thread that lists the blocks: three cuts and a new group a
+    // stretch, at most.  (A group in two pieces is as good as a whole one, should the call end here.)
+    make_room_for_groups(c, 4 * st_list.size());
+    for (size_t k = 0; k < st_list.size(); ++k) {
+      const int f = st_list[k].first, b0 = begin[f] / kBlock;
+      split_groups_of(c, slots[k], b0);
+      if (!st_list[k].in_place) continue;
+      split_groups_of(c, slots[k], b0 + blocks_of(keep[f]));
+      split_groups_of(c, slots[k], blocks_of(end[f]));
+    }
+    for (int i = 0; i < n; ++i)
+      if (stretch_of[i] >= 0) {
+        std::vector<BlockRun>& rs = c->runs[slot_of(c, tid[i])];
+        make_room(rs, rs.size() + 1);
+      }
+  }
   Staging* stg = nullptr;
   if (!c->host_only) {
-    rc = refuse_capture(c, st);
-    if (rc == APAR_OK) rc = sync_device_tables(c, slots.data(), (int)slots.size(), st);
+    rc = sync_device_tables(c, slots.data(), (int)slots.size(), st);
     if (rc == APAR_OK && !few_go) rc = acquire(c, &stg);
     if (rc) return rc;
   }
-  std::vector<EvictEntry> entries;
-  std::vector<int32_t> dst;
+  // ---- from here on nothing runs out of memory
   const int lh = c->num_layers * c->cfg.num_kv_heads;
   int32_t max_rows = 0, max_len = 0;
   int64_t list = 0;
-  std::vector<int32_t> dst_of(st_list.size(), 0);
   for (size_t k = 0; k < st_list.size(); ++k) {
     const Stretch& x = st_list[k];
     const int f = x.first, rows = end[f] - begin[f];
@@ -2161,13 +2219,6 @@ apar_status apar_evict(apar_ctx* c, int32_t n, const int32_t* tid, const int32_t
     std::vector<BlockRun>& rs = c->runs[s];
     const bool first = i == x.first;
     if (c->track_runs) {
-      if (first) {                                       // (for every thread that lists the blocks)
-        split_groups_of(c, s, b0);
-        if (x.in_place) {
-          split_groups_of(c, s, b0 + kb);
-          split_groups_of(c, s, b1);
-        }
-      }
       const int32_t gone0 = x.in_place ? b0 + kb : b0;
       size_t w = 0;
       for (size_t k = 0; k < rs.size(); ++k) {
