@@ -1737,13 +1737,14 @@ apar_status apar_read_kv(apar_ctx* c, int32_t layer, int32_t n, const int32_t* t
     return APAR_ERR_INVALID_ARG;
   if (c->host_only) return APAR_ERR_UNSUPPORTED;
   cudaStream_t st = (cudaStream_t)cuda_stream;
-  int64_t rows = 0;
+  int64_t rows = 0, pieces = 0;         // (of blocks)
   for (int i = 0; i < n; ++i) {
     const int s = slot_of(c, tid[i]);
     if (s < 0) return APAR_ERR_BAD_THREAD;
     if (begin[i] < 0 || count[i] < 0 || (int64_t)begin[i] + count[i] > c->slots[s].len)
       return APAR_ERR_INVALID_ARG;
     rows += count[i];
+    if (count[i]) pieces += (begin[i] + count[i] - 1) / kBlock - begin[i] / kBlock + 1;
   }
   if (rows == 0) return APAR_OK;        // (the outputs may then be empty, without an address)
   if (!k_out || !v_out || (((uintptr_t)k_out | (uintptr_t)v_out) & 15)) return APAR_ERR_INVALID_ARG;
@@ -1755,12 +1756,46 @@ apar_status apar_read_kv(apar_ctx* c, int32_t layer, int32_t n, const int32_t* t
   }
   const char* kp = (const char*)c->cfg.k_pool + (size_t)layer * c->layer_bytes;
   const char* vp = (const char*)c->cfg.v_pool + (size_t)layer * c->layer_bytes;
-  // Pieces of blocks: a few of them travel with the launch, more of them through the staging area (28.8 k rows
-  // listed one by one took 7 to 10 us to upload, their pieces take 4).
+  // Few pieces of blocks travel with the launch; many go through the staging area, row by row, or piece by piece
+  // where that is a shorter upload and hardly more CTAs: a piece has those of a whole block, and with many heads
+  // the kernel that finds rows in the list is the faster one anyway.  (Rows and pieces, bf16: 4096 threads' last
+  // rows, 8 heads 15 and 31 us, 40 heads 35 and 119; 4096 x 8 rows, 8 heads 53 and 59; 2000 x 24 of two blocks,
+  // 8 heads 74 and 70; 32 x 900 rows, 2 heads 21 and 17, 8 heads 48 and 45, 40 heads 190 and 190; 2000 x 56, 8
+  // heads 160 and 155, 16 heads 298 and 306, 40 heads 710 and 743; 4 bits, 32 heads 513 and 647.)
+  char* d_stage = c->ws(c->lay.stage);
+  if (pieces > ReadPieces::kMax && (rows < 12 * pieces || c->cfg.num_kv_heads > 8)) {
+    const int64_t cap_rows = (int64_t)(c->lay.stage_cap / 4);
+    int64_t first_row = 0;
+    int i = 0;
+    int32_t done = 0;                   // rows of entry i already listed
+    while (first_row < rows) {
+      Staging* stg;
+      apar_status rc = acquire(c, &stg);
+      if (rc) return rc;
+      int32_t* list = (int32_t*)stg->host;
+      int64_t filled = 0;
+      while (i < n && filled < cap_rows) {
+        const int32_t* tab = c->row(slot_of(c, tid[i]));
+        for (; done < count[i] && filled < cap_rows; ++done) {
+          const int32_t pos = begin[i] + done;
+          list[filled++] = tab[pos / kBlock] * kBlock + pos % kBlock;
+        }
+        if (done < count[i]) break;
+        ++i;
+        done = 0;
+      }
+      rc = send(c, stg, d_stage, (size_t)filled * 4, st);
+      if (rc) return rc;
+      APAR_CUDA(c, launch_read_rows(c->q4, kp, vp, k_out, v_out, (const int32_t*)d_stage, first_row,
+                                    (int)filled, c->cfg.num_kv_heads, st));
+      ++c->kernels_total;
+      first_row += filled;
+    }
+    return APAR_OK;
+  }
   ReadPieces few;
   ReadPiece* list = few.p;
   Staging* stg = nullptr;
-  char* d_stage = c->ws(c->lay.stage);
   const int cap = (int)std::min<size_t>(c->lay.stage_cap / sizeof(ReadPiece), 1 << 20);
   int64_t out = 0;
   int filled = 0;
@@ -1770,8 +1805,8 @@ apar_status apar_read_kv(apar_ctx* c, int32_t layer, int32_t n, const int32_t* t
       if (rc) return rc;
     }
     const ReadPiece* many = stg ? (const ReadPiece*)d_stage : nullptr;
-    APAR_CUDA(c, launch_read_rows(c->q4, kp, vp, k_out, v_out, few, many, filled,
-                                  c->cfg.num_kv_heads, st));
+    APAR_CUDA(c, launch_read_pieces(c->q4, kp, vp, k_out, v_out, few, many, filled,
+                                    c->cfg.num_kv_heads, st));
     ++c->kernels_total;
     stg = nullptr;
     filled = 0;

@@ -240,8 +240,12 @@ struct ReadPieces {              // (as a kernel's argument)
   ReadPiece p[kMax];
 };
 // n pieces of a pool as bf16; at `many` (device), or where that is NULL the first n of `few`.
+cudaError_t launch_read_pieces(bool q4, const void* k_pool, const void* v_pool, void* k_out,
+                               void* v_out, const ReadPieces& few, const ReadPiece* many, int n,
+                               int num_kv_heads, cudaStream_t st);
+// Rows d_slots[0..n_rows) (16 * block + row) of a pool as bf16, to rows first_row.. of k_out and v_out.
 cudaError_t launch_read_rows(bool q4, const void* k_pool, const void* v_pool, void* k_out,
-                             void* v_out, const ReadPieces& few, const ReadPiece* many, int n,
+                             void* v_out, const int32_t* d_slots, int64_t first_row, int n_rows,
                              int num_kv_heads, cudaStream_t st);
 // The items of a plan made with mma_min_rows = 1, reordered by width: n_wide with more than kQ4Rows
 // rows (tcgen05 kernel), n_mid, n_narrow with at most kQ4NarrowRows (both warp-stream kernel).

@@ -194,23 +194,13 @@ __global__ void __launch_bounds__(256) q4_row_move_kernel(uint8_t* __restrict__ 
 }
 
 // ------------------------------------------------------------------ rows read back as bf16
-// One thread per sixteen dims of a row; blockIdx.y selects K or V, blockIdx.z which 32 of a piece's
-// (row, head) pairs.  A 4-bit row reads as bf16(lo + s * c), the sum taken in 32 bits and rounded once
-// more to the output's type.
+// One thread per sixteen dims of a row; blockIdx.y selects K or V.  A 4-bit row reads as bf16(lo + s * c), the sum
+// taken in 32 bits and rounded once more to the output's type.
 template <bool kQ4>
-__global__ void __launch_bounds__(256) read_rows_kernel(const uint8_t* __restrict__ k_pool,
-                                                        const uint8_t* __restrict__ v_pool,
-                                                        uint4* __restrict__ k_out,
-                                                        uint4* __restrict__ v_out,
-                                                        const __grid_constant__ ReadPieces few,
-                                                        const ReadPiece* __restrict__ many,
-                                                        int num_kv_heads) {
-  const ReadPiece p = many ? many[blockIdx.x] : few.p[blockIdx.x];
-  const int rh = blockIdx.z * (blockDim.x / 8) + (threadIdx.x >> 3);
-  if (rh >= p.count * num_kv_heads) return;
+__device__ __forceinline__ void read_row(const uint8_t* __restrict__ k_pool, const uint8_t* __restrict__ v_pool,
+                                         uint4* __restrict__ k_out, uint4* __restrict__ v_out, size_t tile, int row,
+                                         int64_t out_row) {
   const int c = threadIdx.x & 7;
-  const int r = rh / num_kv_heads, h = rh - r * num_kv_heads, row = p.row + r;
-  const size_t tile = (size_t)p.block * num_kv_heads + h;
   const uint8_t* pool = blockIdx.y ? v_pool : k_pool;
   uint4 out[2];
 #pragma unroll
@@ -230,9 +220,37 @@ __global__ void __launch_bounds__(256) read_rows_kernel(const uint8_t* __restric
       out[i] = ((const uint4*)pool)[(tile * kBlock + row) * 16 + 2 * c + i];
     }
   }
-  uint4* dst = (blockIdx.y ? v_out : k_out) + (p.out * num_kv_heads + rh) * 16 + 2 * c;
+  uint4* dst = (blockIdx.y ? v_out : k_out) + out_row * 16 + 2 * c;
   dst[0] = out[0];
   dst[1] = out[1];
+}
+// By pieces of blocks; blockIdx.z selects which 32 of a piece's (row, head) pairs.
+template <bool kQ4>
+__global__ void __launch_bounds__(256) read_pieces_kernel(const uint8_t* __restrict__ k_pool,
+                                                          const uint8_t* __restrict__ v_pool,
+                                                          uint4* __restrict__ k_out, uint4* __restrict__ v_out,
+                                                          const __grid_constant__ ReadPieces few,
+                                                          const ReadPiece* __restrict__ many, int num_kv_heads) {
+  const ReadPiece p = many ? many[blockIdx.x] : few.p[blockIdx.x];
+  const int rh = blockIdx.z * (blockDim.x / 8) + (threadIdx.x >> 3);
+  if (rh >= p.count * num_kv_heads) return;
+  const int r = rh / num_kv_heads, h = rh - r * num_kv_heads;
+  read_row<kQ4>(k_pool, v_pool, k_out, v_out, (size_t)p.block * num_kv_heads + h, p.row + r,
+                p.out * num_kv_heads + rh);
+}
+// By rows: row i of the list, (block, row of it), goes to row first_row + i.
+template <bool kQ4>
+__global__ void __launch_bounds__(256) read_rows_kernel(const uint8_t* __restrict__ k_pool,
+                                                        const uint8_t* __restrict__ v_pool,
+                                                        uint4* __restrict__ k_out, uint4* __restrict__ v_out,
+                                                        const int32_t* __restrict__ slots, int64_t first_row,
+                                                        int n_rows, int num_kv_heads) {
+  const uint32_t rh = blockIdx.x * (blockDim.x / 8) + (threadIdx.x >> 3);   // (row, head) < 2^31
+  if (rh >= (uint32_t)n_rows * (uint32_t)num_kv_heads) return;
+  const int r = (int)(rh / (uint32_t)num_kv_heads), h = (int)(rh - (uint32_t)r * (uint32_t)num_kv_heads);
+  const int slot = slots[r];
+  read_row<kQ4>(k_pool, v_pool, k_out, v_out, (size_t)(slot >> 4) * num_kv_heads + h, slot & 15,
+                first_row * num_kv_heads + rh);
 }
 
 }  // namespace
@@ -265,14 +283,26 @@ cudaError_t launch_q4_row_moves(void* k_pool, void* v_pool, const RowMove* d_mov
   return cudaGetLastError();
 }
 
-cudaError_t launch_read_rows(bool q4, const void* k_pool, const void* v_pool, void* k_out,
-                             void* v_out, const ReadPieces& few, const ReadPiece* many, int n,
-                             int num_kv_heads, cudaStream_t st) {
+cudaError_t launch_read_pieces(bool q4, const void* k_pool, const void* v_pool, void* k_out,
+                               void* v_out, const ReadPieces& few, const ReadPiece* many, int n,
+                               int num_kv_heads, cudaStream_t st) {
   if (n <= 0) return cudaSuccess;
   const dim3 grid(n, 2, (kBlock * num_kv_heads + 31) / 32);
-  auto kernel = q4 ? read_rows_kernel<true> : read_rows_kernel<false>;
+  auto kernel = q4 ? read_pieces_kernel<true> : read_pieces_kernel<false>;
   kernel<<<grid, 256, 0, st>>>((const uint8_t*)k_pool, (const uint8_t*)v_pool, (uint4*)k_out,
                                (uint4*)v_out, few, many, num_kv_heads);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_read_rows(bool q4, const void* k_pool, const void* v_pool, void* k_out,
+                             void* v_out, const int32_t* d_slots, int64_t first_row, int n_rows,
+                             int num_kv_heads, cudaStream_t st) {
+  if (n_rows <= 0) return cudaSuccess;
+  const int64_t total = (int64_t)n_rows * num_kv_heads * 8;
+  const dim3 grid((unsigned)((total + 255) / 256), 2);
+  auto kernel = q4 ? read_rows_kernel<true> : read_rows_kernel<false>;
+  kernel<<<grid, 256, 0, st>>>((const uint8_t*)k_pool, (const uint8_t*)v_pool, (uint4*)k_out,
+                               (uint4*)v_out, d_slots, first_row, n_rows, num_kv_heads);
   return cudaGetLastError();
 }
 

@@ -585,3 +585,23 @@ def test_the_current_stream_with_and_without_the_short_way(monkeypatch):
         assert PagedSession._stream() == torch.cuda.current_stream().cuda_stream
         with torch.cuda.stream(stream):
             assert PagedSession._stream() == stream.cuda_stream
+
+
+@pytest.mark.parametrize("fmt", ["q4", "bf16"])
+@pytest.mark.parametrize("heads,entries,begin,count", [(1, 70001, 14, 4), (3, 129, 0, 1), (8, 5000, 9, 8),
+                                                       (10, 300, 5, 90)])
+def test_read_kv_of_many_short_pieces_and_many_heads(fmt, heads, entries, begin, count):
+    """Lists of rows: more than one upload holds, entries that cross blocks, whole blocks of many heads."""
+    sess = PagedSession(LayerShape(heads, heads), 64, 4, 16, kv_format=fmt)
+    tids = sess.new_threads(3)
+    n = 140
+    k, v = rows(3 * n, heads, 240), rows(3 * n, heads, 241)
+    sess.append(tids, [n] * 3, k, v)
+    want = [torch.from_numpy(_expect_rows(x)).to(torch.bfloat16).cuda() if fmt == "q4" else x for x in (k, v)]
+    who = [i % 3 for i in range(entries)]
+    first = [begin + i % 31 for i in range(entries)]
+    got = sess.read_kv([tids[i] for i in who], first, [count] * entries)
+    at = (torch.tensor(who) * n + torch.tensor(first))[:, None] + torch.arange(count)
+    for g, w in zip(got, want):
+        assert torch.equal(g, w[at.flatten().cuda()])
+    sess.close()
