@@ -563,7 +563,7 @@ apar_status apar_evict(apar_ctx* ctx, int32_t n, const int32_t* tid /*[host]*/,
  *     score[b] + x[b][v] - log sum_u exp(x[b][u]),      x the beam's row of logits.
  * Chosen are the num_select pairs of the highest values over all beams and the whole vocabulary,
  * highest first; of equal values the lower beam's, then the lower token.  Values are compared in 64
- * bits; each sum of exponentials is taken in 32. */
+ * bits; sums of exponentials are off by less than 10^-5 of themselves, however long the rows. */
 enum {
   APAR_LOGITS_BF16 = 0,
   APAR_LOGITS_F16 = 1,

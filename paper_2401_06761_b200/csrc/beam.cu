@@ -7,7 +7,7 @@
 //
 // beam_scan_kernel   one CTA per piece of a row.  A thread goes over its elements a step of 16 at a time,
 //     sixteen bytes to a load where the row begins on such a boundary, the next step's on their way
-//     meanwhile, and keeps the largest, the sum of 2^((x - it) log2 e) and, in shared memory, each step's
+//     meanwhile, and keeps the largest, a sum of 2^((x - a reference) log2 e) and, in shared memory, each step's
 //     largest.  Which thread holds which element, and so the order of the sums, depends on the element
 //     alone: equal rows tie exactly.  A threshold that at least num_select elements reach comes from the
 //     threads' maxima: with j = num_select / 8 rounded up, the least of the eight warps' j-th largest.
@@ -323,10 +323,13 @@ __global__ void __launch_bounds__(kThreads, Packs<T>::kCtas) beam_scan_kernel(co
     return;
   }
   if (threadIdx.x == 0) n_cand = n_hit = 0;
-  // ---- this thread's elements: the largest, and the sum of 2^((x - it) log2 e).  (The difference first: no
-  // logit is too large or, as the lowest number of its type, too small for it.)
-  float mine = -INFINITY;
+  // ---- this thread's elements: the largest, and the sum of 2^((x - ref) log2 e).  (The difference first: no
+  // logit is too large or, as the lowest number of its type, too small for it.)  The reference follows the
+  // largest once that is 8 above it, so that a slowly rising row's sum is not scaled, and rounded, at every
+  // step; 128 terms at most are added up in 32 bits, in two sums, and their totals in 64, however long the row.
+  float mine = -INFINITY, ref = -INFINITY;
   u64 part = 0;                                // two sums
+  double total = 0.0;
   const u64 scale = pair_of(kLog2e, kLog2e);
   auto load = [&](uint4 (&v)[kHeld], int c0) { load_packs<T, kThreads>(v, x, n_in, c0 + threadIdx.x); };
   const int steps = (end - begin + kChunk - 1) / kChunk, of_slot = (steps + kSlots - 1) / kSlots;
@@ -339,16 +342,19 @@ __global__ void __launch_bounds__(kThreads, Packs<T>::kCtas) beam_scan_kernel(co
       W::numbers(v[k], e);
       peak = largest(peak, e);
     }
-    const float now = fmaxf(mine, peak);
+    mine = fmaxf(mine, peak);
+    if (mine > ref + 8.f) {
+      const float less = ref == -INFINITY ? 0.f : ex2((ref - mine) * kLog2e);
+      part = mul2(part, pair_of(less, less));
+      total *= less;
+      ref = mine;
+    }
     if (--left == 0) {
       peaks[slot++][threadIdx.x] = peak;
       peak = -INFINITY;
       left = of_slot;
     }
-    const float less = mine == -INFINITY ? 0.f : ex2((mine - now) * kLog2e);
-    part = mul2(part, pair_of(less, less));
-    mine = now;
-    const float from = now == -INFINITY ? 0.f : now;
+    const float from = ref == -INFINITY ? 0.f : ref;
     const u64 minus = pair_of(-from, -from);
 #pragma unroll
     for (int k = 0; k < kHeld; ++k) {
@@ -361,6 +367,10 @@ __global__ void __launch_bounds__(kThreads, Packs<T>::kCtas) beam_scan_kernel(co
       }
     }
   };
+  auto fold = [&]() {
+    total += (double)parts_of(part).x + (double)parts_of(part).y;
+    part = 0;
+  };
   uint4 v0[kHeld], v1[kHeld];                  // one on its way while the other is added
   load(v0, begin);
 #pragma unroll 1
@@ -370,6 +380,7 @@ __global__ void __launch_bounds__(kThreads, Packs<T>::kCtas) beam_scan_kernel(co
     if (c0 + kChunk >= end) break;
     if (c0 + 2 * kChunk < end) load(v0, c0 + 2 * kChunk);
     add(v1);
+    if (((c0 - begin) & 7 * kChunk) == 6 * kChunk) fold();   // (after eight steps)
   }
   if (left != of_slot) peaks[slot++][threadIdx.x] = peak;
   // ---- the threads together
@@ -382,8 +393,9 @@ __global__ void __launch_bounds__(kThreads, Packs<T>::kCtas) beam_scan_kernel(co
         if (at < kCand) hit[at] = (uint16_t)(k * kThreads + threadIdx.x);
       }
   const float top = unordered(most);
-  float sum = parts_of(part).x + parts_of(part).y;
-  if (mine != top) sum *= ex2((mine - top) * kLog2e);
+  fold();
+  float sum = (float)total;
+  if (ref != top) sum *= ex2((ref - top) * kLog2e);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
   if (lane == 0) sums[warp] = sum;

@@ -260,3 +260,44 @@ def test_same_bits_every_time():
     for _ in range(5):
         for u, v in zip(first, sel(x, s)):
             assert torch.equal(u, v)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_sums_of_very_long_rows(dtype):
+    """Rows of 2^22 logits in two pieces: a thread adds up 8192 exponentials, all but a few of them the same, so
+    that in a running 32-bit sum they round the same way (off by up to 1e-4 in the end).  LSE_TOL holds: no
+    more than 64 are added up one after the other in 32 bits."""
+    vocab, beams = 1 << 22, 64
+    x = torch.empty(1, beams, vocab, dtype=dtype, device="cuda")
+    low = -(torch.arange(beams, device="cuda") + 1).to(dtype) / 64           # (exact)
+    x[:] = low[None, :, None]
+    zeros = 0
+    for at in range(0, vocab, vocab // 4):
+        x[:, :, at:at + 65536] = 0
+        zeros += 65536
+    select = BeamSelect(beams, vocab, 3)
+    for b in range(0, beams, 3):
+        s = torch.full((1, beams), -float("inf"), device="cuda")
+        s[0, b] = 0.0
+        best, beam, token = select(x, s)
+        want = -np.log(zeros + (vocab - zeros) * np.exp(-(b + 1) / 64))
+        assert beam.tolist() == [[b] * 3] and token.tolist() == [[0, 1, 2]]
+        got = best.double().cpu().numpy()
+        assert np.abs(got - want).max() <= LSE_TOL + abs(want) * 2.0 ** -24, (b, got - want)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("rise", [0.01, 3.0, 9.0])
+def test_rows_that_rise_with_every_step(rise, dtype):
+    """The reference of a thread's sum moves a little, by steps, or at each: rows of 100003 logits in one piece."""
+    vocab, rows = 100003, 1500
+    at = torch.arange(vocab, device="cuda")
+    x = ((at // 1024) * rise - (at % 1024) / 512.0).to(dtype).expand(rows // 4, 4, vocab)
+    scores = -0.3 * torch.arange(4, device="cuda", dtype=torch.float32).expand(rows // 4, 4).contiguous()
+    best, beam, token = BeamSelect(4, vocab, 5)(x.contiguous(), scores)
+    assert all(torch.equal(t, t[:1].expand_as(t)) for t in (best, beam, token))
+    value = reference(x[:1], scores[:1], None, None)[0]
+    order = np.lexsort((np.arange(4 * vocab), -value))[:5]
+    assert beam[0].tolist() == (order // vocab).tolist() and token[0].tolist() == (order % vocab).tolist()
+    tol = LSE_TOL + np.abs(value[order]) * 2.0 ** -24
+    assert np.all(np.abs(best[0].cpu().numpy() - value[order]) <= tol)
