@@ -2326,7 +2326,7 @@ apar_status apar_evict(apar_ctx* c, int32_t n, const int32_t* tid, const int32_t
   a.layer_floats = c->layer_weights();
   a.moves = (int2*)(c->weights + c->wlay.moves);
   a.counts = (int32_t*)(c->weights + c->wlay.counts);
-  APAR_CUDA(c, launch_evict(a, few, (int)entries.size(), c->num_layers, max_len, max_rows, st));
+  APAR_CUDA(c, launch_evict(a, few, (int)entries.size(), c->num_layers, max_len, max_rows, c->num_sms, st));
   c->kernels_total += 2;
   return APAR_OK;
 } catch (...) {               // (the host's memory)

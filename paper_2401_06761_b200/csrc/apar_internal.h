@@ -326,11 +326,12 @@ struct EvictEntry {
   int32_t dst_begin, list_rows, pad;
   int64_t list_begin;
 };
-struct EvictFew {                // (as a kernel's argument)
+struct EvictFew {                // (as a kernel's argument: with an EvictArgs below the 4 KB that every launch may have)
   static constexpr int kEntries = 8, kBlocks = 640;
   EvictEntry entries[kEntries];
   int32_t dst_blocks[kBlocks];
 };
+static_assert(sizeof(EvictFew) <= 3072, "of 4 KB");
 struct EvictArgs {
   const EvictEntry* entries;     // NULL: entries and blocks are those of an EvictFew
   const int32_t* dst_blocks;
@@ -364,7 +365,7 @@ cudaError_t launch_weights_read(const float* w, const int32_t* d_tables, int tab
                                 int num_kv_heads, float* out, cudaStream_t st);
 // max_len: rows of the longest stretch; max_rows: rows the entry that moves most may move.
 cudaError_t launch_evict(const EvictArgs& a, const EvictFew& few, int n, int num_layers, int max_len,
-                         int max_rows, cudaStream_t st);
+                         int max_rows, int num_sms, cudaStream_t st);
 
 // ---- planner (planner.cpp) ----
 // A run of consecutive table positions whose blocks are held by the same set of threads

@@ -48,6 +48,9 @@ constexpr int kBuf = 128;                     // keys a warp holds where more do
 constexpr int kMaxSelect = 64, kMaxBeams = 64;
 constexpr int kMaxPieces = 16;                // of a row
 constexpr int kMaxLists = 128;                // pieces of a sequence's rows
+// SMs that rows are cut for.  A constant, as the scratch depends on it and its size may be asked for where there is no
+// device; on a part of a B200 the pieces are as right, if more than they need be.
+constexpr int kSms = 148;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr unsigned kAll = 0xffffffffu;
 typedef unsigned long long u64;
@@ -471,7 +474,7 @@ __global__ void __launch_bounds__(kThreads, Packs<T>::kCtas) beam_scan_kernel(co
 // where there are more rows than CTAs of the other kernel run at a time (64000 rows of 1000, 32 pairs, f32: 195
 // us and 542, 64 pairs, bf16: 259 and 855; 16000 of 1500: 45 and 121; 800 of 2048: 6.8 and 8.9; but 256 of
 // 2000: 8.4 and 6.3, one: 8.9 and 6.5).  Bound by instruction issue.
-constexpr int kShort = 2048, kShortRows = 4 * 148;
+constexpr int kShort = 2048, kShortRows = 4 * kSms;
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 2) beam_rows_kernel(const BeamArgs a) {
   using W = Packs<T>;
@@ -798,8 +801,8 @@ int pieces_of(const apar_beam_config* c, int32_t n_seq) {
   const int64_t rows = (int64_t)n_seq * c->num_beams;
   const bool f32 = c->logits_type == APAR_LOGITS_F32;
   const int64_t held = f32 ? 8192 : 16384;
-  const int64_t round = 148 * (f32 ? Packs<float>::kCtas : Packs<__half>::kCtas);
-  const int64_t few = std::min<int64_t>((2 * 148 + rows - 1) / rows, (c->vocab + 2047) / 2048);
+  const int64_t round = kSms * (f32 ? Packs<float>::kCtas : Packs<__half>::kCtas);
+  const int64_t few = std::min<int64_t>((2 * kSms + rows - 1) / rows, (c->vocab + 2047) / 2048);
   const int64_t fit = std::min<int64_t>((2 * round + rows - 1) / rows, (c->vocab + held - 1) / held);
   return (int)std::min<int64_t>({std::max(few, fit), kMaxPieces, kMaxLists / c->num_beams});
 }

@@ -656,18 +656,18 @@ cudaError_t launch_weights_read(const float* w, const int32_t* d_tables, int tab
 }
 
 cudaError_t launch_evict(const EvictArgs& a, const EvictFew& few, int n, int num_layers, int max_len,
-                         int max_rows, cudaStream_t st) {
+                         int max_rows, int num_sms, cudaStream_t st) {
   if (n <= 0) return cudaSuccess;
   const int lh = num_layers * a.num_kv_heads;
   cudaError_t e;
   const int64_t stretches = (int64_t)n * lh;
-  if (max_len <= kPickFew * (stretches > 148 ? kPickFewKeys : 2)) {
+  if (max_len <= kPickFew * (stretches > num_sms ? kPickFewKeys : 2)) {
     e = launch_kernel(evict_pick_kernel<kPickFew, kPickFewKeys>, dim3(n, lh), dim3(kPickFew), 0, st, false, a,
                       few, 1);
   } else if (max_len <= kPickCluster * kPickRows) {
     int n_cta = 1;                               // of a stretch
     while (n_cta < kPickCluster &&
-           (max_len > n_cta * kPickRows || (max_len > n_cta * 8192 && 2 * n_cta * stretches <= 148)))
+           (max_len > n_cta * kPickRows || (max_len > n_cta * 8192 && 2 * n_cta * stretches <= num_sms)))
       n_cta *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(n * n_cta, lh);
