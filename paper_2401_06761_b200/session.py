@@ -311,7 +311,8 @@ class PagedSession:
         """The same for runs of queries, as prefill_attention takes them."""
         assert q.is_cuda and q.is_contiguous() and q.dtype == torch.bfloat16
         assert lse.is_cuda and lse.is_contiguous() and lse.dtype == torch.float32
-        assert lse.shape == q.shape[:2] and q.shape[0] == sum(q_count)
+        q_count, total = self._counts(q_count)
+        assert lse.shape == q.shape[:2] and q.shape[0] == total
         B.apar_add_weights_prefill(self.ctx, layer, tids, q_begin, q_count, q.data_ptr(),
                                    lse.data_ptr(), self.sm_scale if sm_scale is None else sm_scale,
                                    replace, self._stream())

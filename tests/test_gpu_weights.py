@@ -901,3 +901,19 @@ def test_no_replay_over_other_queries_weights():
     # threads, one call of all (a weight is off by less than 1e-4 of itself, see Forest.add)
     total = f.s.weights[0].nan_to_num(0).double().sum((0, 2)).cpu().numpy()
     assert np.abs(total - 4 * (5 * 2 + len(tids))).max() <= 4 * (10 + len(tids)) * 1e-4
+
+
+def test_lists_may_be_made_beforehand():
+    """Lists that int32_array made, and arrays, as the prompt's attention takes them."""
+    f, tids = small_forest(8, 2)
+    n = [len(f.names[t]) for t in tids[:2]]
+    q, lse = rows(sum(n), 8, 5), torch.empty(sum(n), 8, device="cuda")
+    lists = [tids[:2], [0, 0], n]
+    f.s.prefill_attention(*lists, q, lse=lse)
+    f.s.add_weights_prefill(*lists, q, lse, replace=True)
+    want = f.s.read_weights(*lists)
+    for made in (B.int32_array, np.array):
+        args = [made(x) for x in lists]
+        f.s.prefill_attention(*args, q, lse=lse)
+        f.s.add_weights_prefill(*args, q, lse, replace=True)
+        assert torch.equal(f.s.read_weights(*args), want)
