@@ -144,6 +144,7 @@ class PagedSession:
         cfg.workspace, cfg.workspace_bytes = self.workspace.data_ptr(), ws_bytes
         self.cfg = cfg
         self.ctx = None
+        self._close_left()
         self.ctx = (B.apar_create(cfg) if kv_format == "bf16" else
                     B.apar_create_kv(cfg, B.KV_FORMATS[kv_format]))
         self.sm_scale = 1.0 / math.sqrt(shape.head_dim)
@@ -163,11 +164,22 @@ class PagedSession:
         nb, nt, mb = pool_requirements(spec)
         return cls(spec.shape, nb + extra_blocks, nt, mb, device, poison, kv_format=kv_format)
 
+    # what sessions held that went while a graph was being captured, when nothing may wait for the device
+    _left = []
+
     def close(self):
-        if self.ctx is not None:
+        if self.ctx is None:
+            return
+        self._left.append(dict(vars(self)))
+        self.ctx = None
+        self._close_left()
+
+    @classmethod
+    def _close_left(cls):
+        if cls._left and not torch.cuda.is_current_stream_capturing():
             torch.cuda.synchronize()
-            B.apar_destroy(self.ctx)
-            self.ctx = None
+            while cls._left:
+                B.apar_destroy(cls._left.pop()["ctx"])
 
     def __del__(self):
         try:

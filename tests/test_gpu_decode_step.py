@@ -277,3 +277,27 @@ def test_no_replay_after_attention_of_other_queries():
         sess.attention(tids, q)
         B.apar_note_step_replay(sess.ctx)
     sess.close()
+
+
+def test_a_session_that_goes_during_a_capture():
+    """Its context is kept until nothing is being captured: waiting for the device would end the capture."""
+    from paper_2401_06761_b200.session import PagedSession
+    shape = synth.LayerShape(8, 2)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    gone, closed, kept = (PagedSession(shape, 64, 8, 16, poison=True) for _ in range(3))
+    (t,) = kept.new_threads(1)
+    kept.append([t], [17], _rand((17, 2, 128), g), _rand((17, 2, 128), g))
+    q = _rand((1, 8, 128), g)
+    want = kept.attention([t], q)
+    out = torch.empty_like(q)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        del gone
+        closed.close()
+        kept.attention([t], q, out=out)
+        assert len(PagedSession._left) == 2
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+    kept.close()
+    assert not PagedSession._left
