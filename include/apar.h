@@ -347,9 +347,10 @@ apar_status apar_steps_before_new_block(apar_ctx* ctx, int32_t* steps_out /*[hos
  * longer, exactly what the replayed kernels do on the device.  Launches nothing.
  * Errors: INVALID_ARG if the step list or the plan is no longer the captured one (any
  * bookkeeping call since, attention of other queries), if apar_add_weights has been captured on this
- * context and none that was not has followed the attention call that made the plan, or if a thread of the list would start a new block - make an
- * ordinary apar_decode_step then, and capture again afterwards if block ids matter to the
- * graph (they do not: the captured kernels read tables and lengths from the device). */
+ * context and none that was not has followed the attention call that made the plan, or if a thread
+ * of the list would start a new block - make an ordinary apar_decode_step (and apar_add_weights) then,
+ * and capture again afterwards if block ids matter to the graph (they do not: the captured kernels
+ * read tables and lengths from the device). */
 apar_status apar_note_step_replay(apar_ctx* ctx);
 
 /* ReleaseCache (Algorithm 1; Section 2.3: a finished sequence gives back the cache that no
@@ -467,7 +468,8 @@ apar_status apar_rope(const apar_rope_config* cfg /*[host]*/, int32_t n,
                       int64_t k_stride, void* k_out /*[device]*/, int64_t k_out_stride,
                       void* cuda_stream);
 
-/* (The calls from here to apar_evict return INVALID_ARG, too, where the host's memory runs out.) */
+/* (The calls from here to apar_evict return INVALID_ARG, too, where the host's memory runs out, and change
+ * nothing then.) */
 
 /* Threads go on from other threads' chains (the paper has no counterpart: beam search reorders its
  * beams after every selection).  After the call thread tid[i] holds the chain that source_tid[i]
@@ -493,8 +495,8 @@ apar_status apar_reorder(apar_ctx* ctx, int32_t n, const int32_t* tid /*[host]*/
  *   library's own.  The caller owns the memory and may read and write the weights on the context's
  *   stream; those of rows that are cached when it is attached are what the memory holds. */
 size_t apar_weights_bytes(const apar_config* cfg /*[host]*/);
-/* memory [device] 256-byte aligned, or NULL to detach.  Graphs with calls below that were captured before may not be
- * replayed after it.
+/* memory [device] 256-byte aligned, or NULL to detach.  Graphs that were captured with other memory
+ * attached may not be replayed any more.
  * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE_TOO_SMALL. */
 apar_status apar_attach_weights(apar_ctx* ctx, void* memory /*[device] or NULL*/, size_t bytes);
 /* From now on every attention call of this context also writes lse [device] float

@@ -745,8 +745,9 @@ apar_status upload(apar_ctx* c, const void* src, size_t bytes, char* dst, cudaSt
 }
 
 // Keys of a class's units: the least for which there is a unit for every warp of the machine, but not more,
-// or where 1024 keys to a unit leave more than that, for every warp as many.  (64 x 3 forks of 2400 keys, 32
-// heads on 8, units for 10, 12, 20 and 40 warps of an SM, which has 12: 68, 93, 72 and 78 us.)
+// or where 1024 keys to a unit leave more than that, for every warp as many.  (Units for so many warps of an SM, of
+// which the wider classes have 12, by 10, 12, 20 and 40, 32 heads on 8: 64 prompts of 2048 keys with 4 forks each 83,
+// 78, 80 and 82 us, of 2400 with 3 79, 77, 86 and 82, of 1024 with 16 97, 83, 95 and 106.)
 int key_chunk(const apar_ctx* c, const std::vector<KeyRun>& runs, int cls) {
   constexpr int kMost = 1024;
   int64_t keys = 0, n = 0;

@@ -23,9 +23,9 @@
 //     compared in 64 bits: their difference goes through two log-sum-exps, and 32 bits would round it.
 //
 // Bound: HBM, 4 bytes per f32 logit, and one special-function operation for each.  2048 rows of 32003 f32
-// logits, a fifth of them finished (208 MB read): scan 50 us, 4.2 TB/s; 10 of them are the end of a piece
+// logits, a fifth of them finished (208 MB read): scan 48.5 us, 4.3 TB/s; 10 of them are the end of a piece
 // (threshold, collecting, ordering), a chain of short steps that the SM's other CTAs cover in part.  128 rows
-// of 131072 bf16 logits: 13.5 us, 2.5 TB/s.  4 rows of 32000: 4 us, then 5 for the pick; that of 64 pairs for
+// of 131072 bf16 logits: 13.8 us, 2.4 TB/s.  4 rows of 32000: 4 us, then 5 for the pick; that of 64 pairs for
 // 16 sequences of 64 beams takes 35.  (Tried: the next step's copies into shared memory meanwhile, and whole
 // pieces in registers until the end: 73 and 55 us.)
 #include <algorithm>
@@ -796,7 +796,11 @@ __global__ void __launch_bounds__(kThreads) beam_pick_kernel(const BeamArgs a) {
 // Pieces of a row.  Few rows are cut to fill the machine twice over, no piece shorter than 2048 elements;
 // more rows into pieces of no less than 8192 (f32) or 16384, as long as that gives no more than two rounds of
 // CTAs: the end of a piece costs as much as some thousand elements (256 x 8 rows of 32003, f32, in 1, 2 and 4
-// pieces: 50, 57 and 67 us).
+// pieces: 50, 57 and 67 us).  Scan and pick, with pieces of half that size, of that and of twice as much: bf16, rows of
+// 131072, 64 of them 18.4, 14.8 and 16.3 us, 128 26.5, 20.9 and 19.1, 256 34.0, 34.2 and 29.8; 600 rows of 32000 27.0,
+// 22.3 and 20.0; f32, 128 rows of 131072 33.6, 33.1 and 27.6, 128 of 50000 22.5, 18.2 and 16.1.  With one round of
+// CTAs, two and three: bf16, 128 rows of 131072 23.3, 20.9 and 20.7 us, 1200 of 32000 31.9, 35.8 and 35.9, 2048 of 32003
+// 58.2, 58.0 and 63.4; f32, 128 of 131072 32.2, 33.1 and 36.5, 600 of 32000 32.3, 31.0 and 35.7.
 int pieces_of(const apar_beam_config* c, int32_t n_seq) {
   const int64_t rows = (int64_t)n_seq * c->num_beams;
   const bool f32 = c->logits_type == APAR_LOGITS_F32;
