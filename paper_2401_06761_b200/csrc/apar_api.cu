@@ -610,18 +610,24 @@ apar_status run_attention(apar_ctx* c, int n, const int32_t* qslots, const int32
     }
     plan_host_us = std::chrono::duration_cast<std::chrono::microseconds>(
                        std::chrono::steady_clock::now() - t_plan).count();
+  }
+  const int64_t uploaded = c->last.attn_upload_bytes;
+  if (!tables_in_sync) c->last.attn_upload_bytes = 0;   // (else the caller's uploads count too)
+  apar_status rc = tables_in_sync ? APAR_OK : sync_device_tables(c, qslots, n, st);
+  if (rc) {
+    c->last.attn_upload_bytes = uploaded;
+    return rc;
+  }
+  c->attn_book_seq = 0;
+  c->last.attn_kernels = 0;
+  c->last.attn_plan_host_us = plan_host_us;
+  if (!reuse) {
     std::swap(c->plan, c->next_plan);
     c->plan_epoch = 0;                    // (of the plan before)
     c->plan_verify_n = 0;
     c->plan_min_rows = min_rows;
     c->q4_items = q4_items;
   }
-  c->attn_book_seq = 0;
-  c->last.attn_kernels = 0;
-  c->last.attn_plan_host_us = plan_host_us;
-  if (!tables_in_sync) c->last.attn_upload_bytes = 0;   // (else the caller's uploads count too)
-  apar_status rc = tables_in_sync ? APAR_OK : sync_device_tables(c, qslots, n, st);
-  if (rc) return rc;
 
   const Plan& p = c->plan;
   if (!reuse) {

@@ -917,3 +917,23 @@ def test_lists_may_be_made_beforehand():
         f.s.prefill_attention(*args, q, lse=lse)
         f.s.add_weights_prefill(*args, q, lse, replace=True)
         assert torch.equal(f.s.read_weights(*args), want)
+
+
+def test_a_table_row_larger_than_the_staging_area():
+    """A thread whose new blocks' ids do not fit one upload is refused; the call before it stays."""
+    s = PagedSession(LayerShape(1, 1), 170020, 2, 170000, weights=True)
+    a, b = s.new_threads(2)
+    k = rows(1 << 16, 1, 1)
+    s.append([a], [100], k[:100], k[:100])
+    for _ in range(41):
+        s.append([b], [1 << 16], k, k)                   # 167936 blocks
+    q, lse = rows(1, 1, 2), torch.empty(1, 1, device="cuda")
+    plain = s.attention([a], q, lse=lse)
+    before = s.stats()
+    with pytest.raises(B.AparError) as e:
+        s.attention([b], q)
+    assert e.value.code == "WORKSPACE_TOO_SMALL" and s.stats() == before
+    s.add_weights(q, lse)
+    # (weights of one query and head sum up to one; every one is off by less than 1e-4 of itself)
+    assert abs(s.read_weights([a], [0], [100]).double().sum().item() - 1) <= 1e-4
+    assert torch.equal(s.attention([a], q), plain)
